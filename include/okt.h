@@ -513,6 +513,164 @@ typedef struct okt_chunk {
 int okt_balance_plan(const uint64_t* h_sizes, uint32_t P, okt_chunk* h_plan_out,
                      uint32_t plan_capacity, uint32_t* h_plan_len_out, int* h_triggered_out);
 
+/*
+ * Operators of a layer's training step.  Between its matrix products a layer whose
+ * gradient the calls above sparsify has dropout, norms around each block with the
+ * residual stream, and attention; the calls below are those, forward and backward.
+ * Tensors are fp32, bf16 or fp16 in memory (okt_dtype), arithmetic, statistics and sums
+ * are fp32, every output is rounded once, to nearest; parameters (weights, biases,
+ * gates) and their gradients are fp32, so that a gradient can be written straight into
+ * its place in the flat vector that okt_accumulate_select takes (that place must be
+ * 4-byte aligned, parameters 16-byte).  Parameter gradients are overwritten, not added
+ * to.  Results do not change from run to run: no call uses atomics.
+ *
+ * Dropout.  A random field of 16-bit values is a function of a 64-bit seed and a 32-bit
+ * site: Philox4x32 with seven rounds (Salmon et al., SC'11), key = (seed low, seed high),
+ * counter = (c0, c1, c2, site); a block is eight values, value 2w + h being half h
+ * (0 = low) of output word w.  A place is kept where its value is below
+ * bar = floor((1 - p) 65536 + 0.5), and then multiplied by 65536 / bar, so p is
+ * rounded to a multiple of 2^-16 and expectations are kept exactly.  Places are numbered
+ *   okt_dropout, element e:        c0 = (e / 8) mod 2^32, c1 = (e / 8) >> 32, c2 = 0;  value e % 8
+ *   okt_residual_norm, (row, col): c0 = col / 8, c1 = row mod 2^32, c2 = row >> 32;    value col % 8
+ *   okt_attention, (b, h, i, j):   c0 = j / 4, c1 = i / 2, c2 = b heads + h;            value 2 (j % 4) + i % 2
+ * The mask is not stored: the backward pass draws it again and must see the same seed and
+ * site.  The seed is read from device memory, so a captured graph can be replayed with
+ * another one; give every call of a step its own site.
+ */
+typedef enum okt_dtype { OKT_F32 = 0, OKT_BF16 = 1, OKT_F16 = 2 } okt_dtype;
+
+/*
+ * Dropout: y[e] = x[e] * 65536 / bar where the field keeps e, else 0 (whatever x[e] is).
+ * The backward pass is the same call on the gradient of y.
+ *   d_x     in   [n] of `dtype`, 16-byte aligned, contiguous
+ *   d_y     out  [n]; may be d_x itself, must not overlap it otherwise
+ *   n       at most 2^43; 0 is a no-op
+ *   p       probability of dropping, 0 <= p <= 1
+ *   d_seed  in   uint64[1] on the device
+ */
+int okt_dropout(const void* d_x, void* d_y, uint64_t n, int dtype, double p, const uint64_t* d_seed,
+                uint32_t site, void* stream);
+
+typedef enum okt_norm_kind { OKT_NORM_LAYER = 0, OKT_NORM_RMS = 1 } okt_norm_kind;
+
+/*
+ * What stands between two blocks of a layer, on `rows` tokens of `width` channels:
+ *   a = Npost(u), or u without d_post_weight      norm after the block
+ *   h = residual_scale * x + gate * drop(a)       (gate 1 without d_gate, no dropout at p = 0)
+ *   y = Npre(h), none without d_pre_weight        norm before the next block
+ * where N(v) = (v - m) r weight + bias, m = mean(v) (OKT_NORM_RMS: 0), r = 1 / sqrt(mean
+ * (v - m)^2 + eps); Npre is taken of h as it was rounded for storing.  A norm after the sum
+ * alone, one before the block alone, both, with or without a gate for each channel or for
+ * each channel of each sequence, are all this call.
+ */
+typedef struct okt_residual_norm {
+    uint64_t rows;                /* at most 2^40 */
+    uint32_t width;               /* 1 to 16384 */
+    int32_t dtype;                /* of u, x, h, y and their gradients */
+    int32_t kind;                 /* okt_norm_kind of both norms */
+    float eps;                    /* >= 0 */
+    float residual_scale;
+    uint32_t site;
+    double dropout_p;
+    const uint64_t* d_seed;       /* uint64[1] on the device; may be NULL where nothing is dropped */
+    const float* d_post_weight;   /* fp32[width] on the device, 16-byte aligned; NULL: no norm */
+    const float* d_post_bias;     /* NULL: none */
+    const float* d_gate;          /* fp32[ceil(rows / rows_per_gate)][width]; NULL: 1 */
+    uint64_t rows_per_gate;       /* rows in a row that share a gate; 0: all */
+    const float* d_pre_weight;    /* as the post norm's */
+    const float* d_pre_bias;
+    /* elements from a row to the next, width to 2^20; 0 stands for width.  Rows need the
+     * alignment of an element only. */
+    uint64_t u_stride, x_stride, h_stride, y_stride, dh_stride, dy_stride, dx_stride, du_stride;
+} okt_residual_norm;
+
+/* Bytes of workspace okt_residual_norm_backward needs (the forward pass needs none);
+ * 0 if width or rows are out of range.  Pure host arithmetic. */
+size_t okt_residual_norm_workspace_bytes(uint64_t rows, uint32_t width, uint64_t rows_per_gate);
+
+/*
+ * Forward.  d_h_out may be NULL where d_y_out is wanted alone, and may be d_x or d_u;
+ * d_y_out is NULL without d_pre_weight, and may be d_u or d_x if d_h_out is neither.
+ *   d_stats_out  out  fp32[rows][4], 16-byte aligned: m and r of the post norm, m and r of
+ *                     the pre norm (0 where there is none); NULL if no backward pass follows
+ * rows = 0 is a no-op.  One launch.
+ */
+int okt_residual_norm_forward(const okt_residual_norm* op, const void* d_u, const void* d_x, void* d_h_out,
+                              void* d_y_out, float* d_stats_out, void* stream);
+
+/*
+ * Backward, from the gradients of h and y to those of x and u and of the parameters.
+ *   d_u      in   read where there is a post norm or a gate (else may be NULL)
+ *   d_h      in   as written by the forward pass; read where there is a pre norm
+ *   d_stats  in   as written by the forward pass
+ *   d_dh     in   gradient of h from its other uses; NULL for zero if there is a pre norm
+ *   d_dy     in   gradient of y; NULL exactly where there is no pre norm
+ *   d_dx_out, d_du_out  out  may be any of the inputs that are read (the first kernel
+ *                            reads a place before it writes it), not each other
+ *   d_d*_weight_out, d_d*_bias_out  out  fp32[width], d_dgate_out fp32[gates][width]; each may
+ *                            be NULL, and must be where there is no such parameter
+ * rows = 0 writes zeros to the parameter gradients (one gate).  Two launches.
+ */
+int okt_residual_norm_backward(const okt_residual_norm* op, const void* d_u, const void* d_h,
+                               const float* d_stats, const void* d_dh, const void* d_dy, void* d_dx_out,
+                               void* d_du_out, float* d_dpost_weight_out, float* d_dpost_bias_out,
+                               float* d_dgate_out, float* d_dpre_weight_out, float* d_dpre_bias_out,
+                               void* d_ws, size_t ws_bytes, void* stream);
+
+/*
+ * Attention over a batch of sequences, query heads sharing key heads in groups of
+ * heads / kv_heads (query head h reads key head h / (heads / kv_heads)):
+ *   s_ij = scale q_i . k_j      for visible (i, j):  i < Q, j < K, and if causal j <= i + K - Q
+ *   lse_i = log sum_j exp s_ij,  p_ij = exp(s_ij - lse_i),  pd_ij = drop(p_ij),  o_i = sum_j pd_ij v_j
+ * with Q = q_len and K = k_len, or sequence b's own lengths d_q_lens[b] and d_k_lens[b] (taken
+ * as 0 to q_len and 0 to k_len).  A row that sees nothing, or lies past its length, has o = 0 and
+ * lse = -inf and takes part in no gradient; keys and values past their length are not
+ * looked at, whatever they hold, and get the gradient 0.  Within the lengths, values
+ * have to be finite: a NaN in a hidden place can reach every row of its sequence.
+ * Backward, from dO, the probabilities taken again from q, k and lse:
+ *   dpd_ij = do_i . v_j,  D_i = do_i . o_i,  ds_ij = p_ij (drop(dpd_ij) - D_i)
+ *   dv_j = sum_i pd_ij do_i,  dq_i = scale sum_j ds_ij k_j,  dk_j = scale sum_i ds_ij q_i
+ * dv and dk summed over the query heads of a group.  Products are taken by the matrix
+ * units from 16-bit inputs with fp32 sums; p and ds are rounded to the tensors' type for the
+ * second product of each pass.
+ * A tensor is [batch][length][heads][head_dim] by strides {batch, length, heads} in elements,
+ * head_dim contiguous; strides are multiples of 8, bases 16-byte aligned, so the parts
+ * of a common projection are taken as they lie.
+ */
+typedef struct okt_attention {
+    uint32_t batch, heads, kv_heads;   /* heads a multiple of kv_heads; batch * heads <= 2^20 */
+    uint32_t q_len, k_len;             /* 0 to 2^24 */
+    uint32_t head_dim;                 /* 8, 16, ... 128 */
+    int32_t dtype;                     /* OKT_BF16 or OKT_F16 */
+    int32_t causal;
+    float scale;                       /* > 0, finite */
+    uint32_t site;
+    double dropout_p;
+    const uint64_t* d_seed;            /* uint64[1] on the device; may be NULL where nothing is dropped */
+    const int32_t* d_q_lens;           /* int32[batch] on the device, or NULL */
+    const int32_t* d_k_lens;
+    uint64_t q_stride[3], k_stride[3], v_stride[3], o_stride[3];
+    uint64_t do_stride[3], dq_stride[3], dk_stride[3], dv_stride[3];   /* backward only */
+} okt_attention;
+
+/* Bytes of workspace that suffice for both passes.  Pure host arithmetic. */
+size_t okt_attention_workspace_bytes(uint32_t batch, uint32_t heads, uint32_t kv_heads, uint32_t q_len,
+                                     uint32_t k_len, uint32_t head_dim);
+
+/*
+ *   d_lse_out  out  fp32[batch][heads][q_len], contiguous; NULL if no backward pass follows
+ */
+int okt_attention_forward(const okt_attention* op, const void* d_q, const void* d_k, const void* d_v,
+                          void* d_o_out, float* d_lse_out, void* d_ws, size_t ws_bytes, void* stream);
+
+/*
+ * d_o and d_lse as the forward pass wrote them.  d_dq_out, d_dk_out and d_dv_out are written as
+ * a whole (past the lengths with zeros); they may lie in one buffer, but overlap no input.
+ */
+int okt_attention_backward(const okt_attention* op, const void* d_q, const void* d_k, const void* d_v,
+                           const void* d_o, const float* d_lse, const void* d_do, void* d_dq_out,
+                           void* d_dk_out, void* d_dv_out, void* d_ws, size_t ws_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

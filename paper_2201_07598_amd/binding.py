@@ -9,12 +9,14 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB = None
 
-c_u32, c_u64, c_sz, c_vp, c_f32, c_int = (ctypes.c_uint32, ctypes.c_uint64, ctypes.c_size_t,
-                                          ctypes.c_void_p, ctypes.c_float, ctypes.c_int)
+c_u32, c_u64, c_sz, c_vp, c_f32, c_f64, c_int = (ctypes.c_uint32, ctypes.c_uint64, ctypes.c_size_t,
+                                                 ctypes.c_void_p, ctypes.c_float, ctypes.c_double,
+                                                 ctypes.c_int)
 
 # name -> (restype, argtypes); mirrors include/okt.h
 SIGNATURES = {
@@ -56,6 +58,13 @@ SIGNATURES = {
     "okt_balance_plan": (c_int, [c_vp, c_u32, c_vp, c_u32, c_vp, c_vp]),
     "okt_sparse_reduce_batch": (c_int, [c_vp, c_vp, c_vp, c_vp, c_u32, c_u32, c_u32, c_vp, c_vp,
                                         c_u64, c_vp, c_vp, c_vp, c_sz, c_vp]),
+    "okt_dropout": (c_int, [c_vp, c_vp, c_u64, c_int, c_f64, c_vp, c_u32, c_vp]),
+    "okt_residual_norm_workspace_bytes": (c_sz, [c_u64, c_u32, c_u64]),
+    "okt_residual_norm_forward": (c_int, [c_vp, c_vp, c_vp, c_vp, c_vp, c_vp, c_vp]),
+    "okt_residual_norm_backward": (c_int, [c_vp] * 14 + [c_sz, c_vp]),
+    "okt_attention_workspace_bytes": (c_sz, [c_u32] * 6),
+    "okt_attention_forward": (c_int, [c_vp] * 7 + [c_sz, c_vp]),
+    "okt_attention_backward": (c_int, [c_vp] * 11 + [c_sz, c_vp]),
 }
 
 
@@ -487,3 +496,239 @@ def okt_balance_plan(sizes):
         ctypes.cast(ctypes.pointer(triggered), c_vp)))
     return bool(triggered.value), [(c.src, c.dst, c.src_offset, c.dst_offset, c.count)
                                    for c in plan[:n.value]]
+
+
+# --------------------------------------------------------------------------
+# Operators of a layer's training step.  Their arguments travel in structs of the header,
+# which are packed here as bytes: members lie in the order of the declaration and every one is
+# aligned by what stands before it.
+_NORM = struct.Struct("=QIiiffId7Q8Q")          # okt_residual_norm
+_ATTENTION = struct.Struct("=6I2ifId3Q24Q")     # okt_attention
+_NORM_KINDS = {"layer": 0, "rms": 1}
+_DTYPES = {}
+
+
+def _dtype_code(t, name):
+    if not _DTYPES:
+        torch = _torch()
+        _DTYPES.update({torch.float32: 0, torch.bfloat16: 1, torch.float16: 2})
+    code = _DTYPES.get(t.dtype)
+    if code is None:
+        raise TypeError(f"{name} must be float32, bfloat16 or float16, got {t.dtype}")
+    return code
+
+
+def _seed(seed, p):
+    if p == 0.0 and seed is None:
+        return 0
+    if seed is None:
+        raise TypeError("seed is required where something is dropped")
+    if seed.numel() < 1:
+        raise ValueError("seed needs one element")
+    return _ptr(seed, _torch().int64, "seed")
+
+
+def okt_dropout(x, y, p: float, seed, site: int = 0, stream=None) -> None:
+    """y = dropout(x); with the gradient of y in place of x, that of x.  seed: int64[1] on
+    the device (the bytes of the uint64); y may be x."""
+    _torch()
+    code = _dtype_code(x, "x")
+    if x.numel() != y.numel():
+        raise ValueError("x and y must have the same length")
+    if seed is None:
+        raise TypeError("seed is required")
+    _check("okt_dropout", load_library().okt_dropout(
+        _ptr(x, x.dtype, "x"), _ptr(y, x.dtype, "y"), x.numel(), code, float(p), _seed(seed, p), int(site),
+        _stream(stream)))
+
+
+def _rows(t, like, name, allow_none=False):
+    """(pointer, row stride) of a [rows, width] tensor like `like`, rows any distance apart."""
+    if t is None:
+        if allow_none:
+            return None, 0
+        raise TypeError(f"{name} is required")
+    if not t.is_cuda:
+        raise TypeError(f"{name} must be a CUDA tensor (device memory)")
+    if t.dtype is not like.dtype:
+        raise TypeError(f"{name} must have dtype {like.dtype}, got {t.dtype}")
+    if t.shape != like.shape:
+        raise ValueError(f"{name} must have the shape {tuple(like.shape)}, got {tuple(t.shape)}")
+    rows, width = t.shape
+    step, unit = t.stride()
+    if unit != 1 and width > 1:
+        raise ValueError(f"{name} must have contiguous rows")
+    if rows > 1 and step < width:
+        raise ValueError(f"rows of {name} must not overlap")
+    return t.data_ptr(), step if rows > 1 else 0
+
+
+def _parameter(t, numel, name):
+    if t is None:
+        return None
+    if t.numel() != numel:
+        raise ValueError(f"{name} needs {numel} elements, got {t.numel()}")
+    return _ptr(t, _TORCH.float32, name)
+
+
+def _norm_struct(like, kind, eps, residual_scale, post_weight, post_bias, gate, rows_per_gate, pre_weight,
+                 pre_bias, dropout_p, seed, site, strides):
+    rows, width = like.shape
+    share = int(rows_per_gate)
+    gates = max(1, -(-rows // share)) if share else 1
+    return gates, _NORM.pack(
+        rows, width, _dtype_code(like, "u"), _NORM_KINDS[kind], eps, residual_scale, site, dropout_p,
+        _seed(seed, dropout_p), _parameter(post_weight, width, "post_weight") or 0,
+        _parameter(post_bias, width, "post_bias") or 0, _parameter(gate, gates * width, "gate") or 0, share,
+        _parameter(pre_weight, width, "pre_weight") or 0, _parameter(pre_bias, width, "pre_bias") or 0,
+        *strides)
+
+
+def okt_residual_norm_workspace_bytes(rows: int, width: int, rows_per_gate: int = 0) -> int:
+    return load_library().okt_residual_norm_workspace_bytes(int(rows), int(width), int(rows_per_gate))
+
+
+def okt_residual_norm_forward(u, x, h_out, y_out, stats_out, *, kind: str = "layer", eps: float = 1e-5,
+                              residual_scale: float = 1.0, post_weight=None, post_bias=None, gate=None,
+                              rows_per_gate: int = 0, pre_weight=None, pre_bias=None,
+                              dropout_p: float = 0.0, seed=None, site: int = 0, stream=None) -> None:
+    """h = residual_scale x + gate * dropout(norm(u)), y = norm(h) on [rows, width] tensors;
+    a norm is there where its weight is.  kind: "layer" or "rms".  h_out may be None, stats_out
+    (float32 [rows, 4]) too where no backward pass follows."""
+    torch = _torch()
+    if u.dim() != 2:
+        raise ValueError("u must be [rows, width]")
+    pu, su = _rows(u, u, "u")
+    px, sx = _rows(x, u, "x")
+    ph, sh = _rows(h_out, u, "h_out", allow_none=True)
+    py, sy = _rows(y_out, u, "y_out", allow_none=True)
+    if stats_out is not None and stats_out.numel() < 4 * u.shape[0]:
+        raise ValueError("stats_out needs four elements a row")
+    _, op = _norm_struct(u, kind, eps, residual_scale, post_weight, post_bias, gate, rows_per_gate,
+                         pre_weight, pre_bias, dropout_p, seed, site, (su, sx, sh, sy, 0, 0, 0, 0))
+    _check("okt_residual_norm_forward", load_library().okt_residual_norm_forward(
+        op, pu, px, ph, py, _ptr(stats_out, torch.float32, "stats_out", allow_none=True), _stream(stream)))
+
+
+def okt_residual_norm_backward(u, h, stats, dh, dy, dx_out, du_out, ws, *, dpost_weight=None,
+                               dpost_bias=None, dgate=None, dpre_weight=None, dpre_bias=None,
+                               kind: str = "layer", eps: float = 1e-5, residual_scale: float = 1.0,
+                               post_weight=None, post_bias=None, gate=None, rows_per_gate: int = 0,
+                               pre_weight=None, pre_bias=None, dropout_p: float = 0.0, seed=None,
+                               site: int = 0, stream=None) -> None:
+    """Gradients of x, u and the parameters from those of h (dh, None for zero) and y (dy, None
+    without a pre norm).  The parameters' gradients are float32 and are overwritten; None
+    leaves one out."""
+    torch = _torch()
+    if du_out is None or du_out.dim() != 2:
+        raise ValueError("du_out must be [rows, width]")
+    like = du_out
+    pu, su = _rows(u, like, "u", allow_none=True)
+    ph, sh = _rows(h, like, "h", allow_none=True)
+    pdh, sdh = _rows(dh, like, "dh", allow_none=True)
+    pdy, sdy = _rows(dy, like, "dy", allow_none=True)
+    pdx, sdx = _rows(dx_out, like, "dx_out")
+    pdu, sdu = _rows(du_out, like, "du_out")
+    if stats.numel() < 4 * like.shape[0]:
+        raise ValueError("stats needs four elements a row")
+    gates, op = _norm_struct(like, kind, eps, residual_scale, post_weight, post_bias, gate, rows_per_gate,
+                             pre_weight, pre_bias, dropout_p, seed, site, (su, 0, sh, 0, sdh, sdy, sdx, sdu))
+    width = like.shape[1]
+    _check("okt_residual_norm_backward", load_library().okt_residual_norm_backward(
+        op, pu, ph, _ptr(stats, torch.float32, "stats"), pdh, pdy, pdx, pdu,
+        _parameter(dpost_weight, width, "dpost_weight"), _parameter(dpost_bias, width, "dpost_bias"),
+        _parameter(dgate, gates * width, "dgate"), _parameter(dpre_weight, width, "dpre_weight"),
+        _parameter(dpre_bias, width, "dpre_bias"), _ptr(ws, torch.uint8, "ws"), ws.numel(),
+        _stream(stream)))
+
+
+def okt_attention_workspace_bytes(batch: int, heads: int, kv_heads: int, q_len: int, k_len: int,
+                                  head_dim: int) -> int:
+    return load_library().okt_attention_workspace_bytes(int(batch), int(heads), int(kv_heads), int(q_len),
+                                                        int(k_len), int(head_dim))
+
+
+def _heads(t, dtype, shape, name):
+    """(pointer, batch stride, length stride, head stride) of a [batch, length, heads, dim]
+    tensor; a stride that is never taken reads as 0."""
+    if not t.is_cuda:
+        raise TypeError(f"{name} must be a CUDA tensor (device memory)")
+    if t.dtype is not dtype:
+        raise TypeError(f"{name} must have dtype {dtype}, got {t.dtype}")
+    if t.shape != shape:
+        raise ValueError(f"{name} must have the shape {tuple(shape)}, got {tuple(t.shape)}")
+    b, n, h, unit = t.stride()
+    if unit != 1:
+        raise ValueError(f"{name} must have contiguous head vectors")
+    return t.data_ptr(), (b if shape[0] > 1 else 0, n if shape[1] > 1 else 0, h if shape[2] > 1 else 0)
+
+
+def _lengths(t, batch, name):
+    if t is None:
+        return 0
+    if t.numel() != batch:
+        raise ValueError(f"{name} needs one element a sequence")
+    return _ptr(t, _TORCH.int32, name)
+
+
+_NO_STRIDES = (0,) * 12
+
+
+def _attention_struct(q, k, causal, scale, dropout_p, seed, site, q_lens, k_lens, strides):
+    batch, q_len, heads, dim = q.shape
+    return _ATTENTION.pack(
+        batch, heads, k.shape[2], q_len, k.shape[1], dim, _dtype_code(q, "q"), 1 if causal else 0,
+        dim ** -0.5 if scale is None else scale, site, dropout_p, _seed(seed, dropout_p),
+        _lengths(q_lens, batch, "q_lens"), _lengths(k_lens, batch, "k_lens"), *strides)
+
+
+def _attention_inputs(q, k, v):
+    if q.dim() != 4 or k.dim() != 4:
+        raise ValueError("q, k and v must be [batch, length, heads, head_dim]")
+    shape, keys = q.shape, k.shape
+    if keys[0] != shape[0] or keys[3] != shape[3]:
+        raise ValueError("q and k must agree in batch and head_dim")
+    pq, sq = _heads(q, q.dtype, shape, "q")
+    pk, sk = _heads(k, q.dtype, keys, "k")
+    pv, sv = _heads(v, q.dtype, keys, "v")
+    return shape, keys, pq, pk, pv, sq + sk + sv
+
+
+def okt_attention_forward(q, k, v, o_out, lse_out, ws=None, *, causal: bool = False, scale=None,
+                          q_lens=None, k_lens=None, dropout_p: float = 0.0, seed=None, site: int = 0,
+                          stream=None) -> None:
+    """o = dropout(softmax(scale q k' over the visible keys)) v on [batch, length, heads, head_dim]
+    tensors of any strides; scale defaults to head_dim ** -0.5.  q_lens, k_lens: int32 [batch] on the
+    device, the sequences' own lengths.  lse_out (float32 [batch, heads, q_len]) may be None where
+    no backward pass follows."""
+    torch = _torch()
+    shape, _, pq, pk, pv, strides = _attention_inputs(q, k, v)
+    po, so = _heads(o_out, q.dtype, shape, "o_out")
+    if lse_out is not None and lse_out.numel() != shape[0] * shape[1] * shape[2]:
+        raise ValueError("lse_out must be [batch, heads, q_len]")
+    op = _attention_struct(q, k, causal, scale, dropout_p, seed, site, q_lens, k_lens,
+                           strides + so + _NO_STRIDES)
+    _check("okt_attention_forward", load_library().okt_attention_forward(
+        op, pq, pk, pv, po, _ptr(lse_out, torch.float32, "lse_out", allow_none=True),
+        _ptr(ws, torch.uint8, "ws", allow_none=True), 0 if ws is None else ws.numel(), _stream(stream)))
+
+
+def okt_attention_backward(q, k, v, o, lse, do, dq_out, dk_out, dv_out, ws, *, causal: bool = False,
+                           scale=None, q_lens=None, k_lens=None, dropout_p: float = 0.0, seed=None,
+                           site: int = 0, stream=None) -> None:
+    """Gradients of q, k and v from that of o, with o and lse of the forward pass and the same
+    options (seed and site above all)."""
+    torch = _torch()
+    shape, keys, pq, pk, pv, strides = _attention_inputs(q, k, v)
+    po, so = _heads(o, q.dtype, shape, "o")
+    pdo, sdo = _heads(do, q.dtype, shape, "do")
+    pdq, sdq = _heads(dq_out, q.dtype, shape, "dq_out")
+    pdk, sdk = _heads(dk_out, q.dtype, keys, "dk_out")
+    pdv, sdv = _heads(dv_out, q.dtype, keys, "dv_out")
+    if lse.numel() != shape[0] * shape[1] * shape[2]:
+        raise ValueError("lse must be [batch, heads, q_len]")
+    op = _attention_struct(q, k, causal, scale, dropout_p, seed, site, q_lens, k_lens,
+                           strides + so + sdo + sdq + sdk + sdv)
+    _check("okt_attention_backward", load_library().okt_attention_backward(
+        op, pq, pk, pv, po, _ptr(lse, torch.float32, "lse"), pdo, pdq, pdk, pdv,
+        _ptr(ws, torch.uint8, "ws"), ws.numel(), _stream(stream)))

@@ -1,0 +1,231 @@
+// What the attention kernels share: the matrix unit's tiles, the tiles of rows in LDS, the
+// dropout mask's shares, and the host's checks.
+//
+// Products are 32 x 32 x 16 steps of the matrix unit, C += A B with 16-bit inputs:
+//   A  lane l holds row l % 32, columns 8 (l / 32) .. + 7
+//   B  lane l holds column l % 32, rows 8 (l / 32) .. + 7
+//   C  lane l holds column l % 32, element r is row 8 (r / 4) + 4 (l / 32) + r % 4
+// Rows of A are kept in LDS in the order that makes element r of C the row 16 (l / 32) + r
+// of the tile (row_of_slot): then elements 8t .. 8t + 7 of C are, as they lie, the B operand of
+// step t of a product that sums over those rows.  Scores therefore go from the
+// first product through the softmax into the second one without leaving their registers.
+#ifndef OKT_ATTENTION_H
+#define OKT_ATTENTION_H
+
+#include "okt_element.h"
+#include "okt_random.h"
+
+namespace okt {
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef short i16x4 __attribute__((ext_vector_type(4)));
+typedef short i16x8 __attribute__((ext_vector_type(8)));
+
+template <typename T> using frag = typename Eight<T>::vec;
+
+__device__ __forceinline__ f32x16 mfma(frag<__bf16> a, frag<__bf16> b, f32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x16 mfma(frag<_Float16> a, frag<_Float16> b, f32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
+}
+
+// Eight neighbouring elements of a C tile as a B operand.
+template <typename T>
+__device__ __forceinline__ frag<T> to_operand(const f32x16& c, int t) {
+    f32x8 v;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = c[8 * t + i];
+    return __builtin_convertvector(v, frag<T>);
+}
+
+// The row of a 32-row tile that slot s of the A operand holds.
+__device__ __forceinline__ constexpr uint32_t row_of_slot(uint32_t s) {
+    return (s & ~31u) | ((s & 4) << 2) | ((s >> 1) & 12) | (s & 3);
+}
+
+// ------------------------------------------------------------------ tiles of rows in LDS
+
+// ROWS rows of DIM elements, row order by slots, DIM / 8 chunks of 16 bytes a row.  Chunk c of slot s lies
+// at place c ^ turn(s): sixteen neighbouring slots then read one chunk from sixteen
+// different groups of banks (A operands, row by row), and the eight slots that a
+// transposing read touches lie in all four quarters of the banks.
+template <typename T, int DIM, int ROWS, int THREADS>
+struct RowTile {
+    static constexpr int CHUNKS = DIM / 8;
+    static constexpr int BYTES = ROWS * DIM * 2;
+    static constexpr int LOADS = ROWS * CHUNKS / THREADS;       // 16-byte loads of a thread
+
+    static __device__ __forceinline__ uint32_t turn(uint32_t s) {
+        return DIM == 64 ? ((s >> 1 & 1) << 2) | (s >> 2 & 3) : ((s & 3) << 2) | (s >> 2 & 3);
+    }
+
+    // Fetches rows first .. first + ROWS - 1 of a tensor straight into LDS; rows outside
+    // [lo, hi] are replaced by the nearest inside, so that what lies there is never looked
+    // at and what is multiplied by a masked 0 is finite.  Chunks past head_dim are not
+    // written (they hold the zeros that clear() left).
+    static __device__ __forceinline__ void fetch(char* tile, const T* base, uint64_t stride, int64_t first, int64_t lo,
+                                                 int64_t hi, uint32_t head_dim) {
+        const uint32_t wave = uniform(threadIdx.x / WAVE), lane = threadIdx.x % WAVE;
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+            const uint32_t at = (i * (THREADS / WAVE) + wave) * WAVE;           // of the wave's first chunk
+            const uint32_t slot = (at + lane) / CHUNKS, place = (at + lane) % CHUNKS;
+            const uint32_t chunk = place ^ turn(slot);
+            int64_t row = first + row_of_slot(slot);
+            row = row < lo ? lo : row > hi ? hi : row;
+            if (DIM == (int)head_dim || chunk * 8 < head_dim)
+                __builtin_amdgcn_global_load_lds(
+                    (const __attribute__((address_space(1))) void*)(base + row * stride + chunk * 8),
+                    (__attribute__((address_space(3))) void*)(tile + at * 16), 16, 0, 0);
+        }
+    }
+
+    static __device__ __forceinline__ void clear(char* tile) {
+        for (int i = threadIdx.x; i < BYTES / 16; i += THREADS) reinterpret_cast<float4*>(tile)[i] = make_float4(0, 0, 0, 0);
+    }
+
+    // A operand: rows of the 32-row tile at slot0, columns 16 step .. + 15.
+    static __device__ __forceinline__ frag<T> rows(const char* tile, uint32_t slot0, int step) {
+        const uint32_t lane = threadIdx.x % WAVE, slot = slot0 + lane % 32;
+        return *reinterpret_cast<const frag<T>*>(tile + slot * (DIM * 2) + ((2 * step + lane / 32) ^ turn(slot)) * 16);
+    }
+
+    // A operand of the transpose: rows = columns 32 dt .. + 31 of the tile, columns = the
+    // sixteen rows of step t of its 32-row tile at slot0.
+    static __device__ __forceinline__ frag<T> columns(const char* tile, uint32_t slot0, int dt, int t) {
+        const uint32_t lane = threadIdx.x % WAVE, in = lane % 16;
+        const uint32_t chunk = 4 * dt + 2 * (lane / 16 % 2) + (in % 4) / 2;
+        i16x4 half[2];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const uint32_t slot = slot0 + 8 * (2 * t + u) + 4 * (lane / 32) + in / 4;
+            const char* p = tile + slot * (DIM * 2) + (chunk ^ turn(slot)) * 16 + (in % 2) * 8;
+            half[u] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4*)p);
+        }
+        return __builtin_bit_cast(frag<T>, __builtin_shufflevector(half[0], half[1], 0, 1, 2, 3, 4, 5, 6, 7));
+    }
+};
+
+// Waits for this wave's fetches into LDS, then for the others.
+__device__ __forceinline__ void fetched() {
+    __builtin_amdgcn_s_waitcnt(0x0F70);           // vmcnt(0)
+    __syncthreads();
+}
+
+// B operand straight from memory: lane's row, columns 16 step + 8 (l / 32) .. + 7.
+template <typename T>
+__device__ __forceinline__ frag<T> row_operand(const T* row, int step, uint32_t head_dim) {
+    const uint32_t d = 16 * step + 8 * (threadIdx.x % WAVE / 32);
+    frag<T> v = {};
+    if (d < head_dim) v = *reinterpret_cast<const frag<T>*>(row + d);
+    return v;
+}
+
+// Between a lane and the one 32 away.
+__device__ __forceinline__ float max_halves(float v) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float sum_halves(float v) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+// Stores a transposed C tile column by column: lane's row, columns 32 dt + 8a + 4 (l / 32) .. + 3.
+template <typename T, int TILES>
+__device__ __forceinline__ void store_row(T* row, const f32x16 (&c)[TILES], float scale, uint32_t head_dim) {
+    typedef T four __attribute__((ext_vector_type(4)));
+    typedef float f32x4 __attribute__((ext_vector_type(4)));
+#pragma unroll
+    for (int dt = 0; dt < TILES; ++dt)
+#pragma unroll
+        for (int a = 0; a < 4; ++a) {
+            const uint32_t d = 32 * dt + 8 * a + 4 * (threadIdx.x % WAVE / 32);
+            const f32x4 v = {c[dt][4 * a] * scale, c[dt][4 * a + 1] * scale, c[dt][4 * a + 2] * scale, c[dt][4 * a + 3] * scale};
+            if (d < head_dim) *reinterpret_cast<four*>(row + d) = __builtin_convertvector(v, four);
+        }
+}
+
+// ------------------------------------------------------------------ the dropout mask
+//
+// A block of the random field is two queries by four keys, so that lanes which hold a
+// query's keys and lanes which hold a key's queries both share blocks with neighbours
+// and none is drawn twice in a pass over a tile.
+
+template <int CTRL>
+__device__ __forceinline__ uint32_t quad(uint32_t v) {
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xf, 0xf, true);
+}
+
+// Lane = query, element r = key 16 (l / 32) + r of the tile that begins at key0 (a multiple of 32): bit r
+// of the result says that element r is kept.  The two lanes of a pair draw two of the four
+// blocks each.
+__device__ __forceinline__ void kept_keys(uint32_t (&w)[16], uint32_t query, uint32_t key0, uint32_t plane, RandomKey key,
+                                          uint32_t site) {
+    const uint32_t lane = threadIdx.x % WAVE, odd = lane & 1;
+    RandomBlock b[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+        b[i] = random_block(key, key0 / 4 + 4 * (lane / 32) + 2 * odd + i, query / 2, plane, site);
+#pragma unroll
+    for (int r = 0; r < 16; ++r) w[r] = r < 8 ? quad<0xA0>(b[r / 4 % 2].w[r % 4]) : quad<0xF5>(b[r / 4 % 2].w[r % 4]);
+}
+
+// Lane = key, element r = query 16 (l / 32) + r of the tile that begins at query0 (a multiple of 32):
+// w[p] is the word of queries 2p and 2p + 1.  Each of the four lanes of a quad draws two of
+// the eight blocks, and a 4 x 4 transpose hands every lane its key's words.
+__device__ __forceinline__ void kept_queries(uint32_t (&w)[8], uint32_t key_index, uint32_t query0, uint32_t plane,
+                                             RandomKey key, uint32_t site) {
+    const uint32_t lane = threadIdx.x % WAVE;
+    const bool one = lane & 1, two = lane & 2;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        RandomBlock b = random_block(key, key_index / 4, query0 / 2 + 8 * (lane / 32) + 4 * i + lane % 4, plane, site);
+#pragma unroll
+        for (int p = 0; p < 4; p += 2) {
+            const uint32_t got = quad<0xB1>(one ? b.w[p] : b.w[p + 1]);
+            b.w[p] = one ? got : b.w[p];
+            b.w[p + 1] = one ? b.w[p + 1] : got;
+        }
+#pragma unroll
+        for (int p = 0; p < 2; ++p) {
+            const uint32_t got = quad<0x4E>(two ? b.w[p] : b.w[p + 2]);
+            b.w[p] = two ? got : b.w[p];
+            b.w[p + 2] = two ? b.w[p + 2] : got;
+        }
+#pragma unroll
+        for (int p = 0; p < 4; ++p) w[4 * i + p] = b.w[p];
+    }
+}
+
+// ------------------------------------------------------------------ arguments
+
+struct Strides { uint64_t batch, row, head; };
+
+struct AttentionArgs {
+    uint32_t batch, heads, kv_heads, group, q_len, k_len, head_dim, site;
+    bool causal;
+    float scale, scale_log2;                     // scale * log2 e: scores are taken to base 2
+    DropoutRule drop;
+    const uint64_t* seed;
+    const int32_t *q_lens, *k_lens;
+    Strides q, k, v, o, d_o, dq, dk, dv;
+};
+
+// Checks the arguments of a direction and fills the kernels'; false if refused.
+bool attention_args(const okt_attention* op, bool backward, AttentionArgs& a);
+
+// Lengths of a sequence, held to the tensors'.
+__device__ __forceinline__ int sequence_length(const int32_t* lens, uint32_t b, uint32_t most) {
+    if (!lens) return (int)most;
+    const int n = lens[b];
+    return n < 0 ? 0 : n > (int)most ? (int)most : n;
+}
+
+// Bytes before the backward pass's parts of the workspace end.
+size_t attention_ws_bytes(uint32_t batch, uint32_t heads, uint32_t q_len);
+
+}  // namespace okt
+
+#endif

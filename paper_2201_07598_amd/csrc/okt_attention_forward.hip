@@ -1,0 +1,210 @@
+// okt_attention_forward: one pass over the keys with a running maximum and sum.
+//
+// A wave owns 32 queries, a workgroup four waves; the keys and values come by in tiles of
+// 64 rows that all four share in LDS, the next tile on its way while one is used.  Scores
+// are taken transposed (keys down, queries across): a lane then holds one query's
+// scores, so maximum and sum stay in the lane but for one exchange with the lane 32 away,
+// and the probabilities are the second product's operand as they lie.
+#include "okt_attention.h"
+
+namespace okt {
+
+constexpr int FWD_THREADS = 256;
+constexpr int FWD_QUERIES = FWD_THREADS / WAVE * 32;
+constexpr int FWD_KEYS = 64;
+
+template <typename T, int DIM, bool DROP>
+__global__ __launch_bounds__(FWD_THREADS) void attention_forward_kernel(AttentionArgs a, const T* q, const T* k, const T* v,
+                                                                        T* o, float* lse, uint32_t blocks) {
+    using Tile = RowTile<T, DIM, FWD_KEYS, FWD_THREADS>;
+    __shared__ __attribute__((aligned(1024))) char shared[4 * Tile::BYTES];
+    const uint32_t plane = blockIdx.x / blocks, b = plane / a.heads, h = plane % a.heads, kv = h / a.group;
+    const uint32_t wave = uniform(threadIdx.x / WAVE), lane = threadIdx.x % WAVE;
+    const int ql = sequence_length(a.q_lens, b, a.q_len), kl = sequence_length(a.k_lens, b, a.k_len);
+    const int q0 = blockIdx.x % blocks * FWD_QUERIES, w0 = q0 + 32 * (int)wave, i = w0 + (int)(lane % 32);
+    T* out = o + b * a.o.batch + (uint64_t)i * a.o.row + h * a.o.head;
+
+    // keys that the last query of the workgroup, and that the first and last of the wave see
+    const int past = a.causal ? kl - ql + 1 : 0;
+    const auto seen = [&](int query) { const int n = query + past; return !a.causal || n > kl ? kl : n < 0 ? 0 : n; };
+    const int last = q0 + FWD_QUERIES < ql ? q0 + FWD_QUERIES - 1 : ql - 1;
+    const int keys = q0 < ql ? seen(last) : 0;
+    const int mine = i < ql ? seen(i) : 0, wave_least = w0 + 31 < ql ? seen(w0) : 0;
+
+    frag<T> qf[DIM / 16];
+    f32x16 acc[DIM / 32];
+    float top = -INFINITY, total = 0.0f;
+#pragma unroll
+    for (int d = 0; d < DIM / 32; ++d) acc[d] = 0.0f;
+    if (keys > 0) {
+        const T* kb = k + b * a.k.batch + kv * a.k.head;
+        const T* vb = v + b * a.v.batch + kv * a.v.head;
+        const T* qrow = q + b * a.q.batch + (uint64_t)(i < ql ? i : ql - 1) * a.q.row + h * a.q.head;
+#pragma unroll
+        for (int s = 0; s < DIM / 16; ++s) qf[s] = row_operand(qrow, s, a.head_dim);
+        RandomKey key = {0, 0};
+        if (DROP) key = random_key(a.seed);
+        if (a.head_dim != DIM) {
+            for (int n = 0; n < 4; ++n) Tile::clear(shared + n * Tile::BYTES);
+            __syncthreads();
+        }
+        Tile::fetch(shared, kb, a.k.row, 0, 0, kl - 1, a.head_dim);
+        Tile::fetch(shared + Tile::BYTES, vb, a.v.row, 0, 0, kl - 1, a.head_dim);
+        for (int key0 = 0, turn = 0; key0 < keys; key0 += FWD_KEYS, turn ^= 1) {
+            fetched();
+            const char* kt = shared + turn * 2 * Tile::BYTES;
+            const char* vt = kt + Tile::BYTES;
+            if (key0 + FWD_KEYS < keys) {
+                char* next = shared + (turn ^ 1) * 2 * Tile::BYTES;
+                Tile::fetch(next, kb, a.k.row, key0 + FWD_KEYS, 0, kl - 1, a.head_dim);
+                Tile::fetch(next + Tile::BYTES, vb, a.v.row, key0 + FWD_KEYS, 0, kl - 1, a.head_dim);
+            }
+            f32x16 s[FWD_KEYS / 32];
+#pragma unroll
+            for (int n = 0; n < FWD_KEYS / 32; ++n) {
+                s[n] = 0.0f;
+#pragma unroll
+                for (int e = 0; e < DIM / 16; ++e) s[n] = mfma(Tile::rows(kt, 32 * n, e), qf[e], s[n]);
+            }
+            float most = -INFINITY;
+            if (key0 + FWD_KEYS > wave_least) {                // some of the tile is hidden from some lane
+#pragma unroll
+                for (int n = 0; n < FWD_KEYS / 32; ++n)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r)
+                        s[n][r] = key0 + 32 * n + 16 * (int)(lane / 32) + r < mine ? s[n][r] * a.scale_log2 : -INFINITY;
+            } else {
+#pragma unroll
+                for (int n = 0; n < FWD_KEYS / 32; ++n) s[n] *= a.scale_log2;
+            }
+#pragma unroll
+            for (int n = 0; n < FWD_KEYS / 32; ++n)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) most = fmaxf(most, s[n][r]);
+            most = fmaxf(top, max_halves(most));
+            const float base = most == -INFINITY ? 0.0f : most;
+            const float fade = __builtin_amdgcn_exp2f(top - base);
+            top = most;
+            total *= fade;
+#pragma unroll
+            for (int d = 0; d < DIM / 32; ++d) acc[d] *= fade;
+#pragma unroll
+            for (int n = 0; n < FWD_KEYS / 32; ++n) {
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    s[n][r] = __builtin_amdgcn_exp2f(s[n][r] - base);
+                    total += s[n][r];
+                }
+                if (DROP) {
+                    uint32_t w[16];
+                    kept_keys(w, i, key0 + 32 * n, plane, key, a.site);
+                    const uint32_t mask = lane & 1 ? 0xffffffffu : 0xffffu, bar = a.drop.bar << (16 * (lane & 1));
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) s[n][r] = (w[r] & mask) < bar ? s[n][r] : 0.0f;
+                }
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
+                    const frag<T> p = to_operand<T>(s[n], t);
+#pragma unroll
+                    for (int d = 0; d < DIM / 32; ++d) acc[d] = mfma(Tile::columns(vt, 32 * n, d, t), p, acc[d]);
+                }
+            }
+        }
+    }
+    total = sum_halves(total);
+    if (i < (int)a.q_len) {
+        store_row(out, acc, mine > 0 ? a.drop.scale / total : 0.0f, a.head_dim);
+        if (lse && lane < 32)
+            lse[(uint64_t)plane * a.q_len + i] = mine > 0 ? (top + __builtin_amdgcn_logf(total)) * 0.693147180559945f : -INFINITY;
+    }
+}
+
+template <typename T, int DIM>
+static void launch_forward(const AttentionArgs& a, const void* q, const void* k, const void* v, void* o, float* lse, hipStream_t s) {
+    const uint32_t blocks = (a.q_len + FWD_QUERIES - 1) / FWD_QUERIES;
+    auto* kernel = a.drop.bar == 65536u ? attention_forward_kernel<T, DIM, false> : attention_forward_kernel<T, DIM, true>;
+    hipLaunchKernelGGL(kernel, dim3(blocks * a.batch * a.heads), dim3(FWD_THREADS), 0, s, a, (const T*)q, (const T*)k,
+                       (const T*)v, (T*)o, lse, blocks);
+}
+
+static bool strides(const uint64_t (&s)[3], Strides& to) {
+    to = {s[0], s[1], s[2]};
+    for (uint64_t n : s)
+        if (n % 8 || n > (1ull << 40)) return false;
+    return true;
+}
+
+bool attention_args(const okt_attention* op, bool backward, AttentionArgs& a) {
+    if (!op || (op->dtype != OKT_BF16 && op->dtype != OKT_F16)) return false;
+    if (op->kv_heads == 0 || op->heads == 0 || op->heads % op->kv_heads) return false;
+    if ((uint64_t)op->batch * op->heads > (1u << 20) || op->q_len > (1u << 24) || op->k_len > (1u << 24)) return false;
+    // workgroups of a launch: a block of 128 rows of one head each
+    if (((uint64_t)(op->q_len > op->k_len ? op->q_len : op->k_len) / 128 + 1) * op->batch * op->heads > (1u << 30)) return false;
+    if (op->head_dim == 0 || op->head_dim > 128 || op->head_dim % 8) return false;
+    if (!(op->scale > 0.0f) || op->scale > 3.0e38f) return false;
+    if (!dropout_rule(op->dropout_p, a.drop)) return false;
+    if (a.drop.bar != 65536u && (!op->d_seed || !aligned(op->d_seed, 8))) return false;
+    if (!aligned(op->d_q_lens, 4) || !aligned(op->d_k_lens, 4)) return false;
+    if (!strides(op->q_stride, a.q) || !strides(op->k_stride, a.k) ||
+        !strides(op->v_stride, a.v) || !strides(op->o_stride, a.o)) return false;
+    if (backward && (!strides(op->do_stride, a.d_o) || !strides(op->dq_stride, a.dq) ||
+                     !strides(op->dk_stride, a.dk) || !strides(op->dv_stride, a.dv))) return false;
+    a.batch = op->batch;
+    a.heads = op->heads;
+    a.kv_heads = op->kv_heads;
+    a.group = op->heads / op->kv_heads;
+    a.q_len = op->q_len;
+    a.k_len = op->k_len;
+    a.head_dim = op->head_dim;
+    a.site = op->site;
+    a.causal = op->causal != 0;
+    a.scale = op->scale;
+    a.scale_log2 = (float)((double)op->scale * 1.4426950408889634);
+    a.seed = op->d_seed;
+    a.q_lens = op->d_q_lens;
+    a.k_lens = op->d_k_lens;
+    return true;
+}
+
+size_t attention_ws_bytes(uint32_t batch, uint32_t heads, uint32_t q_len) {
+    return ((size_t)batch * heads * q_len * sizeof(float) + 255) & ~(size_t)255;      // D of every row
+}
+
+}  // namespace okt
+
+extern "C" {
+
+size_t okt_attention_workspace_bytes(uint32_t batch, uint32_t heads, uint32_t kv_heads, uint32_t q_len, uint32_t k_len,
+                                     uint32_t head_dim) {
+    (void)kv_heads;
+    (void)k_len;
+    (void)head_dim;
+    const size_t need = okt::attention_ws_bytes(batch, heads, q_len);
+    return need ? need : 256;
+}
+
+int okt_attention_forward(const okt_attention* op, const void* d_q, const void* d_k, const void* d_v, void* d_o_out,
+                          float* d_lse_out, void* d_ws, size_t ws_bytes, void* stream) {
+    using namespace okt;
+    AttentionArgs a;
+    if (!attention_args(op, false, a)) return OKT_ERR_INVALID_ARG;
+    if (a.batch == 0 || a.q_len == 0) return OKT_OK;
+    if (!d_q || !d_o_out || (a.k_len && (!d_k || !d_v))) return OKT_ERR_INVALID_ARG;
+    if (!aligned(d_q, 16) || !aligned(d_k, 16) || !aligned(d_v, 16) || !aligned(d_o_out, 16) || !aligned(d_lse_out, 4)) return OKT_ERR_INVALID_ARG;
+    (void)d_ws;
+    (void)ws_bytes;
+    const hipStream_t s = (hipStream_t)stream;
+    const bool narrow = a.head_dim <= 64;
+    timing_before(s);
+    if (op->dtype == OKT_BF16) {
+        if (narrow) launch_forward<__bf16, 64>(a, d_q, d_k, d_v, d_o_out, d_lse_out, s);
+        else launch_forward<__bf16, 128>(a, d_q, d_k, d_v, d_o_out, d_lse_out, s);
+    } else {
+        if (narrow) launch_forward<_Float16, 64>(a, d_q, d_k, d_v, d_o_out, d_lse_out, s);
+        else launch_forward<_Float16, 128>(a, d_q, d_k, d_v, d_o_out, d_lse_out, s);
+    }
+    timing_after(s);
+    return launch_status();
+}
+
+}  // extern "C"

@@ -1,0 +1,573 @@
+// okt_residual_norm_forward / _backward: what stands between two blocks of a layer, in one
+// pass over the rows.
+//
+//   a = Npost(u) or u        the norm after the block
+//   h = alpha x + g drop(a)  dropout, gate and the scaled residual stream
+//   y = Npre(h)              the norm before the next block
+//
+// with N(v) = (v - m) r w + b, m = mean (0 for RMS), r = 1 / sqrt(mean (v - m)^2 + eps).
+// Backward, with w' = dout w and xhat = (v - m) r:
+//   dv = r (w' - mean w' - xhat mean(w' xhat))     (RMS: without mean w')
+//   dw = sum over rows of dout xhat,  db = sum of dout,  dg = sum of dh drop(a)
+//
+// A row lives in the registers of a wave or of a workgroup (LANES threads of VECS groups of
+// eight columns), so the mean, the centred squares and the result are taken from one read
+// of it; everything is fp32 between the load and the one rounding of the store.  The second norm reads h as it was
+// stored, since that is what the backward pass has.  The mask of the dropout is drawn
+// again in the backward pass: a group of eight columns is a block of the random field.
+// Workgroups walk over the rows and keep the parameters, and backward the sums over rows, in
+// registers; those sums leave as one partial row per workgroup, which a second launch
+// adds in a fixed order (no atomics: the result does not change from run to run).
+// Bound by memory: forward 4 elements a place, backward 5 or 6.
+#include "okt_element.h"
+#include "okt_random.h"
+
+namespace okt {
+
+// ------------------------------------------------------------------ sizes (host)
+
+constexpr uint32_t NORM_MAX_WIDTH = 16384;
+constexpr uint64_t NORM_MAX_ROWS = 1ull << 40;
+constexpr uint32_t NORM_BACKWARD_GROUPS = 512;     // workgroups aimed at: two to a CU
+constexpr uint32_t NORM_SUMS = 5;                  // pre w, pre b, post w, post b, gate
+
+struct NormShape { uint32_t lanes, vecs; };
+
+// The fewest threads that hold a row of 16 columns each; up to 512 columns of 8.
+static NormShape norm_shape(uint32_t width) {
+    if (width <= 512) return {64, 1};
+    if (width <= 1024) return {64, 2};
+    if (width <= 2048) return {256, 1};
+    if (width <= 4096) return {256, 2};
+    if (width <= 8192) return {512, 2};
+    return {1024, 2};
+}
+
+static uint32_t rows_at_once(NormShape s) { return s.lanes == 64 ? 4 : 1; }
+
+// How the backward pass deals out rows.  A workgroup owns `chunk` rows that either are
+// whole gates' rows (parts == 1: it writes their dgate itself) or lie within one gate
+// (parts workgroups to a gate, whose partial sums the second launch adds).
+struct NormPlan { uint64_t chunk, rows_per_gate, gates, groups; uint32_t parts; };
+
+static NormPlan norm_plan(uint64_t rows, uint32_t width, uint64_t rows_per_gate) {
+    NormPlan p;
+    const uint32_t at_once = rows_at_once(norm_shape(width));
+    p.rows_per_gate = rows_per_gate == 0 || rows_per_gate > rows ? rows : rows_per_gate;
+    if (rows == 0) return {1, 1, 1, 0, 0};             // sums over nothing
+    p.gates = (rows + p.rows_per_gate - 1) / p.rows_per_gate;
+    p.chunk = (rows + NORM_BACKWARD_GROUPS - 1) / NORM_BACKWARD_GROUPS;
+    p.chunk = (p.chunk + at_once - 1) / at_once * at_once;
+    if (p.rows_per_gate <= p.chunk) {
+        p.chunk = (p.chunk + p.rows_per_gate - 1) / p.rows_per_gate * p.rows_per_gate;
+        p.parts = 1;
+        p.groups = (rows + p.chunk - 1) / p.chunk;
+    } else {
+        p.parts = (uint32_t)((p.rows_per_gate + p.chunk - 1) / p.chunk);
+        p.chunk = (p.rows_per_gate + p.parts - 1) / p.parts;
+        p.groups = p.gates * p.parts;
+    }
+    return p;
+}
+
+static size_t norm_ws_bytes(uint64_t rows, uint32_t width, uint64_t rows_per_gate) {
+    return (size_t)(NORM_SUMS * norm_plan(rows, width, rows_per_gate).groups * width * sizeof(float) + 255) & ~(size_t)255;
+}
+
+// ------------------------------------------------------------------ device
+
+struct NormArgs {
+    uint64_t rows, rows_per_gate;
+    uint32_t width, site;
+    float eps, alpha, inv_width;
+    bool layer;
+    DropoutRule drop;                               // bar 65536: none
+    const uint64_t* seed;
+    const float *post_w, *post_b, *gate, *pre_w, *pre_b;
+    uint64_t u_stride, x_stride, h_stride, y_stride, dh_stride, dy_stride, dx_stride, du_stride;
+    float4* stats;
+    // backward
+    uint64_t chunk, groups;
+    uint32_t parts;
+    float* partial;                                 // [NORM_SUMS][groups][width]
+    float* dgate;
+};
+
+// Sum over the wave, the same in every lane, in the vector unit alone.
+__device__ __forceinline__ float wave_sum_f32(float v) {
+#define OKT_DPP_ADD(ctrl, rows) \
+    v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), ctrl, rows, 0xf, false))
+    OKT_DPP_ADD(0xB1, 0xf);                         // neighbours
+    OKT_DPP_ADD(0x4E, 0xf);                         // pairs of a quad
+    OKT_DPP_ADD(0x141, 0xf);                        // quads of half a row
+    OKT_DPP_ADD(0x140, 0xf);                        // halves of a row of 16
+    OKT_DPP_ADD(0x142, 0xa);                        // row 0 into 1, 2 into 3
+    OKT_DPP_ADD(0x143, 0xc);                        // rows 0-1 into 2-3
+#undef OKT_DPP_ADD
+    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
+}
+
+// Two sums over the LANES threads of a row.  `turn` alternates between two sets of slots,
+// so one barrier a call is enough: a set is written again only after the next call's barrier.
+template <int LANES>
+__device__ __forceinline__ void row_sums(float& a, float& b, float2 (*slots)[LANES / WAVE], int& turn) {
+    a = wave_sum_f32(a);
+    b = wave_sum_f32(b);
+    if (LANES > WAVE) {
+        const int wave = threadIdx.x / WAVE;
+        if (threadIdx.x % WAVE == 0) slots[turn][wave] = make_float2(a, b);
+        __syncthreads();
+        a = b = 0.0f;
+#pragma unroll
+        for (int w = 0; w < LANES / WAVE; ++w) {
+            a += slots[turn][w].x;
+            b += slots[turn][w].y;
+        }
+        turn ^= 1;
+    }
+}
+
+__device__ __forceinline__ float sum_eight(f32x8 v) {
+    return ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
+}
+
+// The columns of one thread: VECS groups of eight, LANES groups apart.
+template <int LANES, int VECS>
+struct Columns {
+    uint32_t lane, width;
+    __device__ __forceinline__ uint32_t group(int v) const { return v * LANES + lane; }
+    __device__ __forceinline__ int count(int v) const {
+        const int left = (int)width - (int)(group(v) * 8);
+        return left >= 8 ? 8 : left > 0 ? left : 0;
+    }
+    template <typename T>
+    __device__ __forceinline__ void load(f32x8 (&to)[VECS], const T* row, float rest = 0.0f) const {
+#pragma unroll
+        for (int v = 0; v < VECS; ++v) {
+            const int n = count(v);
+            const T* p = row + group(v) * 8;
+            to[v] = n == 8 ? load_eight(p) : load_some(p, n, rest);
+        }
+    }
+    template <typename T>
+    __device__ __forceinline__ void store(T* row, const f32x8 (&from)[VECS]) const {
+#pragma unroll
+        for (int v = 0; v < VECS; ++v) {
+            const int n = count(v);
+            T* p = row + group(v) * 8;
+            if (n == 8) store_eight(p, from[v]);
+            else store_some(p, from[v], n);
+        }
+    }
+};
+
+// Mean and reciprocal deviation of a row: the mean first, then the centred squares.
+template <int LANES, int VECS>
+__device__ __forceinline__ float2 row_statistics(const f32x8 (&v)[VECS], const Columns<LANES, VECS>& cols, const NormArgs& a,
+                                                 float2 (*slots)[LANES / WAVE], int& turn) {
+    float mean = 0.0f, none = 0.0f, squares = 0.0f;
+    if (a.layer) {
+#pragma unroll
+        for (int i = 0; i < VECS; ++i) mean += sum_eight(v[i]);      // columns past the width hold 0
+        row_sums<LANES>(mean, none, slots, turn);
+        mean *= a.inv_width;
+    }
+#pragma unroll
+    for (int i = 0; i < VECS; ++i) {
+        const int n = cols.count(i);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const float d = j < n ? v[i][j] - mean : 0.0f;
+            squares = __builtin_fmaf(d, d, squares);
+        }
+    }
+    none = 0.0f;
+    row_sums<LANES>(squares, none, slots, turn);
+    return make_float2(mean, 1.0f / __builtin_sqrtf(__builtin_fmaf(squares, a.inv_width, a.eps)));
+}
+
+// Multiplies by scale what the random field keeps and clears the rest.
+template <int LANES, int VECS>
+__device__ __forceinline__ void drop_row(f32x8 (&v)[VECS], const Columns<LANES, VECS>& cols, uint64_t row, RandomKey key,
+                                         const NormArgs& a) {
+#pragma unroll
+    for (int i = 0; i < VECS; ++i) {
+        const RandomBlock b = random_block(key, cols.group(i), (uint32_t)row, (uint32_t)(row >> 32), a.site);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[i][j] = kept(b, j, a.drop.bar) ? v[i][j] * a.drop.scale : 0.0f;
+    }
+}
+
+template <int LANES, int VECS>
+constexpr int norm_threads() { return LANES == WAVE ? 256 : LANES; }
+
+template <typename T, int LANES, int VECS>
+__global__ __launch_bounds__((norm_threads<LANES, VECS>())) void norm_forward_kernel(NormArgs a, const T* u, const T* x, T* h,
+                                                                                   T* y) {
+    constexpr int AT_ONCE = norm_threads<LANES, VECS>() / LANES;
+    __shared__ float2 slots[2][LANES / WAVE];
+    int turn = 0;
+    const Columns<LANES, VECS> cols = {threadIdx.x % LANES, a.width};
+    const bool drops = a.drop.bar != 65536u;
+    RandomKey key = {0, 0};
+    if (drops) key = random_key(a.seed);
+    f32x8 pre_w[VECS], pre_b[VECS];
+    if (a.pre_w) cols.load(pre_w, a.pre_w);
+    if (a.pre_b) cols.load(pre_b, a.pre_b);
+    for (uint64_t row = (uint64_t)blockIdx.x * AT_ONCE + threadIdx.x / LANES; row < a.rows; row += (uint64_t)gridDim.x * AT_ONCE) {
+        f32x8 s[VECS], r[VECS];
+        float4 st = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        cols.load(s, u + row * a.u_stride);
+        cols.load(r, x + row * a.x_stride);
+        if (a.post_w) {
+            const float2 m = row_statistics<LANES, VECS>(s, cols, a, slots, turn);
+            st.x = m.x;
+            st.y = m.y;
+            f32x8 w[VECS];
+            cols.load(w, a.post_w);
+#pragma unroll
+            for (int i = 0; i < VECS; ++i) s[i] = (s[i] - m.x) * m.y * w[i];
+            if (a.post_b) {
+                cols.load(w, a.post_b);
+#pragma unroll
+                for (int i = 0; i < VECS; ++i) s[i] += w[i];
+            }
+        }
+        if (drops) drop_row<LANES, VECS>(s, cols, row, key, a);
+        if (a.gate) {
+            f32x8 g[VECS];
+            cols.load(g, a.gate + row / a.rows_per_gate * a.width);
+#pragma unroll
+            for (int i = 0; i < VECS; ++i) s[i] *= g[i];
+        }
+#pragma unroll
+        for (int i = 0; i < VECS; ++i) s[i] = __builtin_convertvector(
+            __builtin_convertvector(a.alpha * r[i] + s[i], typename Eight<T>::vec), f32x8);
+        if (h) cols.store(h + row * a.h_stride, s);
+        if (a.pre_w) {
+            const float2 m = row_statistics<LANES, VECS>(s, cols, a, slots, turn);
+            st.z = m.x;
+            st.w = m.y;
+#pragma unroll
+            for (int i = 0; i < VECS; ++i) s[i] = (s[i] - m.x) * m.y * pre_w[i];
+            if (a.pre_b) {
+#pragma unroll
+                for (int i = 0; i < VECS; ++i) s[i] += pre_b[i];
+            }
+            cols.store(y + row * a.y_stride, s);
+        }
+        if (a.stats && cols.lane == 0) a.stats[row] = st;
+    }
+}
+
+// The gradient of a norm's input from the gradient of its output (in place), and what this
+// row adds to the gradients of its weight and bias.
+template <int LANES, int VECS>
+__device__ __forceinline__ void norm_input_gradient(f32x8 (&d)[VECS], const f32x8 (&v)[VECS], const f32x8 (&w)[VECS],
+                                                    float mean, float r, f32x8 (&dw)[VECS], f32x8 (&db)[VECS],
+                                                    const NormArgs& a, float2 (*slots)[LANES / WAVE], int& turn) {
+    float plain = 0.0f, along = 0.0f;
+    f32x8 xhat[VECS];
+#pragma unroll
+    for (int i = 0; i < VECS; ++i) {
+        xhat[i] = (v[i] - mean) * r;
+        const f32x8 p = d[i] * xhat[i];
+        dw[i] += p;
+        db[i] += d[i];
+        d[i] *= w[i];
+        plain += sum_eight(d[i]);
+        along += sum_eight(p * w[i]);
+    }
+    row_sums<LANES>(plain, along, slots, turn);
+    plain = a.layer ? plain * a.inv_width : 0.0f;
+    along *= a.inv_width;
+#pragma unroll
+    for (int i = 0; i < VECS; ++i) d[i] = (d[i] - plain - xhat[i] * along) * r;
+}
+
+// Adds what the waves of a workgroup that work on different rows hold, and writes it out.
+template <int LANES, int VECS>
+__device__ __forceinline__ void put_sums(f32x8 (&v)[VECS], const Columns<LANES, VECS>& cols, float* to, float* shared) {
+    if (LANES == WAVE) {
+        constexpr int SPAN = LANES * VECS * 8;
+        const int wave = threadIdx.x / WAVE;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < VECS; ++i) *reinterpret_cast<f32x8*>(shared + wave * SPAN + cols.group(i) * 8) = v[i];
+        __syncthreads();
+        for (uint32_t c = threadIdx.x; c < cols.width; c += 256)
+            to[c] = (shared[c] + shared[SPAN + c]) + (shared[2 * SPAN + c] + shared[3 * SPAN + c]);
+    } else {
+        cols.store(to, v);
+    }
+}
+
+// ALL: with a norm after the block or a gate; without, the registers they take are free.
+template <typename T, int LANES, int VECS, bool ALL>
+__global__ __launch_bounds__((norm_threads<LANES, VECS>())) void norm_backward_kernel(
+    NormArgs a, const T* u, const T* h, const T* dh, const T* dy, T* dx, T* du) {
+    constexpr int AT_ONCE = norm_threads<LANES, VECS>() / LANES;
+    __shared__ float2 slots[2][LANES / WAVE];
+    __shared__ __attribute__((aligned(32))) float shared[LANES == WAVE ? 4 * LANES * VECS * 8 : 1];
+    int turn = 0;
+    const Columns<LANES, VECS> cols = {threadIdx.x % LANES, a.width};
+    const bool drops = a.drop.bar != 65536u;
+    RandomKey key = {0, 0};
+    if (drops) key = random_key(a.seed);
+    f32x8 pre_w[VECS], dpre_w[VECS], dpre_b[VECS], dpost_w[VECS], dpost_b[VECS], dgate[VECS];
+#pragma unroll
+    for (int i = 0; i < VECS; ++i) dpre_w[i] = dpre_b[i] = dpost_w[i] = dpost_b[i] = dgate[i] = 0.0f;
+    if (a.pre_w) cols.load(pre_w, a.pre_w);
+
+    const uint64_t gate0 = a.parts > 1 ? blockIdx.x / a.parts : blockIdx.x * (a.chunk / a.rows_per_gate);
+    uint64_t begin = a.parts > 1 ? gate0 * a.rows_per_gate + blockIdx.x % a.parts * a.chunk : blockIdx.x * a.chunk;
+    uint64_t last = begin + a.chunk;
+    if (a.parts > 1 && last > (gate0 + 1) * a.rows_per_gate) last = (gate0 + 1) * a.rows_per_gate;
+    if (last > a.rows) last = a.rows;
+    for (uint64_t gate = gate0; begin < last || gate == gate0; ++gate) {
+        // the rows of one gate; a workgroup whose part of it is empty passes through once
+        uint64_t end = (gate + 1) * a.rows_per_gate;
+        if (end > last) end = last;
+        f32x8 g[VECS];
+        if (ALL && a.gate) cols.load(g, a.gate + gate * a.width);
+        for (uint64_t row = begin + threadIdx.x / LANES; row < end; row += AT_ONCE) {
+            const float4 st = a.stats[row];
+            f32x8 d[VECS], v[VECS];
+            if (dh) {
+                cols.load(d, dh + row * a.dh_stride);
+            } else {
+#pragma unroll
+                for (int i = 0; i < VECS; ++i) d[i] = 0.0f;
+            }
+            f32x8 su[VECS];
+            if (ALL) cols.load(su, u + row * a.u_stride);
+            if (a.pre_w) {
+                f32x8 o[VECS];
+                cols.load(v, h + row * a.h_stride);
+                cols.load(o, dy + row * a.dy_stride);
+                norm_input_gradient<LANES, VECS>(o, v, pre_w, st.z, st.w, dpre_w, dpre_b, a, slots, turn);
+#pragma unroll
+                for (int i = 0; i < VECS; ++i) d[i] += o[i];
+            }
+#pragma unroll
+            for (int i = 0; i < VECS; ++i) v[i] = a.alpha * d[i];
+            cols.store(dx + row * a.dx_stride, v);
+            if (drops) drop_row<LANES, VECS>(d, cols, row, key, a);
+            if (ALL) {
+                f32x8 w[VECS];
+                if (a.post_w) cols.load(w, a.post_w);
+                if (a.gate) {
+                    f32x8 b[VECS];
+                    if (a.post_b) cols.load(b, a.post_b);
+#pragma unroll
+                    for (int i = 0; i < VECS; ++i) {
+                        f32x8 s = su[i];
+                        if (a.post_w) s = (s - st.x) * st.y * w[i];
+                        if (a.post_b) s += b[i];
+                        dgate[i] += d[i] * s;       // d holds the mask and its scale already
+                        d[i] *= g[i];
+                    }
+                }
+                if (a.post_w) norm_input_gradient<LANES, VECS>(d, su, w, st.x, st.y, dpost_w, dpost_b, a, slots, turn);
+            }
+            cols.store(du + row * a.du_stride, d);
+        }
+        if (ALL && a.dgate) {
+            float* to = a.parts > 1 ? a.partial + (4 * a.groups + blockIdx.x) * a.width : a.dgate + gate * a.width;
+            put_sums<LANES, VECS>(dgate, cols, to, shared);
+#pragma unroll
+            for (int i = 0; i < VECS; ++i) dgate[i] = 0.0f;
+        }
+        begin = end > begin ? end : begin;
+        if (begin >= last) break;
+    }
+    const auto at = [&](int sum) { return a.partial + (sum * a.groups + blockIdx.x) * a.width; };
+    if (a.pre_w) {
+        put_sums<LANES, VECS>(dpre_w, cols, at(0), shared);
+        if (a.pre_b) put_sums<LANES, VECS>(dpre_b, cols, at(1), shared);
+    }
+    if (ALL && a.post_w) {
+        put_sums<LANES, VECS>(dpost_w, cols, at(2), shared);
+        if (a.post_b) put_sums<LANES, VECS>(dpost_b, cols, at(3), shared);
+    }
+}
+
+// Adds partial rows: 64 columns a workgroup, four slices of the rows, always in the same
+// order.  blockIdx.y: one of the four parameter gradients (rows = all groups), or 4 + gate
+// (rows = that gate's parts).
+struct NormOutputs { float* to[4]; };
+constexpr int NORM_ADD_BLOCK = 256;
+
+__global__ __launch_bounds__(NORM_ADD_BLOCK) void norm_add_kernel(NormOutputs out, float* dgate, const float* partial,
+                                                                  uint64_t groups, uint32_t parts, uint32_t width) {
+    __shared__ float shared[NORM_ADD_BLOCK];
+    const uint32_t which = blockIdx.y, col = blockIdx.x * WAVE + threadIdx.x % WAVE, slice = threadIdx.x / WAVE;
+    float* to = which < 4 ? out.to[which] : dgate + (uint64_t)(which - 4) * width;
+    if (!to) return;
+    const float* from = partial + (which < 4 ? which * groups : 4 * groups + (uint64_t)(which - 4) * parts) * width;
+    const uint64_t rows = which < 4 ? groups : parts;
+    float sum = 0.0f;
+    if (col < width) {
+        const uint64_t each = (rows + 3) / 4, end = (slice + 1) * each < rows ? (slice + 1) * each : rows;
+#pragma unroll 8
+        for (uint64_t r = slice * each; r < end; ++r) sum += from[r * width + col];
+    }
+    shared[threadIdx.x] = sum;
+    __syncthreads();
+    if (slice == 0 && col < width)
+        to[col] = (shared[threadIdx.x] + shared[WAVE + threadIdx.x]) +
+                  (shared[2 * WAVE + threadIdx.x] + shared[3 * WAVE + threadIdx.x]);
+}
+
+// ------------------------------------------------------------------ host
+
+// Checks what both directions share and fills the kernels' arguments; false if refused.
+static bool norm_args(const okt_residual_norm* op, NormArgs& a) {
+    if (!op || !known_dtype(op->dtype) || op->rows > NORM_MAX_ROWS || op->width == 0 || op->width > NORM_MAX_WIDTH) return false;
+    if (op->kind != OKT_NORM_LAYER && op->kind != OKT_NORM_RMS) return false;
+    if (!(op->eps >= 0.0f) || op->residual_scale != op->residual_scale) return false;
+    if (!dropout_rule(op->dropout_p, a.drop)) return false;
+    if (a.drop.bar != 65536u && (!op->d_seed || !aligned(op->d_seed, 8))) return false;
+    if ((op->d_post_bias && !op->d_post_weight) || (op->d_pre_bias && !op->d_pre_weight)) return false;
+    for (const float* p : {op->d_post_weight, op->d_post_bias, op->d_gate, op->d_pre_weight, op->d_pre_bias})
+        if (!aligned(p, 16)) return false;
+    const auto stride = [&](uint64_t s) { return s ? s : (uint64_t)op->width; };
+    a.u_stride = stride(op->u_stride);
+    a.x_stride = stride(op->x_stride);
+    a.h_stride = stride(op->h_stride);
+    a.y_stride = stride(op->y_stride);
+    a.dh_stride = stride(op->dh_stride);
+    a.dy_stride = stride(op->dy_stride);
+    a.dx_stride = stride(op->dx_stride);
+    a.du_stride = stride(op->du_stride);
+    for (uint64_t s : {a.u_stride, a.x_stride, a.h_stride, a.y_stride, a.dh_stride, a.dy_stride, a.dx_stride, a.du_stride})
+        if (s < op->width || s > (1ull << 20)) return false;
+    a.rows = op->rows;
+    a.width = op->width;
+    a.site = op->site;
+    a.eps = op->eps;
+    a.alpha = op->residual_scale;
+    a.inv_width = 1.0f / (float)op->width;
+    a.layer = op->kind == OKT_NORM_LAYER;
+    a.seed = op->d_seed;
+    a.post_w = op->d_post_weight;
+    a.post_b = op->d_post_bias;
+    a.gate = op->d_gate;
+    a.pre_w = op->d_pre_weight;
+    a.pre_b = op->d_pre_bias;
+    a.rows_per_gate = op->rows_per_gate == 0 || op->rows_per_gate > op->rows ? (op->rows ? op->rows : 1) : op->rows_per_gate;
+    a.stats = nullptr;
+    a.partial = a.dgate = nullptr;
+    a.chunk = a.groups = 0;
+    a.parts = 1;
+    return true;
+}
+
+struct NormPointers { const void *u, *x, *h, *dh, *dy; void *out_h, *out_y, *dx, *du; };
+
+template <typename T, int LANES, int VECS>
+static void launch_norm(const NormArgs& a, const NormPointers& p, bool backward, unsigned groups, hipStream_t s) {
+    const dim3 grid(groups), block(norm_threads<LANES, VECS>());
+    if (!backward) {
+        hipLaunchKernelGGL((norm_forward_kernel<T, LANES, VECS>), grid, block, 0, s, a, (const T*)p.u, (const T*)p.x,
+                           (T*)p.out_h, (T*)p.out_y);
+    } else if (a.post_w || a.gate) {
+        hipLaunchKernelGGL((norm_backward_kernel<T, LANES, VECS, true>), grid, block, 0, s, a, (const T*)p.u, (const T*)p.h,
+                           (const T*)p.dh, (const T*)p.dy, (T*)p.dx, (T*)p.du);
+    } else {
+        hipLaunchKernelGGL((norm_backward_kernel<T, LANES, VECS, false>), grid, block, 0, s, a, (const T*)p.u, (const T*)p.h,
+                           (const T*)p.dh, (const T*)p.dy, (T*)p.dx, (T*)p.du);
+    }
+}
+
+template <typename T>
+static void launch_norm_shape(const NormArgs& a, const NormPointers& p, bool backward, unsigned groups, hipStream_t s) {
+    const NormShape n = norm_shape(a.width);
+    if (n.lanes == 64 && n.vecs == 1) launch_norm<T, 64, 1>(a, p, backward, groups, s);
+    else if (n.lanes == 64) launch_norm<T, 64, 2>(a, p, backward, groups, s);
+    else if (n.lanes == 256 && n.vecs == 1) launch_norm<T, 256, 1>(a, p, backward, groups, s);
+    else if (n.lanes == 256) launch_norm<T, 256, 2>(a, p, backward, groups, s);
+    else if (n.lanes == 512) launch_norm<T, 512, 2>(a, p, backward, groups, s);
+    else launch_norm<T, 1024, 2>(a, p, backward, groups, s);
+}
+
+static void launch_norm_type(int dtype, const NormArgs& a, const NormPointers& p, bool backward, unsigned groups, hipStream_t s) {
+    if (dtype == OKT_F32) launch_norm_shape<float>(a, p, backward, groups, s);
+    else if (dtype == OKT_BF16) launch_norm_shape<__bf16>(a, p, backward, groups, s);
+    else launch_norm_shape<_Float16>(a, p, backward, groups, s);
+}
+
+}  // namespace okt
+
+extern "C" {
+
+size_t okt_residual_norm_workspace_bytes(uint64_t rows, uint32_t width, uint64_t rows_per_gate) {
+    if (width == 0 || width > okt::NORM_MAX_WIDTH || rows > okt::NORM_MAX_ROWS) return 0;
+    const size_t need = okt::norm_ws_bytes(rows, width, rows_per_gate);
+    return need ? need : 256;
+}
+
+int okt_residual_norm_forward(const okt_residual_norm* op, const void* d_u, const void* d_x, void* d_h_out, void* d_y_out,
+                              float* d_stats_out, void* stream) {
+    using namespace okt;
+    NormArgs a;
+    if (!norm_args(op, a)) return OKT_ERR_INVALID_ARG;
+    if (a.rows == 0) return OKT_OK;
+    if (!d_u || !d_x || (!d_h_out && !a.pre_w) || (a.pre_w && !d_y_out) || (!a.pre_w && d_y_out)) return OKT_ERR_INVALID_ARG;
+    const size_t e = dtype_bytes(op->dtype);
+    for (const void* p : {d_u, d_x, (const void*)d_h_out, (const void*)d_y_out})
+        if (!aligned(p, e)) return OKT_ERR_INVALID_ARG;
+    if (!aligned(d_stats_out, 16)) return OKT_ERR_INVALID_ARG;
+    a.stats = (float4*)d_stats_out;
+    const uint64_t at_once = rows_at_once(norm_shape(a.width));
+    const uint64_t want = (a.rows + at_once - 1) / at_once, most = (uint64_t)device_cus() * 8;
+    timing_before((hipStream_t)stream);
+    launch_norm_type(op->dtype, a, {d_u, d_x, nullptr, nullptr, nullptr, d_h_out, d_y_out, nullptr, nullptr}, false,
+                     (unsigned)(want < most ? want : most), (hipStream_t)stream);
+    timing_after((hipStream_t)stream);
+    return launch_status();
+}
+
+int okt_residual_norm_backward(const okt_residual_norm* op, const void* d_u, const void* d_h, const float* d_stats,
+                               const void* d_dh, const void* d_dy, void* d_dx_out, void* d_du_out, float* d_dpost_weight_out,
+                               float* d_dpost_bias_out, float* d_dgate_out, float* d_dpre_weight_out, float* d_dpre_bias_out,
+                               void* d_ws, size_t ws_bytes, void* stream) {
+    using namespace okt;
+    NormArgs a;
+    if (!norm_args(op, a)) return OKT_ERR_INVALID_ARG;
+    if ((d_dpost_weight_out && !a.post_w) || (d_dpost_bias_out && !a.post_b) || (d_dgate_out && !a.gate) ||
+        (d_dpre_weight_out && !a.pre_w) || (d_dpre_bias_out && !a.pre_b)) return OKT_ERR_INVALID_ARG;
+    for (const float* p : {d_dpost_weight_out, d_dpost_bias_out, d_dgate_out, d_dpre_weight_out, d_dpre_bias_out})
+        if (!aligned(p, 4)) return OKT_ERR_INVALID_ARG;
+    const bool all = a.post_w || a.gate;
+    if (a.rows) {
+        if (!d_dx_out || !d_du_out || !d_stats || !aligned(d_stats, 16) || (all && !d_u)) return OKT_ERR_INVALID_ARG;
+        if ((a.pre_w && (!d_h || !d_dy)) || (!a.pre_w && (d_dy || !d_dh))) return OKT_ERR_INVALID_ARG;
+        const size_t e = dtype_bytes(op->dtype);
+        for (const void* p : {d_u, d_h, d_dh, d_dy, (const void*)d_dx_out, (const void*)d_du_out})
+            if (!aligned(p, e)) return OKT_ERR_INVALID_ARG;
+    }
+    const NormPlan plan = norm_plan(a.rows, a.width, a.rows_per_gate);
+    if (!d_ws || !aligned(d_ws, 256) || ws_bytes < norm_ws_bytes(a.rows, a.width, a.rows_per_gate)) return OKT_ERR_WORKSPACE;
+    a.stats = (float4*)d_stats;
+    a.partial = (float*)d_ws;
+    a.dgate = d_dgate_out;
+    a.chunk = plan.chunk;
+    a.groups = plan.groups;
+    a.parts = plan.parts;
+    const hipStream_t s = (hipStream_t)stream;
+    if (a.rows) {
+        timing_before(s);
+        launch_norm_type(op->dtype, a, {d_u, nullptr, d_h, d_dh, d_dy, nullptr, nullptr, d_dx_out, d_du_out}, true,
+                         (unsigned)plan.groups, s);
+        timing_after(s);
+    }
+    NormOutputs out = {{d_dpre_weight_out, d_dpre_bias_out, d_dpost_weight_out, d_dpost_bias_out}};
+    const bool gates = d_dgate_out && plan.parts != 1;
+    if (out.to[0] || out.to[1] || out.to[2] || out.to[3] || gates)
+        hipLaunchKernelGGL(norm_add_kernel, dim3((a.width + WAVE - 1) / WAVE, 4 + (gates ? (unsigned)plan.gates : 0)),
+                           dim3(NORM_ADD_BLOCK), 0, s, out, d_dgate_out, (const float*)d_ws, plan.groups, plan.parts, a.width);
+    return launch_status();
+}
+
+}  // extern "C"
