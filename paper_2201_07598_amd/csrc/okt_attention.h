@@ -46,6 +46,23 @@ __device__ __forceinline__ constexpr uint32_t row_of_slot(uint32_t s) {
 
 // ------------------------------------------------------------------ tiles of rows in LDS
 
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+
+constexpr uint32_t OUTSIDE = 0xffff0000u;     // an offset that no buffer reaches
+
+// 16 bytes a lane from `buffer` at its byte offset to LDS, lane after lane from `lds` on; 0
+// where the offset is outside the buffer.  Written out because the compiler, which cannot
+// tell the tile that is being filled from the one that is read, would wait for it before the next read
+// of LDS; fetched() waits where it has to be.
+__device__ __forceinline__ void fetch_to_lds(uint32_t lds, uint32_t offset, i32x4 buffer) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+                 :: "s"(lds), "v"(offset), "s"(buffer) : "memory");
+}
+
+__device__ __forceinline__ uint32_t lds_address(const void* p) {
+    return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void*)p;
+}
+
 // ROWS rows of DIM elements, row order by slots, DIM / 8 chunks of 16 bytes a row.  Chunk c of slot s lies
 // at place c ^ turn(s): sixteen neighbouring slots then read one chunk from sixteen
 // different groups of banks (A operands, row by row), and the eight slots that a
@@ -60,29 +77,39 @@ struct RowTile {
         return DIM == 64 ? ((s >> 1 & 1) << 2) | (s >> 2 & 3) : ((s & 3) << 2) | (s >> 2 & 3);
     }
 
-    // Fetches rows first .. first + ROWS - 1 of a tensor straight into LDS; rows outside
-    // [lo, hi] are replaced by the nearest inside, so that what lies there is never looked
-    // at and what is multiplied by a masked 0 is finite.  Chunks past head_dim are not
-    // written (they hold the zeros that clear() left).
-    static __device__ __forceinline__ void fetch(char* tile, const T* base, uint64_t stride, int64_t first, int64_t lo,
-                                                 int64_t hi, uint32_t head_dim) {
-        const uint32_t wave = uniform(threadIdx.x / WAVE), lane = threadIdx.x % WAVE;
+    // What a thread fetches of every tile, in bytes from the tile's first row; places past
+    // head_dim lie beyond any tensor and read as 0.
+    struct Places {
+        uint32_t at[LOADS];
+        __device__ __forceinline__ Places(uint32_t row_bytes, uint32_t head_dim) {
 #pragma unroll
-        for (int i = 0; i < LOADS; ++i) {
-            const uint32_t at = (i * (THREADS / WAVE) + wave) * WAVE;           // of the wave's first chunk
-            const uint32_t slot = (at + lane) / CHUNKS, place = (at + lane) % CHUNKS;
-            const uint32_t chunk = place ^ turn(slot);
-            int64_t row = first + row_of_slot(slot);
-            row = row < lo ? lo : row > hi ? hi : row;
-            if (DIM == (int)head_dim || chunk * 8 < head_dim)
-                __builtin_amdgcn_global_load_lds(
-                    (const __attribute__((address_space(1))) void*)(base + row * stride + chunk * 8),
-                    (__attribute__((address_space(3))) void*)(tile + at * 16), 16, 0, 0);
+            for (int i = 0; i < LOADS; ++i) {
+                const uint32_t n = i * THREADS + threadIdx.x, slot = n / CHUNKS, chunk = n % CHUNKS ^ turn(slot);
+                at[i] = DIM == (int)head_dim || chunk * 8 < head_dim ? row_of_slot(slot) * row_bytes + chunk * 16 : OUTSIDE;
+            }
         }
-    }
+    };
 
-    static __device__ __forceinline__ void clear(char* tile) {
-        for (int i = threadIdx.x; i < BYTES / 16; i += THREADS) reinterpret_cast<float4*>(tile)[i] = make_float4(0, 0, 0, 0);
+    // Fetches rows first .. first + ROWS - 1 of a tensor (its row 0 at `base`, `count` rows)
+    // straight into LDS.  The buffer's bounds end with the last row, so that rows past it
+    // arrive as zeros whatever lies there, as do rows before `lo`.
+    static __device__ __forceinline__ void fetch(uint32_t tile, const T* base, uint32_t row_bytes, const Places& p, int first,
+                                                 int lo, int count, uint32_t head_dim) {
+        const uint32_t wave = uniform(threadIdx.x / WAVE);
+        const uint64_t from = (uint64_t)base + (uint64_t)first * row_bytes;
+        const uint64_t bytes = (uint64_t)(count - first - 1) * row_bytes + head_dim * 2;
+        const i32x4 buffer = {(int)uniform((uint32_t)from), (int)uniform((uint32_t)(from >> 32)),
+                              (int)(bytes < OUTSIDE ? uniform((uint32_t)bytes) : OUTSIDE), 0x00020000};
+        if (first >= lo) {
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i) fetch_to_lds(tile + (i * (THREADS / WAVE) + wave) * 1024, p.at[i], buffer);
+        } else {
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i) {
+                const bool before = first + (int)row_of_slot((i * THREADS + threadIdx.x) / CHUNKS) < lo;
+                fetch_to_lds(tile + (i * (THREADS / WAVE) + wave) * 1024, before ? OUTSIDE : p.at[i], buffer);
+            }
+        }
     }
 
     // A operand: rows of the 32-row tile at slot0, columns 16 step .. + 15.
@@ -145,6 +172,14 @@ __device__ __forceinline__ void store_row(T* row, const f32x16 (&c)[TILES], floa
             const f32x4 v = {c[dt][4 * a] * scale, c[dt][4 * a + 1] * scale, c[dt][4 * a + 2] * scale, c[dt][4 * a + 3] * scale};
             if (d < head_dim) *reinterpret_cast<four*>(row + d) = __builtin_convertvector(v, four);
         }
+}
+
+// Workgroups are dealt to the eight dies in turn.  Gives each die a run of neighbouring
+// places, so that the blocks of one head, which read the same keys, share an L2.
+__device__ __forceinline__ uint32_t near_place(uint32_t block, uint32_t blocks) {
+    constexpr uint32_t DIES = 8;
+    const uint32_t die = block % DIES, each = blocks / DIES, more = blocks % DIES;
+    return die * each + (die < more ? die : more) + block / DIES;
 }
 
 // ------------------------------------------------------------------ the dropout mask

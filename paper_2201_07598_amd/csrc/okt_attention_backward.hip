@@ -21,20 +21,21 @@ constexpr int BWD_TILE = 64;                          // keys or queries that pa
 __device__ __forceinline__ float lse_log2(float lse) { return lse == -INFINITY ? INFINITY : lse * 1.44269504088896f; }
 
 template <typename T, int DIM, bool DROP>
-__global__ __launch_bounds__(BWD_THREADS) void attention_backward_queries_kernel(
+__global__ __launch_bounds__(BWD_THREADS, DIM == 64 ? 2 : 1) void attention_backward_queries_kernel(
     AttentionArgs a, const T* q, const T* k, const T* v, const T* o, const float* lse, const T* d_o, T* dq, float* rows_d,
     uint32_t blocks) {
     using Tile = RowTile<T, DIM, BWD_TILE, BWD_THREADS>;
     __shared__ __attribute__((aligned(1024))) char shared[4 * Tile::BYTES];
-    const uint32_t plane = blockIdx.x / blocks, b = plane / a.heads, h = plane % a.heads, kv = h / a.group;
+    const uint32_t place = near_place(blockIdx.x, gridDim.x), plane = place / blocks;
+    const uint32_t b = plane / a.heads, h = plane % a.heads, kv = h / a.group;
     const uint32_t wave = uniform(threadIdx.x / WAVE), lane = threadIdx.x % WAVE;
     const int ql = sequence_length(a.q_lens, b, a.q_len), kl = sequence_length(a.k_lens, b, a.k_len);
-    const int q0 = blockIdx.x % blocks * BWD_ROWS, w0 = q0 + 32 * (int)wave, i = w0 + (int)(lane % 32);
-    const int past = a.causal ? kl - ql + 1 : 0;
-    const auto seen = [&](int query) { const int n = query + past; return !a.causal || n > kl ? kl : n < 0 ? 0 : n; };
-    const int last = q0 + BWD_ROWS < ql ? q0 + BWD_ROWS - 1 : ql - 1;
-    const int keys = q0 < ql ? seen(last) : 0;
-    const int mine = i < ql ? seen(i) : 0, wave_least = w0 + 31 < ql ? seen(w0) : 0;
+    const int q0 = (blocks - 1 - place % blocks) * BWD_ROWS, w0 = q0 + 32 * (int)wave, i = w0 + (int)(lane % 32);
+    const int past = kl - ql + 1;
+    const auto seen = [&](int query) { const int n = query + past; return query >= ql ? 0 : !a.causal || n > kl ? kl : n < 0 ? 0 : n; };
+    const int keys = q0 < ql ? seen(q0 + BWD_ROWS < ql ? q0 + BWD_ROWS - 1 : ql - 1) : 0;
+    const int mine = seen(i), wave_least = w0 + 31 < ql ? seen(w0) : 0;
+    const int wave_most = w0 < ql ? seen(w0 + 32 < ql ? w0 + 31 : ql - 1) : 0;
 
     f32x16 acc[DIM / 32];
 #pragma unroll
@@ -46,12 +47,11 @@ __global__ __launch_bounds__(BWD_THREADS) void attention_backward_queries_kernel
         const T* q_row = q + b * a.q.batch + row * a.q.row + h * a.q.head;
         const T* do_row = d_o + b * a.d_o.batch + row * a.d_o.row + h * a.d_o.head;
         const T* o_row = o + b * a.o.batch + row * a.o.row + h * a.o.head;
-        if (a.head_dim != DIM) {
-            for (int n = 0; n < 4; ++n) Tile::clear(shared + n * Tile::BYTES);
-            __syncthreads();
-        }
-        Tile::fetch(shared, kb, a.k.row, 0, 0, kl - 1, a.head_dim);
-        Tile::fetch(shared + Tile::BYTES, vb, a.v.row, 0, 0, kl - 1, a.head_dim);
+        const uint32_t k_row = (uint32_t)a.k.row * 2, v_row = (uint32_t)a.v.row * 2;
+        const typename Tile::Places k_at(k_row, a.head_dim), v_at(v_row, a.head_dim);
+        const uint32_t lds = lds_address(shared);
+        Tile::fetch(lds, kb, k_row, k_at, 0, 0, kl, a.head_dim);
+        Tile::fetch(lds + Tile::BYTES, vb, v_row, v_at, 0, 0, kl, a.head_dim);
         frag<T> qf[DIM / 16], df[DIM / 16];
         float sum = 0.0f;
 #pragma unroll
@@ -63,7 +63,6 @@ __global__ __launch_bounds__(BWD_THREADS) void attention_backward_queries_kernel
             for (int e = 0; e < 8; ++e) sum = __builtin_fmaf(x[e], y[e], sum);
         }
         sum = sum_halves(sum);
-        if (lane < 32 && i < ql) rows_d[(uint64_t)plane * a.q_len + i] = sum;
         const float base = lse_log2(lse[(uint64_t)plane * a.q_len + row]);
         RandomKey key = {0, 0};
         if (DROP) key = random_key(a.seed);
@@ -73,10 +72,11 @@ __global__ __launch_bounds__(BWD_THREADS) void attention_backward_queries_kernel
             const char* kt = shared + turn * 2 * Tile::BYTES;
             const char* vt = kt + Tile::BYTES;
             if (key0 + BWD_TILE < keys) {
-                char* next = shared + (turn ^ 1) * 2 * Tile::BYTES;
-                Tile::fetch(next, kb, a.k.row, key0 + BWD_TILE, 0, kl - 1, a.head_dim);
-                Tile::fetch(next + Tile::BYTES, vb, a.v.row, key0 + BWD_TILE, 0, kl - 1, a.head_dim);
+                const uint32_t next = lds + (turn ^ 1) * 2 * Tile::BYTES;
+                Tile::fetch(next, kb, k_row, k_at, key0 + BWD_TILE, 0, kl, a.head_dim);
+                Tile::fetch(next + Tile::BYTES, vb, v_row, v_at, key0 + BWD_TILE, 0, kl, a.head_dim);
             }
+            if (key0 >= wave_most) continue;
             const bool masked = key0 + BWD_TILE > wave_least;
 #pragma unroll
             for (int n = 0; n < BWD_TILE / 32; ++n) {
@@ -93,11 +93,23 @@ __global__ __launch_bounds__(BWD_THREADS) void attention_backward_queries_kernel
                     for (int r = 0; r < 16; ++r) dp[r] = (w[r] & mask) < bar ? dp[r] * a.drop.scale : 0.0f;
                 }
 #pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], a.scale_log2, -base));
-                    if (masked) p = key0 + 32 * n + 16 * (int)(lane / 32) + r < mine ? p : 0.0f;
-                    s[r] = p * (dp[r] - sum);
+                for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], a.scale_log2, -base));
+                if (masked) {
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) s[r] = key0 + 32 * n + 16 * (int)(lane / 32) + r < mine ? s[r] : 0.0f;
                 }
+                if (n == 0 && key0 == 0) {
+                    // A row that sees no key past this tile takes D from what it has here, sum_j p dP: few
+                    // probabilities are large ones, and the rounding of o would show in dP - D.
+                    float few = 0.0f;
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) few = __builtin_fmaf(s[r], dp[r], few);
+                    few = sum_halves(few);
+                    sum = mine <= 32 ? few : sum;
+                    if (lane < 32 && i < ql) rows_d[(uint64_t)plane * a.q_len + i] = sum;
+                }
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[r] *= dp[r] - sum;
 #pragma unroll
                 for (int t = 0; t < 2; ++t) {
                     const frag<T> ds = to_operand<T>(s, t);
@@ -118,20 +130,21 @@ __global__ __launch_bounds__(BWD_THREADS) void attention_backward_queries_kernel
 }
 
 template <typename T, int DIM, bool DROP>
-__global__ __launch_bounds__(BWD_THREADS) void attention_backward_keys_kernel(
+__global__ __launch_bounds__(BWD_THREADS, DIM == 64 ? 2 : 1) void attention_backward_keys_kernel(
     AttentionArgs a, const T* q, const T* k, const T* v, const float* lse, const T* d_o, const float* rows_d, T* dk, T* dv,
     uint32_t blocks) {
     using Tile = RowTile<T, DIM, BWD_TILE, BWD_THREADS>;
     __shared__ __attribute__((aligned(1024))) char shared[4 * Tile::BYTES];
     __shared__ float2 rows_of[2][BWD_TILE];                    // log-sum-exp and D of the tile's rows
-    const uint32_t b = blockIdx.x / blocks / a.kv_heads, kv = blockIdx.x / blocks % a.kv_heads;
+    const uint32_t place = near_place(blockIdx.x, gridDim.x), b = place / blocks / a.kv_heads, kv = place / blocks % a.kv_heads;
     const uint32_t wave = uniform(threadIdx.x / WAVE), lane = threadIdx.x % WAVE;
     const int ql = sequence_length(a.q_lens, b, a.q_len), kl = sequence_length(a.k_lens, b, a.k_len);
-    const int k0 = blockIdx.x % blocks * BWD_ROWS, w0 = k0 + 32 * (int)wave, j = w0 + (int)(lane % 32);
+    const int k0 = place % blocks * BWD_ROWS, w0 = k0 + 32 * (int)wave, j = w0 + (int)(lane % 32);
     // the first query that sees key j, and the first that sees any
     const auto first_for = [&](int key) { const int n = a.causal ? key - (kl - ql) : 0; return n < 0 ? 0 : n; };
     const int lo = first_for(0), begin = first_for(k0) / BWD_TILE * BWD_TILE;
-    const int mine = j < kl ? first_for(j) : ql, wave_most = w0 + 31 < kl ? first_for(w0 + 31) : ql;
+    const int mine = j < kl ? first_for(j) : ql;
+    const int wave_least = w0 < kl ? first_for(w0) : ql + BWD_TILE, wave_most = w0 + 31 < kl ? first_for(w0 + 31) : ql;
     const int tiles = k0 < kl && begin < ql ? (ql - begin + BWD_TILE - 1) / BWD_TILE : 0;
 
     f32x16 dkacc[DIM / 32], dvacc[DIM / 32];
@@ -149,16 +162,14 @@ __global__ __launch_bounds__(BWD_THREADS) void attention_backward_keys_kernel(
         }
         RandomKey key = {0, 0};
         if (DROP) key = random_key(a.seed);
-        if (a.head_dim != DIM) {
-            for (int n = 0; n < 4; ++n) Tile::clear(shared + n * Tile::BYTES);
-            __syncthreads();
-        }
+        const uint32_t q_row = (uint32_t)a.q.row * 2, do_row = (uint32_t)a.d_o.row * 2, lds = lds_address(shared);
+        const typename Tile::Places q_at(q_row, a.head_dim), do_at(do_row, a.head_dim);
         const auto fetch = [&](int it, int turn) {
             const uint32_t h = kv * a.group + it / tiles;
             const int first = begin + it % tiles * BWD_TILE;
-            char* to = shared + turn * 2 * Tile::BYTES;
-            Tile::fetch(to, q + b * a.q.batch + h * a.q.head, a.q.row, first, lo, ql - 1, a.head_dim);
-            Tile::fetch(to + Tile::BYTES, d_o + b * a.d_o.batch + h * a.d_o.head, a.d_o.row, first, lo, ql - 1, a.head_dim);
+            const uint32_t to = lds + turn * 2 * Tile::BYTES;
+            Tile::fetch(to, q + b * a.q.batch + h * a.q.head, q_row, q_at, first, lo, ql, a.head_dim);
+            Tile::fetch(to + Tile::BYTES, d_o + b * a.d_o.batch + h * a.d_o.head, do_row, do_at, first, lo, ql, a.head_dim);
             if (threadIdx.x < BWD_TILE) {
                 const int i = first + (int)threadIdx.x;
                 const uint64_t at = ((uint64_t)b * a.heads + h) * a.q_len + (i < lo ? lo : i > ql - 1 ? ql - 1 : i);
@@ -174,6 +185,7 @@ __global__ __launch_bounds__(BWD_THREADS) void attention_backward_keys_kernel(
             if (it + 1 < steps) fetch(it + 1, turn ^ 1);
             const uint32_t plane = b * a.heads + kv * a.group + it / tiles;
             const int query0 = begin + it % tiles * BWD_TILE;
+            if (query0 + BWD_TILE <= wave_least) continue;
             const bool masked = query0 < wave_most || query0 + BWD_TILE > ql;
 #pragma unroll
             for (int n = 0; n < BWD_TILE / 32; ++n) {

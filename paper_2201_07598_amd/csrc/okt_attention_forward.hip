@@ -14,51 +14,51 @@ constexpr int FWD_QUERIES = FWD_THREADS / WAVE * 32;
 constexpr int FWD_KEYS = 64;
 
 template <typename T, int DIM, bool DROP>
-__global__ __launch_bounds__(FWD_THREADS) void attention_forward_kernel(AttentionArgs a, const T* q, const T* k, const T* v,
-                                                                        T* o, float* lse, uint32_t blocks) {
+__global__ __launch_bounds__(FWD_THREADS, 2) void attention_forward_kernel(AttentionArgs a, const T* q, const T* k, const T* v,
+                                                                           T* o, float* lse, uint32_t blocks) {
     using Tile = RowTile<T, DIM, FWD_KEYS, FWD_THREADS>;
     __shared__ __attribute__((aligned(1024))) char shared[4 * Tile::BYTES];
-    const uint32_t plane = blockIdx.x / blocks, b = plane / a.heads, h = plane % a.heads, kv = h / a.group;
+    const uint32_t place = near_place(blockIdx.x, gridDim.x), plane = place / blocks;
+    const uint32_t b = plane / a.heads, h = plane % a.heads, kv = h / a.group;
     const uint32_t wave = uniform(threadIdx.x / WAVE), lane = threadIdx.x % WAVE;
     const int ql = sequence_length(a.q_lens, b, a.q_len), kl = sequence_length(a.k_lens, b, a.k_len);
-    const int q0 = blockIdx.x % blocks * FWD_QUERIES, w0 = q0 + 32 * (int)wave, i = w0 + (int)(lane % 32);
-    T* out = o + b * a.o.batch + (uint64_t)i * a.o.row + h * a.o.head;
+    const int q0 = (blocks - 1 - place % blocks) * FWD_QUERIES, w0 = q0 + 32 * (int)wave, i = w0 + (int)(lane % 32);
 
-    // keys that the last query of the workgroup, and that the first and last of the wave see
-    const int past = a.causal ? kl - ql + 1 : 0;
-    const auto seen = [&](int query) { const int n = query + past; return !a.causal || n > kl ? kl : n < 0 ? 0 : n; };
-    const int last = q0 + FWD_QUERIES < ql ? q0 + FWD_QUERIES - 1 : ql - 1;
-    const int keys = q0 < ql ? seen(last) : 0;
-    const int mine = i < ql ? seen(i) : 0, wave_least = w0 + 31 < ql ? seen(w0) : 0;
+    // keys that a query sees; the most of the workgroup's queries, the least and most of the wave's
+    const int past = kl - ql + 1;
+    const auto seen = [&](int query) { const int n = query + past; return query >= ql ? 0 : !a.causal || n > kl ? kl : n < 0 ? 0 : n; };
+    const int keys = q0 < ql ? seen(q0 + FWD_QUERIES < ql ? q0 + FWD_QUERIES - 1 : ql - 1) : 0;
+    const int mine = seen(i), wave_least = w0 + 31 < ql ? seen(w0) : 0;
+    const int wave_most = w0 < ql ? seen(w0 + 32 < ql ? w0 + 31 : ql - 1) : 0;
 
-    frag<T> qf[DIM / 16];
     f32x16 acc[DIM / 32];
-    float top = -INFINITY, total = 0.0f;
+    float top = -INFINITY, total = 0.0f;          // of the scores times scale_log2
 #pragma unroll
     for (int d = 0; d < DIM / 32; ++d) acc[d] = 0.0f;
     if (keys > 0) {
         const T* kb = k + b * a.k.batch + kv * a.k.head;
         const T* vb = v + b * a.v.batch + kv * a.v.head;
+        const uint32_t k_row = (uint32_t)a.k.row * 2, v_row = (uint32_t)a.v.row * 2;
+        const typename Tile::Places k_at(k_row, a.head_dim), v_at(v_row, a.head_dim);
+        const uint32_t lds = lds_address(shared);
+        Tile::fetch(lds, kb, k_row, k_at, 0, 0, kl, a.head_dim);
+        Tile::fetch(lds + Tile::BYTES, vb, v_row, v_at, 0, 0, kl, a.head_dim);
         const T* qrow = q + b * a.q.batch + (uint64_t)(i < ql ? i : ql - 1) * a.q.row + h * a.q.head;
+        frag<T> qf[DIM / 16];
 #pragma unroll
         for (int s = 0; s < DIM / 16; ++s) qf[s] = row_operand(qrow, s, a.head_dim);
         RandomKey key = {0, 0};
         if (DROP) key = random_key(a.seed);
-        if (a.head_dim != DIM) {
-            for (int n = 0; n < 4; ++n) Tile::clear(shared + n * Tile::BYTES);
-            __syncthreads();
-        }
-        Tile::fetch(shared, kb, a.k.row, 0, 0, kl - 1, a.head_dim);
-        Tile::fetch(shared + Tile::BYTES, vb, a.v.row, 0, 0, kl - 1, a.head_dim);
         for (int key0 = 0, turn = 0; key0 < keys; key0 += FWD_KEYS, turn ^= 1) {
             fetched();
             const char* kt = shared + turn * 2 * Tile::BYTES;
             const char* vt = kt + Tile::BYTES;
             if (key0 + FWD_KEYS < keys) {
-                char* next = shared + (turn ^ 1) * 2 * Tile::BYTES;
-                Tile::fetch(next, kb, a.k.row, key0 + FWD_KEYS, 0, kl - 1, a.head_dim);
-                Tile::fetch(next + Tile::BYTES, vb, a.v.row, key0 + FWD_KEYS, 0, kl - 1, a.head_dim);
+                const uint32_t next = lds + (turn ^ 1) * 2 * Tile::BYTES;
+                Tile::fetch(next, kb, k_row, k_at, key0 + FWD_KEYS, 0, kl, a.head_dim);
+                Tile::fetch(next + Tile::BYTES, vb, v_row, v_at, key0 + FWD_KEYS, 0, kl, a.head_dim);
             }
+            if (key0 >= wave_most) continue;
             f32x16 s[FWD_KEYS / 32];
 #pragma unroll
             for (int n = 0; n < FWD_KEYS / 32; ++n) {
@@ -66,33 +66,36 @@ __global__ __launch_bounds__(FWD_THREADS) void attention_forward_kernel(Attentio
 #pragma unroll
                 for (int e = 0; e < DIM / 16; ++e) s[n] = mfma(Tile::rows(kt, 32 * n, e), qf[e], s[n]);
             }
-            float most = -INFINITY;
             if (key0 + FWD_KEYS > wave_least) {                // some of the tile is hidden from some lane
 #pragma unroll
                 for (int n = 0; n < FWD_KEYS / 32; ++n)
 #pragma unroll
                     for (int r = 0; r < 16; ++r)
-                        s[n][r] = key0 + 32 * n + 16 * (int)(lane / 32) + r < mine ? s[n][r] * a.scale_log2 : -INFINITY;
-            } else {
-#pragma unroll
-                for (int n = 0; n < FWD_KEYS / 32; ++n) s[n] *= a.scale_log2;
+                        s[n][r] = key0 + 32 * n + 16 * (int)(lane / 32) + r < mine ? s[n][r] : -INFINITY;
             }
+            float most = s[0][0];
 #pragma unroll
             for (int n = 0; n < FWD_KEYS / 32; ++n)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) most = fmaxf(most, s[n][r]);
-            most = fmaxf(top, max_halves(most));
-            const float base = most == -INFINITY ? 0.0f : most;
-            const float fade = __builtin_amdgcn_exp2f(top - base);
-            top = most;
-            total *= fade;
+            most = max_halves(most) * a.scale_log2;
+            // Sums are kept relative to `top`, which follows the maximum in steps: as long as no
+            // lane's has grown by more than a factor of 2^8, which changes neither the relative precision of
+            // a probability nor of a sum, there is nothing to rescale.
+            if (__any(most > top + 8.0f)) {
+                most = fmaxf(top, most);
+                const float fade = __builtin_amdgcn_exp2f(top - (most == -INFINITY ? 0.0f : most));
+                top = most;
+                total *= fade;
 #pragma unroll
-            for (int d = 0; d < DIM / 32; ++d) acc[d] *= fade;
+                for (int d = 0; d < DIM / 32; ++d) acc[d] *= fade;
+            }
+            const float base = top == -INFINITY ? 0.0f : top;
 #pragma unroll
             for (int n = 0; n < FWD_KEYS / 32; ++n) {
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
-                    s[n][r] = __builtin_amdgcn_exp2f(s[n][r] - base);
+                    s[n][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[n][r], a.scale_log2, -base));
                     total += s[n][r];
                 }
                 if (DROP) {
@@ -113,7 +116,7 @@ __global__ __launch_bounds__(FWD_THREADS) void attention_forward_kernel(Attentio
     }
     total = sum_halves(total);
     if (i < (int)a.q_len) {
-        store_row(out, acc, mine > 0 ? a.drop.scale / total : 0.0f, a.head_dim);
+        store_row(o + b * a.o.batch + (uint64_t)i * a.o.row + h * a.o.head, acc, mine > 0 ? a.drop.scale / total : 0.0f, a.head_dim);
         if (lse && lane < 32)
             lse[(uint64_t)plane * a.q_len + i] = mine > 0 ? (top + __builtin_amdgcn_logf(total)) * 0.693147180559945f : -INFINITY;
     }
@@ -131,7 +134,7 @@ static bool strides(const uint64_t (&s)[3], Strides& to) {
     to = {s[0], s[1], s[2]};
     for (uint64_t n : s)
         if (n % 8 || n > (1ull << 40)) return false;
-    return true;
+    return s[1] <= (1u << 24);                   // so that a tile's offsets fit 32 bits
 }
 
 bool attention_args(const okt_attention* op, bool backward, AttentionArgs& a) {
