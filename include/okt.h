@@ -565,7 +565,7 @@ typedef enum okt_norm_kind { OKT_NORM_LAYER = 0, OKT_NORM_RMS = 1 } okt_norm_kin
  */
 typedef struct okt_residual_norm {
     uint64_t rows;                /* at most 2^40 */
-    uint32_t width;               /* 1 to 16384 */
+    uint32_t width;               /* 8 to 16384 */
     int32_t dtype;                /* of u, x, h, y and their gradients */
     int32_t kind;                 /* okt_norm_kind of both norms */
     float eps;                    /* >= 0 */

@@ -44,7 +44,10 @@ __global__ __launch_bounds__(DROP_BLOCK) void dropout_kernel(const T* x, T* y, u
             store_eight(y + group * 8, drop_eight<T>(load_eight(x + group * 8), group, key, site, rule));
         } else if (group * 8 < n) {
             const int count = (int)(n - group * 8);
-            store_some(y + group * 8, drop_eight<T>(load_some(x + group * 8, count, 0.0f), group, key, site, rule), count);
+            f32x8 v = 0.0f;
+            if (n >= 8) v = __builtin_convertvector(skip_elements<T>(raw_eight(x + n - 8), 8 - count), f32x8);
+            else for (int i = 0; i < count; ++i) v[i] = (float)x[i];
+            store_some(y + group * 8, drop_eight<T>(v, group, key, site, rule), count);
         }
     }
 }

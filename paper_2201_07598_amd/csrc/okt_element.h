@@ -32,15 +32,40 @@ __device__ __forceinline__ void store_eight(T* p, f32x8 v) {
     reinterpret_cast<typename Eight<T>::any*>(p)->v = __builtin_convertvector(v, typename Eight<T>::vec);
 }
 
-// The first `count` of them; the rest reads as `rest` and is not written.
+// Eight elements as they lie in memory.
 template <typename T>
-__device__ __forceinline__ f32x8 load_some(const T* p, int count, float rest) {
-    f32x8 v;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = i < count ? (float)p[i] : rest;
-    return v;
+__device__ __forceinline__ typename Eight<T>::vec raw_eight(const T* p) {
+    return reinterpret_cast<const typename Eight<T>::any*>(p)->v;
 }
 
+// Drops the first `skip` (1 or more) of eight elements, moves the rest to the front and puts zeros
+// behind.  The ragged end of a row is the last eight elements of the row moved so: a
+// load for each element, merged one by one, waits for memory each time.
+template <typename T>
+__device__ __forceinline__ typename Eight<T>::vec skip_elements(typename Eight<T>::vec v, uint32_t skip) {
+    constexpr int WORDS = 2 * sizeof(T), PER = 4 / sizeof(T);          // words, elements of a word
+    typedef uint32_t words __attribute__((ext_vector_type(WORDS)));
+    words w = __builtin_bit_cast(words, v);
+#pragma unroll
+    for (int step = 4; step >= PER; step >>= 1)
+#pragma unroll
+        for (int i = 0; i < WORDS; ++i) {
+            const uint32_t from = i + step / PER < WORDS ? w[i + step / PER < WORDS ? i + step / PER : 0] : 0;
+            w[i] = skip & step ? from : w[i];
+        }
+    if (PER == 2) {
+#pragma unroll
+        for (int i = 0; i < WORDS; ++i) {
+            const uint32_t from = (w[i] >> 16) | (i + 1 < WORDS ? w[i + 1 < WORDS ? i + 1 : 0] << 16 : 0);
+            w[i] = skip & 1 ? from : w[i];
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < WORDS; ++i) w[i] = skip >= 8 ? 0 : w[i];
+    return __builtin_bit_cast(typename Eight<T>::vec, w);
+}
+
+// Writes the first `count` of them.
 template <typename T>
 __device__ __forceinline__ void store_some(T* p, f32x8 v, int count) {
 #pragma unroll

@@ -26,33 +26,34 @@ namespace okt {
 
 // ------------------------------------------------------------------ sizes (host)
 
-constexpr uint32_t NORM_MAX_WIDTH = 16384;
+constexpr uint32_t NORM_MIN_WIDTH = 8, NORM_MAX_WIDTH = 16384;
 constexpr uint64_t NORM_MAX_ROWS = 1ull << 40;
 constexpr uint32_t NORM_BACKWARD_GROUPS = 512;     // workgroups aimed at: two to a CU
 constexpr uint32_t NORM_SUMS = 5;                  // pre w, pre b, post w, post b, gate
 
+// Threads that hold a row, eight columns each `vecs` times over.  One wave where it can: its
+// sums need no barrier, and four rows of four waves are on their way together.  The kernel of a gated block
+// holds twice the sums, and two groups of them cost it all but one wave of a SIMD: it takes
+// a second wave above 512 columns instead (4099 rows of 2500 at two groups 134 us, at one
+// and 320 threads 37 us).
 struct NormShape { uint32_t lanes, vecs; };
 
-// The fewest threads that hold a row of 16 columns each; up to 512 columns of 8.
-static NormShape norm_shape(uint32_t width) {
-    if (width <= 512) return {64, 1};
-    if (width <= 1024) return {64, 2};
-    if (width <= 2048) return {256, 1};
-    if (width <= 4096) return {256, 2};
-    if (width <= 8192) return {512, 2};
+static NormShape norm_shape(uint32_t width, bool gated_backward) {
+    if (width <= 512) return {WAVE, 1};
+    if (width <= 1024 && !gated_backward) return {WAVE, 2};
+    if (width <= 8192) return {(width + WAVE * 8 - 1) / (WAVE * 8) * WAVE, 1};
     return {1024, 2};
 }
 
-static uint32_t rows_at_once(NormShape s) { return s.lanes == 64 ? 4 : 1; }
+static uint32_t rows_at_once(NormShape s) { return s.lanes == WAVE ? 4 : 1; }
 
 // How the backward pass deals out rows.  A workgroup owns `chunk` rows that either are
 // whole gates' rows (parts == 1: it writes their dgate itself) or lie within one gate
 // (parts workgroups to a gate, whose partial sums the second launch adds).
 struct NormPlan { uint64_t chunk, rows_per_gate, gates, groups; uint32_t parts; };
 
-static NormPlan norm_plan(uint64_t rows, uint32_t width, uint64_t rows_per_gate) {
+static NormPlan norm_plan(uint64_t rows, uint64_t rows_per_gate, uint32_t at_once) {
     NormPlan p;
-    const uint32_t at_once = rows_at_once(norm_shape(width));
     p.rows_per_gate = rows_per_gate == 0 || rows_per_gate > rows ? rows : rows_per_gate;
     if (rows == 0) return {1, 1, 1, 0, 0};             // sums over nothing
     p.gates = (rows + p.rows_per_gate - 1) / p.rows_per_gate;
@@ -71,7 +72,12 @@ static NormPlan norm_plan(uint64_t rows, uint32_t width, uint64_t rows_per_gate)
 }
 
 static size_t norm_ws_bytes(uint64_t rows, uint32_t width, uint64_t rows_per_gate) {
-    return (size_t)(NORM_SUMS * norm_plan(rows, width, rows_per_gate).groups * width * sizeof(float) + 255) & ~(size_t)255;
+    uint64_t groups = 0;
+    for (uint32_t at_once : {1u, 4u}) {
+        const uint64_t n = norm_plan(rows, rows_per_gate, at_once).groups;
+        groups = n > groups ? n : groups;
+    }
+    return (size_t)(NORM_SUMS * groups * width * sizeof(float) + 255) & ~(size_t)255;
 }
 
 // ------------------------------------------------------------------ device
@@ -107,21 +113,28 @@ __device__ __forceinline__ float wave_sum_f32(float v) {
     return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
 }
 
-// Two sums over the LANES threads of a row.  `turn` alternates between two sets of slots,
-// so one barrier a call is enough: a set is written again only after the next call's barrier.
-template <int LANES>
-__device__ __forceinline__ void row_sums(float& a, float& b, float2 (*slots)[LANES / WAVE], int& turn) {
+// How a kernel holds rows: ONE wave each, or a workgroup of up to THREADS each; VECS groups
+// of eight columns a thread.
+template <bool ONE, int VECS, int THREADS>
+struct Layout {
+    static constexpr bool one = ONE;
+    static constexpr int vecs = VECS, threads = THREADS, slots = 2 * THREADS / WAVE;
+    };
+
+// Two sums over the threads of a row.  `turn` alternates between two sets of slots, so one
+// barrier a call is enough: a set is written again only after the next call's barrier.
+template <typename L>
+__device__ __forceinline__ void row_sums(float& a, float& b, float2* slots, int& turn) {
     a = wave_sum_f32(a);
     b = wave_sum_f32(b);
-    if (LANES > WAVE) {
-        const int wave = threadIdx.x / WAVE;
-        if (threadIdx.x % WAVE == 0) slots[turn][wave] = make_float2(a, b);
+    if (!L::one) {
+        float2* s = slots + turn * (L::threads / WAVE);
+        if (threadIdx.x % WAVE == 0) s[threadIdx.x / WAVE] = make_float2(a, b);
         __syncthreads();
         a = b = 0.0f;
-#pragma unroll
-        for (int w = 0; w < LANES / WAVE; ++w) {
-            a += slots[turn][w].x;
-            b += slots[turn][w].y;
+        for (uint32_t w = 0; w < blockDim.x / WAVE; ++w) {
+            a += s[w].x;
+            b += s[w].y;
         }
         turn ^= 1;
     }
@@ -131,49 +144,68 @@ __device__ __forceinline__ float sum_eight(f32x8 v) {
     return ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
 }
 
-// The columns of one thread: VECS groups of eight, LANES groups apart.
-template <int LANES, int VECS>
+// The columns of one thread: groups of eight, as many apart as threads hold the row.  A
+// group that the row ends in, or before, is read as the last eight elements of the row and moved into
+// place, so every load of a row is one wide load that depends on nothing.
+template <typename L>
 struct Columns {
-    uint32_t lane, width;
-    __device__ __forceinline__ uint32_t group(int v) const { return v * LANES + lane; }
-    __device__ __forceinline__ int count(int v) const {
-        const int left = (int)width - (int)(group(v) * 8);
-        return left >= 8 ? 8 : left > 0 ? left : 0;
+    uint32_t lane, lanes, width, at[L::vecs], skip[L::vecs];
+    __device__ __forceinline__ Columns(uint32_t lane_, uint32_t lanes_, uint32_t width_) : lane(lane_), lanes(lanes_), width(width_) {
+#pragma unroll
+        for (int v = 0; v < L::vecs; ++v) {
+            const uint32_t col = group(v) * 8;
+            at[v] = col + 8 <= width ? col : width - 8;
+            skip[v] = col - at[v];
+        }
+    }
+    __device__ __forceinline__ uint32_t group(int v) const { return v * lanes + lane; }
+    __device__ __forceinline__ int count(int v) const { return skip[v] < 8 ? 8 - (int)skip[v] : 0; }
+
+    template <typename T>
+    struct Raw { typename Eight<T>::vec v[L::vecs]; };
+
+    template <typename T>
+    __device__ __forceinline__ Raw<T> fetch(const T* row) const {
+        Raw<T> r;
+#pragma unroll
+        for (int v = 0; v < L::vecs; ++v) r.v[v] = raw_eight(row + at[v]);
+        return r;
     }
     template <typename T>
-    __device__ __forceinline__ void load(f32x8 (&to)[VECS], const T* row, float rest = 0.0f) const {
+    __device__ __forceinline__ void open(f32x8 (&to)[L::vecs], Raw<T> r) const {
 #pragma unroll
-        for (int v = 0; v < VECS; ++v) {
-            const int n = count(v);
-            const T* p = row + group(v) * 8;
-            to[v] = n == 8 ? load_eight(p) : load_some(p, n, rest);
+        for (int v = 0; v < L::vecs; ++v) {
+            if (skip[v]) r.v[v] = skip_elements<T>(r.v[v], skip[v]);
+            to[v] = __builtin_convertvector(r.v[v], f32x8);
         }
     }
     template <typename T>
-    __device__ __forceinline__ void store(T* row, const f32x8 (&from)[VECS]) const {
+    __device__ __forceinline__ void load(f32x8 (&to)[L::vecs], const T* row) const { open<T>(to, fetch<T>(row)); }
+
+    template <typename T>
+    __device__ __forceinline__ void store(T* row, const f32x8 (&from)[L::vecs]) const {
 #pragma unroll
-        for (int v = 0; v < VECS; ++v) {
-            const int n = count(v);
+        for (int v = 0; v < L::vecs; ++v) {
             T* p = row + group(v) * 8;
-            if (n == 8) store_eight(p, from[v]);
-            else store_some(p, from[v], n);
+            if (!skip[v]) store_eight(p, from[v]);
+            else store_some(p, from[v], count(v));
         }
     }
 };
 
 // Mean and reciprocal deviation of a row: the mean first, then the centred squares.
-template <int LANES, int VECS>
-__device__ __forceinline__ float2 row_statistics(const f32x8 (&v)[VECS], const Columns<LANES, VECS>& cols, const NormArgs& a,
-                                                 float2 (*slots)[LANES / WAVE], int& turn) {
+template <typename L>
+__device__ __forceinline__ float2 row_statistics(const f32x8 (&v)[L::vecs], const Columns<L>& cols, const NormArgs& a,
+                                                 float2* slots, int& turn) {
     float mean = 0.0f, none = 0.0f, squares = 0.0f;
     if (a.layer) {
 #pragma unroll
-        for (int i = 0; i < VECS; ++i) mean += sum_eight(v[i]);      // columns past the width hold 0
-        row_sums<LANES>(mean, none, slots, turn);
+        for (int i = 0; i < L::vecs; ++i) mean += sum_eight(v[i]);      // columns past the width hold 0
+        row_sums<L>(mean, none, slots, turn);
         mean *= a.inv_width;
     }
 #pragma unroll
-    for (int i = 0; i < VECS; ++i) {
+    for (int i = 0; i < L::vecs; ++i) {
         const int n = cols.count(i);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
@@ -182,77 +214,74 @@ __device__ __forceinline__ float2 row_statistics(const f32x8 (&v)[VECS], const C
         }
     }
     none = 0.0f;
-    row_sums<LANES>(squares, none, slots, turn);
+    row_sums<L>(squares, none, slots, turn);
     return make_float2(mean, 1.0f / __builtin_sqrtf(__builtin_fmaf(squares, a.inv_width, a.eps)));
 }
 
 // Multiplies by scale what the random field keeps and clears the rest.
-template <int LANES, int VECS>
-__device__ __forceinline__ void drop_row(f32x8 (&v)[VECS], const Columns<LANES, VECS>& cols, uint64_t row, RandomKey key,
+template <typename L>
+__device__ __forceinline__ void drop_row(f32x8 (&v)[L::vecs], const Columns<L>& cols, uint64_t row, RandomKey key,
                                          const NormArgs& a) {
 #pragma unroll
-    for (int i = 0; i < VECS; ++i) {
+    for (int i = 0; i < L::vecs; ++i) {
         const RandomBlock b = random_block(key, cols.group(i), (uint32_t)row, (uint32_t)(row >> 32), a.site);
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[i][j] = kept(b, j, a.drop.bar) ? v[i][j] * a.drop.scale : 0.0f;
     }
 }
 
-template <int LANES, int VECS>
-constexpr int norm_threads() { return LANES == WAVE ? 256 : LANES; }
-
-template <typename T, int LANES, int VECS>
-__global__ __launch_bounds__((norm_threads<LANES, VECS>())) void norm_forward_kernel(NormArgs a, const T* u, const T* x, T* h,
+template <typename T, typename L>
+__global__ __launch_bounds__(L::threads) void norm_forward_kernel(NormArgs a, const T* u, const T* x, T* h,
                                                                                    T* y) {
-    constexpr int AT_ONCE = norm_threads<LANES, VECS>() / LANES;
-    __shared__ float2 slots[2][LANES / WAVE];
+    constexpr int AT_ONCE = L::one ? L::threads / WAVE : 1;
+    __shared__ float2 slots[L::slots];
     int turn = 0;
-    const Columns<LANES, VECS> cols = {threadIdx.x % LANES, a.width};
+    const Columns<L> cols(L::one ? threadIdx.x % WAVE : threadIdx.x, L::one ? WAVE : blockDim.x, a.width);
     const bool drops = a.drop.bar != 65536u;
     RandomKey key = {0, 0};
     if (drops) key = random_key(a.seed);
-    f32x8 pre_w[VECS], pre_b[VECS];
+    f32x8 pre_w[L::vecs], pre_b[L::vecs];
     if (a.pre_w) cols.load(pre_w, a.pre_w);
     if (a.pre_b) cols.load(pre_b, a.pre_b);
-    for (uint64_t row = (uint64_t)blockIdx.x * AT_ONCE + threadIdx.x / LANES; row < a.rows; row += (uint64_t)gridDim.x * AT_ONCE) {
-        f32x8 s[VECS], r[VECS];
+    for (uint64_t row = (uint64_t)blockIdx.x * AT_ONCE + (L::one ? threadIdx.x / WAVE : 0); row < a.rows; row += (uint64_t)gridDim.x * AT_ONCE) {
+        f32x8 s[L::vecs], r[L::vecs];
         float4 st = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
         cols.load(s, u + row * a.u_stride);
         cols.load(r, x + row * a.x_stride);
         if (a.post_w) {
-            const float2 m = row_statistics<LANES, VECS>(s, cols, a, slots, turn);
+            const float2 m = row_statistics<L>(s, cols, a, slots, turn);
             st.x = m.x;
             st.y = m.y;
-            f32x8 w[VECS];
+            f32x8 w[L::vecs];
             cols.load(w, a.post_w);
 #pragma unroll
-            for (int i = 0; i < VECS; ++i) s[i] = (s[i] - m.x) * m.y * w[i];
+            for (int i = 0; i < L::vecs; ++i) s[i] = (s[i] - m.x) * m.y * w[i];
             if (a.post_b) {
                 cols.load(w, a.post_b);
 #pragma unroll
-                for (int i = 0; i < VECS; ++i) s[i] += w[i];
+                for (int i = 0; i < L::vecs; ++i) s[i] += w[i];
             }
         }
-        if (drops) drop_row<LANES, VECS>(s, cols, row, key, a);
+        if (drops) drop_row<L>(s, cols, row, key, a);
         if (a.gate) {
-            f32x8 g[VECS];
+            f32x8 g[L::vecs];
             cols.load(g, a.gate + row / a.rows_per_gate * a.width);
 #pragma unroll
-            for (int i = 0; i < VECS; ++i) s[i] *= g[i];
+            for (int i = 0; i < L::vecs; ++i) s[i] *= g[i];
         }
 #pragma unroll
-        for (int i = 0; i < VECS; ++i) s[i] = __builtin_convertvector(
+        for (int i = 0; i < L::vecs; ++i) s[i] = __builtin_convertvector(
             __builtin_convertvector(a.alpha * r[i] + s[i], typename Eight<T>::vec), f32x8);
         if (h) cols.store(h + row * a.h_stride, s);
         if (a.pre_w) {
-            const float2 m = row_statistics<LANES, VECS>(s, cols, a, slots, turn);
+            const float2 m = row_statistics<L>(s, cols, a, slots, turn);
             st.z = m.x;
             st.w = m.y;
 #pragma unroll
-            for (int i = 0; i < VECS; ++i) s[i] = (s[i] - m.x) * m.y * pre_w[i];
+            for (int i = 0; i < L::vecs; ++i) s[i] = (s[i] - m.x) * m.y * pre_w[i];
             if (a.pre_b) {
 #pragma unroll
-                for (int i = 0; i < VECS; ++i) s[i] += pre_b[i];
+                for (int i = 0; i < L::vecs; ++i) s[i] += pre_b[i];
             }
             cols.store(y + row * a.y_stride, s);
         }
@@ -262,14 +291,14 @@ __global__ __launch_bounds__((norm_threads<LANES, VECS>())) void norm_forward_ke
 
 // The gradient of a norm's input from the gradient of its output (in place), and what this
 // row adds to the gradients of its weight and bias.
-template <int LANES, int VECS>
-__device__ __forceinline__ void norm_input_gradient(f32x8 (&d)[VECS], const f32x8 (&v)[VECS], const f32x8 (&w)[VECS],
-                                                    float mean, float r, f32x8 (&dw)[VECS], f32x8 (&db)[VECS],
-                                                    const NormArgs& a, float2 (*slots)[LANES / WAVE], int& turn) {
+template <typename L>
+__device__ __forceinline__ void norm_input_gradient(f32x8 (&d)[L::vecs], const f32x8 (&v)[L::vecs], const f32x8 (&w)[L::vecs],
+                                                    float mean, float r, f32x8 (&dw)[L::vecs], f32x8 (&db)[L::vecs],
+                                                    const NormArgs& a, float2* slots, int& turn) {
     float plain = 0.0f, along = 0.0f;
-    f32x8 xhat[VECS];
+    f32x8 xhat[L::vecs];
 #pragma unroll
-    for (int i = 0; i < VECS; ++i) {
+    for (int i = 0; i < L::vecs; ++i) {
         xhat[i] = (v[i] - mean) * r;
         const f32x8 p = d[i] * xhat[i];
         dw[i] += p;
@@ -278,22 +307,22 @@ __device__ __forceinline__ void norm_input_gradient(f32x8 (&d)[VECS], const f32x
         plain += sum_eight(d[i]);
         along += sum_eight(p * w[i]);
     }
-    row_sums<LANES>(plain, along, slots, turn);
+    row_sums<L>(plain, along, slots, turn);
     plain = a.layer ? plain * a.inv_width : 0.0f;
     along *= a.inv_width;
 #pragma unroll
-    for (int i = 0; i < VECS; ++i) d[i] = (d[i] - plain - xhat[i] * along) * r;
+    for (int i = 0; i < L::vecs; ++i) d[i] = (d[i] - plain - xhat[i] * along) * r;
 }
 
 // Adds what the waves of a workgroup that work on different rows hold, and writes it out.
-template <int LANES, int VECS>
-__device__ __forceinline__ void put_sums(f32x8 (&v)[VECS], const Columns<LANES, VECS>& cols, float* to, float* shared) {
-    if (LANES == WAVE) {
-        constexpr int SPAN = LANES * VECS * 8;
+template <typename L>
+__device__ __forceinline__ void put_sums(f32x8 (&v)[L::vecs], const Columns<L>& cols, float* to, float* shared) {
+    if (L::one) {
+        constexpr int SPAN = WAVE * L::vecs * 8;
         const int wave = threadIdx.x / WAVE;
         __syncthreads();
 #pragma unroll
-        for (int i = 0; i < VECS; ++i) *reinterpret_cast<f32x8*>(shared + wave * SPAN + cols.group(i) * 8) = v[i];
+        for (int i = 0; i < L::vecs; ++i) *reinterpret_cast<f32x8*>(shared + wave * SPAN + cols.group(i) * 8) = v[i];
         __syncthreads();
         for (uint32_t c = threadIdx.x; c < cols.width; c += 256)
             to[c] = (shared[c] + shared[SPAN + c]) + (shared[2 * SPAN + c] + shared[3 * SPAN + c]);
@@ -303,127 +332,139 @@ __device__ __forceinline__ void put_sums(f32x8 (&v)[VECS], const Columns<LANES, 
 }
 
 // ALL: with a norm after the block or a gate; without, the registers they take are free.
-template <typename T, int LANES, int VECS, bool ALL>
-__global__ __launch_bounds__((norm_threads<LANES, VECS>())) void norm_backward_kernel(
+template <typename T, typename L, bool ALL>
+__global__ __launch_bounds__(L::threads, L::threads == 512 ? 3 : 1) void norm_backward_kernel(
     NormArgs a, const T* u, const T* h, const T* dh, const T* dy, T* dx, T* du) {
-    constexpr int AT_ONCE = norm_threads<LANES, VECS>() / LANES;
-    __shared__ float2 slots[2][LANES / WAVE];
-    __shared__ __attribute__((aligned(32))) float shared[LANES == WAVE ? 4 * LANES * VECS * 8 : 1];
+    constexpr int AT_ONCE = L::one ? L::threads / WAVE : 1;
+    __shared__ float2 slots[L::slots];
+    __shared__ __attribute__((aligned(32))) float shared[L::one ? L::threads * L::vecs * 8 : 1];
     int turn = 0;
-    const Columns<LANES, VECS> cols = {threadIdx.x % LANES, a.width};
+    const Columns<L> cols(L::one ? threadIdx.x % WAVE : threadIdx.x, L::one ? WAVE : blockDim.x, a.width);
     const bool drops = a.drop.bar != 65536u;
     RandomKey key = {0, 0};
     if (drops) key = random_key(a.seed);
-    f32x8 pre_w[VECS], dpre_w[VECS], dpre_b[VECS], dpost_w[VECS], dpost_b[VECS], dgate[VECS];
+    f32x8 pre_w[L::vecs], post_w[L::vecs], post_b[L::vecs], dpre_w[L::vecs], dpre_b[L::vecs], dpost_w[L::vecs], dpost_b[L::vecs],
+        dgate[L::vecs];
 #pragma unroll
-    for (int i = 0; i < VECS; ++i) dpre_w[i] = dpre_b[i] = dpost_w[i] = dpost_b[i] = dgate[i] = 0.0f;
+    for (int i = 0; i < L::vecs; ++i) dpre_w[i] = dpre_b[i] = dpost_w[i] = dpost_b[i] = dgate[i] = 0.0f;
     if (a.pre_w) cols.load(pre_w, a.pre_w);
+    if (ALL && a.post_w) cols.load(post_w, a.post_w);
+    if (ALL && a.post_b) cols.load(post_b, a.post_b);
 
     const uint64_t gate0 = a.parts > 1 ? blockIdx.x / a.parts : blockIdx.x * (a.chunk / a.rows_per_gate);
     uint64_t begin = a.parts > 1 ? gate0 * a.rows_per_gate + blockIdx.x % a.parts * a.chunk : blockIdx.x * a.chunk;
     uint64_t last = begin + a.chunk;
     if (a.parts > 1 && last > (gate0 + 1) * a.rows_per_gate) last = (gate0 + 1) * a.rows_per_gate;
     if (last > a.rows) last = a.rows;
+
+    // A row's loads are issued before the row ahead of it is worked on.
+    typename Columns<L>::template Raw<T> next_dh, next_u, next_h, next_dy;
+    float4 next_st;
+    const auto fetch = [&](uint64_t row) {
+        next_st = a.stats[row];
+        if (dh) next_dh = cols.fetch(dh + row * a.dh_stride);
+        if (ALL) next_u = cols.fetch(u + row * a.u_stride);
+        if (a.pre_w) {
+            next_h = cols.fetch(h + row * a.h_stride);
+            next_dy = cols.fetch(dy + row * a.dy_stride);
+        }
+    };
     for (uint64_t gate = gate0; begin < last || gate == gate0; ++gate) {
         // the rows of one gate; a workgroup whose part of it is empty passes through once
         uint64_t end = (gate + 1) * a.rows_per_gate;
         if (end > last) end = last;
-        f32x8 g[VECS];
+        f32x8 g[L::vecs];
         if (ALL && a.gate) cols.load(g, a.gate + gate * a.width);
-        for (uint64_t row = begin + threadIdx.x / LANES; row < end; row += AT_ONCE) {
-            const float4 st = a.stats[row];
-            f32x8 d[VECS], v[VECS];
-            if (dh) {
-                cols.load(d, dh + row * a.dh_stride);
-            } else {
+        uint64_t row = begin + (L::one ? threadIdx.x / WAVE : 0);
+        if (row < end) fetch(row);
+        for (; row < end; row += AT_ONCE) {
+            const float4 st = next_st;
+            f32x8 d[L::vecs], v[L::vecs], o[L::vecs], su[L::vecs];
 #pragma unroll
-                for (int i = 0; i < VECS; ++i) d[i] = 0.0f;
-            }
-            f32x8 su[VECS];
-            if (ALL) cols.load(su, u + row * a.u_stride);
+            for (int i = 0; i < L::vecs; ++i) d[i] = 0.0f;
+            if (dh) cols.template open<T>(d, next_dh);
+            if (ALL) cols.template open<T>(su, next_u);
             if (a.pre_w) {
-                f32x8 o[VECS];
-                cols.load(v, h + row * a.h_stride);
-                cols.load(o, dy + row * a.dy_stride);
-                norm_input_gradient<LANES, VECS>(o, v, pre_w, st.z, st.w, dpre_w, dpre_b, a, slots, turn);
+                cols.template open<T>(v, next_h);
+                cols.template open<T>(o, next_dy);
+            }
+            if (row + AT_ONCE < end) fetch(row + AT_ONCE);
+            if (a.pre_w) {
+                norm_input_gradient<L>(o, v, pre_w, st.z, st.w, dpre_w, dpre_b, a, slots, turn);
 #pragma unroll
-                for (int i = 0; i < VECS; ++i) d[i] += o[i];
+                for (int i = 0; i < L::vecs; ++i) d[i] += o[i];
             }
 #pragma unroll
-            for (int i = 0; i < VECS; ++i) v[i] = a.alpha * d[i];
+            for (int i = 0; i < L::vecs; ++i) v[i] = a.alpha * d[i];
             cols.store(dx + row * a.dx_stride, v);
-            if (drops) drop_row<LANES, VECS>(d, cols, row, key, a);
+            if (drops) drop_row<L>(d, cols, row, key, a);
             if (ALL) {
-                f32x8 w[VECS];
-                if (a.post_w) cols.load(w, a.post_w);
                 if (a.gate) {
-                    f32x8 b[VECS];
-                    if (a.post_b) cols.load(b, a.post_b);
 #pragma unroll
-                    for (int i = 0; i < VECS; ++i) {
+                    for (int i = 0; i < L::vecs; ++i) {
                         f32x8 s = su[i];
-                        if (a.post_w) s = (s - st.x) * st.y * w[i];
-                        if (a.post_b) s += b[i];
+                        if (a.post_w) s = (s - st.x) * st.y * post_w[i];
+                        if (a.post_b) s += post_b[i];
                         dgate[i] += d[i] * s;       // d holds the mask and its scale already
                         d[i] *= g[i];
                     }
                 }
-                if (a.post_w) norm_input_gradient<LANES, VECS>(d, su, w, st.x, st.y, dpost_w, dpost_b, a, slots, turn);
+                if (a.post_w) norm_input_gradient<L>(d, su, post_w, st.x, st.y, dpost_w, dpost_b, a, slots, turn);
             }
             cols.store(du + row * a.du_stride, d);
         }
         if (ALL && a.dgate) {
             float* to = a.parts > 1 ? a.partial + (4 * a.groups + blockIdx.x) * a.width : a.dgate + gate * a.width;
-            put_sums<LANES, VECS>(dgate, cols, to, shared);
+            put_sums<L>(dgate, cols, to, shared);
 #pragma unroll
-            for (int i = 0; i < VECS; ++i) dgate[i] = 0.0f;
+            for (int i = 0; i < L::vecs; ++i) dgate[i] = 0.0f;
         }
         begin = end > begin ? end : begin;
         if (begin >= last) break;
     }
     const auto at = [&](int sum) { return a.partial + (sum * a.groups + blockIdx.x) * a.width; };
     if (a.pre_w) {
-        put_sums<LANES, VECS>(dpre_w, cols, at(0), shared);
-        if (a.pre_b) put_sums<LANES, VECS>(dpre_b, cols, at(1), shared);
+        put_sums<L>(dpre_w, cols, at(0), shared);
+        if (a.pre_b) put_sums<L>(dpre_b, cols, at(1), shared);
     }
     if (ALL && a.post_w) {
-        put_sums<LANES, VECS>(dpost_w, cols, at(2), shared);
-        if (a.post_b) put_sums<LANES, VECS>(dpost_b, cols, at(3), shared);
+        put_sums<L>(dpost_w, cols, at(2), shared);
+        if (a.post_b) put_sums<L>(dpost_b, cols, at(3), shared);
     }
 }
 
-// Adds partial rows: 64 columns a workgroup, four slices of the rows, always in the same
+// Adds partial rows: 32 columns a workgroup, 32 slices of the rows, always in the same
 // order.  blockIdx.y: one of the four parameter gradients (rows = all groups), or 4 + gate
 // (rows = that gate's parts).
 struct NormOutputs { float* to[4]; };
-constexpr int NORM_ADD_BLOCK = 256;
+constexpr int NORM_ADD_COLS = 32, NORM_ADD_SLICES = 32, NORM_ADD_BLOCK = NORM_ADD_COLS * NORM_ADD_SLICES;
 
 __global__ __launch_bounds__(NORM_ADD_BLOCK) void norm_add_kernel(NormOutputs out, float* dgate, const float* partial,
                                                                   uint64_t groups, uint32_t parts, uint32_t width) {
-    __shared__ float shared[NORM_ADD_BLOCK];
-    const uint32_t which = blockIdx.y, col = blockIdx.x * WAVE + threadIdx.x % WAVE, slice = threadIdx.x / WAVE;
+    __shared__ float shared[NORM_ADD_SLICES][NORM_ADD_COLS];
+    const uint32_t which = blockIdx.y, c = threadIdx.x % NORM_ADD_COLS, slice = threadIdx.x / NORM_ADD_COLS;
+    const uint32_t col = blockIdx.x * NORM_ADD_COLS + c;
     float* to = which < 4 ? out.to[which] : dgate + (uint64_t)(which - 4) * width;
     if (!to) return;
-    const float* from = partial + (which < 4 ? which * groups : 4 * groups + (uint64_t)(which - 4) * parts) * width;
-    const uint64_t rows = which < 4 ? groups : parts;
+    const float* from = partial + (which < 4 ? which * groups : 4 * groups + (uint64_t)(which - 4) * parts) * width + col;
+    const uint32_t rows = which < 4 ? (uint32_t)groups : parts;
     float sum = 0.0f;
-    if (col < width) {
-        const uint64_t each = (rows + 3) / 4, end = (slice + 1) * each < rows ? (slice + 1) * each : rows;
+    if (col < width)
 #pragma unroll 8
-        for (uint64_t r = slice * each; r < end; ++r) sum += from[r * width + col];
-    }
-    shared[threadIdx.x] = sum;
+        for (uint32_t r = slice; r < rows; r += NORM_ADD_SLICES) sum += from[(uint64_t)r * width];
+    shared[slice][c] = sum;
     __syncthreads();
-    if (slice == 0 && col < width)
-        to[col] = (shared[threadIdx.x] + shared[WAVE + threadIdx.x]) +
-                  (shared[2 * WAVE + threadIdx.x] + shared[3 * WAVE + threadIdx.x]);
+    if (slice == 0 && col < width) {
+        for (int i = 1; i < NORM_ADD_SLICES; ++i) sum += shared[i][c];
+        to[col] = sum;
+    }
 }
 
 // ------------------------------------------------------------------ host
 
 // Checks what both directions share and fills the kernels' arguments; false if refused.
 static bool norm_args(const okt_residual_norm* op, NormArgs& a) {
-    if (!op || !known_dtype(op->dtype) || op->rows > NORM_MAX_ROWS || op->width == 0 || op->width > NORM_MAX_WIDTH) return false;
+    if (!op || !known_dtype(op->dtype) || op->rows > NORM_MAX_ROWS || op->width < NORM_MIN_WIDTH || op->width > NORM_MAX_WIDTH) return false;
     if (op->kind != OKT_NORM_LAYER && op->kind != OKT_NORM_RMS) return false;
     if (!(op->eps >= 0.0f) || op->residual_scale != op->residual_scale) return false;
     if (!dropout_rule(op->dropout_p, a.drop)) return false;
@@ -465,36 +506,35 @@ static bool norm_args(const okt_residual_norm* op, NormArgs& a) {
 
 struct NormPointers { const void *u, *x, *h, *dh, *dy; void *out_h, *out_y, *dx, *du; };
 
-template <typename T, int LANES, int VECS>
-static void launch_norm(const NormArgs& a, const NormPointers& p, bool backward, unsigned groups, hipStream_t s) {
-    const dim3 grid(groups), block(norm_threads<LANES, VECS>());
+template <typename T, typename L>
+static void launch_norm(const NormArgs& a, const NormPointers& p, bool backward, unsigned groups, unsigned threads, hipStream_t s) {
+    const dim3 grid(groups), block(threads);
     if (!backward) {
-        hipLaunchKernelGGL((norm_forward_kernel<T, LANES, VECS>), grid, block, 0, s, a, (const T*)p.u, (const T*)p.x,
-                           (T*)p.out_h, (T*)p.out_y);
+        hipLaunchKernelGGL((norm_forward_kernel<T, L>), grid, block, 0, s, a, (const T*)p.u, (const T*)p.x, (T*)p.out_h, (T*)p.out_y);
     } else if (a.post_w || a.gate) {
-        hipLaunchKernelGGL((norm_backward_kernel<T, LANES, VECS, true>), grid, block, 0, s, a, (const T*)p.u, (const T*)p.h,
+        if constexpr (!(L::one && L::vecs == 2))           // norm_shape gives a gated row another one
+        hipLaunchKernelGGL((norm_backward_kernel<T, L, true>), grid, block, 0, s, a, (const T*)p.u, (const T*)p.h,
                            (const T*)p.dh, (const T*)p.dy, (T*)p.dx, (T*)p.du);
     } else {
-        hipLaunchKernelGGL((norm_backward_kernel<T, LANES, VECS, false>), grid, block, 0, s, a, (const T*)p.u, (const T*)p.h,
+        hipLaunchKernelGGL((norm_backward_kernel<T, L, false>), grid, block, 0, s, a, (const T*)p.u, (const T*)p.h,
                            (const T*)p.dh, (const T*)p.dy, (T*)p.dx, (T*)p.du);
     }
 }
 
 template <typename T>
-static void launch_norm_shape(const NormArgs& a, const NormPointers& p, bool backward, unsigned groups, hipStream_t s) {
-    const NormShape n = norm_shape(a.width);
-    if (n.lanes == 64 && n.vecs == 1) launch_norm<T, 64, 1>(a, p, backward, groups, s);
-    else if (n.lanes == 64) launch_norm<T, 64, 2>(a, p, backward, groups, s);
-    else if (n.lanes == 256 && n.vecs == 1) launch_norm<T, 256, 1>(a, p, backward, groups, s);
-    else if (n.lanes == 256) launch_norm<T, 256, 2>(a, p, backward, groups, s);
-    else if (n.lanes == 512) launch_norm<T, 512, 2>(a, p, backward, groups, s);
-    else launch_norm<T, 1024, 2>(a, p, backward, groups, s);
+static void launch_norm_shape(const NormArgs& a, const NormPointers& p, bool backward, NormShape n, unsigned groups, hipStream_t s) {
+    if (n.lanes == WAVE && n.vecs == 1) launch_norm<T, Layout<true, 1, 256>>(a, p, backward, groups, 256, s);
+    else if (n.lanes == WAVE) launch_norm<T, Layout<true, 2, 256>>(a, p, backward, groups, 256, s);
+    else if (n.lanes <= 512) launch_norm<T, Layout<false, 1, 512>>(a, p, backward, groups, n.lanes, s);
+    else if (n.vecs == 1) launch_norm<T, Layout<false, 1, 1024>>(a, p, backward, groups, n.lanes, s);
+    else launch_norm<T, Layout<false, 2, 1024>>(a, p, backward, groups, n.lanes, s);
 }
 
-static void launch_norm_type(int dtype, const NormArgs& a, const NormPointers& p, bool backward, unsigned groups, hipStream_t s) {
-    if (dtype == OKT_F32) launch_norm_shape<float>(a, p, backward, groups, s);
-    else if (dtype == OKT_BF16) launch_norm_shape<__bf16>(a, p, backward, groups, s);
-    else launch_norm_shape<_Float16>(a, p, backward, groups, s);
+static void launch_norm_type(int dtype, const NormArgs& a, const NormPointers& p, bool backward, NormShape n, unsigned groups,
+                             hipStream_t s) {
+    if (dtype == OKT_F32) launch_norm_shape<float>(a, p, backward, n, groups, s);
+    else if (dtype == OKT_BF16) launch_norm_shape<__bf16>(a, p, backward, n, groups, s);
+    else launch_norm_shape<_Float16>(a, p, backward, n, groups, s);
 }
 
 }  // namespace okt
@@ -502,7 +542,7 @@ static void launch_norm_type(int dtype, const NormArgs& a, const NormPointers& p
 extern "C" {
 
 size_t okt_residual_norm_workspace_bytes(uint64_t rows, uint32_t width, uint64_t rows_per_gate) {
-    if (width == 0 || width > okt::NORM_MAX_WIDTH || rows > okt::NORM_MAX_ROWS) return 0;
+    if (width < okt::NORM_MIN_WIDTH || width > okt::NORM_MAX_WIDTH || rows > okt::NORM_MAX_ROWS) return 0;
     const size_t need = okt::norm_ws_bytes(rows, width, rows_per_gate);
     return need ? need : 256;
 }
@@ -519,10 +559,11 @@ int okt_residual_norm_forward(const okt_residual_norm* op, const void* d_u, cons
         if (!aligned(p, e)) return OKT_ERR_INVALID_ARG;
     if (!aligned(d_stats_out, 16)) return OKT_ERR_INVALID_ARG;
     a.stats = (float4*)d_stats_out;
-    const uint64_t at_once = rows_at_once(norm_shape(a.width));
+    const NormShape shape = norm_shape(a.width, false);
+    const uint64_t at_once = rows_at_once(shape);
     const uint64_t want = (a.rows + at_once - 1) / at_once, most = (uint64_t)device_cus() * 8;
     timing_before((hipStream_t)stream);
-    launch_norm_type(op->dtype, a, {d_u, d_x, nullptr, nullptr, nullptr, d_h_out, d_y_out, nullptr, nullptr}, false,
+    launch_norm_type(op->dtype, a, {d_u, d_x, nullptr, nullptr, nullptr, d_h_out, d_y_out, nullptr, nullptr}, false, shape,
                      (unsigned)(want < most ? want : most), (hipStream_t)stream);
     timing_after((hipStream_t)stream);
     return launch_status();
@@ -547,7 +588,8 @@ int okt_residual_norm_backward(const okt_residual_norm* op, const void* d_u, con
         for (const void* p : {d_u, d_h, d_dh, d_dy, (const void*)d_dx_out, (const void*)d_du_out})
             if (!aligned(p, e)) return OKT_ERR_INVALID_ARG;
     }
-    const NormPlan plan = norm_plan(a.rows, a.width, a.rows_per_gate);
+    const NormShape shape = norm_shape(a.width, all);
+    const NormPlan plan = norm_plan(a.rows, a.rows_per_gate, rows_at_once(shape));
     if (!d_ws || !aligned(d_ws, 256) || ws_bytes < norm_ws_bytes(a.rows, a.width, a.rows_per_gate)) return OKT_ERR_WORKSPACE;
     a.stats = (float4*)d_stats;
     a.partial = (float*)d_ws;
@@ -559,13 +601,13 @@ int okt_residual_norm_backward(const okt_residual_norm* op, const void* d_u, con
     if (a.rows) {
         timing_before(s);
         launch_norm_type(op->dtype, a, {d_u, nullptr, d_h, d_dh, d_dy, nullptr, nullptr, d_dx_out, d_du_out}, true,
-                         (unsigned)plan.groups, s);
+                         shape, (unsigned)plan.groups, s);
         timing_after(s);
     }
     NormOutputs out = {{d_dpre_weight_out, d_dpre_bias_out, d_dpost_weight_out, d_dpost_bias_out}};
     const bool gates = d_dgate_out && plan.parts != 1;
     if (out.to[0] || out.to[1] || out.to[2] || out.to[3] || gates)
-        hipLaunchKernelGGL(norm_add_kernel, dim3((a.width + WAVE - 1) / WAVE, 4 + (gates ? (unsigned)plan.gates : 0)),
+        hipLaunchKernelGGL(norm_add_kernel, dim3((a.width + NORM_ADD_COLS - 1) / NORM_ADD_COLS, 4 + (gates ? (unsigned)plan.gates : 0)),
                            dim3(NORM_ADD_BLOCK), 0, s, out, d_dgate_out, (const float*)d_ws, plan.groups, plan.parts, a.width);
     return launch_status();
 }
