@@ -63,18 +63,25 @@ __device__ __forceinline__ uint32_t lds_address(const void* p) {
     return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void*)p;
 }
 
-// ROWS rows of DIM elements, row order by slots, DIM / 8 chunks of 16 bytes a row.  Chunk c of slot s lies
-// at place c ^ turn(s): sixteen neighbouring slots then read one chunk from sixteen
-// different groups of banks (A operands, row by row), and the eight slots that a
-// transposing read touches lie in all four quarters of the banks.
+// ROWS rows of DIM elements, rows in the order of slots, as blocks of sixteen slots by four
+// chunks of eight elements: 1024 bytes, what one fetch of a wave fills, four lanes to 64 bytes of
+// a row.  In a block chunk c of slot s lies at 64 s + 16 (c ^ s / 4).  Sixteen neighbouring
+// slots then read one chunk from all banks (A operands, row by row), and so do the four
+// slots by four chunks of a transposing read; and what a lane adds for another tile, step or
+// column is a constant, so a kernel keeps four offsets for all its reads.
+struct TileReads {
+    uint32_t rows[2], columns[2];                   // of even and odd steps; of the two halves of a step
+};
+
 template <typename T, int DIM, int ROWS, int THREADS>
 struct RowTile {
-    static constexpr int CHUNKS = DIM / 8;
+    static constexpr int ACROSS = DIM / 32;                     // blocks of sixteen slots
     static constexpr int BYTES = ROWS * DIM * 2;
-    static constexpr int LOADS = ROWS * CHUNKS / THREADS;       // 16-byte loads of a thread
+    static constexpr int LOADS = BYTES / 1024 / (THREADS / WAVE);   // of a wave
 
-    static __device__ __forceinline__ uint32_t turn(uint32_t s) {
-        return DIM == 64 ? ((s >> 1 & 1) << 2) | (s >> 2 & 3) : ((s & 3) << 2) | (s >> 2 & 3);
+    static __device__ __forceinline__ uint32_t fetched_slot(int i) {
+        const uint32_t lane = threadIdx.x % WAVE, block = i * (THREADS / WAVE) + threadIdx.x / WAVE;
+        return block / ACROSS * 16 + lane / 4;
     }
 
     // What a thread fetches of every tile, in bytes from the tile's first row; places past
@@ -84,8 +91,9 @@ struct RowTile {
         __device__ __forceinline__ Places(uint32_t row_bytes, uint32_t head_dim) {
 #pragma unroll
             for (int i = 0; i < LOADS; ++i) {
-                const uint32_t n = i * THREADS + threadIdx.x, slot = n / CHUNKS, chunk = n % CHUNKS ^ turn(slot);
-                at[i] = DIM == (int)head_dim || chunk * 8 < head_dim ? row_of_slot(slot) * row_bytes + chunk * 16 : OUTSIDE;
+                const uint32_t block = i * (THREADS / WAVE) + threadIdx.x / WAVE, lane = threadIdx.x % WAVE;
+                const uint32_t chunk = block % ACROSS * 4 + (lane % 4 ^ lane / 16);
+                at[i] = DIM == (int)head_dim || chunk * 8 < head_dim ? row_of_slot(fetched_slot(i)) * row_bytes + chunk * 16 : OUTSIDE;
             }
         }
     };
@@ -106,33 +114,52 @@ struct RowTile {
         } else {
 #pragma unroll
             for (int i = 0; i < LOADS; ++i) {
-                const bool before = first + (int)row_of_slot((i * THREADS + threadIdx.x) / CHUNKS) < lo;
+                const bool before = first + (int)row_of_slot(fetched_slot(i)) < lo;
                 fetch_to_lds(tile + (i * (THREADS / WAVE) + wave) * 1024, before ? OUTSIDE : p.at[i], buffer);
             }
         }
     }
 
+    static __device__ __forceinline__ TileReads reads() {
+        const uint32_t lane = threadIdx.x % WAVE, in = lane % 16;
+        TileReads r;
+#pragma unroll
+        for (uint32_t odd = 0; odd < 2; ++odd) {
+            const uint32_t c = 2 * odd + lane / 32;
+            r.rows[odd] = lane % 32 / 16 * (ACROSS * 1024) + in * 64 + (c ^ in / 4) * 16;
+        }
+#pragma unroll
+        for (uint32_t u = 0; u < 2; ++u) {
+            const uint32_t c = 2 * (lane / 16 % 2) + in % 4 / 2;
+            r.columns[u] = (8 * u + 4 * (lane / 32) + in / 4) * 64 + (c ^ (2 * u + lane / 32)) * 16 + in % 2 * 8;
+        }
+        return r;
+    }
+
     // A operand: rows of the 32-row tile at slot0, columns 16 step .. + 15.
-    static __device__ __forceinline__ frag<T> rows(const char* tile, uint32_t slot0, int step) {
-        const uint32_t lane = threadIdx.x % WAVE, slot = slot0 + lane % 32;
-        return *reinterpret_cast<const frag<T>*>(tile + slot * (DIM * 2) + ((2 * step + lane / 32) ^ turn(slot)) * 16);
+    static __device__ __forceinline__ frag<T> rows(const char* tile, const TileReads& r, uint32_t slot0, int step) {
+        return *reinterpret_cast<const frag<T>*>(tile + r.rows[step % 2] + slot0 / 16 * (ACROSS * 1024) + step / 2 * 1024);
     }
 
     // A operand of the transpose: rows = columns 32 dt .. + 31 of the tile, columns = the
     // sixteen rows of step t of its 32-row tile at slot0.
-    static __device__ __forceinline__ frag<T> columns(const char* tile, uint32_t slot0, int dt, int t) {
-        const uint32_t lane = threadIdx.x % WAVE, in = lane % 16;
-        const uint32_t chunk = 4 * dt + 2 * (lane / 16 % 2) + (in % 4) / 2;
+    static __device__ __forceinline__ frag<T> columns(const char* tile, const TileReads& r, uint32_t slot0, int dt, int t) {
         i16x4 half[2];
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            const uint32_t slot = slot0 + 8 * (2 * t + u) + 4 * (lane / 32) + in / 4;
-            const char* p = tile + slot * (DIM * 2) + (chunk ^ turn(slot)) * 16 + (in % 2) * 8;
-            half[u] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4*)p);
-        }
+        for (int u = 0; u < 2; ++u)
+            half[u] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4*)(
+                tile + r.columns[u] + (slot0 / 16 + t) * (ACROSS * 1024) + dt * 1024));
         return __builtin_bit_cast(frag<T>, __builtin_shufflevector(half[0], half[1], 0, 1, 2, 3, 4, 5, 6, 7));
     }
 };
+
+// 16 bytes a lane of what lies between `from` and `to`, straight into LDS by one wave; zeros past `to`.
+__device__ __forceinline__ void fetch_line(uint32_t lds, const void* from, const void* to) {
+    const uint64_t at = (uint64_t)from, bytes = (uint64_t)to - at;
+    const i32x4 buffer = {(int)uniform((uint32_t)at), (int)uniform((uint32_t)(at >> 32)),
+                          (int)(bytes < OUTSIDE ? uniform((uint32_t)bytes) : OUTSIDE), 0x00020000};
+    fetch_to_lds(lds, threadIdx.x % WAVE * 16, buffer);
+}
 
 // Waits for this wave's fetches into LDS, then for the others.
 __device__ __forceinline__ void fetched() {
@@ -174,12 +201,20 @@ __device__ __forceinline__ void store_row(T* row, const f32x16 (&c)[TILES], floa
         }
 }
 
-// Workgroups are dealt to the eight dies in turn.  Gives each die a run of neighbouring
-// places, so that the blocks of one head, which read the same keys, share an L2.
-__device__ __forceinline__ uint32_t near_place(uint32_t block, uint32_t blocks) {
+// Workgroups are dealt to the eight dies in turn.  A unit is what shares keys (a sequence's
+// key head, `each` workgroups): its workgroups go to one die, so that they share an L2, and
+// neighbouring units to different dies, so that long and short sequences spread over all of
+// them (a padded batch dealt in runs of neighbours: 187 us backward, so 140).
+struct Place { uint32_t unit, in; };
+
+__device__ __forceinline__ Place place_of(uint32_t block, uint32_t units, uint32_t each) {
     constexpr uint32_t DIES = 8;
-    const uint32_t die = block % DIES, each = blocks / DIES, more = blocks % DIES;
-    return die * each + (die < more ? die : more) + block / DIES;
+    const auto first = [](uint32_t die, uint32_t n) { const uint32_t more = n % DIES; return die * (n / DIES) + (die < more ? die : more); };
+    const uint32_t at = first(block % DIES, units * each) + block / DIES;       // every die a run of places
+    const uint32_t run = at / each, more = units % DIES, long_runs = more * (units / DIES + 1);
+    // run `run` of units is number i of a die's share: units die, die + 8, ...
+    const uint32_t die = run < long_runs ? run / (units / DIES + 1) : more + (run - long_runs) / (units / DIES);
+    return {(run - first(die, units)) * DIES + die, at % each};
 }
 
 // ------------------------------------------------------------------ the dropout mask

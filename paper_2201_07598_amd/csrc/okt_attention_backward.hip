@@ -9,35 +9,41 @@
 //            S = Q K', dP = dO V' (queries down, keys across), dV' += dO' P, dK' += Q' dS
 // The scores and dP are formed twice, 7 products where 5 would do: the alternative adds dQ in
 // memory from every key block, in an order that changes from run to run.
+//
+// With dropout, scaled by c = 65536 / bar where kept:  ds = p (c kept(dp) - D) = c p (kept(dp) - D / c)
+// and dv = c sum kept(p) do, so c is applied once at the end, not to every pair.
 #include "okt_attention.h"
 
 namespace okt {
 
 constexpr int BWD_THREADS = 256;
-constexpr int BWD_ROWS = BWD_THREADS / WAVE * 32;     // queries or keys of a workgroup
-constexpr int BWD_TILE = 64;                          // keys or queries that pass by together
+constexpr int BWD_QUERIES = BWD_THREADS / WAVE * 32;  // of a workgroup of the queries' kernel
+constexpr int BWD_KEYS = 64;                          // that pass by it together
 
-// log-sum-exp to base 2, +inf for a row that sees nothing: its probabilities come out as 0
-__device__ __forceinline__ float lse_log2(float lse) { return lse == -INFINITY ? INFINITY : lse * 1.44269504088896f; }
+// What the keys' kernel has to know of a query: its log-sum-exp to base 2 (+inf for a row that
+// sees nothing, whose probabilities come out as 0) and D / c.
+typedef float2 RowNumbers;
 
 template <typename T, int DIM, bool DROP>
-__global__ __launch_bounds__(BWD_THREADS, DIM == 64 ? 2 : 1) void attention_backward_queries_kernel(
-    AttentionArgs a, const T* q, const T* k, const T* v, const T* o, const float* lse, const T* d_o, T* dq, float* rows_d,
+__global__ __launch_bounds__(BWD_THREADS, 2) void attention_backward_queries_kernel(
+    AttentionArgs a, const T* q, const T* k, const T* v, const T* o, const float* lse, const T* d_o, T* dq, RowNumbers* rows,
     uint32_t blocks) {
-    using Tile = RowTile<T, DIM, BWD_TILE, BWD_THREADS>;
+    using Tile = RowTile<T, DIM, BWD_KEYS, BWD_THREADS>;
     __shared__ __attribute__((aligned(1024))) char shared[4 * Tile::BYTES];
-    const uint32_t place = near_place(blockIdx.x, gridDim.x), plane = place / blocks;
-    const uint32_t b = plane / a.heads, h = plane % a.heads, kv = h / a.group;
+    const Place at = place_of(blockIdx.x, a.batch * a.kv_heads, a.group * blocks);
+    const uint32_t b = at.unit / a.kv_heads, kv = at.unit % a.kv_heads, h = kv * a.group + at.in / blocks, plane = b * a.heads + h;
     const uint32_t wave = uniform(threadIdx.x / WAVE), lane = threadIdx.x % WAVE;
     const int ql = sequence_length(a.q_lens, b, a.q_len), kl = sequence_length(a.k_lens, b, a.k_len);
-    const int q0 = (blocks - 1 - place % blocks) * BWD_ROWS, w0 = q0 + 32 * (int)wave, i = w0 + (int)(lane % 32);
+    const int q0 = (blocks - 1 - at.in % blocks) * BWD_QUERIES, w0 = q0 + 32 * (int)wave, i = w0 + (int)(lane % 32);
     const int past = kl - ql + 1;
     const auto seen = [&](int query) { const int n = query + past; return query >= ql ? 0 : !a.causal || n > kl ? kl : n < 0 ? 0 : n; };
-    const int keys = q0 < ql ? seen(q0 + BWD_ROWS < ql ? q0 + BWD_ROWS - 1 : ql - 1) : 0;
+    const int keys = q0 < ql ? seen(q0 + BWD_QUERIES < ql ? q0 + BWD_QUERIES - 1 : ql - 1) : 0;
     const int mine = seen(i), wave_least = w0 + 31 < ql ? seen(w0) : 0;
     const int wave_most = w0 < ql ? seen(w0 + 32 < ql ? w0 + 31 : ql - 1) : 0;
+    const float drop_scale = DROP ? a.drop.scale : 1.0f;
 
     f32x16 acc[DIM / 32];
+    float base = INFINITY, sum = 0.0f;            // log-sum-exp, D / c
 #pragma unroll
     for (int d = 0; d < DIM / 32; ++d) acc[d] = 0.0f;
     if (keys > 0) {
@@ -53,7 +59,6 @@ __global__ __launch_bounds__(BWD_THREADS, DIM == 64 ? 2 : 1) void attention_back
         Tile::fetch(lds, kb, k_row, k_at, 0, 0, kl, a.head_dim);
         Tile::fetch(lds + Tile::BYTES, vb, v_row, v_at, 0, 0, kl, a.head_dim);
         frag<T> qf[DIM / 16], df[DIM / 16];
-        float sum = 0.0f;
 #pragma unroll
         for (int s = 0; s < DIM / 16; ++s) {
             qf[s] = row_operand(q_row, s, a.head_dim);
@@ -62,35 +67,37 @@ __global__ __launch_bounds__(BWD_THREADS, DIM == 64 ? 2 : 1) void attention_back
 #pragma unroll
             for (int e = 0; e < 8; ++e) sum = __builtin_fmaf(x[e], y[e], sum);
         }
-        sum = sum_halves(sum);
-        const float base = lse_log2(lse[(uint64_t)plane * a.q_len + row]);
+        sum = mine > 0 ? sum_halves(sum) / drop_scale : 0.0f;
+        if (mine > 0) base = lse[(uint64_t)plane * a.q_len + row] * 1.44269504088896f;
+        const TileReads reads = Tile::reads();
         RandomKey key = {0, 0};
         if (DROP) key = random_key(a.seed);
 
-        for (int key0 = 0, turn = 0; key0 < keys; key0 += BWD_TILE, turn ^= 1) {
+        for (int key0 = 0, turn = 0; key0 < keys; key0 += BWD_KEYS, turn ^= 1) {
             fetched();
             const char* kt = shared + turn * 2 * Tile::BYTES;
             const char* vt = kt + Tile::BYTES;
-            if (key0 + BWD_TILE < keys) {
+            if (key0 + BWD_KEYS < keys) {
                 const uint32_t next = lds + (turn ^ 1) * 2 * Tile::BYTES;
-                Tile::fetch(next, kb, k_row, k_at, key0 + BWD_TILE, 0, kl, a.head_dim);
-                Tile::fetch(next + Tile::BYTES, vb, v_row, v_at, key0 + BWD_TILE, 0, kl, a.head_dim);
+                Tile::fetch(next, kb, k_row, k_at, key0 + BWD_KEYS, 0, kl, a.head_dim);
+                Tile::fetch(next + Tile::BYTES, vb, v_row, v_at, key0 + BWD_KEYS, 0, kl, a.head_dim);
             }
             if (key0 >= wave_most) continue;
-            const bool masked = key0 + BWD_TILE > wave_least;
+            const bool masked = key0 + BWD_KEYS > wave_least;
 #pragma unroll
-            for (int n = 0; n < BWD_TILE / 32; ++n) {
+            for (int n = 0; n < BWD_KEYS / 32; ++n) {
                 f32x16 s = 0.0f, dp = 0.0f;
 #pragma unroll
-                for (int e = 0; e < DIM / 16; ++e) s = mfma(Tile::rows(kt, 32 * n, e), qf[e], s);
-#pragma unroll
-                for (int e = 0; e < DIM / 16; ++e) dp = mfma(Tile::rows(vt, 32 * n, e), df[e], dp);
+                for (int e = 0; e < DIM / 16; ++e) {
+                    s = mfma(Tile::rows(kt, reads, 32 * n, e), qf[e], s);
+                    dp = mfma(Tile::rows(vt, reads, 32 * n, e), df[e], dp);
+                }
                 if (DROP) {
                     uint32_t w[16];
                     kept_keys(w, i, key0 + 32 * n, plane, key, a.site);
                     const uint32_t mask = lane & 1 ? 0xffffffffu : 0xffffu, bar = a.drop.bar << (16 * (lane & 1));
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) dp[r] = (w[r] & mask) < bar ? dp[r] * a.drop.scale : 0.0f;
+                    for (int r = 0; r < 16; ++r) dp[r] = (w[r] & mask) < bar ? dp[r] : 0.0f;
                 }
 #pragma unroll
                 for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], a.scale_log2, -base));
@@ -106,7 +113,6 @@ __global__ __launch_bounds__(BWD_THREADS, DIM == 64 ? 2 : 1) void attention_back
                     for (int r = 0; r < 16; ++r) few = __builtin_fmaf(s[r], dp[r], few);
                     few = sum_halves(few);
                     sum = mine <= 32 ? few : sum;
-                    if (lane < 32 && i < ql) rows_d[(uint64_t)plane * a.q_len + i] = sum;
                 }
 #pragma unroll
                 for (int r = 0; r < 16; ++r) s[r] *= dp[r] - sum;
@@ -114,43 +120,73 @@ __global__ __launch_bounds__(BWD_THREADS, DIM == 64 ? 2 : 1) void attention_back
                 for (int t = 0; t < 2; ++t) {
                     const frag<T> ds = to_operand<T>(s, t);
 #pragma unroll
-                    for (int d = 0; d < DIM / 32; ++d) acc[d] = mfma(Tile::columns(kt, 32 * n, d, t), ds, acc[d]);
+                    for (int d = 0; d < DIM / 32; ++d) acc[d] = mfma(Tile::columns(kt, reads, 32 * n, d, t), ds, acc[d]);
                 }
             }
         }
     }
+    if (lane < 32 && i < ql) rows[(uint64_t)plane * a.q_len + i] = make_float2(base, sum);
     if (i < (int)a.q_len) {
         T* out = dq + b * a.dq.batch + (uint64_t)i * a.dq.row + h * a.dq.head;
         if (mine == 0) {
 #pragma unroll
             for (int d = 0; d < DIM / 32; ++d) acc[d] = 0.0f;
         }
-        store_row(out, acc, a.scale, a.head_dim);
+        store_row(out, acc, a.scale * drop_scale, a.head_dim);
     }
 }
 
+// The workgroup's four waves: `GROUPS` groups of 32 keys, each `HALVES` times, once for every
+// part of a tile of queries.
+template <int DIM_> struct KeysShape;
+template <> struct KeysShape<64> { static constexpr int GROUPS = 4, HALVES = 1, TILE = 64; };
+template <> struct KeysShape<128> { static constexpr int GROUPS = 2, HALVES = 2, TILE = 128; };
+
 template <typename T, int DIM, bool DROP>
 __global__ __launch_bounds__(BWD_THREADS, DIM == 64 ? 2 : 1) void attention_backward_keys_kernel(
-    AttentionArgs a, const T* q, const T* k, const T* v, const float* lse, const T* d_o, const float* rows_d, T* dk, T* dv,
-    uint32_t blocks) {
-    using Tile = RowTile<T, DIM, BWD_TILE, BWD_THREADS>;
-    __shared__ __attribute__((aligned(1024))) char shared[4 * Tile::BYTES];
-    __shared__ float2 rows_of[2][BWD_TILE];                    // log-sum-exp and D of the tile's rows
-    const uint32_t place = near_place(blockIdx.x, gridDim.x), b = place / blocks / a.kv_heads, kv = place / blocks % a.kv_heads;
+    AttentionArgs a, const T* q, const T* k, const T* v, const T* d_o, const RowNumbers* rows, T* dk, T* dv, uint32_t blocks) {
+    using Shape = KeysShape<DIM>;
+    constexpr int TILE = Shape::TILE, OWN = TILE / Shape::HALVES;          // queries of a tile, of a wave's part
+    using Tile = RowTile<T, DIM, TILE, BWD_THREADS>;
+    constexpr int NUMBERS = TILE * (int)sizeof(RowNumbers) < 1024 ? 1024 : TILE * (int)sizeof(RowNumbers);
+    constexpr int BUFFER = 2 * Tile::BYTES + NUMBERS;
+    __shared__ __attribute__((aligned(1024))) char shared[2 * BUFFER];
+    const Place at = place_of(blockIdx.x, a.batch * a.kv_heads, blocks);
+    const uint32_t b = at.unit / a.kv_heads, kv = at.unit % a.kv_heads;
     const uint32_t wave = uniform(threadIdx.x / WAVE), lane = threadIdx.x % WAVE;
+    const uint32_t part = wave / Shape::GROUPS;
     const int ql = sequence_length(a.q_lens, b, a.q_len), kl = sequence_length(a.k_lens, b, a.k_len);
-    const int k0 = place % blocks * BWD_ROWS, w0 = k0 + 32 * (int)wave, j = w0 + (int)(lane % 32);
-    // the first query that sees key j, and the first that sees any
+    const int k0 = at.in * (Shape::GROUPS * 32), w0 = k0 + 32 * (int)(wave % Shape::GROUPS), j = w0 + (int)(lane % 32);
+    // the first query that sees a key: any key, the workgroup's, the wave's first and last, the lane's
     const auto first_for = [&](int key) { const int n = a.causal ? key - (kl - ql) : 0; return n < 0 ? 0 : n; };
-    const int lo = first_for(0), begin = first_for(k0) / BWD_TILE * BWD_TILE;
+    const int lo = first_for(0), begin = first_for(k0) / TILE * TILE;
     const int mine = j < kl ? first_for(j) : ql;
-    const int wave_least = w0 < kl ? first_for(w0) : ql + BWD_TILE, wave_most = w0 + 31 < kl ? first_for(w0 + 31) : ql;
-    const int tiles = k0 < kl && begin < ql ? (ql - begin + BWD_TILE - 1) / BWD_TILE : 0;
+    const int wave_least = w0 < kl ? first_for(w0) : ql + TILE, wave_most = w0 + 31 < kl ? first_for(w0 + 31) : ql;
+    const int tiles = k0 < kl && begin < ql ? (ql - begin + TILE - 1) / TILE : 0;
+    const float drop_scale = DROP ? a.drop.scale : 1.0f;
 
     f32x16 dkacc[DIM / 32], dvacc[DIM / 32];
 #pragma unroll
     for (int d = 0; d < DIM / 32; ++d) dkacc[d] = dvacc[d] = 0.0f;
     if (tiles > 0) {
+        const uint32_t q_row = (uint32_t)a.q.row * 2, do_row = (uint32_t)a.d_o.row * 2, lds = lds_address(shared);
+        const typename Tile::Places q_at(q_row, a.head_dim), do_at(do_row, a.head_dim);
+        // the tile that is fetched next, head after head of the group
+        uint32_t fetch_head = kv * a.group;
+        int fetch_query = begin;
+        const auto fetch = [&](int turn) {
+            const uint32_t to = lds + turn * BUFFER;
+            Tile::fetch(to, q + b * a.q.batch + fetch_head * a.q.head, q_row, q_at, fetch_query, lo, ql, a.head_dim);
+            Tile::fetch(to + Tile::BYTES, d_o + b * a.d_o.batch + fetch_head * a.d_o.head, do_row, do_at, fetch_query, lo, ql, a.head_dim);
+            const RowNumbers* from = rows + ((uint64_t)b * a.heads + fetch_head) * a.q_len;
+            if (wave == 0) fetch_line(to + 2 * Tile::BYTES, from + fetch_query, from + ql);
+            fetch_query += TILE;
+            if (fetch_query >= ql) {
+                fetch_query = begin;
+                ++fetch_head;
+            }
+        };
+        fetch(0);
         const uint64_t row = j < kl ? j : kl - 1;
         const T* k_row = k + b * a.k.batch + row * a.k.row + kv * a.k.head;
         const T* v_row = v + b * a.v.batch + row * a.v.row + kv * a.v.head;
@@ -160,93 +196,124 @@ __global__ __launch_bounds__(BWD_THREADS, DIM == 64 ? 2 : 1) void attention_back
             kf[s] = row_operand(k_row, s, a.head_dim);
             vf[s] = row_operand(v_row, s, a.head_dim);
         }
+        const TileReads reads = Tile::reads();
         RandomKey key = {0, 0};
         if (DROP) key = random_key(a.seed);
-        const uint32_t q_row = (uint32_t)a.q.row * 2, do_row = (uint32_t)a.d_o.row * 2, lds = lds_address(shared);
-        const typename Tile::Places q_at(q_row, a.head_dim), do_at(do_row, a.head_dim);
-        const auto fetch = [&](int it, int turn) {
-            const uint32_t h = kv * a.group + it / tiles;
-            const int first = begin + it % tiles * BWD_TILE;
-            const uint32_t to = lds + turn * 2 * Tile::BYTES;
-            Tile::fetch(to, q + b * a.q.batch + h * a.q.head, q_row, q_at, first, lo, ql, a.head_dim);
-            Tile::fetch(to + Tile::BYTES, d_o + b * a.d_o.batch + h * a.d_o.head, do_row, do_at, first, lo, ql, a.head_dim);
-            if (threadIdx.x < BWD_TILE) {
-                const int i = first + (int)threadIdx.x;
-                const uint64_t at = ((uint64_t)b * a.heads + h) * a.q_len + (i < lo ? lo : i > ql - 1 ? ql - 1 : i);
-                rows_of[turn][threadIdx.x] = make_float2(lse_log2(lse[at]), rows_d[at]);
-            }
-        };
-        fetch(0, 0);
         const int steps = tiles * (int)a.group;
+        uint32_t plane = b * a.heads + kv * a.group;
+        int query0 = begin;
         for (int it = 0, turn = 0; it < steps; ++it, turn ^= 1) {
             fetched();
-            const char* qt = shared + turn * 2 * Tile::BYTES;
+            const char* qt = shared + turn * BUFFER;
             const char* dt = qt + Tile::BYTES;
-            if (it + 1 < steps) fetch(it + 1, turn ^ 1);
-            const uint32_t plane = b * a.heads + kv * a.group + it / tiles;
-            const int query0 = begin + it % tiles * BWD_TILE;
-            if (query0 + BWD_TILE <= wave_least) continue;
-            const bool masked = query0 < wave_most || query0 + BWD_TILE > ql;
+            const RowNumbers* numbers = reinterpret_cast<const RowNumbers*>(dt + Tile::BYTES);
+            if (it + 1 < steps) fetch(turn ^ 1);
+            const int own0 = query0 + (int)part * OWN;
+            if (own0 + OWN > wave_least && own0 < ql) {
+                const bool masked = own0 < wave_most || own0 + OWN > ql;
+#pragma unroll 1
+                for (int n = 0; n < OWN / 32; ++n) {
+                    const uint32_t slot0 = part * OWN + 32 * n;
+                    f32x16 s = 0.0f, dp = 0.0f;
 #pragma unroll
-            for (int n = 0; n < BWD_TILE / 32; ++n) {
-                f32x16 s = 0.0f, dp = 0.0f;
-#pragma unroll
-                for (int e = 0; e < DIM / 16; ++e) s = mfma(Tile::rows(qt, 32 * n, e), kf[e], s);
-#pragma unroll
-                for (int e = 0; e < DIM / 16; ++e) dp = mfma(Tile::rows(dt, 32 * n, e), vf[e], dp);
-                uint32_t w[8];
-                if (DROP) kept_queries(w, j, query0 + 32 * n, plane, key, a.site);
-                const int at = 32 * n + 16 * (int)(lane / 32);
-#pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    const float2 ld = rows_of[turn][at + r];
-                    const int i = query0 + at + r;
-                    float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], a.scale_log2, -ld.x));
-                    if (masked) p = i >= mine && i < ql ? p : 0.0f;
-                    float d = dp[r];
-                    s[r] = p;
-                    if (DROP) {
-                        const bool keep = r & 1 ? w[r / 2] < a.drop.bar << 16 : (w[r / 2] & 0xffffu) < a.drop.bar;
-                        d = keep ? d * a.drop.scale : 0.0f;
-                        s[r] = keep ? p * a.drop.scale : 0.0f;
+                    for (int e = 0; e < DIM / 16; ++e) {
+                        s = mfma(Tile::rows(qt, reads, slot0, e), kf[e], s);
+                        dp = mfma(Tile::rows(dt, reads, slot0, e), vf[e], dp);
                     }
-                    dp[r] = p * (d - ld.y);
+                    const float4* number = reinterpret_cast<const float4*>(numbers + slot0 + 16 * (lane / 32));
+                    float few[16];
+#pragma unroll
+                    for (int r = 0; r < 16; r += 2) {
+                        const float4 two = number[r / 2];
+                        s[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], a.scale_log2, -two.x));
+                        s[r + 1] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r + 1], a.scale_log2, -two.z));
+                        few[r] = two.y;
+                        few[r + 1] = two.w;
+                    }
+                    if (masked) {
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) {
+                            const int i = own0 + 32 * n + 16 * (int)(lane / 32) + r;
+                            s[r] = i >= mine && i < ql ? s[r] : 0.0f;
+                        }
+                    }
+                    if (DROP) {
+                        uint32_t w[8];
+                        kept_queries(w, j, own0 + 32 * n, plane, key, a.site);
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) {
+                            const bool keep = r & 1 ? w[r / 2] < a.drop.bar << 16 : (w[r / 2] & 0xffffu) < a.drop.bar;
+                            const float p = s[r];
+                            s[r] = keep ? p : 0.0f;
+                            dp[r] = p * ((keep ? dp[r] : 0.0f) - few[r]);
+                        }
+                    } else {
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) dp[r] = s[r] * (dp[r] - few[r]);
+                    }
+#pragma unroll
+                    for (int t = 0; t < 2; ++t) {
+                        const frag<T> p = to_operand<T>(s, t), ds = to_operand<T>(dp, t);
+#pragma unroll
+                        for (int d = 0; d < DIM / 32; ++d) {
+                            dvacc[d] = mfma(Tile::columns(dt, reads, slot0, d, t), p, dvacc[d]);
+                            dkacc[d] = mfma(Tile::columns(qt, reads, slot0, d, t), ds, dkacc[d]);
+                        }
+                    }
                 }
+            }
+            query0 += TILE;
+            if (query0 >= ql) {
+                query0 = begin;
+                ++plane;
+            }
+        }
+        if (Shape::HALVES == 2) {                              // the waves of the other part hand over their sums
+            f32x16* sums = reinterpret_cast<f32x16*>(shared) + (wave % Shape::GROUPS) * (DIM / 16) * WAVE + lane;
+            __syncthreads();
+            if (part == 1) {
 #pragma unroll
-                for (int t = 0; t < 2; ++t) {
-                    const frag<T> p = to_operand<T>(s, t), ds = to_operand<T>(dp, t);
+                for (int d = 0; d < DIM / 32; ++d) {
+                    sums[2 * d * WAVE] = dkacc[d];
+                    sums[(2 * d + 1) * WAVE] = dvacc[d];
+                }
+            }
+            __syncthreads();
+            if (part == 0) {
 #pragma unroll
-                    for (int d = 0; d < DIM / 32; ++d) dvacc[d] = mfma(Tile::columns(dt, 32 * n, d, t), p, dvacc[d]);
-#pragma unroll
-                    for (int d = 0; d < DIM / 32; ++d) dkacc[d] = mfma(Tile::columns(qt, 32 * n, d, t), ds, dkacc[d]);
+                for (int d = 0; d < DIM / 32; ++d) {
+                    dkacc[d] += sums[2 * d * WAVE];
+                    dvacc[d] += sums[(2 * d + 1) * WAVE];
                 }
             }
         }
     }
-    if (j < (int)a.k_len) {
+    if (part == 0 && j < (int)a.k_len) {
         if (mine >= ql) {
 #pragma unroll
             for (int d = 0; d < DIM / 32; ++d) dkacc[d] = dvacc[d] = 0.0f;
         }
-        store_row(dk + b * a.dk.batch + (uint64_t)j * a.dk.row + kv * a.dk.head, dkacc, a.scale, a.head_dim);
-        store_row(dv + b * a.dv.batch + (uint64_t)j * a.dv.row + kv * a.dv.head, dvacc, 1.0f, a.head_dim);
+        store_row(dk + b * a.dk.batch + (uint64_t)j * a.dk.row + kv * a.dk.head, dkacc, a.scale * drop_scale, a.head_dim);
+        store_row(dv + b * a.dv.batch + (uint64_t)j * a.dv.row + kv * a.dv.head, dvacc, drop_scale, a.head_dim);
     }
 }
 
-struct BackwardPointers { const void *q, *k, *v, *o, *d_o; const float* lse; void *dq, *dk, *dv; float* rows_d; };
+struct BackwardPointers { const void *q, *k, *v, *o, *d_o; const float* lse; void *dq, *dk, *dv; RowNumbers* rows; };
 
 template <typename T, int DIM, bool DROP>
 static void launch_backward(const AttentionArgs& a, const BackwardPointers& p, hipStream_t s) {
     if (a.q_len) {
-        const uint32_t blocks = (a.q_len + BWD_ROWS - 1) / BWD_ROWS;
-        hipLaunchKernelGGL((attention_backward_queries_kernel<T, DIM, DROP>), dim3(blocks * a.batch * a.heads), dim3(BWD_THREADS), 0, s, a, (const T*)p.q,
-                           (const T*)p.k, (const T*)p.v, (const T*)p.o, p.lse, (const T*)p.d_o, (T*)p.dq, p.rows_d, blocks);
+        const uint32_t blocks = (a.q_len + BWD_QUERIES - 1) / BWD_QUERIES;
+        hipLaunchKernelGGL((attention_backward_queries_kernel<T, DIM, DROP>), dim3(blocks * a.batch * a.heads), dim3(BWD_THREADS), 0, s,
+                           a, (const T*)p.q, (const T*)p.k, (const T*)p.v, (const T*)p.o, p.lse, (const T*)p.d_o, (T*)p.dq, p.rows, blocks);
     }
     if (a.k_len) {
-        const uint32_t blocks = (a.k_len + BWD_ROWS - 1) / BWD_ROWS;
+        constexpr uint32_t KEYS = KeysShape<DIM>::GROUPS * 32;
+        const uint32_t blocks = (a.k_len + KEYS - 1) / KEYS;
         timing_before(s);
-        hipLaunchKernelGGL((attention_backward_keys_kernel<T, DIM, DROP>), dim3(blocks * a.batch * a.kv_heads), dim3(BWD_THREADS), 0, s, a, (const T*)p.q,
-                           (const T*)p.k, (const T*)p.v, p.lse, (const T*)p.d_o, (const float*)p.rows_d, (T*)p.dk, (T*)p.dv, blocks);
+        hipLaunchKernelGGL((attention_backward_keys_kernel<T, DIM, DROP>), dim3(blocks * a.batch * a.kv_heads), dim3(BWD_THREADS), 0, s,
+                           a, (const T*)p.q, (const T*)p.k, (const T*)p.v, (const T*)p.d_o, (const RowNumbers*)p.rows, (T*)p.dk, (T*)p.dv,
+                           blocks);
         timing_after(s);
     }
 }
@@ -273,7 +340,7 @@ extern "C" int okt_attention_backward(const okt_attention* op, const void* d_q, 
         if (!aligned(p, 16)) return OKT_ERR_INVALID_ARG;
     if (!aligned(d_lse, 4)) return OKT_ERR_INVALID_ARG;
     if (!d_ws || !aligned(d_ws, 256) || ws_bytes < attention_ws_bytes(a.batch, a.heads, a.q_len)) return OKT_ERR_WORKSPACE;
-    const BackwardPointers p = {d_q, d_k, d_v, d_o, d_do, d_lse, d_dq_out, d_dk_out, d_dv_out, (float*)d_ws};
+    const BackwardPointers p = {d_q, d_k, d_v, d_o, d_do, d_lse, d_dq_out, d_dk_out, d_dv_out, (RowNumbers*)d_ws};
     const hipStream_t s = (hipStream_t)stream;
     if (op->dtype == OKT_BF16) launch_backward_shape<__bf16>(a, p, s);
     else launch_backward_shape<_Float16>(a, p, s);

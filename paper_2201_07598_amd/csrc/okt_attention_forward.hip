@@ -18,11 +18,11 @@ __global__ __launch_bounds__(FWD_THREADS, 2) void attention_forward_kernel(Atten
                                                                            T* o, float* lse, uint32_t blocks) {
     using Tile = RowTile<T, DIM, FWD_KEYS, FWD_THREADS>;
     __shared__ __attribute__((aligned(1024))) char shared[4 * Tile::BYTES];
-    const uint32_t place = near_place(blockIdx.x, gridDim.x), plane = place / blocks;
-    const uint32_t b = plane / a.heads, h = plane % a.heads, kv = h / a.group;
+    const Place at = place_of(blockIdx.x, a.batch * a.kv_heads, a.group * blocks);
+    const uint32_t b = at.unit / a.kv_heads, kv = at.unit % a.kv_heads, h = kv * a.group + at.in / blocks, plane = b * a.heads + h;
     const uint32_t wave = uniform(threadIdx.x / WAVE), lane = threadIdx.x % WAVE;
     const int ql = sequence_length(a.q_lens, b, a.q_len), kl = sequence_length(a.k_lens, b, a.k_len);
-    const int q0 = (blocks - 1 - place % blocks) * FWD_QUERIES, w0 = q0 + 32 * (int)wave, i = w0 + (int)(lane % 32);
+    const int q0 = (blocks - 1 - at.in % blocks) * FWD_QUERIES, w0 = q0 + 32 * (int)wave, i = w0 + (int)(lane % 32);
 
     // keys that a query sees; the most of the workgroup's queries, the least and most of the wave's
     const int past = kl - ql + 1;
@@ -47,6 +47,7 @@ __global__ __launch_bounds__(FWD_THREADS, 2) void attention_forward_kernel(Atten
         frag<T> qf[DIM / 16];
 #pragma unroll
         for (int s = 0; s < DIM / 16; ++s) qf[s] = row_operand(qrow, s, a.head_dim);
+        const TileReads reads = Tile::reads();
         RandomKey key = {0, 0};
         if (DROP) key = random_key(a.seed);
         for (int key0 = 0, turn = 0; key0 < keys; key0 += FWD_KEYS, turn ^= 1) {
@@ -64,7 +65,7 @@ __global__ __launch_bounds__(FWD_THREADS, 2) void attention_forward_kernel(Atten
             for (int n = 0; n < FWD_KEYS / 32; ++n) {
                 s[n] = 0.0f;
 #pragma unroll
-                for (int e = 0; e < DIM / 16; ++e) s[n] = mfma(Tile::rows(kt, 32 * n, e), qf[e], s[n]);
+                for (int e = 0; e < DIM / 16; ++e) s[n] = mfma(Tile::rows(kt, reads, 32 * n, e), qf[e], s[n]);
             }
             if (key0 + FWD_KEYS > wave_least) {                // some of the tile is hidden from some lane
 #pragma unroll
@@ -109,7 +110,7 @@ __global__ __launch_bounds__(FWD_THREADS, 2) void attention_forward_kernel(Atten
                 for (int t = 0; t < 2; ++t) {
                     const frag<T> p = to_operand<T>(s[n], t);
 #pragma unroll
-                    for (int d = 0; d < DIM / 32; ++d) acc[d] = mfma(Tile::columns(vt, 32 * n, d, t), p, acc[d]);
+                    for (int d = 0; d < DIM / 32; ++d) acc[d] = mfma(Tile::columns(vt, reads, 32 * n, d, t), p, acc[d]);
                 }
             }
         }
@@ -170,7 +171,7 @@ bool attention_args(const okt_attention* op, bool backward, AttentionArgs& a) {
 }
 
 size_t attention_ws_bytes(uint32_t batch, uint32_t heads, uint32_t q_len) {
-    return ((size_t)batch * heads * q_len * sizeof(float) + 255) & ~(size_t)255;      // D of every row
+    return ((size_t)batch * heads * q_len * 2 * sizeof(float) + 255) & ~(size_t)255;      // two numbers of every row
 }
 
 }  // namespace okt

@@ -38,7 +38,7 @@ __device__ __forceinline__ typename Eight<T>::vec raw_eight(const T* p) {
     return reinterpret_cast<const typename Eight<T>::any*>(p)->v;
 }
 
-// Drops the first `skip` (1 or more) of eight elements, moves the rest to the front and puts zeros
+// Drops the first `skip` (1 to 7) of eight elements, moves the rest to the front and puts zeros
 // behind.  The ragged end of a row is the last eight elements of the row moved so: a
 // load for each element, merged one by one, waits for memory each time.
 template <typename T>
@@ -60,17 +60,22 @@ __device__ __forceinline__ typename Eight<T>::vec skip_elements(typename Eight<T
             w[i] = skip & 1 ? from : w[i];
         }
     }
-#pragma unroll
-    for (int i = 0; i < WORDS; ++i) w[i] = skip >= 8 ? 0 : w[i];
     return __builtin_bit_cast(typename Eight<T>::vec, w);
 }
 
-// Writes the first `count` of them.
+// Writes the first `count` (0 to 7) of them, in pieces of four, two and one.
 template <typename T>
 __device__ __forceinline__ void store_some(T* p, f32x8 v, int count) {
+    struct __attribute__((packed, aligned(sizeof(T)))) Four { T v[4]; };
+    struct __attribute__((packed, aligned(sizeof(T)))) Two { T v[2]; };
+    T e[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-        if (i < count) p[i] = (T)v[i];
+    for (int i = 0; i < 7; ++i) e[i] = (T)v[i];
+    if (count & 4) *reinterpret_cast<Four*>(p) = Four{{e[0], e[1], e[2], e[3]}};
+    const T a = count & 4 ? e[4] : e[0], b = count & 4 ? e[5] : e[1], c = count & 4 ? e[6] : e[2];
+    p += count & 4;
+    if (count & 2) *reinterpret_cast<Two*>(p) = Two{{a, b}};
+    if (count & 1) p[count & 2] = count & 2 ? c : a;
 }
 
 inline bool known_dtype(int dtype) { return dtype == OKT_F32 || dtype == OKT_BF16 || dtype == OKT_F16; }

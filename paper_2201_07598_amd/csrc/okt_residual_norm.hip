@@ -113,6 +113,15 @@ __device__ __forceinline__ float wave_sum_f32(float v) {
     return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
 }
 
+// Clears the slots of row_sums, before its first call.
+template <typename L>
+__device__ __forceinline__ void clear_slots(float2* slots) {
+    if (!L::one) {
+        if (threadIdx.x < L::slots) slots[threadIdx.x] = make_float2(0.0f, 0.0f);
+        __syncthreads();
+    }
+}
+
 // How a kernel holds rows: ONE wave each, or a workgroup of up to THREADS each; VECS groups
 // of eight columns a thread.
 template <bool ONE, int VECS, int THREADS>
@@ -132,7 +141,8 @@ __device__ __forceinline__ void row_sums(float& a, float& b, float2* slots, int&
         if (threadIdx.x % WAVE == 0) s[threadIdx.x / WAVE] = make_float2(a, b);
         __syncthreads();
         a = b = 0.0f;
-        for (uint32_t w = 0; w < blockDim.x / WAVE; ++w) {
+#pragma unroll
+        for (int w = 0; w < L::threads / WAVE; ++w) {          // slots of waves there are not hold 0
             a += s[w].x;
             b += s[w].y;
         }
@@ -175,8 +185,8 @@ struct Columns {
     __device__ __forceinline__ void open(f32x8 (&to)[L::vecs], Raw<T> r) const {
 #pragma unroll
         for (int v = 0; v < L::vecs; ++v) {
-            if (skip[v]) r.v[v] = skip_elements<T>(r.v[v], skip[v]);
-            to[v] = __builtin_convertvector(r.v[v], f32x8);
+            if (skip[v] - 1u < 7u) r.v[v] = skip_elements<T>(r.v[v], skip[v]);
+            to[v] = skip[v] < 8 ? __builtin_convertvector(r.v[v], f32x8) : 0.0f;
         }
     }
     template <typename T>
@@ -188,7 +198,7 @@ struct Columns {
         for (int v = 0; v < L::vecs; ++v) {
             T* p = row + group(v) * 8;
             if (!skip[v]) store_eight(p, from[v]);
-            else store_some(p, from[v], count(v));
+            else if (skip[v] < 8) store_some(p, from[v], 8 - (int)skip[v]);
         }
     }
 };
@@ -235,6 +245,7 @@ __global__ __launch_bounds__(L::threads) void norm_forward_kernel(NormArgs a, co
                                                                                    T* y) {
     constexpr int AT_ONCE = L::one ? L::threads / WAVE : 1;
     __shared__ float2 slots[L::slots];
+    clear_slots<L>(slots);
     int turn = 0;
     const Columns<L> cols(L::one ? threadIdx.x % WAVE : threadIdx.x, L::one ? WAVE : blockDim.x, a.width);
     const bool drops = a.drop.bar != 65536u;
@@ -289,20 +300,43 @@ __global__ __launch_bounds__(L::threads) void norm_forward_kernel(NormArgs a, co
     }
 }
 
+// A sum over rows for each column of a thread: in registers, or in LDS where a row takes 1024 threads,
+// which have 128 registers each (in scratch memory instead: 4,099 rows of 8192, two norms and a gate, 320 us).
+template <typename L, bool LDS>
+struct ColumnSums {
+    f32x8 r[LDS ? 1 : L::vecs];
+    float* at;                                          // this thread's eight columns of the first group
+    __device__ __forceinline__ explicit ColumnSums(float* shared) : at(shared + threadIdx.x * 8) { clear(); }
+    __device__ __forceinline__ void clear() {
+#pragma unroll
+        for (int i = 0; i < L::vecs; ++i) {
+            if (LDS) *reinterpret_cast<f32x8*>(at + i * L::threads * 8) = 0.0f;
+            else r[LDS ? 0 : i] = 0.0f;
+        }
+    }
+    __device__ __forceinline__ void add(int i, f32x8 v) {
+        if (LDS) *reinterpret_cast<f32x8*>(at + i * L::threads * 8) += v;
+        else r[LDS ? 0 : i] += v;
+    }
+    __device__ __forceinline__ void get(f32x8 (&to)[L::vecs]) const {
+#pragma unroll
+        for (int i = 0; i < L::vecs; ++i) to[i] = LDS ? *reinterpret_cast<const f32x8*>(at + i * L::threads * 8) : r[LDS ? 0 : i];
+    }
+};
+
 // The gradient of a norm's input from the gradient of its output (in place), and what this
 // row adds to the gradients of its weight and bias.
-template <typename L>
+template <typename L, bool BIAS, typename W, typename B>
 __device__ __forceinline__ void norm_input_gradient(f32x8 (&d)[L::vecs], const f32x8 (&v)[L::vecs], const f32x8 (&w)[L::vecs],
-                                                    float mean, float r, f32x8 (&dw)[L::vecs], f32x8 (&db)[L::vecs],
-                                                    const NormArgs& a, float2* slots, int& turn) {
+                                                    float mean, float r, W& dw, B& db, const NormArgs& a, float2* slots, int& turn) {
     float plain = 0.0f, along = 0.0f;
     f32x8 xhat[L::vecs];
 #pragma unroll
     for (int i = 0; i < L::vecs; ++i) {
         xhat[i] = (v[i] - mean) * r;
         const f32x8 p = d[i] * xhat[i];
-        dw[i] += p;
-        db[i] += d[i];
+        dw.add(i, p);
+        if (BIAS) db.add(i, d[i]);
         d[i] *= w[i];
         plain += sum_eight(d[i]);
         along += sum_eight(p * w[i]);
@@ -315,8 +349,10 @@ __device__ __forceinline__ void norm_input_gradient(f32x8 (&d)[L::vecs], const f
 }
 
 // Adds what the waves of a workgroup that work on different rows hold, and writes it out.
-template <typename L>
-__device__ __forceinline__ void put_sums(f32x8 (&v)[L::vecs], const Columns<L>& cols, float* to, float* shared) {
+template <typename L, typename S>
+__device__ __forceinline__ void put_sums(const S& sums, const Columns<L>& cols, float* to, float* shared) {
+    f32x8 v[L::vecs];
+    sums.get(v);
     if (L::one) {
         constexpr int SPAN = WAVE * L::vecs * 8;
         const int wave = threadIdx.x / WAVE;
@@ -331,25 +367,27 @@ __device__ __forceinline__ void put_sums(f32x8 (&v)[L::vecs], const Columns<L>& 
     }
 }
 
-// ALL: with a norm after the block or a gate; without, the registers they take are free.
-template <typename T, typename L, bool ALL>
-__global__ __launch_bounds__(L::threads, L::threads == 512 ? 3 : 1) void norm_backward_kernel(
+// ALL: with a norm after the block or a gate; BIAS: a norm has one.  Without, the registers
+// they take are free.
+template <typename T, typename L, bool ALL, bool BIAS>
+__global__ __launch_bounds__(L::threads) void norm_backward_kernel(
     NormArgs a, const T* u, const T* h, const T* dh, const T* dy, T* dx, T* du) {
     constexpr int AT_ONCE = L::one ? L::threads / WAVE : 1;
     __shared__ float2 slots[L::slots];
-    __shared__ __attribute__((aligned(32))) float shared[L::one ? L::threads * L::vecs * 8 : 1];
+    clear_slots<L>(slots);
+    constexpr bool IN_LDS = ALL && L::threads == 1024;
+    __shared__ __attribute__((aligned(32))) float shared[L::one ? L::threads * L::vecs * 8 : IN_LDS ? 2 * L::threads * L::vecs * 8 : 8];
     int turn = 0;
     const Columns<L> cols(L::one ? threadIdx.x % WAVE : threadIdx.x, L::one ? WAVE : blockDim.x, a.width);
     const bool drops = a.drop.bar != 65536u;
     RandomKey key = {0, 0};
     if (drops) key = random_key(a.seed);
-    f32x8 pre_w[L::vecs], post_w[L::vecs], post_b[L::vecs], dpre_w[L::vecs], dpre_b[L::vecs], dpost_w[L::vecs], dpost_b[L::vecs],
-        dgate[L::vecs];
-#pragma unroll
-    for (int i = 0; i < L::vecs; ++i) dpre_w[i] = dpre_b[i] = dpost_w[i] = dpost_b[i] = dgate[i] = 0.0f;
+    f32x8 pre_w[L::vecs], post_w[L::vecs], post_b[L::vecs];
+    ColumnSums<L, false> dpre_w(shared), dpre_b(shared), dpost_b(shared);
+    ColumnSums<L, IN_LDS> dpost_w(shared), dgate(shared + (IN_LDS ? L::threads * L::vecs * 8 : 0));
     if (a.pre_w) cols.load(pre_w, a.pre_w);
     if (ALL && a.post_w) cols.load(post_w, a.post_w);
-    if (ALL && a.post_b) cols.load(post_b, a.post_b);
+    if (ALL && BIAS && a.post_b) cols.load(post_b, a.post_b);
 
     const uint64_t gate0 = a.parts > 1 ? blockIdx.x / a.parts : blockIdx.x * (a.chunk / a.rows_per_gate);
     uint64_t begin = a.parts > 1 ? gate0 * a.rows_per_gate + blockIdx.x % a.parts * a.chunk : blockIdx.x * a.chunk;
@@ -390,7 +428,7 @@ __global__ __launch_bounds__(L::threads, L::threads == 512 ? 3 : 1) void norm_ba
             }
             if (row + AT_ONCE < end) fetch(row + AT_ONCE);
             if (a.pre_w) {
-                norm_input_gradient<L>(o, v, pre_w, st.z, st.w, dpre_w, dpre_b, a, slots, turn);
+                norm_input_gradient<L, BIAS>(o, v, pre_w, st.z, st.w, dpre_w, dpre_b, a, slots, turn);
 #pragma unroll
                 for (int i = 0; i < L::vecs; ++i) d[i] += o[i];
             }
@@ -404,20 +442,19 @@ __global__ __launch_bounds__(L::threads, L::threads == 512 ? 3 : 1) void norm_ba
                     for (int i = 0; i < L::vecs; ++i) {
                         f32x8 s = su[i];
                         if (a.post_w) s = (s - st.x) * st.y * post_w[i];
-                        if (a.post_b) s += post_b[i];
-                        dgate[i] += d[i] * s;       // d holds the mask and its scale already
+                        if (BIAS && a.post_b) s += post_b[i];
+                        dgate.add(i, d[i] * s);       // d holds the mask and its scale already
                         d[i] *= g[i];
                     }
                 }
-                if (a.post_w) norm_input_gradient<L>(d, su, post_w, st.x, st.y, dpost_w, dpost_b, a, slots, turn);
+                if (a.post_w) norm_input_gradient<L, BIAS>(d, su, post_w, st.x, st.y, dpost_w, dpost_b, a, slots, turn);
             }
             cols.store(du + row * a.du_stride, d);
         }
         if (ALL && a.dgate) {
             float* to = a.parts > 1 ? a.partial + (4 * a.groups + blockIdx.x) * a.width : a.dgate + gate * a.width;
             put_sums<L>(dgate, cols, to, shared);
-#pragma unroll
-            for (int i = 0; i < L::vecs; ++i) dgate[i] = 0.0f;
+            dgate.clear();
         }
         begin = end > begin ? end : begin;
         if (begin >= last) break;
@@ -425,11 +462,11 @@ __global__ __launch_bounds__(L::threads, L::threads == 512 ? 3 : 1) void norm_ba
     const auto at = [&](int sum) { return a.partial + (sum * a.groups + blockIdx.x) * a.width; };
     if (a.pre_w) {
         put_sums<L>(dpre_w, cols, at(0), shared);
-        if (a.pre_b) put_sums<L>(dpre_b, cols, at(1), shared);
+        if (BIAS && a.pre_b) put_sums<L>(dpre_b, cols, at(1), shared);
     }
     if (ALL && a.post_w) {
         put_sums<L>(dpost_w, cols, at(2), shared);
-        if (a.post_b) put_sums<L>(dpost_b, cols, at(3), shared);
+        if (BIAS && a.post_b) put_sums<L>(dpost_b, cols, at(3), shared);
     }
 }
 
@@ -511,14 +548,14 @@ static void launch_norm(const NormArgs& a, const NormPointers& p, bool backward,
     const dim3 grid(groups), block(threads);
     if (!backward) {
         hipLaunchKernelGGL((norm_forward_kernel<T, L>), grid, block, 0, s, a, (const T*)p.u, (const T*)p.x, (T*)p.out_h, (T*)p.out_y);
-    } else if (a.post_w || a.gate) {
-        if constexpr (!(L::one && L::vecs == 2))           // norm_shape gives a gated row another one
-        hipLaunchKernelGGL((norm_backward_kernel<T, L, true>), grid, block, 0, s, a, (const T*)p.u, (const T*)p.h,
-                           (const T*)p.dh, (const T*)p.dy, (T*)p.dx, (T*)p.du);
-    } else {
-        hipLaunchKernelGGL((norm_backward_kernel<T, L, false>), grid, block, 0, s, a, (const T*)p.u, (const T*)p.h,
-                           (const T*)p.dh, (const T*)p.dy, (T*)p.dx, (T*)p.du);
+        return;
     }
+    const bool bias = a.post_b || a.pre_b;
+    auto* kernel = bias ? norm_backward_kernel<T, L, false, true> : norm_backward_kernel<T, L, false, false>;
+    if constexpr (!(L::one && L::vecs == 2)) {                 // norm_shape gives a gated row another layout
+        if (a.post_w || a.gate) kernel = bias ? norm_backward_kernel<T, L, true, true> : norm_backward_kernel<T, L, true, false>;
+    }
+    hipLaunchKernelGGL(kernel, grid, block, 0, s, a, (const T*)p.u, (const T*)p.h, (const T*)p.dh, (const T*)p.dy, (T*)p.dx, (T*)p.du);
 }
 
 template <typename T>
