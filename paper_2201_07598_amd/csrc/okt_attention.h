@@ -269,6 +269,61 @@ __device__ __forceinline__ void kept_queries(uint32_t (&w)[8], uint32_t key_inde
     }
 }
 
+// ------------------------------------------------------------------ work split over the long axis
+//
+// A workgroup owns a block of rows and passes over the other axis; where blocks are few, each
+// is dealt to several workgroups that pass over a part each and leave fp32 sums in the
+// workspace, which another launch joins in a fixed order.
+
+// Stores a transposed C tile as fp32: lane's row of DIM floats.
+template <int TILES>
+__device__ __forceinline__ void store_partial(float* row, const f32x16 (&c)[TILES], float scale) {
+#pragma unroll
+    for (int dt = 0; dt < TILES; ++dt)
+#pragma unroll
+        for (int a = 0; a < 4; ++a)
+            *reinterpret_cast<float4*>(row + 32 * dt + 8 * a + 4 * (threadIdx.x % WAVE / 32)) = make_float4(
+                c[dt][4 * a] * scale, c[dt][4 * a + 1] * scale, c[dt][4 * a + 2] * scale, c[dt][4 * a + 3] * scale);
+}
+
+// Steps [first, last) of `steps` that part `part` takes; part 0 takes step 0 if there is one.
+struct Part { int first, last; };
+__device__ __forceinline__ Part part_of(int steps, uint32_t part, uint32_t parts) {
+    const auto cut = [&](uint32_t p) { return (int)(((uint64_t)steps * p + parts - 1) / parts); };
+    return parts == 1 ? Part{0, steps} : Part{cut(part), cut(part + 1)};
+}
+
+// How many parts: enough to give every CU two workgroups, none of fewer than `least` steps,
+// whose time has to be worth the second launch (some 5 us).
+constexpr uint32_t PART_MAX = 32;
+inline uint32_t parts_for(uint64_t workgroups, uint64_t steps, uint32_t least) {
+    constexpr uint64_t WANTED = 512;
+    if (workgroups == 0 || workgroups * 2 > WANTED) return 1;
+    uint64_t n = (WANTED + workgroups - 1) / workgroups;
+    if (n > steps / least) n = steps / least;
+    if (n > PART_MAX) n = PART_MAX;
+    return n ? (uint32_t)n : 1;
+}
+
+// The launches of a call and the parts of the workspace, from its sizes alone.
+struct AttentionPlan {
+    uint32_t dim;                                   // 64 or 128
+    uint32_t forward_parts, query_parts, key_parts;
+    size_t rows_at;                                 // backward: two numbers of every row
+    size_t dq_at, dkv_at;                           // backward: partial sums
+    size_t forward_bytes, bytes;
+};
+AttentionPlan attention_plan(uint32_t batch, uint32_t heads, uint32_t kv_heads, uint32_t q_len, uint32_t k_len, uint32_t head_dim);
+
+constexpr uint32_t ATTENTION_QUERIES = 128;         // a workgroup of the forward and the queries' kernels
+constexpr uint32_t ATTENTION_KEYS = 64;             // keys that pass by it together
+
+// The keys' kernel: four waves are GROUPS groups of 32 keys, each HALVES times, once for every
+// part of a tile of TILE queries.
+template <int DIM> struct KeysShape;
+template <> struct KeysShape<64> { static constexpr int GROUPS = 4, HALVES = 1, TILE = 64; };
+template <> struct KeysShape<128> { static constexpr int GROUPS = 2, HALVES = 2, TILE = 128; };
+
 // ------------------------------------------------------------------ arguments
 
 struct Strides { uint64_t batch, row, head; };
@@ -292,9 +347,6 @@ __device__ __forceinline__ int sequence_length(const int32_t* lens, uint32_t b, 
     const int n = lens[b];
     return n < 0 ? 0 : n > (int)most ? (int)most : n;
 }
-
-// Bytes before the backward pass's parts of the workspace end.
-size_t attention_ws_bytes(uint32_t batch, uint32_t heads, uint32_t q_len);
 
 }  // namespace okt
 

@@ -17,8 +17,8 @@
 namespace okt {
 
 constexpr int BWD_THREADS = 256;
-constexpr int BWD_QUERIES = BWD_THREADS / WAVE * 32;  // of a workgroup of the queries' kernel
-constexpr int BWD_KEYS = 64;                          // that pass by it together
+constexpr int BWD_QUERIES = ATTENTION_QUERIES, BWD_KEYS = ATTENTION_KEYS;
+static_assert(BWD_QUERIES == BWD_THREADS / WAVE * 32, "a wave owns 32 queries");
 
 // What the keys' kernel has to know of a query: its log-sum-exp to base 2 (+inf for a row that
 // sees nothing, whose probabilities come out as 0) and D / c.
@@ -27,26 +27,30 @@ typedef float2 RowNumbers;
 template <typename T, int DIM, bool DROP>
 __global__ __launch_bounds__(BWD_THREADS, 2) void attention_backward_queries_kernel(
     AttentionArgs a, const T* q, const T* k, const T* v, const T* o, const float* lse, const T* d_o, T* dq, RowNumbers* rows,
-    uint32_t blocks) {
+    uint32_t blocks, uint32_t parts, float* partial) {
     using Tile = RowTile<T, DIM, BWD_KEYS, BWD_THREADS>;
     __shared__ __attribute__((aligned(1024))) char shared[4 * Tile::BYTES];
-    const Place at = place_of(blockIdx.x, a.batch * a.kv_heads, a.group * blocks);
-    const uint32_t b = at.unit / a.kv_heads, kv = at.unit % a.kv_heads, h = kv * a.group + at.in / blocks, plane = b * a.heads + h;
+    const Place at = place_of(blockIdx.x, a.batch * a.kv_heads, a.group * blocks * parts);
+    const uint32_t part = at.in % parts, block = at.in / parts % blocks;
+    const uint32_t b = at.unit / a.kv_heads, kv = at.unit % a.kv_heads, h = kv * a.group + at.in / parts / blocks, plane = b * a.heads + h;
     const uint32_t wave = uniform(threadIdx.x / WAVE), lane = threadIdx.x % WAVE;
     const int ql = sequence_length(a.q_lens, b, a.q_len), kl = sequence_length(a.k_lens, b, a.k_len);
-    const int q0 = (blocks - 1 - at.in % blocks) * BWD_QUERIES, w0 = q0 + 32 * (int)wave, i = w0 + (int)(lane % 32);
+    const int q0 = (blocks - 1 - block) * BWD_QUERIES, w0 = q0 + 32 * (int)wave, i = w0 + (int)(lane % 32);
     const int past = kl - ql + 1;
     const auto seen = [&](int query) { const int n = query + past; return query >= ql ? 0 : !a.causal || n > kl ? kl : n < 0 ? 0 : n; };
     const int keys = q0 < ql ? seen(q0 + BWD_QUERIES < ql ? q0 + BWD_QUERIES - 1 : ql - 1) : 0;
     const int mine = seen(i), wave_least = w0 + 31 < ql ? seen(w0) : 0;
     const int wave_most = w0 < ql ? seen(w0 + 32 < ql ? w0 + 31 : ql - 1) : 0;
     const float drop_scale = DROP ? a.drop.scale : 1.0f;
+    // the tiles of this part; part 0 also leaves the rows' numbers
+    const Part mine_of = part_of((keys + BWD_KEYS - 1) / BWD_KEYS, part, parts);
+    const int begin = mine_of.first * BWD_KEYS, end = mine_of.last * BWD_KEYS < keys ? mine_of.last * BWD_KEYS : keys;
 
     f32x16 acc[DIM / 32];
     float base = INFINITY, sum = 0.0f;            // log-sum-exp, D / c
 #pragma unroll
     for (int d = 0; d < DIM / 32; ++d) acc[d] = 0.0f;
-    if (keys > 0) {
+    if (begin < end) {
         const T* kb = k + b * a.k.batch + kv * a.k.head;
         const T* vb = v + b * a.v.batch + kv * a.v.head;
         const uint64_t row = i < ql ? i : ql - 1;
@@ -56,8 +60,8 @@ __global__ __launch_bounds__(BWD_THREADS, 2) void attention_backward_queries_ker
         const uint32_t k_row = (uint32_t)a.k.row * 2, v_row = (uint32_t)a.v.row * 2;
         const typename Tile::Places k_at(k_row, a.head_dim), v_at(v_row, a.head_dim);
         const uint32_t lds = lds_address(shared);
-        Tile::fetch(lds, kb, k_row, k_at, 0, 0, kl, a.head_dim);
-        Tile::fetch(lds + Tile::BYTES, vb, v_row, v_at, 0, 0, kl, a.head_dim);
+        Tile::fetch(lds, kb, k_row, k_at, begin, 0, kl, a.head_dim);
+        Tile::fetch(lds + Tile::BYTES, vb, v_row, v_at, begin, 0, kl, a.head_dim);
         frag<T> qf[DIM / 16], df[DIM / 16];
 #pragma unroll
         for (int s = 0; s < DIM / 16; ++s) {
@@ -73,11 +77,11 @@ __global__ __launch_bounds__(BWD_THREADS, 2) void attention_backward_queries_ker
         RandomKey key = {0, 0};
         if (DROP) key = random_key(a.seed);
 
-        for (int key0 = 0, turn = 0; key0 < keys; key0 += BWD_KEYS, turn ^= 1) {
+        for (int key0 = begin, turn = 0; key0 < end; key0 += BWD_KEYS, turn ^= 1) {
             fetched();
             const char* kt = shared + turn * 2 * Tile::BYTES;
             const char* vt = kt + Tile::BYTES;
-            if (key0 + BWD_KEYS < keys) {
+            if (key0 + BWD_KEYS < end) {
                 const uint32_t next = lds + (turn ^ 1) * 2 * Tile::BYTES;
                 Tile::fetch(next, kb, k_row, k_at, key0 + BWD_KEYS, 0, kl, a.head_dim);
                 Tile::fetch(next + Tile::BYTES, vb, v_row, v_at, key0 + BWD_KEYS, 0, kl, a.head_dim);
@@ -125,38 +129,35 @@ __global__ __launch_bounds__(BWD_THREADS, 2) void attention_backward_queries_ker
             }
         }
     }
-    if (lane < 32 && i < ql) rows[(uint64_t)plane * a.q_len + i] = make_float2(base, sum);
+    if (part == 0 && lane < 32 && i < ql) rows[(uint64_t)plane * a.q_len + i] = make_float2(base, sum);
     if (i < (int)a.q_len) {
         T* out = dq + b * a.dq.batch + (uint64_t)i * a.dq.row + h * a.dq.head;
         if (mine == 0) {
 #pragma unroll
             for (int d = 0; d < DIM / 32; ++d) acc[d] = 0.0f;
         }
-        store_row(out, acc, a.scale * drop_scale, a.head_dim);
+        if (parts > 1) store_partial(partial + (((uint64_t)part * a.batch * a.heads + plane) * a.q_len + i) * DIM, acc, a.scale * drop_scale);
+        else store_row(out, acc, a.scale * drop_scale, a.head_dim);
     }
 }
 
-// The workgroup's four waves: `GROUPS` groups of 32 keys, each `HALVES` times, once for every
-// part of a tile of queries.
-template <int DIM_> struct KeysShape;
-template <> struct KeysShape<64> { static constexpr int GROUPS = 4, HALVES = 1, TILE = 64; };
-template <> struct KeysShape<128> { static constexpr int GROUPS = 2, HALVES = 2, TILE = 128; };
-
 template <typename T, int DIM, bool DROP>
 __global__ __launch_bounds__(BWD_THREADS, DIM == 64 ? 2 : 1) void attention_backward_keys_kernel(
-    AttentionArgs a, const T* q, const T* k, const T* v, const T* d_o, const RowNumbers* rows, T* dk, T* dv, uint32_t blocks) {
+    AttentionArgs a, const T* q, const T* k, const T* v, const T* d_o, const RowNumbers* rows, T* dk, T* dv, uint32_t blocks,
+    uint32_t parts, float* partial) {
     using Shape = KeysShape<DIM>;
     constexpr int TILE = Shape::TILE, OWN = TILE / Shape::HALVES;          // queries of a tile, of a wave's part
     using Tile = RowTile<T, DIM, TILE, BWD_THREADS>;
     constexpr int NUMBERS = TILE * (int)sizeof(RowNumbers) < 1024 ? 1024 : TILE * (int)sizeof(RowNumbers);
     constexpr int BUFFER = 2 * Tile::BYTES + NUMBERS;
     __shared__ __attribute__((aligned(1024))) char shared[2 * BUFFER];
-    const Place at = place_of(blockIdx.x, a.batch * a.kv_heads, blocks);
+    const Place at = place_of(blockIdx.x, a.batch * a.kv_heads, blocks * parts);
+    const uint32_t share = at.in % parts;
     const uint32_t b = at.unit / a.kv_heads, kv = at.unit % a.kv_heads;
     const uint32_t wave = uniform(threadIdx.x / WAVE), lane = threadIdx.x % WAVE;
     const uint32_t part = wave / Shape::GROUPS;
     const int ql = sequence_length(a.q_lens, b, a.q_len), kl = sequence_length(a.k_lens, b, a.k_len);
-    const int k0 = at.in * (Shape::GROUPS * 32), w0 = k0 + 32 * (int)(wave % Shape::GROUPS), j = w0 + (int)(lane % 32);
+    const int k0 = at.in / parts * (Shape::GROUPS * 32), w0 = k0 + 32 * (int)(wave % Shape::GROUPS), j = w0 + (int)(lane % 32);
     // the first query that sees a key: any key, the workgroup's, the wave's first and last, the lane's
     const auto first_for = [&](int key) { const int n = a.causal ? key - (kl - ql) : 0; return n < 0 ? 0 : n; };
     const int lo = first_for(0), begin = first_for(k0) / TILE * TILE;
@@ -164,16 +165,18 @@ __global__ __launch_bounds__(BWD_THREADS, DIM == 64 ? 2 : 1) void attention_back
     const int wave_least = w0 < kl ? first_for(w0) : ql + TILE, wave_most = w0 + 31 < kl ? first_for(w0 + 31) : ql;
     const int tiles = k0 < kl && begin < ql ? (ql - begin + TILE - 1) / TILE : 0;
     const float drop_scale = DROP ? a.drop.scale : 1.0f;
+    // the steps of this share: the tiles of every head of the group, head after head
+    const Part steps = part_of(tiles * (int)a.group, share, parts);
 
     f32x16 dkacc[DIM / 32], dvacc[DIM / 32];
 #pragma unroll
     for (int d = 0; d < DIM / 32; ++d) dkacc[d] = dvacc[d] = 0.0f;
-    if (tiles > 0) {
+    if (steps.first < steps.last) {
         const uint32_t q_row = (uint32_t)a.q.row * 2, do_row = (uint32_t)a.d_o.row * 2, lds = lds_address(shared);
         const typename Tile::Places q_at(q_row, a.head_dim), do_at(do_row, a.head_dim);
         // the tile that is fetched next, head after head of the group
-        uint32_t fetch_head = kv * a.group;
-        int fetch_query = begin;
+        uint32_t fetch_head = kv * a.group + steps.first / tiles;
+        int fetch_query = begin + steps.first % tiles * TILE;
         const auto fetch = [&](int turn) {
             const uint32_t to = lds + turn * BUFFER;
             Tile::fetch(to, q + b * a.q.batch + fetch_head * a.q.head, q_row, q_at, fetch_query, lo, ql, a.head_dim);
@@ -199,15 +202,14 @@ __global__ __launch_bounds__(BWD_THREADS, DIM == 64 ? 2 : 1) void attention_back
         const TileReads reads = Tile::reads();
         RandomKey key = {0, 0};
         if (DROP) key = random_key(a.seed);
-        const int steps = tiles * (int)a.group;
-        uint32_t plane = b * a.heads + kv * a.group;
-        int query0 = begin;
-        for (int it = 0, turn = 0; it < steps; ++it, turn ^= 1) {
+        uint32_t plane = b * a.heads + kv * a.group + steps.first / tiles;
+        int query0 = begin + steps.first % tiles * TILE;
+        for (int it = steps.first, turn = 0; it < steps.last; ++it, turn ^= 1) {
             fetched();
             const char* qt = shared + turn * BUFFER;
             const char* dt = qt + Tile::BYTES;
             const RowNumbers* numbers = reinterpret_cast<const RowNumbers*>(dt + Tile::BYTES);
-            if (it + 1 < steps) fetch(turn ^ 1);
+            if (it + 1 < steps.last) fetch(turn ^ 1);
             const int own0 = query0 + (int)part * OWN;
             if (own0 + OWN > wave_least && own0 < ql) {
                 const bool masked = own0 < wave_most || own0 + OWN > ql;
@@ -293,36 +295,78 @@ __global__ __launch_bounds__(BWD_THREADS, DIM == 64 ? 2 : 1) void attention_back
 #pragma unroll
             for (int d = 0; d < DIM / 32; ++d) dkacc[d] = dvacc[d] = 0.0f;
         }
+        if (parts > 1) {
+            float* to = partial + (((uint64_t)share * a.batch * a.kv_heads + b * a.kv_heads + kv) * a.k_len + j) * DIM;
+            store_partial(to, dkacc, a.scale * drop_scale);
+            store_partial(to + (uint64_t)parts * a.batch * a.kv_heads * a.k_len * DIM, dvacc, drop_scale);
+            return;
+        }
         store_row(dk + b * a.dk.batch + (uint64_t)j * a.dk.row + kv * a.dk.head, dkacc, a.scale * drop_scale, a.head_dim);
         store_row(dv + b * a.dv.batch + (uint64_t)j * a.dv.row + kv * a.dv.head, dvacc, drop_scale, a.head_dim);
     }
 }
 
-struct BackwardPointers { const void *q, *k, *v, *o, *d_o; const float* lse; void *dq, *dk, *dv; RowNumbers* rows; };
+// Adds the parts of up to three tensors, four columns a lane, always in the same order.
+struct Sum { const float* from; void* to; Strides strides; uint64_t rows; uint32_t parts, length, heads; };
+struct Sums { Sum of[3]; };
+
+template <typename T, int DIM>
+__global__ __launch_bounds__(BWD_THREADS) void attention_add_kernel(Sums sums, uint32_t head_dim) {
+    typedef T four __attribute__((ext_vector_type(4)));
+    typedef float f32x4 __attribute__((ext_vector_type(4)));
+    const Sum& s = sums.of[blockIdx.y];
+    const uint64_t at = (uint64_t)blockIdx.x * BWD_THREADS + threadIdx.x, row = at / (DIM / 4);
+    const uint32_t d = at % (DIM / 4) * 4;
+    if (row >= s.rows || d >= head_dim) return;
+    f32x4 sum = 0.0f;
+#pragma unroll 4
+    for (uint32_t p = 0; p < s.parts; ++p) sum += *reinterpret_cast<const f32x4*>(s.from + (p * s.rows + row) * DIM + d);
+    const uint64_t i = row % s.length, plane = row / s.length, h = plane % s.heads, b = plane / s.heads;
+    *reinterpret_cast<four*>((T*)s.to + b * s.strides.batch + i * s.strides.row + h * s.strides.head + d) = __builtin_convertvector(sum, four);
+}
+
+struct BackwardPointers { const void *q, *k, *v, *o, *d_o; const float* lse; void *dq, *dk, *dv; char* ws; };
 
 template <typename T, int DIM, bool DROP>
-static void launch_backward(const AttentionArgs& a, const BackwardPointers& p, hipStream_t s) {
+static void launch_backward(const AttentionArgs& a, const AttentionPlan& plan, const BackwardPointers& p, hipStream_t s) {
+    RowNumbers* rows = (RowNumbers*)(p.ws + plan.rows_at);
+    float *dq_sums = (float*)(p.ws + plan.dq_at), *dkv_sums = (float*)(p.ws + plan.dkv_at);
+    Sums sums = {};
+    uint32_t n = 0;
     if (a.q_len) {
-        const uint32_t blocks = (a.q_len + BWD_QUERIES - 1) / BWD_QUERIES;
-        hipLaunchKernelGGL((attention_backward_queries_kernel<T, DIM, DROP>), dim3(blocks * a.batch * a.heads), dim3(BWD_THREADS), 0, s,
-                           a, (const T*)p.q, (const T*)p.k, (const T*)p.v, (const T*)p.o, p.lse, (const T*)p.d_o, (T*)p.dq, p.rows, blocks);
+        const uint32_t blocks = (a.q_len + BWD_QUERIES - 1) / BWD_QUERIES, parts = plan.query_parts;
+        hipLaunchKernelGGL((attention_backward_queries_kernel<T, DIM, DROP>), dim3(blocks * a.batch * a.heads * parts),
+                           dim3(BWD_THREADS), 0, s, a, (const T*)p.q, (const T*)p.k, (const T*)p.v, (const T*)p.o, p.lse,
+                           (const T*)p.d_o, (T*)p.dq, rows, blocks, parts, dq_sums);
+        if (parts > 1) sums.of[n++] = {dq_sums, p.dq, a.dq, (uint64_t)a.batch * a.heads * a.q_len, parts, a.q_len, a.heads};
     }
     if (a.k_len) {
         constexpr uint32_t KEYS = KeysShape<DIM>::GROUPS * 32;
-        const uint32_t blocks = (a.k_len + KEYS - 1) / KEYS;
+        const uint32_t blocks = (a.k_len + KEYS - 1) / KEYS, parts = plan.key_parts;
+        const uint64_t keys = (uint64_t)a.batch * a.kv_heads * a.k_len;
         timing_before(s);
-        hipLaunchKernelGGL((attention_backward_keys_kernel<T, DIM, DROP>), dim3(blocks * a.batch * a.kv_heads), dim3(BWD_THREADS), 0, s,
-                           a, (const T*)p.q, (const T*)p.k, (const T*)p.v, (const T*)p.d_o, (const RowNumbers*)p.rows, (T*)p.dk, (T*)p.dv,
-                           blocks);
+        hipLaunchKernelGGL((attention_backward_keys_kernel<T, DIM, DROP>), dim3(blocks * a.batch * a.kv_heads * parts),
+                           dim3(BWD_THREADS), 0, s, a, (const T*)p.q, (const T*)p.k, (const T*)p.v, (const T*)p.d_o,
+                           (const RowNumbers*)rows, (T*)p.dk, (T*)p.dv, blocks, parts, dkv_sums);
         timing_after(s);
+        if (parts > 1) {
+            sums.of[n++] = {dkv_sums, p.dk, a.dk, keys, parts, a.k_len, a.kv_heads};
+            sums.of[n++] = {dkv_sums + parts * keys * DIM, p.dv, a.dv, keys, parts, a.k_len, a.kv_heads};
+        }
+    }
+    if (n) {
+        uint64_t most = 0;
+        for (uint32_t i = 0; i < n; ++i) most = sums.of[i].rows > most ? sums.of[i].rows : most;
+        hipLaunchKernelGGL((attention_add_kernel<T, DIM>), dim3((unsigned)((most * (DIM / 4) + BWD_THREADS - 1) / BWD_THREADS), n),
+                           dim3(BWD_THREADS), 0, s, sums, a.head_dim);
     }
 }
 
 template <typename T>
-static void launch_backward_shape(const AttentionArgs& a, const BackwardPointers& p, hipStream_t s) {
+static void launch_backward_shape(const AttentionArgs& a, const AttentionPlan& plan, const BackwardPointers& p, hipStream_t s) {
     const bool drop = a.drop.bar != 65536u;
-    if (a.head_dim <= 64) drop ? launch_backward<T, 64, true>(a, p, s) : launch_backward<T, 64, false>(a, p, s);
-    else drop ? launch_backward<T, 128, true>(a, p, s) : launch_backward<T, 128, false>(a, p, s);
+    if (plan.dim == 64) drop ? launch_backward<T, 64, true>(a, plan, p, s) : launch_backward<T, 64, false>(a, plan, p, s);
+    else drop ? launch_backward<T, 128, true>(a, plan, p, s) : launch_backward<T, 128, false>(a, plan, p, s);
 }
 
 }  // namespace okt
@@ -339,10 +383,11 @@ extern "C" int okt_attention_backward(const okt_attention* op, const void* d_q, 
     for (const void* p : {d_q, d_k, d_v, d_o, d_do, (const void*)d_dq_out, (const void*)d_dk_out, (const void*)d_dv_out})
         if (!aligned(p, 16)) return OKT_ERR_INVALID_ARG;
     if (!aligned(d_lse, 4)) return OKT_ERR_INVALID_ARG;
-    if (!d_ws || !aligned(d_ws, 256) || ws_bytes < attention_ws_bytes(a.batch, a.heads, a.q_len)) return OKT_ERR_WORKSPACE;
-    const BackwardPointers p = {d_q, d_k, d_v, d_o, d_do, d_lse, d_dq_out, d_dk_out, d_dv_out, (RowNumbers*)d_ws};
+    const AttentionPlan plan = attention_plan(a.batch, a.heads, a.kv_heads, a.q_len, a.k_len, a.head_dim);
+    if (!d_ws || !aligned(d_ws, 256) || ws_bytes < plan.bytes) return OKT_ERR_WORKSPACE;
+    const BackwardPointers p = {d_q, d_k, d_v, d_o, d_do, d_lse, d_dq_out, d_dk_out, d_dv_out, (char*)d_ws};
     const hipStream_t s = (hipStream_t)stream;
-    if (op->dtype == OKT_BF16) launch_backward_shape<__bf16>(a, p, s);
-    else launch_backward_shape<_Float16>(a, p, s);
+    if (op->dtype == OKT_BF16) launch_backward_shape<__bf16>(a, plan, p, s);
+    else launch_backward_shape<_Float16>(a, plan, p, s);
     return launch_status();
 }

@@ -10,19 +10,21 @@
 namespace okt {
 
 constexpr int FWD_THREADS = 256;
-constexpr int FWD_QUERIES = FWD_THREADS / WAVE * 32;
-constexpr int FWD_KEYS = 64;
+constexpr int FWD_QUERIES = ATTENTION_QUERIES, FWD_KEYS = ATTENTION_KEYS;
+static_assert(FWD_QUERIES == FWD_THREADS / WAVE * 32, "a wave owns 32 queries");
 
 template <typename T, int DIM, bool DROP>
 __global__ __launch_bounds__(FWD_THREADS, 2) void attention_forward_kernel(AttentionArgs a, const T* q, const T* k, const T* v,
-                                                                           T* o, float* lse, uint32_t blocks) {
+                                                                           T* o, float* lse, uint32_t blocks, uint32_t parts,
+                                                                           float* partial, float2* sums) {
     using Tile = RowTile<T, DIM, FWD_KEYS, FWD_THREADS>;
     __shared__ __attribute__((aligned(1024))) char shared[4 * Tile::BYTES];
-    const Place at = place_of(blockIdx.x, a.batch * a.kv_heads, a.group * blocks);
-    const uint32_t b = at.unit / a.kv_heads, kv = at.unit % a.kv_heads, h = kv * a.group + at.in / blocks, plane = b * a.heads + h;
+    const Place at = place_of(blockIdx.x, a.batch * a.kv_heads, a.group * blocks * parts);
+    const uint32_t part = at.in % parts, block = at.in / parts % blocks;
+    const uint32_t b = at.unit / a.kv_heads, kv = at.unit % a.kv_heads, h = kv * a.group + at.in / parts / blocks, plane = b * a.heads + h;
     const uint32_t wave = uniform(threadIdx.x / WAVE), lane = threadIdx.x % WAVE;
     const int ql = sequence_length(a.q_lens, b, a.q_len), kl = sequence_length(a.k_lens, b, a.k_len);
-    const int q0 = (blocks - 1 - at.in % blocks) * FWD_QUERIES, w0 = q0 + 32 * (int)wave, i = w0 + (int)(lane % 32);
+    const int q0 = (blocks - 1 - block) * FWD_QUERIES, w0 = q0 + 32 * (int)wave, i = w0 + (int)(lane % 32);
 
     // keys that a query sees; the most of the workgroup's queries, the least and most of the wave's
     const int past = kl - ql + 1;
@@ -31,18 +33,22 @@ __global__ __launch_bounds__(FWD_THREADS, 2) void attention_forward_kernel(Atten
     const int mine = seen(i), wave_least = w0 + 31 < ql ? seen(w0) : 0;
     const int wave_most = w0 < ql ? seen(w0 + 32 < ql ? w0 + 31 : ql - 1) : 0;
 
+    // the tiles of this part
+    const Part mine_of = part_of((keys + FWD_KEYS - 1) / FWD_KEYS, part, parts);
+    const int begin = mine_of.first * FWD_KEYS, end = mine_of.last * FWD_KEYS < keys ? mine_of.last * FWD_KEYS : keys;
+
     f32x16 acc[DIM / 32];
     float top = -INFINITY, total = 0.0f;          // of the scores times scale_log2
 #pragma unroll
     for (int d = 0; d < DIM / 32; ++d) acc[d] = 0.0f;
-    if (keys > 0) {
+    if (begin < end) {
         const T* kb = k + b * a.k.batch + kv * a.k.head;
         const T* vb = v + b * a.v.batch + kv * a.v.head;
         const uint32_t k_row = (uint32_t)a.k.row * 2, v_row = (uint32_t)a.v.row * 2;
         const typename Tile::Places k_at(k_row, a.head_dim), v_at(v_row, a.head_dim);
         const uint32_t lds = lds_address(shared);
-        Tile::fetch(lds, kb, k_row, k_at, 0, 0, kl, a.head_dim);
-        Tile::fetch(lds + Tile::BYTES, vb, v_row, v_at, 0, 0, kl, a.head_dim);
+        Tile::fetch(lds, kb, k_row, k_at, begin, 0, kl, a.head_dim);
+        Tile::fetch(lds + Tile::BYTES, vb, v_row, v_at, begin, 0, kl, a.head_dim);
         const T* qrow = q + b * a.q.batch + (uint64_t)(i < ql ? i : ql - 1) * a.q.row + h * a.q.head;
         frag<T> qf[DIM / 16];
 #pragma unroll
@@ -50,11 +56,11 @@ __global__ __launch_bounds__(FWD_THREADS, 2) void attention_forward_kernel(Atten
         const TileReads reads = Tile::reads();
         RandomKey key = {0, 0};
         if (DROP) key = random_key(a.seed);
-        for (int key0 = 0, turn = 0; key0 < keys; key0 += FWD_KEYS, turn ^= 1) {
+        for (int key0 = begin, turn = 0; key0 < end; key0 += FWD_KEYS, turn ^= 1) {
             fetched();
             const char* kt = shared + turn * 2 * Tile::BYTES;
             const char* vt = kt + Tile::BYTES;
-            if (key0 + FWD_KEYS < keys) {
+            if (key0 + FWD_KEYS < end) {
                 const uint32_t next = lds + (turn ^ 1) * 2 * Tile::BYTES;
                 Tile::fetch(next, kb, k_row, k_at, key0 + FWD_KEYS, 0, kl, a.head_dim);
                 Tile::fetch(next + Tile::BYTES, vb, v_row, v_at, key0 + FWD_KEYS, 0, kl, a.head_dim);
@@ -116,6 +122,14 @@ __global__ __launch_bounds__(FWD_THREADS, 2) void attention_forward_kernel(Atten
         }
     }
     total = sum_halves(total);
+    if (parts > 1) {
+        if (i < (int)a.q_len) {
+            const uint64_t row = ((uint64_t)part * a.batch * a.heads + plane) * a.q_len + i;
+            store_partial(partial + row * DIM, acc, 1.0f);
+            if (lane < 32) sums[row] = make_float2(top, total);
+        }
+        return;
+    }
     if (i < (int)a.q_len) {
         store_row(o + b * a.o.batch + (uint64_t)i * a.o.row + h * a.o.head, acc, mine > 0 ? a.drop.scale / total : 0.0f, a.head_dim);
         if (lse && lane < 32)
@@ -123,12 +137,73 @@ __global__ __launch_bounds__(FWD_THREADS, 2) void attention_forward_kernel(Atten
     }
 }
 
+// Joins the parts of a row: o = sum 2^(top - most) acc / sum 2^(top - most) total.  DIM / 4 lanes a
+// row, four columns a lane.
 template <typename T, int DIM>
-static void launch_forward(const AttentionArgs& a, const void* q, const void* k, const void* v, void* o, float* lse, hipStream_t s) {
-    const uint32_t blocks = (a.q_len + FWD_QUERIES - 1) / FWD_QUERIES;
+__global__ __launch_bounds__(FWD_THREADS) void attention_join_kernel(AttentionArgs a, T* o, float* lse, uint32_t parts,
+                                                                     const float* partial, const float2* sums) {
+    constexpr uint32_t LANES = DIM / 4;
+    typedef T four __attribute__((ext_vector_type(4)));
+    typedef float f32x4 __attribute__((ext_vector_type(4)));
+    const uint64_t rows = (uint64_t)a.batch * a.heads * a.q_len;
+    const uint64_t row = (uint64_t)blockIdx.x * (FWD_THREADS / LANES) + threadIdx.x / LANES;
+    const uint32_t d = threadIdx.x % LANES * 4;
+    if (row >= rows) return;
+    float most = -INFINITY;
+    for (uint32_t p = 0; p < parts; ++p) most = fmaxf(most, sums[p * rows + row].x);
+    f32x4 acc = 0.0f;
+    float total = 0.0f;
+    for (uint32_t p = 0; p < parts; ++p) {
+        const float2 s = sums[p * rows + row];
+        const float weight = s.x == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(s.x - most);
+        total = __builtin_fmaf(s.y, weight, total);
+        acc += weight * *reinterpret_cast<const f32x4*>(partial + (p * rows + row) * DIM + d);
+    }
+    const bool any = most != -INFINITY;
+    acc *= any ? a.drop.scale / total : 0.0f;
+    const uint32_t i = row % a.q_len, h = row / a.q_len % a.heads, b = row / a.q_len / a.heads;
+    if (d < a.head_dim)
+        *reinterpret_cast<four*>(o + b * a.o.batch + (uint64_t)i * a.o.row + h * a.o.head + d) = __builtin_convertvector(acc, four);
+    if (lse && d == 0) lse[row] = any ? (most + __builtin_amdgcn_logf(total)) * 0.693147180559945f : -INFINITY;
+}
+
+template <typename T, int DIM>
+static void launch_forward(const AttentionArgs& a, const AttentionPlan& plan, const void* q, const void* k, const void* v, void* o,
+                           float* lse, void* ws, hipStream_t s) {
+    const uint32_t blocks = (a.q_len + FWD_QUERIES - 1) / FWD_QUERIES, parts = plan.forward_parts;
+    const uint64_t rows = (uint64_t)a.batch * a.heads * a.q_len;
+    float* partial = (float*)ws;
+    float2* sums = (float2*)(partial + parts * rows * DIM);
     auto* kernel = a.drop.bar == 65536u ? attention_forward_kernel<T, DIM, false> : attention_forward_kernel<T, DIM, true>;
-    hipLaunchKernelGGL(kernel, dim3(blocks * a.batch * a.heads), dim3(FWD_THREADS), 0, s, a, (const T*)q, (const T*)k,
-                       (const T*)v, (T*)o, lse, blocks);
+    timing_before(s);
+    hipLaunchKernelGGL(kernel, dim3(blocks * a.batch * a.heads * parts), dim3(FWD_THREADS), 0, s, a, (const T*)q, (const T*)k,
+                       (const T*)v, (T*)o, lse, blocks, parts, partial, sums);
+    timing_after(s);
+    if (parts > 1)
+        hipLaunchKernelGGL((attention_join_kernel<T, DIM>), dim3((unsigned)((rows * (DIM / 4) + FWD_THREADS - 1) / FWD_THREADS)),
+                           dim3(FWD_THREADS), 0, s, a, (T*)o, lse, parts, (const float*)partial, (const float2*)sums);
+}
+
+AttentionPlan attention_plan(uint32_t batch, uint32_t heads, uint32_t kv_heads, uint32_t q_len, uint32_t k_len, uint32_t head_dim) {
+    AttentionPlan p;
+    p.dim = head_dim <= 64 ? 64 : 128;
+    const uint32_t key_block = p.dim == 64 ? KeysShape<64>::GROUPS * 32 : KeysShape<128>::GROUPS * 32;
+    const uint32_t query_tile = p.dim == 64 ? KeysShape<64>::TILE : KeysShape<128>::TILE;
+    const uint64_t units = (uint64_t)batch * kv_heads, planes = (uint64_t)batch * heads, group = kv_heads ? heads / kv_heads : 0;
+    const uint64_t query_blocks = (q_len + ATTENTION_QUERIES - 1) / ATTENTION_QUERIES * planes;
+    const uint64_t key_steps = (k_len + ATTENTION_KEYS - 1) / ATTENTION_KEYS;
+    p.forward_parts = parts_for(query_blocks, key_steps, 4);
+    p.query_parts = parts_for(query_blocks, key_steps, 3);
+    p.key_parts = parts_for((k_len + key_block - 1) / key_block * units, (q_len + query_tile - 1) / query_tile * group, 2);
+    const auto round = [](uint64_t n) { return (size_t)((n + 255) & ~255ull); };
+    const uint64_t rows = planes * q_len, keys = units * k_len;
+    p.forward_bytes = p.forward_parts > 1 ? round(p.forward_parts * rows * (p.dim + 2) * sizeof(float)) : 0;
+    p.rows_at = 0;
+    p.dq_at = round(rows * 2 * sizeof(float));
+    p.dkv_at = p.dq_at + (p.query_parts > 1 ? round(p.query_parts * rows * p.dim * sizeof(float)) : 0);
+    p.bytes = p.dkv_at + (p.key_parts > 1 ? round(2 * p.key_parts * keys * p.dim * sizeof(float)) : 0);
+    if (p.bytes < p.forward_bytes) p.bytes = p.forward_bytes;
+    return p;
 }
 
 static bool strides(const uint64_t (&s)[3], Strides& to) {
@@ -142,8 +217,8 @@ bool attention_args(const okt_attention* op, bool backward, AttentionArgs& a) {
     if (!op || (op->dtype != OKT_BF16 && op->dtype != OKT_F16)) return false;
     if (op->kv_heads == 0 || op->heads == 0 || op->heads % op->kv_heads) return false;
     if ((uint64_t)op->batch * op->heads > (1u << 20) || op->q_len > (1u << 24) || op->k_len > (1u << 24)) return false;
-    // workgroups of a launch: a block of 128 rows of one head each
-    if (((uint64_t)(op->q_len > op->k_len ? op->q_len : op->k_len) / 128 + 1) * op->batch * op->heads > (1u << 30)) return false;
+    // workgroups of a launch: a block of 64 rows or more of one head each
+    if (((uint64_t)(op->q_len > op->k_len ? op->q_len : op->k_len) / 64 + 1) * op->batch * op->heads > (1u << 30)) return false;
     if (op->head_dim == 0 || op->head_dim > 128 || op->head_dim % 8) return false;
     if (!(op->scale > 0.0f) || op->scale > 3.0e38f) return false;
     if (!dropout_rule(op->dropout_p, a.drop)) return false;
@@ -170,20 +245,13 @@ bool attention_args(const okt_attention* op, bool backward, AttentionArgs& a) {
     return true;
 }
 
-size_t attention_ws_bytes(uint32_t batch, uint32_t heads, uint32_t q_len) {
-    return ((size_t)batch * heads * q_len * 2 * sizeof(float) + 255) & ~(size_t)255;      // two numbers of every row
-}
-
 }  // namespace okt
 
 extern "C" {
 
 size_t okt_attention_workspace_bytes(uint32_t batch, uint32_t heads, uint32_t kv_heads, uint32_t q_len, uint32_t k_len,
                                      uint32_t head_dim) {
-    (void)kv_heads;
-    (void)k_len;
-    (void)head_dim;
-    const size_t need = okt::attention_ws_bytes(batch, heads, q_len);
+    const size_t need = okt::attention_plan(batch, heads, kv_heads, q_len, k_len, head_dim).bytes;
     return need ? need : 256;
 }
 
@@ -195,19 +263,17 @@ int okt_attention_forward(const okt_attention* op, const void* d_q, const void* 
     if (a.batch == 0 || a.q_len == 0) return OKT_OK;
     if (!d_q || !d_o_out || (a.k_len && (!d_k || !d_v))) return OKT_ERR_INVALID_ARG;
     if (!aligned(d_q, 16) || !aligned(d_k, 16) || !aligned(d_v, 16) || !aligned(d_o_out, 16) || !aligned(d_lse_out, 4)) return OKT_ERR_INVALID_ARG;
-    (void)d_ws;
-    (void)ws_bytes;
+    const AttentionPlan plan = attention_plan(a.batch, a.heads, a.kv_heads, a.q_len, a.k_len, a.head_dim);
+    if (plan.forward_bytes && (!d_ws || !aligned(d_ws, 256) || ws_bytes < plan.forward_bytes)) return OKT_ERR_WORKSPACE;
     const hipStream_t s = (hipStream_t)stream;
-    const bool narrow = a.head_dim <= 64;
-    timing_before(s);
+    const bool narrow = plan.dim == 64;
     if (op->dtype == OKT_BF16) {
-        if (narrow) launch_forward<__bf16, 64>(a, d_q, d_k, d_v, d_o_out, d_lse_out, s);
-        else launch_forward<__bf16, 128>(a, d_q, d_k, d_v, d_o_out, d_lse_out, s);
+        if (narrow) launch_forward<__bf16, 64>(a, plan, d_q, d_k, d_v, d_o_out, d_lse_out, d_ws, s);
+        else launch_forward<__bf16, 128>(a, plan, d_q, d_k, d_v, d_o_out, d_lse_out, d_ws, s);
     } else {
-        if (narrow) launch_forward<_Float16, 64>(a, d_q, d_k, d_v, d_o_out, d_lse_out, s);
-        else launch_forward<_Float16, 128>(a, d_q, d_k, d_v, d_o_out, d_lse_out, s);
+        if (narrow) launch_forward<_Float16, 64>(a, plan, d_q, d_k, d_v, d_o_out, d_lse_out, d_ws, s);
+        else launch_forward<_Float16, 128>(a, plan, d_q, d_k, d_v, d_o_out, d_lse_out, d_ws, s);
     }
-    timing_after(s);
     return launch_status();
 }
 
