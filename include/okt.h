@@ -565,7 +565,7 @@ typedef enum okt_norm_kind { OKT_NORM_LAYER = 0, OKT_NORM_RMS = 1 } okt_norm_kin
  */
 typedef struct okt_residual_norm {
     uint64_t rows;                /* at most 2^40 */
-    uint32_t width;               /* 8 to 16384 */
+    uint32_t width;               /* 8 to 8192 */
     int32_t dtype;                /* of u, x, h, y and their gradients */
     int32_t kind;                 /* okt_norm_kind of both norms */
     float eps;                    /* >= 0 */
@@ -634,8 +634,8 @@ int okt_residual_norm_backward(const okt_residual_norm* op, const void* d_u, con
  * units from 16-bit inputs with fp32 sums; p and ds are rounded to the tensors' type for the
  * second product of each pass.
  * A tensor is [batch][length][heads][head_dim] by strides {batch, length, heads} in elements,
- * head_dim contiguous; strides are multiples of 8, bases 16-byte aligned, so the parts
- * of a common projection are taken as they lie.
+ * head_dim contiguous; strides are multiples of 8 (that of the length at most 2^24), bases
+ * 16-byte aligned, so the parts of a common projection are taken as they lie.
  */
 typedef struct okt_attention {
     uint32_t batch, heads, kv_heads;   /* heads a multiple of kv_heads; batch * heads <= 2^20 */

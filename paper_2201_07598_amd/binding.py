@@ -542,46 +542,58 @@ def okt_dropout(x, y, p: float, seed, site: int = 0, stream=None) -> None:
         _stream(stream)))
 
 
-def _rows(t, like, name, allow_none=False):
-    """(pointer, row stride) of a [rows, width] tensor like `like`, rows any distance apart."""
+# What such a call costs the host is what short sequences wait for, as above: the usual outcome
+# of a tensor's checks is decided first, by comparisons alone.
+def _rows(t, dtype, shape, name, allow_none=False):
+    """(pointer, row stride) of a [rows, width] tensor, rows any distance apart."""
+    if t is not None and t.dtype is dtype and t.is_cuda and t.shape == shape:
+        step, unit = t.stride()
+        if unit == 1 and step >= shape[1]:
+            return t.data_ptr(), step if shape[0] > 1 else 0
     if t is None:
         if allow_none:
             return None, 0
         raise TypeError(f"{name} is required")
     if not t.is_cuda:
         raise TypeError(f"{name} must be a CUDA tensor (device memory)")
-    if t.dtype is not like.dtype:
-        raise TypeError(f"{name} must have dtype {like.dtype}, got {t.dtype}")
-    if t.shape != like.shape:
-        raise ValueError(f"{name} must have the shape {tuple(like.shape)}, got {tuple(t.shape)}")
-    rows, width = t.shape
+    if t.dtype is not dtype:
+        raise TypeError(f"{name} must have dtype {dtype}, got {t.dtype}")
+    if t.shape != shape:
+        raise ValueError(f"{name} must have the shape {tuple(shape)}, got {tuple(t.shape)}")
     step, unit = t.stride()
-    if unit != 1 and width > 1:
+    if unit != 1 and shape[1] > 1:
         raise ValueError(f"{name} must have contiguous rows")
-    if rows > 1 and step < width:
+    if shape[0] > 1 and step < shape[1]:
         raise ValueError(f"rows of {name} must not overlap")
-    return t.data_ptr(), step if rows > 1 else 0
+    return t.data_ptr(), step if shape[0] > 1 else 0
 
 
 def _parameter(t, numel, name):
+    """The address of a float32 parameter on the device, 0 for none."""
     if t is None:
-        return None
+        return 0
+    if t.dtype is _TORCH.float32 and t.is_cuda and t.numel() == numel and t.is_contiguous():
+        return t.data_ptr()
     if t.numel() != numel:
         raise ValueError(f"{name} needs {numel} elements, got {t.numel()}")
     return _ptr(t, _TORCH.float32, name)
 
 
-def _norm_struct(like, kind, eps, residual_scale, post_weight, post_bias, gate, rows_per_gate, pre_weight,
-                 pre_bias, dropout_p, seed, site, strides):
-    rows, width = like.shape
-    share = int(rows_per_gate)
-    gates = max(1, -(-rows // share)) if share else 1
-    return gates, _NORM.pack(
-        rows, width, _dtype_code(like, "u"), _NORM_KINDS[kind], eps, residual_scale, site, dropout_p,
-        _seed(seed, dropout_p), _parameter(post_weight, width, "post_weight") or 0,
-        _parameter(post_bias, width, "post_bias") or 0, _parameter(gate, gates * width, "gate") or 0, share,
-        _parameter(pre_weight, width, "pre_weight") or 0, _parameter(pre_bias, width, "pre_bias") or 0,
-        *strides)
+def _norm_struct(dtype, shape, kind, eps, residual_scale, post_weight, post_bias, gate, rows_per_gate,
+                 pre_weight, pre_bias, dropout_p, seed, site, strides):
+    rows, width = shape
+    return _NORM.pack(
+        rows, width, _DTYPES[dtype], _NORM_KINDS[kind], eps, residual_scale, site, dropout_p,
+        0 if seed is None and dropout_p == 0.0 else _seed(seed, dropout_p),
+        0 if post_weight is None else _parameter(post_weight, width, "post_weight"),
+        0 if post_bias is None else _parameter(post_bias, width, "post_bias"),
+        0 if gate is None else _parameter(gate, _gates(rows, rows_per_gate) * width, "gate"), rows_per_gate,
+        0 if pre_weight is None else _parameter(pre_weight, width, "pre_weight"),
+        0 if pre_bias is None else _parameter(pre_bias, width, "pre_bias"), *strides)
+
+
+def _gates(rows, rows_per_gate):
+    return max(1, -(-rows // rows_per_gate)) if rows_per_gate else 1
 
 
 def okt_residual_norm_workspace_bytes(rows: int, width: int, rows_per_gate: int = 0) -> int:
@@ -595,19 +607,20 @@ def okt_residual_norm_forward(u, x, h_out, y_out, stats_out, *, kind: str = "lay
     """h = residual_scale x + gate * dropout(norm(u)), y = norm(h) on [rows, width] tensors;
     a norm is there where its weight is.  kind: "layer" or "rms".  h_out may be None, stats_out
     (float32 [rows, 4]) too where no backward pass follows."""
-    torch = _torch()
-    if u.dim() != 2:
+    _dtype_code(u, "u")
+    dtype, shape = u.dtype, u.shape
+    if len(shape) != 2:
         raise ValueError("u must be [rows, width]")
-    pu, su = _rows(u, u, "u")
-    px, sx = _rows(x, u, "x")
-    ph, sh = _rows(h_out, u, "h_out", allow_none=True)
-    py, sy = _rows(y_out, u, "y_out", allow_none=True)
-    if stats_out is not None and stats_out.numel() < 4 * u.shape[0]:
+    pu, su = _rows(u, dtype, shape, "u")
+    px, sx = _rows(x, dtype, shape, "x")
+    ph, sh = _rows(h_out, dtype, shape, "h_out", True)
+    py, sy = _rows(y_out, dtype, shape, "y_out", True)
+    if stats_out is not None and stats_out.numel() < 4 * shape[0]:
         raise ValueError("stats_out needs four elements a row")
-    _, op = _norm_struct(u, kind, eps, residual_scale, post_weight, post_bias, gate, rows_per_gate,
+    op = _norm_struct(dtype, shape, kind, eps, residual_scale, post_weight, post_bias, gate, rows_per_gate,
                          pre_weight, pre_bias, dropout_p, seed, site, (su, sx, sh, sy, 0, 0, 0, 0))
     _check("okt_residual_norm_forward", load_library().okt_residual_norm_forward(
-        op, pu, px, ph, py, _ptr(stats_out, torch.float32, "stats_out", allow_none=True), _stream(stream)))
+        op, pu, px, ph, py, _ptr(stats_out, _TORCH.float32, "stats_out", True), _stream(stream)))
 
 
 def okt_residual_norm_backward(u, h, stats, dh, dy, dx_out, du_out, ws, *, dpost_weight=None,
@@ -619,27 +632,27 @@ def okt_residual_norm_backward(u, h, stats, dh, dy, dx_out, du_out, ws, *, dpost
     """Gradients of x, u and the parameters from those of h (dh, None for zero) and y (dy, None
     without a pre norm).  The parameters' gradients are float32 and are overwritten; None
     leaves one out."""
-    torch = _torch()
     if du_out is None or du_out.dim() != 2:
         raise ValueError("du_out must be [rows, width]")
-    like = du_out
-    pu, su = _rows(u, like, "u", allow_none=True)
-    ph, sh = _rows(h, like, "h", allow_none=True)
-    pdh, sdh = _rows(dh, like, "dh", allow_none=True)
-    pdy, sdy = _rows(dy, like, "dy", allow_none=True)
-    pdx, sdx = _rows(dx_out, like, "dx_out")
-    pdu, sdu = _rows(du_out, like, "du_out")
-    if stats.numel() < 4 * like.shape[0]:
+    _dtype_code(du_out, "du_out")
+    dtype, shape = du_out.dtype, du_out.shape
+    pu, su = _rows(u, dtype, shape, "u", True)
+    ph, sh = _rows(h, dtype, shape, "h", True)
+    pdh, sdh = _rows(dh, dtype, shape, "dh", True)
+    pdy, sdy = _rows(dy, dtype, shape, "dy", True)
+    pdx, sdx = _rows(dx_out, dtype, shape, "dx_out")
+    pdu, sdu = _rows(du_out, dtype, shape, "du_out")
+    rows, width = shape
+    if stats.numel() < 4 * rows:
         raise ValueError("stats needs four elements a row")
-    gates, op = _norm_struct(like, kind, eps, residual_scale, post_weight, post_bias, gate, rows_per_gate,
-                             pre_weight, pre_bias, dropout_p, seed, site, (su, 0, sh, 0, sdh, sdy, sdx, sdu))
-    width = like.shape[1]
+    op = _norm_struct(dtype, shape, kind, eps, residual_scale, post_weight, post_bias, gate, rows_per_gate,
+                      pre_weight, pre_bias, dropout_p, seed, site, (su, 0, sh, 0, sdh, sdy, sdx, sdu))
     _check("okt_residual_norm_backward", load_library().okt_residual_norm_backward(
-        op, pu, ph, _ptr(stats, torch.float32, "stats"), pdh, pdy, pdx, pdu,
+        op, pu, ph, _ptr(stats, _TORCH.float32, "stats"), pdh, pdy, pdx, pdu,
         _parameter(dpost_weight, width, "dpost_weight"), _parameter(dpost_bias, width, "dpost_bias"),
-        _parameter(dgate, gates * width, "dgate"), _parameter(dpre_weight, width, "dpre_weight"),
-        _parameter(dpre_bias, width, "dpre_bias"), _ptr(ws, torch.uint8, "ws"), ws.numel(),
-        _stream(stream)))
+        0 if dgate is None else _parameter(dgate, _gates(rows, rows_per_gate) * width, "dgate"),
+        _parameter(dpre_weight, width, "dpre_weight"), _parameter(dpre_bias, width, "dpre_bias"),
+        _ptr(ws, _TORCH.uint8, "ws"), ws.numel(), _stream(stream)))
 
 
 def okt_attention_workspace_bytes(batch: int, heads: int, kv_heads: int, q_len: int, k_len: int,
@@ -649,18 +662,19 @@ def okt_attention_workspace_bytes(batch: int, heads: int, kv_heads: int, q_len: 
 
 
 def _heads(t, dtype, shape, name):
-    """(pointer, batch stride, length stride, head stride) of a [batch, length, heads, dim]
-    tensor; a stride that is never taken reads as 0."""
+    """(pointer, (batch stride, length stride, head stride)) of a [batch, length, heads, dim]
+    tensor."""
+    if t.dtype is dtype and t.is_cuda and t.shape == shape:
+        strides = t.stride()
+        if strides[3] == 1:
+            return t.data_ptr(), strides[:3]
     if not t.is_cuda:
         raise TypeError(f"{name} must be a CUDA tensor (device memory)")
     if t.dtype is not dtype:
         raise TypeError(f"{name} must have dtype {dtype}, got {t.dtype}")
     if t.shape != shape:
         raise ValueError(f"{name} must have the shape {tuple(shape)}, got {tuple(t.shape)}")
-    b, n, h, unit = t.stride()
-    if unit != 1:
-        raise ValueError(f"{name} must have contiguous head vectors")
-    return t.data_ptr(), (b if shape[0] > 1 else 0, n if shape[1] > 1 else 0, h if shape[2] > 1 else 0)
+    raise ValueError(f"{name} must have contiguous head vectors")
 
 
 def _lengths(t, batch, name):
@@ -674,24 +688,27 @@ def _lengths(t, batch, name):
 _NO_STRIDES = (0,) * 12
 
 
-def _attention_struct(q, k, causal, scale, dropout_p, seed, site, q_lens, k_lens, strides):
-    batch, q_len, heads, dim = q.shape
+def _attention_struct(dtype, shape, keys, causal, scale, dropout_p, seed, site, q_lens, k_lens, strides):
+    batch, q_len, heads, dim = shape
     return _ATTENTION.pack(
-        batch, heads, k.shape[2], q_len, k.shape[1], dim, _dtype_code(q, "q"), 1 if causal else 0,
-        dim ** -0.5 if scale is None else scale, site, dropout_p, _seed(seed, dropout_p),
-        _lengths(q_lens, batch, "q_lens"), _lengths(k_lens, batch, "k_lens"), *strides)
+        batch, heads, keys[2], q_len, keys[1], dim, _DTYPES[dtype], 1 if causal else 0,
+        dim ** -0.5 if scale is None else scale, site, dropout_p,
+        0 if seed is None and dropout_p == 0.0 else _seed(seed, dropout_p),
+        0 if q_lens is None else _lengths(q_lens, batch, "q_lens"),
+        0 if k_lens is None else _lengths(k_lens, batch, "k_lens"), *strides)
 
 
 def _attention_inputs(q, k, v):
-    if q.dim() != 4 or k.dim() != 4:
+    _dtype_code(q, "q")
+    dtype, shape, keys = q.dtype, q.shape, k.shape
+    if len(shape) != 4 or len(keys) != 4:
         raise ValueError("q, k and v must be [batch, length, heads, head_dim]")
-    shape, keys = q.shape, k.shape
     if keys[0] != shape[0] or keys[3] != shape[3]:
         raise ValueError("q and k must agree in batch and head_dim")
-    pq, sq = _heads(q, q.dtype, shape, "q")
-    pk, sk = _heads(k, q.dtype, keys, "k")
-    pv, sv = _heads(v, q.dtype, keys, "v")
-    return shape, keys, pq, pk, pv, sq + sk + sv
+    pq, sq = _heads(q, dtype, shape, "q")
+    pk, sk = _heads(k, dtype, keys, "k")
+    pv, sv = _heads(v, dtype, keys, "v")
+    return dtype, shape, keys, pq, pk, pv, sq + sk + sv
 
 
 def okt_attention_forward(q, k, v, o_out, lse_out, ws=None, *, causal: bool = False, scale=None,
@@ -701,16 +718,15 @@ def okt_attention_forward(q, k, v, o_out, lse_out, ws=None, *, causal: bool = Fa
     tensors of any strides; scale defaults to head_dim ** -0.5.  q_lens, k_lens: int32 [batch] on the
     device, the sequences' own lengths.  lse_out (float32 [batch, heads, q_len]) may be None where
     no backward pass follows."""
-    torch = _torch()
-    shape, _, pq, pk, pv, strides = _attention_inputs(q, k, v)
-    po, so = _heads(o_out, q.dtype, shape, "o_out")
+    dtype, shape, keys, pq, pk, pv, strides = _attention_inputs(q, k, v)
+    po, so = _heads(o_out, dtype, shape, "o_out")
     if lse_out is not None and lse_out.numel() != shape[0] * shape[1] * shape[2]:
         raise ValueError("lse_out must be [batch, heads, q_len]")
-    op = _attention_struct(q, k, causal, scale, dropout_p, seed, site, q_lens, k_lens,
+    op = _attention_struct(dtype, shape, keys, causal, scale, dropout_p, seed, site, q_lens, k_lens,
                            strides + so + _NO_STRIDES)
     _check("okt_attention_forward", load_library().okt_attention_forward(
-        op, pq, pk, pv, po, _ptr(lse_out, torch.float32, "lse_out", allow_none=True),
-        _ptr(ws, torch.uint8, "ws", allow_none=True), 0 if ws is None else ws.numel(), _stream(stream)))
+        op, pq, pk, pv, po, _ptr(lse_out, _TORCH.float32, "lse_out", True),
+        _ptr(ws, _TORCH.uint8, "ws", True), 0 if ws is None else ws.numel(), _stream(stream)))
 
 
 def okt_attention_backward(q, k, v, o, lse, do, dq_out, dk_out, dv_out, ws, *, causal: bool = False,
@@ -718,17 +734,16 @@ def okt_attention_backward(q, k, v, o, lse, do, dq_out, dk_out, dv_out, ws, *, c
                            site: int = 0, stream=None) -> None:
     """Gradients of q, k and v from that of o, with o and lse of the forward pass and the same
     options (seed and site above all)."""
-    torch = _torch()
-    shape, keys, pq, pk, pv, strides = _attention_inputs(q, k, v)
-    po, so = _heads(o, q.dtype, shape, "o")
-    pdo, sdo = _heads(do, q.dtype, shape, "do")
-    pdq, sdq = _heads(dq_out, q.dtype, shape, "dq_out")
-    pdk, sdk = _heads(dk_out, q.dtype, keys, "dk_out")
-    pdv, sdv = _heads(dv_out, q.dtype, keys, "dv_out")
+    dtype, shape, keys, pq, pk, pv, strides = _attention_inputs(q, k, v)
+    po, so = _heads(o, dtype, shape, "o")
+    pdo, sdo = _heads(do, dtype, shape, "do")
+    pdq, sdq = _heads(dq_out, dtype, shape, "dq_out")
+    pdk, sdk = _heads(dk_out, dtype, keys, "dk_out")
+    pdv, sdv = _heads(dv_out, dtype, keys, "dv_out")
     if lse.numel() != shape[0] * shape[1] * shape[2]:
         raise ValueError("lse must be [batch, heads, q_len]")
-    op = _attention_struct(q, k, causal, scale, dropout_p, seed, site, q_lens, k_lens,
+    op = _attention_struct(dtype, shape, keys, causal, scale, dropout_p, seed, site, q_lens, k_lens,
                            strides + so + sdo + sdq + sdk + sdv)
     _check("okt_attention_backward", load_library().okt_attention_backward(
-        op, pq, pk, pv, po, _ptr(lse, torch.float32, "lse"), pdo, pdq, pdk, pdv,
-        _ptr(ws, torch.uint8, "ws"), ws.numel(), _stream(stream)))
+        op, pq, pk, pv, po, _ptr(lse, _TORCH.float32, "lse"), pdo, pdq, pdk, pdv,
+        _ptr(ws, _TORCH.uint8, "ws"), ws.numel(), _stream(stream)))

@@ -111,11 +111,15 @@ __global__ __launch_bounds__(BWD_THREADS, 2) void attention_backward_queries_ker
                 }
                 if (n == 0 && key0 == 0) {
                     // A row that sees no key past this tile takes D from what it has here, sum_j p dP: few
-                    // probabilities are large ones, and the rounding of o would show in dP - D.
-                    float few = 0.0f;
+                    // probabilities are large ones, and the rounding of o would show in dP - D.  Taken
+                    // from the largest dP on, so that a row with one key gets its dP itself and ds = 0.
+                    float from = -INFINITY, few = 0.0f;
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) few = __builtin_fmaf(s[r], dp[r], few);
-                    few = sum_halves(few);
+                    for (int r = 0; r < 16; ++r) from = fmaxf(from, 16 * (int)(lane / 32) + r < mine ? dp[r] : -INFINITY);
+                    from = mine > 0 ? max_halves(from) : 0.0f;
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) few = __builtin_fmaf(s[r], dp[r] - from, few);
+                    few = from + sum_halves(few);
                     sum = mine <= 32 ? few : sum;
                 }
 #pragma unroll

@@ -206,11 +206,12 @@ AttentionPlan attention_plan(uint32_t batch, uint32_t heads, uint32_t kv_heads, 
     return p;
 }
 
-static bool strides(const uint64_t (&s)[3], Strides& to) {
-    to = {s[0], s[1], s[2]};
-    for (uint64_t n : s)
+// Strides of a tensor of these sizes; one that is never taken may be anything.
+static bool strides(const uint64_t (&s)[3], uint32_t batch, uint32_t length, uint32_t heads, Strides& to) {
+    to = {batch > 1 ? s[0] : 0, length > 1 ? s[1] : 0, heads > 1 ? s[2] : 0};
+    for (uint64_t n : {to.batch, to.row, to.head})
         if (n % 8 || n > (1ull << 40)) return false;
-    return s[1] <= (1u << 24);                   // so that a tile's offsets fit 32 bits
+    return to.row <= (1u << 24);                 // so that a tile's offsets fit 32 bits
 }
 
 bool attention_args(const okt_attention* op, bool backward, AttentionArgs& a) {
@@ -224,10 +225,13 @@ bool attention_args(const okt_attention* op, bool backward, AttentionArgs& a) {
     if (!dropout_rule(op->dropout_p, a.drop)) return false;
     if (a.drop.bar != 65536u && (!op->d_seed || !aligned(op->d_seed, 8))) return false;
     if (!aligned(op->d_q_lens, 4) || !aligned(op->d_k_lens, 4)) return false;
-    if (!strides(op->q_stride, a.q) || !strides(op->k_stride, a.k) ||
-        !strides(op->v_stride, a.v) || !strides(op->o_stride, a.o)) return false;
-    if (backward && (!strides(op->do_stride, a.d_o) || !strides(op->dq_stride, a.dq) ||
-                     !strides(op->dk_stride, a.dk) || !strides(op->dv_stride, a.dv))) return false;
+    const auto take = [&](const uint64_t (&from)[3], bool keys, Strides& to) {
+        return strides(from, op->batch, keys ? op->k_len : op->q_len, keys ? op->kv_heads : op->heads, to);
+    };
+    if (!take(op->q_stride, false, a.q) || !take(op->k_stride, true, a.k) || !take(op->v_stride, true, a.v) ||
+        !take(op->o_stride, false, a.o)) return false;
+    if (backward && (!take(op->do_stride, false, a.d_o) || !take(op->dq_stride, false, a.dq) ||
+                     !take(op->dk_stride, true, a.dk) || !take(op->dv_stride, true, a.dv))) return false;
     a.batch = op->batch;
     a.heads = op->heads;
     a.kv_heads = op->kv_heads;

@@ -26,7 +26,7 @@ namespace okt {
 
 // ------------------------------------------------------------------ sizes (host)
 
-constexpr uint32_t NORM_MIN_WIDTH = 8, NORM_MAX_WIDTH = 16384;
+constexpr uint32_t NORM_MIN_WIDTH = 8, NORM_MAX_WIDTH = 8192;
 constexpr uint64_t NORM_MAX_ROWS = 1ull << 40;
 constexpr uint32_t NORM_BACKWARD_GROUPS = 512;     // workgroups aimed at: two to a CU
 constexpr uint32_t NORM_SUMS = 5;                  // pre w, pre b, post w, post b, gate
@@ -41,8 +41,8 @@ struct NormShape { uint32_t lanes, vecs; };
 static NormShape norm_shape(uint32_t width, bool gated_backward) {
     if (width <= 512) return {WAVE, 1};
     if (width <= 1024 && !gated_backward) return {WAVE, 2};
-    if (width <= 8192) return {(width + WAVE * 8 - 1) / (WAVE * 8) * WAVE, 1};
-    return {1024, 2};
+    if (width <= 4096) return {(width + WAVE * 8 - 1) / (WAVE * 8) * WAVE, 1};
+    return {512, 2};
 }
 
 static uint32_t rows_at_once(NormShape s) { return s.lanes == WAVE ? 4 : 1; }
@@ -300,8 +300,7 @@ __global__ __launch_bounds__(L::threads) void norm_forward_kernel(NormArgs a, co
     }
 }
 
-// A sum over rows for each column of a thread: in registers, or in LDS where a row takes 1024 threads,
-// which have 128 registers each (in scratch memory instead: 4,099 rows of 8192, two norms and a gate, 320 us).
+// A sum over rows for each column of a thread: in registers, or in LDS.
 template <typename L, bool LDS>
 struct ColumnSums {
     f32x8 r[LDS ? 1 : L::vecs];
@@ -375,16 +374,22 @@ __global__ __launch_bounds__(L::threads) void norm_backward_kernel(
     constexpr int AT_ONCE = L::one ? L::threads / WAVE : 1;
     __shared__ float2 slots[L::slots];
     clear_slots<L>(slots);
-    constexpr bool IN_LDS = ALL && L::threads == 1024;
-    __shared__ __attribute__((aligned(32))) float shared[L::one ? L::threads * L::vecs * 8 : IN_LDS ? 2 * L::threads * L::vecs * 8 : 8];
+    // rows of two groups a thread: as many sums as LDS holds lie there, and where registers are
+    // short all the same no row is fetched ahead
+    constexpr int SPAN = L::threads * L::vecs * 8, LDS_SUMS = ALL && !L::one && L::vecs == 2 ? 32768 / SPAN : 0;
+    constexpr bool AHEAD = L::one || L::vecs == 1 || sizeof(T) == 2;
+    __shared__ __attribute__((aligned(32))) float shared[L::one ? SPAN : LDS_SUMS ? LDS_SUMS * SPAN : 8];
     int turn = 0;
     const Columns<L> cols(L::one ? threadIdx.x % WAVE : threadIdx.x, L::one ? WAVE : blockDim.x, a.width);
     const bool drops = a.drop.bar != 65536u;
     RandomKey key = {0, 0};
     if (drops) key = random_key(a.seed);
     f32x8 pre_w[L::vecs], post_w[L::vecs], post_b[L::vecs];
-    ColumnSums<L, false> dpre_w(shared), dpre_b(shared), dpost_b(shared);
-    ColumnSums<L, IN_LDS> dpost_w(shared), dgate(shared + (IN_LDS ? L::threads * L::vecs * 8 : 0));
+    ColumnSums<L, (LDS_SUMS > 0)> dpost_w(shared);
+    ColumnSums<L, (LDS_SUMS > 1)> dgate(shared + (LDS_SUMS > 1 ? SPAN : 0));
+    ColumnSums<L, (LDS_SUMS > 2)> dpre_w(shared + (LDS_SUMS > 2 ? 2 * SPAN : 0));
+    ColumnSums<L, (LDS_SUMS > 3 && BIAS)> dpost_b(shared + (LDS_SUMS > 3 ? 3 * SPAN : 0));
+    ColumnSums<L, false> dpre_b(shared);
     if (a.pre_w) cols.load(pre_w, a.pre_w);
     if (ALL && a.post_w) cols.load(post_w, a.post_w);
     if (ALL && BIAS && a.post_b) cols.load(post_b, a.post_b);
@@ -414,8 +419,9 @@ __global__ __launch_bounds__(L::threads) void norm_backward_kernel(
         f32x8 g[L::vecs];
         if (ALL && a.gate) cols.load(g, a.gate + gate * a.width);
         uint64_t row = begin + (L::one ? threadIdx.x / WAVE : 0);
-        if (row < end) fetch(row);
+        if (AHEAD && row < end) fetch(row);
         for (; row < end; row += AT_ONCE) {
+            if (!AHEAD) fetch(row);
             const float4 st = next_st;
             f32x8 d[L::vecs], v[L::vecs], o[L::vecs], su[L::vecs];
 #pragma unroll
@@ -426,7 +432,7 @@ __global__ __launch_bounds__(L::threads) void norm_backward_kernel(
                 cols.template open<T>(v, next_h);
                 cols.template open<T>(o, next_dy);
             }
-            if (row + AT_ONCE < end) fetch(row + AT_ONCE);
+            if (AHEAD && row + AT_ONCE < end) fetch(row + AT_ONCE);
             if (a.pre_w) {
                 norm_input_gradient<L, BIAS>(o, v, pre_w, st.z, st.w, dpre_w, dpre_b, a, slots, turn);
 #pragma unroll
@@ -562,9 +568,8 @@ template <typename T>
 static void launch_norm_shape(const NormArgs& a, const NormPointers& p, bool backward, NormShape n, unsigned groups, hipStream_t s) {
     if (n.lanes == WAVE && n.vecs == 1) launch_norm<T, Layout<true, 1, 256>>(a, p, backward, groups, 256, s);
     else if (n.lanes == WAVE) launch_norm<T, Layout<true, 2, 256>>(a, p, backward, groups, 256, s);
-    else if (n.lanes <= 512) launch_norm<T, Layout<false, 1, 512>>(a, p, backward, groups, n.lanes, s);
-    else if (n.vecs == 1) launch_norm<T, Layout<false, 1, 1024>>(a, p, backward, groups, n.lanes, s);
-    else launch_norm<T, Layout<false, 2, 1024>>(a, p, backward, groups, n.lanes, s);
+    else if (n.vecs == 1) launch_norm<T, Layout<false, 1, 512>>(a, p, backward, groups, n.lanes, s);
+    else launch_norm<T, Layout<false, 2, 512>>(a, p, backward, groups, n.lanes, s);
 }
 
 static void launch_norm_type(int dtype, const NormArgs& a, const NormPointers& p, bool backward, NormShape n, unsigned groups,
