@@ -217,6 +217,14 @@ __device__ __forceinline__ Place place_of(uint32_t block, uint32_t units, uint32
     return {(run - first(die, units)) * DIES + die, at % each};
 }
 
+// A die deals its workgroups in turn, too, over its four parts.  Turns the blocks of every four
+// by `turn`, another number for every head, so that no part of a die gets all first or all last blocks, of which
+// those of a padded batch are full and empty, and those of a causal one long and short.
+__device__ __forceinline__ uint32_t turned(uint32_t block, uint32_t blocks, uint32_t turn) {
+    const uint32_t first = block & ~3u, n = blocks - first < 4 ? blocks - first : 4;
+    return first + (block - first + turn) % n;
+}
+
 // ------------------------------------------------------------------ the dropout mask
 //
 // A block of the random field is two queries by four keys, so that lanes which hold a

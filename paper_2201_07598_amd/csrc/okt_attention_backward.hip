@@ -31,7 +31,7 @@ __global__ __launch_bounds__(BWD_THREADS, 2) void attention_backward_queries_ker
     using Tile = RowTile<T, DIM, BWD_KEYS, BWD_THREADS>;
     __shared__ __attribute__((aligned(1024))) char shared[4 * Tile::BYTES];
     const Place at = place_of(blockIdx.x, a.batch * a.kv_heads, a.group * blocks * parts);
-    const uint32_t part = at.in % parts, block = at.in / parts % blocks;
+    const uint32_t part = at.in % parts, block = turned(at.in / parts % blocks, blocks, at.unit / 8 + at.in / parts / blocks);
     const uint32_t b = at.unit / a.kv_heads, kv = at.unit % a.kv_heads, h = kv * a.group + at.in / parts / blocks, plane = b * a.heads + h;
     const uint32_t wave = uniform(threadIdx.x / WAVE), lane = threadIdx.x % WAVE;
     const int ql = sequence_length(a.q_lens, b, a.q_len), kl = sequence_length(a.k_lens, b, a.k_len);
@@ -161,7 +161,7 @@ __global__ __launch_bounds__(BWD_THREADS, DIM == 64 ? 2 : 1) void attention_back
     const uint32_t wave = uniform(threadIdx.x / WAVE), lane = threadIdx.x % WAVE;
     const uint32_t part = wave / Shape::GROUPS;
     const int ql = sequence_length(a.q_lens, b, a.q_len), kl = sequence_length(a.k_lens, b, a.k_len);
-    const int k0 = at.in / parts * (Shape::GROUPS * 32), w0 = k0 + 32 * (int)(wave % Shape::GROUPS), j = w0 + (int)(lane % 32);
+    const int k0 = turned(at.in / parts, blocks, at.unit / 8) * (Shape::GROUPS * 32), w0 = k0 + 32 * (int)(wave % Shape::GROUPS), j = w0 + (int)(lane % 32);
     // the first query that sees a key: any key, the workgroup's, the wave's first and last, the lane's
     const auto first_for = [&](int key) { const int n = a.causal ? key - (kl - ql) : 0; return n < 0 ? 0 : n; };
     const int lo = first_for(0), begin = first_for(k0) / TILE * TILE;

@@ -20,7 +20,7 @@ __global__ __launch_bounds__(FWD_THREADS, 2) void attention_forward_kernel(Atten
     using Tile = RowTile<T, DIM, FWD_KEYS, FWD_THREADS>;
     __shared__ __attribute__((aligned(1024))) char shared[4 * Tile::BYTES];
     const Place at = place_of(blockIdx.x, a.batch * a.kv_heads, a.group * blocks * parts);
-    const uint32_t part = at.in % parts, block = at.in / parts % blocks;
+    const uint32_t part = at.in % parts, block = turned(at.in / parts % blocks, blocks, at.unit / 8 + at.in / parts / blocks);
     const uint32_t b = at.unit / a.kv_heads, kv = at.unit % a.kv_heads, h = kv * a.group + at.in / parts / blocks, plane = b * a.heads + h;
     const uint32_t wave = uniform(threadIdx.x / WAVE), lane = threadIdx.x % WAVE;
     const int ql = sequence_length(a.q_lens, b, a.q_len), kl = sequence_length(a.k_lens, b, a.k_len);
