@@ -201,28 +201,48 @@ __device__ __forceinline__ void store_row(T* row, const f32x16 (&c)[TILES], floa
         }
 }
 
-// Workgroups are dealt to the eight dies in turn.  A unit is what shares keys (a sequence's
-// key head, `each` workgroups): its workgroups go to one die, so that they share an L2, and
-// neighbouring units to different dies, so that long and short sequences spread over all of
-// them (a padded batch dealt in runs of neighbours: 187 us backward, so 140).
-struct Place { uint32_t unit, in; };
+// Which block of which head a workgroup takes.  A unit is what shares keys (a sequence's key
+// head): `heads` heads of `blocks` blocks, the longest block first.
+//   dies   Workgroups are dealt to the eight dies in turn.  A unit goes to one die, whose
+//          L2 its workgroups share, and neighbouring units to different dies, so that long and
+//          short sequences spread over all of them.
+//   end    Under a causal mask the last `window` heads of a die are taken block by block, not
+//          head by head, so that what starts last is short (2 x 16 heads x 4096 x 128: 65 % of
+//          the CUs' time was in use without, and the ends of the last heads took the rest).
+//   parts  A die deals its workgroups in turn over its own four parts.  Before the end, the
+//          blocks of every four are turned by another number for every head, so that no part
+//          gets the first, or the empty last, block of each.
+struct Place { uint32_t unit, head, block; };
 
-__device__ __forceinline__ Place place_of(uint32_t block, uint32_t units, uint32_t each) {
+__device__ __forceinline__ Place place_of(uint32_t index, uint32_t units, uint32_t heads, uint32_t blocks, uint32_t window) {
     constexpr uint32_t DIES = 8;
     const auto first = [](uint32_t die, uint32_t n) { const uint32_t more = n % DIES; return die * (n / DIES) + (die < more ? die : more); };
-    const uint32_t at = first(block % DIES, units * each) + block / DIES;       // every die a run of places
-    const uint32_t run = at / each, more = units % DIES, long_runs = more * (units / DIES + 1);
-    // run `run` of units is number i of a die's share: units die, die + 8, ...
+    const uint32_t total = units * heads * blocks, end = first(index % DIES + 1, total);
+    uint32_t at = first(index % DIES, total) + index / DIES;
+    const uint32_t whole = (end - first(index % DIES, total)) / blocks, rows = window < whole ? window : whole;
+    const uint32_t from = end - rows * blocks;
+    const bool ending = at >= from;
+    if (ending) {
+        const uint32_t k = at - from, block = k / rows;
+        at = from + k % rows * blocks + (block + blocks - from % blocks) % blocks;      // at % blocks is `block`
+    }
+    // units in the order of the dies' shares: number i of a die's share is unit 8 i + die
+    const uint32_t run = at / (heads * blocks), more = units % DIES, long_runs = more * (units / DIES + 1);
     const uint32_t die = run < long_runs ? run / (units / DIES + 1) : more + (run - long_runs) / (units / DIES);
-    return {(run - first(die, units)) * DIES + die, at % each};
+    Place p = {(run - first(die, units)) * DIES + die, at / blocks % heads, at % blocks};
+    if (!ending && units * heads % DIES == 0) {            // whole heads of every die
+        const uint32_t four = p.block & ~3u, n = blocks - four < 4 ? blocks - four : 4;
+        p.block = four + (p.block - four + p.unit / DIES + p.head) % n;
+    }
+    return p;
 }
 
-// A die deals its workgroups in turn, too, over its four parts.  Turns the blocks of every four
-// by `turn`, another number for every head, so that no part of a die gets all first or all last blocks, of which
-// those of a padded batch are full and empty, and those of a causal one long and short.
-__device__ __forceinline__ uint32_t turned(uint32_t block, uint32_t blocks, uint32_t turn) {
-    const uint32_t first = block & ~3u, n = blocks - first < 4 ? blocks - first : 4;
-    return first + (block - first + turn) % n;
+// Heads that a die takes block by block at its end: as many as its L2 holds the keys and
+// values of, and at least eight; none where blocks are alike.
+inline uint32_t window_of(bool causal, uint32_t k_len, uint32_t dim, uint32_t group) {
+    if (!causal) return 0;
+    const uint64_t unit_bytes = (uint64_t)k_len * dim * 4 + 1, n = (4ull << 20) / unit_bytes * group;
+    return n < 8 ? 8 : n > 64 ? 64 : (uint32_t)n;
 }
 
 // ------------------------------------------------------------------ the dropout mask

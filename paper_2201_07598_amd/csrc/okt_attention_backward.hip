@@ -27,12 +27,12 @@ typedef float2 RowNumbers;
 template <typename T, int DIM, bool DROP>
 __global__ __launch_bounds__(BWD_THREADS, 2) void attention_backward_queries_kernel(
     AttentionArgs a, const T* q, const T* k, const T* v, const T* o, const float* lse, const T* d_o, T* dq, RowNumbers* rows,
-    uint32_t blocks, uint32_t parts, float* partial) {
+    uint32_t blocks, uint32_t parts, uint32_t window, float* partial) {
     using Tile = RowTile<T, DIM, BWD_KEYS, BWD_THREADS>;
     __shared__ __attribute__((aligned(1024))) char shared[4 * Tile::BYTES];
-    const Place at = place_of(blockIdx.x, a.batch * a.kv_heads, a.group * blocks * parts);
-    const uint32_t part = at.in % parts, block = turned(at.in / parts % blocks, blocks, at.unit / 8 + at.in / parts / blocks);
-    const uint32_t b = at.unit / a.kv_heads, kv = at.unit % a.kv_heads, h = kv * a.group + at.in / parts / blocks, plane = b * a.heads + h;
+    const Place at = place_of(blockIdx.x, a.batch * a.kv_heads, a.group, blocks * parts, window);
+    const uint32_t part = at.block % parts, block = at.block / parts;
+    const uint32_t b = at.unit / a.kv_heads, kv = at.unit % a.kv_heads, h = kv * a.group + at.head, plane = b * a.heads + h;
     const uint32_t wave = uniform(threadIdx.x / WAVE), lane = threadIdx.x % WAVE;
     const int ql = sequence_length(a.q_lens, b, a.q_len), kl = sequence_length(a.k_lens, b, a.k_len);
     const int q0 = (blocks - 1 - block) * BWD_QUERIES, w0 = q0 + 32 * (int)wave, i = w0 + (int)(lane % 32);
@@ -148,20 +148,20 @@ __global__ __launch_bounds__(BWD_THREADS, 2) void attention_backward_queries_ker
 template <typename T, int DIM, bool DROP>
 __global__ __launch_bounds__(BWD_THREADS, DIM == 64 ? 2 : 1) void attention_backward_keys_kernel(
     AttentionArgs a, const T* q, const T* k, const T* v, const T* d_o, const RowNumbers* rows, T* dk, T* dv, uint32_t blocks,
-    uint32_t parts, float* partial) {
+    uint32_t parts, uint32_t window, float* partial) {
     using Shape = KeysShape<DIM>;
     constexpr int TILE = Shape::TILE, OWN = TILE / Shape::HALVES;          // queries of a tile, of a wave's part
     using Tile = RowTile<T, DIM, TILE, BWD_THREADS>;
     constexpr int NUMBERS = TILE * (int)sizeof(RowNumbers) < 1024 ? 1024 : TILE * (int)sizeof(RowNumbers);
     constexpr int BUFFER = 2 * Tile::BYTES + NUMBERS;
     __shared__ __attribute__((aligned(1024))) char shared[2 * BUFFER];
-    const Place at = place_of(blockIdx.x, a.batch * a.kv_heads, blocks * parts);
-    const uint32_t share = at.in % parts;
+    const Place at = place_of(blockIdx.x, a.batch * a.kv_heads, 1, blocks * parts, window);
+    const uint32_t share = at.block % parts;
     const uint32_t b = at.unit / a.kv_heads, kv = at.unit % a.kv_heads;
     const uint32_t wave = uniform(threadIdx.x / WAVE), lane = threadIdx.x % WAVE;
     const uint32_t part = wave / Shape::GROUPS;
     const int ql = sequence_length(a.q_lens, b, a.q_len), kl = sequence_length(a.k_lens, b, a.k_len);
-    const int k0 = turned(at.in / parts, blocks, at.unit / 8) * (Shape::GROUPS * 32), w0 = k0 + 32 * (int)(wave % Shape::GROUPS), j = w0 + (int)(lane % 32);
+    const int k0 = at.block / parts * (Shape::GROUPS * 32), w0 = k0 + 32 * (int)(wave % Shape::GROUPS), j = w0 + (int)(lane % 32);
     // the first query that sees a key: any key, the workgroup's, the wave's first and last, the lane's
     const auto first_for = [&](int key) { const int n = a.causal ? key - (kl - ql) : 0; return n < 0 ? 0 : n; };
     const int lo = first_for(0), begin = first_for(k0) / TILE * TILE;
@@ -341,7 +341,7 @@ static void launch_backward(const AttentionArgs& a, const AttentionPlan& plan, c
         const uint32_t blocks = (a.q_len + BWD_QUERIES - 1) / BWD_QUERIES, parts = plan.query_parts;
         hipLaunchKernelGGL((attention_backward_queries_kernel<T, DIM, DROP>), dim3(blocks * a.batch * a.heads * parts),
                            dim3(BWD_THREADS), 0, s, a, (const T*)p.q, (const T*)p.k, (const T*)p.v, (const T*)p.o, p.lse,
-                           (const T*)p.d_o, (T*)p.dq, rows, blocks, parts, dq_sums);
+                           (const T*)p.d_o, (T*)p.dq, rows, blocks, parts, window_of(a.causal, a.k_len, DIM, a.group), dq_sums);
         if (parts > 1) sums.of[n++] = {dq_sums, p.dq, a.dq, (uint64_t)a.batch * a.heads * a.q_len, parts, a.q_len, a.heads};
     }
     if (a.k_len) {
@@ -351,7 +351,7 @@ static void launch_backward(const AttentionArgs& a, const AttentionPlan& plan, c
         timing_before(s);
         hipLaunchKernelGGL((attention_backward_keys_kernel<T, DIM, DROP>), dim3(blocks * a.batch * a.kv_heads * parts),
                            dim3(BWD_THREADS), 0, s, a, (const T*)p.q, (const T*)p.k, (const T*)p.v, (const T*)p.d_o,
-                           (const RowNumbers*)rows, (T*)p.dk, (T*)p.dv, blocks, parts, dkv_sums);
+                           (const RowNumbers*)rows, (T*)p.dk, (T*)p.dv, blocks, parts, window_of(a.causal, a.q_len, DIM, 1), dkv_sums);
         timing_after(s);
         if (parts > 1) {
             sums.of[n++] = {dkv_sums, p.dk, a.dk, keys, parts, a.k_len, a.kv_heads};

@@ -16,12 +16,12 @@ static_assert(FWD_QUERIES == FWD_THREADS / WAVE * 32, "a wave owns 32 queries");
 template <typename T, int DIM, bool DROP>
 __global__ __launch_bounds__(FWD_THREADS, 2) void attention_forward_kernel(AttentionArgs a, const T* q, const T* k, const T* v,
                                                                            T* o, float* lse, uint32_t blocks, uint32_t parts,
-                                                                           float* partial, float2* sums) {
+                                                                           uint32_t window, float* partial, float2* sums) {
     using Tile = RowTile<T, DIM, FWD_KEYS, FWD_THREADS>;
     __shared__ __attribute__((aligned(1024))) char shared[4 * Tile::BYTES];
-    const Place at = place_of(blockIdx.x, a.batch * a.kv_heads, a.group * blocks * parts);
-    const uint32_t part = at.in % parts, block = turned(at.in / parts % blocks, blocks, at.unit / 8 + at.in / parts / blocks);
-    const uint32_t b = at.unit / a.kv_heads, kv = at.unit % a.kv_heads, h = kv * a.group + at.in / parts / blocks, plane = b * a.heads + h;
+    const Place at = place_of(blockIdx.x, a.batch * a.kv_heads, a.group, blocks * parts, window);
+    const uint32_t part = at.block % parts, block = at.block / parts;
+    const uint32_t b = at.unit / a.kv_heads, kv = at.unit % a.kv_heads, h = kv * a.group + at.head, plane = b * a.heads + h;
     const uint32_t wave = uniform(threadIdx.x / WAVE), lane = threadIdx.x % WAVE;
     const int ql = sequence_length(a.q_lens, b, a.q_len), kl = sequence_length(a.k_lens, b, a.k_len);
     const int q0 = (blocks - 1 - block) * FWD_QUERIES, w0 = q0 + 32 * (int)wave, i = w0 + (int)(lane % 32);
@@ -177,7 +177,7 @@ static void launch_forward(const AttentionArgs& a, const AttentionPlan& plan, co
     auto* kernel = a.drop.bar == 65536u ? attention_forward_kernel<T, DIM, false> : attention_forward_kernel<T, DIM, true>;
     timing_before(s);
     hipLaunchKernelGGL(kernel, dim3(blocks * a.batch * a.heads * parts), dim3(FWD_THREADS), 0, s, a, (const T*)q, (const T*)k,
-                       (const T*)v, (T*)o, lse, blocks, parts, partial, sums);
+                       (const T*)v, (T*)o, lse, blocks, parts, window_of(a.causal, a.k_len, DIM, a.group), partial, sums);
     timing_after(s);
     if (parts > 1)
         hipLaunchKernelGGL((attention_join_kernel<T, DIM>), dim3((unsigned)((rows * (DIM / 4) + FWD_THREADS - 1) / FWD_THREADS)),
