@@ -253,21 +253,36 @@ inline uint32_t window_of(bool causal, uint32_t k_len, uint32_t dim, uint32_t gr
 
 template <int CTRL>
 __device__ __forceinline__ uint32_t quad(uint32_t v) {
-    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xf, 0xf, true);
+    return (uint32_t)__builtin_amdgcn_mov_dpp((int)v, CTRL, 0xf, 0xf, true);
 }
 
-// Lane = query, element r = key 16 (l / 32) + r of the tile that begins at key0 (a multiple of 32): bit r
-// of the result says that element r is kept.  The two lanes of a pair draw two of the four
-// blocks each.
-__device__ __forceinline__ void kept_keys(uint32_t (&w)[16], uint32_t query, uint32_t key0, uint32_t plane, RandomKey key,
+// Whether element r is kept, of sixteen whose values lie two to a word.
+__device__ __forceinline__ bool kept_element(const uint32_t (&w)[8], int r, uint32_t bar) {
+    return r & 1 ? w[r / 2] < bar << 16 : (uint16_t)w[r / 2] < (uint16_t)bar;       // bar is below 65536 here
+}
+
+// Lane = query, element r = key 16 (l / 32) + r of the tile that begins at key0 (a multiple of 32).  The
+// two lanes of a pair draw two of the four blocks each, keep their own query's halves and
+// hand the other's over.
+__device__ __forceinline__ void kept_keys(uint32_t (&w)[8], uint32_t query, uint32_t key0, uint32_t plane, RandomKey key,
                                           uint32_t site) {
     const uint32_t lane = threadIdx.x % WAVE, odd = lane & 1;
-    RandomBlock b[2];
+    const uint32_t low = 0x05040100u, high = 0x07060302u, mine = odd ? high : low, other = odd ? low : high;
+    uint32_t own[4], got[4];
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
-        b[i] = random_block(key, key0 / 4 + 4 * (lane / 32) + 2 * odd + i, query / 2, plane, site);
+    for (int i = 0; i < 2; ++i) {
+        const RandomBlock b = random_block(key, key0 / 4 + 4 * (lane / 32) + 2 * odd + i, query / 2, plane, site);
 #pragma unroll
-    for (int r = 0; r < 16; ++r) w[r] = r < 8 ? quad<0xA0>(b[r / 4 % 2].w[r % 4]) : quad<0xF5>(b[r / 4 % 2].w[r % 4]);
+        for (int p = 0; p < 2; ++p) {
+            own[2 * i + p] = __builtin_amdgcn_perm(b.w[2 * p + 1], b.w[2 * p], mine);
+            got[2 * i + p] = quad<0xB1>(__builtin_amdgcn_perm(b.w[2 * p + 1], b.w[2 * p], other));
+        }
+    }
+#pragma unroll
+    for (int p = 0; p < 4; ++p) {
+        w[p] = odd ? got[p] : own[p];
+        w[p + 4] = odd ? own[p] : got[p];
+    }
 }
 
 // Lane = key, element r = query 16 (l / 32) + r of the tile that begins at query0 (a multiple of 32):

@@ -97,11 +97,10 @@ __global__ __launch_bounds__(BWD_THREADS, 2) void attention_backward_queries_ker
                     dp = mfma(Tile::rows(vt, reads, 32 * n, e), df[e], dp);
                 }
                 if (DROP) {
-                    uint32_t w[16];
+                    uint32_t w[8];
                     kept_keys(w, i, key0 + 32 * n, plane, key, a.site);
-                    const uint32_t mask = lane & 1 ? 0xffffffffu : 0xffffu, bar = a.drop.bar << (16 * (lane & 1));
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) dp[r] = (w[r] & mask) < bar ? dp[r] : 0.0f;
+                    for (int r = 0; r < 16; ++r) dp[r] = kept_element(w, r, a.drop.bar) ? dp[r] : 0.0f;
                 }
 #pragma unroll
                 for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], a.scale_log2, -base));
@@ -248,7 +247,7 @@ __global__ __launch_bounds__(BWD_THREADS, DIM == 64 ? 2 : 1) void attention_back
                         kept_queries(w, j, own0 + 32 * n, plane, key, a.site);
 #pragma unroll
                         for (int r = 0; r < 16; ++r) {
-                            const bool keep = r & 1 ? w[r / 2] < a.drop.bar << 16 : (w[r / 2] & 0xffffu) < a.drop.bar;
+                            const bool keep = kept_element(w, r, a.drop.bar);
                             const float p = s[r];
                             s[r] = keep ? p : 0.0f;
                             dp[r] = p * ((keep ? dp[r] : 0.0f) - few[r]);

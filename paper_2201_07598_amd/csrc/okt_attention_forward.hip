@@ -106,11 +106,10 @@ __global__ __launch_bounds__(FWD_THREADS, 2) void attention_forward_kernel(Atten
                     total += s[n][r];
                 }
                 if (DROP) {
-                    uint32_t w[16];
+                    uint32_t w[8];
                     kept_keys(w, i, key0 + 32 * n, plane, key, a.site);
-                    const uint32_t mask = lane & 1 ? 0xffffffffu : 0xffffu, bar = a.drop.bar << (16 * (lane & 1));
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) s[n][r] = (w[r] & mask) < bar ? s[n][r] : 0.0f;
+                    for (int r = 0; r < 16; ++r) s[n][r] = kept_element(w, r, a.drop.bar) ? s[n][r] : 0.0f;
                 }
 #pragma unroll
                 for (int t = 0; t < 2; ++t) {

@@ -22,15 +22,20 @@ __device__ __forceinline__ RandomKey random_key(const uint64_t* d_seed) {
     return {uniform((uint32_t)s), uniform((uint32_t)(s >> 32))};
 }
 
+// a ^ b ^ c in one instruction.
+__device__ __forceinline__ uint32_t xor_three(uint32_t a, uint32_t b, uint32_t c) {
+    return __builtin_amdgcn_bitop3_b32(a, b, c, 0x96);
+}
+
 __device__ __forceinline__ RandomBlock random_block(RandomKey key, uint32_t c0, uint32_t c1, uint32_t c2,
                                                     uint32_t site) {
     uint32_t c3 = site;
 #pragma unroll
     for (int r = 0; r < RANDOM_ROUNDS; ++r) {
         const uint64_t a = (uint64_t)c0 * 0xD2511F53u, b = (uint64_t)c2 * 0xCD9E8D57u;
-        c0 = (uint32_t)(b >> 32) ^ c1 ^ key.lo;
+        c0 = xor_three((uint32_t)(b >> 32), c1, key.lo);
         c1 = (uint32_t)b;
-        c2 = (uint32_t)(a >> 32) ^ c3 ^ key.hi;
+        c2 = xor_three((uint32_t)(a >> 32), c3, key.hi);
         c3 = (uint32_t)a;
         key.lo += 0x9E3779B9u;
         key.hi += 0xBB67AE85u;
