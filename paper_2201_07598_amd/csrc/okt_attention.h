@@ -12,6 +12,7 @@
 #ifndef OKT_ATTENTION_H
 #define OKT_ATTENTION_H
 
+#include "okt_attention_layout.h"
 #include "okt_element.h"
 #include "okt_random.h"
 
@@ -37,11 +38,6 @@ __device__ __forceinline__ frag<T> to_operand(const f32x16& c, int t) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = c[8 * t + i];
     return __builtin_convertvector(v, frag<T>);
-}
-
-// The row of a 32-row tile that slot s of the A operand holds.
-__device__ __forceinline__ constexpr uint32_t row_of_slot(uint32_t s) {
-    return (s & ~31u) | ((s & 4) << 2) | ((s >> 1) & 12) | (s & 3);
 }
 
 // ------------------------------------------------------------------ tiles of rows in LDS
@@ -201,50 +197,6 @@ __device__ __forceinline__ void store_row(T* row, const f32x16 (&c)[TILES], floa
         }
 }
 
-// Which block of which head a workgroup takes.  A unit is what shares keys (a sequence's key
-// head): `heads` heads of `blocks` blocks, the longest block first.
-//   dies   Workgroups are dealt to the eight dies in turn.  A unit goes to one die, whose
-//          L2 its workgroups share, and neighbouring units to different dies, so that long and
-//          short sequences spread over all of them.
-//   end    Under a causal mask the last `window` heads of a die are taken block by block, not
-//          head by head, so that what starts last is short (2 x 16 heads x 4096 x 128: 65 % of
-//          the CUs' time was in use without, and the ends of the last heads took the rest).
-//   parts  A die deals its workgroups in turn over its own four parts.  Before the end, the
-//          blocks of every four are turned by another number for every head, so that no part
-//          gets the first, or the empty last, block of each.
-struct Place { uint32_t unit, head, block; };
-
-__device__ __forceinline__ Place place_of(uint32_t index, uint32_t units, uint32_t heads, uint32_t blocks, uint32_t window) {
-    constexpr uint32_t DIES = 8;
-    const auto first = [](uint32_t die, uint32_t n) { const uint32_t more = n % DIES; return die * (n / DIES) + (die < more ? die : more); };
-    const uint32_t total = units * heads * blocks, end = first(index % DIES + 1, total);
-    uint32_t at = first(index % DIES, total) + index / DIES;
-    const uint32_t whole = (end - first(index % DIES, total)) / blocks, rows = window < whole ? window : whole;
-    const uint32_t from = end - rows * blocks;
-    const bool ending = at >= from;
-    if (ending) {
-        const uint32_t k = at - from, block = k / rows;
-        at = from + k % rows * blocks + (block + blocks - from % blocks) % blocks;      // at % blocks is `block`
-    }
-    // units in the order of the dies' shares: number i of a die's share is unit 8 i + die
-    const uint32_t run = at / (heads * blocks), more = units % DIES, long_runs = more * (units / DIES + 1);
-    const uint32_t die = run < long_runs ? run / (units / DIES + 1) : more + (run - long_runs) / (units / DIES);
-    Place p = {(run - first(die, units)) * DIES + die, at / blocks % heads, at % blocks};
-    if (!ending && units * heads % DIES == 0) {            // whole heads of every die
-        const uint32_t four = p.block & ~3u, n = blocks - four < 4 ? blocks - four : 4;
-        p.block = four + (p.block - four + p.unit / DIES + p.head) % n;
-    }
-    return p;
-}
-
-// Heads that a die takes block by block at its end: as many as its L2 holds the keys and
-// values of, and at least eight; none where blocks are alike.
-inline uint32_t window_of(bool causal, uint32_t k_len, uint32_t dim, uint32_t group) {
-    if (!causal) return 0;
-    const uint64_t unit_bytes = (uint64_t)k_len * dim * 4 + 1, n = (4ull << 20) / unit_bytes * group;
-    return n < 8 ? 8 : n > 64 ? 64 : (uint32_t)n;
-}
-
 // ------------------------------------------------------------------ the dropout mask
 //
 // A block of the random field is two queries by four keys, so that lanes which hold a
@@ -327,25 +279,6 @@ __device__ __forceinline__ void store_partial(float* row, const f32x16 (&c)[TILE
         for (int a = 0; a < 4; ++a)
             *reinterpret_cast<float4*>(row + 32 * dt + 8 * a + 4 * (threadIdx.x % WAVE / 32)) = make_float4(
                 c[dt][4 * a] * scale, c[dt][4 * a + 1] * scale, c[dt][4 * a + 2] * scale, c[dt][4 * a + 3] * scale);
-}
-
-// Steps [first, last) of `steps` that part `part` takes; part 0 takes step 0 if there is one.
-struct Part { int first, last; };
-__device__ __forceinline__ Part part_of(int steps, uint32_t part, uint32_t parts) {
-    const auto cut = [&](uint32_t p) { return (int)(((uint64_t)steps * p + parts - 1) / parts); };
-    return parts == 1 ? Part{0, steps} : Part{cut(part), cut(part + 1)};
-}
-
-// How many parts: enough to give every CU two workgroups, none of fewer than `least` steps,
-// whose time has to be worth the second launch (some 5 us).
-constexpr uint32_t PART_MAX = 32;
-inline uint32_t parts_for(uint64_t workgroups, uint64_t steps, uint32_t least) {
-    constexpr uint64_t WANTED = 512;
-    if (workgroups == 0 || workgroups * 2 > WANTED) return 1;
-    uint64_t n = (WANTED + workgroups - 1) / workgroups;
-    if (n > steps / least) n = steps / least;
-    if (n > PART_MAX) n = PART_MAX;
-    return n ? (uint32_t)n : 1;
 }
 
 // The launches of a call and the parts of the workspace, from its sizes alone.

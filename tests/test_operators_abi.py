@@ -1,0 +1,188 @@
+"""The layer's operators at the C ABI, on the CPU: the structs the binding packs are those the
+header declares, arguments out of range are refused on the host, the binding names what is
+wrong with a tensor, and the index arithmetic of the kernels covers everything once."""
+import ctypes
+import os
+import shutil
+import struct
+import subprocess
+
+import pytest
+import torch
+
+import paper_2201_07598_amd as okt
+from paper_2201_07598_amd import binding
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+OK, INVALID, WORKSPACE = 0, -1, -2
+FAKE = 0x10000                 # aligned, never dereferenced on these paths
+
+
+def offsets_in_c(tmp_path, name, members):
+    gcc = shutil.which("gcc")
+    if gcc is None:
+        pytest.skip("no gcc")
+    src, exe = tmp_path / "offsets.c", tmp_path / "offsets"
+    lines = "".join(f'    printf("%zu ", offsetof({name}, {m}));\n' for m in members)
+    src.write_text('#include <stddef.h>\n#include <stdio.h>\n#include "okt.h"\nint main(void) {\n'
+                   f'{lines}    printf("%zu\\n", sizeof({name}));\n    return 0;\n}}\n')
+    subprocess.run([gcc, "-std=c99", "-I", os.path.join(ROOT, "include"), str(src), "-o", str(exe)], check=True)
+    return [int(n) for n in subprocess.run([str(exe)], capture_output=True, text=True).stdout.split()]
+
+
+def offsets_packed(fmt):
+    """Offsets of the members of a packed format, repeats of one letter counted one by one."""
+    out, at, count = [], 0, ""
+    for ch in fmt[1:]:
+        if ch.isdigit():
+            count += ch
+            continue
+        for _ in range(int(count or 1)):
+            out.append(at)
+            at += struct.calcsize("=" + ch)
+        count = ""
+    return out + [at]
+
+
+def test_packed_structs_match_the_header(tmp_path):
+    norm = ["rows", "width", "dtype", "kind", "eps", "residual_scale", "site", "dropout_p", "d_seed",
+            "d_post_weight", "d_post_bias", "d_gate", "rows_per_gate", "d_pre_weight", "d_pre_bias", "u_stride",
+            "x_stride", "h_stride", "y_stride", "dh_stride", "dy_stride", "dx_stride", "du_stride"]
+    assert offsets_in_c(tmp_path, "okt_residual_norm", norm) == offsets_packed(binding._NORM.format)
+    attention = ["batch", "heads", "kv_heads", "q_len", "k_len", "head_dim", "dtype", "causal", "scale", "site",
+                 "dropout_p", "d_seed", "d_q_lens", "d_k_lens"]
+    attention += [f"{t}_stride[{i}]" for t in ("q", "k", "v", "o", "do", "dq", "dk", "dv") for i in range(3)]
+    assert offsets_in_c(tmp_path, "okt_attention", attention) == offsets_packed(binding._ATTENTION.format)
+
+
+def dropout(x=FAKE, y=FAKE, n=64, dtype=1, p=0.1, seed=FAKE):
+    return okt.load_library().okt_dropout(x, y, n, dtype, p, seed, 0, None)
+
+
+def test_dropout_refusals():
+    assert dropout(n=0, x=None, y=None) == OK
+    for bad in ({"x": None}, {"y": None}, {"seed": None}, {"x": FAKE + 8}, {"y": FAKE + 2}, {"seed": FAKE + 4},
+                {"dtype": 3}, {"dtype": -1}, {"p": -0.01}, {"p": 1.01}, {"p": float("nan")}, {"n": (1 << 43) + 1}):
+        assert dropout(**bad) == INVALID, bad
+
+
+NORM = dict(rows=4, width=64, dtype=1, kind=0, eps=1e-5, scale=1.0, site=0, p=0.0, seed=0, post_w=0, post_b=0, gate=0,
+            share=0, pre_w=FAKE, pre_b=FAKE, strides=(0,) * 8)
+
+
+def norm_struct(**change):
+    a = {**NORM, **change}
+    return binding._NORM.pack(a["rows"], a["width"], a["dtype"], a["kind"], a["eps"], a["scale"], a["site"], a["p"],
+                              a["seed"], a["post_w"], a["post_b"], a["gate"], a["share"], a["pre_w"], a["pre_b"], *a["strides"])
+
+
+def test_norm_refusals():
+    lib = okt.load_library()
+
+    def forward(u=FAKE, x=FAKE, h=FAKE, y=FAKE, stats=FAKE, **change):
+        return lib.okt_residual_norm_forward(norm_struct(**change), u, x, h, y, stats, None)
+
+    def backward(u=FAKE, h=FAKE, stats=FAKE, dh=FAKE, dy=FAKE, dx=FAKE, du=FAKE, pw=None, pb=None, g=None, w=None, b=None,
+                 ws=FAKE, ws_bytes=1 << 24, **change):
+        return lib.okt_residual_norm_backward(norm_struct(**change), u, h, stats, dh, dy, dx, du, pw, pb, g, w, b, ws, ws_bytes, None)
+
+    shared = [{"width": 7}, {"width": 8193}, {"rows": (1 << 40) + 1}, {"dtype": 3}, {"kind": 2}, {"eps": -1.0},
+              {"eps": float("nan")}, {"scale": float("nan")}, {"p": 1.5}, {"p": 0.5}, {"p": 0.5, "seed": FAKE + 4},
+              {"post_b": FAKE}, {"pre_w": 0}, {"pre_w": FAKE + 4}, {"strides": (63, 0, 0, 0, 0, 0, 0, 0)},
+              {"strides": (0, 0, 0, 0, 0, 0, 0, (1 << 20) + 1)}]
+    for bad in shared:
+        assert forward(**bad) == INVALID, bad
+        assert backward(**bad) == INVALID, bad
+    for bad in ({"u": None}, {"x": None}, {"y": None}, {"h": FAKE + 1}, {"stats": FAKE + 8},
+                {"pre_w": 0, "pre_b": 0, "y": FAKE}, {"pre_w": 0, "pre_b": 0, "y": None, "h": None}):
+        assert forward(**bad) == INVALID, bad
+    for bad in ({"h": None}, {"dy": None}, {"stats": None}, {"dx": None}, {"du": None}, {"pw": FAKE}, {"g": FAKE},
+                {"b": FAKE, "pre_b": 0}, {"post_w": FAKE, "u": None}, {"gate": FAKE, "u": None},
+                {"pre_w": 0, "pre_b": 0}, {"w": FAKE + 2}):
+        assert backward(**bad) == INVALID, bad
+    assert forward(rows=0, u=None, x=None) == OK
+    for bad in ({"ws": None}, {"ws": FAKE + 16}, {"ws_bytes": 255}):
+        assert backward(**bad) == WORKSPACE, bad
+    # 512 workgroups of 196 rows each would be 100,352 rows: 511 are enough, and each leaves five sums
+    assert okt.okt_residual_norm_workspace_bytes(100_000, 1024, 0) == 5 * 511 * 1024 * 4
+    assert okt.okt_residual_norm_workspace_bytes(4, 7, 0) == 0 and okt.okt_residual_norm_workspace_bytes(0, 64, 0) > 0
+
+
+ATTENTION = dict(batch=2, heads=4, kv_heads=2, q_len=8, k_len=8, dim=64, dtype=1, causal=0, scale=0.125, site=0, p=0.0,
+                 seed=0, q_lens=0, k_lens=0, strides=(2048, 256, 64) * 8)
+
+
+def attention_struct(**change):
+    a = {**ATTENTION, **change}
+    return binding._ATTENTION.pack(a["batch"], a["heads"], a["kv_heads"], a["q_len"], a["k_len"], a["dim"], a["dtype"],
+                                   a["causal"], a["scale"], a["site"], a["p"], a["seed"], a["q_lens"], a["k_lens"], *a["strides"])
+
+
+def test_attention_refusals():
+    lib = okt.load_library()
+
+    def forward(q=FAKE, k=FAKE, v=FAKE, o=FAKE, lse=FAKE, ws=FAKE, ws_bytes=1 << 30, **change):
+        return lib.okt_attention_forward(attention_struct(**change), q, k, v, o, lse, ws, ws_bytes, None)
+
+    def backward(q=FAKE, k=FAKE, v=FAKE, o=FAKE, lse=FAKE, do=FAKE, dq=FAKE, dk=FAKE, dv=FAKE, ws=FAKE, ws_bytes=1 << 30, **change):
+        return lib.okt_attention_backward(attention_struct(**change), q, k, v, o, lse, do, dq, dk, dv, ws, ws_bytes, None)
+
+    shared = [{"kv_heads": 0}, {"heads": 0}, {"heads": 5}, {"dim": 0}, {"dim": 12}, {"dim": 136}, {"dtype": 0}, {"dtype": 3},
+              {"scale": 0.0}, {"scale": -1.0}, {"scale": float("nan")}, {"scale": float("inf")}, {"p": 0.5}, {"p": -0.5},
+              {"q_len": (1 << 24) + 1}, {"batch": 1 << 20}, {"q_lens": FAKE + 2}, {"strides": (2048, 252, 64) * 8},
+              {"strides": (2048, 1 << 25, 64) * 8}, {"q": FAKE + 8}, {"k": None}, {"v": None}, {"o": None}, {"q": None}]
+    for bad in shared:
+        assert forward(**bad) == INVALID, bad
+        assert backward(**bad) == INVALID, bad
+    for bad in ({"lse": None}, {"do": None}, {"dq": None}, {"dk": None}, {"dv": FAKE + 8}):
+        assert backward(**bad) == INVALID, bad
+    for bad in ({"ws": None}, {"ws": FAKE + 16}, {"ws_bytes": 64}):
+        assert backward(**bad) == WORKSPACE, bad
+    # few rows, many keys: the forward pass needs room for its parts as well
+    long = {"q_len": 1, "k_len": 100_000, "heads": 2, "kv_heads": 1, "batch": 1}
+    assert forward(ws=None, ws_bytes=0, **long) == WORKSPACE
+    assert forward(q_len=0) == OK and forward(batch=0) == OK and backward(batch=0) == OK
+
+
+def test_attention_workspace():
+    need = okt.okt_attention_workspace_bytes(2, 16, 4, 4096, 4096, 128)
+    assert need % 256 == 0 and need >= 2 * 16 * 4096 * 8
+    for shape in ((1, 1, 1, 1, 1, 8), (1, 12, 12, 1, 4096, 64), (32, 16, 16, 512, 512, 64), (1, 4, 1, 4096, 3, 128)):
+        assert okt.okt_attention_workspace_bytes(*shape) >= 256
+    # sizes beyond 32 bits do not wrap
+    assert okt.okt_attention_workspace_bytes(1024, 128, 128, 1 << 20, 1, 128) >= 1024 * 128 * (1 << 20) * 8
+
+
+def test_binding_names_what_is_wrong():
+    x = torch.zeros(4, 64)
+    with pytest.raises(TypeError, match="CUDA"):
+        okt.okt_dropout(x, x, 0.1, torch.zeros(1, dtype=torch.int64))
+    with pytest.raises(TypeError, match="seed"):
+        okt.okt_dropout(x, x, 0.1, None)
+    with pytest.raises(ValueError, match="length"):
+        okt.okt_dropout(x, x[:1], 0.1, torch.zeros(1, dtype=torch.int64))
+    with pytest.raises(TypeError, match="float32, bfloat16 or float16"):
+        okt.okt_residual_norm_forward(x.double(), x, x, x, None, pre_weight=x[0])
+    with pytest.raises(ValueError, match="rows, width"):
+        okt.okt_residual_norm_forward(x[0], x, x, x, None, pre_weight=x[0])
+    with pytest.raises(TypeError, match="CUDA"):
+        okt.okt_residual_norm_backward(x, x, x, x, x, x, x, x, pre_weight=x[0])
+    q = torch.zeros(1, 2, 2, 64, dtype=torch.bfloat16)
+    with pytest.raises(ValueError, match="batch, length, heads"):
+        okt.okt_attention_forward(q[0], q, q, q, None)
+    with pytest.raises(ValueError, match="agree"):
+        okt.okt_attention_forward(q, q[..., :32], q, q, None)
+    with pytest.raises(TypeError, match="CUDA"):
+        okt.okt_attention_forward(q, q, q, q, None)
+
+
+def test_attention_layout_covers_everything_once(tmp_path):
+    gxx = shutil.which("g++")
+    if gxx is None:
+        pytest.skip("no g++")
+    exe = tmp_path / "layout_check"
+    subprocess.run([gxx, "-O2", "-std=c++17", "-Wall", "-Werror", "-I",
+                    os.path.join(ROOT, "paper_2201_07598_amd", "csrc"),
+                    os.path.join(ROOT, "tests", "cabi", "attention_layout_check.cpp"), "-o", str(exe)], check=True)
+    out = subprocess.run([str(exe)], capture_output=True, text=True)
+    assert out.returncode == 0 and " 0 violations" in out.stdout, out.stdout
