@@ -71,7 +71,7 @@ __global__ __launch_bounds__(BWD_THREADS, 2) void attention_backward_queries_ker
 #pragma unroll
             for (int e = 0; e < 8; ++e) sum = __builtin_fmaf(x[e], y[e], sum);
         }
-        sum = mine > 0 ? sum_halves(sum) / drop_scale : 0.0f;
+        sum = mine > 0 && drop_scale > 0.0f ? sum_halves(sum) / drop_scale : 0.0f;      // all dropped: no gradient anyway
         if (mine > 0) base = lse[(uint64_t)plane * a.q_len + row] * 1.44269504088896f;
         const TileReads reads = Tile::reads();
         RandomKey key = {0, 0};
@@ -119,7 +119,7 @@ __global__ __launch_bounds__(BWD_THREADS, 2) void attention_backward_queries_ker
 #pragma unroll
                     for (int r = 0; r < 16; ++r) few = __builtin_fmaf(s[r], dp[r] - from, few);
                     few = from + sum_halves(few);
-                    sum = mine <= 32 ? few : sum;
+                    sum = mine > 0 && mine <= 32 ? few : sum;
                 }
 #pragma unroll
                 for (int r = 0; r < 16; ++r) s[r] *= dp[r] - sum;

@@ -1,0 +1,248 @@
+"""okt_attention_forward / _backward on the GPU against the 64-bit oracle: masks, lengths, head
+layouts, strides, types, the split over the long axis, within bounds that add up the
+roundings (operators_harness)."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2201_07598_amd as okt
+from oracle import okt_operators as ops
+from tests.operators_harness import DEV, TYPES, UNIT, attention_bounds, rand, seed_tensor, step, wide, within
+
+pytestmark = pytest.mark.gpu
+
+SEED = (1 << 63) + 12345 - (1 << 64)          # as the int64 that carries the uint64
+
+
+def make(B, H, G, Sq, Sk, D, kind="bf16", scale=1.0):
+    if Sq == Sk:
+        q, k, v = rand((B, Sq, H + 2 * G, D), kind, Sq * 7 + D, scale).split([H, G, G], 2)
+    else:
+        q = rand((B, Sq, H, D), kind, Sq + D, scale)
+        k, v = rand((B, Sk, 2 * G, D), kind, Sk + D, scale).split([G, G], 2)
+    return q, k, v, rand((B, Sq, H, D), kind, 5)
+
+
+def workspace(q, k, fill=0xA5):
+    n = okt.okt_attention_workspace_bytes(q.shape[0], q.shape[2], k.shape[2], q.shape[1], k.shape[1], q.shape[3])
+    return torch.full((n,), fill, dtype=torch.uint8, device=DEV)
+
+
+def forward(q, k, v, **options):
+    o = torch.full(q.shape, 7.0, dtype=q.dtype, device=DEV)
+    lse = torch.full((q.shape[0], q.shape[2], q.shape[1]), 7.0, device=DEV)
+    okt.okt_attention_forward(q, k, v, o, lse, workspace(q, k), **options)
+    return o, lse
+
+
+def backward(q, k, v, o, lse, do, **options):
+    dq, dk, dv = (torch.full(t.shape, 7.0, dtype=q.dtype, device=DEV) for t in (q, k, v))
+    okt.okt_attention_backward(q, k, v, o, lse, do, dq, dk, dv, workspace(q, k), **options)
+    return dq, dk, dv
+
+
+def norm_of(x):
+    return float(np.linalg.norm(x))
+
+
+def check(q, k, v, do, kind, *, causal=False, scale=None, lens=None, p=0.0, site=2):
+    options = dict(causal=causal, scale=scale, dropout_p=p, site=site, seed=seed_tensor(SEED) if p else None)
+    for name, n in zip(("q_lens", "k_lens"), lens or (None, None)):
+        options[name] = None if n is None else torch.tensor(n, dtype=torch.int32, device=DEV)
+    plain = dict(causal=causal, scale=scale, q_lens=lens and lens[0], k_lens=lens and lens[1], dropout_p=p,
+                 seed=SEED & ((1 << 64) - 1), site=site)
+    Q, KK, V, DO = (wide(t) for t in (q, k, v, do))
+    u, least = UNIT[kind], step(kind)
+    o, lse = forward(q, k, v, **options)
+    want_o, want_lse = ops.attention(Q, KK, V, **plain)
+    plain["scale"] = q.shape[-1] ** -0.5 if scale is None else scale
+    bo, blse = attention_bounds(Q, KK, V, kind, **plain)
+    within(o, want_o, bo * (1 + u) + u * np.abs(want_o) + least, "o")
+    within(lse, want_lse, blse, "lse")
+    # independent roundings add up in squares: each is at most u / sqrt 3 of what it rounds
+    assert norm_of(wide(o) - want_o) <= u * norm_of(want_o) + 1e-30
+    got = backward(q, k, v, o, lse, do, **options)
+    want = ops.attention_backward(Q, KK, V, DO, **plain)
+    stored = bo * (1 + u) + u * np.abs(want_o) + least
+    for name, g, w, b in zip(("dq", "dk", "dv"), got, want, attention_bounds(Q, KK, V, kind, do=DO, o=stored, **plain)):
+        within(g, w, b * (1 + u) + u * np.abs(w) + least, name)
+    again = backward(q, k, v, o, lse, do, **options)
+    assert all(torch.equal(a, b) for a, b in zip(got, again)), "runs differ"
+    return o, lse, got
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f16"])
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("Sq,Sk", [(1, 1), (2, 2), (1, 70), (70, 1), (31, 33), (32, 32), (64, 64), (65, 129), (129, 65),
+                                   (128, 128), (200, 200), (257, 300), (300, 257)])
+@pytest.mark.parametrize("D", [64, 128])
+def test_lengths(Sq, Sk, D, causal, kind):
+    check(*make(2, 2, 1, Sq, Sk, D, kind), kind, causal=causal)
+
+
+@pytest.mark.parametrize("D", [8, 16, 24, 32, 40, 56, 72, 80, 96, 104, 120])
+def test_head_sizes(D):
+    check(*make(2, 3, 3, 100, 100, D), "bf16", causal=True, p=0.1)
+
+
+@pytest.mark.parametrize("H,G", [(1, 1), (5, 5), (6, 2), (8, 1), (7, 7)])
+@pytest.mark.parametrize("p", [0.0, 0.25])
+def test_head_groups(H, G, p):
+    check(*make(3, H, G, 90, 150, 64, "f16"), "f16", causal=True, p=p)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("p", [0.0, 0.5])
+def test_padded_batches(D, causal, p):
+    """Lengths of nothing, of one, whole, and such that the causal mask leaves rows empty."""
+    lens = ([140, 0, 1, 77, 140, 100, 33], [140, 140, 0, 1, 33, 140, 64])
+    check(*make(7, 2, 2, 140, 140, D), "bf16", causal=causal, lens=lens, p=p)
+
+
+def test_lengths_out_of_range_are_held_to_the_tensors():
+    q, k, v, do = make(3, 2, 1, 50, 50, 64)
+    o, lse, g = check(q, k, v, do, "bf16", lens=([50, 0, 50], [50, 50, 0]))
+    options = dict(q_lens=torch.tensor([1 << 30, -5, 51], dtype=torch.int32, device=DEV),
+                   k_lens=torch.tensor([50, 99, -1], dtype=torch.int32, device=DEV))
+    o2, lse2 = forward(q, k, v, **options)
+    assert torch.equal(o, o2) and torch.equal(lse, lse2)
+    assert all(torch.equal(a, b) for a, b in zip(g, backward(q, k, v, o2, lse2, do, **options)))
+
+
+@pytest.mark.parametrize("D", [40, 64, 128])
+def test_what_lies_past_the_lengths_is_not_looked_at(D):
+    """Infinities and NaN in the padding, and in rows that the causal mask leaves empty."""
+    B, H, G, S = 2, 2, 1, 150
+    lens = ([100, 150], [37, 90])
+    q, k, v, do = (t.contiguous() for t in make(B, H, G, S, S, D))
+    options = dict(causal=True, q_lens=torch.tensor(lens[0], dtype=torch.int32, device=DEV),
+                   k_lens=torch.tensor(lens[1], dtype=torch.int32, device=DEV))
+    o, lse = forward(q, k, v, **options)
+    clean = backward(q, k, v, o, lse, do, **options)
+    for b in range(B):
+        ql, kl = lens[0][b], lens[1][b]
+        for t, n in ((q, ql), (do, ql), (k, kl), (v, kl)):
+            t[b, n:] = float("nan")
+            t[b, n::3] = float("inf")
+        q[b, :ql - kl] = float("nan")                              # these see no key
+        do[b, :ql - kl] = float("nan")
+    o2, lse2 = forward(q, k, v, **options)
+    assert torch.equal(o, o2) and torch.equal(lse, lse2)
+    assert all(torch.equal(a, b) for a, b in zip(clean, backward(q, k, v, o2, lse2, do, **options)))
+
+
+@pytest.mark.parametrize("D", [24, 40, 72, 104])
+def test_what_lies_between_heads_is_not_looked_at(D):
+    """Narrow heads in wide places: the columns past head_dim belong to somebody else."""
+    B, H, S, room = 2, 2, 70, 128
+    wide_ones = [torch.full((B, S, H, room), float("nan"), dtype=torch.bfloat16, device=DEV) for _ in range(4)]
+    views = [w[..., :D] for w in wide_ones]
+    for n, t in enumerate(views):
+        t.copy_(rand((B, S, H, D), "bf16", 20 + n))
+    check(*views, "bf16", causal=True)
+
+
+def test_strides_of_every_kind():
+    """Length before batch, heads before length, and gradients written into one packed buffer."""
+    S, B, H, D = 90, 3, 2, 64
+    q, k, v, do = (rand((S, B, H, D), "bf16", n).transpose(0, 1) for n in range(4))
+    o, lse, g = check(q, k, v, do, "bf16", causal=True)
+    swapped = [t.permute(0, 2, 1, 3).contiguous().permute(0, 2, 1, 3) for t in (q, k, v, do)]
+    o2, lse2 = forward(*swapped[:3], causal=True)
+    assert torch.equal(o, o2) and torch.equal(lse, lse2)
+    packed = torch.full((B, S, 3 * H, D), 5.0, dtype=torch.bfloat16, device=DEV)
+    dq, dk, dv = packed.split([H, H, H], 2)
+    okt.okt_attention_backward(q, k, v, o, lse, do, dq, dk, dv, workspace(q, k), causal=True)
+    assert all(torch.equal(a, b) for a, b in zip(g, (dq, dk, dv)))
+
+
+def test_offsets_beyond_32_bits():
+    """Sequences that lie more than 2^32 bytes, and 2^31 elements, apart."""
+    B, S, H, D = 2, 70, 1, 64
+    apart = (1 << 31) + (1 << 12)
+    store = torch.empty(apart + S * H * D, dtype=torch.bfloat16, device=DEV)
+    k = store.as_strided((B, S, H, D), (apart, H * D, D, 1))
+    q, _, v, do = make(B, H, H, S, S, D)
+    k.copy_(rand((B, S, H, D), "bf16", 99))
+    check(q, k, v, do, "bf16")
+    del store, k
+    torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("Sq,Sk,H,G,D,causal,p", [(1, 3000, 2, 1, 64, False, 0.0), (40, 2500, 2, 2, 128, True, 0.2),
+                                                  (2500, 3, 4, 1, 128, False, 0.1), (1500, 40, 2, 2, 64, True, 0.0),
+                                                  (700, 700, 3, 1, 64, True, 0.1), (3, 2049, 8, 2, 40, True, 0.0)])
+def test_work_split_over_the_long_axis(Sq, Sk, H, G, D, causal, p):
+    lens = ([Sq, max(1, Sq // 2)], [Sk, max(1, Sk // 3)])
+    check(*make(2, H, G, Sq, Sk, D), "bf16", causal=causal, p=p, lens=lens)
+
+
+@pytest.mark.parametrize("p", [0.0, 0.1])
+def test_scores_of_every_size(p):
+    """A softmax that is all but one key, and one that is nearly even; a maximum that grows along the keys."""
+    q, k, v, do = make(1, 2, 2, 130, 260, 64, "bf16", scale=4.0)
+    check(q, k, v, do, "bf16", p=p)
+    check(q, k, v, do, "bf16", scale=1e-3, p=p)
+    ramp = torch.linspace(0, 1, 260, device=DEV).to(torch.bfloat16)[None, :, None, None]
+    check(q, k * ramp, v, do, "bf16", p=p)
+
+
+def test_one_key_has_no_gradient_but_its_value():
+    q, k, v, do = make(2, 4, 2, 33, 1, 64)
+    _, _, (dq, dk, _) = check(q, k, v, do, "bf16")
+    assert bool((dq == 0).all()) and bool((dk == 0).all())
+
+
+def test_everything_dropped_and_nothing_there():
+    q, k, v, do = make(2, 2, 2, 40, 40, 64)
+    seed = seed_tensor(3)
+    o, lse = forward(q, k, v, dropout_p=1.0, seed=seed)
+    assert bool((o == 0).all()) and bool(torch.isfinite(lse).all())
+    assert all(bool((g == 0).all()) for g in backward(q, k, v, o, lse, do, dropout_p=1.0, seed=seed))
+    none = torch.empty(2, 0, 2, 64, dtype=torch.bfloat16, device=DEV)
+    o, lse = forward(q, none, none)
+    assert bool((o == 0).all()) and bool(torch.isneginf(lse).all())
+    dq, _, _ = backward(q, none, none, o, lse, do)
+    assert bool((dq == 0).all())
+    o, lse = forward(none, k, v)
+    _, dk, dv = backward(none, k, v, o, lse, none)
+    assert bool((dk == 0).all()) and bool((dv == 0).all())
+
+
+def test_another_stream():
+    q, k, v, do = make(2, 2, 1, 100, 100, 64)
+    o, lse = forward(q, k, v, causal=True)
+    side = torch.cuda.Stream()
+    o2, lse2 = torch.empty_like(o), torch.empty_like(lse)
+    ws = workspace(q, k)
+    torch.cuda.synchronize()
+    okt.okt_attention_forward(q, k, v, o2, lse2, ws, causal=True, stream=side)
+    side.synchronize()
+    assert torch.equal(o, o2) and torch.equal(lse, lse2)
+
+
+def test_a_graph_replays_with_new_inputs_and_seeds():
+    q, k, v, do = (t.contiguous() for t in make(2, 4, 2, 150, 700, 64))
+    seed, ws = seed_tensor(1), workspace(q, k)
+    o, lse = torch.empty_like(q), torch.empty(2, 4, 150, device=DEV)
+    grads = [torch.empty_like(t) for t in (q, k, v)]
+    options = dict(dropout_p=0.1, seed=seed)
+
+    def step_():
+        okt.okt_attention_forward(q, k, v, o, lse, ws, **options)
+        okt.okt_attention_backward(q, k, v, o, lse, do, *grads, ws, **options)
+
+    step_()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step_()
+    for n in range(3):
+        seed.fill_(40 + n)
+        q.copy_(rand(q.shape, "bf16", 60 + n))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in (o, lse, *grads)]
+        step_()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, (o, lse, *grads))), n
