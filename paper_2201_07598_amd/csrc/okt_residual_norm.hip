@@ -254,7 +254,8 @@ __global__ __launch_bounds__(L::threads) void norm_forward_kernel(NormArgs a, co
     f32x8 pre_w[L::vecs], pre_b[L::vecs];
     if (a.pre_w) cols.load(pre_w, a.pre_w);
     if (a.pre_b) cols.load(pre_b, a.pre_b);
-    for (uint64_t row = (uint64_t)blockIdx.x * AT_ONCE + (L::one ? threadIdx.x / WAVE : 0); row < a.rows; row += (uint64_t)gridDim.x * AT_ONCE) {
+    for (uint64_t row = (uint64_t)blockIdx.x * AT_ONCE + (L::one ? threadIdx.x / WAVE : 0); row < a.rows;
+         row += (uint64_t)gridDim.x * AT_ONCE) {
         f32x8 s[L::vecs], r[L::vecs];
         float4 st = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
         cols.load(s, u + row * a.u_stride);
@@ -317,6 +318,12 @@ struct ColumnSums {
         if (LDS) *reinterpret_cast<f32x8*>(at + i * L::threads * 8) += v;
         else r[LDS ? 0 : i] += v;
     }
+    __device__ __forceinline__ void add(int i, f32x8 a, f32x8 b) {          // a b, without rounding the product
+        f32x8 sum = LDS ? *reinterpret_cast<f32x8*>(at + i * L::threads * 8) : r[LDS ? 0 : i];
+        sum = __builtin_elementwise_fma(a, b, sum);
+        if (LDS) *reinterpret_cast<f32x8*>(at + i * L::threads * 8) = sum;
+        else r[LDS ? 0 : i] = sum;
+    }
     __device__ __forceinline__ void get(f32x8 (&to)[L::vecs]) const {
 #pragma unroll
         for (int i = 0; i < L::vecs; ++i) to[i] = LDS ? *reinterpret_cast<const f32x8*>(at + i * L::threads * 8) : r[LDS ? 0 : i];
@@ -333,18 +340,18 @@ __device__ __forceinline__ void norm_input_gradient(f32x8 (&d)[L::vecs], const f
 #pragma unroll
     for (int i = 0; i < L::vecs; ++i) {
         xhat[i] = (v[i] - mean) * r;
-        const f32x8 p = d[i] * xhat[i];
-        dw.add(i, p);
+        dw.add(i, d[i], xhat[i]);
         if (BIAS) db.add(i, d[i]);
         d[i] *= w[i];
         plain += sum_eight(d[i]);
-        along += sum_eight(p * w[i]);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) along = __builtin_fmaf(d[i][j], xhat[i][j], along);
     }
     row_sums<L>(plain, along, slots, turn);
     plain = a.layer ? plain * a.inv_width : 0.0f;
     along *= a.inv_width;
 #pragma unroll
-    for (int i = 0; i < L::vecs; ++i) d[i] = (d[i] - plain - xhat[i] * along) * r;
+    for (int i = 0; i < L::vecs; ++i) d[i] = __builtin_elementwise_fma(xhat[i], (f32x8)-along, d[i] - plain) * r;
 }
 
 // Adds what the waves of a workgroup that work on different rows hold, and writes it out.
@@ -449,7 +456,7 @@ __global__ __launch_bounds__(L::threads) void norm_backward_kernel(
                         f32x8 s = su[i];
                         if (a.post_w) s = (s - st.x) * st.y * post_w[i];
                         if (BIAS && a.post_b) s += post_b[i];
-                        dgate.add(i, d[i] * s);       // d holds the mask and its scale already
+                        dgate.add(i, d[i], s);        // d holds the mask and its scale already
                         d[i] *= g[i];
                     }
                 }
