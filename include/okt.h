@@ -634,7 +634,7 @@ int okt_residual_norm_backward(const okt_residual_norm* op, const void* d_u, con
  * units from 16-bit inputs with fp32 sums; p and ds are rounded to the tensors' type for the
  * second product of each pass.
  * A tensor is [batch][length][heads][head_dim] by strides {batch, length, heads} in elements,
- * head_dim contiguous; strides are multiples of 8 (that of the length at most 2^24), bases
+ * head_dim contiguous; strides are multiples of 8 (that of the length from head_dim to 2^24), bases
  * 16-byte aligned, so the parts of a common projection are taken as they lie.
  */
 typedef struct okt_attention {

@@ -94,27 +94,31 @@ struct RowTile {
         }
     };
 
-    // Fetches rows first .. first + ROWS - 1 of a tensor (its row 0 at `base`, `count` rows)
-    // straight into LDS.  The buffer's bounds end with the last row, so that rows past it
-    // arrive as zeros whatever lies there, as do rows before `lo`.
-    static __device__ __forceinline__ void fetch(uint32_t tile, const T* base, uint32_t row_bytes, const Places& p, int first,
-                                                 int lo, int count, uint32_t head_dim) {
-        const uint32_t wave = uniform(threadIdx.x / WAVE);
-        const uint64_t from = (uint64_t)base + (uint64_t)first * row_bytes;
-        const uint64_t bytes = (uint64_t)(count - first - 1) * row_bytes + head_dim * 2;
-        const i32x4 buffer = {(int)uniform((uint32_t)from), (int)uniform((uint32_t)(from >> 32)),
-                              (int)(bytes < OUTSIDE ? uniform((uint32_t)bytes) : OUTSIDE), 0x00020000};
-        if (first >= lo) {
+    // Tiles of a tensor one after the other, straight into LDS.  The buffer's bounds end with the
+    // last row, so that rows past it arrive as zeros whatever lies there.
+    struct Stream {
+        uint64_t at, left, step;                    // of the next tile: its address, bytes to the tensor's end
+        __device__ __forceinline__ Stream(const T* base, uint32_t row_bytes, int first, int count, uint32_t head_dim)
+            : at((uint64_t)base + (uint64_t)first * row_bytes), left((uint64_t)(count - first - 1) * row_bytes + head_dim * 2),
+              step((uint64_t)ROWS * row_bytes) {}
+        // `before`: how many rows at the tile's beginning are not looked at, either
+        __device__ __forceinline__ void fetch(uint32_t tile, const Places& p, int before = 0) {
+            const uint32_t wave = uniform(threadIdx.x / WAVE);
+            const i32x4 buffer = {(int)uniform((uint32_t)at), (int)uniform((uint32_t)(at >> 32)),
+                                  (int)uniform(left < OUTSIDE ? (uint32_t)left : OUTSIDE), 0x00020000};
+            if (before <= 0) {
 #pragma unroll
-            for (int i = 0; i < LOADS; ++i) fetch_to_lds(tile + (i * (THREADS / WAVE) + wave) * 1024, p.at[i], buffer);
-        } else {
+                for (int i = 0; i < LOADS; ++i) fetch_to_lds(tile + (i * (THREADS / WAVE) + wave) * 1024, p.at[i], buffer);
+            } else {
 #pragma unroll
-            for (int i = 0; i < LOADS; ++i) {
-                const bool before = first + (int)row_of_slot(fetched_slot(i)) < lo;
-                fetch_to_lds(tile + (i * (THREADS / WAVE) + wave) * 1024, before ? OUTSIDE : p.at[i], buffer);
+                for (int i = 0; i < LOADS; ++i)
+                    fetch_to_lds(tile + (i * (THREADS / WAVE) + wave) * 1024,
+                                 (int)row_of_slot(fetched_slot(i)) < before ? OUTSIDE : p.at[i], buffer);
             }
+            at += step;
+            left = left > step ? left - step : 0;
         }
-    }
+    };
 
     static __device__ __forceinline__ TileReads reads() {
         const uint32_t lane = threadIdx.x % WAVE, in = lane % 16;
@@ -163,13 +167,20 @@ __device__ __forceinline__ void fetched() {
     __syncthreads();
 }
 
-// B operand straight from memory: lane's row, columns 16 step + 8 (l / 32) .. + 7.
-template <typename T>
-__device__ __forceinline__ frag<T> row_operand(const T* row, int step, uint32_t head_dim) {
-    const uint32_t d = 16 * step + 8 * (threadIdx.x % WAVE / 32);
-    frag<T> v = {};
-    if (d < head_dim) v = *reinterpret_cast<const frag<T>*>(row + d);
-    return v;
+// B operands straight from memory: lane's row, for each step columns 16 step + 8 (l / 32) .. + 7.
+template <int DIM, typename T>
+__device__ __forceinline__ void row_operands(frag<T> (&v)[DIM / 16], const T* row, uint32_t head_dim) {
+    const uint32_t from = 8 * (threadIdx.x % WAVE / 32);
+    if (head_dim == DIM) {
+#pragma unroll
+        for (int s = 0; s < DIM / 16; ++s) v[s] = *reinterpret_cast<const frag<T>*>(row + from + 16 * s);
+    } else {
+#pragma unroll
+        for (int s = 0; s < DIM / 16; ++s) {
+            v[s] = frag<T>{};
+            if (from + 16 * s < head_dim) v[s] = *reinterpret_cast<const frag<T>*>(row + from + 16 * s);
+        }
+    }
 }
 
 // Between a lane and the one 32 away.
@@ -187,14 +198,19 @@ template <typename T, int TILES>
 __device__ __forceinline__ void store_row(T* row, const f32x16 (&c)[TILES], float scale, uint32_t head_dim) {
     typedef T four __attribute__((ext_vector_type(4)));
     typedef float f32x4 __attribute__((ext_vector_type(4)));
+    const uint32_t from = 4 * (threadIdx.x % WAVE / 32);
+    const auto piece = [&](int dt, int a) {
+        const f32x4 v = {c[dt][4 * a] * scale, c[dt][4 * a + 1] * scale, c[dt][4 * a + 2] * scale, c[dt][4 * a + 3] * scale};
+        *reinterpret_cast<four*>(row + from + 32 * dt + 8 * a) = __builtin_convertvector(v, four);
+    };
+    if (head_dim == TILES * 32) {
 #pragma unroll
-    for (int dt = 0; dt < TILES; ++dt)
+        for (int n = 0; n < TILES * 4; ++n) piece(n / 4, n % 4);
+    } else {
 #pragma unroll
-        for (int a = 0; a < 4; ++a) {
-            const uint32_t d = 32 * dt + 8 * a + 4 * (threadIdx.x % WAVE / 32);
-            const f32x4 v = {c[dt][4 * a] * scale, c[dt][4 * a + 1] * scale, c[dt][4 * a + 2] * scale, c[dt][4 * a + 3] * scale};
-            if (d < head_dim) *reinterpret_cast<four*>(row + d) = __builtin_convertvector(v, four);
-        }
+        for (int n = 0; n < TILES * 4; ++n)
+            if (from + 8 * n < head_dim) piece(n / 4, n % 4);
+    }
 }
 
 // ------------------------------------------------------------------ the dropout mask
@@ -306,6 +322,7 @@ struct Strides { uint64_t batch, row, head; };
 
 struct AttentionArgs {
     uint32_t batch, heads, kv_heads, group, q_len, k_len, head_dim, site;
+    Divider by_kv;                               // kv_heads
     bool causal;
     float scale, scale_log2;                     // scale * log2 e: scores are taken to base 2
     DropoutRule drop;

@@ -27,19 +27,20 @@ typedef float2 RowNumbers;
 template <typename T, int DIM, bool DROP>
 __global__ __launch_bounds__(BWD_THREADS, 2) void attention_backward_queries_kernel(
     AttentionArgs a, const T* q, const T* k, const T* v, const T* o, const float* lse, const T* d_o, T* dq, RowNumbers* rows,
-    uint32_t blocks, uint32_t parts, uint32_t window, float* partial) {
+    Places all, uint32_t parts, Divider by_part, float* partial) {
     using Tile = RowTile<T, DIM, BWD_KEYS, BWD_THREADS>;
     __shared__ __attribute__((aligned(1024))) char shared[4 * Tile::BYTES];
-    const Place at = place_of(blockIdx.x, a.batch * a.kv_heads, a.group, blocks * parts, window);
-    const uint32_t part = at.block % parts, block = at.block / parts;
-    const uint32_t b = at.unit / a.kv_heads, kv = at.unit % a.kv_heads, h = kv * a.group + at.head, plane = b * a.heads + h;
+    const Place at = place_of(blockIdx.x, all);
+    const uint32_t block = quotient(at.block, by_part), part = at.block - block * parts, blocks = quotient(all.blocks, by_part);
+    const uint32_t b = quotient(at.unit, a.by_kv), kv = at.unit - b * a.kv_heads, h = kv * a.group + at.head, plane = b * a.heads + h;
     const uint32_t wave = uniform(threadIdx.x / WAVE), lane = threadIdx.x % WAVE;
     const int ql = sequence_length(a.q_lens, b, a.q_len), kl = sequence_length(a.k_lens, b, a.k_len);
     const int q0 = (blocks - 1 - block) * BWD_QUERIES, w0 = q0 + 32 * (int)wave, i = w0 + (int)(lane % 32);
     const int past = kl - ql + 1;
     const auto seen = [&](int query) { const int n = query + past; return query >= ql ? 0 : !a.causal || n > kl ? kl : n < 0 ? 0 : n; };
     const int keys = q0 < ql ? seen(q0 + BWD_QUERIES < ql ? q0 + BWD_QUERIES - 1 : ql - 1) : 0;
-    const int mine = seen(i), wave_least = w0 + 31 < ql ? seen(w0) : 0;
+    // a lane past the last query goes along as that one, so that no tile is masked for its sake
+    const int mine = q0 < ql ? seen(i < ql ? i : ql - 1) : 0, wave_least = w0 < ql ? seen(w0) : 0;
     const int wave_most = w0 < ql ? seen(w0 + 32 < ql ? w0 + 31 : ql - 1) : 0;
     const float drop_scale = DROP ? a.drop.scale : 1.0f;
     // the tiles of this part; part 0 also leaves the rows' numbers
@@ -60,14 +61,17 @@ __global__ __launch_bounds__(BWD_THREADS, 2) void attention_backward_queries_ker
         const uint32_t k_row = (uint32_t)a.k.row * 2, v_row = (uint32_t)a.v.row * 2;
         const typename Tile::Places k_at(k_row, a.head_dim), v_at(v_row, a.head_dim);
         const uint32_t lds = lds_address(shared);
-        Tile::fetch(lds, kb, k_row, k_at, begin, 0, kl, a.head_dim);
-        Tile::fetch(lds + Tile::BYTES, vb, v_row, v_at, begin, 0, kl, a.head_dim);
+        typename Tile::Stream k_tiles(kb, k_row, begin, kl, a.head_dim), v_tiles(vb, v_row, begin, kl, a.head_dim);
+        k_tiles.fetch(lds, k_at);
+        v_tiles.fetch(lds + Tile::BYTES, v_at);
         frag<T> qf[DIM / 16], df[DIM / 16];
+        row_operands<DIM>(qf, q_row, a.head_dim);
+        row_operands<DIM>(df, do_row, a.head_dim);
+        frag<T> of[DIM / 16];
+        row_operands<DIM>(of, o_row, a.head_dim);
 #pragma unroll
         for (int s = 0; s < DIM / 16; ++s) {
-            qf[s] = row_operand(q_row, s, a.head_dim);
-            df[s] = row_operand(do_row, s, a.head_dim);
-            const f32x8 x = __builtin_convertvector(df[s], f32x8), y = __builtin_convertvector(row_operand(o_row, s, a.head_dim), f32x8);
+            const f32x8 x = __builtin_convertvector(df[s], f32x8), y = __builtin_convertvector(of[s], f32x8);
 #pragma unroll
             for (int e = 0; e < 8; ++e) sum = __builtin_fmaf(x[e], y[e], sum);
         }
@@ -83,8 +87,8 @@ __global__ __launch_bounds__(BWD_THREADS, 2) void attention_backward_queries_ker
             const char* vt = kt + Tile::BYTES;
             if (key0 + BWD_KEYS < end) {
                 const uint32_t next = lds + (turn ^ 1) * 2 * Tile::BYTES;
-                Tile::fetch(next, kb, k_row, k_at, key0 + BWD_KEYS, 0, kl, a.head_dim);
-                Tile::fetch(next + Tile::BYTES, vb, v_row, v_at, key0 + BWD_KEYS, 0, kl, a.head_dim);
+                k_tiles.fetch(next, k_at);
+                v_tiles.fetch(next + Tile::BYTES, v_at);
             }
             if (key0 >= wave_most) continue;
             const bool masked = key0 + BWD_KEYS > wave_least;
@@ -135,7 +139,7 @@ __global__ __launch_bounds__(BWD_THREADS, 2) void attention_backward_queries_ker
     if (part == 0 && lane < 32 && i < ql) rows[(uint64_t)plane * a.q_len + i] = make_float2(base, sum);
     if (i < (int)a.q_len) {
         T* out = dq + b * a.dq.batch + (uint64_t)i * a.dq.row + h * a.dq.head;
-        if (mine == 0) {
+        if (mine == 0 || i >= ql) {
 #pragma unroll
             for (int d = 0; d < DIM / 32; ++d) acc[d] = 0.0f;
         }
@@ -146,26 +150,28 @@ __global__ __launch_bounds__(BWD_THREADS, 2) void attention_backward_queries_ker
 
 template <typename T, int DIM, bool DROP>
 __global__ __launch_bounds__(BWD_THREADS, DIM == 64 ? 2 : 1) void attention_backward_keys_kernel(
-    AttentionArgs a, const T* q, const T* k, const T* v, const T* d_o, const RowNumbers* rows, T* dk, T* dv, uint32_t blocks,
-    uint32_t parts, uint32_t window, float* partial) {
+    AttentionArgs a, const T* q, const T* k, const T* v, const T* d_o, const RowNumbers* rows, T* dk, T* dv, Places all,
+    uint32_t parts, Divider by_part, float* partial) {
     using Shape = KeysShape<DIM>;
     constexpr int TILE = Shape::TILE, OWN = TILE / Shape::HALVES;          // queries of a tile, of a wave's part
     using Tile = RowTile<T, DIM, TILE, BWD_THREADS>;
     constexpr int NUMBERS = TILE * (int)sizeof(RowNumbers) < 1024 ? 1024 : TILE * (int)sizeof(RowNumbers);
     constexpr int BUFFER = 2 * Tile::BYTES + NUMBERS;
     __shared__ __attribute__((aligned(1024))) char shared[2 * BUFFER];
-    const Place at = place_of(blockIdx.x, a.batch * a.kv_heads, 1, blocks * parts, window);
-    const uint32_t share = at.block % parts;
-    const uint32_t b = at.unit / a.kv_heads, kv = at.unit % a.kv_heads;
+    const Place at = place_of(blockIdx.x, all);
+    const uint32_t block = quotient(at.block, by_part), share = at.block - block * parts;
+    const uint32_t b = quotient(at.unit, a.by_kv), kv = at.unit - b * a.kv_heads;
     const uint32_t wave = uniform(threadIdx.x / WAVE), lane = threadIdx.x % WAVE;
     const uint32_t part = wave / Shape::GROUPS;
     const int ql = sequence_length(a.q_lens, b, a.q_len), kl = sequence_length(a.k_lens, b, a.k_len);
-    const int k0 = at.block / parts * (Shape::GROUPS * 32), w0 = k0 + 32 * (int)(wave % Shape::GROUPS), j = w0 + (int)(lane % 32);
+    const int k0 = block * (Shape::GROUPS * 32), w0 = k0 + 32 * (int)(wave % Shape::GROUPS), j = w0 + (int)(lane % 32);
     // the first query that sees a key: any key, the workgroup's, the wave's first and last, the lane's
     const auto first_for = [&](int key) { const int n = a.causal ? key - (kl - ql) : 0; return n < 0 ? 0 : n; };
     const int lo = first_for(0), begin = first_for(k0) / TILE * TILE;
-    const int mine = j < kl ? first_for(j) : ql;
-    const int wave_least = w0 < kl ? first_for(w0) : ql + TILE, wave_most = w0 + 31 < kl ? first_for(w0 + 31) : ql;
+    // a lane past the last key goes along as that one, so that no tile is masked for its sake; queries past
+    // the last need no mask, since their rows arrive as zeros
+    const int mine = k0 < kl ? first_for(j < kl ? j : kl - 1) : ql;
+    const int wave_least = w0 < kl ? first_for(w0) : ql + TILE, wave_most = first_for(w0 + 31 < kl ? w0 + 31 : kl - 1);
     const int tiles = k0 < kl && begin < ql ? (ql - begin + TILE - 1) / TILE : 0;
     const float drop_scale = DROP ? a.drop.scale : 1.0f;
     // the steps of this share: the tiles of every head of the group, head after head
@@ -180,16 +186,21 @@ __global__ __launch_bounds__(BWD_THREADS, DIM == 64 ? 2 : 1) void attention_back
         // the tile that is fetched next, head after head of the group
         uint32_t fetch_head = kv * a.group + steps.first / tiles;
         int fetch_query = begin + steps.first % tiles * TILE;
+        const auto q_of = [&](int first) { return typename Tile::Stream(q + b * a.q.batch + fetch_head * a.q.head, q_row, first, ql, a.head_dim); };
+        const auto do_of = [&](int first) { return typename Tile::Stream(d_o + b * a.d_o.batch + fetch_head * a.d_o.head, do_row, first, ql, a.head_dim); };
+        typename Tile::Stream q_tiles = q_of(fetch_query), do_tiles = do_of(fetch_query);
         const auto fetch = [&](int turn) {
             const uint32_t to = lds + turn * BUFFER;
-            Tile::fetch(to, q + b * a.q.batch + fetch_head * a.q.head, q_row, q_at, fetch_query, lo, ql, a.head_dim);
-            Tile::fetch(to + Tile::BYTES, d_o + b * a.d_o.batch + fetch_head * a.d_o.head, do_row, do_at, fetch_query, lo, ql, a.head_dim);
+            q_tiles.fetch(to, q_at, lo - fetch_query);
+            do_tiles.fetch(to + Tile::BYTES, do_at, lo - fetch_query);
             const RowNumbers* from = rows + ((uint64_t)b * a.heads + fetch_head) * a.q_len;
             if (wave == 0) fetch_line(to + 2 * Tile::BYTES, from + fetch_query, from + ql);
             fetch_query += TILE;
             if (fetch_query >= ql) {
                 fetch_query = begin;
                 ++fetch_head;
+                q_tiles = q_of(begin);
+                do_tiles = do_of(begin);
             }
         };
         fetch(0);
@@ -197,11 +208,8 @@ __global__ __launch_bounds__(BWD_THREADS, DIM == 64 ? 2 : 1) void attention_back
         const T* k_row = k + b * a.k.batch + row * a.k.row + kv * a.k.head;
         const T* v_row = v + b * a.v.batch + row * a.v.row + kv * a.v.head;
         frag<T> kf[DIM / 16], vf[DIM / 16];
-#pragma unroll
-        for (int s = 0; s < DIM / 16; ++s) {
-            kf[s] = row_operand(k_row, s, a.head_dim);
-            vf[s] = row_operand(v_row, s, a.head_dim);
-        }
+        row_operands<DIM>(kf, k_row, a.head_dim);
+        row_operands<DIM>(vf, v_row, a.head_dim);
         const TileReads reads = Tile::reads();
         RandomKey key = {0, 0};
         if (DROP) key = random_key(a.seed);
@@ -215,7 +223,7 @@ __global__ __launch_bounds__(BWD_THREADS, DIM == 64 ? 2 : 1) void attention_back
             if (it + 1 < steps.last) fetch(turn ^ 1);
             const int own0 = query0 + (int)part * OWN;
             if (own0 + OWN > wave_least && own0 < ql) {
-                const bool masked = own0 < wave_most || own0 + OWN > ql;
+                const bool masked = own0 < wave_most;
 #pragma unroll 1
                 for (int n = 0; n < OWN / 32; ++n) {
                     const uint32_t slot0 = part * OWN + 32 * n;
@@ -239,7 +247,7 @@ __global__ __launch_bounds__(BWD_THREADS, DIM == 64 ? 2 : 1) void attention_back
 #pragma unroll
                         for (int r = 0; r < 16; ++r) {
                             const int i = own0 + 32 * n + 16 * (int)(lane / 32) + r;
-                            s[r] = i >= mine && i < ql ? s[r] : 0.0f;
+                            s[r] = i >= mine ? s[r] : 0.0f;
                         }
                     }
                     if (DROP) {
@@ -294,7 +302,7 @@ __global__ __launch_bounds__(BWD_THREADS, DIM == 64 ? 2 : 1) void attention_back
         }
     }
     if (part == 0 && j < (int)a.k_len) {
-        if (mine >= ql) {
+        if (mine >= ql || j >= kl) {
 #pragma unroll
             for (int d = 0; d < DIM / 32; ++d) dkacc[d] = dvacc[d] = 0.0f;
         }
@@ -340,7 +348,9 @@ static void launch_backward(const AttentionArgs& a, const AttentionPlan& plan, c
         const uint32_t blocks = (a.q_len + BWD_QUERIES - 1) / BWD_QUERIES, parts = plan.query_parts;
         hipLaunchKernelGGL((attention_backward_queries_kernel<T, DIM, DROP>), dim3(blocks * a.batch * a.heads * parts),
                            dim3(BWD_THREADS), 0, s, a, (const T*)p.q, (const T*)p.k, (const T*)p.v, (const T*)p.o, p.lse,
-                           (const T*)p.d_o, (T*)p.dq, rows, blocks, parts, window_of(a.causal, a.k_len, DIM, a.group), dq_sums);
+                           (const T*)p.d_o, (T*)p.dq, rows,
+                           places(a.batch * a.kv_heads, a.group, blocks * parts, window_of(a.causal, a.k_len, DIM, a.group)), parts,
+                           divider(parts), dq_sums);
         if (parts > 1) sums.of[n++] = {dq_sums, p.dq, a.dq, (uint64_t)a.batch * a.heads * a.q_len, parts, a.q_len, a.heads};
     }
     if (a.k_len) {
@@ -350,7 +360,9 @@ static void launch_backward(const AttentionArgs& a, const AttentionPlan& plan, c
         timing_before(s);
         hipLaunchKernelGGL((attention_backward_keys_kernel<T, DIM, DROP>), dim3(blocks * a.batch * a.kv_heads * parts),
                            dim3(BWD_THREADS), 0, s, a, (const T*)p.q, (const T*)p.k, (const T*)p.v, (const T*)p.d_o,
-                           (const RowNumbers*)rows, (T*)p.dk, (T*)p.dv, blocks, parts, window_of(a.causal, a.q_len, DIM, 1), dkv_sums);
+                           (const RowNumbers*)rows, (T*)p.dk, (T*)p.dv, 
+                           places(a.batch * a.kv_heads, 1, blocks * parts, window_of(a.causal, a.q_len, DIM, 1)), parts, divider(parts),
+                           dkv_sums);
         timing_after(s);
         if (parts > 1) {
             sums.of[n++] = {dkv_sums, p.dk, a.dk, keys, parts, a.k_len, a.kv_heads};

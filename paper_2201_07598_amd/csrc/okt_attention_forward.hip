@@ -15,13 +15,13 @@ static_assert(FWD_QUERIES == FWD_THREADS / WAVE * 32, "a wave owns 32 queries");
 
 template <typename T, int DIM, bool DROP>
 __global__ __launch_bounds__(FWD_THREADS, 2) void attention_forward_kernel(AttentionArgs a, const T* q, const T* k, const T* v,
-                                                                           T* o, float* lse, uint32_t blocks, uint32_t parts,
-                                                                           uint32_t window, float* partial, float2* sums) {
+                                                                           T* o, float* lse, Places all, uint32_t parts,
+                                                                           Divider by_part, float* partial, float2* sums) {
     using Tile = RowTile<T, DIM, FWD_KEYS, FWD_THREADS>;
     __shared__ __attribute__((aligned(1024))) char shared[4 * Tile::BYTES];
-    const Place at = place_of(blockIdx.x, a.batch * a.kv_heads, a.group, blocks * parts, window);
-    const uint32_t part = at.block % parts, block = at.block / parts;
-    const uint32_t b = at.unit / a.kv_heads, kv = at.unit % a.kv_heads, h = kv * a.group + at.head, plane = b * a.heads + h;
+    const Place at = place_of(blockIdx.x, all);
+    const uint32_t block = quotient(at.block, by_part), part = at.block - block * parts, blocks = quotient(all.blocks, by_part);
+    const uint32_t b = quotient(at.unit, a.by_kv), kv = at.unit - b * a.kv_heads, h = kv * a.group + at.head, plane = b * a.heads + h;
     const uint32_t wave = uniform(threadIdx.x / WAVE), lane = threadIdx.x % WAVE;
     const int ql = sequence_length(a.q_lens, b, a.q_len), kl = sequence_length(a.k_lens, b, a.k_len);
     const int q0 = (blocks - 1 - block) * FWD_QUERIES, w0 = q0 + 32 * (int)wave, i = w0 + (int)(lane % 32);
@@ -30,7 +30,8 @@ __global__ __launch_bounds__(FWD_THREADS, 2) void attention_forward_kernel(Atten
     const int past = kl - ql + 1;
     const auto seen = [&](int query) { const int n = query + past; return query >= ql ? 0 : !a.causal || n > kl ? kl : n < 0 ? 0 : n; };
     const int keys = q0 < ql ? seen(q0 + FWD_QUERIES < ql ? q0 + FWD_QUERIES - 1 : ql - 1) : 0;
-    const int mine = seen(i), wave_least = w0 + 31 < ql ? seen(w0) : 0;
+    // a lane past the last query goes along as that one, so that no tile is masked for its sake
+    const int mine = q0 < ql ? seen(i < ql ? i : ql - 1) : 0, wave_least = w0 < ql ? seen(w0) : 0;
     const int wave_most = w0 < ql ? seen(w0 + 32 < ql ? w0 + 31 : ql - 1) : 0;
 
     // the tiles of this part
@@ -47,12 +48,12 @@ __global__ __launch_bounds__(FWD_THREADS, 2) void attention_forward_kernel(Atten
         const uint32_t k_row = (uint32_t)a.k.row * 2, v_row = (uint32_t)a.v.row * 2;
         const typename Tile::Places k_at(k_row, a.head_dim), v_at(v_row, a.head_dim);
         const uint32_t lds = lds_address(shared);
-        Tile::fetch(lds, kb, k_row, k_at, begin, 0, kl, a.head_dim);
-        Tile::fetch(lds + Tile::BYTES, vb, v_row, v_at, begin, 0, kl, a.head_dim);
+        typename Tile::Stream k_tiles(kb, k_row, begin, kl, a.head_dim), v_tiles(vb, v_row, begin, kl, a.head_dim);
+        k_tiles.fetch(lds, k_at);
+        v_tiles.fetch(lds + Tile::BYTES, v_at);
         const T* qrow = q + b * a.q.batch + (uint64_t)(i < ql ? i : ql - 1) * a.q.row + h * a.q.head;
         frag<T> qf[DIM / 16];
-#pragma unroll
-        for (int s = 0; s < DIM / 16; ++s) qf[s] = row_operand(qrow, s, a.head_dim);
+        row_operands<DIM>(qf, qrow, a.head_dim);
         const TileReads reads = Tile::reads();
         RandomKey key = {0, 0};
         if (DROP) key = random_key(a.seed);
@@ -62,8 +63,8 @@ __global__ __launch_bounds__(FWD_THREADS, 2) void attention_forward_kernel(Atten
             const char* vt = kt + Tile::BYTES;
             if (key0 + FWD_KEYS < end) {
                 const uint32_t next = lds + (turn ^ 1) * 2 * Tile::BYTES;
-                Tile::fetch(next, kb, k_row, k_at, key0 + FWD_KEYS, 0, kl, a.head_dim);
-                Tile::fetch(next + Tile::BYTES, vb, v_row, v_at, key0 + FWD_KEYS, 0, kl, a.head_dim);
+                k_tiles.fetch(next, k_at);
+                v_tiles.fetch(next + Tile::BYTES, v_at);
             }
             if (key0 >= wave_most) continue;
             f32x16 s[FWD_KEYS / 32];
@@ -125,14 +126,14 @@ __global__ __launch_bounds__(FWD_THREADS, 2) void attention_forward_kernel(Atten
         if (i < (int)a.q_len) {
             const uint64_t row = ((uint64_t)part * a.batch * a.heads + plane) * a.q_len + i;
             store_partial(partial + row * DIM, acc, 1.0f);
-            if (lane < 32) sums[row] = make_float2(top, total);
+            if (lane < 32) sums[row] = make_float2(i < ql ? top : -INFINITY, total);
         }
         return;
     }
     if (i < (int)a.q_len) {
-        store_row(o + b * a.o.batch + (uint64_t)i * a.o.row + h * a.o.head, acc, mine > 0 ? a.drop.scale / total : 0.0f, a.head_dim);
+        store_row(o + b * a.o.batch + (uint64_t)i * a.o.row + h * a.o.head, acc, mine > 0 && i < ql ? a.drop.scale / total : 0.0f, a.head_dim);
         if (lse && lane < 32)
-            lse[(uint64_t)plane * a.q_len + i] = mine > 0 ? (top + __builtin_amdgcn_logf(total)) * 0.693147180559945f : -INFINITY;
+            lse[(uint64_t)plane * a.q_len + i] = mine > 0 && i < ql ? (top + __builtin_amdgcn_logf(total)) * 0.693147180559945f : -INFINITY;
     }
 }
 
@@ -176,7 +177,8 @@ static void launch_forward(const AttentionArgs& a, const AttentionPlan& plan, co
     auto* kernel = a.drop.bar == 65536u ? attention_forward_kernel<T, DIM, false> : attention_forward_kernel<T, DIM, true>;
     timing_before(s);
     hipLaunchKernelGGL(kernel, dim3(blocks * a.batch * a.heads * parts), dim3(FWD_THREADS), 0, s, a, (const T*)q, (const T*)k,
-                       (const T*)v, (T*)o, lse, blocks, parts, window_of(a.causal, a.k_len, DIM, a.group), partial, sums);
+                       (const T*)v, (T*)o, lse, places(a.batch * a.kv_heads, a.group, blocks * parts, window_of(a.causal, a.k_len, DIM, a.group)),
+                       parts, divider(parts), partial, sums);
     timing_after(s);
     if (parts > 1)
         hipLaunchKernelGGL((attention_join_kernel<T, DIM>), dim3((unsigned)((rows * (DIM / 4) + FWD_THREADS - 1) / FWD_THREADS)),
@@ -205,12 +207,13 @@ AttentionPlan attention_plan(uint32_t batch, uint32_t heads, uint32_t kv_heads, 
     return p;
 }
 
-// Strides of a tensor of these sizes; one that is never taken may be anything.
-static bool strides(const uint64_t (&s)[3], uint32_t batch, uint32_t length, uint32_t heads, Strides& to) {
-    to = {batch > 1 ? s[0] : 0, length > 1 ? s[1] : 0, heads > 1 ? s[2] : 0};
+// Strides of a tensor of these sizes; one that is never taken may be anything.  Rows do not overlap: a
+// fetch's bounds, in bytes, are what keeps it from rows past the last.
+static bool strides(const uint64_t (&s)[3], uint32_t batch, uint32_t length, uint32_t heads, uint32_t head_dim, Strides& to) {
+    to = {batch > 1 ? s[0] : 0, length > 1 ? s[1] : head_dim, heads > 1 ? s[2] : 0};
     for (uint64_t n : {to.batch, to.row, to.head})
         if (n % 8 || n > (1ull << 40)) return false;
-    return to.row <= (1u << 24);                 // so that a tile's offsets fit 32 bits
+    return to.row >= head_dim && to.row <= (1u << 24);        // a tile's offsets fit 32 bits
 }
 
 bool attention_args(const okt_attention* op, bool backward, AttentionArgs& a) {
@@ -225,7 +228,7 @@ bool attention_args(const okt_attention* op, bool backward, AttentionArgs& a) {
     if (a.drop.bar != 65536u && (!op->d_seed || !aligned(op->d_seed, 8))) return false;
     if (!aligned(op->d_q_lens, 4) || !aligned(op->d_k_lens, 4)) return false;
     const auto take = [&](const uint64_t (&from)[3], bool keys, Strides& to) {
-        return strides(from, op->batch, keys ? op->k_len : op->q_len, keys ? op->kv_heads : op->heads, to);
+        return strides(from, op->batch, keys ? op->k_len : op->q_len, keys ? op->kv_heads : op->heads, op->head_dim, to);
     };
     if (!take(op->q_stride, false, a.q) || !take(op->k_stride, true, a.k) || !take(op->v_stride, true, a.v) ||
         !take(op->o_stride, false, a.o)) return false;
@@ -235,6 +238,7 @@ bool attention_args(const okt_attention* op, bool backward, AttentionArgs& a) {
     a.heads = op->heads;
     a.kv_heads = op->kv_heads;
     a.group = op->heads / op->kv_heads;
+    a.by_kv = divider(op->kv_heads);
     a.q_len = op->q_len;
     a.k_len = op->k_len;
     a.head_dim = op->head_dim;

@@ -19,6 +19,21 @@ OKT_LAYOUT_FN constexpr uint32_t row_of_slot(uint32_t s) {
     return (s & ~31u) | ((s & 4) << 2) | ((s >> 1) & 12) | (s & 3);
 }
 
+// A divisor known on the host.  Exact for numbers below 2^30: with 2^shift >= by, mul exceeds
+// 2^(30 + shift) / by by less than one, so the product by less than 2^30 2^-30.  A division by a
+// number that only the kernel's arguments hold takes some twenty instructions, and a
+// workgroup's place takes eight of them.
+struct Divider { uint32_t by, mul, shift; };
+
+OKT_LAYOUT_FN Divider divider(uint32_t by) {
+    Divider d = {by ? by : 1, 0, 0};
+    while (1u << d.shift < d.by) ++d.shift;
+    d.mul = (uint32_t)(((1ull << (30 + d.shift)) + d.by - 1) / d.by);
+    return d;
+}
+OKT_LAYOUT_FN uint32_t quotient(uint32_t n, Divider d) { return (uint32_t)((uint64_t)n * d.mul >> (30 + d.shift)); }
+OKT_LAYOUT_FN uint32_t remainder(uint32_t n, Divider d) { return n - quotient(n, d) * d.by; }
+
 // Which block of which head a workgroup takes.  A unit is what shares keys (a sequence's key
 // head): `heads` heads of `blocks` blocks, the longest block first.
 //   dies   Workgroups are dealt to the eight dies in turn.  A unit goes to one die, whose
@@ -28,29 +43,45 @@ OKT_LAYOUT_FN constexpr uint32_t row_of_slot(uint32_t s) {
 //          head by head, so that what starts last is short (2 x 16 heads x 4096 x 128: 65 % of
 //          the CUs' time was in use without, and the ends of the last heads took the rest).
 //   parts  A die deals its workgroups in turn over its own four parts.  Before the end, the
-//          blocks of every four are turned by another number for every head, so that no part
-//          gets the first, or the empty last, block of each.
+//          blocks of every four (or last two) are turned by another number for every head, so
+//          that no part gets the first, or the empty last, block of each.
+constexpr uint32_t DIES = 8;
+
+struct Places {
+    uint32_t units, heads, blocks, window;
+    Divider by_block, by_head, by_unit, by_short, by_long;     // blocks, heads, heads * blocks, units / 8, units / 8 + 1
+};
+
+OKT_LAYOUT_FN Places places(uint32_t units, uint32_t heads, uint32_t blocks, uint32_t window) {
+    return {units, heads, blocks, window, divider(blocks), divider(heads), divider(heads * blocks), divider(units / DIES),
+            divider(units / DIES + 1)};
+}
+
 struct Place { uint32_t unit, head, block; };
 
-OKT_LAYOUT_FN Place place_of(uint32_t index, uint32_t units, uint32_t heads, uint32_t blocks, uint32_t window) {
-    constexpr uint32_t DIES = 8;
+OKT_LAYOUT_FN Place place_of(uint32_t index, const Places& a) {
     const auto first = [](uint32_t die, uint32_t n) { const uint32_t more = n % DIES; return die * (n / DIES) + (die < more ? die : more); };
-    const uint32_t total = units * heads * blocks, end = first(index % DIES + 1, total);
+    const uint32_t total = a.units * a.heads * a.blocks;
     uint32_t at = first(index % DIES, total) + index / DIES;
-    const uint32_t whole = (end - first(index % DIES, total)) / blocks, rows = window < whole ? window : whole;
-    const uint32_t from = end - rows * blocks;
-    const bool ending = at >= from;
-    if (ending) {
-        const uint32_t k = at - from, block = k / rows;
-        at = from + k % rows * blocks + (block + blocks - from % blocks) % blocks;      // at % blocks is `block`
+    bool ending = false;
+    if (a.window) {
+        const uint32_t end = first(index % DIES + 1, total), whole = quotient(end - first(index % DIES, total), a.by_block);
+        const uint32_t rows = a.window < whole ? a.window : whole, from = end - rows * a.blocks;
+        ending = at >= from;
+        if (ending) {
+            const uint32_t k = at - from, block = k / rows;
+            at = from + k % rows * a.blocks + remainder(block + a.blocks - remainder(from, a.by_block), a.by_block);   // at % blocks is `block`
+        }
     }
     // units in the order of the dies' shares: number i of a die's share is unit 8 i + die
-    const uint32_t run = at / (heads * blocks), more = units % DIES, long_runs = more * (units / DIES + 1);
-    const uint32_t die = run < long_runs ? run / (units / DIES + 1) : more + (run - long_runs) / (units / DIES);
-    Place p = {(run - first(die, units)) * DIES + die, at / blocks % heads, at % blocks};
-    if (!ending && units * heads % DIES == 0) {            // whole heads of every die
-        const uint32_t four = p.block & ~3u, n = blocks - four < 4 ? blocks - four : 4;
-        p.block = four + (p.block - four + p.unit / DIES + p.head) % n;
+    const uint32_t run = quotient(at, a.by_unit), more = a.units % DIES, long_runs = more * (a.units / DIES + 1);
+    const uint32_t die = run < long_runs ? quotient(run, a.by_long) : more + quotient(run - long_runs, a.by_short);
+    const uint32_t row = quotient(at, a.by_block);
+    Place p = {(run - first(die, a.units)) * DIES + die, remainder(row, a.by_head), at - row * a.blocks};
+    if (!ending && a.units * a.heads % DIES == 0) {            // whole heads of every die
+        const uint32_t four = p.block & ~3u, left = a.blocks - four, turn = p.unit / DIES + p.head;
+        if (left >= 4) p.block = four + ((p.block + turn) & 3);
+        else if (left == 2) p.block = four + ((p.block + turn) & 1);
     }
     return p;
 }

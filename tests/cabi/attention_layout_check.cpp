@@ -15,8 +15,9 @@ int main() {
                 for (uint32_t window : {0u, 1u, 8u, 64u}) {
                     std::set<std::tuple<uint32_t, uint32_t, uint32_t>> seen;
                     const uint32_t total = units * heads * blocks;
+                    const okt::Places places = okt::places(units, heads, blocks, window);
                     for (uint32_t i = 0; i < total; ++i) {
-                        const okt::Place p = okt::place_of(i, units, heads, blocks, window);
+                        const okt::Place p = okt::place_of(i, places);
                         if (p.unit >= units || p.head >= heads || p.block >= blocks) ++bad;
                         seen.insert({p.unit, p.head, p.block});
                     }
@@ -42,6 +43,16 @@ int main() {
                 if (n < 1 || n > okt::PART_MAX || (n > 1 && n * (uint64_t)least > steps)) ++bad;
                 ++cases;
             }
+    for (uint32_t by = 1; by < (1u << 30); by = by < 5000 ? by + 1 : by + by / 7 + 1) {
+        const okt::Divider d = okt::divider(by);
+        for (uint32_t m : {0u, 1u, 2u, 3u, 1000u, ((1u << 30) - 1) / by, ((1u << 30) - 1) / by / 2})
+            for (int64_t off : {(int64_t)-1, (int64_t)0, (int64_t)1, (int64_t)(by / 2)}) {
+                const int64_t n = (int64_t)m * by + off;
+                if (n < 0 || n >= (1ll << 30)) continue;
+                if (okt::quotient((uint32_t)n, d) != n / by || okt::remainder((uint32_t)n, d) != n % by) ++bad;
+                ++cases;
+            }
+    }
     uint64_t rows = 0;
     for (uint32_t s = 0; s < 32; ++s) rows |= 1ull << okt::row_of_slot(s);
     if (rows != 0xffffffffull) ++bad;

@@ -130,7 +130,7 @@ def test_attention_refusals():
     shared = [{"kv_heads": 0}, {"heads": 0}, {"heads": 5}, {"dim": 0}, {"dim": 12}, {"dim": 136}, {"dtype": 0}, {"dtype": 3},
               {"scale": 0.0}, {"scale": -1.0}, {"scale": float("nan")}, {"scale": float("inf")}, {"p": 0.5}, {"p": -0.5},
               {"q_len": (1 << 24) + 1}, {"batch": 1 << 20}, {"q_lens": FAKE + 2}, {"strides": (2048, 252, 64) * 8},
-              {"strides": (2048, 1 << 25, 64) * 8}, {"q": FAKE + 8}, {"k": None}, {"v": None}, {"o": None}, {"q": None}]
+              {"strides": (2048, 1 << 25, 64) * 8}, {"strides": (2048, 0, 64) * 8}, {"q": FAKE + 8}, {"k": None}, {"v": None}, {"o": None}, {"q": None}]
     for bad in shared:
         assert forward(**bad) == INVALID, bad
         assert backward(**bad) == INVALID, bad
