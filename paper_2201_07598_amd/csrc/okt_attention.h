@@ -219,9 +219,24 @@ __device__ __forceinline__ void store_row(T* row, const f32x16 (&c)[TILES], floa
 // query's keys and lanes which hold a key's queries both share blocks with neighbours
 // and none is drawn twice in a pass over a tile.
 
-template <int CTRL>
-__device__ __forceinline__ uint32_t quad(uint32_t v) {
-    return (uint32_t)__builtin_amdgcn_mov_dpp((int)v, CTRL, 0xf, 0xf, true);
+// The row of its tile that a lane takes as its own: even rows in one row of sixteen lanes, odd
+// rows in the next, so that those which share blocks can swap words in one instruction.
+__device__ __forceinline__ uint32_t row_of_lane() { return threadIdx.x % 16 * 2 + threadIdx.x / 16 % 2; }
+
+// Even rows of sixteen lanes get `a` of their own and of the lanes after them, odd ones `b` of the
+// lanes before them and of their own.
+__device__ __forceinline__ void swap_sixteens(uint32_t& a, uint32_t& b) {
+    const auto r = __builtin_amdgcn_permlane16_swap(a, b, false, false);
+    a = r[0];
+    b = r[1];
+}
+
+// The same between neighbouring lanes.
+__device__ __forceinline__ void swap_neighbours(uint32_t& a, uint32_t& b) {
+    const bool odd = threadIdx.x & 1;
+    const uint32_t got = (uint32_t)__builtin_amdgcn_mov_dpp((int)(odd ? a : b), 0xB1, 0xf, 0xf, true);
+    a = odd ? got : a;
+    b = odd ? b : got;
 }
 
 // Whether element r is kept, of sixteen whose values lie two to a word.
@@ -230,51 +245,37 @@ __device__ __forceinline__ bool kept_element(const uint32_t (&w)[8], int r, uint
 }
 
 // Lane = query, element r = key 16 (l / 32) + r of the tile that begins at key0 (a multiple of 32).  The
-// two lanes of a pair draw two of the four blocks each, keep their own query's halves and
-// hand the other's over.
+// two lanes of a pair of queries draw two of the four blocks each and swap the halves that
+// are the other's.
 __device__ __forceinline__ void kept_keys(uint32_t (&w)[8], uint32_t query, uint32_t key0, uint32_t plane, RandomKey key,
                                           uint32_t site) {
-    const uint32_t lane = threadIdx.x % WAVE, odd = lane & 1;
-    const uint32_t low = 0x05040100u, high = 0x07060302u, mine = odd ? high : low, other = odd ? low : high;
-    uint32_t own[4], got[4];
+    const uint32_t lane = threadIdx.x % WAVE;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-        const RandomBlock b = random_block(key, key0 / 4 + 4 * (lane / 32) + 2 * odd + i, query / 2, plane, site);
+        const RandomBlock b = random_block(key, key0 / 4 + 4 * (lane / 32) + 2 * (lane / 16 % 2) + i, query / 2, plane, site);
 #pragma unroll
         for (int p = 0; p < 2; ++p) {
-            own[2 * i + p] = __builtin_amdgcn_perm(b.w[2 * p + 1], b.w[2 * p], mine);
-            got[2 * i + p] = quad<0xB1>(__builtin_amdgcn_perm(b.w[2 * p + 1], b.w[2 * p], other));
+            w[2 * i + p] = __builtin_amdgcn_perm(b.w[2 * p + 1], b.w[2 * p], 0x05040100u);          // low halves
+            w[2 * i + p + 4] = __builtin_amdgcn_perm(b.w[2 * p + 1], b.w[2 * p], 0x07060302u);      // high halves
         }
     }
 #pragma unroll
-    for (int p = 0; p < 4; ++p) {
-        w[p] = odd ? got[p] : own[p];
-        w[p + 4] = odd ? own[p] : got[p];
-    }
+    for (int p = 0; p < 4; ++p) swap_sixteens(w[p], w[p + 4]);
 }
 
 // Lane = key, element r = query 16 (l / 32) + r of the tile that begins at query0 (a multiple of 32):
-// w[p] is the word of queries 2p and 2p + 1.  Each of the four lanes of a quad draws two of
-// the eight blocks, and a 4 x 4 transpose hands every lane its key's words.
+// w[p] is the word of queries 2p and 2p + 1.  Each of the four lanes that hold the keys of a
+// block draws two of the eight, and a 4 x 4 transpose hands every lane its key's words.
 __device__ __forceinline__ void kept_queries(uint32_t (&w)[8], uint32_t key_index, uint32_t query0, uint32_t plane,
                                              RandomKey key, uint32_t site) {
     const uint32_t lane = threadIdx.x % WAVE;
-    const bool one = lane & 1, two = lane & 2;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-        RandomBlock b = random_block(key, key_index / 4, query0 / 2 + 8 * (lane / 32) + 4 * i + lane % 4, plane, site);
-#pragma unroll
-        for (int p = 0; p < 4; p += 2) {
-            const uint32_t got = quad<0xB1>(one ? b.w[p] : b.w[p + 1]);
-            b.w[p] = one ? got : b.w[p];
-            b.w[p + 1] = one ? b.w[p + 1] : got;
-        }
-#pragma unroll
-        for (int p = 0; p < 2; ++p) {
-            const uint32_t got = quad<0x4E>(two ? b.w[p] : b.w[p + 2]);
-            b.w[p] = two ? got : b.w[p];
-            b.w[p + 2] = two ? b.w[p + 2] : got;
-        }
+        RandomBlock b = random_block(key, key_index / 4, query0 / 2 + 8 * (lane / 32) + 4 * i + row_of_lane() % 4, plane, site);
+        swap_sixteens(b.w[0], b.w[1]);
+        swap_sixteens(b.w[2], b.w[3]);
+        swap_neighbours(b.w[0], b.w[2]);
+        swap_neighbours(b.w[1], b.w[3]);
 #pragma unroll
         for (int p = 0; p < 4; ++p) w[4 * i + p] = b.w[p];
     }

@@ -35,7 +35,7 @@ __global__ __launch_bounds__(BWD_THREADS, 2) void attention_backward_queries_ker
     const uint32_t b = quotient(at.unit, a.by_kv), kv = at.unit - b * a.kv_heads, h = kv * a.group + at.head, plane = b * a.heads + h;
     const uint32_t wave = uniform(threadIdx.x / WAVE), lane = threadIdx.x % WAVE;
     const int ql = sequence_length(a.q_lens, b, a.q_len), kl = sequence_length(a.k_lens, b, a.k_len);
-    const int q0 = (blocks - 1 - block) * BWD_QUERIES, w0 = q0 + 32 * (int)wave, i = w0 + (int)(lane % 32);
+    const int q0 = (blocks - 1 - block) * BWD_QUERIES, w0 = q0 + 32 * (int)wave, i = w0 + (int)row_of_lane();
     const int past = kl - ql + 1;
     const auto seen = [&](int query) { const int n = query + past; return query >= ql ? 0 : !a.causal || n > kl ? kl : n < 0 ? 0 : n; };
     const int keys = q0 < ql ? seen(q0 + BWD_QUERIES < ql ? q0 + BWD_QUERIES - 1 : ql - 1) : 0;
@@ -164,7 +164,7 @@ __global__ __launch_bounds__(BWD_THREADS, DIM == 64 ? 2 : 1) void attention_back
     const uint32_t wave = uniform(threadIdx.x / WAVE), lane = threadIdx.x % WAVE;
     const uint32_t part = wave / Shape::GROUPS;
     const int ql = sequence_length(a.q_lens, b, a.q_len), kl = sequence_length(a.k_lens, b, a.k_len);
-    const int k0 = block * (Shape::GROUPS * 32), w0 = k0 + 32 * (int)(wave % Shape::GROUPS), j = w0 + (int)(lane % 32);
+    const int k0 = block * (Shape::GROUPS * 32), w0 = k0 + 32 * (int)(wave % Shape::GROUPS), j = w0 + (int)row_of_lane();
     // the first query that sees a key: any key, the workgroup's, the wave's first and last, the lane's
     const auto first_for = [&](int key) { const int n = a.causal ? key - (kl - ql) : 0; return n < 0 ? 0 : n; };
     const int lo = first_for(0), begin = first_for(k0) / TILE * TILE;

@@ -24,7 +24,7 @@ __global__ __launch_bounds__(FWD_THREADS, 2) void attention_forward_kernel(Atten
     const uint32_t b = quotient(at.unit, a.by_kv), kv = at.unit - b * a.kv_heads, h = kv * a.group + at.head, plane = b * a.heads + h;
     const uint32_t wave = uniform(threadIdx.x / WAVE), lane = threadIdx.x % WAVE;
     const int ql = sequence_length(a.q_lens, b, a.q_len), kl = sequence_length(a.k_lens, b, a.k_len);
-    const int q0 = (blocks - 1 - block) * FWD_QUERIES, w0 = q0 + 32 * (int)wave, i = w0 + (int)(lane % 32);
+    const int q0 = (blocks - 1 - block) * FWD_QUERIES, w0 = q0 + 32 * (int)wave, i = w0 + (int)row_of_lane();
 
     // keys that a query sees; the most of the workgroup's queries, the least and most of the wave's
     const int past = kl - ql + 1;
