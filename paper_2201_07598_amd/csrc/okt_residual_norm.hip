@@ -87,6 +87,7 @@ struct NormArgs {
     uint32_t width, site;
     float eps, alpha, inv_width;
     bool layer;
+    uint32_t shift;                                 // see Columns
     DropoutRule drop;                               // bar 65536: none
     const uint64_t* seed;
     const float *post_w, *post_b, *gate, *pre_w, *pre_b;
@@ -156,20 +157,23 @@ __device__ __forceinline__ float sum_eight(f32x8 v) {
 
 // The columns of one thread: groups of eight, as many apart as threads hold the row.  A
 // group that the row ends in, or before, is read as the last eight elements of the row and moved into
-// place, so every load of a row is one wide load that depends on nothing.
+// place, so every load of a row is one wide load that depends on nothing.  An output may take an
+// input's place, so the columns that this reads beside its own have to be the same wave's: where
+// they are not, the threads of a workgroup move up by one (`shift`) and the first has none.
 template <typename L>
 struct Columns {
     uint32_t lane, lanes, width, at[L::vecs], skip[L::vecs];
     __device__ __forceinline__ Columns(uint32_t lane_, uint32_t lanes_, uint32_t width_) : lane(lane_), lanes(lanes_), width(width_) {
 #pragma unroll
         for (int v = 0; v < L::vecs; ++v) {
-            const uint32_t col = group(v) * 8;
+            const uint32_t col = group(v) < (width + 7) / 8 ? group(v) * 8 : width;
             at[v] = col + 8 <= width ? col : width - 8;
-            skip[v] = col - at[v];
+            skip[v] = col - at[v];                                  // 8: no columns
         }
     }
     __device__ __forceinline__ uint32_t group(int v) const { return v * lanes + lane; }
-    __device__ __forceinline__ int count(int v) const { return skip[v] < 8 ? 8 - (int)skip[v] : 0; }
+    __device__ __forceinline__ uint32_t first(int v) const { return at[v] + skip[v]; }
+    __device__ __forceinline__ int count(int v) const { return 8 - (int)skip[v]; }
 
     template <typename T>
     struct Raw { typename Eight<T>::vec v[L::vecs]; };
@@ -196,7 +200,7 @@ struct Columns {
     __device__ __forceinline__ void store(T* row, const f32x8 (&from)[L::vecs]) const {
 #pragma unroll
         for (int v = 0; v < L::vecs; ++v) {
-            T* p = row + group(v) * 8;
+            T* p = row + first(v);
             if (!skip[v]) store_eight(p, from[v]);
             else if (skip[v] < 8) store_some(p, from[v], 8 - (int)skip[v]);
         }
@@ -234,7 +238,7 @@ __device__ __forceinline__ void drop_row(f32x8 (&v)[L::vecs], const Columns<L>& 
                                          const NormArgs& a) {
 #pragma unroll
     for (int i = 0; i < L::vecs; ++i) {
-        const RandomBlock b = random_block(key, cols.group(i), (uint32_t)row, (uint32_t)(row >> 32), a.site);
+        const RandomBlock b = random_block(key, cols.first(i) / 8, (uint32_t)row, (uint32_t)(row >> 32), a.site);
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[i][j] = kept(b, j, a.drop.bar) ? v[i][j] * a.drop.scale : 0.0f;
     }
@@ -247,7 +251,7 @@ __global__ __launch_bounds__(L::threads) void norm_forward_kernel(NormArgs a, co
     __shared__ float2 slots[L::slots];
     clear_slots<L>(slots);
     int turn = 0;
-    const Columns<L> cols(L::one ? threadIdx.x % WAVE : threadIdx.x, L::one ? WAVE : blockDim.x, a.width);
+    const Columns<L> cols(L::one ? threadIdx.x % WAVE : threadIdx.x - a.shift, L::one ? WAVE : blockDim.x, a.width);
     const bool drops = a.drop.bar != 65536u;
     RandomKey key = {0, 0};
     if (drops) key = random_key(a.seed);
@@ -387,7 +391,7 @@ __global__ __launch_bounds__(L::threads) void norm_backward_kernel(
     constexpr bool AHEAD = L::one || L::vecs == 1 || sizeof(T) == 2;
     __shared__ __attribute__((aligned(32))) float shared[L::one ? SPAN : LDS_SUMS ? LDS_SUMS * SPAN : 8];
     int turn = 0;
-    const Columns<L> cols(L::one ? threadIdx.x % WAVE : threadIdx.x, L::one ? WAVE : blockDim.x, a.width);
+    const Columns<L> cols(L::one ? threadIdx.x % WAVE : threadIdx.x - a.shift, L::one ? WAVE : blockDim.x, a.width);
     const bool drops = a.drop.bar != 65536u;
     RandomKey key = {0, 0};
     if (drops) key = random_key(a.seed);
@@ -545,6 +549,7 @@ static bool norm_args(const okt_residual_norm* op, NormArgs& a) {
     a.alpha = op->residual_scale;
     a.inv_width = 1.0f / (float)op->width;
     a.layer = op->kind == OKT_NORM_LAYER;
+    a.shift = op->width % 8 != 0 && op->width / 8 % WAVE == 0;
     a.seed = op->d_seed;
     a.post_w = op->d_post_weight;
     a.post_b = op->d_post_bias;
@@ -612,6 +617,11 @@ int okt_residual_norm_forward(const okt_residual_norm* op, const void* d_u, cons
     for (const void* p : {d_u, d_x, (const void*)d_h_out, (const void*)d_y_out})
         if (!aligned(p, e)) return OKT_ERR_INVALID_ARG;
     if (!aligned(d_stats_out, 16)) return OKT_ERR_INVALID_ARG;
+    // in an input's place, row by row
+    for (const void* out : {(const void*)d_h_out, (const void*)d_y_out}) {
+        const uint64_t stride = out == d_h_out ? a.h_stride : a.y_stride;
+        if (out && a.rows > 1 && ((out == d_u && stride != a.u_stride) || (out == d_x && stride != a.x_stride))) return OKT_ERR_INVALID_ARG;
+    }
     a.stats = (float4*)d_stats_out;
     const NormShape shape = norm_shape(a.width, false);
     const uint64_t at_once = rows_at_once(shape);
@@ -641,6 +651,11 @@ int okt_residual_norm_backward(const okt_residual_norm* op, const void* d_u, con
         const size_t e = dtype_bytes(op->dtype);
         for (const void* p : {d_u, d_h, d_dh, d_dy, (const void*)d_dx_out, (const void*)d_du_out})
             if (!aligned(p, e)) return OKT_ERR_INVALID_ARG;
+        const struct { const void* p; uint64_t stride; } in[] = {{all ? d_u : nullptr, a.u_stride}, {a.pre_w ? d_h : nullptr, a.h_stride},
+                                                                 {d_dh, a.dh_stride}, {d_dy, a.dy_stride}};
+        for (const auto& t : in)                                // in an input's place, row by row
+            if (t.p && a.rows > 1 && ((t.p == d_dx_out && t.stride != a.dx_stride) || (t.p == d_du_out && t.stride != a.du_stride)))
+                return OKT_ERR_INVALID_ARG;
     }
     const NormShape shape = norm_shape(a.width, all);
     const NormPlan plan = norm_plan(a.rows, a.rows_per_gate, rows_at_once(shape));

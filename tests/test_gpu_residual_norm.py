@@ -172,6 +172,24 @@ def test_outputs_in_the_place_of_inputs():
         assert torch.equal(a.grads[n], b.grads[n]), n
 
 
+@pytest.mark.parametrize("form", [dict(), dict(pre=False, gates=1), dict(pre=False, gates=2, post=True, p=0.1)], ids=str)
+@pytest.mark.parametrize("width", [516, 1028, 4100])
+def test_in_place_where_the_last_columns_are_another_wave_s(width, form):
+    """The row's last group reads columns of the group ahead of it, which another wave stores."""
+    a, b = Case(1500, width, "bf16", **form), Case(1500, width, "bf16", **form)
+    a.forward()
+    okt.okt_residual_norm_forward(b.u, b.x, b.x, b.y, b.stats, **b.options)
+    assert torch.equal(a.h, b.x) and (a.y is None or torch.equal(a.y, b.y)) and torch.equal(a.stats, b.stats)
+    a.backward()
+    b.h, b.dx = b.x, b.dh
+    b.backward()
+    assert torch.equal(a.dx, b.dx) and torch.equal(a.du, b.du)
+    b.dh, b.dx, b.du = a.dh, a.dx.clone(), b.u                                      # du over u
+    if form:
+        b.backward()
+        assert torch.equal(a.dx, b.dx) and torch.equal(a.du, b.u)
+
+
 def test_results_do_not_change_from_run_to_run():
     c = Case(3001, 520, "bf16", post=True, gates=3, p=0.2)
     c.forward()

@@ -100,6 +100,9 @@ def test_norm_refusals():
                 {"b": FAKE, "pre_b": 0}, {"post_w": FAKE, "u": None}, {"gate": FAKE, "u": None},
                 {"pre_w": 0, "pre_b": 0}, {"w": FAKE + 2}):
         assert backward(**bad) == INVALID, bad
+    other = FAKE + 4096                                             # in an input's place, with another stride
+    assert forward(u=other, strides=(0, 72, 0, 0, 0, 0, 0, 0), y=other + 4096) == INVALID
+    assert backward(u=None, h=other, dy=other + 4096, du=other + 8192, strides=(0, 0, 0, 0, 72, 0, 0, 0)) == INVALID
     assert forward(rows=0, u=None, x=None) == OK
     for bad in ({"ws": None}, {"ws": FAKE + 16}, {"ws_bytes": 255}):
         assert backward(**bad) == WORKSPACE, bad
