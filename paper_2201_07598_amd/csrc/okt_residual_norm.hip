@@ -87,7 +87,6 @@ struct NormArgs {
     uint32_t width, site;
     float eps, alpha, inv_width;
     bool layer;
-    uint32_t shift;                                 // see Columns
     DropoutRule drop;                               // bar 65536: none
     const uint64_t* seed;
     const float *post_w, *post_b, *gate, *pre_w, *pre_b;
@@ -157,16 +156,15 @@ __device__ __forceinline__ float sum_eight(f32x8 v) {
 
 // The columns of one thread: groups of eight, as many apart as threads hold the row.  A
 // group that the row ends in, or before, is read as the last eight elements of the row and moved into
-// place, so every load of a row is one wide load that depends on nothing.  An output may take an
-// input's place, so the columns that this reads beside its own have to be the same wave's: where
-// they are not, the threads of a workgroup move up by one (`shift`) and the first has none.
+// place, so every load of a row is one wide load that depends on nothing.  What it reads of another
+// thread's columns is dropped, so an output may take an input's place.
 template <typename L>
 struct Columns {
     uint32_t lane, lanes, width, at[L::vecs], skip[L::vecs];
     __device__ __forceinline__ Columns(uint32_t lane_, uint32_t lanes_, uint32_t width_) : lane(lane_), lanes(lanes_), width(width_) {
 #pragma unroll
         for (int v = 0; v < L::vecs; ++v) {
-            const uint32_t col = group(v) < (width + 7) / 8 ? group(v) * 8 : width;
+            const uint32_t col = group(v) * 8 < width ? group(v) * 8 : width;
             at[v] = col + 8 <= width ? col : width - 8;
             skip[v] = col - at[v];                                  // 8: no columns
         }
@@ -251,7 +249,7 @@ __global__ __launch_bounds__(L::threads) void norm_forward_kernel(NormArgs a, co
     __shared__ float2 slots[L::slots];
     clear_slots<L>(slots);
     int turn = 0;
-    const Columns<L> cols(L::one ? threadIdx.x % WAVE : threadIdx.x - a.shift, L::one ? WAVE : blockDim.x, a.width);
+    const Columns<L> cols(L::one ? threadIdx.x % WAVE : threadIdx.x, L::one ? WAVE : blockDim.x, a.width);
     const bool drops = a.drop.bar != 65536u;
     RandomKey key = {0, 0};
     if (drops) key = random_key(a.seed);
@@ -391,7 +389,7 @@ __global__ __launch_bounds__(L::threads) void norm_backward_kernel(
     constexpr bool AHEAD = L::one || L::vecs == 1 || sizeof(T) == 2;
     __shared__ __attribute__((aligned(32))) float shared[L::one ? SPAN : LDS_SUMS ? LDS_SUMS * SPAN : 8];
     int turn = 0;
-    const Columns<L> cols(L::one ? threadIdx.x % WAVE : threadIdx.x - a.shift, L::one ? WAVE : blockDim.x, a.width);
+    const Columns<L> cols(L::one ? threadIdx.x % WAVE : threadIdx.x, L::one ? WAVE : blockDim.x, a.width);
     const bool drops = a.drop.bar != 65536u;
     RandomKey key = {0, 0};
     if (drops) key = random_key(a.seed);
@@ -549,7 +547,6 @@ static bool norm_args(const okt_residual_norm* op, NormArgs& a) {
     a.alpha = op->residual_scale;
     a.inv_width = 1.0f / (float)op->width;
     a.layer = op->kind == OKT_NORM_LAYER;
-    a.shift = op->width % 8 != 0 && op->width / 8 % WAVE == 0;
     a.seed = op->d_seed;
     a.post_w = op->d_post_weight;
     a.post_b = op->d_post_bias;

@@ -174,8 +174,8 @@ def test_outputs_in_the_place_of_inputs():
 
 @pytest.mark.parametrize("form", [dict(), dict(pre=False, gates=1), dict(pre=False, gates=2, post=True, p=0.1)], ids=str)
 @pytest.mark.parametrize("width", [516, 1028, 4100])
-def test_in_place_where_the_last_columns_are_another_wave_s(width, form):
-    """The row's last group reads columns of the group ahead of it, which another wave stores."""
+def test_in_place_at_widths_that_end_inside_a_group(width, form):
+    """The row's last group reads columns that another wave stores, and drops them."""
     a, b = Case(1500, width, "bf16", **form), Case(1500, width, "bf16", **form)
     a.forward()
     okt.okt_residual_norm_forward(b.u, b.x, b.x, b.y, b.stats, **b.options)
