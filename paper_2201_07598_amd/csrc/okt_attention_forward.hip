@@ -142,22 +142,37 @@ __global__ __launch_bounds__(FWD_THREADS, 2) void attention_forward_kernel(Atten
 template <typename T, int DIM>
 __global__ __launch_bounds__(FWD_THREADS) void attention_join_kernel(AttentionArgs a, T* o, float* lse, uint32_t parts,
                                                                      const float* partial, const float2* sums) {
-    constexpr uint32_t LANES = DIM / 4;
+    constexpr uint32_t LANES = DIM / 4, AT_ONCE = 8;
     typedef T four __attribute__((ext_vector_type(4)));
     typedef float f32x4 __attribute__((ext_vector_type(4)));
     const uint64_t rows = (uint64_t)a.batch * a.heads * a.q_len;
     const uint64_t row = (uint64_t)blockIdx.x * (FWD_THREADS / LANES) + threadIdx.x / LANES;
     const uint32_t d = threadIdx.x % LANES * 4;
     if (row >= rows) return;
-    float most = -INFINITY;
-    for (uint32_t p = 0; p < parts; ++p) most = fmaxf(most, sums[p * rows + row].x);
+    float most = -INFINITY, total = 0.0f;
     f32x4 acc = 0.0f;
-    float total = 0.0f;
-    for (uint32_t p = 0; p < parts; ++p) {
-        const float2 s = sums[p * rows + row];
-        const float weight = s.x == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(s.x - most);
-        total = __builtin_fmaf(s.y, weight, total);
-        acc += weight * *reinterpret_cast<const f32x4*>(partial + (p * rows + row) * DIM + d);
+    for (uint32_t p0 = 0; p0 < parts; p0 += AT_ONCE) {          // that many parts' loads are on their way together
+        float2 part[AT_ONCE];
+        f32x4 v[AT_ONCE];
+        float top = most;
+#pragma unroll
+        for (uint32_t n = 0; n < AT_ONCE; ++n) {
+            const uint64_t at = (p0 + n < parts ? p0 + n : parts - 1) * rows + row;
+            part[n] = sums[at];
+            v[n] = *reinterpret_cast<const f32x4*>(partial + at * DIM + d);
+            if (p0 + n >= parts) part[n].x = -INFINITY;
+            top = fmaxf(top, part[n].x);
+        }
+        const float fade = most == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(most - top);
+        most = top;
+        acc *= fade;
+        total *= fade;
+#pragma unroll
+        for (uint32_t n = 0; n < AT_ONCE; ++n) {
+            const float weight = part[n].x == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(part[n].x - most);
+            total = __builtin_fmaf(part[n].y, weight, total);
+            acc += weight * v[n];
+        }
     }
     const bool any = most != -INFINITY;
     acc *= any ? a.drop.scale / total : 0.0f;
@@ -193,11 +208,18 @@ AttentionPlan attention_plan(uint32_t batch, uint32_t heads, uint32_t kv_heads, 
     const uint64_t units = (uint64_t)batch * kv_heads, planes = (uint64_t)batch * heads, group = kv_heads ? heads / kv_heads : 0;
     const uint64_t query_blocks = (q_len + ATTENTION_QUERIES - 1) / ATTENTION_QUERIES * planes;
     const uint64_t key_steps = (k_len + ATTENTION_KEYS - 1) / ATTENTION_KEYS;
-    p.forward_parts = parts_for(query_blocks, key_steps, 4);
-    p.query_parts = parts_for(query_blocks, key_steps, 3);
-    p.key_parts = parts_for((k_len + key_block - 1) / key_block * units, (q_len + query_tile - 1) / query_tile * group, 2);
-    const auto round = [](uint64_t n) { return (size_t)((n + 255) & ~255ull); };
     const uint64_t rows = planes * q_len, keys = units * k_len;
+    const uint64_t query_steps = (q_len + query_tile - 1) / query_tile * group, row_bytes = p.dim * sizeof(float);
+    // what a step takes, fitted to 128 queries and 512 to 2048 keys: 0.75, 1.05 and 1.35 us of 64 columns
+    const auto worth = [&](uint64_t workgroups, uint64_t steps, uint64_t step_ns, uint64_t bytes, bool added) {
+        return parts_worth(parts_for(workgroups, steps, 1), steps, step_ns * p.dim, 2 * bytes, added ? 0 : PART_LAUNCH_NS);
+    };
+    const auto key_parts = [&](bool added) { return worth((k_len + key_block - 1) / key_block * units, query_steps, 21, 2 * keys * row_bytes, added); };
+    p.forward_parts = worth(query_blocks, key_steps, 12, rows * (row_bytes + 8), false);
+    p.key_parts = key_parts(false);
+    p.query_parts = worth(query_blocks, key_steps, 17, rows * row_bytes, p.key_parts > 1);
+    if (p.query_parts > 1) p.key_parts = key_parts(true);
+    const auto round = [](uint64_t n) { return (size_t)((n + 255) & ~255ull); };
     p.forward_bytes = p.forward_parts > 1 ? round(p.forward_parts * rows * (p.dim + 2) * sizeof(float)) : 0;
     p.rows_at = 0;
     p.dq_at = round(rows * 2 * sizeof(float));

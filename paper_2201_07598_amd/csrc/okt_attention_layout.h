@@ -101,8 +101,7 @@ OKT_LAYOUT_FN Part part_of(int steps, uint32_t part, uint32_t parts) {
     return parts == 1 ? Part{0, steps} : Part{cut(part), cut(part + 1)};
 }
 
-// How many parts: enough to give every CU two workgroups, none of fewer than `least` steps,
-// whose time has to be worth the second launch (some 5 us).
+// The most parts: enough to give every CU two workgroups, none of fewer than `least` steps.
 constexpr uint32_t PART_MAX = 32;
 OKT_LAYOUT_FN uint32_t parts_for(uint64_t workgroups, uint64_t steps, uint32_t least) {
     constexpr uint64_t WANTED = 512;
@@ -111,6 +110,24 @@ OKT_LAYOUT_FN uint32_t parts_for(uint64_t workgroups, uint64_t steps, uint32_t l
     if (n > steps / least) n = steps / least;
     if (n > PART_MAX) n = PART_MAX;
     return n ? (uint32_t)n : 1;
+}
+
+// How many of them are worth it: parts shorten what a workgroup does one step after the other, and cost
+// another launch and their sums' way to memory and back.  `step_ns` of a step, `part_bytes` of a part
+// written and read (at 6 TB/s, what such sums, which stay in the caches, were seen to take, and 0.2 us
+// a part for the chain of the kernel that adds them); `launch_ns` 0 where there is that launch anyway.
+constexpr uint64_t PART_LAUNCH_NS = 5000;
+OKT_LAYOUT_FN uint32_t parts_worth(uint32_t most, uint64_t steps, uint64_t step_ns, uint64_t part_bytes, uint64_t launch_ns) {
+    uint32_t best = 1;
+    uint64_t least = steps * step_ns;
+    for (uint32_t n = 2; n <= most; ++n) {
+        const uint64_t ns = (steps + n - 1) / n * step_ns + n * (part_bytes / 6000 + 200) + launch_ns;
+        if (ns < least) {
+            least = ns;
+            best = n;
+        }
+    }
+    return best;
 }
 
 }  // namespace okt

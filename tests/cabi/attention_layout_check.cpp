@@ -41,6 +41,11 @@ int main() {
             for (uint32_t least : {1u, 2u, 4u}) {
                 const uint32_t n = okt::parts_for(groups, steps, least);
                 if (n < 1 || n > okt::PART_MAX || (n > 1 && n * (uint64_t)least > steps)) ++bad;
+                // never slower by its own reckoning than no parts, and no parts where a launch costs more than all steps
+                for (uint64_t bytes : {(uint64_t)0, (uint64_t)1 << 20, (uint64_t)1 << 50}) {
+                    const uint32_t worth = okt::parts_worth(n, steps, 750, bytes, okt::PART_LAUNCH_NS);
+                    if (worth < 1 || worth > n || (bytes >> 50 && worth > 1) || (steps * 750 <= okt::PART_LAUNCH_NS && worth > 1)) ++bad;
+                }
                 ++cases;
             }
     for (uint32_t by = 1; by < (1u << 30); by = by < 5000 ? by + 1 : by + by / 7 + 1) {
