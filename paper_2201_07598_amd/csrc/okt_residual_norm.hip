@@ -10,15 +10,23 @@
 //   dv = r (w' - mean w' - xhat mean(w' xhat))     (RMS: without mean w')
 //   dw = sum over rows of dout xhat,  db = sum of dout,  dg = sum of dh drop(a)
 //
-// A row lives in the registers of a wave or of a workgroup (LANES threads of VECS groups of
-// eight columns), so the mean, the centred squares and the result are taken from one read
+// A row lives in the registers of a wave or of a workgroup (Layout: groups of eight columns a
+// thread), so the mean, the centred squares and the result are taken from one read
 // of it; everything is fp32 between the load and the one rounding of the store.  The second norm reads h as it was
 // stored, since that is what the backward pass has.  The mask of the dropout is drawn
 // again in the backward pass: a group of eight columns is a block of the random field.
 // Workgroups walk over the rows and keep the parameters, and backward the sums over rows, in
 // registers; those sums leave as one partial row per workgroup, which a second launch
 // adds in a fixed order (no atomics: the result does not change from run to run).
-// Bound by memory: forward 4 elements a place, backward 5 or 6.
+// Bound by memory: forward 4 elements a place, backward 5 or 6.  From call to call:
+//   forward   16384 x 1024 bf16   29 us, 4.6 TB/s of 134 MB (the kernel 25)
+//             128 x 768 fp32      9 us: a launch and one chain of load, two sums and store
+//   backward  16384 x 1024 bf16   38 us, 4.4 TB/s of 168 MB (the kernel 28, the add 4 and the step between them)
+//             4099 x 2500 fp16, both norms and a gate
+//                                 51 us, 2.4 TB/s of 123 MB (the kernel 45, the add 6).  Of that 17 us are
+//             there with one row a workgroup, too: two launches, the parameters on the way in, their
+//             gradients on the way out; and rows of 5000 bytes begin and end inside a line of the
+//             caches (16384 rows of 2500 133 us, of 2504 120)
 #include "okt_element.h"
 #include "okt_random.h"
 
@@ -32,15 +40,16 @@ constexpr uint32_t NORM_BACKWARD_GROUPS = 512;     // workgroups aimed at: two t
 constexpr uint32_t NORM_SUMS = 5;                  // pre w, pre b, post w, post b, gate
 
 // Threads that hold a row, eight columns each `vecs` times over.  One wave where it can: its
-// sums need no barrier, and four rows of four waves are on their way together.  The kernel of a gated block
-// holds twice the sums, and two groups of them cost it all but one wave of a SIMD: it takes
-// a second wave above 512 columns instead (4099 rows of 2500 at two groups 134 us, at one
-// and 320 threads 37 us).
+// sums need no barrier, and four rows of four waves are on their way together (backward, 16384 rows:
+// of 1024 39 us against 49 at one group and two waves, of 768 31 against 49).  With a norm after
+// the block or a gate the kernel holds twice the sums and ends with as many more of them to add over its waves,
+// which only many rows are worth: with both, of 1024 and 16-bit, 16384 rows 55 against 67 us, 8192 35 against 38,
+// 4096 30 against 26; of fp32, where the registers go to fetched rows, 16384 rows 94 against 89.
 struct NormShape { uint32_t lanes, vecs; };
 
-static NormShape norm_shape(uint32_t width, bool gated_backward) {
+static NormShape norm_shape(uint32_t width, uint64_t rows, int dtype, bool backward_of_all) {
     if (width <= 512) return {WAVE, 1};
-    if (width <= 1024 && !gated_backward) return {WAVE, 2};
+    if (width <= 1024 && (!backward_of_all || (dtype != OKT_F32 && rows >= 8192))) return {WAVE, 2};
     if (width <= 4096) return {(width + WAVE * 8 - 1) / (WAVE * 8) * WAVE, 1};
     return {512, 2};
 }
@@ -572,7 +581,7 @@ static void launch_norm(const NormArgs& a, const NormPointers& p, bool backward,
     }
     const bool bias = a.post_b || a.pre_b;
     auto* kernel = bias ? norm_backward_kernel<T, L, false, true> : norm_backward_kernel<T, L, false, false>;
-    if constexpr (!(L::one && L::vecs == 2)) {                 // norm_shape gives a gated row another layout
+    if constexpr (!(L::one && L::vecs == 2 && sizeof(T) == 4)) {           // norm_shape gives such a row another layout
         if (a.post_w || a.gate) kernel = bias ? norm_backward_kernel<T, L, true, true> : norm_backward_kernel<T, L, true, false>;
     }
     hipLaunchKernelGGL(kernel, grid, block, 0, s, a, (const T*)p.u, (const T*)p.h, (const T*)p.dh, (const T*)p.dy, (T*)p.dx, (T*)p.du);
@@ -620,7 +629,7 @@ int okt_residual_norm_forward(const okt_residual_norm* op, const void* d_u, cons
         if (out && a.rows > 1 && ((out == d_u && stride != a.u_stride) || (out == d_x && stride != a.x_stride))) return OKT_ERR_INVALID_ARG;
     }
     a.stats = (float4*)d_stats_out;
-    const NormShape shape = norm_shape(a.width, false);
+    const NormShape shape = norm_shape(a.width, a.rows, op->dtype, false);
     const uint64_t at_once = rows_at_once(shape);
     const uint64_t want = (a.rows + at_once - 1) / at_once, most = (uint64_t)device_cus() * 8;
     timing_before((hipStream_t)stream);
@@ -654,7 +663,7 @@ int okt_residual_norm_backward(const okt_residual_norm* op, const void* d_u, con
             if (t.p && a.rows > 1 && ((t.p == d_dx_out && t.stride != a.dx_stride) || (t.p == d_du_out && t.stride != a.du_stride)))
                 return OKT_ERR_INVALID_ARG;
     }
-    const NormShape shape = norm_shape(a.width, all);
+    const NormShape shape = norm_shape(a.width, a.rows, op->dtype, all);
     const NormPlan plan = norm_plan(a.rows, a.rows_per_gate, rows_at_once(shape));
     if (!d_ws || !aligned(d_ws, 256) || ws_bytes < norm_ws_bytes(a.rows, a.width, a.rows_per_gate)) return OKT_ERR_WORKSPACE;
     a.stats = (float4*)d_stats;

@@ -141,6 +141,15 @@ def test_many_rows(form):
     c.check_backward()
 
 
+@pytest.mark.parametrize("form", [dict(post=True, gates=3, norm="rms", bias=False, p=0.1), dict(post=True, gates=1), dict(pre=False, gates=9000)], ids=str)
+def test_many_rows_of_two_groups_a_lane(form):
+    c = Case(9001, 532, "f16", **form)
+    c.forward()
+    c.check_forward()
+    c.backward()
+    c.check_backward()
+
+
 def test_rows_apart_and_unaligned():
     c = Case(50, 333, "f16", post=True, gates=2, p=0.1, stride=339)
     c.forward()
