@@ -659,14 +659,18 @@ size_t okt_attention_workspace_bytes(uint32_t batch, uint32_t heads, uint32_t kv
                                      uint32_t k_len, uint32_t head_dim);
 
 /*
+ *   d_o_out    out  written as a whole (past the lengths with zeros), overlaps no input
  *   d_lse_out  out  fp32[batch][heads][q_len], contiguous; NULL if no backward pass follows
+ * One launch; a second where few queries stand against many keys, which are then dealt to several
+ * workgroups whose sums it joins (only then is the workspace used).
  */
 int okt_attention_forward(const okt_attention* op, const void* d_q, const void* d_k, const void* d_v,
                           void* d_o_out, float* d_lse_out, void* d_ws, size_t ws_bytes, void* stream);
 
 /*
  * d_o and d_lse as the forward pass wrote them.  d_dq_out, d_dk_out and d_dv_out are written as
- * a whole (past the lengths with zeros); they may lie in one buffer, but overlap no input.
+ * a whole (past the lengths with zeros); they may lie in one buffer, but overlap no input.  Two
+ * launches, a third where the work is dealt out as in the forward pass.
  */
 int okt_attention_backward(const okt_attention* op, const void* d_q, const void* d_k, const void* d_v,
                            const void* d_o, const float* d_lse, const void* d_do, void* d_dq_out,

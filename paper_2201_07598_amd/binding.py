@@ -715,7 +715,7 @@ def okt_attention_forward(q, k, v, o_out, lse_out, ws=None, *, causal: bool = Fa
                           q_lens=None, k_lens=None, dropout_p: float = 0.0, seed=None, site: int = 0,
                           stream=None) -> None:
     """o = dropout(softmax(scale q k' over the visible keys)) v on [batch, length, heads, head_dim]
-    tensors of any strides; scale defaults to head_dim ** -0.5.  q_lens, k_lens: int32 [batch] on the
+    tensors, the last axis contiguous, other strides multiples of 8; scale defaults to head_dim ** -0.5.  q_lens, k_lens: int32 [batch] on the
     device, the sequences' own lengths.  lse_out (float32 [batch, heads, q_len]) may be None where
     no backward pass follows."""
     dtype, shape, keys, pq, pk, pv, strides = _attention_inputs(q, k, v)

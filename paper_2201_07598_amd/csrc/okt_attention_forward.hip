@@ -5,6 +5,14 @@
 // are taken transposed (keys down, queries across): a lane then holds one query's
 // scores, so maximum and sum stay in the lane but for one exchange with the lane 32 away,
 // and the probabilities are the second product's operand as they lie.
+//
+// With 64 columns or fewer the kernel is bound by the vector units, not the matrix units: a score
+// takes a maximum, a multiply-add, an exponential (at half the others' rate), an addition and half a
+// conversion, 22 cycles of a SIMD for 64 of them against 16 of its two products, and dropout as much again.  From call to call:
+//   32 x 16 heads x 512 x 64, lengths up to 512, bf16, p = 0.1  49-56 us (p = 0: 42)
+//   2 x 16 heads (4 key heads) x 4096 x 128, causal, bf16       140-147 us, 960 TFLOP/s of visible pairs
+//   12 heads x 128 x 64                                         9 us: latency of a launch and two tiles
+//   one query of 12 heads over 32768 keys of 128                53 us, 3.8 TB/s
 #include "okt_attention.h"
 
 namespace okt {

@@ -40,11 +40,12 @@ OKT_LAYOUT_FN uint32_t remainder(uint32_t n, Divider d) { return n - quotient(n,
 //          L2 its workgroups share, and neighbouring units to different dies, so that long and
 //          short sequences spread over all of them.
 //   end    Under a causal mask the last `window` heads of a die are taken block by block, not
-//          head by head, so that what starts last is short (2 x 16 heads x 4096 x 128: 65 % of
-//          the CUs' time was in use without, and the ends of the last heads took the rest).
+//          head by head, so that what starts last is short (2 x 16 heads x 4096 x 128: forward 157 us,
+//          head by head to the end 171; backward 531 and 545, of 64 columns 323 and 344).
 //   parts  A die deals its workgroups in turn over its own four parts.  Before the end, the
 //          blocks of every four (or last two) are turned by another number for every head, so
-//          that no part gets the first, or the empty last, block of each.
+//          that no part gets the first, or the empty last, block of each (32 x 16 heads x 512 x 64,
+//          lengths up to 512: forward 50 us, not turned 54; backward 149 and 165).
 constexpr uint32_t DIES = 8;
 
 struct Places {

@@ -392,8 +392,9 @@ __global__ __launch_bounds__(L::threads) void norm_backward_kernel(
     constexpr int AT_ONCE = L::one ? L::threads / WAVE : 1;
     __shared__ float2 slots[L::slots];
     clear_slots<L>(slots);
-    // rows of two groups a thread: as many sums as LDS holds lie there, and where registers are
-    // short all the same no row is fetched ahead
+    // rows of two groups a thread: as many sums as LDS holds lie there (2048 rows of 8192 with both norms
+    // and their biases, fp16: 83 us, all in registers 414), and in fp32, where registers are short all the same, no
+    // row is fetched ahead (132 us, ahead 195; fp16 83, not ahead 90)
     constexpr int SPAN = L::threads * L::vecs * 8, LDS_SUMS = ALL && !L::one && L::vecs == 2 ? 32768 / SPAN : 0;
     constexpr bool AHEAD = L::one || L::vecs == 1 || sizeof(T) == 2;
     __shared__ __attribute__((aligned(32))) float shared[L::one ? SPAN : LDS_SUMS ? LDS_SUMS * SPAN : 8];
