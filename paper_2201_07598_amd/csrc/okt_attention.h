@@ -302,11 +302,13 @@ __device__ __forceinline__ void store_partial(float* row, const f32x16 (&c)[TILE
 struct AttentionPlan {
     uint32_t dim;                                   // 64 or 128
     uint32_t forward_parts, query_parts, key_parts;
+    bool packed;                                    // forward: see its kernel
     size_t rows_at;                                 // backward: two numbers of every row
     size_t dq_at, dkv_at;                           // backward: partial sums
-    size_t forward_bytes, bytes;
+    size_t forward_bytes, bytes;                    // of the workspace, forward and backward
 };
-AttentionPlan attention_plan(uint32_t batch, uint32_t heads, uint32_t kv_heads, uint32_t q_len, uint32_t k_len, uint32_t head_dim);
+AttentionPlan attention_plan(uint32_t batch, uint32_t heads, uint32_t kv_heads, uint32_t q_len, uint32_t k_len, uint32_t head_dim,
+                             bool drop);
 
 constexpr uint32_t ATTENTION_QUERIES = 128;         // a workgroup of the forward and the queries' kernels
 constexpr uint32_t ATTENTION_KEYS = 64;             // keys that pass by it together

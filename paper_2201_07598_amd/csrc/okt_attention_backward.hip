@@ -405,7 +405,7 @@ extern "C" int okt_attention_backward(const okt_attention* op, const void* d_q, 
     for (const void* p : {d_q, d_k, d_v, d_o, d_do, (const void*)d_dq_out, (const void*)d_dk_out, (const void*)d_dv_out})
         if (!aligned(p, 16)) return OKT_ERR_INVALID_ARG;
     if (!aligned(d_lse, 4)) return OKT_ERR_INVALID_ARG;
-    const AttentionPlan plan = attention_plan(a.batch, a.heads, a.kv_heads, a.q_len, a.k_len, a.head_dim);
+    const AttentionPlan plan = attention_plan(a.batch, a.heads, a.kv_heads, a.q_len, a.k_len, a.head_dim, a.drop.bar != 65536u);
     if (!d_ws || !aligned(d_ws, 256) || ws_bytes < plan.bytes) return OKT_ERR_WORKSPACE;
     const BackwardPointers p = {d_q, d_k, d_v, d_o, d_do, d_lse, d_dq_out, d_dk_out, d_dv_out, (char*)d_ws};
     const hipStream_t s = (hipStream_t)stream;

@@ -13,6 +13,7 @@
 //   2 x 16 heads (4 key heads) x 4096 x 128, causal, bf16       140-147 us, 960 TFLOP/s of visible pairs
 //   12 heads x 128 x 64                                         9 us: latency of a launch and two tiles
 //   one query of 12 heads over 32768 keys of 128                53 us, 3.8 TB/s
+//   64 x 8 groups of 4 heads of one query, 4096 keys of 128     195 us, 5.5 TB/s
 #include "okt_attention.h"
 
 namespace okt {
@@ -21,26 +22,36 @@ constexpr int FWD_THREADS = 256;
 constexpr int FWD_QUERIES = ATTENTION_QUERIES, FWD_KEYS = ATTENTION_KEYS;
 static_assert(FWD_QUERIES == FWD_THREADS / WAVE * 32, "a wave owns 32 queries");
 
-template <typename T, int DIM, bool DROP>
+// PACKED: few queries, whose rows of all heads of a group are taken one after the other as the
+// rows of one block, so that the group's keys come by once and not once a head.
+template <typename T, int DIM, bool DROP, bool PACKED>
 __global__ __launch_bounds__(FWD_THREADS, 2) void attention_forward_kernel(AttentionArgs a, const T* q, const T* k, const T* v,
                                                                            T* o, float* lse, Places all, uint32_t parts,
-                                                                           Divider by_part, float* partial, float2* sums) {
+                                                                           Divider by_part, Divider by_query,
+                                                                           float* partial, float2* sums) {
+    static_assert(!(DROP && PACKED), "neighbouring rows of a block share its random numbers");
     using Tile = RowTile<T, DIM, FWD_KEYS, FWD_THREADS>;
     __shared__ __attribute__((aligned(1024))) char shared[4 * Tile::BYTES];
     const Place at = place_of(blockIdx.x, all);
     const uint32_t block = quotient(at.block, by_part), part = at.block - block * parts, blocks = quotient(all.blocks, by_part);
-    const uint32_t b = quotient(at.unit, a.by_kv), kv = at.unit - b * a.kv_heads, h = kv * a.group + at.head, plane = b * a.heads + h;
+    const uint32_t b = quotient(at.unit, a.by_kv), kv = at.unit - b * a.kv_heads;
     const uint32_t wave = uniform(threadIdx.x / WAVE), lane = threadIdx.x % WAVE;
     const int ql = sequence_length(a.q_lens, b, a.q_len), kl = sequence_length(a.k_lens, b, a.k_len);
-    const int q0 = (blocks - 1 - block) * FWD_QUERIES, w0 = q0 + 32 * (int)wave, i = w0 + (int)row_of_lane();
+    // the block's first row, the wave's, the lane's; which head and query that is
+    const int q0 = (blocks - 1 - block) * FWD_QUERIES, w0 = q0 + 32 * (int)wave, row = w0 + (int)row_of_lane();
+    const int rows = PACKED ? (int)(a.group * a.q_len) : (int)a.q_len;
+    const uint32_t in_group = PACKED ? quotient(row < rows ? row : rows - 1, by_query) : at.head;
+    const int i = PACKED ? row - (int)(in_group * a.q_len) : row;           // past the last row past the last query, too
+    const uint32_t h = kv * a.group + in_group, plane = b * a.heads + h;
 
     // keys that a query sees; the most of the workgroup's queries, the least and most of the wave's
     const int past = kl - ql + 1;
     const auto seen = [&](int query) { const int n = query + past; return query >= ql ? 0 : !a.causal || n > kl ? kl : n < 0 ? 0 : n; };
-    const int keys = q0 < ql ? seen(q0 + FWD_QUERIES < ql ? q0 + FWD_QUERIES - 1 : ql - 1) : 0;
+    const int last = ql - 1, there = PACKED ? (ql ? rows : 0) : ql;         // rows that have a query
+    const int keys = q0 >= there ? 0 : seen(PACKED || q0 + FWD_QUERIES >= ql ? last : q0 + FWD_QUERIES - 1);
     // a lane past the last query goes along as that one, so that no tile is masked for its sake
-    const int mine = q0 < ql ? seen(i < ql ? i : ql - 1) : 0, wave_least = w0 < ql ? seen(w0) : 0;
-    const int wave_most = w0 < ql ? seen(w0 + 32 < ql ? w0 + 31 : ql - 1) : 0;
+    const int mine = q0 < there ? seen(i < ql ? i : last) : 0;
+    const int wave_least = w0 < there ? seen(PACKED ? 0 : w0) : 0, wave_most = w0 < there ? seen(PACKED || w0 + 32 >= ql ? last : w0 + 31) : 0;
 
     // the tiles of this part
     const Part mine_of = part_of((keys + FWD_KEYS - 1) / FWD_KEYS, part, parts);
@@ -59,7 +70,7 @@ __global__ __launch_bounds__(FWD_THREADS, 2) void attention_forward_kernel(Atten
         typename Tile::Stream k_tiles(kb, k_row, begin, kl, a.head_dim), v_tiles(vb, v_row, begin, kl, a.head_dim);
         k_tiles.fetch(lds, k_at);
         v_tiles.fetch(lds + Tile::BYTES, v_at);
-        const T* qrow = q + b * a.q.batch + (uint64_t)(i < ql ? i : ql - 1) * a.q.row + h * a.q.head;
+        const T* qrow = q + b * a.q.batch + (uint64_t)(i < ql ? i : last) * a.q.row + h * a.q.head;
         frag<T> qf[DIM / 16];
         row_operands<DIM>(qf, qrow, a.head_dim);
         const TileReads reads = Tile::reads();
@@ -130,19 +141,16 @@ __global__ __launch_bounds__(FWD_THREADS, 2) void attention_forward_kernel(Atten
         }
     }
     total = sum_halves(total);
+    if (row >= rows) return;
     if (parts > 1) {
-        if (i < (int)a.q_len) {
-            const uint64_t row = ((uint64_t)part * a.batch * a.heads + plane) * a.q_len + i;
-            store_partial(partial + row * DIM, acc, 1.0f);
-            if (lane < 32) sums[row] = make_float2(i < ql ? top : -INFINITY, total);
-        }
+        const uint64_t to = ((uint64_t)part * a.batch * a.heads + plane) * a.q_len + i;
+        store_partial(partial + to * DIM, acc, 1.0f);
+        if (lane < 32) sums[to] = make_float2(i < ql ? top : -INFINITY, total);
         return;
     }
-    if (i < (int)a.q_len) {
-        store_row(o + b * a.o.batch + (uint64_t)i * a.o.row + h * a.o.head, acc, mine > 0 && i < ql ? a.drop.scale / total : 0.0f, a.head_dim);
-        if (lse && lane < 32)
-            lse[(uint64_t)plane * a.q_len + i] = mine > 0 && i < ql ? (top + __builtin_amdgcn_logf(total)) * 0.693147180559945f : -INFINITY;
-    }
+    store_row(o + b * a.o.batch + (uint64_t)i * a.o.row + h * a.o.head, acc, mine > 0 && i < ql ? a.drop.scale / total : 0.0f, a.head_dim);
+    if (lse && lane < 32)
+        lse[(uint64_t)plane * a.q_len + i] = mine > 0 && i < ql ? (top + __builtin_amdgcn_logf(total)) * 0.693147180559945f : -INFINITY;
 }
 
 // Joins the parts of a row: o = sum 2^(top - most) acc / sum 2^(top - most) total.  DIM / 4 lanes a
@@ -193,22 +201,27 @@ __global__ __launch_bounds__(FWD_THREADS) void attention_join_kernel(AttentionAr
 template <typename T, int DIM>
 static void launch_forward(const AttentionArgs& a, const AttentionPlan& plan, const void* q, const void* k, const void* v, void* o,
                            float* lse, void* ws, hipStream_t s) {
-    const uint32_t blocks = (a.q_len + FWD_QUERIES - 1) / FWD_QUERIES, parts = plan.forward_parts;
     const uint64_t rows = (uint64_t)a.batch * a.heads * a.q_len;
+    const uint32_t block_rows = plan.packed ? a.group * a.q_len : a.q_len, block_heads = plan.packed ? 1 : a.group;
+    const uint32_t blocks = (block_rows + FWD_QUERIES - 1) / FWD_QUERIES, parts = plan.forward_parts;
     float* partial = (float*)ws;
     float2* sums = (float2*)(partial + parts * rows * DIM);
-    auto* kernel = a.drop.bar == 65536u ? attention_forward_kernel<T, DIM, false> : attention_forward_kernel<T, DIM, true>;
+    auto* kernel = a.drop.bar != 65536u ? attention_forward_kernel<T, DIM, true, false>
+                   : plan.packed        ? attention_forward_kernel<T, DIM, false, true>
+                                        : attention_forward_kernel<T, DIM, false, false>;
     timing_before(s);
-    hipLaunchKernelGGL(kernel, dim3(blocks * a.batch * a.heads * parts), dim3(FWD_THREADS), 0, s, a, (const T*)q, (const T*)k,
-                       (const T*)v, (T*)o, lse, places(a.batch * a.kv_heads, a.group, blocks * parts, window_of(a.causal, a.k_len, DIM, a.group)),
-                       parts, divider(parts), partial, sums);
+    hipLaunchKernelGGL(kernel, dim3(blocks * a.batch * a.kv_heads * block_heads * parts), dim3(FWD_THREADS), 0, s, a, (const T*)q,
+                       (const T*)k, (const T*)v, (T*)o, lse,
+                       places(a.batch * a.kv_heads, block_heads, blocks * parts, window_of(a.causal && !plan.packed, a.k_len, DIM, a.group)),
+                       parts, divider(parts), divider(a.q_len), partial, sums);
     timing_after(s);
     if (parts > 1)
         hipLaunchKernelGGL((attention_join_kernel<T, DIM>), dim3((unsigned)((rows * (DIM / 4) + FWD_THREADS - 1) / FWD_THREADS)),
                            dim3(FWD_THREADS), 0, s, a, (T*)o, lse, parts, (const float*)partial, (const float2*)sums);
 }
 
-AttentionPlan attention_plan(uint32_t batch, uint32_t heads, uint32_t kv_heads, uint32_t q_len, uint32_t k_len, uint32_t head_dim) {
+AttentionPlan attention_plan(uint32_t batch, uint32_t heads, uint32_t kv_heads, uint32_t q_len, uint32_t k_len, uint32_t head_dim,
+                             bool drop) {
     AttentionPlan p;
     p.dim = head_dim <= 64 ? 64 : 128;
     const uint32_t key_block = p.dim == 64 ? KeysShape<64>::GROUPS * 32 : KeysShape<128>::GROUPS * 32;
@@ -223,7 +236,12 @@ AttentionPlan attention_plan(uint32_t batch, uint32_t heads, uint32_t kv_heads, 
         return parts_worth(parts_for(workgroups, steps, 1), steps, step_ns * p.dim, 2 * bytes, added ? 0 : PART_LAUNCH_NS);
     };
     const auto key_parts = [&](bool added) { return worth((k_len + key_block - 1) / key_block * units, query_steps, 21, 2 * keys * row_bytes, added); };
-    p.forward_parts = worth(query_blocks, key_steps, 12, rows * (row_bytes + 8), false);
+    // Without dropout, whose random numbers neighbouring queries share, the queries of a group's heads are
+    // packed where at least two heads' fit a block: 64 x 8 groups of 4 heads of one query over 4096 keys of
+    // 128 195 us, each head on its own 415; of 33 queries (8 x 8 groups) 55 and 70.
+    p.packed = !drop && group > 1 && 2 * q_len <= ATTENTION_QUERIES;
+    const uint64_t forward_blocks = p.packed ? (group * q_len + ATTENTION_QUERIES - 1) / ATTENTION_QUERIES * units : query_blocks;
+    p.forward_parts = worth(forward_blocks, key_steps, 12, rows * (row_bytes + 8), false);
     p.key_parts = key_parts(false);
     p.query_parts = worth(query_blocks, key_steps, 17, rows * row_bytes, p.key_parts > 1);
     if (p.query_parts > 1) p.key_parts = key_parts(true);
@@ -233,7 +251,6 @@ AttentionPlan attention_plan(uint32_t batch, uint32_t heads, uint32_t kv_heads, 
     p.dq_at = round(rows * 2 * sizeof(float));
     p.dkv_at = p.dq_at + (p.query_parts > 1 ? round(p.query_parts * rows * p.dim * sizeof(float)) : 0);
     p.bytes = p.dkv_at + (p.key_parts > 1 ? round(2 * p.key_parts * keys * p.dim * sizeof(float)) : 0);
-    if (p.bytes < p.forward_bytes) p.bytes = p.forward_bytes;
     return p;
 }
 
@@ -288,8 +305,12 @@ extern "C" {
 
 size_t okt_attention_workspace_bytes(uint32_t batch, uint32_t heads, uint32_t kv_heads, uint32_t q_len, uint32_t k_len,
                                      uint32_t head_dim) {
-    const size_t need = okt::attention_plan(batch, heads, kv_heads, q_len, k_len, head_dim).bytes;
-    return need ? need : 256;
+    size_t need = 256;
+    for (bool drop : {false, true}) {
+        const okt::AttentionPlan plan = okt::attention_plan(batch, heads, kv_heads, q_len, k_len, head_dim, drop);
+        for (size_t n : {plan.forward_bytes, plan.bytes}) need = n > need ? n : need;
+    }
+    return need;
 }
 
 int okt_attention_forward(const okt_attention* op, const void* d_q, const void* d_k, const void* d_v, void* d_o_out,
@@ -300,7 +321,7 @@ int okt_attention_forward(const okt_attention* op, const void* d_q, const void* 
     if (a.batch == 0 || a.q_len == 0) return OKT_OK;
     if (!d_q || !d_o_out || (a.k_len && (!d_k || !d_v))) return OKT_ERR_INVALID_ARG;
     if (!aligned(d_q, 16) || !aligned(d_k, 16) || !aligned(d_v, 16) || !aligned(d_o_out, 16) || !aligned(d_lse_out, 4)) return OKT_ERR_INVALID_ARG;
-    const AttentionPlan plan = attention_plan(a.batch, a.heads, a.kv_heads, a.q_len, a.k_len, a.head_dim);
+    const AttentionPlan plan = attention_plan(a.batch, a.heads, a.kv_heads, a.q_len, a.k_len, a.head_dim, a.drop.bar != 65536u);
     if (plan.forward_bytes && (!d_ws || !aligned(d_ws, 256) || ws_bytes < plan.forward_bytes)) return OKT_ERR_WORKSPACE;
     const hipStream_t s = (hipStream_t)stream;
     const bool narrow = plan.dim == 64;

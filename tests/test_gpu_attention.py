@@ -178,6 +178,17 @@ def test_work_split_over_the_long_axis(Sq, Sk, H, G, D, causal, p):
     check(*make(2, H, G, Sq, Sk, D), "bf16", causal=causal, p=p, lens=lens)
 
 
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("Sq,Sk,H,G,D", [(1, 1, 8, 2, 64), (1, 700, 8, 2, 128), (1, 3000, 6, 1, 64), (7, 500, 6, 2, 40),
+                                         (33, 100, 9, 3, 64), (64, 64, 10, 2, 128), (64, 200, 5, 1, 8), (64, 40, 4, 1, 64)])
+def test_few_queries_of_a_group_s_heads(Sq, Sk, H, G, D, causal):
+    """Heads that share a block of rows: blocks that end inside one, lengths of their own, sequences of none."""
+    lens = ([Sq, max(1, Sq // 2), 0, Sq, 1], [Sk, max(1, Sk // 3), Sk, 0, 1])
+    q, k, v, do = make(5, H, G, Sq, Sk, D)
+    check(q, k, v, do, "bf16", causal=causal, lens=lens)
+    check(q, k, v, do, "bf16", causal=causal)
+
+
 @pytest.mark.parametrize("p", [0.0, 0.1])
 def test_scores_of_every_size(p):
     """A softmax that is all but one key, and one that is nearly even; a maximum that grows along the keys."""
