@@ -51,7 +51,7 @@ __global__ __launch_bounds__(BWD_THREADS, 2) void attention_backward_queries_ker
     const int wave_most = w0 < ql ? seen(w0 + 32 < ql ? w0 + 31 : ql - 1) : 0;
     const float drop_scale = DROP ? a.drop.scale : 1.0f;
     // the tiles of this part; part 0 also leaves the rows' numbers
-    const Part mine_of = part_of((keys + BWD_KEYS - 1) / BWD_KEYS, part, parts);
+    const Part mine_of = part_of((keys + BWD_KEYS - 1) / BWD_KEYS, part, by_part);
     const int begin = mine_of.first * BWD_KEYS, end = mine_of.last * BWD_KEYS < keys ? mine_of.last * BWD_KEYS : keys;
 
     f32x16 acc[DIM / 32];
@@ -182,7 +182,7 @@ __global__ __launch_bounds__(BWD_THREADS, DIM == 64 ? 2 : 1) void attention_back
     const int tiles = k0 < kl && begin < ql ? (ql - begin + TILE - 1) / TILE : 0;
     const float drop_scale = DROP ? a.drop.scale : 1.0f;
     // the steps of this share: the tiles of every head of the group, head after head
-    const Part steps = part_of(tiles * (int)a.group, share, parts);
+    const Part steps = part_of(tiles * (int)a.group, share, by_part);
 
     f32x16 dkacc[DIM / 32], dvacc[DIM / 32];
 #pragma unroll

@@ -54,7 +54,7 @@ __global__ __launch_bounds__(FWD_THREADS, 2) void attention_forward_kernel(Atten
     const int wave_least = w0 < there ? seen(PACKED ? 0 : w0) : 0, wave_most = w0 < there ? seen(PACKED || w0 + 32 >= ql ? last : w0 + 31) : 0;
 
     // the tiles of this part
-    const Part mine_of = part_of((keys + FWD_KEYS - 1) / FWD_KEYS, part, parts);
+    const Part mine_of = part_of((keys + FWD_KEYS - 1) / FWD_KEYS, part, by_part);
     const int begin = mine_of.first * FWD_KEYS, end = mine_of.last * FWD_KEYS < keys ? mine_of.last * FWD_KEYS : keys;
 
     f32x16 acc[DIM / 32];

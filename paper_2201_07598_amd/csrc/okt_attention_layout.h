@@ -95,11 +95,13 @@ OKT_LAYOUT_FN uint32_t window_of(bool causal, uint32_t k_len, uint32_t dim, uint
     return n < 8 ? 8 : n > 64 ? 64 : (uint32_t)n;
 }
 
-// Steps [first, last) of `steps` that part `part` takes; part 0 takes step 0 if there is one.
+// Steps [first, last) of `steps`, below 2^30, that part `part` of `parts.by` takes, which are equal but
+// for one; part 0 takes step 0 if there is one.
 struct Part { int first, last; };
-OKT_LAYOUT_FN Part part_of(int steps, uint32_t part, uint32_t parts) {
-    const auto cut = [&](uint32_t p) { return (int)(((uint64_t)steps * p + parts - 1) / parts); };
-    return parts == 1 ? Part{0, steps} : Part{cut(part), cut(part + 1)};
+OKT_LAYOUT_FN Part part_of(int steps, uint32_t part, Divider parts) {
+    const uint32_t whole = quotient((uint32_t)steps, parts), rest = (uint32_t)steps - whole * parts.by;
+    const auto cut = [&](uint32_t p) { return (int)(p * whole + quotient(p * rest + parts.by - 1, parts)); };
+    return {cut(part), cut(part + 1)};
 }
 
 // The most parts: enough to give every CU two workgroups, none of fewer than `least` steps.

@@ -24,11 +24,13 @@ int main() {
                     if (seen.size() != total) ++bad;
                     ++cases;
                 }
-    for (int steps = 0; steps < 200; ++steps)
+    const int many[] = {1000, 65537, 12345678, (1 << 30) - 1};
+    for (int n = 0; n < 204; ++n) {
+        const int steps = n < 200 ? n : many[n - 200];
         for (uint32_t parts = 1; parts <= okt::PART_MAX; ++parts) {
             int at = 0;
             for (uint32_t p = 0; p < parts; ++p) {
-                const okt::Part part = okt::part_of(steps, p, parts);
+                const okt::Part part = okt::part_of(steps, p, okt::divider(parts));
                 if (part.first != at || part.last < part.first) ++bad;
                 if (p == 0 && steps && part.last == 0) ++bad;
                 at = part.last;
@@ -36,6 +38,7 @@ int main() {
             if (at != steps) ++bad;
             ++cases;
         }
+    }
     for (uint64_t groups = 0; groups < 2000; groups += 7)
         for (uint64_t steps = 0; steps < 300; steps += 11)
             for (uint32_t least : {1u, 2u, 4u}) {
