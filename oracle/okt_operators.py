@@ -76,6 +76,11 @@ def norm_factor(rows: int, width: int, p: float, seed: int, site: int = 0):
     return kept_rows(rows, width, p, seed, site) * scale_of(p) if p > 0 else 1.0
 
 
+def dropped(v, factor):
+    """v times its factor, 0 where that is 0 whatever v holds."""
+    return np.where(np.equal(factor, 0), 0.0, factor * v)
+
+
 def residual_norm(u, x, *, kind="layer", eps=1e-5, residual_scale=1.0, post_weight=None, post_bias=None,
                   gate=None, rows_per_gate=0, pre_weight=None, pre_bias=None, factor=1.0, store=lambda h: h):
     """(h, y or None, stats [rows, 4]); `factor` is what dropout multiplies by, `store` rounds h as
@@ -87,7 +92,7 @@ def residual_norm(u, x, *, kind="layer", eps=1e-5, residual_scale=1.0, post_weig
         m, r = statistics(u, kind, eps)
         stats[:, 0:1], stats[:, 1:2] = m, r
         a = _norm(u, (m, r), post_weight, post_bias)
-    a = factor * a
+    a = dropped(a, factor)
     if gate is not None:
         a = a * gate[np.arange(rows) // (rows_per_gate or max(rows, 1))]
     h = residual_scale * x + a
@@ -119,12 +124,12 @@ def residual_norm_backward(u, h, stats, dh, dy, *, kind="layer", residual_scale=
         d, out["dpre_weight"], out["dpre_bias"] = _norm_backward(dy, h, stats[:, 2:3], stats[:, 3:4], pre_weight, kind)
         total = total + d
     out["dx"] = residual_scale * total
-    da = factor * total
+    da = dropped(total, factor)
     if gate is not None:
         group = np.arange(rows) // (rows_per_gate or max(rows, 1))
         a = u if post_weight is None else _norm(u, (stats[:, 0:1], stats[:, 1:2]), post_weight, post_bias)
         out["dgate"] = np.zeros_like(gate)
-        np.add.at(out["dgate"], group, da * a)
+        np.add.at(out["dgate"], group, total * dropped(a, factor))
         da = da * gate[group]
     if post_weight is not None:
         da, out["dpost_weight"], out["dpost_bias"] = _norm_backward(da, u, stats[:, 0:1], stats[:, 1:2], post_weight, kind)

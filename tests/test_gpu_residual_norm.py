@@ -239,3 +239,20 @@ def test_a_graph_replays_with_new_inputs_and_seeds():
         okt.okt_residual_norm_backward(c.u, c.h, c.stats, c.dh, c.dy, c.dx, c.du, c.ws, **c.grads, **c.options)
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(got, (c.h, c.y, c.dx, c.du, *c.grads.values()))), n
+
+
+@pytest.mark.parametrize("rows,width,kind,gates", [(40, 100, "bf16", 1), (9000, 536, "f16", 3), (700, 1028, "f16", 700),
+                                                   (600, 2500, "f16", 2), (520, 4104, "f32", 1)])
+def test_what_is_dropped_does_not_reach_the_gradient_of_a_gate(rows, width, kind, gates):
+    """dg sums dh * dropout(a): a place that is dropped adds 0, whatever u holds there."""
+    c = Case(rows, width, kind, pre=False, gates=gates, p=0.3)
+    dropped = torch.from_numpy(~ops.kept_rows(rows, width, 0.3, SEED, 3)).to(DEV)
+    c.u = c.u.masked_fill(dropped, 0.0)
+    c.forward()
+    c.backward()
+    clean = [t.clone() for t in (c.h, c.dx, c.du, c.grads["dgate"])]
+    c.u = c.u.masked_fill(dropped, float("inf"))
+    c.u[:, ::3] = c.u[:, ::3].masked_fill(dropped[:, ::3], float("nan"))
+    c.forward()
+    c.backward()
+    assert all(torch.equal(a, b) for a, b in zip(clean, (c.h, c.dx, c.du, c.grads["dgate"])))

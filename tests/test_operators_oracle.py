@@ -102,3 +102,18 @@ def test_rows_that_see_nothing():
     assert np.all(dq[0, :3] == 0)                                   # the third sees one key: constant
     # every row's values add up to what its queries sent
     assert np.allclose(dv.sum(), 8 * 3)
+
+
+def test_what_is_dropped_does_not_matter():
+    rng = np.random.default_rng(9)
+    rows, width = 6, 24
+    u, x, dh = (rng.standard_normal((rows, width)) for _ in range(3))
+    gate = rng.standard_normal((2, width))
+    factor = ops.norm_factor(rows, width, 0.4, 99, 2)
+    fixed = dict(gate=gate, rows_per_gate=3, factor=factor)
+    clean = ops.residual_norm(u, x, **fixed)[0], ops.residual_norm_backward(u, None, np.zeros((rows, 4)), dh, None, **fixed)
+    u[factor == 0] = np.inf
+    with np.errstate(invalid="ignore"):
+        h, back = ops.residual_norm(u, x, **fixed)[0], ops.residual_norm_backward(u, None, np.zeros((rows, 4)), dh, None, **fixed)
+    assert np.array_equal(h, clean[0])
+    assert all(np.array_equal(back[n], clean[1][n]) for n in ("dx", "du", "dgate"))
