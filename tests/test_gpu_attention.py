@@ -257,3 +257,17 @@ def test_a_graph_replays_with_new_inputs_and_seeds():
         step_()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(got, (o, lse, *grads))), n
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_backward_on_another_stream(D):
+    q, k, v, do = make(2, 4, 2, 100, 700, D)
+    o, lse = forward(q, k, v, causal=True)
+    want = backward(q, k, v, o, lse, do, causal=True)
+    side = torch.cuda.Stream()
+    got = [torch.full(t.shape, 7.0, dtype=q.dtype, device=DEV) for t in (q, k, v)]
+    ws = workspace(q, k)
+    torch.cuda.synchronize()
+    okt.okt_attention_backward(q, k, v, o, lse, do, *got, ws, causal=True, stream=side)
+    side.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(want, got))

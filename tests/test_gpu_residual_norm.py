@@ -256,3 +256,36 @@ def test_what_is_dropped_does_not_reach_the_gradient_of_a_gate(rows, width, kind
     c.forward()
     c.backward()
     assert all(torch.equal(a, b) for a, b in zip(clean, (c.h, c.dx, c.du, c.grads["dgate"])))
+
+
+WIDE_FORMS = [dict(p=0.1), dict(post=True, gates=3, p=0.1), dict(post=True, gates=700), dict(post=True, norm="rms", bias=False, p=0.2),
+              dict(pre=False, gates=7), dict(post=True, pre=False, gates=1, p=0.1)]
+
+
+@pytest.mark.parametrize("form", WIDE_FORMS, ids=str)
+@pytest.mark.parametrize("rows,width,kind", [(1500, 1028, "bf16"), (1600, 760, "f32"), (1300, 2500, "f16"), (1100, 4104, "f16"),
+                                             (1100, 4104, "f32"), (1031, 8192, "bf16")])
+def test_many_rows_of_a_workgroup_each(rows, width, kind, form):
+    """Sums over rows that a workgroup takes one after the other, in registers and in LDS, and gates that
+    end inside its rows."""
+    c = Case(rows, width, kind, **form)
+    c.forward()
+    c.check_forward()
+    c.backward()
+    c.check_backward()
+
+
+@pytest.mark.parametrize("width", [200, 1000, 2500, 5000])
+def test_another_stream(width):
+    c = Case(300, width, "bf16", post=True, gates=2, p=0.1)
+    c.forward()
+    c.backward()
+    want = [t.clone() for t in (c.h, c.y, c.stats, c.dx, c.du, *c.grads.values())]
+    side = torch.cuda.Stream()
+    for t in (c.h, c.y, c.stats, c.dx, c.du, *c.grads.values()):
+        t.fill_(7.0)
+    torch.cuda.synchronize()
+    okt.okt_residual_norm_forward(c.u, c.x, c.h, c.y, c.stats, stream=side, **c.options)
+    okt.okt_residual_norm_backward(c.u, c.h, c.stats, c.dh, c.dy, c.dx, c.du, c.ws, stream=side, **c.grads, **c.options)
+    side.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(want, (c.h, c.y, c.stats, c.dx, c.du, *c.grads.values())))
