@@ -640,7 +640,8 @@ int okt_residual_norm_backward(const okt_residual_norm* op, const void* d_u, con
  */
 typedef struct okt_attention {
     uint32_t batch, heads, kv_heads;   /* heads a multiple of kv_heads; batch * heads <= 2^20 */
-    uint32_t q_len, k_len;             /* 0 to 2^24 */
+    uint32_t q_len, k_len;             /* 0 to 2^24; batch * heads * ceil(q_len / 128) < 2^24, and backward batch *
+                                          kv_heads * ceil(k_len / 128) (k_len / 64 above 64 columns), too */
     uint32_t head_dim;                 /* 8, 16, ... 128 */
     int32_t dtype;                     /* OKT_BF16 or OKT_F16 */
     int32_t causal;

@@ -302,6 +302,7 @@ __device__ __forceinline__ void store_partial(float* row, const f32x16 (&c)[TILE
 struct AttentionPlan {
     uint32_t dim;                                   // 64 or 128
     uint32_t forward_parts, query_parts, key_parts;
+    uint64_t forward_groups, query_groups, key_groups;      // workgroups of each kernel
     bool packed;                                    // forward: see its kernel
     size_t rows_at;                                 // backward: two numbers of every row
     size_t dq_at, dkv_at;                           // backward: partial sums
@@ -336,6 +337,9 @@ struct AttentionArgs {
 
 // Checks the arguments of a direction and fills the kernels'; false if refused.
 bool attention_args(const okt_attention* op, bool backward, AttentionArgs& a);
+
+// Workgroups of 256 threads that a launch can have: it counts work-items in 32 bits.
+constexpr uint64_t LAUNCH_GROUPS = (1ull << 24) - 1;
 
 // Lengths of a sequence, held to the tensors'.
 __device__ __forceinline__ int sequence_length(const int32_t* lens, uint32_t b, uint32_t most) {

@@ -356,7 +356,7 @@ static void launch_backward(const AttentionArgs& a, const AttentionPlan& plan, c
     uint32_t n = 0;
     if (a.q_len) {
         const uint32_t blocks = (a.q_len + BWD_QUERIES - 1) / BWD_QUERIES, parts = plan.query_parts;
-        hipLaunchKernelGGL((attention_backward_queries_kernel<T, DIM, DROP>), dim3(blocks * a.batch * a.heads * parts),
+        hipLaunchKernelGGL((attention_backward_queries_kernel<T, DIM, DROP>), dim3((unsigned)plan.query_groups),
                            dim3(BWD_THREADS), 0, s, a, (const T*)p.q, (const T*)p.k, (const T*)p.v, (const T*)p.o, p.lse,
                            (const T*)p.d_o, (T*)p.dq, rows,
                            places(a.batch * a.kv_heads, a.group, blocks * parts, window_of(a.causal, a.k_len, DIM, a.group)), parts,
@@ -368,7 +368,7 @@ static void launch_backward(const AttentionArgs& a, const AttentionPlan& plan, c
         const uint32_t blocks = (a.k_len + KEYS - 1) / KEYS, parts = plan.key_parts;
         const uint64_t keys = (uint64_t)a.batch * a.kv_heads * a.k_len;
         timing_before(s);
-        hipLaunchKernelGGL((attention_backward_keys_kernel<T, DIM, DROP>), dim3(blocks * a.batch * a.kv_heads * parts),
+        hipLaunchKernelGGL((attention_backward_keys_kernel<T, DIM, DROP>), dim3((unsigned)plan.key_groups),
                            dim3(BWD_THREADS), 0, s, a, (const T*)p.q, (const T*)p.k, (const T*)p.v, (const T*)p.d_o,
                            (const RowNumbers*)rows, (T*)p.dk, (T*)p.dv, 
                            places(a.batch * a.kv_heads, 1, blocks * parts, window_of(a.causal, a.q_len, DIM, 1)), parts, divider(parts),
@@ -409,6 +409,7 @@ extern "C" int okt_attention_backward(const okt_attention* op, const void* d_q, 
         if (!aligned(p, 16)) return OKT_ERR_INVALID_ARG;
     if (!aligned(d_lse, 4)) return OKT_ERR_INVALID_ARG;
     const AttentionPlan plan = attention_plan(a.batch, a.heads, a.kv_heads, a.q_len, a.k_len, a.head_dim, a.drop.bar != 65536u);
+    if (plan.query_groups > LAUNCH_GROUPS || plan.key_groups > LAUNCH_GROUPS) return OKT_ERR_INVALID_ARG;
     if (!d_ws || !aligned(d_ws, 256) || ws_bytes < plan.bytes) return OKT_ERR_WORKSPACE;
     const BackwardPointers p = {d_q, d_k, d_v, d_o, d_do, d_lse, d_dq_out, d_dk_out, d_dv_out, (char*)d_ws};
     const hipStream_t s = (hipStream_t)stream;

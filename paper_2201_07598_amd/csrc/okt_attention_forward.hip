@@ -210,7 +210,7 @@ static void launch_forward(const AttentionArgs& a, const AttentionPlan& plan, co
                    : plan.packed        ? attention_forward_kernel<T, DIM, false, true>
                                         : attention_forward_kernel<T, DIM, false, false>;
     timing_before(s);
-    hipLaunchKernelGGL(kernel, dim3(blocks * a.batch * a.kv_heads * block_heads * parts), dim3(FWD_THREADS), 0, s, a, (const T*)q,
+    hipLaunchKernelGGL(kernel, dim3((unsigned)plan.forward_groups), dim3(FWD_THREADS), 0, s, a, (const T*)q,
                        (const T*)k, (const T*)v, (T*)o, lse,
                        places(a.batch * a.kv_heads, block_heads, blocks * parts, window_of(a.causal && !plan.packed, a.k_len, DIM, a.group)),
                        parts, divider(parts), divider(a.q_len), partial, sums);
@@ -245,6 +245,9 @@ AttentionPlan attention_plan(uint32_t batch, uint32_t heads, uint32_t kv_heads, 
     p.key_parts = key_parts(false);
     p.query_parts = worth(query_blocks, key_steps, 17, rows * row_bytes, p.key_parts > 1);
     if (p.query_parts > 1) p.key_parts = key_parts(true);
+    p.forward_groups = forward_blocks * p.forward_parts;
+    p.query_groups = query_blocks * p.query_parts;
+    p.key_groups = (k_len + key_block - 1) / key_block * units * p.key_parts;
     const auto round = [](uint64_t n) { return (size_t)((n + 255) & ~255ull); };
     p.forward_bytes = p.forward_parts > 1 ? round(p.forward_parts * rows * (p.dim + 2) * sizeof(float)) : 0;
     p.rows_at = 0;
@@ -267,8 +270,6 @@ bool attention_args(const okt_attention* op, bool backward, AttentionArgs& a) {
     if (!op || (op->dtype != OKT_BF16 && op->dtype != OKT_F16)) return false;
     if (op->kv_heads == 0 || op->heads == 0 || op->heads % op->kv_heads) return false;
     if ((uint64_t)op->batch * op->heads > (1u << 20) || op->q_len > (1u << 24) || op->k_len > (1u << 24)) return false;
-    // workgroups of a launch: a block of 64 rows or more of one head each
-    if (((uint64_t)(op->q_len > op->k_len ? op->q_len : op->k_len) / 64 + 1) * op->batch * op->heads > (1u << 30)) return false;
     if (op->head_dim == 0 || op->head_dim > 128 || op->head_dim % 8) return false;
     if (!(op->scale > 0.0f) || op->scale > 3.0e38f) return false;
     if (!dropout_rule(op->dropout_p, a.drop)) return false;
@@ -322,6 +323,7 @@ int okt_attention_forward(const okt_attention* op, const void* d_q, const void* 
     if (!d_q || !d_o_out || (a.k_len && (!d_k || !d_v))) return OKT_ERR_INVALID_ARG;
     if (!aligned(d_q, 16) || !aligned(d_k, 16) || !aligned(d_v, 16) || !aligned(d_o_out, 16) || !aligned(d_lse_out, 4)) return OKT_ERR_INVALID_ARG;
     const AttentionPlan plan = attention_plan(a.batch, a.heads, a.kv_heads, a.q_len, a.k_len, a.head_dim, a.drop.bar != 65536u);
+    if (plan.forward_groups > LAUNCH_GROUPS) return OKT_ERR_INVALID_ARG;
     if (plan.forward_bytes && (!d_ws || !aligned(d_ws, 256) || ws_bytes < plan.forward_bytes)) return OKT_ERR_WORKSPACE;
     const hipStream_t s = (hipStream_t)stream;
     const bool narrow = plan.dim == 64;

@@ -1,0 +1,93 @@
+// Host check of what the layer's operators launch, without a GPU: this program stands in for the runtime's
+// launch, which counts, looks at the sizes and does nothing.  Pointers are made up and never read.
+//   sizes     every launch of a call that is accepted counts its work-items in 32 bits, and the sizes at the
+//             edge of what the header allows are accepted, those past it refused
+// Prints the number of cases and of violations.
+#include <cstdio>
+#include <cstring>
+#include <initializer_list>
+
+#include "okt.h"
+
+struct Dim { uint32_t x, y, z; };
+static int g_launches = 0;
+static bool g_too_many = false;
+
+extern "C" {
+static struct { Dim grid, block; size_t shared; void* stream; } g_next;
+unsigned __hipPushCallConfiguration(Dim grid, Dim block, size_t shared, void* stream) {
+    g_next = {grid, block, shared, stream};
+    return 0;
+}
+int __hipPopCallConfiguration(Dim* grid, Dim* block, size_t* shared, void** stream) {
+    *grid = g_next.grid;
+    *block = g_next.block;
+    *shared = g_next.shared;
+    *stream = g_next.stream;
+    return 0;
+}
+int hipLaunchKernel(const void*, Dim grid, Dim block, void**, size_t, void*) {
+    ++g_launches;
+    if ((uint64_t)grid.x * block.x >> 32 || (uint64_t)grid.y * block.y >> 16 || grid.z != 1) g_too_many = true;
+    return 0;
+}
+int hipGetLastError(void) { return 0; }
+}
+
+static long cases = 0, bad = 0;
+static void* const FAKE = (void*)0x10000;
+static void* at(uint64_t n) { return (void*)(0x10000 + (n << 48)); }        // apart, whatever the sizes
+
+static void judge(int status, bool accepted, const char* what, uint64_t a, uint64_t b, uint64_t c, uint64_t d) {
+    ++cases;
+    const bool fine = (status == OKT_OK) == accepted && !g_too_many && (status == OKT_OK || g_launches == 0) &&
+                      (accepted ? g_launches > 0 : status == OKT_ERR_INVALID_ARG);
+    if (!fine) {
+        ++bad;
+        std::printf("%s %llu %llu %llu %llu: status %d, %d launches%s\n", what, (unsigned long long)a, (unsigned long long)b,
+                    (unsigned long long)c, (unsigned long long)d, status, g_launches, g_too_many ? ", too many work-items" : "");
+    }
+    g_launches = 0;
+    g_too_many = false;
+}
+
+static uint64_t up(uint64_t n, uint64_t by) { return (n + by - 1) / by; }
+
+static void attention(uint64_t batch, uint64_t heads, uint64_t kv_heads, uint64_t q_len, uint64_t k_len, uint32_t dim) {
+    okt_attention op;
+    std::memset(&op, 0, sizeof op);
+    op.batch = (uint32_t)batch;
+    op.heads = (uint32_t)heads;
+    op.kv_heads = (uint32_t)kv_heads;
+    op.q_len = (uint32_t)q_len;
+    op.k_len = (uint32_t)k_len;
+    op.head_dim = dim;
+    op.dtype = OKT_BF16;
+    op.scale = 1.0f;
+    uint64_t* strides[] = {op.q_stride, op.k_stride, op.v_stride, op.o_stride, op.do_stride, op.dq_stride, op.dk_stride, op.dv_stride};
+    for (uint64_t* s : strides) {
+        s[0] = 1ull << 38;
+        s[1] = dim;
+        s[2] = 1ull << 32;
+    }
+    const uint64_t queries = up(q_len, 128) * batch * heads, keys = up(k_len, dim > 64 ? 64 : 128) * batch * kv_heads, most = 1ull << 24;
+    const bool forward = batch * heads <= 1u << 20 && queries < most;
+    const size_t ws = (size_t)1 << 62;
+    int status = okt_attention_forward(&op, at(1), at(2), at(3), at(4), (float*)FAKE, FAKE, ws, nullptr);
+    judge(status, forward, "attention forward", batch * heads, batch * kv_heads, q_len, k_len);
+    status = okt_attention_backward(&op, at(1), at(2), at(3), at(4), (float*)FAKE, at(5), at(6), at(7), at(8), FAKE, ws, nullptr);
+    judge(status, forward && keys < most, "attention backward", batch * heads, batch * kv_heads, q_len, k_len);
+}
+
+int main() {
+    for (uint32_t dim : {8u, 64u, 72u, 128u}) {
+        for (uint64_t planes : {1ull, 3ull, 250ull, 513ull, 1ull << 10, 1ull << 14, (1ull << 20) - 1, 1ull << 20, (1ull << 20) + 1})
+            for (uint64_t length : {1ull, 63ull, 64ull, 65ull, 128ull, 129ull, 1900ull, 2040ull, 2041ull, 2048ull, 2049ull, 1ull << 17, (1ull << 17) + 1, 1ull << 24})
+                for (uint64_t other : {1ull, 64ull, 1025ull, 2048ull, 2049ull, 1ull << 20, 1ull << 24}) {
+                    attention(1, planes, planes, length, other, dim);
+                    attention(planes, 4, 1, length, other, dim);
+                }
+    }
+    std::printf("%ld cases, %ld violations\n", cases, bad);
+    return bad != 0;
+}

@@ -189,3 +189,22 @@ def test_attention_layout_covers_everything_once(tmp_path):
                     os.path.join(ROOT, "tests", "cabi", "attention_layout_check.cpp"), "-o", str(exe)], check=True)
     out = subprocess.run([str(exe)], capture_output=True, text=True)
     assert out.returncode == 0 and " 0 violations" in out.stdout, out.stdout
+
+
+def launch_check(tmp_path, *args):
+    """The host program that stands in for the runtime's launch, linked with the library."""
+    gxx = shutil.which("g++")
+    if gxx is None:
+        pytest.skip("no g++")
+    package, exe = os.path.join(ROOT, "paper_2201_07598_amd"), tmp_path / "launch_check"
+    subprocess.run([gxx, "-O1", "-std=c++17", "-Wall", "-Werror", "-rdynamic", "-I", os.path.join(ROOT, "include"),
+                    os.path.join(ROOT, "tests", "cabi", "launch_check.cpp"), "-L", package, "-lokt",
+                    "-Wl,--unresolved-symbols=ignore-in-shared-libs", "-Wl,-rpath," + package, "-o", str(exe)], check=True)
+    rocm = os.environ.get("ROCM_PATH", "/opt/rocm")
+    env = {**os.environ, "LD_LIBRARY_PATH": os.pathsep.join([os.path.join(rocm, "lib"), os.environ.get("LD_LIBRARY_PATH", "")])}
+    out = subprocess.run([str(exe), *args], capture_output=True, text=True, env=env, timeout=100)
+    assert out.returncode == 0 and " 0 violations" in out.stdout, (out.stdout[-3000:], out.stderr[-2000:])
+
+
+def test_attention_launches_within_the_sizes_of_a_launch(tmp_path):
+    launch_check(tmp_path, "attention")
