@@ -544,7 +544,7 @@ typedef enum okt_dtype { OKT_F32 = 0, OKT_BF16 = 1, OKT_F16 = 2 } okt_dtype;
  * The backward pass is the same call on the gradient of y.
  *   d_x     in   [n] of `dtype`, 16-byte aligned, contiguous
  *   d_y     out  [n]; may be d_x itself, must not overlap it otherwise
- *   n       at most 2^43; 0 is a no-op
+ *   n       at most 2^37 - 2^13; 0 is a no-op
  *   p       probability of dropping, 0 <= p <= 1
  *   d_seed  in   uint64[1] on the device
  */

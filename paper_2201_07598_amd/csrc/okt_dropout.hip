@@ -13,7 +13,7 @@ namespace okt {
 constexpr int DROP_BLOCK = 256;
 constexpr int DROP_GROUPS = 4;
 constexpr uint64_t DROP_TILE = (uint64_t)DROP_BLOCK * DROP_GROUPS * 8;      // elements per workgroup
-constexpr uint64_t DROP_MAX_N = 1ull << 43;                                 // 2^30 workgroups
+constexpr uint64_t DROP_MAX_N = ((1ull << 24) - 1) * DROP_TILE;              // a launch counts work-items in 32 bits
 
 template <typename T>
 __device__ __forceinline__ f32x8 drop_eight(f32x8 v, uint64_t group, RandomKey key, uint32_t site, DropoutRule rule) {

@@ -79,7 +79,11 @@ static void attention(uint64_t batch, uint64_t heads, uint64_t kv_heads, uint64_
     judge(status, forward && keys < most, "attention backward", batch * heads, batch * kv_heads, q_len, k_len);
 }
 
-int main() {
+static void dropout(uint64_t n, int dtype) {
+    judge(okt_dropout(FAKE, FAKE, n, dtype, 0.1, (const uint64_t*)FAKE, 0, nullptr), n < (1ull << 37) - 8191, "dropout", n, dtype, 0, 0);
+}
+
+static void attentions() {
     for (uint32_t dim : {8u, 64u, 72u, 128u}) {
         for (uint64_t planes : {1ull, 3ull, 250ull, 513ull, 1ull << 10, 1ull << 14, (1ull << 20) - 1, 1ull << 20, (1ull << 20) + 1})
             for (uint64_t length : {1ull, 63ull, 64ull, 65ull, 128ull, 129ull, 1900ull, 2040ull, 2041ull, 2048ull, 2049ull, 1ull << 17, (1ull << 17) + 1, 1ull << 24})
@@ -88,6 +92,15 @@ int main() {
                     attention(planes, 4, 1, length, other, dim);
                 }
     }
+}
+
+int main(int, char** what) {
+    if (!std::strcmp(what[1], "attention")) attentions();
+    if (!std::strcmp(what[1], "dropout"))
+        for (int dtype : {OKT_F32, OKT_BF16, OKT_F16}) {
+            const uint64_t most = (1ull << 37) - 8192;
+            for (uint64_t n : {(uint64_t)1, (uint64_t)8193, (uint64_t)1 << 32, (uint64_t)1 << 36, most, most + 1, most + 8192, (uint64_t)1 << 40, (uint64_t)1 << 43}) dropout(n, dtype);
+        }
     std::printf("%ld cases, %ld violations\n", cases, bad);
     return bad != 0;
 }

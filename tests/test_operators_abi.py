@@ -208,3 +208,7 @@ def launch_check(tmp_path, *args):
 
 def test_attention_launches_within_the_sizes_of_a_launch(tmp_path):
     launch_check(tmp_path, "attention")
+
+
+def test_dropout_launches_within_the_sizes_of_a_launch(tmp_path):
+    launch_check(tmp_path, "dropout")
