@@ -349,7 +349,7 @@ __global__ __launch_bounds__(BWD_THREADS) void attention_add_kernel(Sums sums, u
 struct BackwardPointers { const void *q, *k, *v, *o, *d_o; const float* lse; void *dq, *dk, *dv; char* ws; };
 
 template <typename T, int DIM, bool DROP>
-static void launch_backward(const AttentionArgs& a, const AttentionPlan& plan, const BackwardPointers& p, hipStream_t s) {
+static int launch_backward(const AttentionArgs& a, const AttentionPlan& plan, const BackwardPointers& p, hipStream_t s) {
     RowNumbers* rows = (RowNumbers*)(p.ws + plan.rows_at);
     float *dq_sums = (float*)(p.ws + plan.dq_at), *dkv_sums = (float*)(p.ws + plan.dkv_at);
     Sums sums = {};
@@ -361,6 +361,7 @@ static void launch_backward(const AttentionArgs& a, const AttentionPlan& plan, c
                            (const T*)p.d_o, (T*)p.dq, rows,
                            places(a.batch * a.kv_heads, a.group, blocks * parts, window_of(a.causal, a.k_len, DIM, a.group)), parts,
                            divider(parts), dq_sums);
+        if (const int status = launch_status()) return status;          // the keys' kernel would read what this one has not written
         if (parts > 1) sums.of[n++] = {dq_sums, p.dq, a.dq, (uint64_t)a.batch * a.heads * a.q_len, parts, a.q_len, a.heads};
     }
     if (a.k_len) {
@@ -374,6 +375,7 @@ static void launch_backward(const AttentionArgs& a, const AttentionPlan& plan, c
                            places(a.batch * a.kv_heads, 1, blocks * parts, window_of(a.causal, a.q_len, DIM, 1)), parts, divider(parts),
                            dkv_sums);
         timing_after(s);
+        if (const int status = launch_status()) return status;
         if (parts > 1) {
             sums.of[n++] = {dkv_sums, p.dk, a.dk, keys, parts, a.k_len, a.kv_heads};
             sums.of[n++] = {dkv_sums + parts * keys * DIM, p.dv, a.dv, keys, parts, a.k_len, a.kv_heads};
@@ -385,13 +387,14 @@ static void launch_backward(const AttentionArgs& a, const AttentionPlan& plan, c
         hipLaunchKernelGGL((attention_add_kernel<T, DIM>), dim3((unsigned)((most * (DIM / 4) + BWD_THREADS - 1) / BWD_THREADS), n),
                            dim3(BWD_THREADS), 0, s, sums, a.head_dim);
     }
+    return launch_status();
 }
 
 template <typename T>
-static void launch_backward_shape(const AttentionArgs& a, const AttentionPlan& plan, const BackwardPointers& p, hipStream_t s) {
+static int launch_backward_shape(const AttentionArgs& a, const AttentionPlan& plan, const BackwardPointers& p, hipStream_t s) {
     const bool drop = a.drop.bar != 65536u;
-    if (plan.dim == 64) drop ? launch_backward<T, 64, true>(a, plan, p, s) : launch_backward<T, 64, false>(a, plan, p, s);
-    else drop ? launch_backward<T, 128, true>(a, plan, p, s) : launch_backward<T, 128, false>(a, plan, p, s);
+    if (plan.dim == 64) return drop ? launch_backward<T, 64, true>(a, plan, p, s) : launch_backward<T, 64, false>(a, plan, p, s);
+    return drop ? launch_backward<T, 128, true>(a, plan, p, s) : launch_backward<T, 128, false>(a, plan, p, s);
 }
 
 }  // namespace okt
@@ -413,7 +416,5 @@ extern "C" int okt_attention_backward(const okt_attention* op, const void* d_q, 
     if (!d_ws || !aligned(d_ws, 256) || ws_bytes < plan.bytes) return OKT_ERR_WORKSPACE;
     const BackwardPointers p = {d_q, d_k, d_v, d_o, d_do, d_lse, d_dq_out, d_dk_out, d_dv_out, (char*)d_ws};
     const hipStream_t s = (hipStream_t)stream;
-    if (op->dtype == OKT_BF16) launch_backward_shape<__bf16>(a, plan, p, s);
-    else launch_backward_shape<_Float16>(a, plan, p, s);
-    return launch_status();
+    return op->dtype == OKT_BF16 ? launch_backward_shape<__bf16>(a, plan, p, s) : launch_backward_shape<_Float16>(a, plan, p, s);
 }

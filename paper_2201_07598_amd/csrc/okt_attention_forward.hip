@@ -199,7 +199,7 @@ __global__ __launch_bounds__(FWD_THREADS) void attention_join_kernel(AttentionAr
 }
 
 template <typename T, int DIM>
-static void launch_forward(const AttentionArgs& a, const AttentionPlan& plan, const void* q, const void* k, const void* v, void* o,
+static int launch_forward(const AttentionArgs& a, const AttentionPlan& plan, const void* q, const void* k, const void* v, void* o,
                            float* lse, void* ws, hipStream_t s) {
     const uint64_t rows = (uint64_t)a.batch * a.heads * a.q_len;
     const uint32_t block_rows = plan.packed ? a.group * a.q_len : a.q_len, block_heads = plan.packed ? 1 : a.group;
@@ -215,9 +215,13 @@ static void launch_forward(const AttentionArgs& a, const AttentionPlan& plan, co
                        places(a.batch * a.kv_heads, block_heads, blocks * parts, window_of(a.causal && !plan.packed, a.k_len, DIM, a.group)),
                        parts, divider(parts), divider(a.q_len), partial, sums);
     timing_after(s);
-    if (parts > 1)
+    int status = launch_status();
+    if (status == OKT_OK && parts > 1) {
         hipLaunchKernelGGL((attention_join_kernel<T, DIM>), dim3((unsigned)((rows * (DIM / 4) + FWD_THREADS - 1) / FWD_THREADS)),
                            dim3(FWD_THREADS), 0, s, a, (T*)o, lse, parts, (const float*)partial, (const float2*)sums);
+        status = launch_status();
+    }
+    return status;
 }
 
 AttentionPlan attention_plan(uint32_t batch, uint32_t heads, uint32_t kv_heads, uint32_t q_len, uint32_t k_len, uint32_t head_dim,
@@ -327,14 +331,11 @@ int okt_attention_forward(const okt_attention* op, const void* d_q, const void* 
     if (plan.forward_bytes && (!d_ws || !aligned(d_ws, 256) || ws_bytes < plan.forward_bytes)) return OKT_ERR_WORKSPACE;
     const hipStream_t s = (hipStream_t)stream;
     const bool narrow = plan.dim == 64;
-    if (op->dtype == OKT_BF16) {
-        if (narrow) launch_forward<__bf16, 64>(a, plan, d_q, d_k, d_v, d_o_out, d_lse_out, d_ws, s);
-        else launch_forward<__bf16, 128>(a, plan, d_q, d_k, d_v, d_o_out, d_lse_out, d_ws, s);
-    } else {
-        if (narrow) launch_forward<_Float16, 64>(a, plan, d_q, d_k, d_v, d_o_out, d_lse_out, d_ws, s);
-        else launch_forward<_Float16, 128>(a, plan, d_q, d_k, d_v, d_o_out, d_lse_out, d_ws, s);
-    }
-    return launch_status();
+    if (op->dtype == OKT_BF16)
+        return narrow ? launch_forward<__bf16, 64>(a, plan, d_q, d_k, d_v, d_o_out, d_lse_out, d_ws, s)
+                      : launch_forward<__bf16, 128>(a, plan, d_q, d_k, d_v, d_o_out, d_lse_out, d_ws, s);
+    return narrow ? launch_forward<_Float16, 64>(a, plan, d_q, d_k, d_v, d_o_out, d_lse_out, d_ws, s)
+                  : launch_forward<_Float16, 128>(a, plan, d_q, d_k, d_v, d_o_out, d_lse_out, d_ws, s);
 }
 
 }  // extern "C"

@@ -685,6 +685,7 @@ int okt_residual_norm_backward(const okt_residual_norm* op, const void* d_u, con
         launch_norm_type(op->dtype, a, {d_u, nullptr, d_h, d_dh, d_dy, nullptr, nullptr, d_dx_out, d_du_out}, true,
                          shape, (unsigned)plan.groups, s);
         timing_after(s);
+        if (const int status = launch_status()) return status;
     }
     NormOutputs out = {{d_dpre_weight_out, d_dpre_bias_out, d_dpost_weight_out, d_dpost_bias_out}};
     const bool gates = d_dgate_out && plan.parts != 1;

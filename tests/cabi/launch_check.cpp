@@ -1,7 +1,8 @@
 // Host check of what the layer's operators launch, without a GPU: this program stands in for the runtime's
 // launch, which counts, looks at the sizes and does nothing.  Pointers are made up and never read.
 //   sizes     every launch of a call that is accepted counts its work-items in 32 bits, and the sizes at the
-//             edge of what the header allows are accepted, those past it refused
+//             edge of what the header allows are accepted, those past it refused (attention, dropout)
+//   failed    a call ends with the first launch that fails
 // Prints the number of cases and of violations.
 #include <cstdio>
 #include <cstring>
@@ -10,7 +11,7 @@
 #include "okt.h"
 
 struct Dim { uint32_t x, y, z; };
-static int g_launches = 0;
+static int g_launches = 0, g_fail_at = 0, g_error = 0;       // launch number g_fail_at fails
 static bool g_too_many = false;
 
 extern "C" {
@@ -28,10 +29,15 @@ int __hipPopCallConfiguration(Dim* grid, Dim* block, size_t* shared, void** stre
 }
 int hipLaunchKernel(const void*, Dim grid, Dim block, void**, size_t, void*) {
     ++g_launches;
+    if (g_launches == g_fail_at) g_error = 9;                 // an invalid configuration
     if ((uint64_t)grid.x * block.x >> 32 || (uint64_t)grid.y * block.y >> 16 || grid.z != 1) g_too_many = true;
-    return 0;
+    return g_launches == g_fail_at ? 9 : 0;
 }
-int hipGetLastError(void) { return 0; }
+int hipGetLastError(void) {
+    const int e = g_error;
+    g_error = 0;
+    return e;
+}
 }
 
 static long cases = 0, bad = 0;
@@ -53,7 +59,7 @@ static void judge(int status, bool accepted, const char* what, uint64_t a, uint6
 
 static uint64_t up(uint64_t n, uint64_t by) { return (n + by - 1) / by; }
 
-static void attention(uint64_t batch, uint64_t heads, uint64_t kv_heads, uint64_t q_len, uint64_t k_len, uint32_t dim) {
+static okt_attention attention_of(uint64_t batch, uint64_t heads, uint64_t kv_heads, uint64_t q_len, uint64_t k_len, uint32_t dim) {
     okt_attention op;
     std::memset(&op, 0, sizeof op);
     op.batch = (uint32_t)batch;
@@ -70,13 +76,20 @@ static void attention(uint64_t batch, uint64_t heads, uint64_t kv_heads, uint64_
         s[1] = dim;
         s[2] = 1ull << 32;
     }
+    return op;
+}
+
+static const size_t WS = (size_t)1 << 62;
+static int forward(const okt_attention& op) { return okt_attention_forward(&op, at(1), at(2), at(3), at(4), (float*)FAKE, FAKE, WS, nullptr); }
+static int backward(const okt_attention& op) {
+    return okt_attention_backward(&op, at(1), at(2), at(3), at(4), (float*)FAKE, at(5), at(6), at(7), at(8), FAKE, WS, nullptr);
+}
+
+static void attention(uint64_t batch, uint64_t heads, uint64_t kv_heads, uint64_t q_len, uint64_t k_len, uint32_t dim) {
+    const okt_attention op = attention_of(batch, heads, kv_heads, q_len, k_len, dim);
     const uint64_t queries = up(q_len, 128) * batch * heads, keys = up(k_len, dim > 64 ? 64 : 128) * batch * kv_heads, most = 1ull << 24;
-    const bool forward = batch * heads <= 1u << 20 && queries < most;
-    const size_t ws = (size_t)1 << 62;
-    int status = okt_attention_forward(&op, at(1), at(2), at(3), at(4), (float*)FAKE, FAKE, ws, nullptr);
-    judge(status, forward, "attention forward", batch * heads, batch * kv_heads, q_len, k_len);
-    status = okt_attention_backward(&op, at(1), at(2), at(3), at(4), (float*)FAKE, at(5), at(6), at(7), at(8), FAKE, ws, nullptr);
-    judge(status, forward && keys < most, "attention backward", batch * heads, batch * kv_heads, q_len, k_len);
+    judge(forward(op), batch * heads <= 1u << 20 && queries < most, "attention forward", batch * heads, batch * kv_heads, q_len, k_len);
+    judge(backward(op), batch * heads <= 1u << 20 && queries < most && keys < most, "attention backward", batch * heads, batch * kv_heads, q_len, k_len);
 }
 
 static void dropout(uint64_t n, int dtype) {
@@ -94,8 +107,53 @@ static void attentions() {
     }
 }
 
+static okt_residual_norm norm_of(bool gate) {
+    okt_residual_norm op;
+    std::memset(&op, 0, sizeof op);
+    op.rows = 2000;
+    op.width = 768;
+    op.dtype = OKT_BF16;
+    op.eps = 1e-5f;
+    op.residual_scale = 1.0f;
+    op.d_pre_weight = (const float*)FAKE;
+    op.d_gate = gate ? (const float*)FAKE : nullptr;
+    return op;
+}
+
+// A call of `launches` launches, each of which fails in turn.
+template <typename Call>
+static void failing(const char* what, int launches, Call call) {
+    for (int n = 0; n <= launches; ++n) {
+        g_fail_at = n;
+        const int status = call(), wanted = n ? n : launches;
+        ++cases;
+        if (g_launches != wanted || (status == OKT_OK) != (n == 0) || (n && status != OKT_ERR_HIP)) {
+            ++bad;
+            std::printf("%s, launch %d of %d fails: status %d, %d launches\n", what, n, launches, status, g_launches);
+        }
+        g_launches = g_fail_at = 0;
+    }
+}
+
+static void failures() {
+    const okt_attention few = attention_of(1, 2, 2, 1, 100000, 64), plain = attention_of(8, 64, 64, 256, 256, 64), odd = attention_of(1, 4, 2, 300, 3000, 128);
+    failing("attention forward", 1, [&] { return forward(plain); });
+    failing("attention forward in parts", 2, [&] { return forward(few); });
+    failing("attention backward", 2, [&] { return backward(plain); });
+    failing("attention backward in parts", 3, [&] { return backward(odd); });
+    for (bool gate : {false, true}) {
+        const okt_residual_norm op = norm_of(gate);
+        failing("norm forward", 1, [&] { return okt_residual_norm_forward(&op, at(1), at(2), at(3), at(4), (float*)FAKE, nullptr); });
+        failing("norm backward", 2, [&] {
+            return okt_residual_norm_backward(&op, at(1), at(2), (const float*)FAKE, at(3), at(4), at(5), at(6), nullptr, nullptr,
+                                              gate ? (float*)FAKE : nullptr, (float*)FAKE, nullptr, FAKE, WS, nullptr);
+        });
+    }
+}
+
 int main(int, char** what) {
     if (!std::strcmp(what[1], "attention")) attentions();
+    if (!std::strcmp(what[1], "failed")) failures();
     if (!std::strcmp(what[1], "dropout"))
         for (int dtype : {OKT_F32, OKT_BF16, OKT_F16}) {
             const uint64_t most = (1ull << 37) - 8192;

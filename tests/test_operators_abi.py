@@ -212,3 +212,7 @@ def test_attention_launches_within_the_sizes_of_a_launch(tmp_path):
 
 def test_dropout_launches_within_the_sizes_of_a_launch(tmp_path):
     launch_check(tmp_path, "dropout")
+
+
+def test_a_call_ends_with_the_first_launch_that_fails(tmp_path):
+    launch_check(tmp_path, "failed")
