@@ -271,3 +271,30 @@ def test_backward_on_another_stream(D):
     okt.okt_attention_backward(q, k, v, o, lse, do, *got, ws, causal=True, stream=side)
     side.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(want, got))
+
+
+def one_key_above_the_rest(H, K, above, kind, seen=1):
+    """Keys of score 0 but for the first, whose score is `above`; values 1, that key's 0."""
+    q = torch.zeros(1, seen, H, 64, dtype=TYPES[kind], device=DEV)
+    q[..., 0] = 1.0
+    k = torch.zeros(1, K, 1, 64, dtype=TYPES[kind], device=DEV)
+    k[:, 0, :, 0] = above
+    v = torch.ones_like(k)
+    v[:, 0] = 0.0
+    return q, k, v
+
+
+@pytest.mark.parametrize("H", [300, 2])
+def test_the_sum_of_very_many_probabilities(H):
+    """A million keys of 0.3 of the largest: lse by the formula, within the roundings of one exponential, of a
+    tile's sums, of the compensated sum over tiles and of the logarithm; on workgroups of their own and in parts."""
+    K, above = 1 << 20, 1.2
+    q, k, v = one_key_above_the_rest(H, K, above, "bf16")
+    above = float(k[0, 0, 0, 0])
+    ks, vs = (t.expand(1, K, H, 64) for t in (k, v))
+    o, lse = forward(q, ks, vs, scale=1.0)
+    rest = np.exp(-above)
+    total = 1 + (K - 1) * rest
+    want = above + np.log(total)
+    assert np.abs(wide(lse) - want).max() <= 2.0 ** -24 * (24 + 8 * want)
+    assert np.abs(wide(o) - (K - 1) * rest / total).max() <= 2 * UNIT["bf16"]
