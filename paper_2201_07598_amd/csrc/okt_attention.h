@@ -40,6 +40,13 @@ __device__ __forceinline__ frag<T> to_operand(const f32x16& c, int t) {
     return __builtin_convertvector(v, frag<T>);
 }
 
+// Probabilities are operands of the second products in the tensors' type.  bf16 has the exponents of fp32; fp16 ends
+// at 2^-24, below which long flat rows have much of their weight, so there they are taken times a power of two
+// that is divided out of the sums: the forward pass holds a row's largest between 2^7 and 2^15 (fp16 ends at 2^16),
+// the keys' kernel takes 2^12 p.
+template <typename T> struct Raised { static constexpr float forward = 0.0f, keys = 0.0f, keys_factor = 1.0f; };
+template <> struct Raised<_Float16> { static constexpr float forward = 7.0f, keys = 12.0f, keys_factor = 4096.0f; };
+
 // ------------------------------------------------------------------ tiles of rows in LDS
 
 typedef int i32x4 __attribute__((ext_vector_type(4)));

@@ -28,7 +28,7 @@ constexpr int BWD_QUERIES = ATTENTION_QUERIES, BWD_KEYS = ATTENTION_KEYS;
 static_assert(BWD_QUERIES == BWD_THREADS / WAVE * 32, "a wave owns 32 queries");
 
 // What the keys' kernel has to know of a query: its log-sum-exp to base 2 (+inf for a row that
-// sees nothing, whose probabilities come out as 0) and D / c.
+// sees nothing, whose probabilities come out as 0), less what that kernel raises probabilities by, and D / c by as much lower.
 typedef float2 RowNumbers;
 
 template <typename T, int DIM, bool DROP>
@@ -143,7 +143,8 @@ __global__ __launch_bounds__(BWD_THREADS, 2) void attention_backward_queries_ker
             }
         }
     }
-    if (part == 0 && lane < 32 && i < ql) rows[(uint64_t)plane * a.q_len + i] = make_float2(base, sum);
+    if (part == 0 && lane < 32 && i < ql)
+        rows[(uint64_t)plane * a.q_len + i] = make_float2(base - Raised<T>::keys, sum / Raised<T>::keys_factor);
     if (i < (int)a.q_len) {
         T* out = dq + b * a.dq.batch + (uint64_t)i * a.dq.row + h * a.dq.head;
         if (mine == 0 || i >= ql) {
@@ -164,6 +165,7 @@ __global__ __launch_bounds__(BWD_THREADS, DIM == 64 ? 2 : 1) void attention_back
     using Tile = RowTile<T, DIM, TILE, BWD_THREADS>;
     constexpr int NUMBERS = TILE * (int)sizeof(RowNumbers) < 1024 ? 1024 : TILE * (int)sizeof(RowNumbers);
     constexpr int BUFFER = 2 * Tile::BYTES + NUMBERS;
+    constexpr float LOWER = 1.0f / Raised<T>::keys_factor;      // p comes raised, so that ds = p (kept(dp) - D / c) takes the rest lowered
     __shared__ __attribute__((aligned(1024))) char shared[2 * BUFFER];
     const Place at = place_of(blockIdx.x, all);
     const uint32_t block = quotient(at.block, by_part), share = at.block - block * parts;
@@ -268,11 +270,11 @@ __global__ __launch_bounds__(BWD_THREADS, DIM == 64 ? 2 : 1) void attention_back
                             const bool keep = kept_element(w, r, a.drop.bar);
                             const float p = s[r];
                             s[r] = keep ? p : 0.0f;
-                            dp[r] = p * ((keep ? dp[r] : 0.0f) - few[r]);
+                            dp[r] = p * __builtin_fmaf(keep ? dp[r] : 0.0f, LOWER, -few[r]);
                         }
                     } else {
 #pragma unroll
-                        for (int r = 0; r < 16; ++r) dp[r] = s[r] * (dp[r] - few[r]);
+                        for (int r = 0; r < 16; ++r) dp[r] = s[r] * __builtin_fmaf(dp[r], LOWER, -few[r]);
                     }
 #pragma unroll
                     for (int t = 0; t < 2; ++t) {
@@ -319,11 +321,11 @@ __global__ __launch_bounds__(BWD_THREADS, DIM == 64 ? 2 : 1) void attention_back
         if (parts > 1) {
             float* to = partial + (((uint64_t)share * a.batch * a.kv_heads + b * a.kv_heads + kv) * a.k_len + j) * DIM;
             store_partial(to, dkacc, a.scale * drop_scale);
-            store_partial(to + (uint64_t)parts * a.batch * a.kv_heads * a.k_len * DIM, dvacc, drop_scale);
+            store_partial(to + (uint64_t)parts * a.batch * a.kv_heads * a.k_len * DIM, dvacc, drop_scale * LOWER);
             return;
         }
         store_row(dk + b * a.dk.batch + (uint64_t)j * a.dk.row + kv * a.dk.head, dkacc, a.scale * drop_scale, a.head_dim);
-        store_row(dv + b * a.dv.batch + (uint64_t)j * a.dv.row + kv * a.dv.head, dvacc, drop_scale, a.head_dim);
+        store_row(dv + b * a.dv.batch + (uint64_t)j * a.dv.row + kv * a.dv.head, dvacc, drop_scale * LOWER, a.head_dim);
     }
 }
 

@@ -76,7 +76,7 @@ __global__ __launch_bounds__(FWD_THREADS, 2) void attention_forward_kernel(Atten
     const int begin = mine_of.first * FWD_KEYS, end = mine_of.last * FWD_KEYS < keys ? mine_of.last * FWD_KEYS : keys;
 
     f32x16 acc[DIM / 32];
-    float top = -INFINITY;                        // of the scores times scale_log2
+    float top = -INFINITY;                        // of the scores times scale_log2, less what probabilities are raised by
     CompensatedSum total = {0.0f, 0.0f};
 #pragma unroll
     for (int d = 0; d < DIM / 32; ++d) acc[d] = 0.0f;
@@ -124,7 +124,7 @@ __global__ __launch_bounds__(FWD_THREADS, 2) void attention_forward_kernel(Atten
             for (int n = 0; n < FWD_KEYS / 32; ++n)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) most = fmaxf(most, s[n][r]);
-            most = max_halves(most) * a.scale_log2;
+            most = __builtin_fmaf(max_halves(most), a.scale_log2, -Raised<T>::forward);
             // Sums are kept relative to `top`, which follows the maximum in steps: as long as no
             // lane's has grown by more than a factor of 2^8, which changes neither the relative precision of
             // a probability nor of a sum, there is nothing to rescale.

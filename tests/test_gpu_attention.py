@@ -284,6 +284,33 @@ def one_key_above_the_rest(H, K, above, kind, seen=1):
     return q, k, v
 
 
+@pytest.mark.parametrize("H,seen", [(300, 1), (2, 1), (3, 100)])
+def test_small_probabilities_add_up_in_fp16(H, seen):
+    """4095 keys 2^-25.6 of the largest: each is below the smallest fp16 number beside a 1.  o and dv are sums over
+    them; each probability is at least 2^7 and 2^12 times that in the products, so it is off by 2^-32 and
+    2^-37 at the most."""
+    K, above = 4096, 17.75
+    q, k, v = one_key_above_the_rest(H, K, above, "f16", seen)
+    v *= 1000.0
+    rest = np.exp(-above)
+    total = 1 + (K - 1) * rest
+    keys = [t.expand(1, K, H, 64).contiguous() for t in (k, v)]
+    for ks, vs in ((k, v), keys):                              # shared by the heads, and one each
+        o, lse = forward(q, ks, vs, scale=1.0)
+        want = 1000.0 * (K - 1) * rest / total
+        assert np.abs(wide(o) - want).max() <= 1000.0 * (K - 1) * 2.0 ** -32 + 2 * UNIT["f16"] * want
+        assert np.abs(wide(lse) - (above + np.log(total))).max() <= 2.0 ** -24 * (16 + 8 * above)
+        do = torch.full_like(q, 1000.0)
+        _, _, dv = backward(q, ks, vs, o, lse, do, scale=1.0)
+        rows = seen * (H if ks is k else 1)
+        want = 1000.0 * rows * rest / total
+        assert np.abs(wide(dv)[:, 1:] - want).max() <= 1000.0 * rows * 2.0 ** -37 + 2 * UNIT["f16"] * want + step("f16")
+    # differences of the forward pass in the direction of v agree with dv where only v changes (o is linear in it)
+    o2, _ = forward(q, keys[0], keys[1] * 2, scale=1.0)
+    o1, _ = forward(q, keys[0], keys[1], scale=1.0)
+    assert torch.equal(o2, o1 * 2)
+
+
 @pytest.mark.parametrize("H", [300, 2])
 def test_the_sum_of_very_many_probabilities(H):
     """A million keys of 0.3 of the largest: lse by the formula, within the roundings of one exponential, of a
