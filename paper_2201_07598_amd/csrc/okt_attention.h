@@ -59,7 +59,7 @@ constexpr uint32_t OUTSIDE = 0xffff0000u;     // an offset that no buffer reache
 // of LDS; fetched() waits where it has to be.
 __device__ __forceinline__ void fetch_to_lds(uint32_t lds, uint32_t offset, i32x4 buffer) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
-                 :: "s"(lds), "v"(offset), "s"(buffer) : "memory");
+                 :: "s"(lds), "v"(offset), "s"(buffer) : "m0", "memory");
 }
 
 __device__ __forceinline__ uint32_t lds_address(const void* p) {

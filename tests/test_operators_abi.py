@@ -216,3 +216,16 @@ def test_dropout_launches_within_the_sizes_of_a_launch(tmp_path):
 
 def test_a_call_ends_with_the_first_launch_that_fails(tmp_path):
     launch_check(tmp_path, "failed")
+
+
+def test_assembly_names_the_registers_it_sets():
+    """A statement that sets m0 says so; otherwise the compiler may keep something of its own there."""
+    import glob
+    import re
+    setting = 0
+    for path in sorted(glob.glob(os.path.join(ROOT, "paper_2201_07598_amd", "csrc", "*"))):
+        for statement in re.findall(r"\basm\b[^;]*?\(.*?\)\s*;", open(path).read(), flags=re.S):
+            if re.search(r"s_\w+ m0\b", statement):
+                setting += 1
+                assert '"m0"' in statement.rsplit(":", 1)[1], (path, statement)
+    assert setting
