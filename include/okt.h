@@ -589,9 +589,8 @@ typedef struct okt_residual_norm {
 size_t okt_residual_norm_workspace_bytes(uint64_t rows, uint32_t width, uint64_t rows_per_gate);
 
 /*
- * Forward.  d_h_out may be NULL where d_y_out is wanted alone, and may be d_x or d_u;
- * d_y_out is NULL without d_pre_weight, and may be d_u or d_x if d_h_out is neither; in an input's
- * place an output has that input's stride.
+ * Forward.  d_h_out may be NULL where d_y_out is wanted alone; d_y_out is NULL without d_pre_weight.
+ * Either may be d_x or d_u, with that input's stride, but they do not overlap each other, or an input at any other place.
  *   d_stats_out  out  fp32[rows][4], 16-byte aligned: m and r of the post norm, m and r of
  *                     the pre norm (0 where there is none); NULL if no backward pass follows
  * rows = 0 is a no-op.  One launch.
@@ -607,7 +606,8 @@ int okt_residual_norm_forward(const okt_residual_norm* op, const void* d_u, cons
  *   d_dh     in   gradient of h from its other uses; NULL for zero if there is a pre norm
  *   d_dy     in   gradient of y; NULL exactly where there is no pre norm
  *   d_dx_out, d_du_out  out  may be any of the inputs that are read, with that input's stride
- *                            (the first kernel reads a row before it writes it), not each other
+ *                            (the first kernel reads a row before it writes it); they do not overlap each other, or an
+ *                            input at any other place
  *   d_d*_weight_out, d_d*_bias_out  out  fp32[width], d_dgate_out fp32[gates][width]; each may
  *                            be NULL, and must be where there is no such parameter
  * rows = 0 writes zeros to the parameter gradients (one gate).  Two launches.

@@ -577,6 +577,23 @@ static bool norm_args(const okt_residual_norm* op, NormArgs& a) {
     return true;
 }
 
+// Where two [rows, width] tensors share an element.  Rows of unlike strides that lie in the same stretch are taken to
+// share one only where their first rows do.
+static bool rows_overlap(const void* a, uint64_t a_stride, const void* b, uint64_t b_stride, uint64_t rows, uint64_t row_bytes, size_t e) {
+    const uint64_t between = rows - 1;
+    if (!a || !b || !overlap(a, between * a_stride * e + row_bytes, b, between * b_stride * e + row_bytes)) return false;
+    if (rows == 1 || overlap(a, row_bytes, b, row_bytes)) return true;
+    if (a_stride != b_stride) return false;
+    const uint64_t step = a_stride * e, apart = (a < b ? (uintptr_t)b - (uintptr_t)a : (uintptr_t)a - (uintptr_t)b) % step;
+    return apart < row_bytes || step - apart < row_bytes;
+}
+
+// An output may lie in an input's place, row by row, and nowhere else in it.
+static bool misplaced(const void* out, uint64_t out_stride, const void* in, uint64_t in_stride, const NormArgs& a, size_t e) {
+    if (out == in && (out_stride == in_stride || a.rows == 1)) return false;
+    return rows_overlap(out, out_stride, in, in_stride, a.rows, a.width * e, e);
+}
+
 struct NormPointers { const void *u, *x, *h, *dh, *dy; void *out_h, *out_y, *dx, *du; };
 
 template <typename T, typename L>
@@ -630,11 +647,9 @@ int okt_residual_norm_forward(const okt_residual_norm* op, const void* d_u, cons
     for (const void* p : {d_u, d_x, (const void*)d_h_out, (const void*)d_y_out})
         if (!aligned(p, e)) return OKT_ERR_INVALID_ARG;
     if (!aligned(d_stats_out, 16)) return OKT_ERR_INVALID_ARG;
-    // in an input's place, row by row
-    for (const void* out : {(const void*)d_h_out, (const void*)d_y_out}) {
-        const uint64_t stride = out == d_h_out ? a.h_stride : a.y_stride;
-        if (out && a.rows > 1 && ((out == d_u && stride != a.u_stride) || (out == d_x && stride != a.x_stride))) return OKT_ERR_INVALID_ARG;
-    }
+    if (rows_overlap(d_h_out, a.h_stride, d_y_out, a.y_stride, a.rows, a.width * e, e) ||
+        misplaced(d_h_out, a.h_stride, d_u, a.u_stride, a, e) || misplaced(d_h_out, a.h_stride, d_x, a.x_stride, a, e) ||
+        misplaced(d_y_out, a.y_stride, d_u, a.u_stride, a, e) || misplaced(d_y_out, a.y_stride, d_x, a.x_stride, a, e)) return OKT_ERR_INVALID_ARG;
     a.stats = (float4*)d_stats_out;
     const NormShape shape = norm_shape(a.width, a.rows, op->dtype, false);
     const uint64_t at_once = rows_at_once(shape);
@@ -666,13 +681,14 @@ int okt_residual_norm_backward(const okt_residual_norm* op, const void* d_u, con
             if (!aligned(p, e)) return OKT_ERR_INVALID_ARG;
         const struct { const void* p; uint64_t stride; } in[] = {{all ? d_u : nullptr, a.u_stride}, {a.pre_w ? d_h : nullptr, a.h_stride},
                                                                  {d_dh, a.dh_stride}, {d_dy, a.dy_stride}};
-        for (const auto& t : in)                                // in an input's place, row by row
-            if (t.p && a.rows > 1 && ((t.p == d_dx_out && t.stride != a.dx_stride) || (t.p == d_du_out && t.stride != a.du_stride)))
-                return OKT_ERR_INVALID_ARG;
+        for (const auto& t : in)
+            if (misplaced(d_dx_out, a.dx_stride, t.p, t.stride, a, e) || misplaced(d_du_out, a.du_stride, t.p, t.stride, a, e)) return OKT_ERR_INVALID_ARG;
     }
     const NormShape shape = norm_shape(a.width, a.rows, op->dtype, all);
     const NormPlan plan = norm_plan(a.rows, a.rows_per_gate, rows_at_once(shape));
     if (!d_ws || !aligned(d_ws, 256) || ws_bytes < norm_ws_bytes(a.rows, a.width, a.rows_per_gate)) return OKT_ERR_WORKSPACE;
+    if (a.rows && rows_overlap(d_dx_out, a.dx_stride, d_du_out, a.du_stride, a.rows, a.width * dtype_bytes(op->dtype), dtype_bytes(op->dtype)))
+        return OKT_ERR_INVALID_ARG;
     a.stats = (float4*)d_stats;
     a.partial = (float*)d_ws;
     a.dgate = d_dgate_out;

@@ -2,6 +2,7 @@
 // launch, which counts, looks at the sizes and does nothing.  Pointers are made up and never read.
 //   sizes     every launch of a call that is accepted counts its work-items in 32 bits, and the sizes at the
 //             edge of what the header allows are accepted, those past it refused (attention, dropout)
+//   norm      outputs in the place of inputs, side by side and one after the other are taken
 //   failed    a call ends with the first launch that fails
 // Prints the number of cases and of violations.
 #include <cstdio>
@@ -120,6 +121,36 @@ static okt_residual_norm norm_of(bool gate) {
     return op;
 }
 
+static void norms() {
+    const auto place = [](uint64_t n) { return (void*)(0x100000 * n); };
+    void *const u = place(1), *const x = place(2), *const h = place(3), *const y = place(4), *const dx = place(5), *const du = place(6);
+    for (uint64_t stride : {0, 2 * 768}) {
+        okt_residual_norm op = norm_of(false);
+        op.rows = 100;
+        for (uint64_t* s : {&op.u_stride, &op.x_stride, &op.h_stride, &op.y_stride, &op.dh_stride, &op.dy_stride, &op.dx_stride, &op.du_stride}) *s = stride;
+        const auto after = [&](void* p) { return (char*)p + (stride ? 768 * 2 : 100 * 768 * 2); };
+        const auto forward = [&](void* h_out, void* y_out) {
+            judge(okt_residual_norm_forward(&op, u, x, h_out, y_out, nullptr, nullptr), true, "norm forward", (uint64_t)h_out, (uint64_t)y_out, stride, 0);
+        };
+        const auto backward = [&](void* dx_out, void* du_out) {
+            judge(okt_residual_norm_backward(&op, nullptr, h, (const float*)FAKE, u, y, dx_out, du_out, nullptr, nullptr, nullptr, nullptr, nullptr, FAKE,
+                                             (size_t)1 << 40, nullptr), true, "norm backward", (uint64_t)dx_out, (uint64_t)du_out, stride, 0);
+        };
+        forward(x, u);
+        forward(u, x);
+        forward(x, y);
+        forward(h, u);
+        forward(h, after(h));
+        forward(after(u), after(x));
+        backward(u, y);
+        backward(h, u);
+        backward(y, h);
+        backward(dx, after(dx));
+        backward(after(du), du);
+        backward(after(u), after(h));
+    }
+}
+
 // A call of `launches` launches, each of which fails in turn.
 template <typename Call>
 static void failing(const char* what, int launches, Call call) {
@@ -153,6 +184,7 @@ static void failures() {
 
 int main(int, char** what) {
     if (!std::strcmp(what[1], "attention")) attentions();
+    if (!std::strcmp(what[1], "norm")) norms();
     if (!std::strcmp(what[1], "failed")) failures();
     if (!std::strcmp(what[1], "dropout"))
         for (int dtype : {OKT_F32, OKT_BF16, OKT_F16}) {

@@ -289,3 +289,14 @@ def test_another_stream(width):
     okt.okt_residual_norm_backward(c.u, c.h, c.stats, c.dh, c.dy, c.dx, c.du, c.ws, stream=side, **c.grads, **c.options)
     side.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(want, (c.h, c.y, c.stats, c.dx, c.du, *c.grads.values())))
+
+
+@pytest.mark.parametrize("width", [300, 700, 1028, 4100])
+def test_both_outputs_in_the_place_of_inputs(width):
+    """h over one of u and x and y over the other."""
+    for swap in (False, True):
+        a, b = (Case(1500, width, "bf16", post=True, gates=1, p=0.1) for _ in range(2))
+        a.forward()
+        h, y = (b.u, b.x) if swap else (b.x, b.u)
+        okt.okt_residual_norm_forward(b.u, b.x, h, y, b.stats, **b.options)
+        assert torch.equal(a.h, h) and torch.equal(a.y, y) and torch.equal(a.stats, b.stats)

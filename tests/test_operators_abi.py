@@ -229,3 +229,28 @@ def test_assembly_names_the_registers_it_sets():
                 setting += 1
                 assert '"m0"' in statement.rsplit(":", 1)[1], (path, statement)
     assert setting
+
+
+def test_norm_refuses_outputs_that_overlap():
+    """Outputs over each other, and over inputs at another place than row by row; halves of one buffer are apart."""
+    lib = okt.load_library()
+    U, X, H, Y = (FAKE << n for n in range(1, 5))
+    two, apart = (128,) * 8, 64 * 2                                        # rows of 64 in two bytes each, beside another tensor's
+
+    def forward(u=U, x=X, h=H, y=Y, **change):
+        return lib.okt_residual_norm_forward(norm_struct(**change), u, x, h, y, None, None)
+
+    def backward(h=H, dh=U, dy=Y, dx=X, du=FAKE << 5, **change):
+        return lib.okt_residual_norm_backward(norm_struct(**change), None, h, FAKE << 6, dh, dy, dx, du, None, None, None, None, None,
+                                              FAKE << 7, 1 << 24, None)
+
+    for bad in ({"y": H}, {"y": H + 2}, {"y": H + 3 * 128}, {"h": X, "y": X}, {"h": X + 2}, {"y": U - 2}, {"h": U + 128},
+                {"y": H + apart - 2, "strides": two}, {"y": H + 126, "strides": two}, {"rows": 1, "y": H + 126}, {"rows": 1, "h": X + 2}):
+        assert forward(**bad) == INVALID, bad
+    for bad in ({"du": X}, {"du": X - 126}, {"du": X + 3 * 128}, {"dx": H + 2}, {"du": Y + 128}, {"dx": U - 2},
+                {"du": X + 130, "strides": (128,) * 8, "dx": X + 4}, {"rows": 1, "du": X + 2}):
+        assert backward(**bad) == INVALID, bad
+
+
+def test_norm_takes_outputs_in_the_place_of_inputs_and_side_by_side(tmp_path):
+    launch_check(tmp_path, "norm")
