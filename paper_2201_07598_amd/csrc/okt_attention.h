@@ -348,6 +348,9 @@ bool attention_args(const okt_attention* op, bool backward, AttentionArgs& a);
 // Workgroups of 256 threads that a launch can have: it counts work-items in 32 bits.
 constexpr uint64_t LAUNCH_GROUPS = (1ull << 24) - 1;
 
+// Whether two tensors begin in the same place: their first vectors share an element.
+inline bool same_place(const void* a, const void* b, uint32_t head_dim) { return a && b && overlap(a, head_dim * 2, b, head_dim * 2); }
+
 // Lengths of a sequence, held to the tensors'.
 __device__ __forceinline__ int sequence_length(const int32_t* lens, uint32_t b, uint32_t most) {
     if (!lens) return (int)most;

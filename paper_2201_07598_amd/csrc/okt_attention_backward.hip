@@ -416,6 +416,12 @@ extern "C" int okt_attention_backward(const okt_attention* op, const void* d_q, 
     const AttentionPlan plan = attention_plan(a.batch, a.heads, a.kv_heads, a.q_len, a.k_len, a.head_dim, a.drop.bar != 65536u);
     if (plan.query_groups > LAUNCH_GROUPS || plan.key_groups > LAUNCH_GROUPS) return OKT_ERR_INVALID_ARG;
     if (!d_ws || !aligned(d_ws, 256) || ws_bytes < plan.bytes) return OKT_ERR_WORKSPACE;
+    const auto there = [](uint32_t length, const void* p) { return length ? p : nullptr; };
+    const void* const tensors[] = {there(a.q_len, d_dq_out), there(a.k_len, d_dk_out), there(a.k_len, d_dv_out), there(a.q_len, d_q),
+                                   there(a.k_len, d_k), there(a.k_len, d_v), there(a.q_len, d_o), there(a.q_len, d_do)};
+    for (int out = 0; out < 3; ++out)
+        for (int other = out + 1; other < 8; ++other)
+            if (same_place(tensors[out], tensors[other], a.head_dim)) return OKT_ERR_INVALID_ARG;
     const BackwardPointers p = {d_q, d_k, d_v, d_o, d_do, d_lse, d_dq_out, d_dk_out, d_dv_out, (char*)d_ws};
     const hipStream_t s = (hipStream_t)stream;
     return op->dtype == OKT_BF16 ? launch_backward_shape<__bf16>(a, plan, p, s) : launch_backward_shape<_Float16>(a, plan, p, s);

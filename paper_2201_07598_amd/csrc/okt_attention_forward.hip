@@ -349,6 +349,8 @@ int okt_attention_forward(const okt_attention* op, const void* d_q, const void* 
     const AttentionPlan plan = attention_plan(a.batch, a.heads, a.kv_heads, a.q_len, a.k_len, a.head_dim, a.drop.bar != 65536u);
     if (plan.forward_groups > LAUNCH_GROUPS) return OKT_ERR_INVALID_ARG;
     if (plan.forward_bytes && (!d_ws || !aligned(d_ws, 256) || ws_bytes < plan.forward_bytes)) return OKT_ERR_WORKSPACE;
+    for (const void* in : {d_q, a.k_len ? d_k : nullptr, a.k_len ? d_v : nullptr})
+        if (same_place(d_o_out, in, a.head_dim)) return OKT_ERR_INVALID_ARG;
     const hipStream_t s = (hipStream_t)stream;
     const bool narrow = plan.dim == 64;
     if (op->dtype == OKT_BF16)

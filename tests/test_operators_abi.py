@@ -254,3 +254,23 @@ def test_norm_refuses_outputs_that_overlap():
 
 def test_norm_takes_outputs_in_the_place_of_inputs_and_side_by_side(tmp_path):
     launch_check(tmp_path, "norm")
+
+
+def test_attention_refuses_outputs_that_overlap():
+    lib = okt.load_library()
+    at = {n: FAKE << i for i, n in enumerate(("q", "k", "v", "o", "lse", "do", "dq", "dk", "dv", "ws"))}
+
+    def forward(ws_bytes=1 << 30, change=None, **place):
+        a = {**at, **place}
+        return lib.okt_attention_forward(attention_struct(**(change or {})), a["q"], a["k"], a["v"], a["o"], a["lse"], a["ws"], ws_bytes, None)
+
+    def backward(ws_bytes=1 << 30, change=None, **place):
+        a = {**at, **place}
+        return lib.okt_attention_backward(attention_struct(**(change or {})), *(a[n] for n in ("q", "k", "v", "o", "lse", "do", "dq", "dk", "dv", "ws")), ws_bytes, None)
+
+    for name in ("q", "k", "v"):
+        assert forward(o=at[name]) == INVALID, name
+        assert forward(o=at[name] + 112) == INVALID, name
+    for out in ("dq", "dk", "dv"):
+        for name in ("q", "k", "v", "o", "do", *({"dq", "dk", "dv"} - {out})):
+            assert backward(**{out: at[name]}) == INVALID, (out, name)
