@@ -638,7 +638,8 @@ int okt_residual_norm_backward(const okt_residual_norm* op, const void* d_u, con
  * In fp16 a p below 2^-32 of its row's largest (for dv: below 2^-37) and a ds below 2^-25 are rounded to 0.
  * A tensor is [batch][length][heads][head_dim] by strides {batch, length, heads} in elements,
  * head_dim contiguous; strides are multiples of 8 (that of the length from head_dim to 2^24), bases
- * 16-byte aligned, so the parts of a common projection are taken as they lie.
+ * 16-byte aligned, so the parts of a common projection are taken as they lie.  Sequences or heads of an input
+ * may be the same memory (a stride of 0), those of an output may not.
  */
 typedef struct okt_attention {
     uint32_t batch, heads, kv_heads;   /* heads a multiple of kv_heads; batch * heads <= 2^20 */

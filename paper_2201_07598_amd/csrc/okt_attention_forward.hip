@@ -282,11 +282,13 @@ AttentionPlan attention_plan(uint32_t batch, uint32_t heads, uint32_t kv_heads, 
 }
 
 // Strides of a tensor of these sizes; one that is never taken may be anything.  Rows do not overlap: a
-// fetch's bounds, in bytes, are what keeps it from rows past the last.
-static bool strides(const uint64_t (&s)[3], uint32_t batch, uint32_t length, uint32_t heads, uint32_t head_dim, Strides& to) {
+// fetch's bounds, in bytes, are what keeps it from rows past the last.  An input may have sequences or heads in
+// the same memory, an output may not.
+static bool strides(const uint64_t (&s)[3], bool output, uint32_t batch, uint32_t length, uint32_t heads, uint32_t head_dim, Strides& to) {
     to = {batch > 1 ? s[0] : 0, length > 1 ? s[1] : head_dim, heads > 1 ? s[2] : 0};
     for (uint64_t n : {to.batch, to.row, to.head})
         if (n % 8 || n > (1ull << 40)) return false;
+    if (output && ((batch > 1 && to.batch < head_dim) || (heads > 1 && to.head < head_dim))) return false;
     return to.row >= head_dim && to.row <= (1u << 24);        // a tile's offsets fit 32 bits
 }
 
@@ -299,13 +301,13 @@ bool attention_args(const okt_attention* op, bool backward, AttentionArgs& a) {
     if (!dropout_rule(op->dropout_p, a.drop)) return false;
     if (a.drop.bar != 65536u && (!op->d_seed || !aligned(op->d_seed, 8))) return false;
     if (!aligned(op->d_q_lens, 4) || !aligned(op->d_k_lens, 4)) return false;
-    const auto take = [&](const uint64_t (&from)[3], bool keys, Strides& to) {
-        return strides(from, op->batch, keys ? op->k_len : op->q_len, keys ? op->kv_heads : op->heads, op->head_dim, to);
+    const auto take = [&](const uint64_t (&from)[3], bool keys, Strides& to, bool output = false) {
+        return strides(from, output, op->batch, keys ? op->k_len : op->q_len, keys ? op->kv_heads : op->heads, op->head_dim, to);
     };
     if (!take(op->q_stride, false, a.q) || !take(op->k_stride, true, a.k) || !take(op->v_stride, true, a.v) ||
-        !take(op->o_stride, false, a.o)) return false;
-    if (backward && (!take(op->do_stride, false, a.d_o) || !take(op->dq_stride, false, a.dq) ||
-                     !take(op->dk_stride, true, a.dk) || !take(op->dv_stride, true, a.dv))) return false;
+        !take(op->o_stride, false, a.o, !backward)) return false;
+    if (backward && (!take(op->do_stride, false, a.d_o) || !take(op->dq_stride, false, a.dq, true) ||
+                     !take(op->dk_stride, true, a.dk, true) || !take(op->dv_stride, true, a.dv, true))) return false;
     a.batch = op->batch;
     a.heads = op->heads;
     a.kv_heads = op->kv_heads;

@@ -274,3 +274,19 @@ def test_attention_refuses_outputs_that_overlap():
     for out in ("dq", "dk", "dv"):
         for name in ("q", "k", "v", "o", "do", *({"dq", "dk", "dv"} - {out})):
             assert backward(**{out: at[name]}) == INVALID, (out, name)
+
+
+def test_attention_refuses_outputs_whose_places_are_the_same_memory():
+    """One vector for all sequences, or for all heads: inputs may be broadcast so, outputs not."""
+    lib, at = okt.load_library(), [FAKE << i for i in range(10)]
+    strides = [2048, 256, 64] * 8
+    for tensor in (3, 5, 6, 7):
+        for axis in (0, 2):
+            for step in (0, 56):
+                same = list(strides)
+                same[3 * tensor + axis] = step
+                op = attention_struct(strides=same)
+                if tensor == 3:
+                    assert lib.okt_attention_forward(op, *at[:6], 1 << 30, None) == INVALID, (axis, step)
+                else:
+                    assert lib.okt_attention_backward(op, *at, 1 << 30, None) == INVALID, (tensor, axis, step)
