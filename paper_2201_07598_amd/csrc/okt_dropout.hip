@@ -72,6 +72,7 @@ extern "C" int okt_dropout(const void* d_x, void* d_y, uint64_t n, int dtype, do
     if (!known_dtype(dtype) || !dropout_rule(p, rule) || n > DROP_MAX_N) return OKT_ERR_INVALID_ARG;
     if (n == 0) return OKT_OK;
     if (!d_x || !d_y || !d_seed || !aligned(d_x, 16) || !aligned(d_y, 16) || !aligned(d_seed, 8)) return OKT_ERR_INVALID_ARG;
+    if (d_x != d_y && overlap(d_x, n * dtype_bytes(dtype), d_y, n * dtype_bytes(dtype))) return OKT_ERR_INVALID_ARG;
     const hipStream_t s = (hipStream_t)stream;
     if (dtype == OKT_F32) return launch_dropout<float>(d_x, d_y, n, d_seed, site, rule, s);
     if (dtype == OKT_BF16) return launch_dropout<__bf16>(d_x, d_y, n, d_seed, site, rule, s);

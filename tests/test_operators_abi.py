@@ -290,3 +290,9 @@ def test_attention_refuses_outputs_whose_places_are_the_same_memory():
                     assert lib.okt_attention_forward(op, *at[:6], 1 << 30, None) == INVALID, (axis, step)
                 else:
                     assert lib.okt_attention_backward(op, *at, 1 << 30, None) == INVALID, (tensor, axis, step)
+
+
+def test_dropout_refuses_an_output_that_overlaps_its_input():
+    for dtype, size in ((0, 4), (1, 2)):
+        for y in (FAKE + 16, FAKE - 16, FAKE + 64 * size - 16, FAKE - 64 * size + 16):
+            assert dropout(y=y, dtype=dtype) == INVALID, (dtype, y)
