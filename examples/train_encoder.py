@@ -5,9 +5,11 @@
 Everything between the matrix products of a layer is one of this library's operators:
 attention over a padded batch with dropout (okt_attention_forward / _backward), and
 dropout, the sum with the residual stream and the norm after it in one call
-(okt_residual_norm_forward / _backward), and the dropout of the embeddings (okt_dropout).  The gradients of all parameters land in one
-flat fp32 vector.  Each worker accumulates it into its residual and selects its top-k entries
-(okt_accumulate_topk_select), and the reduced entries (okt_sparse_reduce) update the weights.
+(okt_residual_norm_forward / _backward), and the dropout of the embeddings (okt_dropout).
+The gradients of all parameters land in one flat fp32 vector: the norms' are written there by
+the operator, the products' are added there by autograd.  Each worker accumulates the vector into
+its residual and selects its top-k entries (okt_accumulate_topk_select), and the reduced entries
+(okt_sparse_reduce) update the weights.
 
 The task is synthetic: a third of a sequence's tokens are one and the same, and every position has
 to name it, which takes attention.
@@ -74,7 +76,8 @@ class Attention(torch.autograd.Function):
 
 
 class SumNorm(torch.autograd.Function):
-    """norm(x + dropout(u)) on [rows, width]."""
+    """norm(x + dropout(u)) on [rows, width].  The gradients of weight and bias are written where `weight.grad` and
+    `bias.grad` lie, in the flat vector, by the call itself; the graph hands on nothing for them."""
 
     @staticmethod
     def forward(ctx, u, x, weight, bias, seed, site, p):
@@ -82,18 +85,18 @@ class SumNorm(torch.autograd.Function):
         stats = torch.empty(x.shape[0], 4, device=x.device)
         okt.okt_residual_norm_forward(u, x, h, y, stats, pre_weight=weight, pre_bias=bias, dropout_p=p, seed=seed, site=site)
         ctx.save_for_backward(u, h, stats, weight, bias)
-        ctx.rest = (seed, site, p)
+        ctx.rest = (weight.grad, bias.grad, seed, site, p)
         return y
 
     @staticmethod
     def backward(ctx, dy):
         u, h, stats, weight, bias = ctx.saved_tensors
-        seed, site, p = ctx.rest
-        dx, du, dw, db = (torch.empty_like(t) for t in (h, h, weight, bias))
+        dw, db, seed, site, p = ctx.rest
+        dx, du = torch.empty_like(h), torch.empty_like(h)
         ws = torch.empty(okt.okt_residual_norm_workspace_bytes(*h.shape), dtype=torch.uint8, device=h.device)
         okt.okt_residual_norm_backward(u, h, stats, None, dy.contiguous(), dx, du, ws, dpre_weight=dw, dpre_bias=db,
                                        pre_weight=weight, pre_bias=bias, dropout_p=p, seed=seed, site=site)
-        return du, dx, dw, db, None, None, None
+        return du, dx, None, None, None, None, None
 
 
 class Encoder:
