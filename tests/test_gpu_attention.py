@@ -325,3 +325,14 @@ def test_the_sum_of_very_many_probabilities(H):
     want = above + np.log(total)
     assert np.abs(wide(lse) - want).max() <= 2.0 ** -24 * (24 + 8 * want)
     assert np.abs(wide(o) - (K - 1) * rest / total).max() <= 2 * UNIT["bf16"]
+
+
+@pytest.mark.parametrize("kind,p", [("bf16", 0.0), ("f16", 0.1)])
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("D", [64, 128])
+def test_many_tiles_a_workgroup(D, causal, kind, p):
+    """More blocks than are split: fifteen tiles of keys and as many of queries pass by a workgroup, four heads a group."""
+    lens = ([900, 700, 900, 1, 333], [900, 900, 451, 900, 1])
+    q, k, v, do = make(5, 8, 2, 900, 900, D, kind)
+    check(q, k, v, do, kind, causal=causal, p=p)
+    check(q, k, v, do, kind, causal=causal, p=p, lens=lens)
