@@ -633,9 +633,10 @@ int okt_residual_norm_backward(const okt_residual_norm* op, const void* d_u, con
  *   dv_j = sum_i pd_ij do_i,  dq_i = scale sum_j ds_ij k_j,  dk_j = scale sum_i ds_ij q_i
  * dv and dk summed over the query heads of a group.  Products are taken by the matrix
  * units from 16-bit inputs with fp32 sums; p and ds are rounded to the tensors' type for the
- * second product of each pass.  The sum of a row's p is compensated, so lse is good to a few roundings at any
+ * second product of each pass (up to batch * heads * q_len * k_len = 2^16 pairs, where the rounding of one would show,
+ * into two parts, of 16 bits in bf16 and 22 in fp16).  In fp16 a p below 2^-32 of its row's largest (for dv: below
+ * 2^-37) and a ds below 2^-25 are rounded to 0.  The sum of a row's p is compensated, so lse is good to a few roundings at any
  * length; the other sums are plain fp32: over values that are all alike, o is off by 2^-10 at 2^20 keys and by 2^-9 at 2^22.
- * In fp16 a p below 2^-32 of its row's largest (for dv: below 2^-37) and a ds below 2^-25 are rounded to 0.
  * A tensor is [batch][length][heads][head_dim] by strides {batch, length, heads} in elements,
  * head_dim contiguous; strides are multiples of 8 (that of the length from head_dim to 2^24), bases
  * 16-byte aligned, so the parts of a common projection are taken as they lie.  Sequences or heads of an input

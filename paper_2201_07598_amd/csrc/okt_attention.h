@@ -31,13 +31,25 @@ __device__ __forceinline__ f32x16 mfma(frag<_Float16> a, frag<_Float16> b, f32x1
     return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
 }
 
-// Eight neighbouring elements of a C tile as a B operand.
-template <typename T>
-__device__ __forceinline__ frag<T> to_operand(const f32x16& c, int t) {
-    f32x8 v;
+// Eight neighbouring elements of a C tile as a B operand: rounded to the tensors' type, and if FINE a second operand
+// of what the rounding left off, so that the product is that of 16 (fp16: 22) bits.  The rounding is what the matrix units'
+// rate costs: products of fp32 operands run at a sixteenth of it.
+template <typename T, bool FINE>
+struct Operand {
+    frag<T> rounded, rest;
+    __device__ __forceinline__ Operand(const f32x16& c, int t) {
+        f32x8 v;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = c[8 * t + i];
-    return __builtin_convertvector(v, frag<T>);
+        for (int i = 0; i < 8; ++i) v[i] = c[8 * t + i];
+        rounded = __builtin_convertvector(v, frag<T>);
+        if (FINE) rest = __builtin_convertvector(v - __builtin_convertvector(rounded, f32x8), frag<T>);
+    }
+};
+
+template <typename T, bool FINE>
+__device__ __forceinline__ f32x16 mfma(frag<T> a, const Operand<T, FINE>& b, f32x16 c) {
+    if (FINE) c = mfma(a, b.rest, c);
+    return mfma(a, b.rounded, c);
 }
 
 // Probabilities are operands of the second products in the tensors' type.  bf16 has the exponents of fp32; fp16 ends
@@ -311,6 +323,7 @@ struct AttentionPlan {
     uint32_t forward_parts, query_parts, key_parts;
     uint64_t forward_groups, query_groups, key_groups;      // workgroups of each kernel
     bool packed;                                    // forward: see its kernel
+    bool fine;                                      // second products from both parts of their operands
     size_t rows_at;                                 // backward: two numbers of every row
     size_t dq_at, dkv_at;                           // backward: partial sums
     size_t forward_bytes, bytes;                    // of the workspace, forward and backward

@@ -31,7 +31,7 @@ static_assert(BWD_QUERIES == BWD_THREADS / WAVE * 32, "a wave owns 32 queries");
 // sees nothing, whose probabilities come out as 0), less what that kernel raises probabilities by, and D / c by as much lower.
 typedef float2 RowNumbers;
 
-template <typename T, int DIM, bool DROP>
+template <typename T, int DIM, bool DROP, bool FINE>
 __global__ __launch_bounds__(BWD_THREADS, 2) void attention_backward_queries_kernel(
     AttentionArgs a, const T* q, const T* k, const T* v, const T* o, const float* lse, const T* d_o, T* dq, RowNumbers* rows,
     Places all, uint32_t parts, Divider by_part, float* partial) {
@@ -136,7 +136,7 @@ __global__ __launch_bounds__(BWD_THREADS, 2) void attention_backward_queries_ker
                 for (int r = 0; r < 16; ++r) s[r] *= dp[r] - sum;
 #pragma unroll
                 for (int t = 0; t < 2; ++t) {
-                    const frag<T> ds = to_operand<T>(s, t);
+                    const Operand<T, FINE> ds(s, t);
 #pragma unroll
                     for (int d = 0; d < DIM / 32; ++d) acc[d] = mfma(Tile::columns(kt, reads, 32 * n, d, t), ds, acc[d]);
                 }
@@ -156,7 +156,7 @@ __global__ __launch_bounds__(BWD_THREADS, 2) void attention_backward_queries_ker
     }
 }
 
-template <typename T, int DIM, bool DROP>
+template <typename T, int DIM, bool DROP, bool FINE>
 __global__ __launch_bounds__(BWD_THREADS, DIM == 64 ? 2 : 1) void attention_backward_keys_kernel(
     AttentionArgs a, const T* q, const T* k, const T* v, const T* d_o, const RowNumbers* rows, T* dk, T* dv, Places all,
     uint32_t parts, Divider by_part, float* partial) {
@@ -278,7 +278,7 @@ __global__ __launch_bounds__(BWD_THREADS, DIM == 64 ? 2 : 1) void attention_back
                     }
 #pragma unroll
                     for (int t = 0; t < 2; ++t) {
-                        const frag<T> p = to_operand<T>(s, t), ds = to_operand<T>(dp, t);
+                        const Operand<T, FINE> p(s, t), ds(dp, t);
 #pragma unroll
                         for (int d = 0; d < DIM / 32; ++d) {
                             dvacc[d] = mfma(Tile::columns(dt, reads, slot0, d, t), p, dvacc[d]);
@@ -350,7 +350,7 @@ __global__ __launch_bounds__(BWD_THREADS) void attention_add_kernel(Sums sums, u
 
 struct BackwardPointers { const void *q, *k, *v, *o, *d_o; const float* lse; void *dq, *dk, *dv; char* ws; };
 
-template <typename T, int DIM, bool DROP>
+template <typename T, int DIM, bool DROP, bool FINE>
 static int launch_backward(const AttentionArgs& a, const AttentionPlan& plan, const BackwardPointers& p, hipStream_t s) {
     RowNumbers* rows = (RowNumbers*)(p.ws + plan.rows_at);
     float *dq_sums = (float*)(p.ws + plan.dq_at), *dkv_sums = (float*)(p.ws + plan.dkv_at);
@@ -358,7 +358,7 @@ static int launch_backward(const AttentionArgs& a, const AttentionPlan& plan, co
     uint32_t n = 0;
     if (a.q_len) {
         const uint32_t blocks = (a.q_len + BWD_QUERIES - 1) / BWD_QUERIES, parts = plan.query_parts;
-        hipLaunchKernelGGL((attention_backward_queries_kernel<T, DIM, DROP>), dim3((unsigned)plan.query_groups),
+        hipLaunchKernelGGL((attention_backward_queries_kernel<T, DIM, DROP, FINE>), dim3((unsigned)plan.query_groups),
                            dim3(BWD_THREADS), 0, s, a, (const T*)p.q, (const T*)p.k, (const T*)p.v, (const T*)p.o, p.lse,
                            (const T*)p.d_o, (T*)p.dq, rows,
                            places(a.batch * a.kv_heads, a.group, blocks * parts, window_of(a.causal, a.k_len, DIM, a.group)), parts,
@@ -371,7 +371,7 @@ static int launch_backward(const AttentionArgs& a, const AttentionPlan& plan, co
         const uint32_t blocks = (a.k_len + KEYS - 1) / KEYS, parts = plan.key_parts;
         const uint64_t keys = (uint64_t)a.batch * a.kv_heads * a.k_len;
         timing_before(s);
-        hipLaunchKernelGGL((attention_backward_keys_kernel<T, DIM, DROP>), dim3((unsigned)plan.key_groups),
+        hipLaunchKernelGGL((attention_backward_keys_kernel<T, DIM, DROP, FINE>), dim3((unsigned)plan.key_groups),
                            dim3(BWD_THREADS), 0, s, a, (const T*)p.q, (const T*)p.k, (const T*)p.v, (const T*)p.d_o,
                            (const RowNumbers*)rows, (T*)p.dk, (T*)p.dv, 
                            places(a.batch * a.kv_heads, 1, blocks * parts, window_of(a.causal, a.q_len, DIM, 1)), parts, divider(parts),
@@ -392,11 +392,16 @@ static int launch_backward(const AttentionArgs& a, const AttentionPlan& plan, co
     return launch_status();
 }
 
+template <typename T, bool FINE>
+static int launch_backward_columns(const AttentionArgs& a, const AttentionPlan& plan, const BackwardPointers& p, hipStream_t s) {
+    const bool drop = a.drop.bar != 65536u;
+    if (plan.dim == 64) return drop ? launch_backward<T, 64, true, FINE>(a, plan, p, s) : launch_backward<T, 64, false, FINE>(a, plan, p, s);
+    return drop ? launch_backward<T, 128, true, FINE>(a, plan, p, s) : launch_backward<T, 128, false, FINE>(a, plan, p, s);
+}
+
 template <typename T>
 static int launch_backward_shape(const AttentionArgs& a, const AttentionPlan& plan, const BackwardPointers& p, hipStream_t s) {
-    const bool drop = a.drop.bar != 65536u;
-    if (plan.dim == 64) return drop ? launch_backward<T, 64, true>(a, plan, p, s) : launch_backward<T, 64, false>(a, plan, p, s);
-    return drop ? launch_backward<T, 128, true>(a, plan, p, s) : launch_backward<T, 128, false>(a, plan, p, s);
+    return plan.fine ? launch_backward_columns<T, true>(a, plan, p, s) : launch_backward_columns<T, false>(a, plan, p, s);
 }
 
 }  // namespace okt

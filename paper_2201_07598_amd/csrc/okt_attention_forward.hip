@@ -42,7 +42,7 @@ __device__ __forceinline__ float sum_sixteen(const f32x16& v) {
 
 // PACKED: few queries, whose rows of all heads of a group are taken one after the other as the
 // rows of one block, so that the group's keys come by once and not once a head.
-template <typename T, int DIM, bool DROP, bool PACKED>
+template <typename T, int DIM, bool DROP, bool PACKED, bool FINE>
 __global__ __launch_bounds__(FWD_THREADS, 2) void attention_forward_kernel(AttentionArgs a, const T* q, const T* k, const T* v,
                                                                            T* o, float* lse, Places all, uint32_t parts,
                                                                            Divider by_part, Divider by_query,
@@ -152,7 +152,7 @@ __global__ __launch_bounds__(FWD_THREADS, 2) void attention_forward_kernel(Atten
                 }
 #pragma unroll
                 for (int t = 0; t < 2; ++t) {
-                    const frag<T> p = to_operand<T>(s[n], t);
+                    const Operand<T, FINE> p(s[n], t);
 #pragma unroll
                     for (int d = 0; d < DIM / 32; ++d) acc[d] = mfma(Tile::columns(vt, reads, 32 * n, d, t), p, acc[d]);
                 }
@@ -218,7 +218,7 @@ __global__ __launch_bounds__(FWD_THREADS) void attention_join_kernel(AttentionAr
     if (lse && d == 0) lse[row] = any ? (most + __builtin_amdgcn_logf(total)) * 0.693147180559945f : -INFINITY;
 }
 
-template <typename T, int DIM>
+template <typename T, int DIM, bool FINE>
 static int launch_forward(const AttentionArgs& a, const AttentionPlan& plan, const void* q, const void* k, const void* v, void* o,
                            float* lse, void* ws, hipStream_t s) {
     const uint64_t rows = (uint64_t)a.batch * a.heads * a.q_len;
@@ -226,9 +226,9 @@ static int launch_forward(const AttentionArgs& a, const AttentionPlan& plan, con
     const uint32_t blocks = (block_rows + FWD_QUERIES - 1) / FWD_QUERIES, parts = plan.forward_parts;
     float* partial = (float*)ws;
     float2* sums = (float2*)(partial + parts * rows * DIM);
-    auto* kernel = a.drop.bar != 65536u ? attention_forward_kernel<T, DIM, true, false>
-                   : plan.packed        ? attention_forward_kernel<T, DIM, false, true>
-                                        : attention_forward_kernel<T, DIM, false, false>;
+    auto* kernel = a.drop.bar != 65536u ? attention_forward_kernel<T, DIM, true, false, FINE>
+                   : plan.packed        ? attention_forward_kernel<T, DIM, false, true, FINE>
+                                        : attention_forward_kernel<T, DIM, false, false, FINE>;
     timing_before(s);
     hipLaunchKernelGGL(kernel, dim3((unsigned)plan.forward_groups), dim3(FWD_THREADS), 0, s, a, (const T*)q,
                        (const T*)k, (const T*)v, (T*)o, lse,
@@ -243,6 +243,21 @@ static int launch_forward(const AttentionArgs& a, const AttentionPlan& plan, con
     }
     return status;
 }
+
+template <typename T>
+static int launch_forward_shape(const AttentionArgs& a, const AttentionPlan& plan, const void* q, const void* k, const void* v, void* o,
+                                float* lse, void* ws, hipStream_t s) {
+    auto* launch = plan.dim == 64 ? (plan.fine ? launch_forward<T, 64, true> : launch_forward<T, 64, false>)
+                                  : (plan.fine ? launch_forward<T, 128, true> : launch_forward<T, 128, false>);
+    return launch(a, plan, q, k, v, o, lse, ws, s);
+}
+
+// Up to so many pairs the second products are taken from p and ds in two parts.  An output of few pairs has its error
+// from few roundings: in one part, the error against 64 bits of 2 to 50 queries and keys was up to 2.0 times that of
+// outputs rounded once (2 % of 500 drawn sizes over 1.5 times), and from 2^16 pairs on 1.4 to 1.48 times.  In two parts
+// everywhere it would be 1.0 to 1.1 times, and 32 x 16 x 512 x 64 56 -> 67 us, 2 x 16 x 4096 x 128 148 -> 204, their
+// gradients 145 -> 174 and 533 -> 678.  Below the bound it costs up to 1 us (2 x 2 x 128 x 128 x 64 gradient 19 -> 20.5).
+constexpr uint64_t FINE_PAIRS = 1ull << 16;
 
 AttentionPlan attention_plan(uint32_t batch, uint32_t heads, uint32_t kv_heads, uint32_t q_len, uint32_t k_len, uint32_t head_dim,
                              bool drop) {
@@ -265,6 +280,7 @@ AttentionPlan attention_plan(uint32_t batch, uint32_t heads, uint32_t kv_heads, 
     // 128 195 us, each head on its own 415; of 33 queries (8 x 8 groups) 55 and 70.
     p.packed = !drop && group > 1 && 2 * q_len <= ATTENTION_QUERIES;
     const uint64_t forward_blocks = p.packed ? (group * q_len + ATTENTION_QUERIES - 1) / ATTENTION_QUERIES * units : query_blocks;
+    p.fine = rows <= FINE_PAIRS / (k_len ? k_len : 1);
     p.forward_parts = worth(forward_blocks, key_steps, 12, rows * (row_bytes + 8), false);
     p.key_parts = key_parts(false);
     p.query_parts = worth(query_blocks, key_steps, 17, rows * row_bytes, p.key_parts > 1);
@@ -354,12 +370,8 @@ int okt_attention_forward(const okt_attention* op, const void* d_q, const void* 
     for (const void* in : {d_q, a.k_len ? d_k : nullptr, a.k_len ? d_v : nullptr})
         if (same_place(d_o_out, in, a.head_dim)) return OKT_ERR_INVALID_ARG;
     const hipStream_t s = (hipStream_t)stream;
-    const bool narrow = plan.dim == 64;
-    if (op->dtype == OKT_BF16)
-        return narrow ? launch_forward<__bf16, 64>(a, plan, d_q, d_k, d_v, d_o_out, d_lse_out, d_ws, s)
-                      : launch_forward<__bf16, 128>(a, plan, d_q, d_k, d_v, d_o_out, d_lse_out, d_ws, s);
-    return narrow ? launch_forward<_Float16, 64>(a, plan, d_q, d_k, d_v, d_o_out, d_lse_out, d_ws, s)
-                  : launch_forward<_Float16, 128>(a, plan, d_q, d_k, d_v, d_o_out, d_lse_out, d_ws, s);
+    return op->dtype == OKT_BF16 ? launch_forward_shape<__bf16>(a, plan, d_q, d_k, d_v, d_o_out, d_lse_out, d_ws, s)
+                                 : launch_forward_shape<_Float16>(a, plan, d_q, d_k, d_v, d_o_out, d_lse_out, d_ws, s);
 }
 
 }  // extern "C"

@@ -336,3 +336,27 @@ def test_many_tiles_a_workgroup(D, causal, kind, p):
     q, k, v, do = make(5, 8, 2, 900, 900, D, kind)
     check(q, k, v, do, kind, causal=causal, p=p)
     check(q, k, v, do, kind, causal=causal, p=p, lens=lens)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f16"])
+@pytest.mark.parametrize("p", [0.0, 0.1])
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("B,H,G,Sq,Sk,D", [(4, 6, 6, 2, 2, 128), (3, 2, 2, 6, 6, 64), (5, 4, 2, 1, 45, 64), (1, 8, 4, 10, 44, 128),
+                                           (2, 13, 13, 27, 27, 16), (1, 2, 1, 180, 180, 64), (1, 4, 4, 2, 5000, 40), (1, 2, 2, 3000, 7, 128)])
+def test_few_pairs_are_rounded_once(monkeypatch, B, H, G, Sq, Sk, D, causal, p, kind):
+    """Up to 2^16 pairs p and ds go into the products in two parts: what is left of their rounding is twice the square of
+    one, and the outputs are off by little more than their own."""
+    q, k, v, do = make(B, H, G, Sq, Sk, D, kind)
+    options = dict(causal=causal, dropout_p=p, site=2, seed=seed_tensor(SEED) if p else None)
+    plain = dict(causal=causal, scale=D ** -0.5, q_lens=None, k_lens=None, dropout_p=p, seed=SEED & ((1 << 64) - 1), site=2)
+    Q, KK, V, DO = (wide(t) for t in (q, k, v, do))
+    u, least = UNIT[kind], step(kind)
+    o, lse = forward(q, k, v, **options)
+    want_o, _ = ops.attention(Q, KK, V, **plain)
+    got, want = backward(q, k, v, o, lse, do, **options), ops.attention_backward(Q, KK, V, DO, **plain)
+    monkeypatch.setitem(UNIT, kind, 2 * u * u)
+    bo, _ = attention_bounds(Q, KK, V, kind, **plain)
+    stored = bo * (1 + u) + u * np.abs(want_o) + least
+    within(o, want_o, stored, "o")
+    for name, g, w, b in zip(("dq", "dk", "dv"), got, want, attention_bounds(Q, KK, V, kind, do=DO, o=stored, **plain)):
+        within(g, w, b * (1 + u) + u * np.abs(w) + least, name)
