@@ -13,12 +13,17 @@
 // With dropout, scaled by c = 65536 / bar where kept:  ds = p (c kept(dp) - D) = c p (kept(dp) - D / c)
 // and dv = c sum kept(p) do, so c is applied once at the end, not to every pair.
 //
-// Of 64 columns both kernels are bound by the vector units, as the forward pass is; of 128 the queries'
-// is bound by the matrix units (63 % of the time), and the keys', whose sums and operands take
-// more than half of the registers, runs one wave a SIMD and waits on its own chain (36 %).  From call to call:
-//   32 x 16 heads x 512 x 64, lengths up to 512, bf16, p = 0.1  138-148 us (queries 61, keys 80)
-//   2 x 16 heads (4 key heads) x 4096 x 128, causal, bf16       515-535 us, 650 TFLOP/s of visible pairs (194, 345)
-//   3 x 6 heads (2 key heads) x 197 x 333 x 40, fp16, causal    22-24 us: three dependent launches
+// p and ds are rounded for the second products as in the forward pass; D comes from o as it was stored, whose rounding is
+// small beside dP wherever more than a few keys share a row (a row of at most 32 takes it from what it has in registers).
+//
+// Of 64 columns the vector units are the busiest part (queries 47 %, keys 38 % of all cycles in a padded batch with dropout,
+// 34 and 26 without, the matrix units 17 to 21), and no unit is a bound: CUs are empty for a fifth to a quarter of
+// the time, and the keys' kernel has 1.8 waves a SIMD to hide its chain.  Of 128 the queries' is bound by the matrix
+// units (63 % of a busy CU's time), and the keys', whose sums and operands take more than half of the registers, runs one
+// wave a SIMD and waits on its own chain (36 %).  From call to call:
+//   32 x 16 heads x 512 x 64, lengths up to 512, bf16, p = 0.1  138-149 us (queries 61, keys 80)
+//   2 x 16 heads (4 key heads) x 4096 x 128, causal, bf16       515-535 us, 650 TFLOP/s of visible pairs (200, 360 in a trace)
+//   3 x 6 heads (2 key heads) x 197 x 333 x 40, fp16, causal    21-24 us: three dependent launches, 12.6 us of the host
 #include "okt_attention.h"
 
 namespace okt {

@@ -6,14 +6,15 @@
 // scores, so maximum and sum stay in the lane but for one exchange with the lane 32 away,
 // and the probabilities are the second product's operand as they lie.
 //
-// With 64 columns or fewer the kernel is bound by the vector units, not the matrix units: a score
-// takes a maximum, a multiply-add, an exponential (at half the others' rate), an addition and half a
-// conversion, 22 cycles of a SIMD for 64 of them against 16 of its two products, and dropout as much again.  From call to call:
-//   32 x 16 heads x 512 x 64, lengths up to 512, bf16, p = 0.1  49-56 us (p = 0: 42)
-//   2 x 16 heads (4 key heads) x 4096 x 128, causal, bf16       140-147 us, 960 TFLOP/s of visible pairs
-//   12 heads x 128 x 64                                         9 us: latency of a launch and two tiles
-//   one query of 12 heads over 32768 keys of 128                53 us, 3.8 TB/s
-//   64 x 8 groups of 4 heads of one query, 4096 keys of 128     195 us, 5.5 TB/s
+// With 64 columns or fewer the vector units have more to do than the matrix units: 64 scores take 35 cycles of a SIMD
+// there (60 with dropout, as counted) against 16 of their two products.  In a padded batch of short sequences that work
+// fills 38 % of all cycles (49 with dropout); a third of the CUs' time they have no workgroup, before the first tiles
+// and behind the longest sequences, and the rest is waiting.  From call to call:
+//   32 x 16 heads x 512 x 64, lengths up to 512, bf16, p = 0.1  49-56 us (p = 0: 42; the kernels 51 and 35 in a trace)
+//   2 x 16 heads (4 key heads) x 4096 x 128, causal, bf16       145-150 us, 940 TFLOP/s of visible pairs (fp16 167)
+//   12 heads x 128 x 64                                         8-10 us, most of it the host's; the kernel 6, two tiles
+//   one query of 12 heads over 32768 keys of 128                53-58 us, 3.6 TB/s
+//   64 x 8 groups of 4 heads of one query, 4096 keys of 128     193 us, 5.6 TB/s
 #include "okt_attention.h"
 
 namespace okt {
@@ -270,7 +271,9 @@ AttentionPlan attention_plan(uint32_t batch, uint32_t heads, uint32_t kv_heads, 
     const uint64_t key_steps = (k_len + ATTENTION_KEYS - 1) / ATTENTION_KEYS;
     const uint64_t rows = planes * q_len, keys = units * k_len;
     const uint64_t query_steps = (q_len + query_tile - 1) / query_tile * group, row_bytes = p.dim * sizeof(float);
-    // what a step takes, fitted to 128 queries and 512 to 2048 keys: 0.75, 1.05 and 1.35 us of 64 columns
+    // What a step takes: 0.77, 1.09 and 1.34 us of 64 columns and twice that of 128 (forward, queries, keys).  Where a few
+    // workgroups run alone it is 0.7, 0.9 and 1.4 us, and 1.0, 1.4 and 2.0 of 128 columns; with one on every CU, which share
+    // the memory, 1.1, 1.4 and 2.0, and 2.1, 2.3 and 6.
     const auto worth = [&](uint64_t workgroups, uint64_t steps, uint64_t step_ns, uint64_t bytes, bool added) {
         return parts_worth(parts_for(workgroups, steps, 1), steps, step_ns * p.dim, 2 * bytes, added ? 0 : PART_LAUNCH_NS);
     };

@@ -20,13 +20,15 @@
 // adds in a fixed order (no atomics: the result does not change from run to run).
 // Bound by memory: forward 4 elements a place, backward 5 or 6.  From call to call:
 //   forward   16384 x 1024 bf16   29 us, 4.6 TB/s of 134 MB (the kernel 25)
-//             128 x 768 fp32      9 us: a launch and one chain of load, two sums and store
+//             128 x 768 fp32      8-10 us, 8.0 of which are the host's; the kernel 4.8
+//             16384 x 1024 bf16, both norms, 32 gates and dropout 41 us; RMS, one gate, no dropout 34.5
 //   backward  16384 x 1024 bf16   38 us, 4.4 TB/s of 168 MB (the kernel 28, the add 4 and the step between them)
 //             4099 x 2500 fp16, both norms and a gate
-//                                 51 us, 2.4 TB/s of 123 MB (the kernel 45, the add 6).  Of that 17 us are
+//                                 53 us, 2.3 TB/s of 123 MB (the kernel 46, the add 6).  Of that 17 us are
 //             there with one row a workgroup, too: two launches, the parameters on the way in, their
 //             gradients on the way out; and rows of 5000 bytes begin and end inside a line of the
-//             caches (16384 rows of 2500 133 us, of 2504 120)
+//             caches (16384 rows of 2500 133-140 us, of 2504 120).  16384 x 768 50, 16384 x 1024 55, 8192 x 4096 99,
+//             2048 x 8192 71 (no biases): rows of two groups a thread, one workgroup a CU, whose sums are in LDS
 #include "okt_element.h"
 #include "okt_random.h"
 
