@@ -24,7 +24,7 @@
 //             16384 x 1024 bf16, both norms, 32 gates and dropout 41 us; RMS, one gate, no dropout 34.5
 //   backward  16384 x 1024 bf16   38 us, 4.4 TB/s of 168 MB (the kernel 28, the add 4 and the step between them)
 //             4099 x 2500 fp16, both norms and a gate
-//                                 53 us, 2.3 TB/s of 123 MB (the kernel 46, the add 6).  Of that 17 us are
+//                                 52 us, 2.4 TB/s of 123 MB (the kernel 45, the add 6).  Of that 17 us are
 //             there with one row a workgroup, too: two launches, the parameters on the way in, their
 //             gradients on the way out; and rows of 5000 bytes begin and end inside a line of the
 //             caches (16384 rows of 2500 133-140 us, of 2504 120).  16384 x 768 50, 16384 x 1024 55, 8192 x 4096 99,
@@ -387,8 +387,8 @@ __device__ __forceinline__ void put_sums(const S& sums, const Columns<L>& cols, 
 }
 
 // ALL: with a norm after the block or a gate; BIAS: a norm has one.  Without, the registers
-// they take are free.
-template <typename T, typename L, bool ALL, bool BIAS>
+// they take are free.  DROP (of ALL): something may be dropped.
+template <typename T, typename L, bool ALL, bool BIAS, bool DROP>
 __global__ __launch_bounds__(L::threads) void norm_backward_kernel(
     NormArgs a, const T* u, const T* h, const T* dh, const T* dy, T* dx, T* du) {
     constexpr int AT_ONCE = L::one ? L::threads / WAVE : 1;
@@ -478,9 +478,11 @@ __global__ __launch_bounds__(L::threads) void norm_backward_kernel(
                         // d holds the mask and its scale already.  Where it is 0, as at every place that is
                         // dropped, the place adds 0: 0 times a value that is not finite would stay in the gate's sum.
                         // (A branch, and the mask's own words, take 7 to 12 registers more, with which a CU holds one
-                        // workgroup of 4099 x 2500 where it holds two; so it costs 1 us of 54.)
+                        // workgroup of 4099 x 2500 where it holds two; so it costs 1 us of 57.)
+                        if (DROP) {
 #pragma unroll
-                        for (int j = 0; j < 8; ++j) s[j] = d[i][j] != 0.0f ? s[j] : 0.0f;
+                            for (int j = 0; j < 8; ++j) s[j] = d[i][j] != 0.0f ? s[j] : 0.0f;
+                        }
                         dgate.add(i, d[i], s);
                         d[i] *= g[i];
                     }
@@ -605,10 +607,12 @@ static void launch_norm(const NormArgs& a, const NormPointers& p, bool backward,
         hipLaunchKernelGGL((norm_forward_kernel<T, L>), grid, block, 0, s, a, (const T*)p.u, (const T*)p.x, (T*)p.out_h, (T*)p.out_y);
         return;
     }
-    const bool bias = a.post_b || a.pre_b;
-    auto* kernel = bias ? norm_backward_kernel<T, L, false, true> : norm_backward_kernel<T, L, false, false>;
+    const bool bias = a.post_b || a.pre_b, drop = a.drop.bar != 65536u;
+    auto* kernel = bias ? norm_backward_kernel<T, L, false, true, false> : norm_backward_kernel<T, L, false, false, false>;
     if constexpr (!(L::one && L::vecs == 2 && sizeof(T) == 4)) {           // norm_shape gives such a row another layout
-        if (a.post_w || a.gate) kernel = bias ? norm_backward_kernel<T, L, true, true> : norm_backward_kernel<T, L, true, false>;
+        if (a.post_w || a.gate)
+            kernel = drop ? (bias ? norm_backward_kernel<T, L, true, true, true> : norm_backward_kernel<T, L, true, false, true>)
+                          : (bias ? norm_backward_kernel<T, L, true, true, false> : norm_backward_kernel<T, L, true, false, false>);
     }
     hipLaunchKernelGGL(kernel, grid, block, 0, s, a, (const T*)p.u, (const T*)p.h, (const T*)p.dh, (const T*)p.dy, (T*)p.dx, (T*)p.du);
 }

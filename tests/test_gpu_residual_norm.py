@@ -300,3 +300,16 @@ def test_both_outputs_in_the_place_of_inputs(width):
         h, y = (b.u, b.x) if swap else (b.x, b.u)
         okt.okt_residual_norm_forward(b.u, b.x, h, y, b.stats, **b.options)
         assert torch.equal(a.h, h) and torch.equal(a.y, y) and torch.equal(a.stats, b.stats)
+
+
+@pytest.mark.parametrize("width,gates", [(100, 1), (2500, 3)])
+def test_nothing_is_hidden_from_the_gradient_of_a_gate_where_nothing_is_dropped(width, gates):
+    """Without dropout a place with an infinite u and a gradient of 0 makes its gate's gradient NaN, as the formula does."""
+    c = Case(90, width, "bf16", pre=False, gates=gates)
+    c.u = c.u.clone()
+    c.u[7, 5] = float("inf")
+    c.dh = c.dh.clone()
+    c.dh[7, 5] = 0.0
+    c.backward()
+    nan = torch.isnan(c.grads["dgate"])
+    assert bool(nan[0, 5]) and int(nan.sum()) == 1
