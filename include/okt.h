@@ -634,7 +634,8 @@ int okt_residual_norm_backward(const okt_residual_norm* op, const void* d_u, con
  * dv and dk summed over the query heads of a group.  Products are taken by the matrix
  * units from 16-bit inputs with fp32 sums; p and ds are rounded to the tensors' type for the
  * second product of each pass (up to batch * heads * q_len * k_len = 2^16 pairs, where the rounding of one would show,
- * into two parts, of 16 bits in bf16 and 22 in fp16).  In fp16 a p below 2^-32 of its row's largest (for dv: below
+ * into two parts, of 16 bits in bf16 and 22 in fp16).  D_i is taken from o as it was stored, in a row of up to 32 keys
+ * from its p and dpd.  In fp16 a p below 2^-32 of its row's largest (for dv: below
  * 2^-37) and a ds below 2^-25 are rounded to 0.  The sum of a row's p is compensated, so lse is good to a few roundings at any
  * length; the other sums are plain fp32: over values that are all alike, o is off by 2^-10 at 2^20 keys and by 2^-9 at 2^22.
  * A tensor is [batch][length][heads][head_dim] by strides {batch, length, heads} in elements,
@@ -667,7 +668,8 @@ size_t okt_attention_workspace_bytes(uint32_t batch, uint32_t heads, uint32_t kv
  *   d_o_out    out  written as a whole (past the lengths with zeros), overlaps no input
  *   d_lse_out  out  fp32[batch][heads][q_len], contiguous; NULL if no backward pass follows
  * One launch; a second where few queries stand against many keys, which are then dealt to several
- * workgroups whose sums it joins (only then is the workspace used).
+ * workgroups whose sums it joins (only then is the workspace used).  Without dropout the queries of a group's heads
+ * share a workgroup, and its keys come by once, where at least two heads' fit 128 rows; with dropout every head has its own.
  */
 int okt_attention_forward(const okt_attention* op, const void* d_q, const void* d_k, const void* d_v,
                           void* d_o_out, float* d_lse_out, void* d_ws, size_t ws_bytes, void* stream);
