@@ -255,7 +255,7 @@ static int launch_forward_shape(const AttentionArgs& a, const AttentionPlan& pla
 
 // Up to so many pairs the second products are taken from p and ds in two parts.  An output of few pairs has its error
 // from few roundings: in one part, the error against 64 bits of 2 to 50 queries and keys was up to 2.0 times that of
-// outputs rounded once (2 % of 500 drawn sizes over 1.5 times), and from 2^16 pairs on 1.4 to 1.48 times.  In two parts
+// outputs rounded once (2 % of 500 drawn sizes over 1.5 times), and from 2^16 pairs on 1.4 to 1.49 times (of 1,280 drawn sizes).  In two parts
 // everywhere it would be 1.0 to 1.1 times, and 32 x 16 x 512 x 64 56 -> 67 us, 2 x 16 x 4096 x 128 148 -> 204, their
 // gradients 145 -> 174 and 533 -> 678.  Below the bound it costs up to 1 us (2 x 2 x 128 x 128 x 64 gradient 19 -> 20.5).
 constexpr uint64_t FINE_PAIRS = 1ull << 16;
