@@ -683,6 +683,74 @@ int okt_attention_backward(const okt_attention* op, const void* d_q, const void*
                            const void* d_o, const float* d_lse, const void* d_do, void* d_dq_out,
                            void* d_dk_out, void* d_dv_out, void* d_ws, size_t ws_bytes, void* stream);
 
+/*
+ * AdamW over many tensors in one launch, states in 32 bits or in 8.  For an element p with gradient g, averages m and v and
+ * t = the step, counted from 1:
+ *   g = grad_scale g,  m = beta1 m + (1 - beta1) g,  v = beta2 v + (1 - beta2) g^2,  rate = lr rate_scale
+ *   p = (1 - rate weight_decay) p - rate / (1 - beta1^t) m / (sqrt(v) / sqrt(1 - beta2^t) + eps)
+ * in fp32, 1 - beta^t in fp64.  Parameters and gradients are fp32, bf16 or fp16; a 16-bit parameter is
+ * rounded to nearest, and a tensor may have a copy in 16 bits that is written along (rounded from fp32, too), which the
+ * products of the next step read.  The averages are fp32 (OKT_STATE_F32), or both OKT_STATE_E4M3: a block is OKT_ADAMW_BLOCK elements from the tensor's
+ * first on (the last one may be shorter), its scale the power of two, at least 2^-126, by which its largest magnitude lies above 224 and
+ * at most at 448, and the codes are e4m3 (no infinities, largest value 448):
+ *   m = scale_m code_m,  v = (scale_v code_v)^2
+ * all zero codes, with any finite scales, are averages of zero.  A magnitude y between neighbouring values a < b of e4m3 becomes one of them by the
+ * 16-bit value r of the random field (okt_dropout), 2^15 without d_seed: m becomes b where frac + r / 2^16 >= 1 with
+ * frac = (y - a) / (b - a) to 20 bits, so its expectation is y and 2^15 rounds to nearest; the root becomes b where y^2 - a^2 >
+ * r / 2^16 (b^2 - a^2), so the expectation of its square is y^2.  A v above 0 never becomes 0.  Element e of tensor i of the plan:
+ * c0 = (e / 4) mod 2^32, c1 = (e / 4) >> 32, c2 = i; value e % 4 for m, 4 + e % 4 for v.
+ * Rounded to nearest, an average moves only where a step changes it by half a code; give a seed.  A block with a NaN or an infinity
+ * has the scale NaN and codes 0: all of it is NaN from then on.
+ */
+#define OKT_ADAMW_BLOCK 256
+typedef enum okt_adamw_state { OKT_STATE_F32 = 0, OKT_STATE_E4M3 = 1 } okt_adamw_state;
+
+/* One tensor: contiguous device memory at the alignment of an element.  Nothing that is written may overlap
+ * anything else of any tensor; gradients may be shared.  With n = 0 the pointers may be NULL. */
+typedef struct okt_adamw_tensor {
+    void* d_param;
+    const void* d_grad;
+    void* d_m;
+    void* d_v;
+    void* d_copy;                 /* NULL: none */
+    float* d_m_scale;             /* fp32[ceil(n / OKT_ADAMW_BLOCK)]; exactly with OKT_STATE_E4M3 */
+    float* d_v_scale;
+    uint64_t n;
+    double weight_decay;          /* >= 0 */
+    double rate_scale;            /* >= 0; of this tensor's learning rate, usually 1 */
+    int32_t param_dtype, grad_dtype;
+    int32_t copy_dtype;           /* OKT_BF16 or OKT_F16 */
+    int32_t reserved;             /* 0 */
+} okt_adamw_tensor;
+
+/* Bytes of the plan for such tensors; 0 if their lengths are out of range (together below 2^36 elements).  HOST arithmetic. */
+size_t okt_adamw_plan_bytes(const okt_adamw_tensor* h_tensors, uint32_t count);
+
+/*
+ * Checks the tensors and writes their plan to HOST memory (8-byte aligned, plan_bytes of it); the caller copies it to the device
+ * (16-byte aligned) and keeps it there as long as the tensors stay where they are.  No GPU.
+ *   h_chunks_out  out  what okt_adamw.chunks has to be
+ */
+int okt_adamw_plan(const okt_adamw_tensor* h_tensors, uint32_t count, int state, void* h_plan_out, size_t plan_bytes,
+                   uint32_t* h_chunks_out);
+
+typedef struct okt_adamw {
+    uint32_t tensors, chunks;     /* of the plan */
+    int32_t state;                /* okt_adamw_state of the plan */
+    uint32_t site;
+    double lr;                    /* finite; not looked at with d_lr */
+    double beta1, beta2;          /* 0 <= beta < 1 */
+    double eps;                   /* >= 0 */
+    const int64_t* d_step;        /* int64[1] on the device: t; below 1 is taken as 1 */
+    const float* d_lr;            /* fp32[1] on the device, or NULL */
+    const float* d_grad_scale;    /* fp32[1] on the device, or NULL for 1 */
+    const float* d_skip;          /* fp32[1] on the device, or NULL: where it is not 0 (or is NaN) the call changes nothing */
+    const uint64_t* d_seed;       /* uint64[1] on the device, or NULL; looked at with OKT_STATE_E4M3 */
+} okt_adamw;
+
+/* One launch.  Everything that changes from step to step is read from device memory, so a captured step can be replayed. */
+int okt_adamw_step(const okt_adamw* op, const void* d_plan, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -1,0 +1,107 @@
+"""Plain CPU oracle of the operators at the ends of a training step, in 64 bits, written from the formulas in
+include/okt.h: AdamW and its 8-bit averages.  numpy only, no thought of speed; shares
+nothing with the GPU path."""
+from __future__ import annotations
+
+import numpy as np
+
+from oracle.okt_operators import philox, values
+
+# ------------------------------------------------------------------ AdamW
+
+BLOCK = 256
+
+
+def adamw(p, g, m, v, *, step, lr, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.0, rate_scale=1.0, grad_scale=1.0):
+    """(p, m, v) after a step, of arrays in 64 bits."""
+    t, rate = max(int(step), 1), lr * rate_scale
+    g = grad_scale * g
+    m = beta1 * m + (1.0 - beta1) * g
+    v = beta2 * v + (1.0 - beta2) * g * g
+    with np.errstate(divide="ignore", invalid="ignore"):
+        change = m / (1.0 - beta1 ** t) / (np.sqrt(v / (1.0 - beta2 ** t)) + eps)
+    return p - rate * weight_decay * p - rate * change, m, v
+
+
+def averages32(g, m, v, beta1, beta2, grad_scale=1.0):
+    """The averages as fp32 arithmetic has them, each operation rounded: what 8-bit codes are made of."""
+    f = np.float32
+    g = g.astype(f) * f(grad_scale)
+    with np.errstate(over="ignore", invalid="ignore"):
+        return f(beta1) * m + f(1.0 - beta1) * g, f(beta2) * v + f(1.0 - beta2) * g * g
+
+
+def e4m3_values():
+    """The 127 values from 0 to 448: four bits of exponent, three of mantissa, the last code is no number."""
+    code = np.arange(127)
+    e, f = code // 8, code % 8
+    return np.where(e == 0, f * 2.0 ** -9, (1.0 + f / 8.0) * 2.0 ** (e - 7.0))
+
+
+def element_halves(n, tensor, seed, site=0):
+    """The 16-bit values of n elements for m and for v; the middle without a seed."""
+    if seed is None:
+        return np.full(n, 0x8000), np.full(n, 0x8000)
+    four = np.arange(-(-n // 4), dtype=np.uint64)
+    r = values(philox(four & np.uint64(0xFFFFFFFF), four >> np.uint64(32), tensor, site, seed)).astype(np.int64)
+    return r[:, :4].reshape(-1)[:n], r[:, 4:].reshape(-1)[:n]
+
+
+def _blocks(x):
+    for first in range(0, x.size, BLOCK):
+        yield first, x[first:first + BLOCK]
+
+
+def block_scale(x):
+    """The power of two by which a block's largest magnitude lies above 224 and at most at 448, at least 2^-126; NaN
+    where that is not finite."""
+    top = float(np.max(np.abs(x)))
+    if not np.isfinite(top):
+        return np.nan
+    e = -126
+    while top > 448.0 * 2.0 ** e:
+        e += 1
+    return 2.0 ** e
+
+
+def to_e4m3(x, halves):
+    """Codes (sign in bit 7) and scales of an array of fp32 values."""
+    table, codes, scales = e4m3_values(), np.zeros(x.size, np.uint8), []
+    for first, block in _blocks(x):
+        scale = block_scale(block)
+        scales.append(scale)
+        if np.isnan(scale):
+            continue
+        y = np.abs(block.astype(np.float64)) / scale
+        at = np.searchsorted(table, y, side="right") - 1
+        a, b = table[at], table[np.minimum(at + 1, 126)]
+        frac = np.where(at < 126, (y - a) / np.where(at < 126, b - a, 1.0), 0.0)
+        up = np.rint(frac * 2.0 ** 20) / 2.0 ** 20 + halves[first:first + BLOCK] / 65536.0 >= 1.0
+        codes[first:first + BLOCK] = at + up + 128 * np.signbit(block)
+    return codes, np.array(scales, np.float32)
+
+
+def to_e4m3_root(v, halves):
+    """Codes and scales of the roots of an array of fp32 values."""
+    table, codes, scales = e4m3_values(), np.zeros(v.size, np.uint8), []
+    root = np.sqrt(v.astype(np.float32))
+    f = np.float32
+    for first, block in _blocks(root):
+        scale = block_scale(block)
+        scales.append(scale)
+        if np.isnan(scale):
+            continue
+        y = f(block / f(scale)) if scale > 2.0 ** -126 else (block.astype(np.float64) / scale).astype(f)
+        at = np.searchsorted(table, y.astype(np.float64), side="right") - 1
+        a, b = table[at].astype(f), table[np.minimum(at + 1, 126)].astype(f)
+        share = halves[first:first + BLOCK].astype(f) * f(2.0 ** -16)
+        up = (y * y - a * a > share * (b * b - a * a)) & (at < 126)      # in fp32: a border is where fp32 has it
+        code = at + up
+        codes[first:first + BLOCK] = np.where((code == 0) & (block > 0), 1, code)
+    return codes, np.array(scales, np.float32)
+
+
+def from_e4m3(codes, scales):
+    table = np.append(e4m3_values(), np.nan)
+    with np.errstate(invalid="ignore"):
+        return np.where(codes & 128, -1.0, 1.0) * table[codes & 127] * np.repeat(scales.astype(np.float64), BLOCK)[:codes.size]

@@ -65,6 +65,9 @@ SIGNATURES = {
     "okt_attention_workspace_bytes": (c_sz, [c_u32] * 6),
     "okt_attention_forward": (c_int, [c_vp] * 7 + [c_sz, c_vp]),
     "okt_attention_backward": (c_int, [c_vp] * 11 + [c_sz, c_vp]),
+    "okt_adamw_plan_bytes": (c_sz, [c_vp, c_u32]),
+    "okt_adamw_plan": (c_int, [c_vp, c_u32, c_int, c_vp, c_sz, c_vp]),
+    "okt_adamw_step": (c_int, [c_vp, c_vp, c_vp]),
 }
 
 
@@ -747,3 +750,124 @@ def okt_attention_backward(q, k, v, o, lse, do, dq_out, dk_out, dv_out, ws, *, c
     _check("okt_attention_backward", load_library().okt_attention_backward(
         op, pq, pk, pv, po, _ptr(lse, _TORCH.float32, "lse"), pdo, pdq, pdk, pdv,
         _ptr(ws, _TORCH.uint8, "ws"), ws.numel(), _stream(stream)))
+
+
+# --------------------------------------------------------------------------
+# Where a call's tensors lie: all on the current device, whose stream it is enqueued on.
+def _stream_for(stream, *tensors):
+    device = _TORCH._C._cuda_getDevice()
+    for t in tensors:
+        if t is not None and t.get_device() != device:
+            raise ValueError(f"tensors must be on the current device ({device}), got one on {t.device}")
+    if stream is None:
+        return _TORCH._C._cuda_getCurrentRawStream(device)
+    if stream.device_index != device:
+        raise ValueError(f"stream must be of the current device ({device}), got {stream.device}")
+    return stream.cuda_stream
+
+
+# --------------------------------------------------------------------------
+# AdamW over many tensors
+_ADAMW_TENSOR = struct.Struct("=7QQ2d4i")       # okt_adamw_tensor
+_ADAMW = struct.Struct("=2IiI4d5Q")             # okt_adamw
+ADAMW_BLOCK = 256                               # OKT_ADAMW_BLOCK
+
+
+class AdamWPlan:
+    """What okt_adamw_step needs of its tensors, on their device; keeps them alive.  To be made again when one of
+    them moves (okt_adamw_plan); their contents may change at will."""
+
+    def __init__(self, device_bytes, tensors, chunks, state, held):
+        self.device_bytes, self.tensors, self.chunks, self.state, self.held = device_bytes, tensors, chunks, state, held
+
+
+def okt_adamw_plan_bytes(lengths) -> int:
+    """Bytes of the plan of tensors of such lengths; 0 if they are out of range."""
+    table = b"".join(_ADAMW_TENSOR.pack(*(0,) * 7, int(n), 0.0, 1.0, 0, 0, 1, 0) for n in lengths)
+    return load_library().okt_adamw_plan_bytes(table, len(lengths))
+
+
+def _each(value, count, name):
+    """One number for all tensors, or one for each."""
+    if isinstance(value, (int, float)):
+        return [float(value)] * count
+    value = [float(x) for x in value]
+    if len(value) != count:
+        raise ValueError(f"{name} needs one value a tensor ({count}), got {len(value)}")
+    return value
+
+
+def okt_adamw_plan(params, grads, ms, vs, *, m_scales=None, v_scales=None, copies=None, weight_decay=0.0,
+                   rate_scale=1.0) -> AdamWPlan:
+    """The plan of okt_adamw_step over lists of tensors, which are contiguous and on one device: params and grads float32,
+    bfloat16 or float16; the averages ms and vs float32, or float8_e4m3fn with a float32 scale for every ADAMW_BLOCK
+    elements in m_scales and v_scales (v is the square of what vs stands for); copies, if given, bfloat16
+    or float16 (or None for a tensor without one).  weight_decay and rate_scale: one for all or one a tensor.  Copies the plan to the device,
+    on the current stream."""
+    torch = _torch()
+    count = len(params)
+    if count == 0:
+        raise ValueError("params must not be empty")
+    lists = {"grads": grads, "ms": ms, "vs": vs, "m_scales": m_scales, "v_scales": v_scales, "copies": copies}
+    for name, tensors in lists.items():
+        if tensors is not None and len(tensors) != count:
+            raise ValueError(f"{name} needs one tensor a parameter ({count}), got {len(tensors)}")
+    for name in ("grads", "ms", "vs"):
+        if lists[name] is None:
+            raise TypeError(f"{name} is required")
+    state_type = ms[0].dtype
+    if state_type not in (torch.float32, torch.float8_e4m3fn):
+        raise TypeError(f"ms and vs must be float32 or float8_e4m3fn, got {state_type}")
+    eight = state_type == torch.float8_e4m3fn
+    if eight != (m_scales is not None) or eight != (v_scales is not None):
+        raise TypeError("m_scales and v_scales belong to averages in float8_e4m3fn, both of them")
+    decays, rates = _each(weight_decay, count, "weight_decay"), _each(rate_scale, count, "rate_scale")
+    device, packed, held = params[0].device, [], []
+    for i in range(count):
+        p, g, c = params[i], grads[i], None if copies is None else copies[i]
+        n = p.numel()
+        parts = [(p, None, "params", n), (g, None, "grads", n), (ms[i], state_type, "ms", n), (vs[i], state_type, "vs", n)]
+        if c is not None:
+            parts.append((c, None, "copies", n))
+        if eight:
+            parts += [(m_scales[i], torch.float32, "m_scales", -(-n // ADAMW_BLOCK)), (v_scales[i], torch.float32, "v_scales", -(-n // ADAMW_BLOCK))]
+        for t, dtype, name, numel in parts:
+            if t is None:
+                raise TypeError(f"{name}[{i}] is required")
+            if dtype is None:
+                _dtype_code(t, f"{name}[{i}]")
+            _ptr(t, dtype or t.dtype, f"{name}[{i}]")
+            if t.numel() != numel:
+                raise ValueError(f"{name}[{i}] needs {numel} elements, got {t.numel()}")
+            if t.device != device:
+                raise ValueError(f"{name}[{i}] must be on {device}, got {t.device}")
+            held.append(t)
+        if c is not None and c.dtype is torch.float32:
+            raise TypeError(f"copies[{i}] must be bfloat16 or float16")
+        packed.append(_ADAMW_TENSOR.pack(
+            p.data_ptr(), g.data_ptr(), ms[i].data_ptr(), vs[i].data_ptr(), 0 if c is None else c.data_ptr(),
+            m_scales[i].data_ptr() if eight else 0, v_scales[i].data_ptr() if eight else 0, n, decays[i], rates[i],
+            _DTYPES[p.dtype], _DTYPES[g.dtype], 1 if c is None else _DTYPES[c.dtype], 0))
+    table, lib = b"".join(packed), load_library()
+    nbytes = lib.okt_adamw_plan_bytes(table, count)
+    host, chunks = torch.empty(max(nbytes, 256), dtype=torch.uint8), c_u32(0)
+    _check("okt_adamw_plan", lib.okt_adamw_plan(table, count, 1 if eight else 0, host.data_ptr(), nbytes,
+                                                ctypes.cast(ctypes.pointer(chunks), c_vp)))
+    return AdamWPlan(host.to(device), count, chunks.value, 1 if eight else 0, held)
+
+
+def okt_adamw_step(plan: AdamWPlan, step, *, lr, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8, grad_scale=None,
+                   skip=None, seed=None, site: int = 0, stream=None) -> None:
+    """One AdamW step over the plan's tensors.  step: int64[1] on the device, counted from 1 (the caller counts); lr: a number
+    or float32[1] on the device; grad_scale, skip: float32[1] on the device or None - gradients are
+    multiplied by the one, and nothing is changed where the other is not 0; seed: int64[1] on the device, for averages in 8 bits."""
+    f32, i64 = _TORCH.float32, _TORCH.int64
+    on_device = not isinstance(lr, (int, float))
+    for t, name in ((step, "step"), (lr if on_device else None, "lr"), (grad_scale, "grad_scale"), (skip, "skip"), (seed, "seed")):
+        if t is not None and t.numel() < 1:
+            raise ValueError(f"{name} needs one element")
+    op = _ADAMW.pack(plan.tensors, plan.chunks, plan.state, site, 0.0 if on_device else lr, beta1, beta2, eps,
+                     _ptr(step, i64, "step"), _ptr(lr, f32, "lr") if on_device else 0, _ptr(grad_scale, f32, "grad_scale", True) or 0,
+                     _ptr(skip, f32, "skip", True) or 0, _ptr(seed, i64, "seed", True) or 0)
+    handle = _stream_for(stream, plan.device_bytes, step, lr if on_device else None, grad_scale, skip, seed)
+    _check("okt_adamw_step", load_library().okt_adamw_step(op, plan.device_bytes.data_ptr(), handle))
