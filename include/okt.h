@@ -684,6 +684,58 @@ int okt_attention_backward(const okt_attention* op, const void* d_q, const void*
                            void* d_dk_out, void* d_dv_out, void* d_ws, size_t ws_bytes, void* stream);
 
 /*
+ * What stands between the projection of queries and keys and attention: a norm of every head and the rotation of its pairs
+ * by the token's position, in one pass.  For a head vector x of a token
+ *   n = (x - m) r weight, or x without a weight     m = mean(x) (OKT_NORM_RMS: 0), r = 1 / sqrt(mean (x - m)^2 + eps)
+ *   y_a = n_a cos t - n_b sin t,  y_b = n_a sin t + n_b cos t,   t = position[axis_of_pair[j]] inv_freq[j]
+ * for the pairs j < rot_dim / 2: (a, b) = (j, j + rot_dim / 2), or (2j, 2j + 1) if `adjacent`; elements from
+ * rot_dim on stay n.  Several axes (time, height, width) turn pairs of their own.  The angle is taken in fp64, so
+ * far positions lose nothing; the rest is fp32, an output is rounded once.  Queries and keys are [batch][length][heads][head_dim] by strides
+ * {batch, length, heads} in elements, head_dim contiguous, at the alignment of an element; so parts of a common
+ * projection are taken as they lie, and keys can be written to where they are kept.  The norm is there where its weight is, for queries and keys
+ * apart.  One of the two may have no heads.
+ */
+typedef struct okt_norm_rotary {
+    uint32_t batch, length;        /* batch * length < 2^24; 0: a no-op (backward: zeros to the weights' gradients) */
+    uint32_t heads, kv_heads;      /* each at most 2^16, one of them above 0 */
+    uint32_t head_dim;             /* 8, 16, ... 256 */
+    uint32_t rot_dim;              /* 0, 8, ... head_dim */
+    int32_t dtype;                 /* of queries, keys and their gradients */
+    int32_t kind;                  /* okt_norm_kind of both norms */
+    float eps;                     /* >= 0 */
+    int32_t adjacent;
+    uint32_t axes;                 /* 1 to 8 */
+    uint32_t reserved;             /* 0 */
+    uint8_t axis_of_pair[128];     /* below axes; the first rot_dim / 2 are looked at */
+    const float* d_inv_freq;       /* fp32[rot_dim / 2] on the device */
+    const int32_t* d_positions;    /* int32[batch][length][axes] on the device; NULL: the place in the sequence (one axis) */
+    uint64_t position_stride[2];   /* from a sequence (0: all share) and a token to the next, in elements */
+    const float* d_q_weight;       /* fp32[head_dim] on the device, or NULL */
+    const float* d_k_weight;
+    uint64_t q_stride[3], k_stride[3];           /* inputs of the forward pass */
+    uint64_t q_out_stride[3], k_out_stride[3];   /* what the call writes */
+    uint64_t dq_stride[3], dk_stride[3];         /* backward: gradients of what the forward pass wrote */
+} okt_norm_rotary;
+
+/* Bytes of workspace the backward pass needs (the forward pass needs none); 0 if sizes are out of range.  Pure host arithmetic. */
+size_t okt_norm_rotary_workspace_bytes(uint32_t batch, uint32_t length, uint32_t heads, uint32_t kv_heads, uint32_t head_dim);
+
+/* d_q_out may be d_q with its strides, d_k_out d_k; they overlap nothing otherwise.  One launch. */
+int okt_norm_rotary_forward(const okt_norm_rotary* op, const void* d_q, const void* d_k, void* d_q_out, void* d_k_out,
+                            void* stream);
+
+/*
+ * From the gradients d_dq and d_dk of the outputs to those of the inputs, d_dq_out and d_dk_out, and of the weights.
+ *   d_q, d_k  in   as the forward pass read them; looked at where there is a weight (else may be NULL)
+ *   d_dq_out, d_dk_out  out  may be d_dq and d_dk, or d_q and d_k, with their strides; overlap nothing otherwise
+ *   d_dq_weight_out, d_dk_weight_out  out  fp32[head_dim], 4-byte aligned; NULL: not wanted, and where there is no weight
+ * The workspace is needed for weights' gradients only.  Two launches, one without those.
+ */
+int okt_norm_rotary_backward(const okt_norm_rotary* op, const void* d_q, const void* d_k, const void* d_dq, const void* d_dk,
+                             void* d_dq_out, void* d_dk_out, float* d_dq_weight_out, float* d_dk_weight_out, void* d_ws,
+                             size_t ws_bytes, void* stream);
+
+/*
  * AdamW over many tensors in one launch, states in 32 bits or in 8.  For an element p with gradient g, averages m and v and
  * t = the step, counted from 1:
  *   g = grad_scale g,  m = beta1 m + (1 - beta1) g,  v = beta2 v + (1 - beta2) g^2,  rate = lr rate_scale

@@ -105,3 +105,57 @@ def from_e4m3(codes, scales):
     table = np.append(e4m3_values(), np.nan)
     with np.errstate(invalid="ignore"):
         return np.where(codes & 128, -1.0, 1.0) * table[codes & 127] * np.repeat(scales.astype(np.float64), BLOCK)[:codes.size]
+
+
+# ------------------------------------------------------------------ norms and rotation of heads
+
+def _pairs(dim, rot, adjacent):
+    j = np.arange(rot // 2)
+    return (2 * j, 2 * j + 1) if adjacent else (j, j + rot // 2)
+
+
+def angles(batch, length, inv_freq, positions=None, axis_of_pair=None):
+    """[batch, length, 1, pairs]; positions [batch, length, axes]."""
+    pairs = 0 if inv_freq is None else len(inv_freq)
+    if positions is None:
+        positions = np.broadcast_to(np.arange(length)[None, :, None], (batch, length, 1))
+    axis = np.zeros(pairs, int) if axis_of_pair is None else np.asarray(axis_of_pair, int)
+    freq = np.zeros(0) if inv_freq is None else np.asarray(inv_freq, np.float64)
+    # positions are whole and frequencies have 24 bits: the product is exact in the long double that it is reduced in
+    turns = positions[:, :, axis].astype(np.longdouble) * freq.astype(np.longdouble)
+    return np.mod(turns, 2 * np.longdouble(np.pi) + np.longdouble(1.2246467991473532e-16) * 2).astype(np.float64)[:, :, None]
+
+
+def turned(x, angle, adjacent, back=False):
+    a, b = _pairs(x.shape[-1], 2 * angle.shape[-1], adjacent)
+    c, s = np.cos(angle), np.sin(angle) * (-1.0 if back else 1.0)
+    y = x.copy()
+    y[..., a] = x[..., a] * c - x[..., b] * s
+    y[..., b] = x[..., a] * s + x[..., b] * c
+    return y
+
+
+def head_statistics(x, kind, eps):
+    mean = x.mean(-1, keepdims=True) if kind == "layer" else np.zeros(x.shape[:-1] + (1,))
+    return mean, 1.0 / np.sqrt(((x - mean) ** 2).mean(-1, keepdims=True) + eps)
+
+
+def norm_rotary(x, angle, *, weight=None, kind="rms", eps=1e-6, adjacent=False):
+    if weight is not None:
+        mean, r = head_statistics(x, kind, eps)
+        x = (x - mean) * r * weight
+    return turned(x, angle, adjacent)
+
+
+def norm_rotary_backward(x, dy, angle, *, weight=None, kind="rms", eps=1e-6, adjacent=False):
+    """(dx, dweight), dweight None without a weight."""
+    d = turned(dy, angle, adjacent, back=True)
+    if weight is None:
+        return d, None
+    mean, r = head_statistics(x, kind, eps)
+    h = (x - mean) * r
+    w = d * weight
+    dx = w - h * (w * h).mean(-1, keepdims=True)
+    if kind == "layer":
+        dx = dx - w.mean(-1, keepdims=True)
+    return r * dx, (d * h).sum((0, 1, 2))

@@ -65,6 +65,9 @@ SIGNATURES = {
     "okt_attention_workspace_bytes": (c_sz, [c_u32] * 6),
     "okt_attention_forward": (c_int, [c_vp] * 7 + [c_sz, c_vp]),
     "okt_attention_backward": (c_int, [c_vp] * 11 + [c_sz, c_vp]),
+    "okt_norm_rotary_workspace_bytes": (c_sz, [c_u32] * 5),
+    "okt_norm_rotary_forward": (c_int, [c_vp] * 6),
+    "okt_norm_rotary_backward": (c_int, [c_vp] * 10 + [c_sz, c_vp]),
     "okt_adamw_plan_bytes": (c_sz, [c_vp, c_u32]),
     "okt_adamw_plan": (c_int, [c_vp, c_u32, c_int, c_vp, c_sz, c_vp]),
     "okt_adamw_step": (c_int, [c_vp, c_vp, c_vp]),
@@ -764,6 +767,118 @@ def _stream_for(stream, *tensors):
     if stream.device_index != device:
         raise ValueError(f"stream must be of the current device ({device}), got {stream.device}")
     return stream.cuda_stream
+
+
+# --------------------------------------------------------------------------
+# Norms and rotation of heads
+_ROTARY = struct.Struct("=6I2ifi2I128sQQ2Q2Q18Q")    # okt_norm_rotary
+
+
+def okt_norm_rotary_workspace_bytes(batch: int, length: int, heads: int, kv_heads: int, head_dim: int) -> int:
+    return load_library().okt_norm_rotary_workspace_bytes(int(batch), int(length), int(heads), int(kv_heads), int(head_dim))
+
+
+def _positions(t, batch, length, axes):
+    """(pointer, batch stride, token stride) of int32 [batch, length, axes] or [length, axes]; one axis may be left out."""
+    if t is None:
+        return 0, 0, 0
+    if not t.is_cuda:
+        raise TypeError("positions must be a CUDA tensor (device memory)")
+    if t.dtype is not _TORCH.int32:
+        raise TypeError(f"positions must have dtype {_TORCH.int32}, got {t.dtype}")
+    if axes == 1 and (t.dim() == 1 or (t.dim() == 2 and t.shape == (batch, length) and t.shape != (length, 1))):
+        t = t.unsqueeze(-1)
+    if t.shape != (batch, length, axes) and t.shape != (length, axes):
+        raise ValueError(f"positions must have the shape {(batch, length, axes)} or {(length, axes)}, got {tuple(t.shape)}")
+    if axes > 1 and t.stride(-1) != 1:
+        raise ValueError("positions must have contiguous axes")
+    strides = t.stride()
+    return t.data_ptr(), strides[0] if t.dim() == 3 else 0, strides[-2]
+
+
+_NO_HEADS = (0, 0, 0)
+
+
+def _rotary_struct(dtype, shape, kv_heads, inv_freq, positions, axis_of_pair, adjacent, kind, eps, q_weight, k_weight, strides):
+    batch, length, heads, dim = shape
+    pairs = 0 if inv_freq is None else inv_freq.numel()
+    axes = 1
+    table = b""
+    if axis_of_pair is not None:
+        if len(axis_of_pair) != pairs:
+            raise ValueError(f"axis_of_pair needs one axis a pair ({pairs}), got {len(axis_of_pair)}")
+        table = bytes(axis_of_pair)
+        axes = max(table, default=0) + 1
+    if positions is not None and positions.dim() == 3:
+        axes = max(axes, positions.shape[2])
+    elif positions is not None and axes > 1 and positions.dim() == 2:
+        axes = max(axes, positions.shape[1])
+    at, by_batch, by_token = _positions(positions, batch, length, axes)
+    return _ROTARY.pack(
+        batch, length, heads, kv_heads, dim, 2 * pairs, _DTYPES[dtype], _NORM_KINDS[kind], eps, 1 if adjacent else 0, axes, 0, table,
+        0 if inv_freq is None else _parameter(inv_freq, pairs, "inv_freq"), at, by_batch, by_token,
+        _parameter(q_weight, dim, "q_weight"), _parameter(k_weight, dim, "k_weight"), *strides)
+
+
+def okt_norm_rotary_forward(q, k, q_out, k_out, inv_freq, *, positions=None, axis_of_pair=None, adjacent: bool = False,
+                            kind: str = "rms", eps: float = 1e-6, q_weight=None, k_weight=None, stream=None) -> None:
+    """Norm (where there is a weight) and rotation of every head of [batch, length, heads, head_dim] tensors, the last axis
+    contiguous.  k and k_out may be None.  inv_freq: float32, one frequency a pair, so 2 * inv_freq.numel() leading elements of a head
+    are rotated (None: none).  positions: int32 [batch, length, axes] or [length, axes] on the device (of one axis [batch, length] or
+    [length], too), None for the place in the
+    sequence; axis_of_pair: which axis turns each pair (a sequence of numbers; None: the first).  Outputs may be their inputs."""
+    _dtype_code(q, "q")
+    dtype, shape = q.dtype, q.shape
+    if len(shape) != 4:
+        raise ValueError("q and k must be [batch, length, heads, head_dim]")
+    pq, sq = _heads(q, dtype, shape, "q")
+    po, so = _heads(q_out, dtype, shape, "q_out")
+    pk, sk, pko, sko, kv_heads = 0, _NO_HEADS, 0, _NO_HEADS, 0
+    if k is not None:
+        keys = k.shape
+        if len(keys) != 4 or keys[:2] != shape[:2] or keys[3] != shape[3]:
+            raise ValueError("q and k must agree in batch, length and head_dim")
+        kv_heads = keys[2]
+        pk, sk = _heads(k, dtype, keys, "k")
+        pko, sko = _heads(k_out, dtype, keys, "k_out")
+    op = _rotary_struct(dtype, shape, kv_heads, inv_freq, positions, axis_of_pair, adjacent, kind, eps, q_weight, k_weight,
+                        (*sq, *sk, *so, *sko, *_NO_HEADS, *_NO_HEADS))
+    handle = _stream_for(stream, q, k, q_out, k_out, inv_freq, positions, q_weight, k_weight)
+    _check("okt_norm_rotary_forward", load_library().okt_norm_rotary_forward(op, pq, pk, po, pko, handle))
+
+
+def okt_norm_rotary_backward(q, k, dq, dk, dq_out, dk_out, inv_freq, ws=None, *, dq_weight_out=None, dk_weight_out=None,
+                             positions=None, axis_of_pair=None, adjacent: bool = False, kind: str = "rms", eps: float = 1e-6,
+                             q_weight=None, k_weight=None, stream=None) -> None:
+    """Gradients of q, k and the weights from those of the outputs, dq and dk, with the options of the forward pass.  q and k as
+    the forward pass read them (None where there is no weight).  dq_out may be dq, dk_out dk."""
+    _dtype_code(dq, "dq")
+    dtype, shape = dq.dtype, dq.shape
+    if len(shape) != 4:
+        raise ValueError("dq and dk must be [batch, length, heads, head_dim]")
+    pd, sd = _heads(dq, dtype, shape, "dq")
+    po, so = _heads(dq_out, dtype, shape, "dq_out")
+    if q is None and q_weight is not None:
+        raise TypeError("q is required where it has a norm")
+    pq, sq = (0, _NO_HEADS) if q is None else _heads(q, dtype, shape, "q")
+    pk, sk, pdk, sdk, pko, sko, kv_heads = 0, _NO_HEADS, 0, _NO_HEADS, 0, _NO_HEADS, 0
+    if dk is not None:
+        keys = dk.shape
+        if len(keys) != 4 or keys[:2] != shape[:2] or keys[3] != shape[3]:
+            raise ValueError("dq and dk must agree in batch, length and head_dim")
+        kv_heads = keys[2]
+        if k is None and k_weight is not None:
+            raise TypeError("k is required where it has a norm")
+        pk, sk = (0, _NO_HEADS) if k is None else _heads(k, dtype, keys, "k")
+        pdk, sdk = _heads(dk, dtype, keys, "dk")
+        pko, sko = _heads(dk_out, dtype, keys, "dk_out")
+    op = _rotary_struct(dtype, shape, kv_heads, inv_freq, positions, axis_of_pair, adjacent, kind, eps, q_weight, k_weight,
+                        (*sq, *sk, *so, *sko, *sd, *sdk))
+    dim = shape[3]
+    handle = _stream_for(stream, q, k, dq, dk, dq_out, dk_out, inv_freq, positions, q_weight, k_weight, dq_weight_out, dk_weight_out, ws)
+    _check("okt_norm_rotary_backward", load_library().okt_norm_rotary_backward(
+        op, pq, pk, pd, pdk, po, pko, _parameter(dq_weight_out, dim, "dq_weight_out"), _parameter(dk_weight_out, dim, "dk_weight_out"),
+        _ptr(ws, _TORCH.uint8, "ws", True), 0 if ws is None else ws.numel(), handle))
 
 
 # --------------------------------------------------------------------------

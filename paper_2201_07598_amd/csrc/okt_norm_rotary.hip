@@ -1,0 +1,520 @@
+// okt_norm_rotary_forward / _backward: a norm of each head of queries and keys and the rotation of its pairs by position.
+//
+//   n = (x - m) r w  (or x),   y_a = n_a cos - n_b sin,   y_b = n_a sin + n_b cos   for the pair (a, b) of angle position * freq
+//
+// Backward the rotation is turned back, then dx = r (d w - h mean(h d w) - mean(d w)), h = (x - m) r, and dw = sum d h.
+// Every element comes once and goes once (backward: two come, one goes), so memory bounds it.
+//
+// A workgroup takes a few tokens.  First its threads make the cosines and sines of those tokens, each once, in LDS, where
+// all heads find them: the angle in fp64 turns of which the whole ones are dropped, because a position of 10^5 times a frequency
+// has lost 2^-7 of a turn in fp32.  Then lanes take heads: eight elements a lane as two fours, which are the two halves of four pairs (or
+// four adjacent pairs), so a pair never leaves its lane and a norm's sums cross 8, 16 or 32 lanes inside the vector unit.
+#include <math.h>
+
+#include "okt_element.h"
+
+namespace okt {
+
+constexpr int ROT_THREADS = 256;
+constexpr uint32_t ROT_MAX_DIM = 256, ROT_MAX_TOKENS = 32;           // of a workgroup at a time
+constexpr uint32_t ROT_ANGLES = 2048;                                // a workgroup's tokens times pairs
+constexpr uint32_t ROT_BACKWARD_GROUPS = 1024;
+constexpr int ROT_AHEAD = 4;                                         // heads of a lane that are on their way together
+
+struct HeadStrides { uint64_t batch, row, head; };
+
+struct RotTensor {                                                   // queries or keys
+    uint32_t heads;
+    const float* weight;
+    HeadStrides in, d, out;
+};
+
+struct RotArgs {
+    uint64_t tokens, tiles;
+    uint32_t length, dim, rot, tile, groups;                         // tokens a tile; workgroups (backward)
+    int kind;
+    bool adjacent;
+    float eps;
+    const float* inv_freq;
+    const int32_t* positions;
+    uint64_t position_stride[2];
+    RotTensor t[2];
+    float* partial;
+    uint8_t axis_of_pair[ROT_MAX_DIM / 2];
+};
+
+struct RotPointers { const void* x[2]; const void* d[2]; void* out[2]; };
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+template <typename T>
+__device__ __forceinline__ f32x4 load_four(const T* p) {
+    typedef T vec __attribute__((ext_vector_type(4), aligned(sizeof(T))));
+    return __builtin_convertvector(*reinterpret_cast<const vec*>(p), f32x4);
+}
+template <typename T>
+__device__ __forceinline__ void store_four(T* p, f32x4 v) {
+    typedef T vec __attribute__((ext_vector_type(4), aligned(sizeof(T))));
+    *reinterpret_cast<vec*>(p) = __builtin_convertvector(v, vec);
+}
+
+// Sum over LANES (8, 16 or 32) neighbouring lanes, in each of them.
+template <int LANES>
+__device__ __forceinline__ float head_sum(float v) {
+#define OKT_SUM_STEP(ctrl) v += __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), ctrl, 0xf, 0xf, true))
+    OKT_SUM_STEP(0xB1);           // quad_perm [1, 0, 3, 2]
+    OKT_SUM_STEP(0x4E);           // quad_perm [2, 3, 0, 1]
+    OKT_SUM_STEP(0x141);          // row_half_mirror: the other four of eight
+    if (LANES >= 16) OKT_SUM_STEP(0x140);     // row_mirror: the other eight of sixteen
+#undef OKT_SUM_STEP
+    if (LANES >= 32) {
+        const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        v = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+    }
+    return v;
+}
+
+struct Eights { f32x4 a, b; };                                       // four pairs: first and second of each
+
+__device__ __forceinline__ float sum_of(const Eights& x) {
+    const f32x4 s = x.a + x.b;
+    return (s[0] + s[1]) + (s[2] + s[3]);
+}
+__device__ __forceinline__ float dot_of(const Eights& x, const Eights& y) {
+    const f32x4 s = x.a * y.a + x.b * y.b;
+    return (s[0] + s[1]) + (s[2] + s[3]);
+}
+
+struct TokenPlace { uint64_t in[2], d[2], out[2]; };
+
+// What a workgroup's threads share about its tokens.
+struct RotShared {
+    f32x4 cosine[ROT_ANGLES / 4], sine[ROT_ANGLES / 4];              // [token][pair], dim / 2 pairs; the unrotated are turned by 0
+    TokenPlace place[ROT_MAX_TOKENS];
+    float sums[2][ROT_MAX_DIM * (ROT_THREADS / WAVE)];
+};
+
+template <bool BACKWARD>
+__device__ __forceinline__ void rot_tokens(const RotArgs& a, RotShared& s, uint64_t first, uint32_t count) {
+    const uint32_t pairs = a.dim / 2;
+    for (uint32_t n = threadIdx.x; n < count * pairs; n += ROT_THREADS) {
+        const uint32_t t = n / pairs, j = n % pairs;
+        float c = 1.0f, d = 0.0f;
+        if (j < a.rot / 2) {
+            const uint64_t token = first + t, b = token / a.length;
+            const uint32_t i = (uint32_t)(token % a.length);
+            const int32_t position = a.positions ? a.positions[b * a.position_stride[0] + i * a.position_stride[1] + a.axis_of_pair[j]] : (int32_t)i;
+            const double turns = (double)position * (double)a.inv_freq[j] * 0.15915494309189533577;        // 1 / 2 pi
+            sincospif((float)(2.0 * (turns - rint(turns))), &d, &c);
+        }
+        reinterpret_cast<float*>(s.cosine)[n] = c;
+        reinterpret_cast<float*>(s.sine)[n] = d;
+    }
+    if (threadIdx.x < count) {
+        const uint64_t token = first + threadIdx.x, b = token / a.length, i = token % a.length;
+        TokenPlace p;
+#pragma unroll
+        for (int n = 0; n < 2; ++n) {
+            p.in[n] = b * a.t[n].in.batch + i * a.t[n].in.row;
+            if (BACKWARD) p.d[n] = b * a.t[n].d.batch + i * a.t[n].d.row;
+            p.out[n] = b * a.t[n].out.batch + i * a.t[n].out.row;
+        }
+        s.place[threadIdx.x] = p;
+    }
+}
+
+// Where a lane's two fours lie in a head, and back and forth between them and pairs.
+struct LanePlace {
+    uint32_t first, second, unit;
+    bool there;
+    template <int LANES>
+    static __device__ __forceinline__ LanePlace of(const RotArgs& a) {
+        const uint32_t unit = threadIdx.x % LANES;
+        const bool apart = !a.adjacent && unit < a.rot / 8;
+        return {apart ? unit * 4 : unit * 8, apart ? a.rot / 2 + unit * 4 : unit * 8 + 4, unit, unit * 8 < a.dim};
+    }
+    template <typename T>
+    __device__ __forceinline__ Eights load(const T* head, bool adjacent) const {
+        return pairs(Eights{load_four(head + first), load_four(head + second)}, adjacent);
+    }
+    template <typename T>
+    __device__ __forceinline__ void store(T* head, const Eights& v, bool adjacent) const {
+        f32x4 x = v.a, y = v.b;
+        if (adjacent) {
+            x = f32x4{v.a[0], v.b[0], v.a[1], v.b[1]};
+            y = f32x4{v.a[2], v.b[2], v.a[3], v.b[3]};
+        }
+        store_four(head + first, x);
+        store_four(head + second, y);
+    }
+    static __device__ __forceinline__ Eights pairs(Eights v, bool adjacent) {
+        if (!adjacent) return v;
+        return {f32x4{v.a[0], v.a[2], v.b[0], v.b[2]}, f32x4{v.a[1], v.a[3], v.b[1], v.b[3]}};
+    }
+};
+
+// Heads of a tile in the order in which a lane's group takes them.
+struct HeadWalk {
+    uint32_t token, head;
+    __device__ __forceinline__ void settle(uint32_t heads) {
+        while (head >= heads) {
+            head -= heads;
+            ++token;
+        }
+    }
+};
+
+template <typename T, int LANES, int N>
+__device__ __forceinline__ void rot_forward(const RotArgs& a, const RotShared& s, uint32_t count, const T* x, T* out) {
+    const RotTensor& t = a.t[N];
+    const LanePlace at = LanePlace::of<LANES>(a);
+    const uint32_t step = ROT_THREADS / LANES;
+    Eights w = {1.0f, 1.0f};
+    if (t.weight && at.there) w = at.load(t.weight, a.adjacent);
+    const float share = 1.0f / (float)a.dim;
+    HeadWalk walk = {0, threadIdx.x / LANES};
+    walk.settle(t.heads);
+    while (walk.token < count) {
+        HeadWalk mine[ROT_AHEAD];
+        Eights v[ROT_AHEAD];
+#pragma unroll
+        for (int k = 0; k < ROT_AHEAD; ++k) {
+            mine[k] = walk;
+            v[k] = {0.0f, 0.0f};
+            if (walk.token < count && at.there) v[k] = at.load(x + s.place[walk.token].in[N] + walk.head * t.in.head, a.adjacent);
+            walk.head += step;
+            walk.settle(t.heads);
+        }
+#pragma unroll
+        for (int k = 0; k < ROT_AHEAD; ++k) {
+            if (mine[k].token >= count) break;                  // the same for all lanes of a head
+            if (t.weight) {
+                if (a.kind == OKT_NORM_LAYER) {
+                    const float mean = head_sum<LANES>(sum_of(v[k])) * share;
+                    if (at.there) {
+                        v[k].a -= mean;
+                        v[k].b -= mean;
+                    }
+                }
+                const float r = 1.0f / sqrtf(head_sum<LANES>(dot_of(v[k], v[k])) * share + a.eps);
+                v[k].a *= r * w.a;
+                v[k].b *= r * w.b;
+            }
+            if (!at.there) continue;
+            const uint32_t angle = mine[k].token * (a.dim / 8) + at.unit;
+            const f32x4 c = s.cosine[angle], d = s.sine[angle];
+            at.store(out + s.place[mine[k].token].out[N] + mine[k].head * t.out.head,
+                     Eights{v[k].a * c - v[k].b * d, v[k].a * d + v[k].b * c}, a.adjacent);
+        }
+    }
+}
+
+template <typename T, int LANES>
+__global__ __launch_bounds__(ROT_THREADS) void norm_rotary_forward_kernel(RotArgs a, RotPointers p) {
+    __shared__ RotShared s;
+    const uint64_t first = (uint64_t)blockIdx.x * a.tile;
+    const uint32_t count = (uint32_t)(a.tokens - first < a.tile ? a.tokens - first : a.tile);
+    rot_tokens<false>(a, s, first, count);
+    __syncthreads();
+    if (a.t[0].heads) rot_forward<T, LANES, 0>(a, s, count, (const T*)p.x[0], (T*)p.out[0]);
+    if (a.t[1].heads) rot_forward<T, LANES, 1>(a, s, count, (const T*)p.x[1], (T*)p.out[1]);
+}
+
+template <typename T, int LANES, int N>
+__device__ __forceinline__ void rot_backward(const RotArgs& a, const RotShared& s, uint32_t count, const T* x, const T* dy, T* out,
+                                             Eights& dw) {
+    constexpr int AHEAD = ROT_AHEAD / 2;
+    const RotTensor& t = a.t[N];
+    const LanePlace at = LanePlace::of<LANES>(a);
+    const uint32_t step = ROT_THREADS / LANES;
+    Eights w = {1.0f, 1.0f};
+    if (t.weight && at.there) w = at.load(t.weight, a.adjacent);
+    const float share = 1.0f / (float)a.dim;
+    HeadWalk walk = {0, threadIdx.x / LANES};
+    walk.settle(t.heads);
+    while (walk.token < count) {
+        HeadWalk mine[AHEAD];
+        Eights v[AHEAD], d[AHEAD];
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) {
+            mine[k] = walk;
+            v[k] = d[k] = {0.0f, 0.0f};
+            if (walk.token < count && at.there) {
+                d[k] = at.load(dy + s.place[walk.token].d[N] + walk.head * t.d.head, a.adjacent);
+                if (t.weight) v[k] = at.load(x + s.place[walk.token].in[N] + walk.head * t.in.head, a.adjacent);
+            }
+            walk.head += step;
+            walk.settle(t.heads);
+        }
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) {
+            if (mine[k].token >= count) break;
+            const uint32_t angle = mine[k].token * (a.dim / 8) + (at.there ? at.unit : 0);
+            const f32x4 c = s.cosine[angle], e = s.sine[angle];
+            Eights g = {d[k].a * c + d[k].b * e, d[k].b * c - d[k].a * e};
+            if (t.weight) {
+                const bool layer = a.kind == OKT_NORM_LAYER;
+                if (layer) {
+                    const float mean = head_sum<LANES>(sum_of(v[k])) * share;
+                    if (at.there) {
+                        v[k].a -= mean;
+                        v[k].b -= mean;
+                    }
+                }
+                const float r = 1.0f / sqrtf(head_sum<LANES>(dot_of(v[k], v[k])) * share + a.eps);
+                v[k].a *= r;                                    // h
+                v[k].b *= r;
+                dw.a += g.a * v[k].a;
+                dw.b += g.b * v[k].b;
+                g.a *= w.a;
+                g.b *= w.b;
+                const float along = head_sum<LANES>(dot_of(g, v[k])) * share;
+                const float level = layer ? head_sum<LANES>(sum_of(g)) * share : 0.0f;
+                g.a = r * (g.a - v[k].a * along - level);
+                g.b = r * (g.b - v[k].b * along - level);
+            }
+            if (at.there) at.store(out + s.place[mine[k].token].out[N] + mine[k].head * t.out.head, g, a.adjacent);
+        }
+    }
+}
+
+// A workgroup's sums of a weight's gradient, over its lanes of one unit; in the order of the elements of a head.
+template <int LANES>
+__device__ __forceinline__ void rot_sums(const RotArgs& a, RotShared& s, int n, const Eights& dw, float* to) {
+    const LanePlace at = LanePlace::of<LANES>(a);
+    float v[8] = {dw.a[0], dw.a[1], dw.a[2], dw.a[3], dw.b[0], dw.b[1], dw.b[2], dw.b[3]};
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+        for (int m = LANES; m < WAVE; m <<= 1) v[i] += __shfl_xor(v[i], m, WAVE);
+    if (threadIdx.x % WAVE < LANES && at.there)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            // element i of the pairs' order in the head's
+            const uint32_t e = a.adjacent ? at.unit * 8 + 2 * (i % 4) + i / 4 : (i < 4 ? at.first + i : at.second + i - 4);
+            s.sums[n][threadIdx.x / WAVE * ROT_MAX_DIM + e] = v[i];
+        }
+    __syncthreads();
+    for (uint32_t e = threadIdx.x; e < a.dim; e += ROT_THREADS) {
+        float sum = 0.0f;
+#pragma unroll
+        for (int wave = 0; wave < ROT_THREADS / WAVE; ++wave) sum += s.sums[n][wave * ROT_MAX_DIM + e];
+        to[e] = sum;
+    }
+}
+
+template <typename T, int LANES>
+__global__ __launch_bounds__(ROT_THREADS) void norm_rotary_backward_kernel(RotArgs a, RotPointers p) {
+    __shared__ RotShared s;
+    Eights dw[2] = {{0.0f, 0.0f}, {0.0f, 0.0f}};
+    for (uint64_t tile = blockIdx.x; tile < a.tiles; tile += a.groups) {
+        const uint64_t first = tile * a.tile;
+        const uint32_t count = (uint32_t)(a.tokens - first < a.tile ? a.tokens - first : a.tile);
+        rot_tokens<true>(a, s, first, count);
+        __syncthreads();
+        if (a.t[0].heads) rot_backward<T, LANES, 0>(a, s, count, (const T*)p.x[0], (const T*)p.d[0], (T*)p.out[0], dw[0]);
+        if (a.t[1].heads) rot_backward<T, LANES, 1>(a, s, count, (const T*)p.x[1], (const T*)p.d[1], (T*)p.out[1], dw[1]);
+        __syncthreads();
+    }
+    if (!a.partial) return;
+#pragma unroll
+    for (int n = 0; n < 2; ++n)
+        rot_sums<LANES>(a, s, n, dw[n], a.partial + ((uint64_t)n * a.groups + blockIdx.x) * a.dim);
+}
+
+// Adds the workgroups' sums, always in the same order: sixteen columns by sixteen parts a workgroup.
+constexpr int ROT_ADD_COLS = 16;
+struct RotGradients { float* to[2]; };
+__global__ __launch_bounds__(ROT_THREADS) void norm_rotary_add_kernel(const float* partial, uint32_t groups, uint32_t dim, RotGradients g) {
+    constexpr int PARTS = ROT_THREADS / ROT_ADD_COLS;
+    __shared__ float sums[PARTS][ROT_ADD_COLS];
+    const uint32_t n = blockIdx.y, part = threadIdx.x / ROT_ADD_COLS, col = threadIdx.x % ROT_ADD_COLS, e = blockIdx.x * ROT_ADD_COLS + col;
+    float sum = 0.0f;
+    if (e < dim)
+#pragma unroll 8
+        for (uint32_t k = part; k < groups; k += PARTS) sum += partial[((uint64_t)n * groups + k) * dim + e];
+    sums[part][col] = sum;
+    __syncthreads();
+    if (part != 0 || e >= dim || !g.to[n]) return;
+#pragma unroll
+    for (int k = 1; k < PARTS; ++k) sum += sums[k][col];
+    g.to[n][e] = sum;
+}
+
+// ------------------------------------------------------------------ host
+
+static uint32_t rot_lanes(uint32_t dim) { return dim <= 64 ? 8 : dim <= 128 ? 16 : 32; }
+
+// Tokens a workgroup takes at a time: eight heads a lane, but no fewer workgroups than fill the chip four times, and
+// what the shared memory holds.
+static uint32_t rot_tile(uint64_t tokens, uint32_t heads, uint32_t dim) {
+    const uint64_t at_once = ROT_THREADS / rot_lanes(dim), wanted = (8 * at_once + heads - 1) / heads;
+    const uint64_t spread = (tokens + 1023) / 1024, room = ROT_ANGLES / (dim / 2);
+    uint64_t t = wanted;
+    for (const uint64_t most : {spread, room, (uint64_t)ROT_MAX_TOKENS}) t = most < t ? most : t;
+    return t ? (uint32_t)t : 1;
+}
+static uint32_t rot_groups(uint64_t tiles) { return (uint32_t)(tiles < ROT_BACKWARD_GROUPS ? tiles : ROT_BACKWARD_GROUPS); }
+
+static bool rot_sizes(uint32_t batch, uint32_t length, uint32_t heads, uint32_t kv_heads, uint32_t dim) {
+    return heads <= 1u << 16 && kv_heads <= 1u << 16 && heads + kv_heads > 0 && dim >= 8 && dim <= ROT_MAX_DIM && dim % 8 == 0 &&
+           length <= 1u << 31 && (uint64_t)batch * length < 1ull << 24;
+}
+
+static bool rot_args(const okt_norm_rotary* op, RotArgs& a) {
+    if (!op || !rot_sizes(op->batch, op->length, op->heads, op->kv_heads, op->head_dim) || !known_dtype(op->dtype)) return false;
+    if (op->rot_dim > op->head_dim || op->rot_dim % 8 != 0 || op->axes < 1 || op->axes > 8) return false;
+    if (op->kind != OKT_NORM_LAYER && op->kind != OKT_NORM_RMS) return false;
+    if (!(op->eps >= 0.0f) || !isfinite(op->eps)) return false;
+    if (op->rot_dim && (!op->d_inv_freq || !aligned(op->d_inv_freq, 4))) return false;
+    if (!aligned(op->d_positions, 4) || (!op->d_positions && op->axes != 1)) return false;
+    for (const float* w : {op->d_q_weight, op->d_k_weight})
+        if (!aligned(w, 4)) return false;
+    for (uint32_t j = 0; j < op->rot_dim / 2; ++j) {
+        if (op->axis_of_pair[j] >= op->axes) return false;
+        a.axis_of_pair[j] = op->axis_of_pair[j];
+    }
+    a.tokens = (uint64_t)op->batch * op->length;
+    a.length = op->length;
+    a.dim = op->head_dim;
+    a.rot = op->rot_dim;
+    a.kind = op->kind;
+    a.adjacent = op->adjacent != 0;
+    a.eps = op->eps;
+    a.inv_freq = op->d_inv_freq;
+    a.positions = op->d_positions;
+    a.position_stride[0] = op->position_stride[0];
+    a.position_stride[1] = op->position_stride[1];
+    const auto strides = [](const uint64_t* s) { return HeadStrides{s[0], s[1], s[2]}; };
+    a.t[0] = {op->heads, op->d_q_weight, strides(op->q_stride), strides(op->dq_stride), strides(op->q_out_stride)};
+    a.t[1] = {op->kv_heads, op->d_k_weight, strides(op->k_stride), strides(op->dk_stride), strides(op->k_out_stride)};
+    a.partial = nullptr;
+    if (a.tokens == 0) return true;
+    a.tile = rot_tile(a.tokens, op->heads + op->kv_heads, op->head_dim);
+    a.tiles = (a.tokens + a.tile - 1) / a.tile;
+    a.groups = rot_groups(a.tiles);
+    return true;
+}
+
+struct Placed { const void* p; HeadStrides s; uint32_t heads; };
+
+// An output whose tokens or heads are the same memory.
+static bool shares_places(const RotArgs& a, const HeadStrides& s, uint32_t heads) {
+    const uint64_t batch = a.tokens / a.length;
+    return (batch > 1 && s.batch < a.dim) || (a.length > 1 && s.row < a.dim) || (heads > 1 && s.head < a.dim);
+}
+
+// Whether an output and another tensor share an element: exactly where their strides are alike, as parts of one
+// projection's are, else by their first heads.  One in the very place of the other is seen by the caller.
+static bool clash(const Placed& x, const Placed& y, uint32_t dim, size_t e) {
+    if (!x.p || !y.p || !x.heads || !y.heads) return false;
+    if (x.s.batch == y.s.batch && x.s.row == y.s.row && (x.s.head == y.s.head || x.heads == 1 || y.heads == 1)) {
+        const uint64_t step = (x.heads == 1 ? y.s.head : x.s.head) * e, bytes = dim * e;
+        const bool before = (uintptr_t)x.p <= (uintptr_t)y.p;
+        const Placed &lo = before ? x : y, &hi = before ? y : x;
+        const uint64_t apart = (uint64_t)((uintptr_t)hi.p - (uintptr_t)lo.p);
+        for (uint64_t h = step ? apart / step : 0, n = 0; n < 2; ++h, ++n) {        // heads of the lower one around the higher one's first
+            if (h >= lo.heads) break;
+            const uint64_t from = h * step;
+            if (from < apart + bytes && apart < from + bytes) return true;
+        }
+        return false;
+    }
+    return overlap(x.p, dim * e, y.p, dim * e);
+}
+static bool same(const Placed& x, const Placed& y) {
+    return x.p == y.p && x.s.batch == y.s.batch && x.s.row == y.s.row && (x.s.head == y.s.head || x.heads == 1) && x.heads == y.heads;
+}
+
+template <typename T, int LANES>
+static void launch_rot(const RotArgs& a, const RotPointers& p, bool backward, hipStream_t s) {
+    if (backward) hipLaunchKernelGGL((norm_rotary_backward_kernel<T, LANES>), dim3(a.groups), dim3(ROT_THREADS), 0, s, a, p);
+    else hipLaunchKernelGGL((norm_rotary_forward_kernel<T, LANES>), dim3((unsigned)a.tiles), dim3(ROT_THREADS), 0, s, a, p);
+}
+template <typename T>
+static void launch_rot_lanes(const RotArgs& a, const RotPointers& p, bool backward, hipStream_t s) {
+    const uint32_t lanes = rot_lanes(a.dim);
+    if (lanes == 8) launch_rot<T, 8>(a, p, backward, s);
+    else if (lanes == 16) launch_rot<T, 16>(a, p, backward, s);
+    else launch_rot<T, 32>(a, p, backward, s);
+}
+static int launch_rot_type(int dtype, const RotArgs& a, const RotPointers& p, bool backward, hipStream_t s) {
+    timing_before(s);
+    if (dtype == OKT_F32) launch_rot_lanes<float>(a, p, backward, s);
+    else if (dtype == OKT_BF16) launch_rot_lanes<__bf16>(a, p, backward, s);
+    else launch_rot_lanes<_Float16>(a, p, backward, s);
+    timing_after(s);
+    return launch_status();
+}
+
+}  // namespace okt
+
+extern "C" {
+
+size_t okt_norm_rotary_workspace_bytes(uint32_t batch, uint32_t length, uint32_t heads, uint32_t kv_heads, uint32_t head_dim) {
+    using namespace okt;
+    if (!rot_sizes(batch, length, heads, kv_heads, head_dim)) return 0;
+    const uint64_t tokens = (uint64_t)batch * length;
+    if (tokens == 0) return 256;
+    const uint32_t tile = rot_tile(tokens, heads + kv_heads, head_dim);
+    return ((size_t)rot_groups((tokens + tile - 1) / tile) * 2 * head_dim * 4 + 255) / 256 * 256;
+}
+
+int okt_norm_rotary_forward(const okt_norm_rotary* op, const void* d_q, const void* d_k, void* d_q_out, void* d_k_out, void* stream) {
+    using namespace okt;
+    RotArgs a;
+    if (!rot_args(op, a)) return OKT_ERR_INVALID_ARG;
+    if (a.tokens == 0) return OKT_OK;
+    const size_t e = dtype_bytes(op->dtype);
+    const RotPointers p = {{d_q, d_k}, {nullptr, nullptr}, {d_q_out, d_k_out}};
+    Placed in[2], out[2];
+    for (int n = 0; n < 2; ++n) {
+        in[n] = {p.x[n], a.t[n].in, a.t[n].heads};
+        out[n] = {p.out[n], a.t[n].out, a.t[n].heads};
+        if (!a.t[n].heads) continue;
+        if (!p.x[n] || !p.out[n] || !aligned(p.x[n], e) || !aligned(p.out[n], e) || shares_places(a, a.t[n].out, a.t[n].heads)) return OKT_ERR_INVALID_ARG;
+    }
+    if (clash(out[0], out[1], a.dim, e)) return OKT_ERR_INVALID_ARG;
+    for (int n = 0; n < 2; ++n)
+        for (int m = 0; m < 2; ++m)
+            if (!(n == m && same(out[n], in[m])) && clash(out[n], in[m], a.dim, e)) return OKT_ERR_INVALID_ARG;
+    return launch_rot_type(op->dtype, a, p, false, (hipStream_t)stream);
+}
+
+int okt_norm_rotary_backward(const okt_norm_rotary* op, const void* d_q, const void* d_k, const void* d_dq, const void* d_dk,
+                             void* d_dq_out, void* d_dk_out, float* d_dq_weight_out, float* d_dk_weight_out, void* d_ws,
+                             size_t ws_bytes, void* stream) {
+    using namespace okt;
+    RotArgs a;
+    if (!rot_args(op, a)) return OKT_ERR_INVALID_ARG;
+    RotGradients g = {{d_dq_weight_out, d_dk_weight_out}};
+    const size_t e = dtype_bytes(op->dtype);
+    const RotPointers p = {{d_q, d_k}, {d_dq, d_dk}, {d_dq_out, d_dk_out}};
+    Placed in[2], d[2], out[2];
+    for (int n = 0; n < 2; ++n) {
+        if (!aligned(g.to[n], 4) || (g.to[n] && (!a.t[n].weight || !a.t[n].heads))) return OKT_ERR_INVALID_ARG;
+        in[n] = {a.t[n].weight ? p.x[n] : nullptr, a.t[n].in, a.t[n].heads};
+        d[n] = {p.d[n], a.t[n].d, a.t[n].heads};
+        out[n] = {p.out[n], a.t[n].out, a.t[n].heads};
+        if (!a.t[n].heads || a.tokens == 0) continue;
+        if ((a.t[n].weight && !p.x[n]) || !p.d[n] || !p.out[n] || !aligned(p.x[n], e) || !aligned(p.d[n], e) || !aligned(p.out[n], e) ||
+            shares_places(a, a.t[n].out, a.t[n].heads)) return OKT_ERR_INVALID_ARG;
+    }
+    const bool sums = g.to[0] || g.to[1];
+    if (a.tokens) {
+        if (clash(out[0], out[1], a.dim, e)) return OKT_ERR_INVALID_ARG;
+        for (int n = 0; n < 2; ++n)
+            for (int m = 0; m < 2; ++m)
+                if ((!(n == m && same(out[n], in[m])) && clash(out[n], in[m], a.dim, e)) ||
+                    (!(n == m && same(out[n], d[m])) && clash(out[n], d[m], a.dim, e))) return OKT_ERR_INVALID_ARG;
+        if (sums && (!d_ws || !aligned(d_ws, 256) || ws_bytes < (size_t)a.groups * 2 * a.dim * 4)) return OKT_ERR_WORKSPACE;
+        if (sums) a.partial = (float*)d_ws;
+        if (const int status = launch_rot_type(op->dtype, a, p, true, (hipStream_t)stream)) return status;
+    }
+    if (sums)
+        hipLaunchKernelGGL(norm_rotary_add_kernel, dim3((a.dim + ROT_ADD_COLS - 1) / ROT_ADD_COLS, 2), dim3(ROT_THREADS), 0, (hipStream_t)stream,
+                           (const float*)d_ws, a.tokens ? a.groups : 0, a.dim, g);
+    return sums ? launch_status() : OKT_OK;
+}
+
+}  // extern "C"
