@@ -736,6 +736,55 @@ int okt_norm_rotary_backward(const okt_norm_rotary* op, const void* d_q, const v
                              size_t ws_bytes, void* stream);
 
 /*
+ * The loss at the end: softmax cross entropy over a vocabulary, from the last hidden vectors and the output matrix, without
+ * the logits in memory.  For row n with label y = labels[n], 0 <= y < vocab,
+ *   s_v = h_n . W_v + b_v,  lse_n = log sum_v exp s_v,  loss_n = lse_n - s_y
+ * and a row whose label is outside (-100, say) has loss 0 and lse 0, takes part in no gradient whatever its h holds, and costs nothing.
+ * Backward, g_n being the gradient of loss_n,  d_nv = g_n (exp(s_nv - lse_n) - [v = y]):
+ *   dh_n = sum_v d_nv W_v,  dW_v = sum_n d_nv h_n,  db_v = sum_n d_nv
+ * The logits are made again, a piece of the vocabulary at a time.  Products are taken by the matrix units from 16-bit inputs with fp32
+ * sums.  For the second products d is rounded to the tensors' type, so dh and dW have the precision of that type, also where dW is fp32 (so that it
+ * can lie in the flat vector of the accumulate calls); db is summed in fp32 before that rounding.  In fp16 d is scaled by a power of two from the
+ * largest |g|; a d below 2^-39 of that is rounded to 0.  A bias of -infinity takes an entry out of the vocabulary.
+ * Tensors are rows of `width` contiguous elements, 16-byte aligned, strides (in elements; 0 stands for width) multiples of 8, at most
+ * 2^20; an fp32 dW needs 4-byte alignment and any stride.
+ */
+typedef struct okt_cross_entropy {
+    uint64_t rows;                 /* at most 2^22; 0: nothing (backward: zeros to dW and db) */
+    uint32_t width;                /* 8, 16, ... 2^15 */
+    uint32_t vocab;                /* 1 to 2^22 */
+    int32_t dtype;                 /* of h, W and dh: OKT_BF16 or OKT_F16 */
+    int32_t dweight_dtype;         /* backward: `dtype` or OKT_F32 */
+    uint32_t dloss_stride;         /* backward: 1, or 0 for one g for all rows */
+    uint32_t reserved;             /* 0 */
+    const float* d_bias;           /* fp32[vocab] on the device, or NULL */
+    uint64_t h_stride, weight_stride, dh_stride, dweight_stride;
+} okt_cross_entropy;
+
+/* Bytes of workspace that suffice for both passes; 0 if sizes are out of range.  Pure host arithmetic. */
+size_t okt_cross_entropy_workspace_bytes(uint64_t rows, uint32_t width, uint32_t vocab);
+
+/*
+ *   d_labels    in   int64[rows]
+ *   d_loss_out  out  fp32[rows]
+ *   d_lse_out   out  fp32[rows]; NULL if no backward pass follows
+ * Outputs overlap neither each other nor an input.  Four launches.
+ */
+int okt_cross_entropy_forward(const okt_cross_entropy* op, const void* d_h, const void* d_weight, const int64_t* d_labels,
+                              float* d_loss_out, float* d_lse_out, void* d_ws, size_t ws_bytes, void* stream);
+
+/*
+ *   d_lse    in   as the forward pass wrote it
+ *   d_dloss  in   fp32[rows] or fp32[1], see dloss_stride
+ *   d_dh_out, d_dweight_out, d_dbias_out  out  overwritten; each may be NULL (not all; the last one has to be without a bias), and
+ *            none overlaps another or an input, from its first element to its last
+ * Two launches and up to three a piece of the vocabulary, and two more.
+ */
+int okt_cross_entropy_backward(const okt_cross_entropy* op, const void* d_h, const void* d_weight, const int64_t* d_labels,
+                               const float* d_lse, const float* d_dloss, void* d_dh_out, void* d_dweight_out, float* d_dbias_out,
+                               void* d_ws, size_t ws_bytes, void* stream);
+
+/*
  * AdamW over many tensors in one launch, states in 32 bits or in 8.  For an element p with gradient g, averages m and v and
  * t = the step, counted from 1:
  *   g = grad_scale g,  m = beta1 m + (1 - beta1) g,  v = beta2 v + (1 - beta2) g^2,  rate = lr rate_scale

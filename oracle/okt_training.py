@@ -159,3 +159,34 @@ def norm_rotary_backward(x, dy, angle, *, weight=None, kind="rms", eps=1e-6, adj
     if kind == "layer":
         dx = dx - w.mean(-1, keepdims=True)
     return r * dx, (d * h).sum((0, 1, 2))
+
+
+# ------------------------------------------------------------------ cross entropy over a vocabulary
+
+def logits(h, weight, bias=None):
+    s = h @ weight.T
+    return s if bias is None else s + bias
+
+
+def cross_entropy(h, weight, labels, bias=None):
+    """(loss, lse) of every row; 0 where the label is not in the vocabulary."""
+    rows = np.flatnonzero((labels >= 0) & (labels < weight.shape[0]))
+    loss, lse = np.zeros(len(labels)), np.zeros(len(labels))
+    s = logits(h[rows], weight, bias)
+    top = s.max(1, keepdims=True)
+    lse[rows] = np.log(np.exp(s - top).sum(1)) + top[:, 0]
+    loss[rows] = lse[rows] - s[np.arange(len(rows)), labels[rows]]
+    return loss, lse
+
+
+def cross_entropy_backward(h, weight, labels, g, bias=None):
+    """(dh, dweight, dbias)."""
+    rows = np.flatnonzero((labels >= 0) & (labels < weight.shape[0]))
+    s = logits(h[rows], weight, bias)
+    p = np.exp(s - s.max(1, keepdims=True))
+    d = p / p.sum(1, keepdims=True)
+    d[np.arange(len(rows)), labels[rows]] -= 1.0
+    d *= g[rows, None]
+    dh = np.zeros(h.shape)
+    dh[rows] = d @ weight
+    return dh, d.T @ h[rows], d.sum(0)

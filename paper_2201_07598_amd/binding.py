@@ -68,6 +68,9 @@ SIGNATURES = {
     "okt_norm_rotary_workspace_bytes": (c_sz, [c_u32] * 5),
     "okt_norm_rotary_forward": (c_int, [c_vp] * 6),
     "okt_norm_rotary_backward": (c_int, [c_vp] * 10 + [c_sz, c_vp]),
+    "okt_cross_entropy_workspace_bytes": (c_sz, [c_u64, c_u32, c_u32]),
+    "okt_cross_entropy_forward": (c_int, [c_vp] * 7 + [c_sz, c_vp]),
+    "okt_cross_entropy_backward": (c_int, [c_vp] * 10 + [c_sz, c_vp]),
     "okt_adamw_plan_bytes": (c_sz, [c_vp, c_u32]),
     "okt_adamw_plan": (c_int, [c_vp, c_u32, c_int, c_vp, c_sz, c_vp]),
     "okt_adamw_step": (c_int, [c_vp, c_vp, c_vp]),
@@ -879,6 +882,75 @@ def okt_norm_rotary_backward(q, k, dq, dk, dq_out, dk_out, inv_freq, ws=None, *,
     _check("okt_norm_rotary_backward", load_library().okt_norm_rotary_backward(
         op, pq, pk, pd, pdk, po, pko, _parameter(dq_weight_out, dim, "dq_weight_out"), _parameter(dk_weight_out, dim, "dk_weight_out"),
         _ptr(ws, _TORCH.uint8, "ws", True), 0 if ws is None else ws.numel(), handle))
+
+
+# --------------------------------------------------------------------------
+# Cross entropy over a vocabulary
+_CROSS_ENTROPY = struct.Struct("=Q2I2i2IQ4Q")        # okt_cross_entropy
+
+
+def okt_cross_entropy_workspace_bytes(rows: int, width: int, vocab: int) -> int:
+    return load_library().okt_cross_entropy_workspace_bytes(int(rows), int(width), int(vocab))
+
+
+def _cross_entropy_inputs(h, weight, labels):
+    if h.dtype not in (_torch().bfloat16, _TORCH.float16):
+        raise TypeError(f"h must be bfloat16 or float16, got {h.dtype}")
+    _dtype_code(h, "h")
+    if h.dim() != 2 or weight.dim() != 2:
+        raise ValueError("h must be [rows, width] and weight [vocab, width]")
+    rows, width = h.shape
+    if weight.shape[1] != width:
+        raise ValueError("h and weight must agree in width")
+    ph, sh = _rows(h, h.dtype, h.shape, "h")
+    pw, sw = _rows(weight, h.dtype, weight.shape, "weight")
+    if labels.numel() != rows:
+        raise ValueError(f"labels needs one element a row ({rows}), got {labels.numel()}")
+    return rows, width, weight.shape[0], ph, sh, pw, sw, _ptr(labels, _TORCH.int64, "labels")
+
+
+def _per_row(t, rows, name, allow_none=False):
+    if t is not None and t.numel() != rows:
+        raise ValueError(f"{name} needs one element a row ({rows}), got {t.numel()}")
+    return _ptr(t, _TORCH.float32, name, allow_none)
+
+
+def okt_cross_entropy_forward(h, weight, labels, loss_out, lse_out, ws, *, bias=None, stream=None) -> None:
+    """loss = logsumexp(h weight' + bias) - the label's logit for every row of h [rows, width] (bfloat16 or float16), weight
+    [vocab, width]; labels int64 [rows]; 0 for a row whose label is not in the vocabulary.  loss_out and
+    lse_out float32 [rows]; lse_out may be None where no backward pass follows; bias float32 [vocab]."""
+    rows, width, vocab, ph, sh, pw, sw, py = _cross_entropy_inputs(h, weight, labels)
+    op = _CROSS_ENTROPY.pack(rows, width, vocab, _DTYPES[h.dtype], _DTYPES[h.dtype], 1, 0, _parameter(bias, vocab, "bias"), sh, sw, 0, 0)
+    ploss, plse = _per_row(loss_out, rows, "loss_out"), _per_row(lse_out, rows, "lse_out", True)
+    pws = _ptr(ws, _TORCH.uint8, "ws")
+    handle = _stream_for(stream, h, weight, labels, loss_out, lse_out, ws, bias)
+    _check("okt_cross_entropy_forward", load_library().okt_cross_entropy_forward(op, ph, pw, py, ploss, plse, pws, ws.numel(), handle))
+
+
+def okt_cross_entropy_backward(h, weight, labels, lse, dloss, dh_out, dweight_out, ws, *, bias=None, dbias_out=None,
+                               stream=None) -> None:
+    """Gradients of h, weight and bias from that of the loss: dloss float32 [rows], or one value for all rows (one element, or
+    expanded from one).  dh_out is of h's type, dweight_out of that or float32; either may be None."""
+    rows, width, vocab, ph, sh, pw, sw, py = _cross_entropy_inputs(h, weight, labels)
+    f32 = _TORCH.float32
+    if not dloss.is_cuda:
+        raise TypeError("dloss must be a CUDA tensor (device memory)")
+    if dloss.dtype is not f32:
+        raise TypeError(f"dloss must have dtype {f32}, got {dloss.dtype}")
+    if dloss.numel() != rows and dloss.numel() != 1:
+        raise ValueError(f"dloss needs one element a row ({rows}) or one, got {dloss.numel()}")
+    one = dloss.numel() == 1 or all(s == 0 for s in dloss.stride())
+    if not one and not dloss.is_contiguous():
+        raise TypeError("dloss must be contiguous, or one value for all rows")
+    pdh, sdh = _rows(dh_out, h.dtype, h.shape, "dh_out", True)
+    wide = dweight_out is not None and dweight_out.dtype is f32
+    pdw, sdw = _rows(dweight_out, f32 if wide else h.dtype, weight.shape, "dweight_out", True)
+    op = _CROSS_ENTROPY.pack(rows, width, vocab, _DTYPES[h.dtype], 0 if wide else _DTYPES[h.dtype], 0 if one else 1, 0,
+                             _parameter(bias, vocab, "bias"), sh, sw, sdh, sdw)
+    plse, pdb, pws = _per_row(lse, rows, "lse"), _parameter(dbias_out, vocab, "dbias_out"), _ptr(ws, _TORCH.uint8, "ws")
+    handle = _stream_for(stream, h, weight, labels, lse, dloss, dh_out, dweight_out, dbias_out, bias, ws)
+    _check("okt_cross_entropy_backward", load_library().okt_cross_entropy_backward(
+        op, ph, pw, py, plse, dloss.data_ptr(), pdh, pdw, pdb, pws, ws.numel(), handle))
 
 
 # --------------------------------------------------------------------------

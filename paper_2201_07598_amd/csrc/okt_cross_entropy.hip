@@ -1,0 +1,687 @@
+// okt_cross_entropy_forward / _backward: softmax cross entropy of s = h W' + b over a vocabulary, and its gradient, without the logits.
+//
+//   loss_n = lse_n - s_ny,  lse_n = log sum_v exp s_nv,    d_nv = g_n (exp(s_nv - lse_n) - [v = y_n])
+//   dh = d W,  dW = d' h,  db_v = sum_n d_nv
+//
+// Rows without a label take no part: the others' numbers are listed first, their h copied side by side (and
+// padded to whole tiles with zeros), and every later kernel works on the list, whose length it reads from device memory.  With 15 % of the
+// rows labelled that is 15 % of the work.
+//
+// Forward, a tile of logits is a matrix product whose epilogue leaves the largest and the sum of exponentials of its part of a row; a
+// second kernel joins a row's parts.  Backward the logits are made again, a piece of the vocabulary at a time, and leave the
+// epilogue as d, rounded to the tensors' type, in the workspace; two more products take it from there.  dW of a piece is final; dh
+// is summed over the pieces in fp32.  Four products where a kept matrix of logits would need three.
+//
+// In fp16 d is taken times a power of two that brings the largest |g| to between 2^14 and 2^15, and divided out of the sums: g is one over the number of rows
+// and p one over the vocabulary's size, and fp16 ends at 2^-24.
+#include <math.h>
+
+#include "okt_product.h"
+
+namespace okt {
+
+constexpr uint32_t CE_PAD = 256;                                     // rows, and columns of a piece, are padded to the largest tile
+constexpr uint64_t CE_PIECE_BYTES = 512ull << 20;                    // of d in the workspace
+constexpr uint32_t CE_SPLIT_TILES = 512;                             // of dh and parts of k together, where tiles are fewer
+constexpr uint32_t CE_MAX = 1u << 22;                                // rows, vocabulary
+constexpr uint32_t CE_MAX_WIDTH = 1u << 15;
+constexpr int CE_THREADS = 256;
+constexpr float LOG2E = 1.44269504088896340736f;
+constexpr double LN2 = 0.69314718055994530942;
+
+typedef ProductShape<4, 4, 2, 2> Large;                              // 256 x 256, one workgroup a CU
+typedef ProductShape<2, 2, 2, 2> Small;                              // 128 x 128, two
+
+template <typename T> constexpr bool RAISED = false;
+template <> constexpr bool RAISED<_Float16> = true;
+
+struct CeHeader { uint32_t count; float raise, lower; uint32_t pad; };
+
+struct CeArgs {
+    uint32_t rows, width, vocab, rows_pad, width_pad;
+    uint64_t h_stride, weight_stride, dh_stride, dweight_stride;
+    uint32_t dloss_step;
+    const float* bias;
+    const int64_t* labels;
+    // workspace
+    CeHeader* header;
+    uint32_t* list;                                                  // numbers of the labelled rows
+    int32_t* label_of;                                               // of listed row n
+    void* h;                                                         // [rows_pad][width_pad]
+    float* stats;                                                    // forward: [parts][rows_pad][2]
+    float* said;                                                     // forward: s_ny
+    float *lse_of, *g_of;                                            // backward, of listed row n
+    void* d;                                                         // [rows_pad][piece]
+    float* dh_sums;                                                  // [parts][rows of whole tiles][width_pad]
+    float* dbias_sums;                                               // [parts][vocab_pad]
+    uint32_t piece, vocab_pad;
+};
+
+// ------------------------------------------------------------------ the list of labelled rows
+
+constexpr int CE_LIST_THREADS = 1024, CE_LIST_EACH = 8;
+
+__device__ __forceinline__ bool labelled(int64_t y, uint32_t vocab) { return y >= 0 && y < (int64_t)vocab; }
+
+__global__ __launch_bounds__(CE_LIST_THREADS) void cross_entropy_list_kernel(CeArgs a, float* loss, float* lse, const float* dloss, bool raised) {
+    __shared__ uint32_t waves[CE_LIST_THREADS / WAVE];
+    __shared__ float tops[CE_LIST_THREADS / WAVE];
+    const int lane = lane_id(), wave = threadIdx.x / WAVE;
+    uint32_t before = 0;
+    float top = 0.0f;
+    for (uint64_t base = 0; base < a.rows; base += CE_LIST_THREADS * CE_LIST_EACH) {
+        const uint64_t first = base + threadIdx.x * CE_LIST_EACH;
+        int64_t y[CE_LIST_EACH];
+        uint32_t mine = 0;
+#pragma unroll
+        for (int i = 0; i < CE_LIST_EACH; ++i) y[i] = first + i < a.rows ? a.labels[first + i] : -1;
+#pragma unroll
+        for (int i = 0; i < CE_LIST_EACH; ++i) mine += labelled(y[i], a.vocab);
+        const uint32_t scan = wave_inclusive_scan_u32(mine);
+        if (lane == WAVE - 1) waves[wave] = scan;
+        __syncthreads();
+        uint32_t at = before + scan - mine, all = 0;
+#pragma unroll
+        for (int w = 0; w < CE_LIST_THREADS / WAVE; ++w) {
+            if (w < wave) at += waves[w];
+            all += waves[w];
+        }
+        before += all;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < CE_LIST_EACH; ++i) {
+            if (first + i >= a.rows) break;
+            if (labelled(y[i], a.vocab)) {
+                a.list[at] = (uint32_t)(first + i);
+                a.label_of[at++] = (int32_t)y[i];
+                if (raised) {
+                    const float g = fabsf(dloss[(first + i) * a.dloss_step]);
+                    top = g > top ? g : top;                         // a NaN does not raise it
+                }
+            } else if (loss) {
+                loss[first + i] = 0.0f;
+                if (lse) lse[first + i] = 0.0f;
+            }
+        }
+    }
+    if (raised) {
+#pragma unroll
+        for (int m = 1; m < WAVE; m <<= 1) top = fmaxf(top, __shfl_xor(top, m, WAVE));
+        if (lane == 0) tops[wave] = top;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < CE_LIST_THREADS / WAVE; ++w) top = fmaxf(top, tops[w]);
+    }
+    if (threadIdx.x == 0) {
+        int e = 0;                                                   // top in [2^(e - 1), 2^e)
+        if (top > 0.0f && top < __builtin_inff()) frexpf(top, &e);
+        const int by = raised && top > 0.0f && top < __builtin_inff() ? min(max(15 - e, -120), 120) : 0;
+        *a.header = {before, ldexpf(1.0f, by), ldexpf(1.0f, -by), 0};
+    }
+}
+
+// A wave a row: listed rows of h side by side, zeros behind the last one up to whole tiles; and zeros for the gradients of rows that
+// are not listed.
+template <typename T>
+__global__ __launch_bounds__(CE_THREADS) void cross_entropy_gather_kernel(CeArgs a, const T* h, const float* lse, const float* dloss, T* dh) {
+    typedef typename Eight<T>::vec vec;
+    const uint32_t n = blockIdx.x * (CE_THREADS / WAVE) + threadIdx.x / WAVE, lane = threadIdx.x % WAVE;
+    const uint32_t count = a.header->count;
+    if (n < (count + CE_PAD - 1) / CE_PAD * CE_PAD) {
+        const bool there = n < count;
+        const uint32_t row = there ? a.list[n] : 0;
+        const T* from = h + row * a.h_stride;
+        T* to = (T*)a.h + (uint64_t)n * a.width_pad;
+        for (uint32_t c = lane * 8; c < a.width_pad; c += WAVE * 8) {
+            vec v = {};
+            if (there && c < a.width) v = *reinterpret_cast<const vec*>(from + c);
+            *reinterpret_cast<vec*>(to + c) = v;
+        }
+        if (lane == 0 && !there) a.label_of[n] = -1;
+        if (lane == 0 && dloss) {
+            a.lse_of[n] = there ? lse[row] : 0.0f;
+            a.g_of[n] = there ? dloss[(uint64_t)row * a.dloss_step] : 0.0f;
+        }
+    }
+    if (dh && n < a.rows && !labelled(a.labels[n], a.vocab))
+        for (uint32_t c = lane * 8; c < a.width; c += WAVE * 8) *reinterpret_cast<vec*>(dh + n * a.dh_stride + c) = vec{};
+}
+
+// ------------------------------------------------------------------ logits
+
+// What is added to a tile's logits, in LDS: the bias, -infinity past the vocabulary.
+template <class S>
+__device__ __forceinline__ void load_bias(float* tile, const CeArgs& a, uint32_t v) {
+    for (uint32_t i = threadIdx.x; i < S::TILE_M; i += S::THREADS) tile[i] = v + i >= a.vocab ? -__builtin_inff() : a.bias ? a.bias[v + i] : 0.0f;
+}
+
+// Logits of a lane's row of column n of the wave's squares; `part`: the wave's part of that tile.
+template <class S>
+__device__ __forceinline__ void logits_of_row(float (&s)[S::MT * 16], const f32x16 (&c)[S::MT][S::NT], int n, const float* part, bool biased) {
+#pragma unroll
+    for (int m = 0; m < S::MT; ++m)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[m * 16 + r] = c[m][n][r];
+    if (!biased) return;
+#pragma unroll
+    for (int m = 0; m < S::MT; ++m)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const float4 b = *reinterpret_cast<const float4*>(part + m * 32 + threadIdx.x % WAVE / 32 * 16 + q * 4);
+            s[m * 16 + 4 * q] += b.x;
+            s[m * 16 + 4 * q + 1] += b.y;
+            s[m * 16 + 4 * q + 2] += b.z;
+            s[m * 16 + 4 * q + 3] += b.w;
+        }
+}
+
+template <typename T, class S>
+__device__ __forceinline__ void logits(f32x16 (&c)[S::MT][S::NT], const CeArgs& a, const T* weight, uint32_t v, uint32_t n, char* lds) {
+    KMajor<T, S::TILE_M, S::WAVES, true> x(weight + v * a.weight_stride, weight + (a.vocab - 1) * a.weight_stride + a.width, (uint32_t)(a.weight_stride * 2));
+    const T* h = (const T*)a.h;
+    KMajor<T, S::TILE_N, S::WAVES, false> y(h + (uint64_t)n * a.width_pad, h + (uint64_t)a.rows_pad * a.width_pad, a.width_pad * 2);
+    product<T, S>(c, x, y, lds, a.width);
+}
+
+template <typename T, class S>
+__global__ __launch_bounds__(S::THREADS) void cross_entropy_forward_kernel(CeArgs a, const T* weight) {
+    __shared__ __attribute__((aligned(1024))) char lds[S::BYTES];
+    __shared__ float bias[S::TILE_M];
+    const uint32_t count = a.header->count;
+    const TilePlace tile = tile_place(blockIdx.x, (a.vocab + S::TILE_M - 1) / S::TILE_M, (count + S::TILE_N - 1) / S::TILE_N);
+    if (!tile.there) return;
+    load_bias<S>(bias, a, tile.m * S::TILE_M);
+    f32x16 c[S::MT][S::NT];
+    logits<T, S>(c, a, weight, tile.m * S::TILE_M, tile.n * S::TILE_N, lds);
+    const uint32_t lane = threadIdx.x % WAVE, part = tile.m * S::WM + S::wave_m();
+    const uint32_t v0 = part * (S::MT * 32), n0 = tile.n * S::TILE_N + S::wave_n() * (S::NT * 32) + lane % 32;
+    const bool biased = a.bias || v0 + S::MT * 32 > a.vocab;
+#pragma unroll
+    for (int n = 0; n < S::NT; ++n) {
+        const uint32_t row = n0 + n * 32;
+        float s[S::MT * 16];
+        logits_of_row<S>(s, c, n, bias + S::wave_m() * (S::MT * 32), biased);
+        float top = -__builtin_inff();
+#pragma unroll
+        for (int i = 0; i < S::MT * 16; ++i) top = fmaxf(top, s[i]);
+        top = max_halves(top);
+        const float base = top == -__builtin_inff() ? 0.0f : -top * LOG2E;
+        float sum = 0.0f;
+#pragma unroll
+        for (int i = 0; i < S::MT * 16; ++i) sum += __builtin_amdgcn_exp2f(fmaf(s[i], LOG2E, base));
+        sum = sum_halves(sum);
+        if (lane < 32 && row < count)
+            *reinterpret_cast<float2*>(a.stats + ((uint64_t)part * a.rows_pad + row) * 2) = make_float2(top, sum);
+        const uint32_t mine = (uint32_t)a.label_of[row] - v0 - lane / 32 * 16;          // far above a wave's part where it is none of its
+        if (__ballot(mine < S::MT * 32u)) {
+#pragma unroll
+            for (int m = 0; m < S::MT; ++m)
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    if (mine == m * 32u + r) a.said[row] = s[m * 16 + r];
+        }
+    }
+}
+
+// Sixteen rows a workgroup, sixteen threads a row, each every sixteenth part.
+__global__ __launch_bounds__(CE_THREADS) void cross_entropy_join_kernel(CeArgs a, uint32_t parts, float* loss, float* lse) {
+    __shared__ float tops[16][17], sums[16][17];
+    const uint32_t count = a.header->count, r = threadIdx.x % 16, share = threadIdx.x / 16, row = blockIdx.x * 16 + r;
+    if (blockIdx.x * 16 >= count) return;
+    float top = -__builtin_inff(), sum = 0.0f;
+    const auto add = [&](float t, float s) {
+        const float more = fmaxf(top, t);
+        if (more == -__builtin_inff()) {
+            sum += s;                                                // 0, or NaN
+            return;
+        }
+        sum = sum * __builtin_amdgcn_exp2f((top - more) * LOG2E) + s * __builtin_amdgcn_exp2f((t - more) * LOG2E);
+        top = more;
+    };
+    if (row < count)
+#pragma unroll 8
+        for (uint32_t p = share; p < parts; p += 16) {
+            const float2 v = *reinterpret_cast<const float2*>(a.stats + ((uint64_t)p * a.rows_pad + row) * 2);
+            add(v.x, v.y);
+        }
+    tops[share][r] = top;
+    sums[share][r] = sum;
+    __syncthreads();
+    if (share != 0 || row >= count) return;
+    for (int k = 1; k < 16; ++k) add(tops[k][r], sums[k][r]);
+    const float all = top == -__builtin_inff() && sum == 0.0f ? top : top + logf(sum);
+    const uint32_t to = a.list[row];
+    loss[to] = all - a.said[row];
+    if (lse) lse[to] = all;
+}
+
+// ------------------------------------------------------------------ the gradient of the logits
+
+// Sums over the 32 lanes of a half of N values each; lane l % 32 gets those of values N / 32 (l % 32) on.  Every step hands over the half of the
+// values that the other lane goes on with, so all steps together cost two exchanges a value and not five.
+template <int N>
+__device__ __forceinline__ void sums_over_lanes(float (&v)[N]) {
+    static_assert(N == 64 || N == 32, "");
+#pragma unroll
+    for (int i = 0; i < N / 2; ++i) {
+        const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v[i]), __float_as_uint(v[i + N / 2]), false, false);
+        v[i] = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+    }
+#define OKT_HALVE(KEEP, BIT, CTRL)                                                                                         \
+    _Pragma("unroll") for (int i = 0; i < (KEEP); ++i) {                                                                  \
+        const bool upper = threadIdx.x & (BIT);                                                                             \
+        const float mine = upper ? v[i + (KEEP)] : v[i], theirs = upper ? v[i] : v[i + (KEEP)];                            \
+        v[i] = mine + __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(theirs), CTRL, 0xf, 0xf, true));             \
+    }
+    OKT_HALVE(N / 4, 8, 0x140)        // row_mirror
+    OKT_HALVE(N / 8, 4, 0x141)        // row_half_mirror
+    OKT_HALVE(N / 16, 2, 0x4E)        // quad_perm [2, 3, 0, 1]
+    OKT_HALVE(N / 32, 1, 0xB1)        // quad_perm [1, 0, 3, 2]
+#undef OKT_HALVE
+}
+
+// d of a piece of the vocabulary that begins at `from`.
+template <typename T, class S>
+__global__ __launch_bounds__(S::THREADS) void cross_entropy_gradient_kernel(CeArgs a, const T* weight, uint32_t from, uint32_t columns) {
+    __shared__ __attribute__((aligned(1024))) char lds[S::BYTES];
+    __shared__ float bias[S::TILE_M];
+    const uint32_t count = a.header->count;
+    const TilePlace tile = tile_place(blockIdx.x, (columns + S::TILE_M - 1) / S::TILE_M, (count + S::TILE_N - 1) / S::TILE_N);
+    if (!tile.there) return;
+    load_bias<S>(bias, a, from + tile.m * S::TILE_M);
+    f32x16 c[S::MT][S::NT];
+    logits<T, S>(c, a, weight, from + tile.m * S::TILE_M, tile.n * S::TILE_N, lds);
+    const uint32_t lane = threadIdx.x % WAVE, at = tile.m * S::TILE_M + S::wave_m() * (S::MT * 32), v0 = from + at;
+    const uint32_t part = tile.n * S::WN + S::wave_n(), n0 = part * (S::NT * 32) + lane % 32;
+    const bool biased = a.bias || v0 + S::MT * 32 > a.vocab;
+    const float raise = RAISED<T> ? a.header->raise : 1.0f;
+    float sums[S::MT * 16];
+#pragma unroll
+    for (int i = 0; i < S::MT * 16; ++i) sums[i] = 0.0f;
+#pragma unroll
+    for (int n = 0; n < S::NT; ++n) {
+        const uint32_t row = n0 + n * 32;
+        const bool there = row < count;
+        const float g = a.g_of[row], base = -a.lse_of[row] * LOG2E;
+        const uint32_t mine = (uint32_t)a.label_of[row] - v0 - lane / 32 * 16;
+float s[S::MT * 16];
+        logits_of_row<S>(s, c, n, bias + S::wave_m() * (S::MT * 32), biased);
+#pragma unroll
+        for (int i = 0; i < S::MT * 16; ++i) s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], LOG2E, base));
+        if (__ballot(mine < S::MT * 32u)) {
+#pragma unroll
+            for (int m = 0; m < S::MT; ++m)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[m * 16 + r] -= mine == m * 32u + r ? 1.0f : 0.0f;
+        }
+        T* to = (T*)a.d + (uint64_t)row * a.piece + at + lane / 32 * 16;
+#pragma unroll
+        for (int m = 0; m < S::MT; ++m) {
+            f32x8 low, high;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const float d = there ? s[m * 16 + r] * g : 0.0f;       // rows behind the last one: zeros, whatever the bias is
+                sums[m * 16 + r] += d;
+                (r < 8 ? low : high)[r % 8] = RAISED<T> ? d * raise : d;
+            }
+            store_eight(to + m * 32, low);
+            store_eight(to + m * 32 + 8, high);
+        }
+    }
+    if (!a.dbias_sums) return;
+    sums_over_lanes(sums);
+    constexpr int EACH = S::MT * 16 / 32;
+    const uint32_t first = lane % 32 * EACH;
+    float* to = a.dbias_sums + (uint64_t)part * a.vocab_pad + v0 + first / 16 * 32 + lane / 32 * 16 + first % 16;
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) to[i] = sums[i];
+}
+
+// ------------------------------------------------------------------ gradients of h, W and the bias
+
+// How many parts the sum over a piece is dealt to, so that a few rows' tiles fill the chip as well.
+struct Split { uint32_t tiles_n, parts; };
+template <class S>
+__device__ __forceinline__ Split dh_split(uint32_t count, uint32_t width_pad) {
+    const uint32_t tiles_n = (count + S::TILE_N - 1) / S::TILE_N, tiles = max(1u, tiles_n * ((width_pad + S::TILE_M - 1) / S::TILE_M));
+    return {tiles_n, max(1u, CE_SPLIT_TILES / 2 / tiles)};
+}
+
+// dh += d W over a piece.
+template <typename T, class S>
+__global__ __launch_bounds__(S::THREADS) void cross_entropy_dh_kernel(CeArgs a, const T* weight, uint32_t from, uint32_t columns) {
+    __shared__ __attribute__((aligned(1024))) char lds[S::BYTES];
+    const uint32_t count = a.header->count, tiles_m = (a.width_pad + S::TILE_M - 1) / S::TILE_M;
+    if (count == 0) return;
+    const Split split = dh_split<S>(count, a.width_pad);
+    const TilePlace tile = tile_place(blockIdx.x, tiles_m, split.tiles_n * split.parts);
+    if (!tile.there) return;
+    const uint32_t part = tile.n / split.tiles_n, n_tile = tile.n % split.tiles_n;
+    const uint32_t pieces = (columns + PRODUCT_K - 1) / PRODUCT_K;
+    const uint32_t k0 = (uint32_t)((uint64_t)pieces * part / split.parts) * PRODUCT_K, k1 = (uint32_t)((uint64_t)pieces * (part + 1) / split.parts) * PRODUCT_K;
+    const uint32_t col = tile.m * S::TILE_M, row = n_tile * S::TILE_N;
+    Transposed<T, S::TILE_M, S::WAVES, true> x(weight + (from + k0) * a.weight_stride + col, weight + (a.vocab - 1) * a.weight_stride + a.width,
+                                               a.weight_stride * 2, a.width - min(a.width, col));
+    const T* d = (const T*)a.d;
+    KMajor<T, S::TILE_N, S::WAVES, false> y(d + (uint64_t)row * a.piece + k0, d + (uint64_t)a.rows_pad * a.piece, a.piece * 2);
+    f32x16 c[S::MT][S::NT];
+    product<T, S>(c, x, y, lds, k1 - k0);
+    const uint32_t lane = threadIdx.x % WAVE, m0 = col + S::wave_m() * (S::MT * 32) + lane / 32 * 16, n0 = row + S::wave_n() * (S::NT * 32) + lane % 32;
+    const bool first = from == 0;
+#pragma unroll
+    for (int n = 0; n < S::NT; ++n) {
+        if (n0 + n * 32 >= count) continue;
+        float* to = a.dh_sums + ((uint64_t)part * split.tiles_n * S::TILE_N + n0 + n * 32) * a.width_pad + m0;
+#pragma unroll
+        for (int m = 0; m < S::MT; ++m) {
+            if (m0 + m * 32 >= a.width_pad) continue;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                float4* at = reinterpret_cast<float4*>(to + m * 32 + q * 4);
+                float4 v = make_float4(c[m][n][4 * q], c[m][n][4 * q + 1], c[m][n][4 * q + 2], c[m][n][4 * q + 3]);
+                if (!first) {
+                    const float4 w = *at;
+                    v = make_float4(v.x + w.x, v.y + w.y, v.z + w.z, v.w + w.w);
+                }
+                *at = v;
+            }
+        }
+    }
+}
+
+// The parts of dh, rounded; a wave a row.
+template <typename T, class S>
+__global__ __launch_bounds__(CE_THREADS) void cross_entropy_dh_join_kernel(CeArgs a, T* dh) {
+    const uint32_t n = blockIdx.x * (CE_THREADS / WAVE) + threadIdx.x / WAVE, lane = threadIdx.x % WAVE, count = a.header->count;
+    if (n >= count) return;
+    const Split split = dh_split<S>(count, a.width_pad);
+    const float lower = RAISED<T> ? a.header->lower : 1.0f;
+    T* to = dh + a.list[n] * a.dh_stride;
+    for (uint32_t c = lane * 8; c < a.width; c += WAVE * 8) {
+        f32x8 sum = 0.0f;
+#pragma unroll 4
+        for (uint32_t p = 0; p < split.parts; ++p)
+            sum += load_eight(a.dh_sums + ((uint64_t)p * split.tiles_n * S::TILE_N + n) * a.width_pad + c);
+        store_eight(to + c, sum * lower);
+    }
+}
+
+// dW = d' h over the listed rows, of the vocabulary's piece.
+template <typename T, typename W, class S>
+__global__ __launch_bounds__(S::THREADS) void cross_entropy_dweight_kernel(CeArgs a, W* dweight, uint32_t from, uint32_t columns) {
+    __shared__ __attribute__((aligned(1024))) char lds[S::BYTES];
+    const uint32_t count = a.header->count;
+    const TilePlace tile = tile_place(blockIdx.x, (a.width_pad + S::TILE_M - 1) / S::TILE_M, (columns + S::TILE_N - 1) / S::TILE_N);
+    if (!tile.there) return;
+    const uint32_t col = tile.m * S::TILE_M, v = tile.n * S::TILE_N;
+    const T *h = (const T*)a.h, *d = (const T*)a.d;
+    Transposed<T, S::TILE_M, S::WAVES, true> x(h + col, h + (uint64_t)a.rows_pad * a.width_pad, a.width_pad * 2, a.width_pad - min(a.width_pad, col));
+    Transposed<T, S::TILE_N, S::WAVES, false> y(d + v, d + (uint64_t)a.rows_pad * a.piece, (uint64_t)a.piece * 2, a.piece - v);
+    f32x16 c[S::MT][S::NT];
+    product<T, S>(c, x, y, lds, (count + PRODUCT_K - 1) / PRODUCT_K * PRODUCT_K);
+    const float lower = RAISED<T> ? a.header->lower : 1.0f;
+    const uint32_t lane = threadIdx.x % WAVE, m0 = col + S::wave_m() * (S::MT * 32) + lane / 32 * 16, n0 = v + S::wave_n() * (S::NT * 32) + lane % 32;
+#pragma unroll
+    for (int n = 0; n < S::NT; ++n) {
+        if (n0 + n * 32 >= columns) continue;
+        W* to = dweight + (from + n0 + n * 32) * a.dweight_stride + m0;
+#pragma unroll
+        for (int m = 0; m < S::MT; ++m)
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                if (m0 + m * 32 + half * 8 >= a.width) continue;
+                f32x8 e;
+#pragma unroll
+                for (int r = 0; r < 8; ++r) e[r] = c[m][n][half * 8 + r] * lower;
+                store_eight(to + m * 32 + half * 8, e);
+            }
+    }
+}
+
+template <class S>
+__global__ __launch_bounds__(CE_THREADS) void cross_entropy_dbias_kernel(CeArgs a, float* dbias) {
+    const uint32_t v = blockIdx.x * CE_THREADS + threadIdx.x;
+    if (v >= a.vocab) return;
+    const uint32_t parts = (a.header->count + S::TILE_N - 1) / S::TILE_N * S::WN;
+    float sum = 0.0f;
+#pragma unroll 8
+    for (uint32_t p = 0; p < parts; ++p) sum += a.dbias_sums[(uint64_t)p * a.vocab_pad + v];
+    dbias[v] = sum;
+}
+
+// ------------------------------------------------------------------ host
+
+struct CePlan {
+    uint32_t rows_pad, width_pad, vocab_pad, piece;
+    bool small_logits, small_dh, small_dweight;
+    uint64_t logit_groups, piece_groups, dh_groups, dweight_groups;
+    size_t list_at, label_at, h_at, lse_at, g_at;                    // shared and backward
+    size_t stats_at, said_at, forward_bytes;
+    size_t d_at, dh_at, dbias_at, backward_bytes;
+};
+
+static uint64_t ce_up(uint64_t n, uint64_t by) { return (n + by - 1) / by * by; }
+
+// Tiles of 256 x 256 where they fill the chip, else of 128 x 128, two workgroups a CU.
+static bool ce_small(uint64_t m, uint64_t n) { return n <= 128 || (m + 255) / 256 * ((n + 255) / 256) < 200; }
+
+static bool ce_plan(uint64_t rows, uint32_t width, uint32_t vocab, CePlan& p) {
+    if (rows > CE_MAX || vocab == 0 || vocab > CE_MAX || width < 8 || width > CE_MAX_WIDTH || width % 8 != 0) return false;
+    const uint64_t some = rows ? rows : 1;
+    p.rows_pad = (uint32_t)ce_up(some, CE_PAD);
+    p.width_pad = (uint32_t)ce_up(width, PRODUCT_K);
+    p.vocab_pad = (uint32_t)ce_up(vocab, CE_PAD);
+    uint64_t most = CE_PIECE_BYTES / (2ull * p.rows_pad) / CE_PAD * CE_PAD;
+    if (most < 4096) most = 4096;
+    const uint64_t pieces = (p.vocab_pad + most - 1) / most;
+    p.piece = (uint32_t)ce_up((p.vocab_pad + pieces - 1) / pieces, CE_PAD);
+    const auto tiles = [](uint64_t n, bool small) { return (n + (small ? 127 : 255)) / (small ? 128 : 256); };
+    p.small_logits = ce_small(vocab, some);
+    p.small_dh = some <= 128;
+    p.small_dweight = ce_small(p.width_pad, p.piece);
+    p.logit_groups = tile_groups(tiles(vocab, p.small_logits) * tiles(some, p.small_logits));
+    p.piece_groups = tile_groups(tiles(p.piece, p.small_logits) * tiles(some, p.small_logits));
+    const uint64_t dh_tiles = tiles(p.width_pad, p.small_dh) * tiles(some, p.small_dh);
+    p.dh_groups = tile_groups(dh_tiles > CE_SPLIT_TILES ? dh_tiles : CE_SPLIT_TILES);
+    p.dweight_groups = tile_groups(tiles(p.width_pad, p.small_dweight) * tiles(p.piece, p.small_dweight));
+    for (const uint64_t groups : {p.logit_groups, p.piece_groups, p.dh_groups, p.dweight_groups})
+        if (groups > LAUNCH_GROUPS / 2) return false;
+    size_t at = 256;
+    const auto place = [&](size_t bytes) {
+        const size_t here = at;
+        at += (bytes + 255) / 256 * 256;
+        return here;
+    };
+    p.list_at = place(4ull * p.rows_pad);
+    p.label_at = place(4ull * p.rows_pad);
+    p.h_at = place(2ull * p.rows_pad * p.width_pad);
+    const size_t shared = at;
+    p.stats_at = place(8ull * p.rows_pad * (p.vocab_pad / 64));
+    p.said_at = place(4ull * p.rows_pad);
+    p.forward_bytes = at;
+    at = shared;
+    p.lse_at = place(4ull * p.rows_pad);
+    p.g_at = place(4ull * p.rows_pad);
+    p.d_at = place(2ull * p.rows_pad * p.piece);
+    // sums of dh: all rows once, or the parts of fewer
+    const uint64_t tile = p.small_dh ? 128 * 128 : 256 * 256, once = (uint64_t)p.rows_pad * p.width_pad, parts = CE_SPLIT_TILES * tile;
+    p.dh_at = place(4 * (once > parts ? once : parts));
+    p.dbias_at = place(4ull * (p.rows_pad / 64) * p.vocab_pad);
+    p.backward_bytes = at;
+    return true;
+}
+
+static bool ce_args(const okt_cross_entropy* op, CePlan& p, CeArgs& a) {
+    if (!op || !ce_plan(op->rows, op->width, op->vocab, p)) return false;
+    if (op->dtype != OKT_BF16 && op->dtype != OKT_F16) return false;
+    const auto stride = [&](uint64_t s, uint64_t& to) {
+        to = s ? s : op->width;
+        return to >= op->width && to <= 1u << 20 && to % 8 == 0;
+    };
+    if (!stride(op->h_stride, a.h_stride) || !stride(op->weight_stride, a.weight_stride) || !stride(op->dh_stride, a.dh_stride)) return false;
+    a.dweight_stride = op->dweight_stride ? op->dweight_stride : op->width;
+    if (a.dweight_stride < op->width || a.dweight_stride > 1u << 20 || op->dloss_stride > 1) return false;
+    if (op->d_bias && !aligned(op->d_bias, 4)) return false;
+    a.rows = (uint32_t)op->rows;
+    a.width = op->width;
+    a.vocab = op->vocab;
+    a.rows_pad = p.rows_pad;
+    a.width_pad = p.width_pad;
+    a.vocab_pad = p.vocab_pad;
+    a.piece = p.piece;
+    a.dloss_step = op->dloss_stride;
+    a.bias = op->d_bias;
+    return true;
+}
+
+static void ce_workspace(CeArgs& a, const CePlan& p, char* ws, bool backward) {
+    a.header = (CeHeader*)ws;
+    a.list = (uint32_t*)(ws + p.list_at);
+    a.label_of = (int32_t*)(ws + p.label_at);
+    a.h = ws + p.h_at;
+    a.stats = backward ? nullptr : (float*)(ws + p.stats_at);
+    a.said = backward ? nullptr : (float*)(ws + p.said_at);
+    a.lse_of = backward ? (float*)(ws + p.lse_at) : nullptr;
+    a.g_of = backward ? (float*)(ws + p.g_at) : nullptr;
+    a.d = backward ? ws + p.d_at : nullptr;
+    a.dh_sums = backward ? (float*)(ws + p.dh_at) : nullptr;
+    a.dbias_sums = backward ? (float*)(ws + p.dbias_at) : nullptr;
+}
+
+// From a tensor's first element to its last one's end.
+static size_t ce_extent(uint64_t rows, uint64_t stride, uint32_t width, size_t e) { return rows ? ((rows - 1) * stride + width) * e : 0; }
+
+template <typename T>
+static int ce_listed(const CeArgs& a, const void* h, float* loss, const float* lse_in, float* lse_out, const float* dloss, void* dh, hipStream_t s) {
+    hipLaunchKernelGGL(cross_entropy_list_kernel, dim3(1), dim3(CE_LIST_THREADS), 0, s, a, loss, lse_out, dloss, RAISED<T> && dloss);
+    if (const int status = launch_status()) return status;
+    hipLaunchKernelGGL(cross_entropy_gather_kernel<T>, dim3(a.rows_pad / (CE_THREADS / WAVE)), dim3(CE_THREADS), 0, s, a, (const T*)h, lse_in, dloss, (T*)dh);
+    return launch_status();
+}
+
+template <typename T, class S>
+static int ce_forward(const CeArgs& a, const CePlan& p, const void* weight, float* loss, float* lse, hipStream_t s) {
+    timing_before(s);
+    hipLaunchKernelGGL((cross_entropy_forward_kernel<T, S>), dim3((unsigned)p.logit_groups), dim3(S::THREADS), 0, s, a, (const T*)weight);
+    timing_after(s);
+    if (const int status = launch_status()) return status;
+    hipLaunchKernelGGL(cross_entropy_join_kernel, dim3((a.rows + 15) / 16), dim3(CE_THREADS), 0, s, a, (a.vocab + S::TILE_M - 1) / S::TILE_M * S::WM, loss, lse);
+    return launch_status();
+}
+
+struct CeGradients { void *dh, *dweight; float* dbias; };
+
+template <typename T, class S>
+static int ce_dh(const CeArgs& a, const CePlan& p, const void* weight, uint32_t from, uint32_t columns, hipStream_t s) {
+    hipLaunchKernelGGL((cross_entropy_dh_kernel<T, S>), dim3((unsigned)p.dh_groups), dim3(S::THREADS), 0, s, a, (const T*)weight, from, columns);
+    return launch_status();
+}
+template <typename T, class S>
+static int ce_dweight(const CeArgs& a, const CePlan& p, void* dweight, bool wide, uint32_t from, uint32_t columns, hipStream_t s) {
+    if (wide) hipLaunchKernelGGL((cross_entropy_dweight_kernel<T, float, S>), dim3((unsigned)p.dweight_groups), dim3(S::THREADS), 0, s, a, (float*)dweight, from, columns);
+    else hipLaunchKernelGGL((cross_entropy_dweight_kernel<T, T, S>), dim3((unsigned)p.dweight_groups), dim3(S::THREADS), 0, s, a, (T*)dweight, from, columns);
+    return launch_status();
+}
+
+template <typename T, class S>
+static int ce_backward(const CeArgs& a, const CePlan& p, const void* weight, const CeGradients& g, bool wide, hipStream_t s) {
+    for (uint64_t from = 0; from < a.vocab; from += p.piece) {
+        const uint32_t first = (uint32_t)from, columns = a.vocab - first < p.piece ? a.vocab - first : p.piece;
+        timing_before(s);
+        hipLaunchKernelGGL((cross_entropy_gradient_kernel<T, S>), dim3((unsigned)p.piece_groups), dim3(S::THREADS), 0, s, a, (const T*)weight, first, columns);
+        timing_after(s);
+        if (const int status = launch_status()) return status;
+        if (g.dh)
+            if (const int status = p.small_dh ? ce_dh<T, Small>(a, p, weight, first, columns, s) : ce_dh<T, Large>(a, p, weight, first, columns, s)) return status;
+        if (g.dweight)
+            if (const int status = p.small_dweight ? ce_dweight<T, Small>(a, p, g.dweight, wide, first, columns, s) : ce_dweight<T, Large>(a, p, g.dweight, wide, first, columns, s))
+                return status;
+    }
+    if (g.dh) {
+        const dim3 rows((a.rows + CE_THREADS / WAVE - 1) / (CE_THREADS / WAVE));
+        if (p.small_dh) hipLaunchKernelGGL((cross_entropy_dh_join_kernel<T, Small>), rows, dim3(CE_THREADS), 0, s, a, (T*)g.dh);
+        else hipLaunchKernelGGL((cross_entropy_dh_join_kernel<T, Large>), rows, dim3(CE_THREADS), 0, s, a, (T*)g.dh);
+        if (const int status = launch_status()) return status;
+    }
+    if (g.dbias) hipLaunchKernelGGL(cross_entropy_dbias_kernel<S>, dim3((a.vocab + CE_THREADS - 1) / CE_THREADS), dim3(CE_THREADS), 0, s, a, g.dbias);
+    return launch_status();
+}
+
+template <typename T>
+static int ce_run_forward(const CeArgs& a, const CePlan& p, const void* h, const void* weight, float* loss, float* lse, hipStream_t s) {
+    if (const int status = ce_listed<T>(a, h, loss, nullptr, lse, nullptr, nullptr, s)) return status;
+    return p.small_logits ? ce_forward<T, Small>(a, p, weight, loss, lse, s) : ce_forward<T, Large>(a, p, weight, loss, lse, s);
+}
+template <typename T>
+static int ce_run_backward(const CeArgs& a, const CePlan& p, const void* h, const void* weight, const float* lse, const float* dloss, const CeGradients& g, bool wide,
+                           hipStream_t s) {
+    if (const int status = ce_listed<T>(a, h, nullptr, lse, nullptr, dloss, g.dh, s)) return status;
+    return p.small_logits ? ce_backward<T, Small>(a, p, weight, g, wide, s) : ce_backward<T, Large>(a, p, weight, g, wide, s);
+}
+
+}  // namespace okt
+
+extern "C" {
+
+size_t okt_cross_entropy_workspace_bytes(uint64_t rows, uint32_t width, uint32_t vocab) {
+    okt::CePlan p;
+    if (!okt::ce_plan(rows, width, vocab, p)) return 0;
+    return p.forward_bytes > p.backward_bytes ? p.forward_bytes : p.backward_bytes;
+}
+
+int okt_cross_entropy_forward(const okt_cross_entropy* op, const void* d_h, const void* d_weight, const int64_t* d_labels, float* d_loss_out,
+                              float* d_lse_out, void* d_ws, size_t ws_bytes, void* stream) {
+    using namespace okt;
+    CePlan p;
+    CeArgs a;
+    if (!ce_args(op, p, a)) return OKT_ERR_INVALID_ARG;
+    if (a.rows == 0) return OKT_OK;
+    if (!d_h || !d_weight || !d_labels || !d_loss_out || !aligned(d_h, 16) || !aligned(d_weight, 16) || !aligned(d_labels, 8) ||
+        !aligned(d_loss_out, 4) || !aligned(d_lse_out, 4)) return OKT_ERR_INVALID_ARG;
+    const struct { const void* p; size_t bytes; } in[] = {{d_h, ce_extent(a.rows, a.h_stride, a.width, 2)}, {d_weight, ce_extent(a.vocab, a.weight_stride, a.width, 2)},
+                                                          {d_labels, 8ull * a.rows}, {a.bias, a.bias ? 4ull * a.vocab : 0}};
+    for (const auto& t : in)
+        for (const float* out : {d_loss_out, d_lse_out})
+            if (out && t.bytes && overlap(out, 4ull * a.rows, t.p, t.bytes)) return OKT_ERR_INVALID_ARG;
+    if (d_lse_out && overlap(d_loss_out, 4ull * a.rows, d_lse_out, 4ull * a.rows)) return OKT_ERR_INVALID_ARG;
+    if (!d_ws || !aligned(d_ws, 256) || ws_bytes < p.forward_bytes) return OKT_ERR_WORKSPACE;
+    a.labels = d_labels;
+    ce_workspace(a, p, (char*)d_ws, false);
+    const hipStream_t s = (hipStream_t)stream;
+    return op->dtype == OKT_BF16 ? ce_run_forward<__bf16>(a, p, d_h, d_weight, d_loss_out, d_lse_out, s)
+                                 : ce_run_forward<_Float16>(a, p, d_h, d_weight, d_loss_out, d_lse_out, s);
+}
+
+int okt_cross_entropy_backward(const okt_cross_entropy* op, const void* d_h, const void* d_weight, const int64_t* d_labels, const float* d_lse,
+                               const float* d_dloss, void* d_dh_out, void* d_dweight_out, float* d_dbias_out, void* d_ws, size_t ws_bytes, void* stream) {
+    using namespace okt;
+    CePlan p;
+    CeArgs a;
+    if (!ce_args(op, p, a)) return OKT_ERR_INVALID_ARG;
+    const bool wide = op->dweight_dtype == OKT_F32;
+    if (!wide && op->dweight_dtype != op->dtype) return OKT_ERR_INVALID_ARG;
+    if (!wide && a.dweight_stride % 8 != 0) return OKT_ERR_INVALID_ARG;
+    if ((d_dbias_out && !a.bias) || (!d_dh_out && !d_dweight_out && !d_dbias_out)) return OKT_ERR_INVALID_ARG;
+    if (!aligned(d_dweight_out, wide ? 4 : 16) || !aligned(d_dbias_out, 4) || !aligned(d_dh_out, 16)) return OKT_ERR_INVALID_ARG;
+    if (!d_weight || !aligned(d_weight, 16)) return OKT_ERR_INVALID_ARG;
+    if (a.rows && (!d_h || !d_labels || !d_lse || !d_dloss || !aligned(d_h, 16) || !aligned(d_labels, 8) || !aligned(d_lse, 4) || !aligned(d_dloss, 4)))
+        return OKT_ERR_INVALID_ARG;
+    const size_t scalars = 4ull * (a.rows ? (a.rows - 1ull) * a.dloss_step + 1 : 0);
+    const struct { const void* p; size_t bytes; } t[] = {
+        {d_dh_out, ce_extent(a.rows, a.dh_stride, a.width, 2)}, {d_dweight_out, ce_extent(a.vocab, a.dweight_stride, a.width, wide ? 4 : 2)},
+        {d_dbias_out, 4ull * a.vocab}, {d_h, ce_extent(a.rows, a.h_stride, a.width, 2)}, {d_weight, ce_extent(a.vocab, a.weight_stride, a.width, 2)},
+        {d_labels, 8ull * a.rows}, {d_lse, 4ull * a.rows}, {d_dloss, scalars}, {a.bias, 4ull * a.vocab}};
+    for (int out = 0; out < 3; ++out)
+        for (int other = out + 1; other < 9; ++other)
+            if (t[out].p && t[other].p && t[out].bytes && t[other].bytes && overlap(t[out].p, t[out].bytes, t[other].p, t[other].bytes)) return OKT_ERR_INVALID_ARG;
+    if (!d_ws || !aligned(d_ws, 256) || ws_bytes < p.backward_bytes) return OKT_ERR_WORKSPACE;
+    a.labels = d_labels;
+    ce_workspace(a, p, (char*)d_ws, true);
+    if (!d_dbias_out) a.dbias_sums = nullptr;
+    const hipStream_t s = (hipStream_t)stream;
+    const CeGradients g = {d_dh_out, d_dweight_out, d_dbias_out};
+    return op->dtype == OKT_BF16 ? ce_run_backward<__bf16>(a, p, d_h, d_weight, d_lse, d_dloss, g, wide, s)
+                                 : ce_run_backward<_Float16>(a, p, d_h, d_weight, d_lse, d_dloss, g, wide, s);
+}
+
+}  // extern "C"
