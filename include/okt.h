@@ -768,7 +768,7 @@ size_t okt_cross_entropy_workspace_bytes(uint64_t rows, uint32_t width, uint32_t
  *   d_labels    in   int64[rows]
  *   d_loss_out  out  fp32[rows]
  *   d_lse_out   out  fp32[rows]; NULL if no backward pass follows
- * Outputs overlap neither each other nor an input.  Four launches.
+ * Outputs overlap neither each other nor an input.  Four launches, three up to 2048 rows.
  */
 int okt_cross_entropy_forward(const okt_cross_entropy* op, const void* d_h, const void* d_weight, const int64_t* d_labels,
                               float* d_loss_out, float* d_lse_out, void* d_ws, size_t ws_bytes, void* stream);
@@ -778,7 +778,7 @@ int okt_cross_entropy_forward(const okt_cross_entropy* op, const void* d_h, cons
  *   d_dloss  in   fp32[rows] or fp32[1], see dloss_stride
  *   d_dh_out, d_dweight_out, d_dbias_out  out  overwritten; each may be NULL (not all; the last one has to be without a bias), and
  *            none overlaps another or an input, from its first element to its last
- * Two launches and up to three a piece of the vocabulary, and two more.
+ * Two launches (one up to 2048 rows), up to three a piece of the vocabulary, and two more.
  */
 int okt_cross_entropy_backward(const okt_cross_entropy* op, const void* d_h, const void* d_weight, const int64_t* d_labels,
                                const float* d_lse, const float* d_dloss, void* d_dh_out, void* d_dweight_out, float* d_dbias_out,

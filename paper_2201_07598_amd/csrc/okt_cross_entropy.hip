@@ -21,15 +21,14 @@
 namespace okt {
 
 constexpr uint32_t CE_PAD = 256;                                     // rows, and columns of a piece, are padded to the largest tile
-constexpr uint64_t CE_PIECE_BYTES = 512ull << 20;                    // of d in the workspace
+constexpr uint64_t CE_PIECE_BYTES = 1ull << 30;                    // of d in the workspace
 constexpr uint32_t CE_SPLIT_TILES = 512;                             // of dh and parts of k together, where tiles are fewer
 constexpr uint32_t CE_MAX = 1u << 22;                                // rows, vocabulary
 constexpr uint32_t CE_MAX_WIDTH = 1u << 15;
 constexpr int CE_THREADS = 256;
 constexpr float LOG2E = 1.44269504088896340736f;
-constexpr double LN2 = 0.69314718055994530942;
 
-typedef ProductShape<4, 4, 2, 2> Large;                              // 256 x 256, one workgroup a CU
+typedef ProductShape<4, 2, 2, 4> Large;                              // 256 x 256, one workgroup of eight waves a CU
 typedef ProductShape<2, 2, 2, 2> Small;                              // 128 x 128, two
 
 template <typename T> constexpr bool RAISED = false;
@@ -45,6 +44,7 @@ struct CeArgs {
     const int64_t* labels;
     // workspace
     CeHeader* header;
+    float2* counts;                                                  // of every block: labelled rows (as bits), largest |g|
     uint32_t* list;                                                  // numbers of the labelled rows
     int32_t* label_of;                                               // of listed row n
     void* h;                                                         // [rows_pad][width_pad]
@@ -59,92 +59,123 @@ struct CeArgs {
 
 // ------------------------------------------------------------------ the list of labelled rows
 
-constexpr int CE_LIST_THREADS = 1024, CE_LIST_EACH = 8;
+constexpr uint32_t CE_BLOCK = 256;                                   // rows that a thread each counts
+constexpr uint32_t CE_GATHERED = 16;                                 // rows that a workgroup gathers
+constexpr uint32_t CE_DIRECT = 2048;                                 // up to so many rows, every workgroup counts all of them by itself
 
 __device__ __forceinline__ bool labelled(int64_t y, uint32_t vocab) { return y >= 0 && y < (int64_t)vocab; }
 
-__global__ __launch_bounds__(CE_LIST_THREADS) void cross_entropy_list_kernel(CeArgs a, float* loss, float* lse, const float* dloss, bool raised) {
-    __shared__ uint32_t waves[CE_LIST_THREADS / WAVE];
-    __shared__ float tops[CE_LIST_THREADS / WAVE];
-    const int lane = lane_id(), wave = threadIdx.x / WAVE;
-    uint32_t before = 0;
-    float top = 0.0f;
-    for (uint64_t base = 0; base < a.rows; base += CE_LIST_THREADS * CE_LIST_EACH) {
-        const uint64_t first = base + threadIdx.x * CE_LIST_EACH;
-        int64_t y[CE_LIST_EACH];
-        uint32_t mine = 0;
+struct CeCount { uint32_t before, all; float top; };                 // labelled rows, and the largest |g| of those
+
+__device__ __forceinline__ CeCount count_together(CeCount c, CeCount (&waves)[CE_THREADS / WAVE]) {
 #pragma unroll
-        for (int i = 0; i < CE_LIST_EACH; ++i) y[i] = first + i < a.rows ? a.labels[first + i] : -1;
-#pragma unroll
-        for (int i = 0; i < CE_LIST_EACH; ++i) mine += labelled(y[i], a.vocab);
-        const uint32_t scan = wave_inclusive_scan_u32(mine);
-        if (lane == WAVE - 1) waves[wave] = scan;
-        __syncthreads();
-        uint32_t at = before + scan - mine, all = 0;
-#pragma unroll
-        for (int w = 0; w < CE_LIST_THREADS / WAVE; ++w) {
-            if (w < wave) at += waves[w];
-            all += waves[w];
-        }
-        before += all;
-        __syncthreads();
-#pragma unroll
-        for (int i = 0; i < CE_LIST_EACH; ++i) {
-            if (first + i >= a.rows) break;
-            if (labelled(y[i], a.vocab)) {
-                a.list[at] = (uint32_t)(first + i);
-                a.label_of[at++] = (int32_t)y[i];
-                if (raised) {
-                    const float g = fabsf(dloss[(first + i) * a.dloss_step]);
-                    top = g > top ? g : top;                         // a NaN does not raise it
-                }
-            } else if (loss) {
-                loss[first + i] = 0.0f;
-                if (lse) lse[first + i] = 0.0f;
-            }
-        }
+    for (int m = 1; m < WAVE; m <<= 1) {
+        c.before += __shfl_xor(c.before, m, WAVE);
+        c.all += __shfl_xor(c.all, m, WAVE);
+        c.top = fmaxf(c.top, __shfl_xor(c.top, m, WAVE));            // a NaN does not raise it
     }
-    if (raised) {
+    if (threadIdx.x % WAVE == 0) waves[threadIdx.x / WAVE] = c;
+    __syncthreads();
+    c = waves[0];
 #pragma unroll
-        for (int m = 1; m < WAVE; m <<= 1) top = fmaxf(top, __shfl_xor(top, m, WAVE));
-        if (lane == 0) tops[wave] = top;
-        __syncthreads();
-#pragma unroll
-        for (int w = 0; w < CE_LIST_THREADS / WAVE; ++w) top = fmaxf(top, tops[w]);
+    for (int w = 1; w < CE_THREADS / WAVE; ++w) {
+        c.before += waves[w].before;
+        c.all += waves[w].all;
+        c.top = fmaxf(c.top, waves[w].top);
     }
-    if (threadIdx.x == 0) {
-        int e = 0;                                                   // top in [2^(e - 1), 2^e)
-        if (top > 0.0f && top < __builtin_inff()) frexpf(top, &e);
-        const int by = raised && top > 0.0f && top < __builtin_inff() ? min(max(15 - e, -120), 120) : 0;
-        *a.header = {before, ldexpf(1.0f, by), ldexpf(1.0f, -by), 0};
-    }
+    return c;
 }
 
-// A wave a row: listed rows of h side by side, zeros behind the last one up to whole tiles; and zeros for the gradients of rows that
-// are not listed.
+__device__ __forceinline__ CeCount count_row(const CeArgs& a, const float* dloss, uint64_t row, uint64_t first) {
+    if (row >= a.rows || !labelled(a.labels[row], a.vocab)) return {0, 0, 0.0f};
+    return {row < first ? 1u : 0u, 1u, dloss ? fabsf(dloss[row * a.dloss_step]) : 0.0f};
+}
+
+__device__ __forceinline__ void add_to(CeCount& c, const CeCount& more) {
+    c.before += more.before;
+    c.all += more.all;
+    c.top = fmaxf(c.top, more.top);
+}
+
+// Labelled rows of every block.
+__global__ __launch_bounds__(CE_THREADS) void cross_entropy_count_kernel(CeArgs a, const float* dloss) {
+    __shared__ CeCount waves[CE_THREADS / WAVE];
+    const CeCount c = count_together(count_row(a, dloss, (uint64_t)blockIdx.x * CE_BLOCK + threadIdx.x, 0), waves);
+    if (threadIdx.x == 0) a.counts[blockIdx.x] = make_float2(__uint_as_float(c.all), c.top);
+}
+
+// Sixteen rows a workgroup: those with a label go side by side into the workspace, behind all labelled ones before them; the others
+// get their zeros.  Zeros fill the last tile, too.
 template <typename T>
-__global__ __launch_bounds__(CE_THREADS) void cross_entropy_gather_kernel(CeArgs a, const T* h, const float* lse, const float* dloss, T* dh) {
+__global__ __launch_bounds__(CE_THREADS) void cross_entropy_gather_kernel(CeArgs a, const T* h, float* loss, const float* lse_in, float* lse_out, const float* dloss, T* dh) {
     typedef typename Eight<T>::vec vec;
-    const uint32_t n = blockIdx.x * (CE_THREADS / WAVE) + threadIdx.x / WAVE, lane = threadIdx.x % WAVE;
-    const uint32_t count = a.header->count;
-    if (n < (count + CE_PAD - 1) / CE_PAD * CE_PAD) {
-        const bool there = n < count;
-        const uint32_t row = there ? a.list[n] : 0;
-        const T* from = h + row * a.h_stride;
-        T* to = (T*)a.h + (uint64_t)n * a.width_pad;
-        for (uint32_t c = lane * 8; c < a.width_pad; c += WAVE * 8) {
-            vec v = {};
-            if (there && c < a.width) v = *reinterpret_cast<const vec*>(from + c);
-            *reinterpret_cast<vec*>(to + c) = v;
+    __shared__ CeCount waves[CE_THREADS / WAVE];
+    const uint64_t first = (uint64_t)blockIdx.x * CE_GATHERED;
+    const uint32_t lane = threadIdx.x % WAVE, wave = uniform(threadIdx.x / WAVE);
+    CeCount c = {0, 0, 0.0f};
+    const float* g = RAISED<T> ? dloss : nullptr;
+    if (a.rows <= CE_DIRECT) {
+        for (uint32_t r = threadIdx.x; r < a.rows; r += CE_THREADS) add_to(c, count_row(a, g, r, first));
+    } else {
+        const uint64_t block = first / CE_BLOCK;
+        for (uint64_t b = threadIdx.x; b * CE_BLOCK < a.rows; b += CE_THREADS) {
+            const float2 v = a.counts[b];
+            const uint32_t n = __float_as_uint(v.x);
+            add_to(c, {b < block ? n : 0u, n, v.y});
         }
-        if (lane == 0 && !there) a.label_of[n] = -1;
-        if (lane == 0 && dloss) {
-            a.lse_of[n] = there ? lse[row] : 0.0f;
-            a.g_of[n] = there ? dloss[(uint64_t)row * a.dloss_step] : 0.0f;
+        c.before += count_row(a, nullptr, block * CE_BLOCK + threadIdx.x, first).before;
+    }
+    c = count_together(c, waves);
+    if (blockIdx.x == 0 && threadIdx.x == 0) {
+        int e = 0;                                                   // top in [2^(e - 1), 2^e)
+        const bool use = RAISED<T> && c.top > 0.0f && c.top < __builtin_inff();
+        if (use) frexpf(c.top, &e);
+        const int by = use ? min(max(15 - e, -120), 120) : 0;
+        *a.header = {c.all, ldexpf(1.0f, by), ldexpf(1.0f, -by), 0};
+    }
+    const auto put = [&](uint32_t n, const T* from) {                // a row, or zeros
+        T* to = (T*)a.h + (uint64_t)n * a.width_pad;
+#pragma unroll 4
+        for (uint32_t x = lane * 8; x < a.width_pad; x += WAVE * 8) {
+            vec v = {};
+            if (from && x < a.width) v = *reinterpret_cast<const vec*>(from + x);
+            *reinterpret_cast<vec*>(to + x) = v;
+        }
+    };
+    uint32_t n = c.before;
+    for (uint32_t i = 0; i < CE_GATHERED; ++i) {
+        const uint64_t row = first + i;
+        if (row >= a.rows) break;
+        const int64_t y = a.labels[row];
+        const bool there = labelled(y, a.vocab), mine = i % (CE_THREADS / WAVE) == wave;
+        if (mine && there) {
+            put(n, h + row * a.h_stride);
+            if (lane == 0) {
+                a.list[n] = (uint32_t)row;
+                a.label_of[n] = (int32_t)y;
+                if (dloss) {
+                    a.lse_of[n] = lse_in[row];
+                    a.g_of[n] = dloss[row * a.dloss_step];
+                }
+            }
+        } else if (mine) {
+            if (dh)
+                for (uint32_t x = lane * 8; x < a.width; x += WAVE * 8) *reinterpret_cast<vec*>(dh + row * a.dh_stride + x) = vec{};
+            if (lane == 0 && loss) {
+                loss[row] = 0.0f;
+                if (lse_out) lse_out[row] = 0.0f;
+            }
+        }
+        n += there;
+    }
+    const uint32_t end = (c.all + CE_PAD - 1) / CE_PAD * CE_PAD;
+    for (uint32_t z = c.all + blockIdx.x * (CE_THREADS / WAVE) + wave; z < end; z += gridDim.x * (CE_THREADS / WAVE)) {
+        put(z, nullptr);
+        if (lane == 0) {
+            a.label_of[z] = -1;
+            if (dloss) a.lse_of[z] = a.g_of[z] = 0.0f;
         }
     }
-    if (dh && n < a.rows && !labelled(a.labels[n], a.vocab))
-        for (uint32_t c = lane * 8; c < a.width; c += WAVE * 8) *reinterpret_cast<vec*>(dh + n * a.dh_stride + c) = vec{};
 }
 
 // ------------------------------------------------------------------ logits
@@ -223,33 +254,41 @@ __global__ __launch_bounds__(S::THREADS) void cross_entropy_forward_kernel(CeArg
     }
 }
 
-// Sixteen rows a workgroup, sixteen threads a row, each every sixteenth part.
-__global__ __launch_bounds__(CE_THREADS) void cross_entropy_join_kernel(CeArgs a, uint32_t parts, float* loss, float* lse) {
-    __shared__ float tops[16][17], sums[16][17];
+// Sixteen rows a workgroup, and 64 threads a row, each every 64th part.
+constexpr int CE_JOIN_THREADS = 1024;
+struct RowSum { float top, sum; };
+__device__ __forceinline__ RowSum together(RowSum x, RowSum y) {
+    const float top = fmaxf(x.top, y.top);
+    if (top == -__builtin_inff()) return {top, x.sum + y.sum};      // 0, or NaN
+    return {top, x.sum * __builtin_amdgcn_exp2f((x.top - top) * LOG2E) + y.sum * __builtin_amdgcn_exp2f((y.top - top) * LOG2E)};
+}
+
+__global__ __launch_bounds__(CE_JOIN_THREADS) void cross_entropy_join_kernel(CeArgs a, uint32_t parts, float* loss, float* lse) {
+    __shared__ RowSum waves[CE_JOIN_THREADS / WAVE][16];
     const uint32_t count = a.header->count, r = threadIdx.x % 16, share = threadIdx.x / 16, row = blockIdx.x * 16 + r;
     if (blockIdx.x * 16 >= count) return;
-    float top = -__builtin_inff(), sum = 0.0f;
-    const auto add = [&](float t, float s) {
-        const float more = fmaxf(top, t);
-        if (more == -__builtin_inff()) {
-            sum += s;                                                // 0, or NaN
-            return;
-        }
-        sum = sum * __builtin_amdgcn_exp2f((top - more) * LOG2E) + s * __builtin_amdgcn_exp2f((t - more) * LOG2E);
-        top = more;
-    };
+    RowSum v = {-__builtin_inff(), 0.0f};
     if (row < count)
-#pragma unroll 8
-        for (uint32_t p = share; p < parts; p += 16) {
-            const float2 v = *reinterpret_cast<const float2*>(a.stats + ((uint64_t)p * a.rows_pad + row) * 2);
-            add(v.x, v.y);
+#pragma unroll 4
+        for (uint32_t p = share; p < parts; p += CE_JOIN_THREADS / 16) {
+            const float2 t = *reinterpret_cast<const float2*>(a.stats + ((uint64_t)p * a.rows_pad + row) * 2);
+            v = together(v, {t.x, t.y});
         }
-    tops[share][r] = top;
-    sums[share][r] = sum;
+    const auto lanes = [&](RowSum x) {                               // the four shares of a wave
+#pragma unroll
+        for (int m = 16; m < WAVE; m <<= 1) x = together(x, {__shfl_xor(x.top, m, WAVE), __shfl_xor(x.sum, m, WAVE)});
+        return x;
+    };
+    v = lanes(v);
+    if (threadIdx.x % WAVE < 16) waves[threadIdx.x / WAVE][r] = v;
     __syncthreads();
+    if (threadIdx.x >= WAVE) return;
+    v = waves[share][r];
+#pragma unroll
+    for (int k = 4; k < CE_JOIN_THREADS / WAVE; k += 4) v = together(v, waves[k + share][r]);
+    v = lanes(v);
     if (share != 0 || row >= count) return;
-    for (int k = 1; k < 16; ++k) add(tops[k][r], sums[k][r]);
-    const float all = top == -__builtin_inff() && sum == 0.0f ? top : top + logf(sum);
+    const float all = v.top == -__builtin_inff() && v.sum == 0.0f ? v.top : v.top + logf(v.sum);
     const uint32_t to = a.list[row];
     loss[to] = all - a.said[row];
     if (lse) lse[to] = all;
@@ -455,7 +494,7 @@ struct CePlan {
     uint32_t rows_pad, width_pad, vocab_pad, piece;
     bool small_logits, small_dh, small_dweight;
     uint64_t logit_groups, piece_groups, dh_groups, dweight_groups;
-    size_t list_at, label_at, h_at, lse_at, g_at;                    // shared and backward
+    size_t counts_at, list_at, label_at, h_at, lse_at, g_at;         // shared and backward
     size_t stats_at, said_at, forward_bytes;
     size_t d_at, dh_at, dbias_at, backward_bytes;
 };
@@ -492,6 +531,7 @@ static bool ce_plan(uint64_t rows, uint32_t width, uint32_t vocab, CePlan& p) {
         at += (bytes + 255) / 256 * 256;
         return here;
     };
+    p.counts_at = place(8ull * (p.rows_pad / CE_BLOCK));
     p.list_at = place(4ull * p.rows_pad);
     p.label_at = place(4ull * p.rows_pad);
     p.h_at = place(2ull * p.rows_pad * p.width_pad);
@@ -536,6 +576,7 @@ static bool ce_args(const okt_cross_entropy* op, CePlan& p, CeArgs& a) {
 
 static void ce_workspace(CeArgs& a, const CePlan& p, char* ws, bool backward) {
     a.header = (CeHeader*)ws;
+    a.counts = (float2*)(ws + p.counts_at);
     a.list = (uint32_t*)(ws + p.list_at);
     a.label_of = (int32_t*)(ws + p.label_at);
     a.h = ws + p.h_at;
@@ -553,9 +594,12 @@ static size_t ce_extent(uint64_t rows, uint64_t stride, uint32_t width, size_t e
 
 template <typename T>
 static int ce_listed(const CeArgs& a, const void* h, float* loss, const float* lse_in, float* lse_out, const float* dloss, void* dh, hipStream_t s) {
-    hipLaunchKernelGGL(cross_entropy_list_kernel, dim3(1), dim3(CE_LIST_THREADS), 0, s, a, loss, lse_out, dloss, RAISED<T> && dloss);
-    if (const int status = launch_status()) return status;
-    hipLaunchKernelGGL(cross_entropy_gather_kernel<T>, dim3(a.rows_pad / (CE_THREADS / WAVE)), dim3(CE_THREADS), 0, s, a, (const T*)h, lse_in, dloss, (T*)dh);
+    if (a.rows > CE_DIRECT) {
+        hipLaunchKernelGGL(cross_entropy_count_kernel, dim3((a.rows + CE_BLOCK - 1) / CE_BLOCK), dim3(CE_THREADS), 0, s, a, RAISED<T> ? dloss : nullptr);
+        if (const int status = launch_status()) return status;
+    }
+    const uint32_t groups = a.rows ? (a.rows + CE_GATHERED - 1) / CE_GATHERED : 1;
+    hipLaunchKernelGGL(cross_entropy_gather_kernel<T>, dim3(groups), dim3(CE_THREADS), 0, s, a, (const T*)h, loss, lse_in, lse_out, dloss, (T*)dh);
     return launch_status();
 }
 
@@ -565,7 +609,7 @@ static int ce_forward(const CeArgs& a, const CePlan& p, const void* weight, floa
     hipLaunchKernelGGL((cross_entropy_forward_kernel<T, S>), dim3((unsigned)p.logit_groups), dim3(S::THREADS), 0, s, a, (const T*)weight);
     timing_after(s);
     if (const int status = launch_status()) return status;
-    hipLaunchKernelGGL(cross_entropy_join_kernel, dim3((a.rows + 15) / 16), dim3(CE_THREADS), 0, s, a, (a.vocab + S::TILE_M - 1) / S::TILE_M * S::WM, loss, lse);
+    hipLaunchKernelGGL(cross_entropy_join_kernel, dim3((a.rows + 15) / 16), dim3(CE_JOIN_THREADS), 0, s, a, (a.vocab + S::TILE_M - 1) / S::TILE_M * S::WM, loss, lse);
     return launch_status();
 }
 

@@ -47,19 +47,12 @@ struct KMajor {
 #pragma unroll
         for (uint32_t s = 0; s < 4; ++s) read[s] = kmajor_read<ORDERED>(lane, s);
     }
-    // `there`: k of this piece that the tensor has
-    __device__ __forceinline__ void fetch(uint32_t lds, uint32_t there) {
-        const uint32_t to = lds + uniform(threadIdx.x / WAVE) * (LOADS * 1024);
-        const i32x4 buffer = from.buffer();
-        if (there >= PRODUCT_K) {
-#pragma unroll
-            for (int i = 0; i < LOADS; ++i) fetch_to_lds(to + i * 1024, at[i], buffer);
-        } else {
-#pragma unroll
-            for (int i = 0; i < LOADS; ++i) fetch_to_lds(to + i * 1024, kmajor_chunk<ORDERED>(threadIdx.x % WAVE, i) * 8 < there ? at[i] : OUTSIDE, buffer);
-        }
-        from.advance(PRODUCT_K * 2);
+    // Fetch i of the wave's of a piece of which the tensor has `there` k.
+    __device__ __forceinline__ void fetch(int i, uint32_t lds, i32x4 buffer, uint32_t there) const {
+        const uint32_t to = lds + uniform(threadIdx.x / WAVE) * (LOADS * 1024) + i * 1024;
+        fetch_to_lds(to, there >= PRODUCT_K || kmajor_chunk<ORDERED>(threadIdx.x % WAVE, i) * 8 < there ? at[i] : OUTSIDE, buffer);
     }
+    __device__ __forceinline__ void advance() { from.advance(PRODUCT_K * 2); }
     __device__ __forceinline__ frag<T> operand(const char* piece, int square, int s) const {
         return *reinterpret_cast<const frag<T>*>(piece + read[s] + square * KMAJOR_SQUARE);
     }
@@ -87,13 +80,10 @@ struct Transposed {
 #pragma unroll
         for (uint32_t half = 0; half < 2; ++half) read[half] = transposed_read<ORDERED>(lane, half);
     }
-    __device__ __forceinline__ void fetch(uint32_t lds, uint32_t) {
-        const uint32_t to = lds + uniform(threadIdx.x / WAVE) * (LOADS * 1024);
-        const i32x4 buffer = from.buffer();
-#pragma unroll
-        for (int i = 0; i < LOADS; ++i) fetch_to_lds(to + i * 1024, at[i], buffer);
-        from.advance(step);
+    __device__ __forceinline__ void fetch(int i, uint32_t lds, i32x4 buffer, uint32_t) const {
+        fetch_to_lds(lds + uniform(threadIdx.x / WAVE) * (LOADS * 1024) + i * 1024, at[i], buffer);
     }
+    __device__ __forceinline__ void advance() { from.advance(step); }
     __device__ __forceinline__ frag<T> operand(const char* piece, int square, int s) const {
         i16x4 half[2];
 #pragma unroll
@@ -114,7 +104,18 @@ struct ProductShape {
     static __device__ __forceinline__ int wave_n() { return (int)uniform(threadIdx.x / WAVE) / WM; }
 };
 
+// Waits for this wave's fetches into LDS and its reads from there, then for the other waves.
+__device__ __forceinline__ void handed_over() {
+    __builtin_amdgcn_s_waitcnt(0x0070);           // vmcnt(0), lgkmcnt(0)
+    __syncthreads();
+}
+
 // The sums over `k`.  Every wave of the workgroup calls it; the tiles in LDS are free again after a barrier.
+//
+// A piece is four steps of sixteen k.  While a step's products run, the wave reads the next step's operands from LDS, a few between every
+// NT products, and the barrier that hands over the next piece stands before the last step, whose operands are in registers by then: so the
+// products of that step cover the first reads of the next piece and the first fetches of the one after it.  Fetches go out one by one
+// between products, too: issued together they hold the wave up for a thousand cycles (8192 x 128000 x 4096: 8.2 ms).
 template <typename T, class S, class A, class B>
 __device__ __forceinline__ void product(f32x16 (&c)[S::MT][S::NT], A& a, B& b, char* lds, uint32_t k) {
 #pragma unroll
@@ -123,32 +124,64 @@ __device__ __forceinline__ void product(f32x16 (&c)[S::MT][S::NT], A& a, B& b, c
         for (int n = 0; n < S::NT; ++n) c[m][n] = 0.0f;
     if (k == 0) return;
     constexpr uint32_t BUFFER = A::BYTES + B::BYTES;
+    constexpr int LOADS = A::LOADS + B::LOADS, STEPS = PRODUCT_K / 16, EACH = (LOADS / 2 + S::MT - 1) / S::MT;
     const uint32_t at = lds_address(lds);
     const int m0 = S::wave_m() * S::MT, n0 = S::wave_n() * S::NT;
-    a.fetch(at, k);
-    b.fetch(at + A::BYTES, k);
+    frag<T> x[2][S::MT], y[2][S::NT];
+    i32x4 buffer_a = a.from.buffer(), buffer_b = b.from.buffer();
+    const auto fetch = [&](int i, uint32_t to, uint32_t there) {
+        if (i < A::LOADS) a.fetch(i, at + to, buffer_a, there);
+        else if (i < LOADS) b.fetch(i - A::LOADS, at + to + A::BYTES, buffer_b, there);
+    };
+    // the operands of a step that a group of products covers
+    const auto read = [&](int set, int m, const char* piece, int s) {
+        x[set][m] = a.operand(piece, m0 + m, s);
+        if (m < S::NT) y[set][m] = b.operand(piece + A::BYTES, n0 + m, s);
+    };
+    static_assert(S::NT <= S::MT, "a group reads one operand of each side");
+    const auto next_piece = [&](uint32_t done) {                     // of which `done` k are before it
+        a.advance();
+        b.advance();
+        buffer_a = a.from.buffer();
+        buffer_b = b.from.buffer();
+        if (done >= k) buffer_a[2] = buffer_b[2] = 0;                // past the end nothing is read
+    };
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) fetch(i, 0, k);
+    next_piece(PRODUCT_K);
     uint32_t now = 0;
-    for (uint32_t done = 0; done < k; done += PRODUCT_K) {
-        fetched();
-        const char* piece = lds + now;
+    handed_over();
+#pragma unroll
+    for (int i = 0; i < LOADS / 2; ++i) fetch(i, BUFFER, k - PRODUCT_K);
+#pragma unroll
+    for (int m = 0; m < S::MT; ++m) read(0, m, lds, 0);
+    for (uint32_t done = PRODUCT_K; ; done += PRODUCT_K) {           // k up to the end of this piece
+        const uint32_t left = done < k ? k - done : PRODUCT_K;       // and of the next one
+#pragma unroll
+        for (int s = 0; s < STEPS; ++s) {
+            if (s == STEPS - 1) {
+                next_piece(done + PRODUCT_K);
+                handed_over();
+            }
+            const char* piece = lds + (s == STEPS - 1 ? now ^ BUFFER : now);
+#pragma unroll
+            for (int m = 0; m < S::MT; ++m) {
+                __builtin_amdgcn_sched_barrier(0);
+                read((s + 1) % 2, m, piece, (s + 1) % STEPS);
+#pragma unroll
+                for (int i = 0; i < EACH; ++i) {
+                    if (s == 0 && m * EACH + i < LOADS - LOADS / 2) fetch(LOADS / 2 + m * EACH + i, now ^ BUFFER, left);
+                    if (s == STEPS - 1 && m * EACH + i < LOADS / 2) fetch(m * EACH + i, now, left > PRODUCT_K ? left - PRODUCT_K : PRODUCT_K);
+                }
+#pragma unroll
+                for (int n = 0; n < S::NT; ++n) c[m][n] = mfma(x[s % 2][m], y[s % 2][n], c[m][n]);
+            }
+        }
         now ^= BUFFER;
-        if (done + PRODUCT_K < k) {
-            a.fetch(at + now, k - done - PRODUCT_K);
-            b.fetch(at + now + A::BYTES, k - done - PRODUCT_K);
-        }
-#pragma unroll
-        for (int s = 0; s < PRODUCT_K / 16; ++s) {
-            frag<T> x[S::MT], y[S::NT];
-#pragma unroll
-            for (int m = 0; m < S::MT; ++m) x[m] = a.operand(piece, m0 + m, s);
-#pragma unroll
-            for (int n = 0; n < S::NT; ++n) y[n] = b.operand(piece + A::BYTES, n0 + n, s);
-#pragma unroll
-            for (int m = 0; m < S::MT; ++m)
-#pragma unroll
-                for (int n = 0; n < S::NT; ++n) c[m][n] = mfma(x[m], y[n], c[m][n]);
-        }
+        if (done >= k) break;
     }
+    __builtin_amdgcn_sched_barrier(0);
+    handed_over();                                                       // nothing is on its way into LDS any more
 }
 
 }  // namespace okt
