@@ -691,7 +691,7 @@ int okt_attention_backward(const okt_attention* op, const void* d_q, const void*
  * for the pairs j < rot_dim / 2: (a, b) = (j, j + rot_dim / 2), or (2j, 2j + 1) if `adjacent`; elements from
  * rot_dim on stay n.  Several axes (time, height, width) turn pairs of their own.  The angle is taken in fp64, so
  * far positions lose nothing; the rest is fp32, an output is rounded once.  Queries and keys are [batch][length][heads][head_dim] by strides
- * {batch, length, heads} in elements, head_dim contiguous, at the alignment of an element; so parts of a common
+ * {batch, length, heads} in elements (up to 2^40, that of the heads 2^30), head_dim contiguous, at the alignment of an element; so parts of a common
  * projection are taken as they lie, and keys can be written to where they are kept.  The norm is there where its weight is, for queries and keys
  * apart.  One of the two may have no heads.
  */

@@ -11,30 +11,39 @@
 // four adjacent pairs), so a pair never leaves its lane and a norm's sums cross 8, 16 or 32 lanes inside the vector unit.
 #include <math.h>
 
+#include "okt_attention_layout.h"
 #include "okt_element.h"
 
 namespace okt {
 
 constexpr int ROT_THREADS = 256;
 constexpr uint32_t ROT_MAX_DIM = 256, ROT_MAX_TOKENS = 32;           // of a workgroup at a time
-constexpr uint32_t ROT_ANGLES = 2048;                                // a workgroup's tokens times pairs
+constexpr uint32_t ROT_ANGLES = 1024;                                // a workgroup's tokens times pairs
 constexpr uint32_t ROT_BACKWARD_GROUPS = 1024;
-constexpr int ROT_AHEAD = 4;                                         // heads of a lane that are on their way together
+// Heads of a lane that are on their way together.  (8 x 4096 tokens of 16 + 4 heads of 128 bf16, backward: one 119 us, two 108, four 128,
+// which takes registers of half the waves; forward two and four 74, one 83.)
+template <typename T> constexpr int ROT_AHEAD = 2;
+template <> constexpr int ROT_AHEAD<float> = 1;
+// Calls that move more than this go around the caches, of which they would find nothing again (the sizes above: 73 and 108 us through them, 68 and 102
+// around); what smaller ones write, attention finds there.
+constexpr uint64_t ROT_CACHED_BYTES = 256ull << 20;
 
-struct HeadStrides { uint64_t batch, row, head; };
+struct HeadStrides { uint64_t batch, row; uint32_t head; };          // in elements
 
 struct RotTensor {                                                   // queries or keys
     uint32_t heads;
+    uint32_t step_tokens, step_heads;                                // what a lane's next head is further than its last one
     const float* weight;
     HeadStrides in, d, out;
 };
 
 struct RotArgs {
-    uint64_t tokens, tiles;
-    uint32_t length, dim, rot, tile, groups;                         // tokens a tile; workgroups (backward)
+    uint32_t tokens, tiles;
+    uint32_t dim, rot, tile, groups, pair_shift;                     // tokens a tile; workgroups (backward); pairs rounded up, as a shift
+    Divider length;
     int kind;
     bool adjacent;
-    float eps;
+    float eps, share;                                                // share: 1 / dim
     const float* inv_freq;
     const int32_t* positions;
     uint64_t position_stride[2];
@@ -47,15 +56,26 @@ struct RotPointers { const void* x[2]; const void* d[2]; void* out[2]; };
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
-template <typename T>
-__device__ __forceinline__ f32x4 load_four(const T* p) {
-    typedef T vec __attribute__((ext_vector_type(4), aligned(sizeof(T))));
-    return __builtin_convertvector(*reinterpret_cast<const vec*>(p), f32x4);
+// Four neighbours as they lie in memory, at the alignment of an element.
+template <typename T> using Four = T __attribute__((ext_vector_type(4)));
+template <typename T> using LooseFour = T __attribute__((ext_vector_type(4), aligned(sizeof(T))));
+template <bool NT, typename T> __device__ __forceinline__ Four<T> raw_four(const T* p) {
+    return NT ? __builtin_nontemporal_load(reinterpret_cast<const LooseFour<T>*>(p)) : *reinterpret_cast<const LooseFour<T>*>(p);
 }
-template <typename T>
-__device__ __forceinline__ void store_four(T* p, f32x4 v) {
-    typedef T vec __attribute__((ext_vector_type(4), aligned(sizeof(T))));
-    *reinterpret_cast<vec*>(p) = __builtin_convertvector(v, vec);
+template <typename T> __device__ __forceinline__ f32x4 wide_four(Four<T> v) { return __builtin_convertvector(v, f32x4); }
+template <bool NT, typename T> __device__ __forceinline__ void store_four(T* p, f32x4 v) {
+    if (NT) __builtin_nontemporal_store(__builtin_convertvector(v, Four<T>), reinterpret_cast<LooseFour<T>*>(p));
+    else *reinterpret_cast<LooseFour<T>*>(p) = __builtin_convertvector(v, Four<T>);
+}
+
+__device__ __forceinline__ f32x4 fma_four(f32x4 a, f32x4 b, f32x4 c) {
+    return f32x4{fmaf(a[0], b[0], c[0]), fmaf(a[1], b[1], c[1]), fmaf(a[2], b[2], c[2]), fmaf(a[3], b[3], c[3])};
+}
+
+// 1 / sqrt, to an ulp: the unit's instruction takes no subnormal numbers.
+__device__ __forceinline__ float reciprocal_root(float v) {
+    const bool tiny = v < 0x1p-96f;
+    return __builtin_amdgcn_rsqf(tiny ? v * 0x1p64f : v) * (tiny ? 0x1p32f : 1.0f);
 }
 
 // Sum over LANES (8, 16 or 32) neighbouring lanes, in each of them.
@@ -81,7 +101,7 @@ __device__ __forceinline__ float sum_of(const Eights& x) {
     return (s[0] + s[1]) + (s[2] + s[3]);
 }
 __device__ __forceinline__ float dot_of(const Eights& x, const Eights& y) {
-    const f32x4 s = x.a * y.a + x.b * y.b;
+    const f32x4 s = fma_four(x.a, y.a, x.b * y.b);
     return (s[0] + s[1]) + (s[2] + s[3]);
 }
 
@@ -91,35 +111,40 @@ struct TokenPlace { uint64_t in[2], d[2], out[2]; };
 struct RotShared {
     f32x4 cosine[ROT_ANGLES / 4], sine[ROT_ANGLES / 4];              // [token][pair], dim / 2 pairs; the unrotated are turned by 0
     TokenPlace place[ROT_MAX_TOKENS];
-    float sums[2][ROT_MAX_DIM * (ROT_THREADS / WAVE)];
 };
 
+// Where the tokens of a tile lie.
 template <bool BACKWARD>
-__device__ __forceinline__ void rot_tokens(const RotArgs& a, RotShared& s, uint64_t first, uint32_t count) {
-    const uint32_t pairs = a.dim / 2;
-    for (uint32_t n = threadIdx.x; n < count * pairs; n += ROT_THREADS) {
-        const uint32_t t = n / pairs, j = n % pairs;
-        float c = 1.0f, d = 0.0f;
-        if (j < a.rot / 2) {
-            const uint64_t token = first + t, b = token / a.length;
-            const uint32_t i = (uint32_t)(token % a.length);
-            const int32_t position = a.positions ? a.positions[b * a.position_stride[0] + i * a.position_stride[1] + a.axis_of_pair[j]] : (int32_t)i;
-            const double turns = (double)position * (double)a.inv_freq[j] * 0.15915494309189533577;        // 1 / 2 pi
-            sincospif((float)(2.0 * (turns - rint(turns))), &d, &c);
-        }
-        reinterpret_cast<float*>(s.cosine)[n] = c;
-        reinterpret_cast<float*>(s.sine)[n] = d;
-    }
-    if (threadIdx.x < count) {
-        const uint64_t token = first + threadIdx.x, b = token / a.length, i = token % a.length;
-        TokenPlace p;
+__device__ __forceinline__ void rot_places(const RotArgs& a, RotShared& s, uint32_t first, uint32_t count) {
+    if (threadIdx.x >= count) return;
+    const uint32_t token = first + threadIdx.x, b = quotient(token, a.length), i = token - b * a.length.by;
+    TokenPlace p;
 #pragma unroll
-        for (int n = 0; n < 2; ++n) {
-            p.in[n] = b * a.t[n].in.batch + i * a.t[n].in.row;
-            if (BACKWARD) p.d[n] = b * a.t[n].d.batch + i * a.t[n].d.row;
-            p.out[n] = b * a.t[n].out.batch + i * a.t[n].out.row;
+    for (int n = 0; n < 2; ++n) {
+        p.in[n] = b * a.t[n].in.batch + i * a.t[n].in.row;
+        if (BACKWARD) p.d[n] = b * a.t[n].d.batch + i * a.t[n].d.row;
+        p.out[n] = b * a.t[n].out.batch + i * a.t[n].out.row;
+    }
+    s.place[threadIdx.x] = p;
+}
+
+// Cosines and sines of their pairs, each once.
+__device__ __forceinline__ void rot_angles(const RotArgs& a, RotShared& s, uint32_t first, uint32_t count) {
+    const uint32_t pairs = a.dim / 2, j = threadIdx.x & ((1u << a.pair_shift) - 1);
+    if (j >= pairs) return;
+    const bool turns = j < a.rot / 2;
+    const double freq = turns ? (double)a.inv_freq[j] * 0.15915494309189533577 : 0.0;        // in turns: 1 / 2 pi
+    const uint32_t axis = turns ? a.axis_of_pair[j] : 0;
+    for (uint32_t t = threadIdx.x >> a.pair_shift; t < count; t += ROT_THREADS >> a.pair_shift) {
+        float c = 1.0f, d = 0.0f;
+        if (turns) {
+            const uint32_t token = first + t, b = quotient(token, a.length), i = token - b * a.length.by;
+            const int32_t position = a.positions ? a.positions[b * a.position_stride[0] + i * a.position_stride[1] + axis] : (int32_t)i;
+            const double angle = (double)position * freq;
+            sincospif((float)(2.0 * (angle - rint(angle))), &d, &c);
         }
-        s.place[threadIdx.x] = p;
+        reinterpret_cast<float*>(s.cosine)[t * pairs + j] = c;
+        reinterpret_cast<float*>(s.sine)[t * pairs + j] = d;
     }
 }
 
@@ -133,154 +158,197 @@ struct LanePlace {
         const bool apart = !a.adjacent && unit < a.rot / 8;
         return {apart ? unit * 4 : unit * 8, apart ? a.rot / 2 + unit * 4 : unit * 8 + 4, unit, unit * 8 < a.dim};
     }
-    template <typename T>
-    __device__ __forceinline__ Eights load(const T* head, bool adjacent) const {
-        return pairs(Eights{load_four(head + first), load_four(head + second)}, adjacent);
-    }
-    template <typename T>
+    template <bool NT, typename T>
     __device__ __forceinline__ void store(T* head, const Eights& v, bool adjacent) const {
         f32x4 x = v.a, y = v.b;
         if (adjacent) {
             x = f32x4{v.a[0], v.b[0], v.a[1], v.b[1]};
             y = f32x4{v.a[2], v.b[2], v.a[3], v.b[3]};
         }
-        store_four(head + first, x);
-        store_four(head + second, y);
+        store_four<NT>(head + first, x);
+        store_four<NT>(head + second, y);
     }
     static __device__ __forceinline__ Eights pairs(Eights v, bool adjacent) {
         if (!adjacent) return v;
         return {f32x4{v.a[0], v.a[2], v.b[0], v.b[2]}, f32x4{v.a[1], v.a[3], v.b[1], v.b[3]}};
     }
+    __device__ __forceinline__ Eights weight(const float* w, bool adjacent) const {
+        if (!w || !there) return {1.0f, 1.0f};
+        return pairs({wide_four<float>(raw_four<false>(w + first)), wide_four<float>(raw_four<false>(w + second))}, adjacent);
+    }
 };
 
-// Heads of a tile in the order in which a lane's group takes them.
+// Heads of a tile in the order in which a group of lanes takes them.
 struct HeadWalk {
     uint32_t token, head;
-    __device__ __forceinline__ void settle(uint32_t heads) {
-        while (head >= heads) {
-            head -= heads;
+    __device__ __forceinline__ void next(const RotTensor& t) {
+        token += t.step_tokens;
+        head += t.step_heads;
+        if (head >= t.heads) {
+            head -= t.heads;
             ++token;
         }
     }
+    template <int LANES>
+    static __device__ __forceinline__ HeadWalk begin(const RotTensor& t) {
+        HeadWalk w = {0, threadIdx.x / LANES};
+        while (w.head >= t.heads) {
+            w.head -= t.heads;
+            ++w.token;
+        }
+        return w;
+    }
 };
 
-template <typename T, int LANES, int N>
-__device__ __forceinline__ void rot_forward(const RotArgs& a, const RotShared& s, uint32_t count, const T* x, T* out) {
-    const RotTensor& t = a.t[N];
-    const LanePlace at = LanePlace::of<LANES>(a);
-    const uint32_t step = ROT_THREADS / LANES;
-    Eights w = {1.0f, 1.0f};
-    if (t.weight && at.there) w = at.load(t.weight, a.adjacent);
-    const float share = 1.0f / (float)a.dim;
-    HeadWalk walk = {0, threadIdx.x / LANES};
-    walk.settle(t.heads);
-    while (walk.token < count) {
-        HeadWalk mine[ROT_AHEAD];
-        Eights v[ROT_AHEAD];
+// A lane's parts of the next heads of its group, as they lie in memory.
+template <typename T, int N, bool BACKWARD, bool NT>
+struct HeadBatch {
+    static constexpr int AHEAD = ROT_AHEAD<T>;
+    HeadWalk at[AHEAD];
+    Four<T> x[AHEAD][2], d[BACKWARD ? AHEAD : 1][2];
+    __device__ __forceinline__ void load(const RotArgs& a, const RotShared& s, const LanePlace& lane, HeadWalk& walk, uint32_t count, const T* px, const T* pd) {
+        const RotTensor& t = a.t[N];
 #pragma unroll
-        for (int k = 0; k < ROT_AHEAD; ++k) {
-            mine[k] = walk;
-            v[k] = {0.0f, 0.0f};
-            if (walk.token < count && at.there) v[k] = at.load(x + s.place[walk.token].in[N] + walk.head * t.in.head, a.adjacent);
-            walk.head += step;
-            walk.settle(t.heads);
-        }
-#pragma unroll
-        for (int k = 0; k < ROT_AHEAD; ++k) {
-            if (mine[k].token >= count) break;                  // the same for all lanes of a head
-            if (t.weight) {
-                if (a.kind == OKT_NORM_LAYER) {
-                    const float mean = head_sum<LANES>(sum_of(v[k])) * share;
-                    if (at.there) {
-                        v[k].a -= mean;
-                        v[k].b -= mean;
-                    }
+        for (int k = 0; k < AHEAD; ++k) {
+            at[k] = walk;
+            x[k][0] = x[k][1] = Four<T>{};
+            if (BACKWARD) d[k][0] = d[k][1] = Four<T>{};
+            if (walk.token < count && lane.there) {
+                if (!BACKWARD || t.weight) {
+                    const T* head = px + s.place[walk.token].in[N] + (uint64_t)walk.head * t.in.head;
+                    x[k][0] = raw_four<NT>(head + lane.first);
+                    x[k][1] = raw_four<NT>(head + lane.second);
                 }
-                const float r = 1.0f / sqrtf(head_sum<LANES>(dot_of(v[k], v[k])) * share + a.eps);
-                v[k].a *= r * w.a;
-                v[k].b *= r * w.b;
+                if (BACKWARD) {
+                    const T* head = pd + s.place[walk.token].d[N] + (uint64_t)walk.head * t.d.head;
+                    d[k][0] = raw_four<NT>(head + lane.first);
+                    d[k][1] = raw_four<NT>(head + lane.second);
+                }
             }
-            if (!at.there) continue;
-            const uint32_t angle = mine[k].token * (a.dim / 8) + at.unit;
-            const f32x4 c = s.cosine[angle], d = s.sine[angle];
-            at.store(out + s.place[mine[k].token].out[N] + mine[k].head * t.out.head,
-                     Eights{v[k].a * c - v[k].b * d, v[k].a * d + v[k].b * c}, a.adjacent);
+            walk.next(t);
         }
     }
+};
+
+// x less its mean (layer norm) and the reciprocal of its deviation.
+template <int LANES>
+__device__ __forceinline__ float head_statistics(const RotArgs& a, const LanePlace& at, Eights& v) {
+    if (a.kind == OKT_NORM_LAYER) {
+        const float mean = head_sum<LANES>(sum_of(v)) * a.share;
+        if (at.there) {
+            v.a -= mean;
+            v.b -= mean;
+        }
+    }
+    return reciprocal_root(fmaf(head_sum<LANES>(dot_of(v, v)), a.share, a.eps));
 }
 
-template <typename T, int LANES>
+template <typename T, int LANES, int N, bool NT>
+struct Forward {
+    typedef HeadBatch<T, N, false, NT> Batch;
+    LanePlace at;
+    HeadWalk walk;
+    Batch now;
+    const T* x;
+    __device__ __forceinline__ Forward(const RotArgs& a, const RotShared& s, uint32_t count, const T* from) : at(LanePlace::of<LANES>(a)), x(from) {
+        if (a.t[N].heads == 0) return;
+        walk = HeadWalk::begin<LANES>(a.t[N]);
+        now.load(a, s, at, walk, count, x, nullptr);
+    }
+    __device__ __forceinline__ void run(const RotArgs& a, const RotShared& s, uint32_t count, T* out) {
+        const RotTensor& t = a.t[N];
+        if (t.heads == 0) return;
+        const Eights w = at.weight(t.weight, a.adjacent);
+        while (now.at[0].token < count) {
+#pragma unroll
+            for (int k = 0; k < Batch::AHEAD; ++k) {
+                if (now.at[k].token >= count) break;            // the same for all lanes of a head
+                Eights v = LanePlace::pairs({wide_four<T>(now.x[k][0]), wide_four<T>(now.x[k][1])}, a.adjacent);
+                const uint32_t angle = now.at[k].token * (a.dim / 8) + (at.there ? at.unit : 0);
+                f32x4 c = s.cosine[angle], d = s.sine[angle];
+                if (t.weight) {
+                    const float r = head_statistics<LANES>(a, at, v);
+                    v.a *= w.a;
+                    v.b *= w.b;
+                    c *= r;
+                    d *= r;
+                }
+                if (at.there)
+                    at.template store<NT>(out + s.place[now.at[k].token].out[N] + (uint64_t)now.at[k].head * t.out.head,
+                             Eights{fma_four(v.a, c, -(v.b * d)), fma_four(v.a, d, v.b * c)}, a.adjacent);
+            }
+            now.load(a, s, at, walk, count, x, nullptr);
+        }
+    }
+};
+
+template <typename T, int LANES, bool NT>
 __global__ __launch_bounds__(ROT_THREADS) void norm_rotary_forward_kernel(RotArgs a, RotPointers p) {
     __shared__ RotShared s;
-    const uint64_t first = (uint64_t)blockIdx.x * a.tile;
-    const uint32_t count = (uint32_t)(a.tokens - first < a.tile ? a.tokens - first : a.tile);
-    rot_tokens<false>(a, s, first, count);
+    const uint32_t first = blockIdx.x * a.tile, count = min(a.tokens - first, a.tile);
+    rot_places<false>(a, s, first, count);
     __syncthreads();
-    if (a.t[0].heads) rot_forward<T, LANES, 0>(a, s, count, (const T*)p.x[0], (T*)p.out[0]);
-    if (a.t[1].heads) rot_forward<T, LANES, 1>(a, s, count, (const T*)p.x[1], (T*)p.out[1]);
+    Forward<T, LANES, 0, NT> q(a, s, count, (const T*)p.x[0]);           // on their way while the angles are made
+    rot_angles(a, s, first, count);
+    __syncthreads();
+    q.run(a, s, count, (T*)p.out[0]);
+    Forward<T, LANES, 1, NT> k(a, s, count, (const T*)p.x[1]);
+    k.run(a, s, count, (T*)p.out[1]);
 }
 
-template <typename T, int LANES, int N>
-__device__ __forceinline__ void rot_backward(const RotArgs& a, const RotShared& s, uint32_t count, const T* x, const T* dy, T* out,
-                                             Eights& dw) {
-    constexpr int AHEAD = ROT_AHEAD / 2;
-    const RotTensor& t = a.t[N];
-    const LanePlace at = LanePlace::of<LANES>(a);
-    const uint32_t step = ROT_THREADS / LANES;
-    Eights w = {1.0f, 1.0f};
-    if (t.weight && at.there) w = at.load(t.weight, a.adjacent);
-    const float share = 1.0f / (float)a.dim;
-    HeadWalk walk = {0, threadIdx.x / LANES};
-    walk.settle(t.heads);
-    while (walk.token < count) {
-        HeadWalk mine[AHEAD];
-        Eights v[AHEAD], d[AHEAD];
+template <typename T, int LANES, int N, bool NT>
+struct Backward {
+    typedef HeadBatch<T, N, true, NT> Batch;
+    LanePlace at;
+    HeadWalk walk;
+    Batch now;
+    const T *x, *dy;
+    __device__ __forceinline__ Backward(const RotArgs& a, const RotShared& s, uint32_t count, const T* px, const T* pd)
+        : at(LanePlace::of<LANES>(a)), x(px), dy(pd) {
+        if (a.t[N].heads == 0) return;
+        walk = HeadWalk::begin<LANES>(a.t[N]);
+        now.load(a, s, at, walk, count, x, dy);
+    }
+    __device__ __forceinline__ void run(const RotArgs& a, const RotShared& s, uint32_t count, T* out, Eights& dw) {
+        const RotTensor& t = a.t[N];
+        if (t.heads == 0) return;
+        const Eights w = at.weight(t.weight, a.adjacent);
+        while (now.at[0].token < count) {
 #pragma unroll
-        for (int k = 0; k < AHEAD; ++k) {
-            mine[k] = walk;
-            v[k] = d[k] = {0.0f, 0.0f};
-            if (walk.token < count && at.there) {
-                d[k] = at.load(dy + s.place[walk.token].d[N] + walk.head * t.d.head, a.adjacent);
-                if (t.weight) v[k] = at.load(x + s.place[walk.token].in[N] + walk.head * t.in.head, a.adjacent);
-            }
-            walk.head += step;
-            walk.settle(t.heads);
-        }
-#pragma unroll
-        for (int k = 0; k < AHEAD; ++k) {
-            if (mine[k].token >= count) break;
-            const uint32_t angle = mine[k].token * (a.dim / 8) + (at.there ? at.unit : 0);
-            const f32x4 c = s.cosine[angle], e = s.sine[angle];
-            Eights g = {d[k].a * c + d[k].b * e, d[k].b * c - d[k].a * e};
-            if (t.weight) {
-                const bool layer = a.kind == OKT_NORM_LAYER;
-                if (layer) {
-                    const float mean = head_sum<LANES>(sum_of(v[k])) * share;
-                    if (at.there) {
-                        v[k].a -= mean;
-                        v[k].b -= mean;
+            for (int k = 0; k < Batch::AHEAD; ++k) {
+                if (now.at[k].token >= count) break;
+                const uint32_t angle = now.at[k].token * (a.dim / 8) + (at.there ? at.unit : 0);
+                const f32x4 c = s.cosine[angle], e = s.sine[angle];
+                const Eights d = LanePlace::pairs({wide_four<T>(now.d[k][0]), wide_four<T>(now.d[k][1])}, a.adjacent);
+                Eights g = {fma_four(d.a, c, d.b * e), fma_four(d.b, c, -(d.a * e))};
+                if (t.weight) {
+                    Eights v = LanePlace::pairs({wide_four<T>(now.x[k][0]), wide_four<T>(now.x[k][1])}, a.adjacent);
+                    const float r = head_statistics<LANES>(a, at, v);
+                    v.a *= r;                                   // h
+                    v.b *= r;
+                    dw.a = fma_four(g.a, v.a, dw.a);
+                    dw.b = fma_four(g.b, v.b, dw.b);
+                    g.a *= w.a;
+                    g.b *= w.b;
+                    const float along = head_sum<LANES>(dot_of(g, v)) * a.share;
+                    if (a.kind == OKT_NORM_LAYER) {
+                        const float level = head_sum<LANES>(sum_of(g)) * a.share;
+                        g.a -= level;
+                        g.b -= level;
                     }
+                    g.a = r * fma_four(v.a, f32x4(-along), g.a);
+                    g.b = r * fma_four(v.b, f32x4(-along), g.b);
                 }
-                const float r = 1.0f / sqrtf(head_sum<LANES>(dot_of(v[k], v[k])) * share + a.eps);
-                v[k].a *= r;                                    // h
-                v[k].b *= r;
-                dw.a += g.a * v[k].a;
-                dw.b += g.b * v[k].b;
-                g.a *= w.a;
-                g.b *= w.b;
-                const float along = head_sum<LANES>(dot_of(g, v[k])) * share;
-                const float level = layer ? head_sum<LANES>(sum_of(g)) * share : 0.0f;
-                g.a = r * (g.a - v[k].a * along - level);
-                g.b = r * (g.b - v[k].b * along - level);
+                if (at.there) at.template store<NT>(out + s.place[now.at[k].token].out[N] + (uint64_t)now.at[k].head * t.out.head, g, a.adjacent);
             }
-            if (at.there) at.store(out + s.place[mine[k].token].out[N] + mine[k].head * t.out.head, g, a.adjacent);
+            now.load(a, s, at, walk, count, x, dy);
         }
     }
-}
+};
 
 // A workgroup's sums of a weight's gradient, over its lanes of one unit; in the order of the elements of a head.
 template <int LANES>
-__device__ __forceinline__ void rot_sums(const RotArgs& a, RotShared& s, int n, const Eights& dw, float* to) {
+__device__ __forceinline__ void rot_sums(const RotArgs& a, float* sums, const Eights& dw, float* to) {
     const LanePlace at = LanePlace::of<LANES>(a);
     float v[8] = {dw.a[0], dw.a[1], dw.a[2], dw.a[3], dw.b[0], dw.b[1], dw.b[2], dw.b[3]};
 #pragma unroll
@@ -292,41 +360,45 @@ __device__ __forceinline__ void rot_sums(const RotArgs& a, RotShared& s, int n, 
         for (int i = 0; i < 8; ++i) {
             // element i of the pairs' order in the head's
             const uint32_t e = a.adjacent ? at.unit * 8 + 2 * (i % 4) + i / 4 : (i < 4 ? at.first + i : at.second + i - 4);
-            s.sums[n][threadIdx.x / WAVE * ROT_MAX_DIM + e] = v[i];
+            sums[threadIdx.x / WAVE * ROT_MAX_DIM + e] = v[i];
         }
     __syncthreads();
     for (uint32_t e = threadIdx.x; e < a.dim; e += ROT_THREADS) {
         float sum = 0.0f;
 #pragma unroll
-        for (int wave = 0; wave < ROT_THREADS / WAVE; ++wave) sum += s.sums[n][wave * ROT_MAX_DIM + e];
+        for (int wave = 0; wave < ROT_THREADS / WAVE; ++wave) sum += sums[wave * ROT_MAX_DIM + e];
         to[e] = sum;
     }
 }
 
-template <typename T, int LANES>
+template <typename T, int LANES, bool NT>
 __global__ __launch_bounds__(ROT_THREADS) void norm_rotary_backward_kernel(RotArgs a, RotPointers p) {
     __shared__ RotShared s;
+    __shared__ float sums[2][ROT_MAX_DIM * (ROT_THREADS / WAVE)];
     Eights dw[2] = {{0.0f, 0.0f}, {0.0f, 0.0f}};
-    for (uint64_t tile = blockIdx.x; tile < a.tiles; tile += a.groups) {
-        const uint64_t first = tile * a.tile;
-        const uint32_t count = (uint32_t)(a.tokens - first < a.tile ? a.tokens - first : a.tile);
-        rot_tokens<true>(a, s, first, count);
+    for (uint32_t tile = blockIdx.x; tile < a.tiles; tile += a.groups) {
+        const uint32_t first = tile * a.tile, count = min(a.tokens - first, a.tile);
+        rot_places<true>(a, s, first, count);
         __syncthreads();
-        if (a.t[0].heads) rot_backward<T, LANES, 0>(a, s, count, (const T*)p.x[0], (const T*)p.d[0], (T*)p.out[0], dw[0]);
-        if (a.t[1].heads) rot_backward<T, LANES, 1>(a, s, count, (const T*)p.x[1], (const T*)p.d[1], (T*)p.out[1], dw[1]);
+        Backward<T, LANES, 0, NT> q(a, s, count, (const T*)p.x[0], (const T*)p.d[0]);
+        rot_angles(a, s, first, count);
+        __syncthreads();
+        q.run(a, s, count, (T*)p.out[0], dw[0]);
+        Backward<T, LANES, 1, NT> k(a, s, count, (const T*)p.x[1], (const T*)p.d[1]);
+        k.run(a, s, count, (T*)p.out[1], dw[1]);
         __syncthreads();
     }
     if (!a.partial) return;
 #pragma unroll
     for (int n = 0; n < 2; ++n)
-        rot_sums<LANES>(a, s, n, dw[n], a.partial + ((uint64_t)n * a.groups + blockIdx.x) * a.dim);
+        rot_sums<LANES>(a, sums[n], dw[n], a.partial + ((uint64_t)n * a.groups + blockIdx.x) * a.dim);
 }
 
-// Adds the workgroups' sums, always in the same order: sixteen columns by sixteen parts a workgroup.
-constexpr int ROT_ADD_COLS = 16;
+// Adds the workgroups' sums, always in the same order: sixteen columns by 64 parts a workgroup.
+constexpr int ROT_ADD_COLS = 16, ROT_ADD_THREADS = 1024;
 struct RotGradients { float* to[2]; };
-__global__ __launch_bounds__(ROT_THREADS) void norm_rotary_add_kernel(const float* partial, uint32_t groups, uint32_t dim, RotGradients g) {
-    constexpr int PARTS = ROT_THREADS / ROT_ADD_COLS;
+__global__ __launch_bounds__(ROT_ADD_THREADS) void norm_rotary_add_kernel(const float* partial, uint32_t groups, uint32_t dim, RotGradients g) {
+    constexpr int PARTS = ROT_ADD_THREADS / ROT_ADD_COLS;
     __shared__ float sums[PARTS][ROT_ADD_COLS];
     const uint32_t n = blockIdx.y, part = threadIdx.x / ROT_ADD_COLS, col = threadIdx.x % ROT_ADD_COLS, e = blockIdx.x * ROT_ADD_COLS + col;
     float sum = 0.0f;
@@ -358,7 +430,7 @@ static uint32_t rot_groups(uint64_t tiles) { return (uint32_t)(tiles < ROT_BACKW
 
 static bool rot_sizes(uint32_t batch, uint32_t length, uint32_t heads, uint32_t kv_heads, uint32_t dim) {
     return heads <= 1u << 16 && kv_heads <= 1u << 16 && heads + kv_heads > 0 && dim >= 8 && dim <= ROT_MAX_DIM && dim % 8 == 0 &&
-           length <= 1u << 31 && (uint64_t)batch * length < 1ull << 24;
+           (uint64_t)batch * length < 1ull << 24;
 }
 
 static bool rot_args(const okt_norm_rotary* op, RotArgs& a) {
@@ -374,9 +446,12 @@ static bool rot_args(const okt_norm_rotary* op, RotArgs& a) {
         if (op->axis_of_pair[j] >= op->axes) return false;
         a.axis_of_pair[j] = op->axis_of_pair[j];
     }
-    a.tokens = (uint64_t)op->batch * op->length;
-    a.length = op->length;
+    a.tokens = op->batch * op->length;
+    a.length = divider(op->length);
     a.dim = op->head_dim;
+    a.share = 1.0f / (float)op->head_dim;
+    a.pair_shift = 2;
+    while (1u << a.pair_shift < op->head_dim / 2) ++a.pair_shift;
     a.rot = op->rot_dim;
     a.kind = op->kind;
     a.adjacent = op->adjacent != 0;
@@ -385,9 +460,13 @@ static bool rot_args(const okt_norm_rotary* op, RotArgs& a) {
     a.positions = op->d_positions;
     a.position_stride[0] = op->position_stride[0];
     a.position_stride[1] = op->position_stride[1];
-    const auto strides = [](const uint64_t* s) { return HeadStrides{s[0], s[1], s[2]}; };
-    a.t[0] = {op->heads, op->d_q_weight, strides(op->q_stride), strides(op->dq_stride), strides(op->q_out_stride)};
-    a.t[1] = {op->kv_heads, op->d_k_weight, strides(op->k_stride), strides(op->dk_stride), strides(op->k_out_stride)};
+    for (const uint64_t* s : {op->q_stride, op->k_stride, op->q_out_stride, op->k_out_stride, op->dq_stride, op->dk_stride})
+        if (s[0] > 1ull << 40 || s[1] > 1ull << 40 || s[2] > 1ull << 30) return false;
+    const auto strides = [](const uint64_t* s) { return HeadStrides{s[0], s[1], (uint32_t)s[2]}; };
+    const uint32_t step = ROT_THREADS / rot_lanes(op->head_dim);
+    const auto steps = [&](uint32_t heads, bool rest) { return heads == 0 ? 0 : rest ? step % heads : step / heads; };
+    a.t[0] = {op->heads, steps(op->heads, false), steps(op->heads, true), op->d_q_weight, strides(op->q_stride), strides(op->dq_stride), strides(op->q_out_stride)};
+    a.t[1] = {op->kv_heads, steps(op->kv_heads, false), steps(op->kv_heads, true), op->d_k_weight, strides(op->k_stride), strides(op->dk_stride), strides(op->k_out_stride)};
     a.partial = nullptr;
     if (a.tokens == 0) return true;
     a.tile = rot_tile(a.tokens, op->heads + op->kv_heads, op->head_dim);
@@ -400,8 +479,8 @@ struct Placed { const void* p; HeadStrides s; uint32_t heads; };
 
 // An output whose tokens or heads are the same memory.
 static bool shares_places(const RotArgs& a, const HeadStrides& s, uint32_t heads) {
-    const uint64_t batch = a.tokens / a.length;
-    return (batch > 1 && s.batch < a.dim) || (a.length > 1 && s.row < a.dim) || (heads > 1 && s.head < a.dim);
+    const uint32_t batch = a.tokens / a.length.by;
+    return (batch > 1 && s.batch < a.dim) || (a.length.by > 1 && s.row < a.dim) || (heads > 1 && s.head < a.dim);
 }
 
 // Whether an output and another tensor share an element: exactly where their strides are alike, as parts of one
@@ -428,8 +507,13 @@ static bool same(const Placed& x, const Placed& y) {
 
 template <typename T, int LANES>
 static void launch_rot(const RotArgs& a, const RotPointers& p, bool backward, hipStream_t s) {
-    if (backward) hipLaunchKernelGGL((norm_rotary_backward_kernel<T, LANES>), dim3(a.groups), dim3(ROT_THREADS), 0, s, a, p);
-    else hipLaunchKernelGGL((norm_rotary_forward_kernel<T, LANES>), dim3((unsigned)a.tiles), dim3(ROT_THREADS), 0, s, a, p);
+    const bool around = (uint64_t)a.tokens * (a.t[0].heads + a.t[1].heads) * a.dim * sizeof(T) * (backward ? 3 : 2) > ROT_CACHED_BYTES;
+    if (backward)
+        hipLaunchKernelGGL((around ? norm_rotary_backward_kernel<T, LANES, true> : norm_rotary_backward_kernel<T, LANES, false>), dim3(a.groups),
+                           dim3(ROT_THREADS), 0, s, a, p);
+    else
+        hipLaunchKernelGGL((around ? norm_rotary_forward_kernel<T, LANES, true> : norm_rotary_forward_kernel<T, LANES, false>), dim3(a.tiles),
+                           dim3(ROT_THREADS), 0, s, a, p);
 }
 template <typename T>
 static void launch_rot_lanes(const RotArgs& a, const RotPointers& p, bool backward, hipStream_t s) {
@@ -512,7 +596,7 @@ int okt_norm_rotary_backward(const okt_norm_rotary* op, const void* d_q, const v
         if (const int status = launch_rot_type(op->dtype, a, p, true, (hipStream_t)stream)) return status;
     }
     if (sums)
-        hipLaunchKernelGGL(norm_rotary_add_kernel, dim3((a.dim + ROT_ADD_COLS - 1) / ROT_ADD_COLS, 2), dim3(ROT_THREADS), 0, (hipStream_t)stream,
+        hipLaunchKernelGGL(norm_rotary_add_kernel, dim3((a.dim + ROT_ADD_COLS - 1) / ROT_ADD_COLS, 2), dim3(ROT_ADD_THREADS), 0, (hipStream_t)stream,
                            (const float*)d_ws, a.tokens ? a.groups : 0, a.dim, g);
     return sums ? launch_status() : OKT_OK;
 }

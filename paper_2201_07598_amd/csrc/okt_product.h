@@ -124,7 +124,8 @@ __device__ __forceinline__ void product(f32x16 (&c)[S::MT][S::NT], A& a, B& b, c
         for (int n = 0; n < S::NT; ++n) c[m][n] = 0.0f;
     if (k == 0) return;
     constexpr uint32_t BUFFER = A::BYTES + B::BYTES;
-    constexpr int LOADS = A::LOADS + B::LOADS, STEPS = PRODUCT_K / 16, EACH = (LOADS / 2 + S::MT - 1) / S::MT;
+    constexpr int LOADS = A::LOADS + B::LOADS, STEPS = PRODUCT_K / 16, EARLY = LOADS / 2, LATE = LOADS - EARLY;      // fetches in the last step, in the first
+    constexpr int EACH = ((EARLY > LATE ? EARLY : LATE) + S::MT - 1) / S::MT;
     const uint32_t at = lds_address(lds);
     const int m0 = S::wave_m() * S::MT, n0 = S::wave_n() * S::NT;
     frag<T> x[2][S::MT], y[2][S::NT];
@@ -152,7 +153,7 @@ __device__ __forceinline__ void product(f32x16 (&c)[S::MT][S::NT], A& a, B& b, c
     uint32_t now = 0;
     handed_over();
 #pragma unroll
-    for (int i = 0; i < LOADS / 2; ++i) fetch(i, BUFFER, k - PRODUCT_K);
+    for (int i = 0; i < EARLY; ++i) fetch(i, BUFFER, k - PRODUCT_K);
 #pragma unroll
     for (int m = 0; m < S::MT; ++m) read(0, m, lds, 0);
     for (uint32_t done = PRODUCT_K; ; done += PRODUCT_K) {           // k up to the end of this piece
@@ -170,8 +171,8 @@ __device__ __forceinline__ void product(f32x16 (&c)[S::MT][S::NT], A& a, B& b, c
                 read((s + 1) % 2, m, piece, (s + 1) % STEPS);
 #pragma unroll
                 for (int i = 0; i < EACH; ++i) {
-                    if (s == 0 && m * EACH + i < LOADS - LOADS / 2) fetch(LOADS / 2 + m * EACH + i, now ^ BUFFER, left);
-                    if (s == STEPS - 1 && m * EACH + i < LOADS / 2) fetch(m * EACH + i, now, left > PRODUCT_K ? left - PRODUCT_K : PRODUCT_K);
+                    if (s == 0 && m * EACH + i < LATE) fetch(EARLY + m * EACH + i, now ^ BUFFER, left);
+                    if (s == STEPS - 1 && m * EACH + i < EARLY) fetch(m * EACH + i, now, left > PRODUCT_K ? left - PRODUCT_K : PRODUCT_K);
                 }
 #pragma unroll
                 for (int n = 0; n < S::NT; ++n) c[m][n] = mfma(x[s % 2][m], y[s % 2][n], c[m][n]);
