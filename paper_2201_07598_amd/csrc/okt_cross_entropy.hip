@@ -28,8 +28,8 @@ constexpr uint32_t CE_MAX_WIDTH = 1u << 15;
 constexpr int CE_THREADS = 256;
 constexpr float LOG2E = 1.44269504088896340736f;
 
-typedef ProductShape<4, 2, 2, 4> Large;                              // 256 x 256, one workgroup of eight waves a CU
-typedef ProductShape<2, 2, 2, 2> Small;                              // 128 x 128, two
+typedef ProductShape<4, 2, 2, 4, 2> Large;                           // 256 x 256, one workgroup of eight waves a CU
+typedef ProductShape<2, 2, 2, 2, 4> Small;                           // 128 x 128, four waves and three pieces on their way
 
 template <typename T> constexpr bool RAISED = false;
 template <> constexpr bool RAISED<_Float16> = true;
@@ -133,44 +133,47 @@ __global__ __launch_bounds__(CE_THREADS) void cross_entropy_gather_kernel(CeArgs
         const int by = use ? min(max(15 - e, -120), 120) : 0;
         *a.header = {c.all, ldexpf(1.0f, by), ldexpf(1.0f, -by), 0};
     }
-    const auto put = [&](uint32_t n, const T* from) {                // a row, or zeros
-        T* to = (T*)a.h + (uint64_t)n * a.width_pad;
-#pragma unroll 4
-        for (uint32_t x = lane * 8; x < a.width_pad; x += WAVE * 8) {
-            vec v = {};
-            if (from && x < a.width) v = *reinterpret_cast<const vec*>(from + x);
-            *reinterpret_cast<vec*>(to + x) = v;
-        }
-    };
-    uint32_t n = c.before;
-    for (uint32_t i = 0; i < CE_GATHERED; ++i) {
+    // the sixteen labels at once; a wave takes four rows, whose vectors are on their way together
+    const bool inside = lane < CE_GATHERED && first + lane < a.rows;
+    const int64_t y = inside ? a.labels[first + lane] : -1;
+    const uint64_t listed = __ballot(labelled(y, a.vocab));
+    constexpr int EACH = CE_GATHERED / (CE_THREADS / WAVE);
+    const T* from[EACH];
+    T* to[EACH];
+#pragma unroll
+    for (int q = 0; q < EACH; ++q) {
+        const uint32_t i = wave * EACH + q;
         const uint64_t row = first + i;
-        if (row >= a.rows) break;
-        const int64_t y = a.labels[row];
-        const bool there = labelled(y, a.vocab), mine = i % (CE_THREADS / WAVE) == wave;
-        if (mine && there) {
-            put(n, h + row * a.h_stride);
-            if (lane == 0) {
-                a.list[n] = (uint32_t)row;
-                a.label_of[n] = (int32_t)y;
-                if (dloss) {
-                    a.lse_of[n] = lse_in[row];
-                    a.g_of[n] = dloss[row * a.dloss_step];
-                }
+        const uint32_t n = c.before + __popcll(listed & ((1ull << i) - 1));
+        from[q] = listed >> i & 1 ? h + row * a.h_stride : nullptr;
+        to[q] = from[q] ? (T*)a.h + (uint64_t)n * a.width_pad : row < a.rows && dh ? dh + row * a.dh_stride : nullptr;
+        if (row >= a.rows || lane != i) continue;
+        if (from[q]) {
+            a.list[n] = (uint32_t)row;
+            a.label_of[n] = (int32_t)y;
+            if (dloss) {
+                a.lse_of[n] = lse_in[row];
+                a.g_of[n] = dloss[row * a.dloss_step];
             }
-        } else if (mine) {
-            if (dh)
-                for (uint32_t x = lane * 8; x < a.width; x += WAVE * 8) *reinterpret_cast<vec*>(dh + row * a.dh_stride + x) = vec{};
-            if (lane == 0 && loss) {
-                loss[row] = 0.0f;
-                if (lse_out) lse_out[row] = 0.0f;
-            }
+        } else if (loss) {
+            loss[row] = 0.0f;
+            if (lse_out) lse_out[row] = 0.0f;
         }
-        n += there;
+    }
+    for (uint32_t x = lane * 8; x < a.width_pad; x += WAVE * 8) {
+        vec v[EACH];
+#pragma unroll
+        for (int q = 0; q < EACH; ++q) {
+            v[q] = vec{};
+            if (from[q] && x < a.width) v[q] = *reinterpret_cast<const vec*>(from[q] + x);
+        }
+#pragma unroll
+        for (int q = 0; q < EACH; ++q)
+            if (to[q] && (from[q] || x < a.width)) *reinterpret_cast<vec*>(to[q] + x) = v[q];
     }
     const uint32_t end = (c.all + CE_PAD - 1) / CE_PAD * CE_PAD;
     for (uint32_t z = c.all + blockIdx.x * (CE_THREADS / WAVE) + wave; z < end; z += gridDim.x * (CE_THREADS / WAVE)) {
-        put(z, nullptr);
+        for (uint32_t x = lane * 8; x < a.width_pad; x += WAVE * 8) *reinterpret_cast<vec*>((T*)a.h + (uint64_t)z * a.width_pad + x) = vec{};
         if (lane == 0) {
             a.label_of[z] = -1;
             if (dloss) a.lse_of[z] = a.g_of[z] = 0.0f;

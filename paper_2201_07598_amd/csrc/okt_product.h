@@ -94,19 +94,21 @@ struct Transposed {
     }
 };
 
-// WM x WN waves of MT x NT squares.
-template <int MT_, int NT_, int WM_, int WN_>
+// WM x WN waves of MT x NT squares, and buffers in LDS for STAGES pieces: one is worked on, the others are on their way.
+template <int MT_, int NT_, int WM_, int WN_, int STAGES_>
 struct ProductShape {
-    static constexpr int MT = MT_, NT = NT_, WM = WM_, WN = WN_, WAVES = WM * WN, THREADS = WAVES * WAVE;
+    static constexpr int MT = MT_, NT = NT_, WM = WM_, WN = WN_, STAGES = STAGES_, WAVES = WM * WN, THREADS = WAVES * WAVE;
     static constexpr int TILE_M = WM * MT * 32, TILE_N = WN * NT * 32;
-    static constexpr int BYTES = 2 * (TILE_M + TILE_N) * PRODUCT_K * 2;
+    static constexpr int BYTES = STAGES * (TILE_M + TILE_N) * PRODUCT_K * 2;
     static __device__ __forceinline__ int wave_m() { return (int)uniform(threadIdx.x / WAVE) % WM; }
     static __device__ __forceinline__ int wave_n() { return (int)uniform(threadIdx.x / WAVE) / WM; }
 };
 
-// Waits for this wave's fetches into LDS and its reads from there, then for the other waves.
+// Waits for this wave's fetches into LDS but the last LEFT, and for its reads from there, then for the other waves.
+template <int LEFT>
 __device__ __forceinline__ void handed_over() {
-    __builtin_amdgcn_s_waitcnt(0x0070);           // vmcnt(0), lgkmcnt(0)
+    static_assert(LEFT < 64, "the counter has six bits");
+    __builtin_amdgcn_s_waitcnt((LEFT & 15) | (LEFT >> 4) << 14 | 0x0070);      // vmcnt(LEFT), lgkmcnt(0)
     __syncthreads();
 }
 
@@ -124,15 +126,26 @@ __device__ __forceinline__ void product(f32x16 (&c)[S::MT][S::NT], A& a, B& b, c
         for (int n = 0; n < S::NT; ++n) c[m][n] = 0.0f;
     if (k == 0) return;
     constexpr uint32_t BUFFER = A::BYTES + B::BYTES;
-    constexpr int LOADS = A::LOADS + B::LOADS, STEPS = PRODUCT_K / 16, EARLY = LOADS / 2, LATE = LOADS - EARLY;      // fetches in the last step, in the first
+    constexpr int LOADS = A::LOADS + B::LOADS, STEPS = PRODUCT_K / 16, LEFT = (S::STAGES - 2) * LOADS;
+    constexpr int EARLY = LOADS / 2, LATE = LOADS - EARLY;           // fetches in the last step, in the first
     constexpr int EACH = ((EARLY > LATE ? EARLY : LATE) + S::MT - 1) / S::MT;
     const uint32_t at = lds_address(lds);
     const int m0 = S::wave_m() * S::MT, n0 = S::wave_n() * S::NT;
     frag<T> x[2][S::MT], y[2][S::NT];
-    i32x4 buffer_a = a.from.buffer(), buffer_b = b.from.buffer();
-    const auto fetch = [&](int i, uint32_t to, uint32_t there) {
+    i32x4 buffer_a, buffer_b;
+    uint32_t ahead = 0, there = 0;                                   // k before the piece that is fetched, and in and behind it
+    const auto fetch = [&](int i, uint32_t to) {
         if (i < A::LOADS) a.fetch(i, at + to, buffer_a, there);
         else if (i < LOADS) b.fetch(i - A::LOADS, at + to + A::BYTES, buffer_b, there);
+    };
+    const auto next_piece = [&] {
+        there = ahead < k ? k - ahead : 0;
+        buffer_a = a.from.buffer();
+        buffer_b = b.from.buffer();
+        if (there == 0) buffer_a[2] = buffer_b[2] = 0;               // past the end nothing is read
+        a.advance();
+        b.advance();
+        ahead += PRODUCT_K;
     };
     // the operands of a step that a group of products covers
     const auto read = [&](int set, int m, const char* piece, int s) {
@@ -140,49 +153,47 @@ __device__ __forceinline__ void product(f32x16 (&c)[S::MT][S::NT], A& a, B& b, c
         if (m < S::NT) y[set][m] = b.operand(piece + A::BYTES, n0 + m, s);
     };
     static_assert(S::NT <= S::MT, "a group reads one operand of each side");
-    const auto next_piece = [&](uint32_t done) {                     // of which `done` k are before it
-        a.advance();
-        b.advance();
-        buffer_a = a.from.buffer();
-        buffer_b = b.from.buffer();
-        if (done >= k) buffer_a[2] = buffer_b[2] = 0;                // past the end nothing is read
-    };
 #pragma unroll
-    for (int i = 0; i < LOADS; ++i) fetch(i, 0, k);
-    next_piece(PRODUCT_K);
-    uint32_t now = 0;
-    handed_over();
+    for (int p = 0; p < S::STAGES - 1; ++p) {
+        next_piece();
 #pragma unroll
-    for (int i = 0; i < EARLY; ++i) fetch(i, BUFFER, k - PRODUCT_K);
+        for (int i = 0; i < LOADS; ++i) fetch(i, p * BUFFER);
+    }
+    handed_over<LEFT>();
+    next_piece();
+    uint32_t now = 0, filled = (S::STAGES - 1) * BUFFER;             // the buffer that is worked on, and the one that is filled
+#pragma unroll
+    for (int i = 0; i < EARLY; ++i) fetch(i, filled);
 #pragma unroll
     for (int m = 0; m < S::MT; ++m) read(0, m, lds, 0);
     for (uint32_t done = PRODUCT_K; ; done += PRODUCT_K) {           // k up to the end of this piece
-        const uint32_t left = done < k ? k - done : PRODUCT_K;       // and of the next one
+        const uint32_t next = now + BUFFER < S::BYTES ? now + BUFFER : 0;
 #pragma unroll
         for (int s = 0; s < STEPS; ++s) {
             if (s == STEPS - 1) {
-                next_piece(done + PRODUCT_K);
-                handed_over();
+                handed_over<LEFT>();
+                next_piece();
+                filled = now;
             }
-            const char* piece = lds + (s == STEPS - 1 ? now ^ BUFFER : now);
+            const char* piece = lds + (s == STEPS - 1 ? next : now);
 #pragma unroll
             for (int m = 0; m < S::MT; ++m) {
                 __builtin_amdgcn_sched_barrier(0);
                 read((s + 1) % 2, m, piece, (s + 1) % STEPS);
 #pragma unroll
                 for (int i = 0; i < EACH; ++i) {
-                    if (s == 0 && m * EACH + i < LATE) fetch(EARLY + m * EACH + i, now ^ BUFFER, left);
-                    if (s == STEPS - 1 && m * EACH + i < EARLY) fetch(m * EACH + i, now, left > PRODUCT_K ? left - PRODUCT_K : PRODUCT_K);
+                    if (s == 0 && m * EACH + i < LATE) fetch(EARLY + m * EACH + i, filled);
+                    if (s == STEPS - 1 && m * EACH + i < EARLY) fetch(m * EACH + i, filled);
                 }
 #pragma unroll
                 for (int n = 0; n < S::NT; ++n) c[m][n] = mfma(x[s % 2][m], y[s % 2][n], c[m][n]);
             }
         }
-        now ^= BUFFER;
+        now = next;
         if (done >= k) break;
     }
     __builtin_amdgcn_sched_barrier(0);
-    handed_over();                                                       // nothing is on its way into LDS any more
+    handed_over<0>();                                                // nothing is on its way into LDS any more
 }
 
 }  // namespace okt
