@@ -209,52 +209,100 @@ __device__ __forceinline__ void logits_of_row(float (&s)[S::MT * 16], const f32x
         }
 }
 
+template <typename T, class S> using LogitProduct = Product<T, S, KMajor<T, S::TILE_M, S::WAVES, true>, KMajor<T, S::TILE_N, S::WAVES, false>>;
+
+// Of the tile that begins at vocabulary v and listed row n.
 template <typename T, class S>
-__device__ __forceinline__ void logits(f32x16 (&c)[S::MT][S::NT], const CeArgs& a, const T* weight, uint32_t v, uint32_t n, char* lds) {
-    KMajor<T, S::TILE_M, S::WAVES, true> x(weight + v * a.weight_stride, weight + (a.vocab - 1) * a.weight_stride + a.width, (uint32_t)(a.weight_stride * 2));
+__device__ __forceinline__ LogitProduct<T, S> logits_at(const CeArgs& a, const T* weight, uint32_t v, uint32_t n, const char* lds) {
     const T* h = (const T*)a.h;
-    KMajor<T, S::TILE_N, S::WAVES, false> y(h + (uint64_t)n * a.width_pad, h + (uint64_t)a.rows_pad * a.width_pad, a.width_pad * 2);
-    product<T, S>(c, x, y, lds, a.width);
+    return LogitProduct<T, S>(
+        {weight + v * a.weight_stride, weight + (a.vocab - 1) * a.weight_stride + a.width, (uint32_t)(a.weight_stride * 2)},
+        {h + (uint64_t)n * a.width_pad, h + (uint64_t)a.rows_pad * a.width_pad, a.width_pad * 2}, a.width, lds);
+}
+
+// What a lane has to know of its rows; fetched before the next tile's operands are, behind which it would arrive.
+template <class S>
+struct RowFacts {
+    uint32_t label[S::NT];
+    float g[S::NT], lse[S::NT];
+    __device__ __forceinline__ RowFacts(const CeArgs& a, uint32_t row, bool backward) {
+#pragma unroll
+        for (int n = 0; n < S::NT; ++n) {
+            label[n] = (uint32_t)a.label_of[row + n * 32];
+            if (backward) {
+                g[n] = a.g_of[row + n * 32];
+                lse[n] = a.lse_of[row + n * 32];
+            }
+        }
+    }
+};
+
+// Tiles of logits.  Where a workgroup has a CU for itself it stays, and the next tile's first operands are on their way while this one's logits are
+// worked on (2458 rows x 1024 x 30522: 164 -> 157 us; small tiles, of which there are few, gain nothing and lose 1.4 us).  `finish` is called with the tile's sums, its place, its bias and its rows' facts.
+template <class S> constexpr bool STAYS = S::STAGES == 2;
+
+template <typename T, class S, bool BACKWARD, class F>
+__device__ __forceinline__ void logit_tiles(const CeArgs& a, const T* weight, uint32_t from, uint32_t columns, const F& finish) {
+    __shared__ __attribute__((aligned(1024))) char lds[S::BYTES];
+    __shared__ float bias[2][S::TILE_M];
+    const uint32_t count = a.header->count, tiles_m = (columns + S::TILE_M - 1) / S::TILE_M, tiles_n = (count + S::TILE_N - 1) / S::TILE_N;
+    uint32_t group = blockIdx.x;
+    TilePlace tile = tile_place(group, tiles_m, tiles_n);
+    if (!tile.there) return;
+    LogitProduct<T, S> p = logits_at<T, S>(a, weight, from + tile.m * S::TILE_M, tile.n * S::TILE_N, lds);
+    p.begin();
+    load_bias<S>(bias[0], a, from + tile.m * S::TILE_M);
+    for (uint32_t turn = 0; ; ++turn) {
+        f32x16 c[S::MT][S::NT];
+        p.run(c, lds);
+        const uint32_t at = tile.m * S::TILE_M + S::wave_m() * (S::MT * 32), part_n = tile.n * S::WN + S::wave_n();
+        const RowFacts<S> facts(a, part_n * (S::NT * 32) + threadIdx.x % 32, BACKWARD);
+        __builtin_amdgcn_sched_barrier(0);
+        group += gridDim.x;
+        const TilePlace next = STAYS<S> ? tile_place(group, tiles_m, tiles_n) : TilePlace{0, 0, false};
+        if (next.there) {
+            p = logits_at<T, S>(a, weight, from + next.m * S::TILE_M, next.n * S::TILE_N, lds);
+            p.begin();
+            load_bias<S>(bias[(turn + 1) % 2], a, from + next.m * S::TILE_M);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        finish(c, at, part_n, bias[turn % 2] + S::wave_m() * (S::MT * 32), facts, count);
+        if (!next.there) return;
+        tile = next;
+    }
 }
 
 template <typename T, class S>
 __global__ __launch_bounds__(S::THREADS) void cross_entropy_forward_kernel(CeArgs a, const T* weight) {
-    __shared__ __attribute__((aligned(1024))) char lds[S::BYTES];
-    __shared__ float bias[S::TILE_M];
-    const uint32_t count = a.header->count;
-    const TilePlace tile = tile_place(blockIdx.x, (a.vocab + S::TILE_M - 1) / S::TILE_M, (count + S::TILE_N - 1) / S::TILE_N);
-    if (!tile.there) return;
-    load_bias<S>(bias, a, tile.m * S::TILE_M);
-    f32x16 c[S::MT][S::NT];
-    logits<T, S>(c, a, weight, tile.m * S::TILE_M, tile.n * S::TILE_N, lds);
-    const uint32_t lane = threadIdx.x % WAVE, part = tile.m * S::WM + S::wave_m();
-    const uint32_t v0 = part * (S::MT * 32), n0 = tile.n * S::TILE_N + S::wave_n() * (S::NT * 32) + lane % 32;
-    const bool biased = a.bias || v0 + S::MT * 32 > a.vocab;
+    logit_tiles<T, S, false>(a, weight, 0, a.vocab, [&](const f32x16 (&c)[S::MT][S::NT], uint32_t v0, uint32_t part_n, const float* bias, const RowFacts<S>& facts, uint32_t count) {
+        const uint32_t lane = threadIdx.x % WAVE, part = v0 / (S::MT * 32);
+        const bool biased = a.bias || v0 + S::MT * 32 > a.vocab;
 #pragma unroll
-    for (int n = 0; n < S::NT; ++n) {
-        const uint32_t row = n0 + n * 32;
-        float s[S::MT * 16];
-        logits_of_row<S>(s, c, n, bias + S::wave_m() * (S::MT * 32), biased);
-        float top = -__builtin_inff();
+        for (int n = 0; n < S::NT; ++n) {
+            const uint32_t row = part_n * (S::NT * 32) + n * 32 + lane % 32;
+            float s[S::MT * 16];
+            logits_of_row<S>(s, c, n, bias, biased);
+            float top = -__builtin_inff();
 #pragma unroll
-        for (int i = 0; i < S::MT * 16; ++i) top = fmaxf(top, s[i]);
-        top = max_halves(top);
-        const float base = top == -__builtin_inff() ? 0.0f : -top * LOG2E;
-        float sum = 0.0f;
+            for (int i = 0; i < S::MT * 16; ++i) top = fmaxf(top, s[i]);
+            top = max_halves(top);
+            const float base = top == -__builtin_inff() ? 0.0f : -top * LOG2E;
+            float sum = 0.0f;
 #pragma unroll
-        for (int i = 0; i < S::MT * 16; ++i) sum += __builtin_amdgcn_exp2f(fmaf(s[i], LOG2E, base));
-        sum = sum_halves(sum);
-        if (lane < 32 && row < count)
-            *reinterpret_cast<float2*>(a.stats + ((uint64_t)part * a.rows_pad + row) * 2) = make_float2(top, sum);
-        const uint32_t mine = (uint32_t)a.label_of[row] - v0 - lane / 32 * 16;          // far above a wave's part where it is none of its
-        if (__ballot(mine < S::MT * 32u)) {
+            for (int i = 0; i < S::MT * 16; ++i) sum += __builtin_amdgcn_exp2f(fmaf(s[i], LOG2E, base));
+            sum = sum_halves(sum);
+            if (lane < 32 && row < count)
+                *reinterpret_cast<float2*>(a.stats + ((uint64_t)part * a.rows_pad + row) * 2) = make_float2(top, sum);
+            const uint32_t mine = facts.label[n] - v0 - lane / 32 * 16;      // far above a wave's part where it is none of its
+            if (__ballot(mine < S::MT * 32u)) {
 #pragma unroll
-            for (int m = 0; m < S::MT; ++m)
+                for (int m = 0; m < S::MT; ++m)
 #pragma unroll
-                for (int r = 0; r < 16; ++r)
-                    if (mine == m * 32u + r) a.said[row] = s[m * 16 + r];
+                    for (int r = 0; r < 16; ++r)
+                        if (mine == m * 32u + r) a.said[row] = s[m * 16 + r];
+            }
         }
-    }
+    });
 }
 
 // Sixteen rows a workgroup, and 64 threads a row, each every 64th part.
@@ -325,58 +373,51 @@ __device__ __forceinline__ void sums_over_lanes(float (&v)[N]) {
 // d of a piece of the vocabulary that begins at `from`.
 template <typename T, class S>
 __global__ __launch_bounds__(S::THREADS) void cross_entropy_gradient_kernel(CeArgs a, const T* weight, uint32_t from, uint32_t columns) {
-    __shared__ __attribute__((aligned(1024))) char lds[S::BYTES];
-    __shared__ float bias[S::TILE_M];
-    const uint32_t count = a.header->count;
-    const TilePlace tile = tile_place(blockIdx.x, (columns + S::TILE_M - 1) / S::TILE_M, (count + S::TILE_N - 1) / S::TILE_N);
-    if (!tile.there) return;
-    load_bias<S>(bias, a, from + tile.m * S::TILE_M);
-    f32x16 c[S::MT][S::NT];
-    logits<T, S>(c, a, weight, from + tile.m * S::TILE_M, tile.n * S::TILE_N, lds);
-    const uint32_t lane = threadIdx.x % WAVE, at = tile.m * S::TILE_M + S::wave_m() * (S::MT * 32), v0 = from + at;
-    const uint32_t part = tile.n * S::WN + S::wave_n(), n0 = part * (S::NT * 32) + lane % 32;
-    const bool biased = a.bias || v0 + S::MT * 32 > a.vocab;
     const float raise = RAISED<T> ? a.header->raise : 1.0f;
-    float sums[S::MT * 16];
+    logit_tiles<T, S, true>(a, weight, from, columns, [&](const f32x16 (&c)[S::MT][S::NT], uint32_t at, uint32_t part_n, const float* bias, const RowFacts<S>& facts, uint32_t count) {
+        const uint32_t lane = threadIdx.x % WAVE, v0 = from + at;
+        const bool biased = a.bias || v0 + S::MT * 32 > a.vocab;
+        float sums[S::MT * 16];
 #pragma unroll
-    for (int i = 0; i < S::MT * 16; ++i) sums[i] = 0.0f;
+        for (int i = 0; i < S::MT * 16; ++i) sums[i] = 0.0f;
 #pragma unroll
-    for (int n = 0; n < S::NT; ++n) {
-        const uint32_t row = n0 + n * 32;
-        const bool there = row < count;
-        const float g = a.g_of[row], base = -a.lse_of[row] * LOG2E;
-        const uint32_t mine = (uint32_t)a.label_of[row] - v0 - lane / 32 * 16;
-float s[S::MT * 16];
-        logits_of_row<S>(s, c, n, bias + S::wave_m() * (S::MT * 32), biased);
+        for (int n = 0; n < S::NT; ++n) {
+            const uint32_t row = part_n * (S::NT * 32) + n * 32 + lane % 32;
+            const bool there = row < count;
+            const float g = facts.g[n], base = -facts.lse[n] * LOG2E;
+            const uint32_t mine = facts.label[n] - v0 - lane / 32 * 16;
+            float s[S::MT * 16];
+            logits_of_row<S>(s, c, n, bias, biased);
 #pragma unroll
-        for (int i = 0; i < S::MT * 16; ++i) s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], LOG2E, base));
-        if (__ballot(mine < S::MT * 32u)) {
+            for (int i = 0; i < S::MT * 16; ++i) s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], LOG2E, base));
+            if (__ballot(mine < S::MT * 32u)) {
 #pragma unroll
-            for (int m = 0; m < S::MT; ++m)
+                for (int m = 0; m < S::MT; ++m)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) s[m * 16 + r] -= mine == m * 32u + r ? 1.0f : 0.0f;
-        }
-        T* to = (T*)a.d + (uint64_t)row * a.piece + at + lane / 32 * 16;
-#pragma unroll
-        for (int m = 0; m < S::MT; ++m) {
-            f32x8 low, high;
-#pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const float d = there ? s[m * 16 + r] * g : 0.0f;       // rows behind the last one: zeros, whatever the bias is
-                sums[m * 16 + r] += d;
-                (r < 8 ? low : high)[r % 8] = RAISED<T> ? d * raise : d;
+                    for (int r = 0; r < 16; ++r) s[m * 16 + r] -= mine == m * 32u + r ? 1.0f : 0.0f;
             }
-            store_eight(to + m * 32, low);
-            store_eight(to + m * 32 + 8, high);
-        }
-    }
-    if (!a.dbias_sums) return;
-    sums_over_lanes(sums);
-    constexpr int EACH = S::MT * 16 / 32;
-    const uint32_t first = lane % 32 * EACH;
-    float* to = a.dbias_sums + (uint64_t)part * a.vocab_pad + v0 + first / 16 * 32 + lane / 32 * 16 + first % 16;
+            T* to = (T*)a.d + (uint64_t)row * a.piece + at + lane / 32 * 16;
 #pragma unroll
-    for (int i = 0; i < EACH; ++i) to[i] = sums[i];
+            for (int m = 0; m < S::MT; ++m) {
+                f32x8 low, high;
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const float d = there ? s[m * 16 + r] * g : 0.0f;        // rows behind the last one: zeros, whatever the bias is
+                    sums[m * 16 + r] += d;
+                    (r < 8 ? low : high)[r % 8] = RAISED<T> ? d * raise : d;
+                }
+                store_eight(to + m * 32, low);
+                store_eight(to + m * 32 + 8, high);
+            }
+        }
+        if (!a.dbias_sums) return;
+        sums_over_lanes(sums);
+        constexpr int EACH = S::MT * 16 / 32;
+        const uint32_t first = lane % 32 * EACH;
+        float* to = a.dbias_sums + (uint64_t)part_n * a.vocab_pad + v0 + first / 16 * 32 + lane / 32 * 16 + first % 16;
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) to[i] = sums[i];
+    });
 }
 
 // ------------------------------------------------------------------ gradients of h, W and the bias
@@ -407,7 +448,9 @@ __global__ __launch_bounds__(S::THREADS) void cross_entropy_dh_kernel(CeArgs a, 
     const T* d = (const T*)a.d;
     KMajor<T, S::TILE_N, S::WAVES, false> y(d + (uint64_t)row * a.piece + k0, d + (uint64_t)a.rows_pad * a.piece, a.piece * 2);
     f32x16 c[S::MT][S::NT];
-    product<T, S>(c, x, y, lds, k1 - k0);
+    Product<T, S, decltype(x), decltype(y)> p(x, y, k1 - k0, lds);
+    p.begin();
+    p.run(c, lds);
     const uint32_t lane = threadIdx.x % WAVE, m0 = col + S::wave_m() * (S::MT * 32) + lane / 32 * 16, n0 = row + S::wave_n() * (S::NT * 32) + lane % 32;
     const bool first = from == 0;
 #pragma unroll
@@ -460,7 +503,9 @@ __global__ __launch_bounds__(S::THREADS) void cross_entropy_dweight_kernel(CeArg
     Transposed<T, S::TILE_M, S::WAVES, true> x(h + col, h + (uint64_t)a.rows_pad * a.width_pad, a.width_pad * 2, a.width_pad - min(a.width_pad, col));
     Transposed<T, S::TILE_N, S::WAVES, false> y(d + v, d + (uint64_t)a.rows_pad * a.piece, (uint64_t)a.piece * 2, a.piece - v);
     f32x16 c[S::MT][S::NT];
-    product<T, S>(c, x, y, lds, (count + PRODUCT_K - 1) / PRODUCT_K * PRODUCT_K);
+    Product<T, S, decltype(x), decltype(y)> p(x, y, (count + PRODUCT_K - 1) / PRODUCT_K * PRODUCT_K, lds);
+    p.begin();
+    p.run(c, lds);
     const float lower = RAISED<T> ? a.header->lower : 1.0f;
     const uint32_t lane = threadIdx.x % WAVE, m0 = col + S::wave_m() * (S::MT * 32) + lane / 32 * 16, n0 = v + S::wave_n() * (S::NT * 32) + lane % 32;
 #pragma unroll
@@ -521,8 +566,12 @@ static bool ce_plan(uint64_t rows, uint32_t width, uint32_t vocab, CePlan& p) {
     p.small_logits = ce_small(vocab, some);
     p.small_dh = some <= 128;
     p.small_dweight = ce_small(p.width_pad, p.piece);
-    p.logit_groups = tile_groups(tiles(vocab, p.small_logits) * tiles(some, p.small_logits));
-    p.piece_groups = tile_groups(tiles(p.piece, p.small_logits) * tiles(some, p.small_logits));
+    // workgroups of large tiles of logits stay on their CU; those of a die keep its tiles
+    const uint64_t stay = ce_up(device_cus(), DIES), logit_tiles = tile_groups(tiles(vocab, p.small_logits) * tiles(some, p.small_logits)),
+                   piece_tiles = tile_groups(tiles(p.piece, p.small_logits) * tiles(some, p.small_logits));
+    if (logit_tiles > UINT32_MAX / 2) return false;
+    p.logit_groups = p.small_logits || logit_tiles < stay ? logit_tiles : stay;
+    p.piece_groups = p.small_logits || piece_tiles < stay ? piece_tiles : stay;
     const uint64_t dh_tiles = tiles(p.width_pad, p.small_dh) * tiles(some, p.small_dh);
     p.dh_groups = tile_groups(dh_tiles > CE_SPLIT_TILES ? dh_tiles : CE_SPLIT_TILES);
     p.dweight_groups = tile_groups(tiles(p.width_pad, p.small_dweight) * tiles(p.piece, p.small_dweight));

@@ -112,33 +112,31 @@ __device__ __forceinline__ void handed_over() {
     __syncthreads();
 }
 
-// The sums over `k`.  Every wave of the workgroup calls it; the tiles in LDS are free again after a barrier.
+// The sums over `k`: begin() sends out the first fetches, run() does the rest.  Every wave of the workgroup calls both; the tiles in LDS have to be
+// free at begin() and are free again after run(), so the next tile's begin() can stand before this one's sums are stored.
 //
 // A piece is four steps of sixteen k.  While a step's products run, the wave reads the next step's operands from LDS, a few between every
 // NT products, and the barrier that hands over the next piece stands before the last step, whose operands are in registers by then: so the
 // products of that step cover the first reads of the next piece and the first fetches of the one after it.  Fetches go out one by one
-// between products, too: issued together they hold the wave up for a thousand cycles (8192 x 128000 x 4096: 8.2 ms).
+// between products, half of a piece's in that step and half in the next one (8192 x 128000 x 4096: 6.5 ms; all together, which holds the wave
+// up for a thousand cycles, 7.2; all in the last step 6.7, over three steps 6.6).  Two waves a SIMD, 128 x 64 each: one of 128 x 128
+// reads a quarter less from LDS and takes 6.7.
 template <typename T, class S, class A, class B>
-__device__ __forceinline__ void product(f32x16 (&c)[S::MT][S::NT], A& a, B& b, char* lds, uint32_t k) {
-#pragma unroll
-    for (int m = 0; m < S::MT; ++m)
-#pragma unroll
-        for (int n = 0; n < S::NT; ++n) c[m][n] = 0.0f;
-    if (k == 0) return;
-    constexpr uint32_t BUFFER = A::BYTES + B::BYTES;
-    constexpr int LOADS = A::LOADS + B::LOADS, STEPS = PRODUCT_K / 16, LEFT = (S::STAGES - 2) * LOADS;
-    constexpr int EARLY = LOADS / 2, LATE = LOADS - EARLY;           // fetches in the last step, in the first
-    constexpr int EACH = ((EARLY > LATE ? EARLY : LATE) + S::MT - 1) / S::MT;
-    const uint32_t at = lds_address(lds);
-    const int m0 = S::wave_m() * S::MT, n0 = S::wave_n() * S::NT;
-    frag<T> x[2][S::MT], y[2][S::NT];
+struct Product {
+    static constexpr uint32_t BUFFER = A::BYTES + B::BYTES;
+    static constexpr int LOADS = A::LOADS + B::LOADS, LEFT = (S::STAGES - 2) * LOADS;
+    static_assert(S::NT <= S::MT, "a group reads one operand of each side");
+    A a;
+    B b;
+    uint32_t k, at;
     i32x4 buffer_a, buffer_b;
-    uint32_t ahead = 0, there = 0;                                   // k before the piece that is fetched, and in and behind it
-    const auto fetch = [&](int i, uint32_t to) {
+    uint32_t ahead, there;                                           // k before the piece that is fetched, and in and behind it
+
+    __device__ __forceinline__ void fetch(int i, uint32_t to) const {
         if (i < A::LOADS) a.fetch(i, at + to, buffer_a, there);
         else if (i < LOADS) b.fetch(i - A::LOADS, at + to + A::BYTES, buffer_b, there);
-    };
-    const auto next_piece = [&] {
+    }
+    __device__ __forceinline__ void next_piece() {
         there = ahead < k ? k - ahead : 0;
         buffer_a = a.from.buffer();
         buffer_b = b.from.buffer();
@@ -146,55 +144,72 @@ __device__ __forceinline__ void product(f32x16 (&c)[S::MT][S::NT], A& a, B& b, c
         a.advance();
         b.advance();
         ahead += PRODUCT_K;
-    };
-    // the operands of a step that a group of products covers
-    const auto read = [&](int set, int m, const char* piece, int s) {
-        x[set][m] = a.operand(piece, m0 + m, s);
-        if (m < S::NT) y[set][m] = b.operand(piece + A::BYTES, n0 + m, s);
-    };
-    static_assert(S::NT <= S::MT, "a group reads one operand of each side");
-#pragma unroll
-    for (int p = 0; p < S::STAGES - 1; ++p) {
-        next_piece();
-#pragma unroll
-        for (int i = 0; i < LOADS; ++i) fetch(i, p * BUFFER);
     }
-    handed_over<LEFT>();
-    next_piece();
-    uint32_t now = 0, filled = (S::STAGES - 1) * BUFFER;             // the buffer that is worked on, and the one that is filled
+    __device__ __forceinline__ Product(const A& a_, const B& b_, uint32_t k_, const char* lds) : a(a_), b(b_), k(k_), at(lds_address(lds)) {}
+
+    __device__ __forceinline__ void begin() {
+        ahead = 0;
+        if (k == 0) return;
 #pragma unroll
-    for (int i = 0; i < EARLY; ++i) fetch(i, filled);
+        for (int p = 0; p < S::STAGES - 1; ++p) {
+            next_piece();
 #pragma unroll
-    for (int m = 0; m < S::MT; ++m) read(0, m, lds, 0);
-    for (uint32_t done = PRODUCT_K; ; done += PRODUCT_K) {           // k up to the end of this piece
-        const uint32_t next = now + BUFFER < S::BYTES ? now + BUFFER : 0;
-#pragma unroll
-        for (int s = 0; s < STEPS; ++s) {
-            if (s == STEPS - 1) {
-                handed_over<LEFT>();
-                next_piece();
-                filled = now;
-            }
-            const char* piece = lds + (s == STEPS - 1 ? next : now);
-#pragma unroll
-            for (int m = 0; m < S::MT; ++m) {
-                __builtin_amdgcn_sched_barrier(0);
-                read((s + 1) % 2, m, piece, (s + 1) % STEPS);
-#pragma unroll
-                for (int i = 0; i < EACH; ++i) {
-                    if (s == 0 && m * EACH + i < LATE) fetch(EARLY + m * EACH + i, filled);
-                    if (s == STEPS - 1 && m * EACH + i < EARLY) fetch(m * EACH + i, filled);
-                }
-#pragma unroll
-                for (int n = 0; n < S::NT; ++n) c[m][n] = mfma(x[s % 2][m], y[s % 2][n], c[m][n]);
-            }
+            for (int i = 0; i < LOADS; ++i) fetch(i, p * BUFFER);
         }
-        now = next;
-        if (done >= k) break;
     }
-    __builtin_amdgcn_sched_barrier(0);
-    handed_over<0>();                                                // nothing is on its way into LDS any more
-}
+
+    __device__ __forceinline__ void run(f32x16 (&c)[S::MT][S::NT], const char* lds) {
+#pragma unroll
+        for (int m = 0; m < S::MT; ++m)
+#pragma unroll
+            for (int n = 0; n < S::NT; ++n) c[m][n] = 0.0f;
+        if (k == 0) return;
+        constexpr int STEPS = PRODUCT_K / 16, EARLY = LOADS / 2, LATE = LOADS - EARLY;       // fetches in the last step, in the first
+        constexpr int EACH = ((EARLY > LATE ? EARLY : LATE) + S::MT - 1) / S::MT;
+        const int m0 = S::wave_m() * S::MT, n0 = S::wave_n() * S::NT;
+        frag<T> x[2][S::MT], y[2][S::NT];
+        // the operands of a step that a group of products covers
+        const auto read = [&](int set, int m, const char* piece, int s) {
+            x[set][m] = a.operand(piece, m0 + m, s);
+            if (m < S::NT) y[set][m] = b.operand(piece + A::BYTES, n0 + m, s);
+        };
+        handed_over<LEFT>();
+        next_piece();
+        uint32_t now = 0, filled = (S::STAGES - 1) * BUFFER;         // the buffer that is worked on, and the one that is filled
+#pragma unroll
+        for (int i = 0; i < EARLY; ++i) fetch(i, filled);
+#pragma unroll
+        for (int m = 0; m < S::MT; ++m) read(0, m, lds, 0);
+        for (uint32_t done = PRODUCT_K; ; done += PRODUCT_K) {       // k up to the end of this piece
+            const uint32_t next = now + BUFFER < S::BYTES ? now + BUFFER : 0;
+#pragma unroll
+            for (int s = 0; s < STEPS; ++s) {
+                if (s == STEPS - 1) {
+                    handed_over<LEFT>();
+                    next_piece();
+                    filled = now;
+                }
+                const char* piece = lds + (s == STEPS - 1 ? next : now);
+#pragma unroll
+                for (int m = 0; m < S::MT; ++m) {
+                    __builtin_amdgcn_sched_barrier(0);
+                    read((s + 1) % 2, m, piece, (s + 1) % STEPS);
+#pragma unroll
+                    for (int i = 0; i < EACH; ++i) {
+                        if (s == 0 && m * EACH + i < LATE) fetch(EARLY + m * EACH + i, filled);
+                        if (s == STEPS - 1 && m * EACH + i < EARLY) fetch(m * EACH + i, filled);
+                    }
+#pragma unroll
+                    for (int n = 0; n < S::NT; ++n) c[m][n] = mfma(x[s % 2][m], y[s % 2][n], c[m][n]);
+                }
+            }
+            now = next;
+            if (done >= k) break;
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        handed_over<0>();                                            // nothing is on its way into LDS any more
+    }
+};
 
 }  // namespace okt
 
