@@ -687,13 +687,13 @@ static int ce_backward(const CeArgs& a, const CePlan& p, const void* weight, con
         hipLaunchKernelGGL((cross_entropy_gradient_kernel<T, S>), dim3((unsigned)p.piece_groups), dim3(S::THREADS), 0, s, a, (const T*)weight, first, columns);
         timing_after(s);
         if (const int status = launch_status()) return status;
-        if (g.dh)
+        if (g.dh && a.rows)
             if (const int status = p.small_dh ? ce_dh<T, Small>(a, p, weight, first, columns, s) : ce_dh<T, Large>(a, p, weight, first, columns, s)) return status;
         if (g.dweight)
             if (const int status = p.small_dweight ? ce_dweight<T, Small>(a, p, g.dweight, wide, first, columns, s) : ce_dweight<T, Large>(a, p, g.dweight, wide, first, columns, s))
                 return status;
     }
-    if (g.dh) {
+    if (g.dh && a.rows) {
         const dim3 rows((a.rows + CE_THREADS / WAVE - 1) / (CE_THREADS / WAVE));
         if (p.small_dh) hipLaunchKernelGGL((cross_entropy_dh_join_kernel<T, Small>), rows, dim3(CE_THREADS), 0, s, a, (T*)g.dh);
         else hipLaunchKernelGGL((cross_entropy_dh_join_kernel<T, Large>), rows, dim3(CE_THREADS), 0, s, a, (T*)g.dh);

@@ -9,6 +9,7 @@
 // all heads find them: the angle in fp64 turns of which the whole ones are dropped, because a position of 10^5 times a frequency
 // has lost 2^-7 of a turn in fp32.  Then lanes take heads: eight elements a lane as two fours, which are the two halves of four pairs (or
 // four adjacent pairs), so a pair never leaves its lane and a norm's sums cross 8, 16 or 32 lanes inside the vector unit.
+#include <algorithm>
 #include <math.h>
 
 #include "okt_attention_layout.h"
@@ -483,26 +484,37 @@ static bool shares_places(const RotArgs& a, const HeadStrides& s, uint32_t heads
     return (batch > 1 && s.batch < a.dim) || (a.length.by > 1 && s.row < a.dim) || (heads > 1 && s.head < a.dim);
 }
 
-// Whether an output and another tensor share an element: exactly where their strides are alike, as parts of one
-// projection's are, else by their first heads.  One in the very place of the other is seen by the caller.
-static bool clash(const Placed& x, const Placed& y, uint32_t dim, size_t e) {
-    if (!x.p || !y.p || !x.heads || !y.heads) return false;
-    if (x.s.batch == y.s.batch && x.s.row == y.s.row && (x.s.head == y.s.head || x.heads == 1 || y.heads == 1)) {
-        const uint64_t step = (x.heads == 1 ? y.s.head : x.s.head) * e, bytes = dim * e;
-        const bool before = (uintptr_t)x.p <= (uintptr_t)y.p;
-        const Placed &lo = before ? x : y, &hi = before ? y : x;
-        const uint64_t apart = (uint64_t)((uintptr_t)hi.p - (uintptr_t)lo.p);
-        for (uint64_t h = step ? apart / step : 0, n = 0; n < 2; ++h, ++n) {        // heads of the lower one around the higher one's first
-            if (h >= lo.heads) break;
-            const uint64_t from = h * step;
-            if (from < apart + bytes && apart < from + bytes) return true;
-        }
-        return false;
-    }
-    return overlap(x.p, dim * e, y.p, dim * e);
+// Whether `apart` elements are some steps along the axes, each axis' within its size, and less than a head's length besides; the axes by
+// falling stride, so that of each only the two nearest numbers of steps come into question.
+struct Axis { int64_t stride, least, most; };
+static bool reachable(int64_t apart, const Axis* axes, int n, int64_t dim) {
+    if (n == 0) return apart > -dim && apart < dim;
+    if (axes->stride == 0) return reachable(apart, axes + 1, n - 1, dim);
+    int64_t q = apart / axes->stride;
+    if (apart % axes->stride < 0) --q;
+    for (int64_t k = q; k <= q + 1; ++k)
+        if (k <= axes->most && k >= axes->least && reachable(apart - k * axes->stride, axes + 1, n - 1, dim)) return true;
+    return false;
 }
-static bool same(const Placed& x, const Placed& y) {
-    return x.p == y.p && x.s.batch == y.s.batch && x.s.row == y.s.row && (x.s.head == y.s.head || x.heads == 1) && x.heads == y.heads;
+
+// Whether an output and another tensor share an element, one in the very place of the other aside, which the caller sees.  Where
+// their strides are alike, as parts of one projection's are, by their heads; else by their first and last elements.
+static bool clash(const RotArgs& a, const Placed& x, const Placed& y, size_t e) {
+    if (!x.p || !y.p || !x.heads || !y.heads) return false;
+    const uint64_t batch = a.tokens / a.length.by, length = a.length.by;
+    const auto extent = [&](const Placed& t) { return ((batch - 1) * t.s.batch + (length - 1) * t.s.row + (uint64_t)(t.heads - 1) * t.s.head + a.dim) * e; };
+    if (!overlap(x.p, extent(x), y.p, extent(y))) return false;
+    if ((batch > 1 && x.s.batch != y.s.batch) || (length > 1 && x.s.row != y.s.row) || (x.heads > 1 && y.heads > 1 && x.s.head != y.s.head)) return true;
+    const int64_t bytes = (int64_t)((uintptr_t)y.p - (uintptr_t)x.p);
+    const int64_t b = (int64_t)batch - 1, l = (int64_t)length - 1;
+    Axis axes[3] = {{(int64_t)(batch > 1 ? x.s.batch : 0), -b, b}, {(int64_t)(length > 1 ? x.s.row : 0), -l, l},
+                    {(int64_t)(x.heads > 1 ? x.s.head : y.heads > 1 ? y.s.head : 0), 1 - (int64_t)y.heads, (int64_t)x.heads - 1}};
+    std::sort(axes, axes + 3, [](const Axis& p, const Axis& q) { return p.stride > q.stride; });
+    return reachable(bytes / (int64_t)e, axes, 3, a.dim);
+}
+static bool same(const RotArgs& a, const Placed& x, const Placed& y) {
+    return x.p == y.p && (x.s.batch == y.s.batch || a.tokens == a.length.by) && (x.s.row == y.s.row || a.length.by == 1) &&
+           (x.s.head == y.s.head || x.heads == 1) && x.heads == y.heads;
 }
 
 template <typename T, int LANES>
@@ -558,10 +570,10 @@ int okt_norm_rotary_forward(const okt_norm_rotary* op, const void* d_q, const vo
         if (!a.t[n].heads) continue;
         if (!p.x[n] || !p.out[n] || !aligned(p.x[n], e) || !aligned(p.out[n], e) || shares_places(a, a.t[n].out, a.t[n].heads)) return OKT_ERR_INVALID_ARG;
     }
-    if (clash(out[0], out[1], a.dim, e)) return OKT_ERR_INVALID_ARG;
+    if (clash(a, out[0], out[1], e)) return OKT_ERR_INVALID_ARG;
     for (int n = 0; n < 2; ++n)
         for (int m = 0; m < 2; ++m)
-            if (!(n == m && same(out[n], in[m])) && clash(out[n], in[m], a.dim, e)) return OKT_ERR_INVALID_ARG;
+            if (!(n == m && same(a, out[n], in[m])) && clash(a, out[n], in[m], e)) return OKT_ERR_INVALID_ARG;
     return launch_rot_type(op->dtype, a, p, false, (hipStream_t)stream);
 }
 
@@ -586,11 +598,11 @@ int okt_norm_rotary_backward(const okt_norm_rotary* op, const void* d_q, const v
     }
     const bool sums = g.to[0] || g.to[1];
     if (a.tokens) {
-        if (clash(out[0], out[1], a.dim, e)) return OKT_ERR_INVALID_ARG;
+        if (clash(a, out[0], out[1], e)) return OKT_ERR_INVALID_ARG;
         for (int n = 0; n < 2; ++n)
             for (int m = 0; m < 2; ++m)
-                if ((!(n == m && same(out[n], in[m])) && clash(out[n], in[m], a.dim, e)) ||
-                    (!(n == m && same(out[n], d[m])) && clash(out[n], d[m], a.dim, e))) return OKT_ERR_INVALID_ARG;
+                if ((!(n == m && same(a, out[n], in[m])) && clash(a, out[n], in[m], e)) ||
+                    (!(n == m && same(a, out[n], d[m])) && clash(a, out[n], d[m], e))) return OKT_ERR_INVALID_ARG;
         if (sums && (!d_ws || !aligned(d_ws, 256) || ws_bytes < (size_t)a.groups * 2 * a.dim * 4)) return OKT_ERR_WORKSPACE;
         if (sums) a.partial = (float*)d_ws;
         if (const int status = launch_rot_type(op->dtype, a, p, true, (hipStream_t)stream)) return status;
