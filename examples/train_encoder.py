@@ -2,14 +2,16 @@
 
     python examples/train_encoder.py [--steps 200]
 
-Everything between the matrix products of a layer is one of this library's operators:
+Everything between the matrix products of a layer is one of this library's operators: norms of
+the query and key heads and their rotation by position (okt_norm_rotary_forward / _backward),
 attention over a padded batch with dropout (okt_attention_forward / _backward), and
 dropout, the sum with the residual stream and the norm after it in one call
-(okt_residual_norm_forward / _backward), and the dropout of the embeddings (okt_dropout).
-The gradients of all parameters land in one flat fp32 vector: the norms' are written there by
-the operator, the products' are added there by autograd.  Each worker accumulates the vector into
+(okt_residual_norm_forward / _backward), and the dropout of the embeddings (okt_dropout).  So is the loss,
+from the last layer's vectors and the output matrix (okt_cross_entropy_forward / _backward).
+The gradients of all parameters land in one flat fp32 vector: the norms' and the output matrix's are
+written there by the operators, the products' are added there by autograd.  Each worker accumulates the vector into
 its residual and selects its top-k entries (okt_accumulate_topk_select), and the reduced entries
-(okt_sparse_reduce) update the weights.
+(okt_sparse_reduce) are the gradient of an AdamW step over all tensors (okt_adamw_step).
 
 The task is synthetic: a third of a sequence's tokens are one and the same, and every position has
 to name it, which takes attention.
@@ -28,7 +30,7 @@ import paper_2201_07598_amd as okt  # noqa: E402
 DEV = "cuda:0"
 WORKERS, BATCH, LENGTH, VOCAB = 2, 16, 96, 32
 LAYERS, WIDTH, HEADS, INNER, DROP = 2, 128, 2, 256, 0.05
-DENSITY, RATE = 0.05, 0.3
+DENSITY, RATE = 0.05, 0.003
 
 
 class Dropout(torch.autograd.Function):
@@ -46,6 +48,57 @@ class Dropout(torch.autograd.Function):
         dx = torch.empty_like(dy)
         okt.okt_dropout(dy, dx, p, seed, site)           # the same mask, drawn again
         return dx, None, None, None
+
+
+class HeadNorms(torch.autograd.Function):
+    """Norms of the query and key heads and their rotation, in the projection's [batch, length, 3 heads, dim]; the values are handed
+    on.  The weights' gradients are written where their `grad` lies."""
+
+    @staticmethod
+    def forward(ctx, qkv, q_weight, k_weight, inv_freq):
+        heads = qkv.shape[2] // 3
+        out = torch.empty_like(qkv)
+        out[:, :, 2 * heads:] = qkv[:, :, 2 * heads:]
+        okt.okt_norm_rotary_forward(*qkv.split(heads, 2)[:2], *out.split(heads, 2)[:2], inv_freq, q_weight=q_weight, k_weight=k_weight)
+        ctx.save_for_backward(qkv, q_weight, k_weight, inv_freq)
+        ctx.places = (q_weight.grad, k_weight.grad)
+        return out
+
+    @staticmethod
+    def backward(ctx, d):
+        qkv, q_weight, k_weight, inv_freq = ctx.saved_tensors
+        batch, length, heads, dim = qkv.shape
+        heads //= 3
+        d = d.contiguous()
+        ws = torch.empty(okt.okt_norm_rotary_workspace_bytes(batch, length, heads, heads, dim), dtype=torch.uint8, device=d.device)
+        dqkv = d.clone()
+        okt.okt_norm_rotary_backward(*qkv.split(heads, 2)[:2], *d.split(heads, 2)[:2], *dqkv.split(heads, 2)[:2], inv_freq, ws,
+                                     dq_weight_out=ctx.places[0], dk_weight_out=ctx.places[1], q_weight=q_weight, k_weight=k_weight)
+        return dqkv, None, None, None
+
+
+class Loss(torch.autograd.Function):
+    """The mean of softmax cross entropies of [rows, width] against labels, rows without one left out.  `weight.grad` is
+    written by the call itself."""
+
+    @staticmethod
+    def forward(ctx, h, weight, labels):
+        w = weight.to(h.dtype)
+        loss, lse = (torch.empty(h.shape[0], device=h.device) for _ in range(2))
+        ws = torch.empty(okt.okt_cross_entropy_workspace_bytes(*h.shape, weight.shape[0]), dtype=torch.uint8, device=h.device)
+        okt.okt_cross_entropy_forward(h, w, labels, loss, lse, ws)
+        share = 1.0 / (labels >= 0).sum()
+        ctx.save_for_backward(h, w, labels, lse, share)
+        ctx.rest = (weight.grad, ws)
+        return loss.sum() * share
+
+    @staticmethod
+    def backward(ctx, d):
+        h, w, labels, lse, share = ctx.saved_tensors
+        place, ws = ctx.rest
+        dh = torch.empty_like(h)
+        okt.okt_cross_entropy_backward(h, w, labels, lse, (d * share).view(1), dh, place, ws)
+        return dh, None, None
 
 
 class Attention(torch.autograd.Function):
@@ -108,11 +161,13 @@ class Encoder:
             shapes |= {f"{n}.qkv": (3 * WIDTH, WIDTH), f"{n}.proj": (WIDTH, WIDTH), f"{n}.up": (INNER, WIDTH),
                        f"{n}.down": (WIDTH, INNER)}
             shapes |= {f"{n}.{norm}_{part}": (WIDTH,) for norm in ("mid", "end") for part in ("weight", "bias")}
+            shapes |= {f"{n}.{side}_weight": (WIDTH // HEADS,) for side in ("q", "k")}
         sizes = {k: -(-torch.Size(s).numel() // 4) * 4 for k, s in shapes.items()}       # 16-byte steps
         self.flat = torch.zeros(sum(sizes.values()), device=DEV)
         self.grad = torch.zeros_like(self.flat)
         self.par, at = {}, 0
         gen = torch.Generator().manual_seed(1)
+        self.inv_freq = 100.0 ** (-torch.arange(0, WIDTH // HEADS, 2, device=DEV) / (WIDTH // HEADS))
         for name, shape in shapes.items():
             n = torch.Size(shape).numel()
             view = self.flat[at:at + n].view(shape)
@@ -135,14 +190,14 @@ class Encoder:
         x = Dropout.apply(x, seed, 100, DROP)
         for n in range(LAYERS):
             qkv = linear(x, f"{n}.qkv").view(*tokens.shape, 3 * HEADS, WIDTH // HEADS)
+            qkv = HeadNorms.apply(qkv, par[f"{n}.q_weight"], par[f"{n}.k_weight"], self.inv_freq)
             o = Attention.apply(qkv, lens, seed, 4 * n, DROP).reshape(rows, WIDTH)
             x = SumNorm.apply(linear(o, f"{n}.proj"), x, par[f"{n}.mid_weight"], par[f"{n}.mid_bias"], seed, 4 * n + 1, DROP)
             inner = torch.relu(linear(x, f"{n}.up"))
             x = SumNorm.apply(linear(inner, f"{n}.down"), x, par[f"{n}.end_weight"], par[f"{n}.end_bias"], seed, 4 * n + 2, DROP)
-        scores = linear(x, "out").float().view(*tokens.shape, VOCAB)
-        counts = torch.arange(tokens.shape[1], device=DEV)[None] < lens[:, None]
-        each = torch.nn.functional.cross_entropy(scores.transpose(1, 2), names[:, None].expand_as(tokens), reduction="none")
-        return (each * counts).sum() / counts.sum()
+        there = torch.arange(tokens.shape[1], device=DEV)[None] < lens[:, None]
+        labels = torch.where(there, names[:, None], -100)
+        return Loss.apply(x, par["out"], labels.reshape(rows))
 
 
 class Worker:
@@ -169,7 +224,7 @@ class Worker:
         model.grad.zero_()
         loss = model.loss(tokens, names, lens, self.seed)
         loss.backward()
-        okt.okt_accumulate_topk_select(model.grad, self.residual, RATE / WORKERS, self.k, self.threshold, self.count,
+        okt.okt_accumulate_topk_select(model.grad, self.residual, 1.0 / WORKERS, self.k, self.threshold, self.count,
                                        self.idx, self.val, self.nnz, self.ws)
         self.seed += 1 << 20                              # another mask for the next step
         return loss.detach()
@@ -183,7 +238,11 @@ def train(steps, report=None):
     capacity = sum(2 * w.k for w in workers)
     red_idx, red_val = torch.zeros(capacity, dtype=torch.int32, device=DEV), torch.zeros(capacity, device=DEV)
     red_nnz = torch.zeros(2, dtype=torch.int64, device=DEV)
-    update = torch.zeros(n, device=DEV)
+    update = torch.zeros(n, device=DEV)                   # the reduced gradient, tensor by tensor where the parameters are
+    parts = [(p, update[p.storage_offset():p.storage_offset() + p.numel()]) for p in model.par.values()]
+    plan = okt.okt_adamw_plan([p.detach() for p, _ in parts], [g for _, g in parts], *([torch.zeros_like(g) for _, g in parts] for _ in range(2)),
+                              weight_decay=[0.01 if p.dim() > 1 else 0.0 for p, _ in parts])
+    count = torch.zeros(1, dtype=torch.int64, device=DEV)
     losses = []
     for step in range(steps):
         losses.append(torch.stack([w.step(model) for w in workers]).mean())
@@ -192,7 +251,8 @@ def train(steps, report=None):
         val = torch.cat([w.val[:c] for w, c in zip(workers, kept)])
         off = torch.tensor([0, *torch.tensor(kept).cumsum(0).tolist()], dtype=torch.int64).to(DEV)
         okt.okt_sparse_reduce(idx, val, off, 0, n, red_idx, red_val, red_nnz, workers[0].ws, dense_out=update)
-        model.flat.detach().sub_(update)
+        count += 1
+        okt.okt_adamw_step(plan, count, lr=RATE)
         if report and (step % report == 0 or step == steps - 1):
             print(f"step {step:4d}  loss {float(losses[-1]):.4f}  entries {sum(kept)} of {n}", flush=True)
     return [float(x) for x in losses]
