@@ -811,7 +811,7 @@ def _rotary_struct(dtype, shape, kv_heads, inv_freq, positions, axis_of_pair, ad
         if len(axis_of_pair) != pairs:
             raise ValueError(f"axis_of_pair needs one axis a pair ({pairs}), got {len(axis_of_pair)}")
         table = bytes(axis_of_pair)
-        axes = max(table, default=0) + 1
+        axes = 1 if table.count(0) == pairs else max(table) + 1
     if positions is not None and positions.dim() == 3:
         axes = max(axes, positions.shape[2])
     elif positions is not None and axes > 1 and positions.dim() == 2:

@@ -83,7 +83,7 @@ def check(c, loss, lse, grads=None):
     d = np.abs(g[rows, None]) * np.abs(p - (np.arange(c.vocab) == y[rows, None]))
     size = np.abs(np.where(np.isfinite(s), s, 0.0))
     e_p = p * (one + e_lse[rows, None] + E * (8 + 3 * size + 4 * np.abs(want_lse[rows, None])))
-    e_d = np.abs(g[rows, None]) * e_p + 2 * E * d
+    e_d = np.abs(g[rows, None]) * (e_p + 2.0 ** -126) + 2 * E * d         # an exponential below 2^-126 may be 0
     e_r = e_d + u * (d + e_d) + tiny                     # as the second products read it
     dh, dw, db = ref.cross_entropy_backward(h, w, y, g, b)
     full = np.zeros(h.shape)
@@ -237,3 +237,11 @@ def test_replayed_and_on_another_stream():
             both(two)
         stream.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(one.out, two.out)), n
+
+
+def test_a_large_bias():
+    """Rows behind the last one see the bias alone, whose exponential need not be finite."""
+    c = Case(rows=130, width=64, vocab=300, bias=True, seed=9)
+    c.bias[5], c.bias[7] = 150.0, 149.0
+    loss, lse = c.forward()
+    check(c, loss, lse, c.backward(lse))
