@@ -744,7 +744,8 @@ int okt_norm_rotary_backward(const okt_norm_rotary* op, const void* d_q, const v
  *   dh_n = sum_v d_nv W_v,  dW_v = sum_n d_nv h_n,  db_v = sum_n d_nv
  * The logits are made again, a piece of the vocabulary at a time.  Products are taken by the matrix units from 16-bit inputs with fp32
  * sums.  For the second products d is rounded to the tensors' type, so dh and dW have the precision of that type, also where dW is fp32 (so that it
- * can lie in the flat vector of the accumulate calls); db is summed in fp32 before that rounding.  In fp16 d is scaled by a power of two from the
+ * can lie in the flat vector of the accumulate calls); with up to 256 labelled rows, where the rounding of single entries would show, d goes in as two
+ * parts of that type.  db is summed in fp32 before any rounding.  In fp16 d is scaled by a power of two from the
  * largest |g|; a d below 2^-39 of that is rounded to 0.  A bias of -infinity takes an entry out of the vocabulary.
  * Tensors are rows of `width` contiguous elements, 16-byte aligned, strides (in elements; 0 stands for width) multiples of 8, at most
  * 2^20; an fp32 dW needs 4-byte alignment and any stride.
@@ -778,7 +779,7 @@ int okt_cross_entropy_forward(const okt_cross_entropy* op, const void* d_h, cons
  *   d_dloss  in   fp32[rows] or fp32[1], see dloss_stride
  *   d_dh_out, d_dweight_out, d_dbias_out  out  overwritten; each may be NULL (not all; the last one has to be without a bias), and
  *            none overlaps another or an input, from its first element to its last
- * Two launches (one up to 2048 rows), up to three a piece of the vocabulary, and two more.
+ * Two launches (one up to 2048 rows), up to three a piece of the vocabulary (a fourth where dW has few tiles and many rows), and two more.
  */
 int okt_cross_entropy_backward(const okt_cross_entropy* op, const void* d_h, const void* d_weight, const int64_t* d_labels,
                                const float* d_lse, const float* d_dloss, void* d_dh_out, void* d_dweight_out, float* d_dbias_out,

@@ -22,14 +22,16 @@ namespace okt {
 
 constexpr uint32_t CE_PAD = 256;                                     // rows, and columns of a piece, are padded to the largest tile
 constexpr uint64_t CE_PIECE_BYTES = 1ull << 30;                    // of d in the workspace
-constexpr uint32_t CE_SPLIT_TILES = 512;                             // of dh and parts of k together, where tiles are fewer
+constexpr uint32_t CE_SPLIT_TILES = 256;                             // of a gradient, with the parts that its sum is dealt to where tiles are fewer
+constexpr uint32_t CE_SPLIT_PIECES = 8;                              // pieces of k that a part has at least: fewer are not worth their sums' way
+constexpr uint32_t CE_FINE_ROWS = 256;                               // up to so many, d goes into the second products in two parts
 constexpr uint32_t CE_MAX = 1u << 22;                                // rows, vocabulary
 constexpr uint32_t CE_MAX_WIDTH = 1u << 15;
 constexpr int CE_THREADS = 256;
 constexpr float LOG2E = 1.44269504088896340736f;
 
 typedef ProductShape<4, 2, 2, 4, 2> Large;                           // 256 x 256, one workgroup of eight waves a CU
-typedef ProductShape<2, 2, 2, 2, 4> Small;                           // 128 x 128, four waves and three pieces on their way
+typedef ProductShape<2, 2, 2, 2, 3> Small;                           // 128 x 128, four waves and two pieces on their way
 
 template <typename T> constexpr bool RAISED = false;
 template <> constexpr bool RAISED<_Float16> = true;
@@ -52,6 +54,8 @@ struct CeArgs {
     float* said;                                                     // forward: s_ny
     float *lse_of, *g_of;                                            // backward, of listed row n
     void* d;                                                         // [rows_pad][piece]
+    void* d_rest;                                                    // [CE_FINE_ROWS][piece]: what d's rounding left off
+    float* dw_sums;                                                  // [parts][columns of whole tiles][width_pad]
     float* dh_sums;                                                  // [parts][rows of whole tiles][width_pad]
     float* dbias_sums;                                               // [parts][vocab_pad]
     uint32_t piece, vocab_pad;
@@ -239,7 +243,7 @@ struct RowFacts {
 
 // Tiles of logits.  Where a workgroup has a CU for itself it stays, and the next tile's first operands are on their way while this one's logits are
 // worked on (2458 rows x 1024 x 30522: 164 -> 157 us; small tiles, of which there are few, gain nothing and lose 1.4 us).  `finish` is called with the tile's sums, its place, its bias and its rows' facts.
-template <class S> constexpr bool STAYS = S::STAGES == 2;
+template <class S> constexpr bool STAYS = S::WAVES == 8;
 
 template <typename T, class S, bool BACKWARD, class F>
 __device__ __forceinline__ void logit_tiles(const CeArgs& a, const T* weight, uint32_t from, uint32_t columns, const F& finish) {
@@ -254,6 +258,7 @@ __device__ __forceinline__ void logit_tiles(const CeArgs& a, const T* weight, ui
     load_bias<S>(bias[0], a, from + tile.m * S::TILE_M);
     for (uint32_t turn = 0; ; ++turn) {
         f32x16 c[S::MT][S::NT];
+        clear<S>(c);
         p.run(c, lds);
         const uint32_t at = tile.m * S::TILE_M + S::wave_m() * (S::MT * 32), part_n = tile.n * S::WN + S::wave_n();
         const RowFacts<S> facts(a, part_n * (S::NT * 32) + threadIdx.x % 32, BACKWARD);
@@ -375,6 +380,7 @@ template <typename T, class S>
 __global__ __launch_bounds__(S::THREADS) void cross_entropy_gradient_kernel(CeArgs a, const T* weight, uint32_t from, uint32_t columns) {
     const float raise = RAISED<T> ? a.header->raise : 1.0f;
     logit_tiles<T, S, true>(a, weight, from, columns, [&](const f32x16 (&c)[S::MT][S::NT], uint32_t at, uint32_t part_n, const float* bias, const RowFacts<S>& facts, uint32_t count) {
+        const bool fine = count <= CE_FINE_ROWS;
         const uint32_t lane = threadIdx.x % WAVE, v0 = from + at;
         const bool biased = a.bias || v0 + S::MT * 32 > a.vocab;
         float sums[S::MT * 16];
@@ -408,6 +414,12 @@ __global__ __launch_bounds__(S::THREADS) void cross_entropy_gradient_kernel(CeAr
                 }
                 store_eight(to + m * 32, low);
                 store_eight(to + m * 32 + 8, high);
+                if (fine) {
+                    const auto rest = [](f32x8 v) { return v - __builtin_convertvector(__builtin_convertvector(v, frag<T>), f32x8); };
+                    T* more = (T*)a.d_rest + (uint64_t)row * a.piece + at + lane / 32 * 16 + m * 32;
+                    store_eight(more, rest(low));
+                    store_eight(more + 8, rest(high));
+                }
             }
         }
         if (!a.dbias_sums) return;
@@ -422,44 +434,37 @@ __global__ __launch_bounds__(S::THREADS) void cross_entropy_gradient_kernel(CeAr
 
 // ------------------------------------------------------------------ gradients of h, W and the bias
 
-// How many parts the sum over a piece is dealt to, so that a few rows' tiles fill the chip as well.
-struct Split { uint32_t tiles_n, parts; };
+// How many parts a sum over so many pieces of k is dealt to, so that few tiles fill the chip as well.
+__host__ __device__ __forceinline__ uint32_t ce_parts(uint32_t tiles, uint32_t pieces) {
+    const uint32_t room = CE_SPLIT_TILES / (tiles ? tiles : 1), worth = pieces / CE_SPLIT_PIECES, parts = room < worth ? room : worth;
+    return parts ? parts : 1;
+}
+struct Split { uint32_t tiles_m, tiles_n, parts; };
 template <class S>
-__device__ __forceinline__ Split dh_split(uint32_t count, uint32_t width_pad) {
-    const uint32_t tiles_n = (count + S::TILE_N - 1) / S::TILE_N, tiles = max(1u, tiles_n * ((width_pad + S::TILE_M - 1) / S::TILE_M));
-    return {tiles_n, max(1u, CE_SPLIT_TILES / 2 / tiles)};
+__device__ __forceinline__ Split ce_split(uint32_t m, uint32_t n, uint32_t k) {
+    const uint32_t tiles_m = (m + S::TILE_M - 1) / S::TILE_M, tiles_n = (n + S::TILE_N - 1) / S::TILE_N;
+    return {tiles_m, tiles_n, ce_parts(tiles_m * tiles_n, (k + PRODUCT_K - 1) / PRODUCT_K)};
+}
+// dh: over the vocabulary of a whole piece; dW: over the listed rows.
+template <class S> __device__ __forceinline__ Split dh_split(const CeArgs& a, uint32_t count) {
+    Split s = ce_split<S>(a.width_pad, count, a.piece);
+    if (count <= CE_FINE_ROWS) s.parts = s.parts > 1 ? s.parts / 2 * 2 : 2;          // every other one of d's rest
+    return s;
+}
+template <class S> __device__ __forceinline__ Split dw_split(const CeArgs& a, uint32_t count, uint32_t columns) {
+    return ce_split<S>(a.width_pad, columns, a.dw_sums ? count : 0);
 }
 
-// dh += d W over a piece.
-template <typename T, class S>
-__global__ __launch_bounds__(S::THREADS) void cross_entropy_dh_kernel(CeArgs a, const T* weight, uint32_t from, uint32_t columns) {
-    __shared__ __attribute__((aligned(1024))) char lds[S::BYTES];
-    const uint32_t count = a.header->count, tiles_m = (a.width_pad + S::TILE_M - 1) / S::TILE_M;
-    if (count == 0) return;
-    const Split split = dh_split<S>(count, a.width_pad);
-    const TilePlace tile = tile_place(blockIdx.x, tiles_m, split.tiles_n * split.parts);
-    if (!tile.there) return;
-    const uint32_t part = tile.n / split.tiles_n, n_tile = tile.n % split.tiles_n;
-    const uint32_t pieces = (columns + PRODUCT_K - 1) / PRODUCT_K;
-    const uint32_t k0 = (uint32_t)((uint64_t)pieces * part / split.parts) * PRODUCT_K, k1 = (uint32_t)((uint64_t)pieces * (part + 1) / split.parts) * PRODUCT_K;
-    const uint32_t col = tile.m * S::TILE_M, row = n_tile * S::TILE_N;
-    Transposed<T, S::TILE_M, S::WAVES, true> x(weight + (from + k0) * a.weight_stride + col, weight + (a.vocab - 1) * a.weight_stride + a.width,
-                                               a.weight_stride * 2, a.width - min(a.width, col));
-    const T* d = (const T*)a.d;
-    KMajor<T, S::TILE_N, S::WAVES, false> y(d + (uint64_t)row * a.piece + k0, d + (uint64_t)a.rows_pad * a.piece, a.piece * 2);
-    f32x16 c[S::MT][S::NT];
-    Product<T, S, decltype(x), decltype(y)> p(x, y, k1 - k0, lds);
-    p.begin();
-    p.run(c, lds);
-    const uint32_t lane = threadIdx.x % WAVE, m0 = col + S::wave_m() * (S::MT * 32) + lane / 32 * 16, n0 = row + S::wave_n() * (S::NT * 32) + lane % 32;
-    const bool first = from == 0;
+// A wave's sums as fp32, row by row of n.
+template <class S>
+__device__ __forceinline__ void store_sums(float* sums, uint32_t width_pad, const f32x16 (&c)[S::MT][S::NT], uint32_t m0, uint32_t n0, uint32_t rows, bool first) {
 #pragma unroll
     for (int n = 0; n < S::NT; ++n) {
-        if (n0 + n * 32 >= count) continue;
-        float* to = a.dh_sums + ((uint64_t)part * split.tiles_n * S::TILE_N + n0 + n * 32) * a.width_pad + m0;
+        if (n0 + n * 32 >= rows) continue;
+        float* to = sums + (uint64_t)(n0 + n * 32) * width_pad + m0;
 #pragma unroll
         for (int m = 0; m < S::MT; ++m) {
-            if (m0 + m * 32 >= a.width_pad) continue;
+            if (m0 + m * 32 >= width_pad) continue;
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
                 float4* at = reinterpret_cast<float4*>(to + m * 32 + q * 4);
@@ -474,40 +479,83 @@ __global__ __launch_bounds__(S::THREADS) void cross_entropy_dh_kernel(CeArgs a, 
     }
 }
 
-// The parts of dh, rounded; a wave a row.
+// dh += d W over a piece.  With few rows one entry of d, the label's, is most of a row's gradient, and its rounding would be the row's
+// error (up to 2.5 times that of the output's own); so d's rest goes in as well, as further parts of the sum, beside which W comes by once.
 template <typename T, class S>
-__global__ __launch_bounds__(CE_THREADS) void cross_entropy_dh_join_kernel(CeArgs a, T* dh) {
-    const uint32_t n = blockIdx.x * (CE_THREADS / WAVE) + threadIdx.x / WAVE, lane = threadIdx.x % WAVE, count = a.header->count;
-    if (n >= count) return;
-    const Split split = dh_split<S>(count, a.width_pad);
-    const float lower = RAISED<T> ? a.header->lower : 1.0f;
-    T* to = dh + a.list[n] * a.dh_stride;
-    for (uint32_t c = lane * 8; c < a.width; c += WAVE * 8) {
-        f32x8 sum = 0.0f;
-#pragma unroll 4
-        for (uint32_t p = 0; p < split.parts; ++p)
-            sum += load_eight(a.dh_sums + ((uint64_t)p * split.tiles_n * S::TILE_N + n) * a.width_pad + c);
-        store_eight(to + c, sum * lower);
-    }
+__global__ __launch_bounds__(S::THREADS) void cross_entropy_dh_kernel(CeArgs a, const T* weight, uint32_t from, uint32_t columns) {
+    __shared__ __attribute__((aligned(1024))) char lds[S::BYTES];
+    const uint32_t count = a.header->count;
+    if (count == 0) return;
+    const Split split = dh_split<S>(a, count);
+    const TilePlace tile = tile_place(blockIdx.x, split.tiles_m, split.tiles_n * split.parts);
+    if (!tile.there) return;
+    const uint32_t part = tile.n / split.tiles_n, n_tile = tile.n % split.tiles_n;
+    const bool fine = count <= CE_FINE_ROWS, rest = fine && part % 2;
+    const uint32_t pieces = (columns + PRODUCT_K - 1) / PRODUCT_K, shares = fine ? split.parts / 2 : split.parts, share = fine ? part / 2 : part;
+    const uint32_t k0 = (uint32_t)((uint64_t)pieces * share / shares) * PRODUCT_K, k1 = (uint32_t)((uint64_t)pieces * (share + 1) / shares) * PRODUCT_K;
+    const uint32_t col = tile.m * S::TILE_M, row = n_tile * S::TILE_N;
+    typedef Transposed<T, S::TILE_M, S::WAVES, true> A;
+    typedef KMajor<T, S::TILE_N, S::WAVES, false> B;
+    const T *d = rest ? (const T*)a.d_rest : (const T*)a.d, *end = d + (uint64_t)(rest ? CE_FINE_ROWS : a.rows_pad) * a.piece;
+    f32x16 c[S::MT][S::NT];
+    clear<S>(c);
+    Product<T, S, A, B> p(A(weight + (from + k0) * a.weight_stride + col, weight + (a.vocab - 1) * a.weight_stride + a.width, a.weight_stride * 2, a.width - min(a.width, col)),
+                          B(d + (uint64_t)row * a.piece + k0, end, a.piece * 2), k1 - k0, lds);
+    p.begin();
+    p.run(c, lds);
+    const uint32_t lane = threadIdx.x % WAVE, m0 = col + S::wave_m() * (S::MT * 32) + lane / 32 * 16, n0 = row + S::wave_n() * (S::NT * 32) + lane % 32;
+    store_sums<S>(a.dh_sums + (uint64_t)part * split.tiles_n * S::TILE_N * a.width_pad, a.width_pad, c, m0, n0, count, from == 0);
 }
 
-// dW = d' h over the listed rows, of the vocabulary's piece.
+// Eight columns a lane of the sum of a row's parts.
+__device__ __forceinline__ f32x8 parts_of_row(const float* sums, uint64_t part_floats, uint32_t parts, uint64_t at) {
+    f32x8 sum = 0.0f;
+#pragma unroll 8
+    for (uint32_t p = 0; p < parts; ++p) sum += load_eight(sums + p * part_floats + at);
+    return sum;
+}
+
+// The parts of dh, rounded; a wave 512 columns of a row.
+template <typename T, class S>
+__global__ __launch_bounds__(CE_THREADS) void cross_entropy_dh_join_kernel(CeArgs a, T* dh) {
+    const uint32_t n = blockIdx.x * (CE_THREADS / WAVE) + threadIdx.x / WAVE, c = (blockIdx.y * WAVE + threadIdx.x % WAVE) * 8, count = a.header->count;
+    if (n >= count || c >= a.width) return;
+    const Split split = dh_split<S>(a, count);
+    const float lower = RAISED<T> ? a.header->lower : 1.0f;
+    store_eight(dh + a.list[n] * a.dh_stride + c,
+                parts_of_row(a.dh_sums, (uint64_t)split.tiles_n * S::TILE_N * a.width_pad, split.parts, (uint64_t)n * a.width_pad + c) * lower);
+}
+
+// dW = d' h over the listed rows, of the vocabulary's piece; its parts as fp32 where there are several.
 template <typename T, typename W, class S>
 __global__ __launch_bounds__(S::THREADS) void cross_entropy_dweight_kernel(CeArgs a, W* dweight, uint32_t from, uint32_t columns) {
     __shared__ __attribute__((aligned(1024))) char lds[S::BYTES];
     const uint32_t count = a.header->count;
-    const TilePlace tile = tile_place(blockIdx.x, (a.width_pad + S::TILE_M - 1) / S::TILE_M, (columns + S::TILE_N - 1) / S::TILE_N);
+    const Split split = dw_split<S>(a, count, columns);
+    const TilePlace tile = tile_place(blockIdx.x, split.tiles_m, split.tiles_n * split.parts);
     if (!tile.there) return;
-    const uint32_t col = tile.m * S::TILE_M, v = tile.n * S::TILE_N;
-    const T *h = (const T*)a.h, *d = (const T*)a.d;
-    Transposed<T, S::TILE_M, S::WAVES, true> x(h + col, h + (uint64_t)a.rows_pad * a.width_pad, a.width_pad * 2, a.width_pad - min(a.width_pad, col));
-    Transposed<T, S::TILE_N, S::WAVES, false> y(d + v, d + (uint64_t)a.rows_pad * a.piece, (uint64_t)a.piece * 2, a.piece - v);
+    const uint32_t part = tile.n / split.tiles_n, pieces = (count + PRODUCT_K - 1) / PRODUCT_K;
+    const uint32_t k0 = (uint32_t)((uint64_t)pieces * part / split.parts) * PRODUCT_K, k1 = (uint32_t)((uint64_t)pieces * (part + 1) / split.parts) * PRODUCT_K;
+    const uint32_t col = tile.m * S::TILE_M, v = tile.n % split.tiles_n * S::TILE_N;
+    const T* h = (const T*)a.h;
+    typedef Transposed<T, S::TILE_M, S::WAVES, true> A;
+    typedef Transposed<T, S::TILE_N, S::WAVES, false> B;
     f32x16 c[S::MT][S::NT];
-    Product<T, S, decltype(x), decltype(y)> p(x, y, (count + PRODUCT_K - 1) / PRODUCT_K * PRODUCT_K, lds);
-    p.begin();
-    p.run(c, lds);
-    const float lower = RAISED<T> ? a.header->lower : 1.0f;
+    clear<S>(c);
+    for (int rest = 0; rest < (count <= CE_FINE_ROWS ? 2 : 1); ++rest) {
+        const T* d = rest ? (const T*)a.d_rest : (const T*)a.d;
+        const T* end = d + (uint64_t)(rest ? CE_FINE_ROWS : a.rows_pad) * a.piece;
+        Product<T, S, A, B> p(A(h + (uint64_t)k0 * a.width_pad + col, h + (uint64_t)a.rows_pad * a.width_pad, a.width_pad * 2, a.width_pad - min(a.width_pad, col)),
+                              B(d + (uint64_t)k0 * a.piece + v, end, (uint64_t)a.piece * 2, a.piece - v), k1 - k0, lds);
+        p.begin();
+        p.run(c, lds);
+    }
     const uint32_t lane = threadIdx.x % WAVE, m0 = col + S::wave_m() * (S::MT * 32) + lane / 32 * 16, n0 = v + S::wave_n() * (S::NT * 32) + lane % 32;
+    if (split.parts > 1) {
+        store_sums<S>(a.dw_sums + (uint64_t)part * split.tiles_n * S::TILE_N * a.width_pad, a.width_pad, c, m0, n0, columns, true);
+        return;
+    }
+    const float lower = RAISED<T> ? a.header->lower : 1.0f;
 #pragma unroll
     for (int n = 0; n < S::NT; ++n) {
         if (n0 + n * 32 >= columns) continue;
@@ -525,6 +573,16 @@ __global__ __launch_bounds__(S::THREADS) void cross_entropy_dweight_kernel(CeArg
     }
 }
 
+template <typename T, typename W, class S>
+__global__ __launch_bounds__(CE_THREADS) void cross_entropy_dweight_join_kernel(CeArgs a, W* dweight, uint32_t from, uint32_t columns) {
+    const uint32_t n = blockIdx.x * (CE_THREADS / WAVE) + threadIdx.x / WAVE, c = (blockIdx.y * WAVE + threadIdx.x % WAVE) * 8;
+    const Split split = dw_split<S>(a, a.header->count, columns);
+    if (n >= columns || c >= a.width || split.parts == 1) return;
+    const float lower = RAISED<T> ? a.header->lower : 1.0f;
+    store_eight(dweight + (from + n) * a.dweight_stride + c,
+                parts_of_row(a.dw_sums, (uint64_t)split.tiles_n * S::TILE_N * a.width_pad, split.parts, (uint64_t)n * a.width_pad + c) * lower);
+}
+
 template <class S>
 __global__ __launch_bounds__(CE_THREADS) void cross_entropy_dbias_kernel(CeArgs a, float* dbias) {
     const uint32_t v = blockIdx.x * CE_THREADS + threadIdx.x;
@@ -540,17 +598,23 @@ __global__ __launch_bounds__(CE_THREADS) void cross_entropy_dbias_kernel(CeArgs 
 
 struct CePlan {
     uint32_t rows_pad, width_pad, vocab_pad, piece;
-    bool small_logits, small_dh, small_dweight;
+    bool small_logits, small_dh, small_dweight, split_dweight;
     uint64_t logit_groups, piece_groups, dh_groups, dweight_groups;
     size_t counts_at, list_at, label_at, h_at, lse_at, g_at;         // shared and backward
     size_t stats_at, said_at, forward_bytes;
-    size_t d_at, dh_at, dbias_at, backward_bytes;
+    size_t d_at, rest_at, dh_at, dw_at, dbias_at, backward_bytes;
 };
 
 static uint64_t ce_up(uint64_t n, uint64_t by) { return (n + by - 1) / by * by; }
 
 // Tiles of 256 x 256 where they fill the chip, else of 128 x 128, two workgroups a CU.
 static bool ce_small(uint64_t m, uint64_t n) { return n <= 128 || (m + 255) / 256 * ((n + 255) / 256) < 200; }
+
+// The same where a sum over k can be dealt to several workgroups.
+static bool ce_small_split(uint64_t m, uint64_t n, uint64_t k) {
+    const uint64_t tiles = (m + 255) / 256 * ((n + 255) / 256), parts = k / (PRODUCT_K * CE_SPLIT_PIECES);
+    return n <= 128 || tiles * (parts ? parts : 1) < 200;
+}
 
 static bool ce_plan(uint64_t rows, uint32_t width, uint32_t vocab, CePlan& p) {
     if (rows > CE_MAX || vocab == 0 || vocab > CE_MAX || width < 8 || width > CE_MAX_WIDTH || width % 8 != 0) return false;
@@ -564,17 +628,22 @@ static bool ce_plan(uint64_t rows, uint32_t width, uint32_t vocab, CePlan& p) {
     p.piece = (uint32_t)ce_up((p.vocab_pad + pieces - 1) / pieces, CE_PAD);
     const auto tiles = [](uint64_t n, bool small) { return (n + (small ? 127 : 255)) / (small ? 128 : 256); };
     p.small_logits = ce_small(vocab, some);
-    p.small_dh = some <= 128;
-    p.small_dweight = ce_small(p.width_pad, p.piece);
+    p.small_dh = ce_small_split(p.width_pad, some, p.piece);
+    p.small_dweight = ce_small_split(p.width_pad, p.piece, some);
     // workgroups of large tiles of logits stay on their CU; those of a die keep its tiles
     const uint64_t stay = ce_up(device_cus(), DIES), logit_tiles = tile_groups(tiles(vocab, p.small_logits) * tiles(some, p.small_logits)),
                    piece_tiles = tile_groups(tiles(p.piece, p.small_logits) * tiles(some, p.small_logits));
     if (logit_tiles > UINT32_MAX / 2) return false;
     p.logit_groups = p.small_logits || logit_tiles < stay ? logit_tiles : stay;
     p.piece_groups = p.small_logits || piece_tiles < stay ? piece_tiles : stay;
-    const uint64_t dh_tiles = tiles(p.width_pad, p.small_dh) * tiles(some, p.small_dh);
+    const uint64_t dh_tiles = tiles(p.width_pad, p.small_dh) * tiles(some, p.small_dh), dw_tiles = tiles(p.width_pad, p.small_dweight) * tiles(p.piece, p.small_dweight);
+    const uint64_t fine_tiles = 2 * tiles(p.width_pad, p.small_dh) * tiles(some < CE_FINE_ROWS ? some : CE_FINE_ROWS, p.small_dh);
     p.dh_groups = tile_groups(dh_tiles > CE_SPLIT_TILES ? dh_tiles : CE_SPLIT_TILES);
-    p.dweight_groups = tile_groups(tiles(p.width_pad, p.small_dweight) * tiles(p.piece, p.small_dweight));
+    if (p.dh_groups < fine_tiles) p.dh_groups = tile_groups(fine_tiles);
+    p.dweight_groups = tile_groups(dw_tiles > CE_SPLIT_TILES ? dw_tiles : CE_SPLIT_TILES);
+    // the last piece of the vocabulary, with fewer tiles, may be split where the others are not
+    const uint64_t least = tiles(p.width_pad, p.small_dweight) * tiles(pieces > 1 ? 1 : vocab, p.small_dweight);
+    p.split_dweight = least <= CE_SPLIT_TILES && ce_parts((uint32_t)least, (uint32_t)((some + PRODUCT_K - 1) / PRODUCT_K)) > 1;
     for (const uint64_t groups : {p.logit_groups, p.piece_groups, p.dh_groups, p.dweight_groups})
         if (groups > LAUNCH_GROUPS / 2) return false;
     size_t at = 256;
@@ -595,9 +664,12 @@ static bool ce_plan(uint64_t rows, uint32_t width, uint32_t vocab, CePlan& p) {
     p.lse_at = place(4ull * p.rows_pad);
     p.g_at = place(4ull * p.rows_pad);
     p.d_at = place(2ull * p.rows_pad * p.piece);
-    // sums of dh: all rows once, or the parts of fewer
-    const uint64_t tile = p.small_dh ? 128 * 128 : 256 * 256, once = (uint64_t)p.rows_pad * p.width_pad, parts = CE_SPLIT_TILES * tile;
-    p.dh_at = place(4 * (once > parts ? once : parts));
+    p.rest_at = place(2ull * CE_FINE_ROWS * p.piece);
+    // sums of dh: all rows once, or the parts of fewer; those of dW where there are parts
+    const auto parts = [](bool small) { return (uint64_t)CE_SPLIT_TILES * (small ? 128 * 128 : 256 * 256); };
+    const uint64_t once = ((uint64_t)p.rows_pad + CE_FINE_ROWS) * p.width_pad;
+    p.dh_at = place(4 * (once > parts(p.small_dh) ? once : parts(p.small_dh)));
+    p.dw_at = place(p.split_dweight ? 4 * parts(p.small_dweight) : 0);
     p.dbias_at = place(4ull * (p.rows_pad / 64) * p.vocab_pad);
     p.backward_bytes = at;
     return true;
@@ -637,7 +709,9 @@ static void ce_workspace(CeArgs& a, const CePlan& p, char* ws, bool backward) {
     a.lse_of = backward ? (float*)(ws + p.lse_at) : nullptr;
     a.g_of = backward ? (float*)(ws + p.g_at) : nullptr;
     a.d = backward ? ws + p.d_at : nullptr;
+    a.d_rest = backward ? ws + p.rest_at : nullptr;
     a.dh_sums = backward ? (float*)(ws + p.dh_at) : nullptr;
+    a.dw_sums = backward && p.split_dweight ? (float*)(ws + p.dw_at) : nullptr;
     a.dbias_sums = backward ? (float*)(ws + p.dbias_at) : nullptr;
 }
 
@@ -650,7 +724,7 @@ static int ce_listed(const CeArgs& a, const void* h, float* loss, const float* l
         hipLaunchKernelGGL(cross_entropy_count_kernel, dim3((a.rows + CE_BLOCK - 1) / CE_BLOCK), dim3(CE_THREADS), 0, s, a, RAISED<T> ? dloss : nullptr);
         if (const int status = launch_status()) return status;
     }
-    const uint32_t groups = a.rows ? (a.rows + CE_GATHERED - 1) / CE_GATHERED : 1;
+    const uint32_t rows = (a.rows + CE_GATHERED - 1) / CE_GATHERED, groups = rows < CE_PAD / CE_GATHERED ? CE_PAD / CE_GATHERED : rows;     // the zeros want some, too
     hipLaunchKernelGGL(cross_entropy_gather_kernel<T>, dim3(groups), dim3(CE_THREADS), 0, s, a, (const T*)h, loss, lse_in, lse_out, dloss, (T*)dh);
     return launch_status();
 }
@@ -672,11 +746,21 @@ static int ce_dh(const CeArgs& a, const CePlan& p, const void* weight, uint32_t 
     hipLaunchKernelGGL((cross_entropy_dh_kernel<T, S>), dim3((unsigned)p.dh_groups), dim3(S::THREADS), 0, s, a, (const T*)weight, from, columns);
     return launch_status();
 }
+// A wave 512 columns of a row.
+static dim3 ce_join_grid(uint32_t rows, uint32_t width) { return dim3((rows + CE_THREADS / WAVE - 1) / (CE_THREADS / WAVE), (width + WAVE * 8 - 1) / (WAVE * 8)); }
+
+template <typename T, typename W, class S>
+static int ce_dweight_type(const CeArgs& a, const CePlan& p, W* dweight, uint32_t from, uint32_t columns, hipStream_t s) {
+    hipLaunchKernelGGL((cross_entropy_dweight_kernel<T, W, S>), dim3((unsigned)p.dweight_groups), dim3(S::THREADS), 0, s, a, dweight, from, columns);
+    if (const int status = launch_status()) return status;
+    const uint64_t tiles = (uint64_t)((a.width_pad + S::TILE_M - 1) / S::TILE_M) * ((columns + S::TILE_N - 1) / S::TILE_N);
+    if (!p.split_dweight || tiles * 2 > CE_SPLIT_TILES) return OKT_OK;
+    hipLaunchKernelGGL((cross_entropy_dweight_join_kernel<T, W, S>), ce_join_grid(columns, a.width), dim3(CE_THREADS), 0, s, a, dweight, from, columns);
+    return launch_status();
+}
 template <typename T, class S>
 static int ce_dweight(const CeArgs& a, const CePlan& p, void* dweight, bool wide, uint32_t from, uint32_t columns, hipStream_t s) {
-    if (wide) hipLaunchKernelGGL((cross_entropy_dweight_kernel<T, float, S>), dim3((unsigned)p.dweight_groups), dim3(S::THREADS), 0, s, a, (float*)dweight, from, columns);
-    else hipLaunchKernelGGL((cross_entropy_dweight_kernel<T, T, S>), dim3((unsigned)p.dweight_groups), dim3(S::THREADS), 0, s, a, (T*)dweight, from, columns);
-    return launch_status();
+    return wide ? ce_dweight_type<T, float, S>(a, p, (float*)dweight, from, columns, s) : ce_dweight_type<T, T, S>(a, p, (T*)dweight, from, columns, s);
 }
 
 template <typename T, class S>
@@ -694,7 +778,7 @@ static int ce_backward(const CeArgs& a, const CePlan& p, const void* weight, con
                 return status;
     }
     if (g.dh && a.rows) {
-        const dim3 rows((a.rows + CE_THREADS / WAVE - 1) / (CE_THREADS / WAVE));
+        const dim3 rows = ce_join_grid(a.rows, a.width);
         if (p.small_dh) hipLaunchKernelGGL((cross_entropy_dh_join_kernel<T, Small>), rows, dim3(CE_THREADS), 0, s, a, (T*)g.dh);
         else hipLaunchKernelGGL((cross_entropy_dh_join_kernel<T, Large>), rows, dim3(CE_THREADS), 0, s, a, (T*)g.dh);
         if (const int status = launch_status()) return status;

@@ -94,6 +94,14 @@ struct Transposed {
     }
 };
 
+template <class S>
+__device__ __forceinline__ void clear(f32x16 (&c)[S::MT][S::NT]) {
+#pragma unroll
+    for (int m = 0; m < S::MT; ++m)
+#pragma unroll
+        for (int n = 0; n < S::NT; ++n) c[m][n] = 0.0f;
+}
+
 // WM x WN waves of MT x NT squares, and buffers in LDS for STAGES pieces: one is worked on, the others are on their way.
 template <int MT_, int NT_, int WM_, int WN_, int STAGES_>
 struct ProductShape {
@@ -158,11 +166,8 @@ struct Product {
         }
     }
 
+    // Adds to c.
     __device__ __forceinline__ void run(f32x16 (&c)[S::MT][S::NT], const char* lds) {
-#pragma unroll
-        for (int m = 0; m < S::MT; ++m)
-#pragma unroll
-            for (int n = 0; n < S::NT; ++n) c[m][n] = 0.0f;
         if (k == 0) return;
         constexpr int STEPS = PRODUCT_K / 16, EARLY = LOADS / 2, LATE = LOADS - EARLY;       // fetches in the last step, in the first
         constexpr int EACH = ((EARLY > LATE ? EARLY : LATE) + S::MT - 1) / S::MT;

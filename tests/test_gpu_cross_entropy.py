@@ -108,7 +108,11 @@ CASES = [
     dict(rows=2600, width=88, vocab=5100, kind="f16", labelled=0.97),
     dict(rows=140, width=1112, vocab=10_300, bias=True),                            # dweight in large tiles
     dict(rows=140, width=1112, vocab=10_300, kind="f16", wide_dw=True),
+    dict(rows=1300, width=328, vocab=200, bias=True), dict(rows=2500, width=136, vocab=130, kind="f16", wide_dw=True, labelled=0.9, pad=8),   # dweight in parts
+    dict(rows=300, width=520, vocab=6000, bias=True, one_g=True),                   # dh in parts
+    dict(rows=257, width=64, vocab=600), dict(rows=256, width=64, vocab=600, kind="f16"),
     dict(rows=65_000, width=64, vocab=9001, labelled=0.006, bias=True),             # three pieces, few rows among many
+    dict(rows=131_000, width=72, vocab=4300, labelled=0.03, bias=True),             # two pieces, the last one's dweight in parts
     dict(rows=65_000, width=40, vocab=4097, labelled=0.02, kind="f16", one_g=True)]
 
 
