@@ -779,7 +779,7 @@ int okt_cross_entropy_forward(const okt_cross_entropy* op, const void* d_h, cons
  *   d_dloss  in   fp32[rows] or fp32[1], see dloss_stride
  *   d_dh_out, d_dweight_out, d_dbias_out  out  overwritten; each may be NULL (not all; the last one has to be without a bias), and
  *            none overlaps another or an input, from its first element to its last
- * Two launches (one up to 2048 rows), up to three a piece of the vocabulary (a fourth where dW has few tiles and many rows), and two more.
+ * Two launches (one up to 2048 rows), two or three a piece of the vocabulary (one more where dW has few tiles and many rows), and one for the sums that are left.
  */
 int okt_cross_entropy_backward(const okt_cross_entropy* op, const void* d_h, const void* d_weight, const int64_t* d_labels,
                                const float* d_lse, const float* d_dloss, void* d_dh_out, void* d_dweight_out, float* d_dbias_out,

@@ -31,6 +31,7 @@ constexpr int CE_THREADS = 256;
 constexpr float LOG2E = 1.44269504088896340736f;
 
 typedef ProductShape<4, 2, 2, 4, 2> Large;                           // 256 x 256, one workgroup of eight waves a CU
+typedef ProductShape<2, 2, 2, 2, 2> Narrow;                          // 128 x 128, two workgroups a CU: many tiles of a short sum
 typedef ProductShape<2, 2, 2, 2, 3> Small;                           // 128 x 128, four waves and two pieces on their way
 
 template <typename T> constexpr bool RAISED = false;
@@ -59,12 +60,14 @@ struct CeArgs {
     float* dh_sums;                                                  // [parts][rows of whole tiles][width_pad]
     float* dbias_sums;                                               // [parts][vocab_pad]
     uint32_t piece, vocab_pad;
+    uint32_t logit_tile_n, logit_parts_n;                            // rows of a tile of logits, and parts they leave of the bias's gradient
+    __device__ __forceinline__ uint32_t dbias_parts(uint32_t count) const { return (count + logit_tile_n - 1) / logit_tile_n * logit_parts_n; }
 };
 
 // ------------------------------------------------------------------ the list of labelled rows
 
 constexpr uint32_t CE_BLOCK = 256;                                   // rows that a thread each counts
-constexpr uint32_t CE_GATHERED = 16;                                 // rows that a workgroup gathers
+constexpr uint32_t CE_GATHERED = 8;                                  // rows that a workgroup gathers
 constexpr uint32_t CE_DIRECT = 2048;                                 // up to so many rows, every workgroup counts all of them by itself
 
 __device__ __forceinline__ bool labelled(int64_t y, uint32_t vocab) { return y >= 0 && y < (int64_t)vocab; }
@@ -108,7 +111,7 @@ __global__ __launch_bounds__(CE_THREADS) void cross_entropy_count_kernel(CeArgs 
     if (threadIdx.x == 0) a.counts[blockIdx.x] = make_float2(__uint_as_float(c.all), c.top);
 }
 
-// Sixteen rows a workgroup: those with a label go side by side into the workspace, behind all labelled ones before them; the others
+// Eight rows a workgroup: those with a label go side by side into the workspace, behind all labelled ones before them; the others
 // get their zeros.  Zeros fill the last tile, too.
 template <typename T>
 __global__ __launch_bounds__(CE_THREADS) void cross_entropy_gather_kernel(CeArgs a, const T* h, float* loss, const float* lse_in, float* lse_out, const float* dloss, T* dh) {
@@ -137,7 +140,7 @@ __global__ __launch_bounds__(CE_THREADS) void cross_entropy_gather_kernel(CeArgs
         const int by = use ? min(max(15 - e, -120), 120) : 0;
         *a.header = {c.all, ldexpf(1.0f, by), ldexpf(1.0f, -by), 0};
     }
-    // the sixteen labels at once; a wave takes four rows, whose vectors are on their way together
+    // the labels at once; a wave takes two rows, whose vectors are on their way together
     const bool inside = lane < CE_GATHERED && first + lane < a.rows;
     const int64_t y = inside ? a.labels[first + lane] : -1;
     const uint64_t listed = __ballot(labelled(y, a.vocab));
@@ -164,6 +167,7 @@ __global__ __launch_bounds__(CE_THREADS) void cross_entropy_gather_kernel(CeArgs
             if (lse_out) lse_out[row] = 0.0f;
         }
     }
+#pragma unroll 2
     for (uint32_t x = lane * 8; x < a.width_pad; x += WAVE * 8) {
         vec v[EACH];
 #pragma unroll
@@ -249,7 +253,7 @@ template <typename T, class S, bool BACKWARD, class F>
 __device__ __forceinline__ void logit_tiles(const CeArgs& a, const T* weight, uint32_t from, uint32_t columns, const F& finish) {
     __shared__ __attribute__((aligned(1024))) char lds[S::BYTES];
     __shared__ float bias[2][S::TILE_M];
-    const uint32_t count = a.header->count, tiles_m = (columns + S::TILE_M - 1) / S::TILE_M, tiles_n = (count + S::TILE_N - 1) / S::TILE_N;
+    const uint32_t count = uniform(a.header->count), tiles_m = (columns + S::TILE_M - 1) / S::TILE_M, tiles_n = (count + S::TILE_N - 1) / S::TILE_N;
     uint32_t group = blockIdx.x;
     TilePlace tile = tile_place(group, tiles_m, tiles_n);
     if (!tile.there) return;
@@ -321,7 +325,7 @@ __device__ __forceinline__ RowSum together(RowSum x, RowSum y) {
 
 __global__ __launch_bounds__(CE_JOIN_THREADS) void cross_entropy_join_kernel(CeArgs a, uint32_t parts, float* loss, float* lse) {
     __shared__ RowSum waves[CE_JOIN_THREADS / WAVE][16];
-    const uint32_t count = a.header->count, r = threadIdx.x % 16, share = threadIdx.x / 16, row = blockIdx.x * 16 + r;
+    const uint32_t count = uniform(a.header->count), r = threadIdx.x % 16, share = threadIdx.x / 16, row = blockIdx.x * 16 + r;
     if (blockIdx.x * 16 >= count) return;
     RowSum v = {-__builtin_inff(), 0.0f};
     if (row < count)
@@ -482,12 +486,10 @@ __device__ __forceinline__ void store_sums(float* sums, uint32_t width_pad, cons
 // dh += d W over a piece.  With few rows one entry of d, the label's, is most of a row's gradient, and its rounding would be the row's
 // error (up to 2.5 times that of the output's own); so d's rest goes in as well, as further parts of the sum, beside which W comes by once.
 template <typename T, class S>
-__global__ __launch_bounds__(S::THREADS) void cross_entropy_dh_kernel(CeArgs a, const T* weight, uint32_t from, uint32_t columns) {
-    __shared__ __attribute__((aligned(1024))) char lds[S::BYTES];
-    const uint32_t count = a.header->count;
+__device__ __forceinline__ void dh_tile(const CeArgs& a, const T* weight, uint32_t from, uint32_t columns, uint32_t group, uint32_t count, char* lds) {
     if (count == 0) return;
     const Split split = dh_split<S>(a, count);
-    const TilePlace tile = tile_place(blockIdx.x, split.tiles_m, split.tiles_n * split.parts);
+    const TilePlace tile = tile_place(group, split.tiles_m, split.tiles_n * split.parts);
     if (!tile.there) return;
     const uint32_t part = tile.n / split.tiles_n, n_tile = tile.n % split.tiles_n;
     const bool fine = count <= CE_FINE_ROWS, rest = fine && part % 2;
@@ -515,24 +517,11 @@ __device__ __forceinline__ f32x8 parts_of_row(const float* sums, uint64_t part_f
     return sum;
 }
 
-// The parts of dh, rounded; a wave 512 columns of a row.
-template <typename T, class S>
-__global__ __launch_bounds__(CE_THREADS) void cross_entropy_dh_join_kernel(CeArgs a, T* dh) {
-    const uint32_t n = blockIdx.x * (CE_THREADS / WAVE) + threadIdx.x / WAVE, c = (blockIdx.y * WAVE + threadIdx.x % WAVE) * 8, count = a.header->count;
-    if (n >= count || c >= a.width) return;
-    const Split split = dh_split<S>(a, count);
-    const float lower = RAISED<T> ? a.header->lower : 1.0f;
-    store_eight(dh + a.list[n] * a.dh_stride + c,
-                parts_of_row(a.dh_sums, (uint64_t)split.tiles_n * S::TILE_N * a.width_pad, split.parts, (uint64_t)n * a.width_pad + c) * lower);
-}
-
 // dW = d' h over the listed rows, of the vocabulary's piece; its parts as fp32 where there are several.
 template <typename T, typename W, class S>
-__global__ __launch_bounds__(S::THREADS) void cross_entropy_dweight_kernel(CeArgs a, W* dweight, uint32_t from, uint32_t columns) {
-    __shared__ __attribute__((aligned(1024))) char lds[S::BYTES];
-    const uint32_t count = a.header->count;
+__device__ __forceinline__ void dweight_tile(const CeArgs& a, W* dweight, uint32_t from, uint32_t columns, uint32_t group, uint32_t count, char* lds) {
     const Split split = dw_split<S>(a, count, columns);
-    const TilePlace tile = tile_place(blockIdx.x, split.tiles_m, split.tiles_n * split.parts);
+    const TilePlace tile = tile_place(group, split.tiles_m, split.tiles_n * split.parts);
     if (!tile.there) return;
     const uint32_t part = tile.n / split.tiles_n, pieces = (count + PRODUCT_K - 1) / PRODUCT_K;
     const uint32_t k0 = (uint32_t)((uint64_t)pieces * part / split.parts) * PRODUCT_K, k1 = (uint32_t)((uint64_t)pieces * (part + 1) / split.parts) * PRODUCT_K;
@@ -540,16 +529,19 @@ __global__ __launch_bounds__(S::THREADS) void cross_entropy_dweight_kernel(CeArg
     const T* h = (const T*)a.h;
     typedef Transposed<T, S::TILE_M, S::WAVES, true> A;
     typedef Transposed<T, S::TILE_N, S::WAVES, false> B;
+    const auto rows_of = [&](uint32_t k) { return A(h + (uint64_t)k * a.width_pad + col, h + (uint64_t)a.rows_pad * a.width_pad, a.width_pad * 2, a.width_pad - min(a.width_pad, col)); };
+    const auto d_of = [&](const void* d, uint32_t rows) { return B((const T*)d + (uint64_t)k0 * a.piece + v, (const T*)d + (uint64_t)rows * a.piece, (uint64_t)a.piece * 2, a.piece - v); };
     f32x16 c[S::MT][S::NT];
     clear<S>(c);
-    for (int rest = 0; rest < (count <= CE_FINE_ROWS ? 2 : 1); ++rest) {
-        const T* d = rest ? (const T*)a.d_rest : (const T*)a.d;
-        const T* end = d + (uint64_t)(rest ? CE_FINE_ROWS : a.rows_pad) * a.piece;
-        Product<T, S, A, B> p(A(h + (uint64_t)k0 * a.width_pad + col, h + (uint64_t)a.rows_pad * a.width_pad, a.width_pad * 2, a.width_pad - min(a.width_pad, col)),
-                              B(d + (uint64_t)k0 * a.piece + v, end, (uint64_t)a.piece * 2, a.piece - v), k1 - k0, lds);
-        p.begin();
-        p.run(c, lds);
+    const bool fine = count <= CE_FINE_ROWS;                         // then d's rest stands behind d, beside the same rows again
+    Product<T, S, A, B, true> p(rows_of(k0), d_of(a.d, a.rows_pad), (k1 - k0) * (fine ? 2 : 1), lds);
+    if (fine) {
+        p.again = k1 - k0;
+        p.again_a = p.a.from;
+        p.again_b = d_of(a.d_rest, CE_FINE_ROWS).from;
     }
+    p.begin();
+    p.run(c, lds);
     const uint32_t lane = threadIdx.x % WAVE, m0 = col + S::wave_m() * (S::MT * 32) + lane / 32 * 16, n0 = v + S::wave_n() * (S::NT * 32) + lane % 32;
     if (split.parts > 1) {
         store_sums<S>(a.dw_sums + (uint64_t)part * split.tiles_n * S::TILE_N * a.width_pad, a.width_pad, c, m0, n0, columns, true);
@@ -573,21 +565,40 @@ __global__ __launch_bounds__(S::THREADS) void cross_entropy_dweight_kernel(CeArg
     }
 }
 
+// Both gradients of a piece in one launch, dh's workgroups before dW's: the ones fill the CUs that the others leave.
 template <typename T, typename W, class S>
-__global__ __launch_bounds__(CE_THREADS) void cross_entropy_dweight_join_kernel(CeArgs a, W* dweight, uint32_t from, uint32_t columns) {
-    const uint32_t n = blockIdx.x * (CE_THREADS / WAVE) + threadIdx.x / WAVE, c = (blockIdx.y * WAVE + threadIdx.x % WAVE) * 8;
-    const Split split = dw_split<S>(a, a.header->count, columns);
-    if (n >= columns || c >= a.width || split.parts == 1) return;
-    const float lower = RAISED<T> ? a.header->lower : 1.0f;
-    store_eight(dweight + (from + n) * a.dweight_stride + c,
-                parts_of_row(a.dw_sums, (uint64_t)split.tiles_n * S::TILE_N * a.width_pad, split.parts, (uint64_t)n * a.width_pad + c) * lower);
+__global__ __launch_bounds__(S::THREADS) void cross_entropy_products_kernel(CeArgs a, const T* weight, W* dweight, uint32_t from, uint32_t columns, uint32_t dh_groups) {
+    __shared__ __attribute__((aligned(1024))) char lds[S::BYTES];
+    const uint32_t count = uniform(a.header->count);
+    if (blockIdx.x < dh_groups) dh_tile<T, S>(a, weight, from, columns, blockIdx.x, count, lds);
+    else dweight_tile<T, W, S>(a, dweight, from, columns, blockIdx.x - dh_groups, count, lds);
 }
 
-template <class S>
-__global__ __launch_bounds__(CE_THREADS) void cross_entropy_dbias_kernel(CeArgs a, float* dbias) {
-    const uint32_t v = blockIdx.x * CE_THREADS + threadIdx.x;
+// What is left when the products are done: the parts of dh and dW, a wave 512 columns of a row, and of the bias's
+// gradient, a thread a column.  Workgroups in this order.
+struct CeFinish { uint32_t dh_groups, dw_groups; };                  // behind them the bias's
+template <typename T, typename W, class S>
+__global__ __launch_bounds__(CE_THREADS) void cross_entropy_finish_kernel(CeArgs a, T* dh, W* dweight, float* dbias, uint32_t from, uint32_t columns, CeFinish f) {
+    const uint32_t count = uniform(a.header->count), across = (a.width + WAVE * 8 - 1) / (WAVE * 8);
+    const float lower = RAISED<T> ? a.header->lower : 1.0f;
+    uint32_t group = blockIdx.x;
+    const bool is_dh = group < f.dh_groups;
+    if (is_dh || group < f.dh_groups + f.dw_groups) {
+        if (!is_dh) group -= f.dh_groups;
+        const Split split = is_dh ? dh_split<S>(a, count) : dw_split<S>(a, count, columns);
+        if (!is_dh && split.parts == 1) return;
+        const uint32_t rows = is_dh ? count : columns, c = (group % across * WAVE + threadIdx.x % WAVE) * 8, step = (is_dh ? f.dh_groups : f.dw_groups) / across;
+        if (c >= a.width) return;
+        for (uint32_t n = group / across * (CE_THREADS / WAVE) + threadIdx.x / WAVE; n < rows; n += step * (CE_THREADS / WAVE)) {
+            const f32x8 sum = lower * parts_of_row(is_dh ? a.dh_sums : a.dw_sums, (uint64_t)split.tiles_n * S::TILE_N * a.width_pad, split.parts, (uint64_t)n * a.width_pad + c);
+            if (is_dh) store_eight(dh + a.list[n] * a.dh_stride + c, sum);
+            else store_eight(dweight + (from + n) * a.dweight_stride + c, sum);
+        }
+        return;
+    }
+    const uint32_t v = (group - f.dh_groups - f.dw_groups) * CE_THREADS + threadIdx.x;
     if (v >= a.vocab) return;
-    const uint32_t parts = (a.header->count + S::TILE_N - 1) / S::TILE_N * S::WN;
+    const uint32_t parts = a.dbias_parts(count);
     float sum = 0.0f;
 #pragma unroll 8
     for (uint32_t p = 0; p < parts; ++p) sum += a.dbias_sums[(uint64_t)p * a.vocab_pad + v];
@@ -598,7 +609,7 @@ __global__ __launch_bounds__(CE_THREADS) void cross_entropy_dbias_kernel(CeArgs 
 
 struct CePlan {
     uint32_t rows_pad, width_pad, vocab_pad, piece;
-    bool small_logits, small_dh, small_dweight, split_dweight;
+    bool small_logits, small_products, narrow_products, split_dweight;
     uint64_t logit_groups, piece_groups, dh_groups, dweight_groups;
     size_t counts_at, list_at, label_at, h_at, lse_at, g_at;         // shared and backward
     size_t stats_at, said_at, forward_bytes;
@@ -628,21 +639,24 @@ static bool ce_plan(uint64_t rows, uint32_t width, uint32_t vocab, CePlan& p) {
     p.piece = (uint32_t)ce_up((p.vocab_pad + pieces - 1) / pieces, CE_PAD);
     const auto tiles = [](uint64_t n, bool small) { return (n + (small ? 127 : 255)) / (small ? 128 : 256); };
     p.small_logits = ce_small(vocab, some);
-    p.small_dh = ce_small_split(p.width_pad, some, p.piece);
-    p.small_dweight = ce_small_split(p.width_pad, p.piece, some);
+    p.small_products = ce_small_split(p.width_pad, some, p.piece) && ce_small_split(p.width_pad, p.piece, some);
     // workgroups of large tiles of logits stay on their CU; those of a die keep its tiles
     const uint64_t stay = ce_up(device_cus(), DIES), logit_tiles = tile_groups(tiles(vocab, p.small_logits) * tiles(some, p.small_logits)),
                    piece_tiles = tile_groups(tiles(p.piece, p.small_logits) * tiles(some, p.small_logits));
     if (logit_tiles > UINT32_MAX / 2) return false;
+    // few rows, for which dW is much to write and little to sum (10 x 256 x 100000: 108 -> 83 us, 100 x 4096 x 60000 628 -> 552; 45 x 1632 x 2982, with
+    // few tiles, would go from 42 to 50)
+    p.narrow_products = some <= CE_FINE_ROWS && tiles(p.width_pad, true) * tiles(p.piece, true) > 1024;
+    if (p.narrow_products) p.small_products = true;
     p.logit_groups = p.small_logits || logit_tiles < stay ? logit_tiles : stay;
     p.piece_groups = p.small_logits || piece_tiles < stay ? piece_tiles : stay;
-    const uint64_t dh_tiles = tiles(p.width_pad, p.small_dh) * tiles(some, p.small_dh), dw_tiles = tiles(p.width_pad, p.small_dweight) * tiles(p.piece, p.small_dweight);
-    const uint64_t fine_tiles = 2 * tiles(p.width_pad, p.small_dh) * tiles(some < CE_FINE_ROWS ? some : CE_FINE_ROWS, p.small_dh);
+    const uint64_t dh_tiles = tiles(p.width_pad, p.small_products) * tiles(some, p.small_products), dw_tiles = tiles(p.width_pad, p.small_products) * tiles(p.piece, p.small_products);
+    const uint64_t fine_tiles = 2 * tiles(p.width_pad, p.small_products) * tiles(some < CE_FINE_ROWS ? some : CE_FINE_ROWS, p.small_products);
     p.dh_groups = tile_groups(dh_tiles > CE_SPLIT_TILES ? dh_tiles : CE_SPLIT_TILES);
     if (p.dh_groups < fine_tiles) p.dh_groups = tile_groups(fine_tiles);
     p.dweight_groups = tile_groups(dw_tiles > CE_SPLIT_TILES ? dw_tiles : CE_SPLIT_TILES);
     // the last piece of the vocabulary, with fewer tiles, may be split where the others are not
-    const uint64_t least = tiles(p.width_pad, p.small_dweight) * tiles(pieces > 1 ? 1 : vocab, p.small_dweight);
+    const uint64_t least = tiles(p.width_pad, p.small_products) * tiles(pieces > 1 ? 1 : vocab, p.small_products);
     p.split_dweight = least <= CE_SPLIT_TILES && ce_parts((uint32_t)least, (uint32_t)((some + PRODUCT_K - 1) / PRODUCT_K)) > 1;
     for (const uint64_t groups : {p.logit_groups, p.piece_groups, p.dh_groups, p.dweight_groups})
         if (groups > LAUNCH_GROUPS / 2) return false;
@@ -668,8 +682,8 @@ static bool ce_plan(uint64_t rows, uint32_t width, uint32_t vocab, CePlan& p) {
     // sums of dh: all rows once, or the parts of fewer; those of dW where there are parts
     const auto parts = [](bool small) { return (uint64_t)CE_SPLIT_TILES * (small ? 128 * 128 : 256 * 256); };
     const uint64_t once = ((uint64_t)p.rows_pad + CE_FINE_ROWS) * p.width_pad;
-    p.dh_at = place(4 * (once > parts(p.small_dh) ? once : parts(p.small_dh)));
-    p.dw_at = place(p.split_dweight ? 4 * parts(p.small_dweight) : 0);
+    p.dh_at = place(4 * (once > parts(p.small_products) ? once : parts(p.small_products)));
+    p.dw_at = place(p.split_dweight ? 4 * parts(p.small_products) : 0);
     p.dbias_at = place(4ull * (p.rows_pad / 64) * p.vocab_pad);
     p.backward_bytes = at;
     return true;
@@ -741,50 +755,50 @@ static int ce_forward(const CeArgs& a, const CePlan& p, const void* weight, floa
 
 struct CeGradients { void *dh, *dweight; float* dbias; };
 
-template <typename T, class S>
-static int ce_dh(const CeArgs& a, const CePlan& p, const void* weight, uint32_t from, uint32_t columns, hipStream_t s) {
-    hipLaunchKernelGGL((cross_entropy_dh_kernel<T, S>), dim3((unsigned)p.dh_groups), dim3(S::THREADS), 0, s, a, (const T*)weight, from, columns);
-    return launch_status();
-}
-// A wave 512 columns of a row.
-static dim3 ce_join_grid(uint32_t rows, uint32_t width) { return dim3((rows + CE_THREADS / WAVE - 1) / (CE_THREADS / WAVE), (width + WAVE * 8 - 1) / (WAVE * 8)); }
-
 template <typename T, typename W, class S>
-static int ce_dweight_type(const CeArgs& a, const CePlan& p, W* dweight, uint32_t from, uint32_t columns, hipStream_t s) {
-    hipLaunchKernelGGL((cross_entropy_dweight_kernel<T, W, S>), dim3((unsigned)p.dweight_groups), dim3(S::THREADS), 0, s, a, dweight, from, columns);
-    if (const int status = launch_status()) return status;
+static int ce_products(const CeArgs& a, const CePlan& p, const void* weight, const CeGradients& g, uint32_t from, uint32_t columns, hipStream_t s) {
+    const uint32_t dh_groups = g.dh ? (uint32_t)p.dh_groups : 0, dw_groups = g.dweight ? (uint32_t)p.dweight_groups : 0;
+    // one launch where dh's tiles do not fill the chip by themselves (8192 x 4096 x 128000: two 19.8 ms, one 20.2; 22 x 752 x 112: two 31 us, one 25)
+    const auto launch = [&](uint32_t dh, uint32_t dw) {              // workgroups of each
+        if (dh + dw == 0) return (int)OKT_OK;
+        hipLaunchKernelGGL((cross_entropy_products_kernel<T, W, S>), dim3(dh + dw), dim3(S::THREADS), 0, s, a, (const T*)weight, (W*)g.dweight, from, columns, dh);
+        return launch_status();
+    };
+    const bool apart = dh_groups > CE_SPLIT_TILES;
+    if (const int status = launch(dh_groups, apart ? 0 : dw_groups)) return status;
+    if (apart)
+        if (const int status = launch(0, dw_groups)) return status;
+    const bool last = from + (uint64_t)columns >= a.vocab;
     const uint64_t tiles = (uint64_t)((a.width_pad + S::TILE_M - 1) / S::TILE_M) * ((columns + S::TILE_N - 1) / S::TILE_N);
-    if (!p.split_dweight || tiles * 2 > CE_SPLIT_TILES) return OKT_OK;
-    hipLaunchKernelGGL((cross_entropy_dweight_join_kernel<T, W, S>), ce_join_grid(columns, a.width), dim3(CE_THREADS), 0, s, a, dweight, from, columns);
+    const uint32_t across = (a.width + WAVE * 8 - 1) / (WAVE * 8);
+    const auto rows = [&](uint32_t n) {                              // workgroups of so many rows, at most 2^16 times `across`
+        const uint32_t blocks = (n + CE_THREADS / WAVE - 1) / (CE_THREADS / WAVE);
+        return (blocks < 1u << 16 ? blocks : 1u << 16) * across;
+    };
+    const CeFinish f = {g.dh && last ? rows(a.rows) : 0, g.dweight && p.split_dweight && tiles * 2 <= CE_SPLIT_TILES ? rows(columns) : 0};
+    const uint32_t bias = g.dbias && last ? (a.vocab + CE_THREADS - 1) / CE_THREADS : 0;
+    if (f.dh_groups + f.dw_groups + bias == 0) return OKT_OK;
+    hipLaunchKernelGGL((cross_entropy_finish_kernel<T, W, S>), dim3(f.dh_groups + f.dw_groups + bias), dim3(CE_THREADS), 0, s, a, (T*)g.dh, (W*)g.dweight, g.dbias, from, columns, f);
     return launch_status();
 }
-template <typename T, class S>
-static int ce_dweight(const CeArgs& a, const CePlan& p, void* dweight, bool wide, uint32_t from, uint32_t columns, hipStream_t s) {
-    return wide ? ce_dweight_type<T, float, S>(a, p, (float*)dweight, from, columns, s) : ce_dweight_type<T, T, S>(a, p, (T*)dweight, from, columns, s);
-}
 
-template <typename T, class S>
-static int ce_backward(const CeArgs& a, const CePlan& p, const void* weight, const CeGradients& g, bool wide, hipStream_t s) {
+template <typename T, typename W>
+static int ce_backward(CeArgs a, const CePlan& p, const void* weight, CeGradients g, hipStream_t s) {
+    if (a.rows == 0) g.dh = nullptr;
+    a.logit_tile_n = p.small_logits ? Small::TILE_N : Large::TILE_N;
+    a.logit_parts_n = p.small_logits ? Small::WN : Large::WN;
     for (uint64_t from = 0; from < a.vocab; from += p.piece) {
         const uint32_t first = (uint32_t)from, columns = a.vocab - first < p.piece ? a.vocab - first : p.piece;
+        const dim3 groups((unsigned)p.piece_groups);
         timing_before(s);
-        hipLaunchKernelGGL((cross_entropy_gradient_kernel<T, S>), dim3((unsigned)p.piece_groups), dim3(S::THREADS), 0, s, a, (const T*)weight, first, columns);
+        if (p.small_logits) hipLaunchKernelGGL((cross_entropy_gradient_kernel<T, Small>), groups, dim3(Small::THREADS), 0, s, a, (const T*)weight, first, columns);
+        else hipLaunchKernelGGL((cross_entropy_gradient_kernel<T, Large>), groups, dim3(Large::THREADS), 0, s, a, (const T*)weight, first, columns);
         timing_after(s);
         if (const int status = launch_status()) return status;
-        if (g.dh && a.rows)
-            if (const int status = p.small_dh ? ce_dh<T, Small>(a, p, weight, first, columns, s) : ce_dh<T, Large>(a, p, weight, first, columns, s)) return status;
-        if (g.dweight)
-            if (const int status = p.small_dweight ? ce_dweight<T, Small>(a, p, g.dweight, wide, first, columns, s) : ce_dweight<T, Large>(a, p, g.dweight, wide, first, columns, s))
-                return status;
+        const auto products = p.narrow_products ? ce_products<T, W, Narrow> : p.small_products ? ce_products<T, W, Small> : ce_products<T, W, Large>;
+        if (const int status = products(a, p, weight, g, first, columns, s)) return status;
     }
-    if (g.dh && a.rows) {
-        const dim3 rows = ce_join_grid(a.rows, a.width);
-        if (p.small_dh) hipLaunchKernelGGL((cross_entropy_dh_join_kernel<T, Small>), rows, dim3(CE_THREADS), 0, s, a, (T*)g.dh);
-        else hipLaunchKernelGGL((cross_entropy_dh_join_kernel<T, Large>), rows, dim3(CE_THREADS), 0, s, a, (T*)g.dh);
-        if (const int status = launch_status()) return status;
-    }
-    if (g.dbias) hipLaunchKernelGGL(cross_entropy_dbias_kernel<S>, dim3((a.vocab + CE_THREADS - 1) / CE_THREADS), dim3(CE_THREADS), 0, s, a, g.dbias);
-    return launch_status();
+    return OKT_OK;
 }
 
 template <typename T>
@@ -796,7 +810,7 @@ template <typename T>
 static int ce_run_backward(const CeArgs& a, const CePlan& p, const void* h, const void* weight, const float* lse, const float* dloss, const CeGradients& g, bool wide,
                            hipStream_t s) {
     if (const int status = ce_listed<T>(a, h, nullptr, lse, nullptr, dloss, g.dh, s)) return status;
-    return p.small_logits ? ce_backward<T, Small>(a, p, weight, g, wide, s) : ce_backward<T, Large>(a, p, weight, g, wide, s);
+    return wide ? ce_backward<T, float>(a, p, weight, g, s) : ce_backward<T, T>(a, p, weight, g, s);
 }
 
 }  // namespace okt

@@ -129,7 +129,7 @@ __device__ __forceinline__ void handed_over() {
 // between products, half of a piece's in that step and half in the next one (8192 x 128000 x 4096: 6.5 ms; all together, which holds the wave
 // up for a thousand cycles, 7.2; all in the last step 6.7, over three steps 6.6).  Two waves a SIMD, 128 x 64 each: one of 128 x 128
 // reads a quarter less from LDS and takes 6.7.
-template <typename T, class S, class A, class B>
+template <typename T, class S, class A, class B, bool AGAIN = false>
 struct Product {
     static constexpr uint32_t BUFFER = A::BYTES + B::BYTES;
     static constexpr int LOADS = A::LOADS + B::LOADS, LEFT = (S::STAGES - 2) * LOADS;
@@ -139,6 +139,8 @@ struct Product {
     uint32_t k, at;
     i32x4 buffer_a, buffer_b;
     uint32_t ahead, there;                                           // k before the piece that is fetched, and in and behind it
+    OperandSource again_a, again_b;                                  // AGAIN: where both sides go on from k = again on
+    uint32_t again = 0;                                              // (0: they do not)
 
     __device__ __forceinline__ void fetch(int i, uint32_t to) const {
         if (i < A::LOADS) a.fetch(i, at + to, buffer_a, there);
@@ -146,6 +148,10 @@ struct Product {
     }
     __device__ __forceinline__ void next_piece() {
         there = ahead < k ? k - ahead : 0;
+        if (AGAIN && again && ahead == again) {
+            a.from = again_a;
+            b.from = again_b;
+        }
         buffer_a = a.from.buffer();
         buffer_b = b.from.buffer();
         if (there == 0) buffer_a[2] = buffer_b[2] = 0;               // past the end nothing is read
@@ -153,7 +159,7 @@ struct Product {
         b.advance();
         ahead += PRODUCT_K;
     }
-    __device__ __forceinline__ Product(const A& a_, const B& b_, uint32_t k_, const char* lds) : a(a_), b(b_), k(k_), at(lds_address(lds)) {}
+    __device__ __forceinline__ Product(const A& a_, const B& b_, uint32_t k_, const char* lds) : a(a_), b(b_), k(uniform(k_)), at(lds_address(lds)) {}
 
     __device__ __forceinline__ void begin() {
         ahead = 0;
