@@ -984,6 +984,29 @@ def _each(value, count, name):
     return value
 
 
+def _adamw_refuse(params, grads, ms, vs, m_scales, v_scales, copies, lengths, blocks, state_type, device):
+    """Says which tensor is not what a plan needs."""
+    torch = _TORCH
+    for i, (n, b) in enumerate(zip(lengths, blocks)):
+        parts = [(params[i], None, "params", n), (grads[i], None, "grads", n), (ms[i], state_type, "ms", n), (vs[i], state_type, "vs", n)]
+        if m_scales is not None:
+            parts += [(m_scales[i], torch.float32, "m_scales", b), (v_scales[i], torch.float32, "v_scales", b)]
+        if copies is not None and copies[i] is not None:
+            parts.append((copies[i], None, "copies", n))
+        for t, dtype, name, numel in parts:
+            if not isinstance(t, torch.Tensor):
+                raise TypeError(f"{name}[{i}] is required")
+            if dtype is None:
+                _dtype_code(t, f"{name}[{i}]")
+            _ptr(t, dtype or t.dtype, f"{name}[{i}]")
+            if t.numel() != numel:
+                raise ValueError(f"{name}[{i}] needs {numel} elements, got {t.numel()}")
+            if t.device != device:
+                raise ValueError(f"{name}[{i}] must be on {device}, got {t.device}")
+            if name == "copies" and t.dtype is torch.float32:
+                raise TypeError(f"copies[{i}] must be bfloat16 or float16")
+
+
 def okt_adamw_plan(params, grads, ms, vs, *, m_scales=None, v_scales=None, copies=None, weight_decay=0.0,
                    rate_scale=1.0) -> AdamWPlan:
     """The plan of okt_adamw_step over lists of tensors, which are contiguous and on one device: params and grads float32,
@@ -1009,32 +1032,35 @@ def okt_adamw_plan(params, grads, ms, vs, *, m_scales=None, v_scales=None, copie
     if eight != (m_scales is not None) or eight != (v_scales is not None):
         raise TypeError("m_scales and v_scales belong to averages in float8_e4m3fn, both of them")
     decays, rates = _each(weight_decay, count, "weight_decay"), _each(rate_scale, count, "rate_scale")
-    device, packed, held = params[0].device, [], []
-    for i in range(count):
-        p, g, c = params[i], grads[i], None if copies is None else copies[i]
-        n = p.numel()
-        parts = [(p, None, "params", n), (g, None, "grads", n), (ms[i], state_type, "ms", n), (vs[i], state_type, "vs", n)]
-        if c is not None:
-            parts.append((c, None, "copies", n))
-        if eight:
-            parts += [(m_scales[i], torch.float32, "m_scales", -(-n // ADAMW_BLOCK)), (v_scales[i], torch.float32, "v_scales", -(-n // ADAMW_BLOCK))]
-        for t, dtype, name, numel in parts:
-            if t is None:
-                raise TypeError(f"{name}[{i}] is required")
-            if dtype is None:
-                _dtype_code(t, f"{name}[{i}]")
-            _ptr(t, dtype or t.dtype, f"{name}[{i}]")
-            if t.numel() != numel:
-                raise ValueError(f"{name}[{i}] needs {numel} elements, got {t.numel()}")
-            if t.device != device:
-                raise ValueError(f"{name}[{i}] must be on {device}, got {t.device}")
-            held.append(t)
-        if c is not None and c.dtype is torch.float32:
-            raise TypeError(f"copies[{i}] must be bfloat16 or float16")
-        packed.append(_ADAMW_TENSOR.pack(
-            p.data_ptr(), g.data_ptr(), ms[i].data_ptr(), vs[i].data_ptr(), 0 if c is None else c.data_ptr(),
-            m_scales[i].data_ptr() if eight else 0, v_scales[i].data_ptr() if eight else 0, n, decays[i], rates[i],
-            _DTYPES[p.dtype], _DTYPES[g.dtype], 1 if c is None else _DTYPES[c.dtype], 0))
+    device, held = params[0].device, [*params, *grads, *ms, *vs]
+    scales = [*m_scales, *v_scales] if eight else []
+    held += scales
+    held += [c for c in copies or () if c is not None]
+    lengths = [p.numel() if isinstance(p, torch.Tensor) else 0 for p in params]
+    blocks = [-(-n // ADAMW_BLOCK) for n in lengths]
+
+    def fine(tensors, types, numels):
+        """The usual outcome, decided by comparisons alone."""
+        return all(type(t) is torch.Tensor and t.device == device and t.is_contiguous() for t in tensors) and device.type == "cuda" and (
+            {t.dtype for t in tensors} <= types and [t.numel() for t in tensors] == numels)
+
+    floats, one = {torch.float32, torch.bfloat16, torch.float16}, {state_type}
+    whole = all(fine(x, t, n) for x, t, n in ((params, floats, lengths), (grads, floats, lengths), (ms, one, lengths), (vs, one, lengths)))
+    whole = whole and (not eight or all(fine(x, {torch.float32}, blocks) for x in (m_scales, v_scales)))
+    there = [] if copies is None else [(c, n) for c, n in zip(copies, lengths) if c is not None]
+    whole = whole and fine([c for c, _ in there], floats - {torch.float32}, [n for _, n in there])
+    if not whole:
+        _adamw_refuse(params, grads, ms, vs, m_scales, v_scales, copies, lengths, blocks, state_type, device)
+    _dtype_code(params[0], "params[0]")
+
+    def places(tensors):
+        return [0] * count if tensors is None else [0 if t is None else t.data_ptr() for t in tensors]
+
+    codes = lambda tensors: [_DTYPES[t.dtype] for t in tensors]  # noqa: E731
+    copy_codes = [1] * count if copies is None else [1 if c is None else _DTYPES[c.dtype] for c in copies]
+    packed = [_ADAMW_TENSOR.pack(*row, 0) for row in zip(
+        places(params), places(grads), places(ms), places(vs), places(copies), places(m_scales), places(v_scales), lengths, decays, rates,
+        codes(params), codes(grads), copy_codes)]
     table, lib = b"".join(packed), load_library()
     nbytes = lib.okt_adamw_plan_bytes(table, count)
     host, chunks = torch.empty(max(nbytes, 256), dtype=torch.uint8), c_u32(0)

@@ -223,3 +223,26 @@ def test_replayed_and_on_another_stream():
         stream.synchronize()
         for a, b in zip(one.buffers(), two.buffers()):
             assert torch.equal(a.view(torch.uint8), b.view(torch.uint8)), n
+
+
+def test_plans_that_are_refused():
+    s = State([100, 300], eight=True, copy="bf16", seed=9)
+    good = dict(m_scales=s.m_scale, v_scales=s.v_scale, copies=s.copies)
+    okt.okt_adamw_plan(s.p, s.g, s.m, s.v, **good)
+    okt.okt_adamw_plan(s.p, s.g, s.m, s.v, **{**good, "copies": [None, s.copies[1]]})
+    cpu = s.p[1].cpu()
+    for error, match, change in (
+            (TypeError, r"params\[1\] must be a CUDA", {"p": [s.p[0], cpu]}), (ValueError, r"grads\[1\] needs 300", {"g": [s.g[0], s.g[0]]}),
+            (TypeError, r"grads\[0\] must be float32, bfloat16 or float16", {"g": [s.g[0].double(), s.g[1]]}),
+            (TypeError, r"ms\[1\] must have dtype", {"m": [s.m[0], s.p[1]]}), (TypeError, r"vs\[0\] is required", {"v": [None, s.v[1]]}),
+            (TypeError, r"params\[1\] must be contiguous", {"p": [s.p[0], s.p_all[::2][:300]]}),
+            (ValueError, r"m_scales\[1\] needs 2", {"m_scales": [s.m_scale[0], s.m_scale[0]]}),
+            (TypeError, r"copies\[0\] must be bfloat16 or float16", {"copies": [s.p[0].clone(), None]}),
+            (okt.OktError, "okt_adamw_plan failed", {"p": [s.p[0], s.p_all[:300]]})):
+        a = {"p": s.p, "g": s.g, "m": s.m, "v": s.v, **good, **change}
+        with pytest.raises(error, match=match):
+            okt.okt_adamw_plan(a["p"], a["g"], a["m"], a["v"], m_scales=a["m_scales"], v_scales=a["v_scales"], copies=a["copies"])
+    with pytest.raises(TypeError, match="step is required"):
+        okt.okt_adamw_step(s.plan(), None, lr=0.1)
+    with pytest.raises(TypeError, match="CUDA"):
+        okt.okt_adamw_step(s.plan(), torch.ones(1, dtype=torch.int64), lr=0.1)
