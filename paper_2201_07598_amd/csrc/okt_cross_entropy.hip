@@ -640,16 +640,13 @@ static bool ce_plan(uint64_t rows, uint32_t width, uint32_t vocab, CePlan& p) {
     const auto tiles = [](uint64_t n, bool small) { return (n + (small ? 127 : 255)) / (small ? 128 : 256); };
     p.small_logits = ce_small(vocab, some);
     p.small_products = ce_small_split(p.width_pad, some, p.piece) && ce_small_split(p.width_pad, p.piece, some);
-    // workgroups of large tiles of logits stay on their CU; those of a die keep its tiles
-    const uint64_t stay = ce_up(device_cus(), DIES), logit_tiles = tile_groups(tiles(vocab, p.small_logits) * tiles(some, p.small_logits)),
-                   piece_tiles = tile_groups(tiles(p.piece, p.small_logits) * tiles(some, p.small_logits));
-    if (logit_tiles > UINT32_MAX / 2) return false;
+    p.logit_groups = tile_groups(tiles(vocab, p.small_logits) * tiles(some, p.small_logits));
+    p.piece_groups = tile_groups(tiles(p.piece, p.small_logits) * tiles(some, p.small_logits));
+    if (p.logit_groups > UINT32_MAX / 2) return false;
     // few rows, for which dW is much to write and little to sum (10 x 256 x 100000: 108 -> 83 us, 100 x 4096 x 60000 628 -> 552; 45 x 1632 x 2982, with
     // few tiles, would go from 42 to 50)
     p.narrow_products = some <= CE_FINE_ROWS && tiles(p.width_pad, true) * tiles(p.piece, true) > 1024;
     if (p.narrow_products) p.small_products = true;
-    p.logit_groups = p.small_logits || logit_tiles < stay ? logit_tiles : stay;
-    p.piece_groups = p.small_logits || piece_tiles < stay ? piece_tiles : stay;
     const uint64_t dh_tiles = tiles(p.width_pad, p.small_products) * tiles(some, p.small_products), dw_tiles = tiles(p.width_pad, p.small_products) * tiles(p.piece, p.small_products);
     const uint64_t fine_tiles = 2 * tiles(p.width_pad, p.small_products) * tiles(some < CE_FINE_ROWS ? some : CE_FINE_ROWS, p.small_products);
     p.dh_groups = tile_groups(dh_tiles > CE_SPLIT_TILES ? dh_tiles : CE_SPLIT_TILES);
@@ -658,7 +655,7 @@ static bool ce_plan(uint64_t rows, uint32_t width, uint32_t vocab, CePlan& p) {
     // the last piece of the vocabulary, with fewer tiles, may be split where the others are not
     const uint64_t least = tiles(p.width_pad, p.small_products) * tiles(pieces > 1 ? 1 : vocab, p.small_products);
     p.split_dweight = least <= CE_SPLIT_TILES && ce_parts((uint32_t)least, (uint32_t)((some + PRODUCT_K - 1) / PRODUCT_K)) > 1;
-    for (const uint64_t groups : {p.logit_groups, p.piece_groups, p.dh_groups, p.dweight_groups})
+    for (const uint64_t groups : {p.small_logits ? p.logit_groups : 0, p.dh_groups, p.dweight_groups})
         if (groups > LAUNCH_GROUPS / 2) return false;
     size_t at = 256;
     const auto place = [&](size_t bytes) {
@@ -743,10 +740,16 @@ static int ce_listed(const CeArgs& a, const void* h, float* loss, const float* l
     return launch_status();
 }
 
+// Workgroups of so many tiles of logits: large ones stay on their CU, those of a die with its tiles.
+static unsigned ce_logit_groups(const CePlan& p, uint64_t tiles) {
+    const uint64_t stay = ce_up(device_cus(), DIES);
+    return (unsigned)(p.small_logits || tiles < stay ? tiles : stay);
+}
+
 template <typename T, class S>
 static int ce_forward(const CeArgs& a, const CePlan& p, const void* weight, float* loss, float* lse, hipStream_t s) {
     timing_before(s);
-    hipLaunchKernelGGL((cross_entropy_forward_kernel<T, S>), dim3((unsigned)p.logit_groups), dim3(S::THREADS), 0, s, a, (const T*)weight);
+    hipLaunchKernelGGL((cross_entropy_forward_kernel<T, S>), dim3(ce_logit_groups(p, p.logit_groups)), dim3(S::THREADS), 0, s, a, (const T*)weight);
     timing_after(s);
     if (const int status = launch_status()) return status;
     hipLaunchKernelGGL(cross_entropy_join_kernel, dim3((a.rows + 15) / 16), dim3(CE_JOIN_THREADS), 0, s, a, (a.vocab + S::TILE_M - 1) / S::TILE_M * S::WM, loss, lse);
@@ -789,7 +792,7 @@ static int ce_backward(CeArgs a, const CePlan& p, const void* weight, CeGradient
     a.logit_parts_n = p.small_logits ? Small::WN : Large::WN;
     for (uint64_t from = 0; from < a.vocab; from += p.piece) {
         const uint32_t first = (uint32_t)from, columns = a.vocab - first < p.piece ? a.vocab - first : p.piece;
-        const dim3 groups((unsigned)p.piece_groups);
+        const dim3 groups(ce_logit_groups(p, p.piece_groups));
         timing_before(s);
         if (p.small_logits) hipLaunchKernelGGL((cross_entropy_gradient_kernel<T, Small>), groups, dim3(Small::THREADS), 0, s, a, (const T*)weight, first, columns);
         else hipLaunchKernelGGL((cross_entropy_gradient_kernel<T, Large>), groups, dim3(Large::THREADS), 0, s, a, (const T*)weight, first, columns);
