@@ -448,7 +448,7 @@ static bool rot_args(const okt_norm_rotary* op, RotArgs& a) {
         a.axis_of_pair[j] = op->axis_of_pair[j];
     }
     a.tokens = op->batch * op->length;
-    a.length = divider(op->length);
+    a.length = divider(a.tokens ? op->length : 1);                   // a length without a batch may be any
     a.dim = op->head_dim;
     a.share = 1.0f / (float)op->head_dim;
     a.pair_shift = 2;

@@ -122,6 +122,14 @@ def test_rotary_refusals():
     assert okt.okt_norm_rotary_workspace_bytes(8, 4096, 16, 4, 128) == 1024 * 2 * 128 * 4
 
 
+@pytest.mark.timeout(30)
+def test_rotary_without_a_batch_takes_any_length():
+    lib = okt.load_library()
+    for sizes in ({"batch": 0, "length": (1 << 32) - 1}, {"batch": (1 << 32) - 1, "length": 0}):
+        assert lib.okt_norm_rotary_forward(rotary_struct(**sizes), *AT[:4], None) == OK
+        assert okt.okt_norm_rotary_workspace_bytes(sizes["batch"], sizes["length"], 8, 8, 64) == 256
+
+
 # ------------------------------------------------------------------ AdamW
 
 TENSOR = dict(p=AT[0], g=AT[1], m=AT[2], v=AT[3], copy=0, ms=0, vs=0, n=1000, decay=0.0, rate=1.0, pt=0, gt=0, ct=1)
