@@ -596,6 +596,7 @@ int okt_norm_rotary_backward(const okt_norm_rotary* op, const void* d_q, const v
         if ((a.t[n].weight && !p.x[n]) || !p.d[n] || !p.out[n] || !aligned(p.x[n], e) || !aligned(p.d[n], e) || !aligned(p.out[n], e) ||
             shares_places(a, a.t[n].out, a.t[n].heads)) return OKT_ERR_INVALID_ARG;
     }
+    if (g.to[0] && g.to[1] && overlap(g.to[0], 4ull * a.dim, g.to[1], 4ull * a.dim)) return OKT_ERR_INVALID_ARG;
     const bool sums = g.to[0] || g.to[1];
     if (a.tokens) {
         if (clash(a, out[0], out[1], e)) return OKT_ERR_INVALID_ARG;

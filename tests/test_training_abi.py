@@ -122,6 +122,13 @@ def test_rotary_refusals():
     assert okt.okt_norm_rotary_workspace_bytes(8, 4096, 16, 4, 128) == 1024 * 2 * 128 * 4
 
 
+def test_rotary_weights_gradients_are_apart():
+    struct = rotary_struct(q_weight=AT[11], k_weight=AT[11])
+    for to in (AT[7], AT[7] + 4 * 63):
+        args = (struct, *AT[:6], AT[7], to, AT[9], 1 << 30, None)
+        assert okt.load_library().okt_norm_rotary_backward(*args) == INVALID
+
+
 @pytest.mark.timeout(30)
 def test_rotary_without_a_batch_takes_any_length():
     lib = okt.load_library()
