@@ -1,5 +1,5 @@
 """Plain CPU oracle of the operators at the ends of a training step, in 64 bits, written from the formulas in
-include/okt.h: AdamW and its 8-bit averages.  numpy only, no thought of speed; shares
+include/okt.h: AdamW and its 8-bit averages, norms and rotation of heads, cross entropy over a vocabulary.  numpy only, no thought of speed; shares
 nothing with the GPU path."""
 from __future__ import annotations
 
