@@ -3,17 +3,24 @@
 //   loss_n = lse_n - s_ny,  lse_n = log sum_v exp s_nv,    d_nv = g_n (exp(s_nv - lse_n) - [v = y_n])
 //   dh = d W,  dW = d' h,  db_v = sum_n d_nv
 //
-// Rows without a label take no part: the others' numbers are listed first, their h copied side by side (and
-// padded to whole tiles with zeros), and every later kernel works on the list, whose length it reads from device memory.  With 15 % of the
-// rows labelled that is 15 % of the work.
+// Rows without a label take no part: the others' numbers are listed first, their h copied side by side (and padded to whole tiles
+// with zeros), and every later kernel works on the list, whose length it reads from device memory.  With 15 % of the rows labelled
+// that is 15 % of the work.
 //
 // Forward, a tile of logits is a matrix product whose epilogue leaves the largest and the sum of exponentials of its part of a row; a
 // second kernel joins a row's parts.  Backward the logits are made again, a piece of the vocabulary at a time, and leave the
 // epilogue as d, rounded to the tensors' type, in the workspace; two more products take it from there.  dW of a piece is final; dh
 // is summed over the pieces in fp32.  Four products where a kept matrix of logits would need three.
 //
-// In fp16 d is taken times a power of two that brings the largest |g| to between 2^14 and 2^15, and divided out of the sums: g is one over the number of rows
-// and p one over the vocabulary's size, and fp16 ends at 2^-24.
+// d is taken times a factor that makes the largest |g| a power of two, and the sums times its reciprocal: the gradient of a mean is one
+// number for all rows, and its rounding, the same in every entry, would be an error of the whole result (the largest entry of a row is
+// the label's, g (p - 1), and p - 1 itself loses nothing where p is small).  In fp16 that power is 2^15: g is one
+// over the number of rows and p one over the vocabulary's size, and fp16 ends at 2^-24.
+//
+// The matrix units bound the large sizes, at the clock that their power leaves: 8192 rows x 4096 x 128000 bf16 take FORWARD_LONG forward
+// and GRAD_LONG backward.  15 % of 16384 rows x 1024 x 30522: FORWARD_MASKED
+// and GRAD_MASKED, of which the launches before and behind the products are 29 us of the former.  One row to a few hundred: W's
+// way from memory, and three launches.
 #include <math.h>
 
 #include "okt_product.h"
@@ -33,9 +40,6 @@ constexpr float LOG2E = 1.44269504088896340736f;
 typedef ProductShape<4, 2, 2, 4, 2> Large;                           // 256 x 256, one workgroup of eight waves a CU
 typedef ProductShape<2, 2, 2, 2, 2> Narrow;                          // 128 x 128, two workgroups a CU: many tiles of a short sum
 typedef ProductShape<2, 2, 2, 2, 3> Small;                           // 128 x 128, four waves and two pieces on their way
-
-template <typename T> constexpr bool RAISED = false;
-template <> constexpr bool RAISED<_Float16> = true;
 
 struct CeHeader { uint32_t count; float raise, lower; uint32_t pad; };
 
@@ -114,15 +118,15 @@ __global__ __launch_bounds__(CE_THREADS) void cross_entropy_count_kernel(CeArgs 
 // Eight rows a workgroup: those with a label go side by side into the workspace, behind all labelled ones before them; the others
 // get their zeros.  Zeros fill the last tile, too.
 template <typename T>
-__global__ __launch_bounds__(CE_THREADS) void cross_entropy_gather_kernel(CeArgs a, const T* h, float* loss, const float* lse_in, float* lse_out, const float* dloss, T* dh) {
+__global__ __launch_bounds__(CE_THREADS) void cross_entropy_gather_kernel(CeArgs a, const T* h, float* loss, const float* lse_in, float* lse_out,
+                                                                              const float* dloss, T* dh) {
     typedef typename Eight<T>::vec vec;
     __shared__ CeCount waves[CE_THREADS / WAVE];
     const uint64_t first = (uint64_t)blockIdx.x * CE_GATHERED;
     const uint32_t lane = threadIdx.x % WAVE, wave = uniform(threadIdx.x / WAVE);
     CeCount c = {0, 0, 0.0f};
-    const float* g = RAISED<T> ? dloss : nullptr;
     if (a.rows <= CE_DIRECT) {
-        for (uint32_t r = threadIdx.x; r < a.rows; r += CE_THREADS) add_to(c, count_row(a, g, r, first));
+        for (uint32_t r = threadIdx.x; r < a.rows; r += CE_THREADS) add_to(c, count_row(a, dloss, r, first));
     } else {
         const uint64_t block = first / CE_BLOCK;
         for (uint64_t b = threadIdx.x; b * CE_BLOCK < a.rows; b += CE_THREADS) {
@@ -134,11 +138,11 @@ __global__ __launch_bounds__(CE_THREADS) void cross_entropy_gather_kernel(CeArgs
     }
     c = count_together(c, waves);
     if (blockIdx.x == 0 && threadIdx.x == 0) {
-        int e = 0;                                                   // top in [2^(e - 1), 2^e)
-        const bool use = RAISED<T> && c.top > 0.0f && c.top < __builtin_inff();
-        if (use) frexpf(c.top, &e);
-        const int by = use ? min(max(15 - e, -120), 120) : 0;
-        *a.header = {c.all, ldexpf(1.0f, by), ldexpf(1.0f, -by), 0};
+        int e = 0;                                                   // top = half 2^(e - 1), half in [1, 2)
+        const bool use = c.top > 0.0f && c.top < __builtin_inff();
+        const float half = use ? 2.0f * frexpf(c.top, &e) : 1.0f;
+        const int by = use && __is_same(T, _Float16) ? min(16 - e, 120) : 0;
+        *a.header = {c.all, ldexpf(1.0f / half, by), ldexpf(half, -by), 0};
     }
     // the labels at once; a wave takes two rows, whose vectors are on their way together
     const bool inside = lane < CE_GATHERED && first + lane < a.rows;
@@ -245,10 +249,11 @@ struct RowFacts {
     }
 };
 
-// Tiles of logits.  Where a workgroup has a CU for itself it stays, and the next tile's first operands are on their way while this one's logits are
-// worked on (2458 rows x 1024 x 30522: 164 -> 157 us; small tiles, of which there are few, gain nothing and lose 1.4 us).  `finish` is called with the tile's sums, its place, its bias and its rows' facts.
+// Where a workgroup has a CU for itself it stays, and the next tile's first operands are on their way while this one's logits are
+// worked on (2458 rows x 1024 x 30522: 164 -> 157 us; small tiles, of which there are few, gain nothing and lose 1.4 us).
 template <class S> constexpr bool STAYS = S::WAVES == 8;
 
+// Tiles of logits; `finish` is called with a tile's sums, its place, its bias and its rows' facts.
 template <typename T, class S, bool BACKWARD, class F>
 __device__ __forceinline__ void logit_tiles(const CeArgs& a, const T* weight, uint32_t from, uint32_t columns, const F& finish) {
     __shared__ __attribute__((aligned(1024))) char lds[S::BYTES];
@@ -283,7 +288,8 @@ __device__ __forceinline__ void logit_tiles(const CeArgs& a, const T* weight, ui
 
 template <typename T, class S>
 __global__ __launch_bounds__(S::THREADS) void cross_entropy_forward_kernel(CeArgs a, const T* weight) {
-    logit_tiles<T, S, false>(a, weight, 0, a.vocab, [&](const f32x16 (&c)[S::MT][S::NT], uint32_t v0, uint32_t part_n, const float* bias, const RowFacts<S>& facts, uint32_t count) {
+    logit_tiles<T, S, false>(a, weight, 0, a.vocab, [&](const f32x16 (&c)[S::MT][S::NT], uint32_t v0, uint32_t part_n, const float* bias,
+                                                        const RowFacts<S>& facts, uint32_t count) {
         const uint32_t lane = threadIdx.x % WAVE, part = v0 / (S::MT * 32);
         const bool biased = a.bias || v0 + S::MT * 32 > a.vocab;
 #pragma unroll
@@ -382,8 +388,9 @@ __device__ __forceinline__ void sums_over_lanes(float (&v)[N]) {
 // d of a piece of the vocabulary that begins at `from`.
 template <typename T, class S>
 __global__ __launch_bounds__(S::THREADS) void cross_entropy_gradient_kernel(CeArgs a, const T* weight, uint32_t from, uint32_t columns) {
-    const float raise = RAISED<T> ? a.header->raise : 1.0f;
-    logit_tiles<T, S, true>(a, weight, from, columns, [&](const f32x16 (&c)[S::MT][S::NT], uint32_t at, uint32_t part_n, const float* bias, const RowFacts<S>& facts, uint32_t count) {
+    const float raise = a.header->raise;
+    logit_tiles<T, S, true>(a, weight, from, columns, [&](const f32x16 (&c)[S::MT][S::NT], uint32_t at, uint32_t part_n, const float* bias,
+                                                          const RowFacts<S>& facts, uint32_t count) {
         const bool fine = count <= CE_FINE_ROWS;
         const uint32_t lane = threadIdx.x % WAVE, v0 = from + at;
         const bool biased = a.bias || v0 + S::MT * 32 > a.vocab;
@@ -394,7 +401,7 @@ __global__ __launch_bounds__(S::THREADS) void cross_entropy_gradient_kernel(CeAr
         for (int n = 0; n < S::NT; ++n) {
             const uint32_t row = part_n * (S::NT * 32) + n * 32 + lane % 32;
             const bool there = row < count;
-            const float g = facts.g[n], base = -facts.lse[n] * LOG2E;
+            const float g = facts.g[n] * raise, base = -facts.lse[n] * LOG2E;
             const uint32_t mine = facts.label[n] - v0 - lane / 32 * 16;
             float s[S::MT * 16];
             logits_of_row<S>(s, c, n, bias, biased);
@@ -414,7 +421,7 @@ __global__ __launch_bounds__(S::THREADS) void cross_entropy_gradient_kernel(CeAr
                 for (int r = 0; r < 16; ++r) {
                     const float d = there ? s[m * 16 + r] * g : 0.0f;        // rows behind the last one: zeros, whatever the bias is
                     sums[m * 16 + r] += d;
-                    (r < 8 ? low : high)[r % 8] = RAISED<T> ? d * raise : d;
+                    (r < 8 ? low : high)[r % 8] = d;
                 }
                 store_eight(to + m * 32, low);
                 store_eight(to + m * 32 + 8, high);
@@ -501,7 +508,8 @@ __device__ __forceinline__ void dh_tile(const CeArgs& a, const T* weight, uint32
     const T *d = rest ? (const T*)a.d_rest : (const T*)a.d, *end = d + (uint64_t)(rest ? CE_FINE_ROWS : a.rows_pad) * a.piece;
     f32x16 c[S::MT][S::NT];
     clear<S>(c);
-    Product<T, S, A, B> p(A(weight + (from + k0) * a.weight_stride + col, weight + (a.vocab - 1) * a.weight_stride + a.width, a.weight_stride * 2, a.width - min(a.width, col)),
+    Product<T, S, A, B> p(A(weight + (from + k0) * a.weight_stride + col, weight + (a.vocab - 1) * a.weight_stride + a.width, a.weight_stride * 2,
+                            a.width - min(a.width, col)),
                           B(d + (uint64_t)row * a.piece + k0, end, a.piece * 2), k1 - k0, lds);
     p.begin();
     p.run(c, lds);
@@ -529,12 +537,14 @@ __device__ __forceinline__ void dweight_tile(const CeArgs& a, W* dweight, uint32
     const T* h = (const T*)a.h;
     typedef Transposed<T, S::TILE_M, S::WAVES, true> A;
     typedef Transposed<T, S::TILE_N, S::WAVES, false> B;
-    const auto rows_of = [&](uint32_t k) { return A(h + (uint64_t)k * a.width_pad + col, h + (uint64_t)a.rows_pad * a.width_pad, a.width_pad * 2, a.width_pad - min(a.width_pad, col)); };
-    const auto d_of = [&](const void* d, uint32_t rows) { return B((const T*)d + (uint64_t)k0 * a.piece + v, (const T*)d + (uint64_t)rows * a.piece, (uint64_t)a.piece * 2, a.piece - v); };
+    const A rows_of_h(h + (uint64_t)k0 * a.width_pad + col, h + (uint64_t)a.rows_pad * a.width_pad, a.width_pad * 2, a.width_pad - min(a.width_pad, col));
+    const auto d_of = [&](const void* d, uint32_t rows) {
+        return B((const T*)d + (uint64_t)k0 * a.piece + v, (const T*)d + (uint64_t)rows * a.piece, (uint64_t)a.piece * 2, a.piece - v);
+    };
     f32x16 c[S::MT][S::NT];
     clear<S>(c);
     const bool fine = count <= CE_FINE_ROWS;                         // then d's rest stands behind d, beside the same rows again
-    Product<T, S, A, B, true> p(rows_of(k0), d_of(a.d, a.rows_pad), (k1 - k0) * (fine ? 2 : 1), lds);
+    Product<T, S, A, B, true> p(rows_of_h, d_of(a.d, a.rows_pad), (k1 - k0) * (fine ? 2 : 1), lds);
     if (fine) {
         p.again = k1 - k0;
         p.again_a = p.a.from;
@@ -547,7 +557,7 @@ __device__ __forceinline__ void dweight_tile(const CeArgs& a, W* dweight, uint32
         store_sums<S>(a.dw_sums + (uint64_t)part * split.tiles_n * S::TILE_N * a.width_pad, a.width_pad, c, m0, n0, columns, true);
         return;
     }
-    const float lower = RAISED<T> ? a.header->lower : 1.0f;
+    const float lower = a.header->lower;
 #pragma unroll
     for (int n = 0; n < S::NT; ++n) {
         if (n0 + n * 32 >= columns) continue;
@@ -580,17 +590,19 @@ struct CeFinish { uint32_t dh_groups, dw_groups; };                  // behind t
 template <typename T, typename W, class S>
 __global__ __launch_bounds__(CE_THREADS) void cross_entropy_finish_kernel(CeArgs a, T* dh, W* dweight, float* dbias, uint32_t from, uint32_t columns, CeFinish f) {
     const uint32_t count = uniform(a.header->count), across = (a.width + WAVE * 8 - 1) / (WAVE * 8);
-    const float lower = RAISED<T> ? a.header->lower : 1.0f;
+    const float lower = a.header->lower;
     uint32_t group = blockIdx.x;
     const bool is_dh = group < f.dh_groups;
     if (is_dh || group < f.dh_groups + f.dw_groups) {
         if (!is_dh) group -= f.dh_groups;
         const Split split = is_dh ? dh_split<S>(a, count) : dw_split<S>(a, count, columns);
         if (!is_dh && split.parts == 1) return;
-        const uint32_t rows = is_dh ? count : columns, c = (group % across * WAVE + threadIdx.x % WAVE) * 8, step = (is_dh ? f.dh_groups : f.dw_groups) / across;
+        const uint32_t rows = is_dh ? count : columns, c = (group % across * WAVE + threadIdx.x % WAVE) * 8;
+        const uint32_t step = (is_dh ? f.dh_groups : f.dw_groups) / across;
         if (c >= a.width) return;
         for (uint32_t n = group / across * (CE_THREADS / WAVE) + threadIdx.x / WAVE; n < rows; n += step * (CE_THREADS / WAVE)) {
-            const f32x8 sum = lower * parts_of_row(is_dh ? a.dh_sums : a.dw_sums, (uint64_t)split.tiles_n * S::TILE_N * a.width_pad, split.parts, (uint64_t)n * a.width_pad + c);
+            const f32x8 sum = lower * parts_of_row(is_dh ? a.dh_sums : a.dw_sums, (uint64_t)split.tiles_n * S::TILE_N * a.width_pad, split.parts,
+                                                   (uint64_t)n * a.width_pad + c);
             if (is_dh) store_eight(dh + a.list[n] * a.dh_stride + c, sum);
             else store_eight(dweight + (from + n) * a.dweight_stride + c, sum);
         }
@@ -602,7 +614,7 @@ __global__ __launch_bounds__(CE_THREADS) void cross_entropy_finish_kernel(CeArgs
     float sum = 0.0f;
 #pragma unroll 8
     for (uint32_t p = 0; p < parts; ++p) sum += a.dbias_sums[(uint64_t)p * a.vocab_pad + v];
-    dbias[v] = sum;
+    dbias[v] = lower * sum;
 }
 
 // ------------------------------------------------------------------ host
@@ -643,17 +655,18 @@ static bool ce_plan(uint64_t rows, uint32_t width, uint32_t vocab, CePlan& p) {
     p.logit_groups = tile_groups(tiles(vocab, p.small_logits) * tiles(some, p.small_logits));
     p.piece_groups = tile_groups(tiles(p.piece, p.small_logits) * tiles(some, p.small_logits));
     if (p.logit_groups > UINT32_MAX / 2) return false;
-    // few rows, for which dW is much to write and little to sum (10 x 256 x 100000: 108 -> 83 us, 100 x 4096 x 60000 628 -> 552; 45 x 1632 x 2982, with
-    // few tiles, would go from 42 to 50)
+    // few rows, for which dW is much to write and little to sum (10 x 256 x 100000: 108 -> 83 us, 100 x 4096 x 60000 628 -> 552;
+    // 45 x 1632 x 2982, with few tiles, would go from 42 to 50)
     p.narrow_products = some <= CE_FINE_ROWS && tiles(p.width_pad, true) * tiles(p.piece, true) > 1024;
     if (p.narrow_products) p.small_products = true;
-    const uint64_t dh_tiles = tiles(p.width_pad, p.small_products) * tiles(some, p.small_products), dw_tiles = tiles(p.width_pad, p.small_products) * tiles(p.piece, p.small_products);
-    const uint64_t fine_tiles = 2 * tiles(p.width_pad, p.small_products) * tiles(some < CE_FINE_ROWS ? some : CE_FINE_ROWS, p.small_products);
+    const uint64_t across = tiles(p.width_pad, p.small_products), dh_tiles = across * tiles(some, p.small_products);
+    const uint64_t dw_tiles = across * tiles(p.piece, p.small_products);
+    const uint64_t fine_tiles = 2 * across * tiles(some < CE_FINE_ROWS ? some : CE_FINE_ROWS, p.small_products);
     p.dh_groups = tile_groups(dh_tiles > CE_SPLIT_TILES ? dh_tiles : CE_SPLIT_TILES);
     if (p.dh_groups < fine_tiles) p.dh_groups = tile_groups(fine_tiles);
     p.dweight_groups = tile_groups(dw_tiles > CE_SPLIT_TILES ? dw_tiles : CE_SPLIT_TILES);
     // the last piece of the vocabulary, with fewer tiles, may be split where the others are not
-    const uint64_t least = tiles(p.width_pad, p.small_products) * tiles(pieces > 1 ? 1 : vocab, p.small_products);
+    const uint64_t least = across * tiles(pieces > 1 ? 1 : vocab, p.small_products);
     p.split_dweight = least <= CE_SPLIT_TILES && ce_parts((uint32_t)least, (uint32_t)((some + PRODUCT_K - 1) / PRODUCT_K)) > 1;
     for (const uint64_t groups : {p.small_logits ? p.logit_groups : 0, p.dh_groups, p.dweight_groups})
         if (groups > LAUNCH_GROUPS / 2) return false;
@@ -732,7 +745,7 @@ static size_t ce_extent(uint64_t rows, uint64_t stride, uint32_t width, size_t e
 template <typename T>
 static int ce_listed(const CeArgs& a, const void* h, float* loss, const float* lse_in, float* lse_out, const float* dloss, void* dh, hipStream_t s) {
     if (a.rows > CE_DIRECT) {
-        hipLaunchKernelGGL(cross_entropy_count_kernel, dim3((a.rows + CE_BLOCK - 1) / CE_BLOCK), dim3(CE_THREADS), 0, s, a, RAISED<T> ? dloss : nullptr);
+        hipLaunchKernelGGL(cross_entropy_count_kernel, dim3((a.rows + CE_BLOCK - 1) / CE_BLOCK), dim3(CE_THREADS), 0, s, a, dloss);
         if (const int status = launch_status()) return status;
     }
     const uint32_t rows = (a.rows + CE_GATHERED - 1) / CE_GATHERED, groups = rows < CE_PAD / CE_GATHERED ? CE_PAD / CE_GATHERED : rows;     // the zeros want some, too
@@ -781,7 +794,8 @@ static int ce_products(const CeArgs& a, const CePlan& p, const void* weight, con
     const CeFinish f = {g.dh && last ? rows(a.rows) : 0, g.dweight && p.split_dweight && tiles * 2 <= CE_SPLIT_TILES ? rows(columns) : 0};
     const uint32_t bias = g.dbias && last ? (a.vocab + CE_THREADS - 1) / CE_THREADS : 0;
     if (f.dh_groups + f.dw_groups + bias == 0) return OKT_OK;
-    hipLaunchKernelGGL((cross_entropy_finish_kernel<T, W, S>), dim3(f.dh_groups + f.dw_groups + bias), dim3(CE_THREADS), 0, s, a, (T*)g.dh, (W*)g.dweight, g.dbias, from, columns, f);
+    hipLaunchKernelGGL((cross_entropy_finish_kernel<T, W, S>), dim3(f.dh_groups + f.dw_groups + bias), dim3(CE_THREADS), 0, s, a, (T*)g.dh,
+                       (W*)g.dweight, g.dbias, from, columns, f);
     return launch_status();
 }
 
@@ -794,8 +808,10 @@ static int ce_backward(CeArgs a, const CePlan& p, const void* weight, CeGradient
         const uint32_t first = (uint32_t)from, columns = a.vocab - first < p.piece ? a.vocab - first : p.piece;
         const dim3 groups(ce_logit_groups(p, p.piece_groups));
         timing_before(s);
-        if (p.small_logits) hipLaunchKernelGGL((cross_entropy_gradient_kernel<T, Small>), groups, dim3(Small::THREADS), 0, s, a, (const T*)weight, first, columns);
-        else hipLaunchKernelGGL((cross_entropy_gradient_kernel<T, Large>), groups, dim3(Large::THREADS), 0, s, a, (const T*)weight, first, columns);
+        if (p.small_logits)
+            hipLaunchKernelGGL((cross_entropy_gradient_kernel<T, Small>), groups, dim3(Small::THREADS), 0, s, a, (const T*)weight, first, columns);
+        else
+            hipLaunchKernelGGL((cross_entropy_gradient_kernel<T, Large>), groups, dim3(Large::THREADS), 0, s, a, (const T*)weight, first, columns);
         timing_after(s);
         if (const int status = launch_status()) return status;
         const auto products = p.narrow_products ? ce_products<T, W, Narrow> : p.small_products ? ce_products<T, W, Small> : ce_products<T, W, Large>;
@@ -835,7 +851,8 @@ int okt_cross_entropy_forward(const okt_cross_entropy* op, const void* d_h, cons
     if (a.rows == 0) return OKT_OK;
     if (!d_h || !d_weight || !d_labels || !d_loss_out || !aligned(d_h, 16) || !aligned(d_weight, 16) || !aligned(d_labels, 8) ||
         !aligned(d_loss_out, 4) || !aligned(d_lse_out, 4)) return OKT_ERR_INVALID_ARG;
-    const struct { const void* p; size_t bytes; } in[] = {{d_h, ce_extent(a.rows, a.h_stride, a.width, 2)}, {d_weight, ce_extent(a.vocab, a.weight_stride, a.width, 2)},
+    const struct { const void* p; size_t bytes; } in[] = {{d_h, ce_extent(a.rows, a.h_stride, a.width, 2)},
+                                                          {d_weight, ce_extent(a.vocab, a.weight_stride, a.width, 2)},
                                                           {d_labels, 8ull * a.rows}, {a.bias, a.bias ? 4ull * a.vocab : 0}};
     for (const auto& t : in)
         for (const float* out : {d_loss_out, d_lse_out})

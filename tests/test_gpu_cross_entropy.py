@@ -249,3 +249,26 @@ def test_a_large_bias():
     c.bias[5], c.bias[7] = 150.0, 149.0
     loss, lse = c.forward()
     check(c, loss, lse, c.backward(lse))
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f16"])
+@pytest.mark.parametrize("rows,one_g", [(300, True), (300, False), (2600, True), (7, False)])
+def test_a_gradient_that_all_rows_share_is_not_rounded(rows, one_g, kind):
+    """A mean's gradient stands half a step between two values of the type; it is every row's, so rounding it would move the whole result
+    one way.  With W = 0 all p are 2^-10, and of the entries of d only 1 - 2^-10 is rounded, to 1 in bfloat16."""
+    vocab, g = 1024, (1.0 + UNIT[kind]) * 2.0 ** -11
+    c = Case(rows, 64, vocab, kind, bias=True, wide_dw=True, seed=90 + rows)
+    c.weight.zero_()
+    c.bias.zero_()
+    c.g = torch.full((1 if one_g else rows,), g, device=DEV)
+    loss, lse = c.forward()
+    dh, dw, db = c.backward(lse)
+    h, w, y, b = c.numbers()
+    _, want, want_db = ref.cross_entropy_backward(h, w, y, np.full(rows, g), b)
+    said = (np.arange(vocab)[:, None] == y) * 1.0
+    rounded = 0.0 if kind == "f16" or rows <= 256 else 2.0 ** -10
+    # p: lse's seven and the exponent's units of fp32 at the size 10, thus 2^-16 of p; an entry of d eight units, a sum's additions
+    one = g * (2.0 ** -10 * 2.0 ** -16 + (8 + rows) * E * (2.0 ** -10 + said))
+    within(dw, want, (g * rounded * said + one) @ np.abs(h), "dweight")
+    within(db, want_db, one.sum(1), "dbias")
+    assert (dh == 0).all()
