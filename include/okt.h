@@ -770,7 +770,7 @@ size_t okt_cross_entropy_workspace_bytes(uint64_t rows, uint32_t width, uint32_t
  *   d_labels    in   int64[rows]
  *   d_loss_out  out  fp32[rows]
  *   d_lse_out   out  fp32[rows]; NULL if no backward pass follows
- * Outputs overlap neither each other nor an input.  Four launches, three up to 2048 rows.
+ * Outputs overlap neither each other nor an input.  Four launches, three up to 2048 rows, two where their tiles are few as well.
  */
 int okt_cross_entropy_forward(const okt_cross_entropy* op, const void* d_h, const void* d_weight, const int64_t* d_labels,
                               float* d_loss_out, float* d_lse_out, void* d_ws, size_t ws_bytes, void* stream);

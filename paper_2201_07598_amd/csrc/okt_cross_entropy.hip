@@ -20,7 +20,7 @@
 // The matrix units bound the large sizes, at the clock that their power leaves: 8192 rows x 4096 x 128000 bf16 take 6.4 ms forward
 // (1.34 PFLOP/s) and 20.1 backward (1.71: operands near 0 take less power).  15 % of 16384 rows x 1024 x 30522 with a bias: 156 to 162 us
 // forward, of which the launches before and behind the product are 15 to 20, and 474 to 487 backward.  One row to a few
-// hundred: W's way from memory, and three launches (125 x 776 x 10007 fp16 20 us, of which the product is 12).
+// hundred: W's way from memory, and two launches (125 x 776 x 10007 fp16 15 us).
 #include <math.h>
 
 #include "okt_product.h"
@@ -40,6 +40,10 @@ constexpr float LOG2E = 1.44269504088896340736f;
 typedef ProductShape<4, 2, 2, 4, 2> Large;                           // 256 x 256, one workgroup of eight waves a CU
 typedef ProductShape<2, 2, 2, 2, 2> Narrow;                          // 128 x 128, two workgroups a CU: many tiles of a short sum
 typedef ProductShape<2, 2, 2, 2, 3> Small;                           // 128 x 128, four waves and two pieces on their way
+// The same by eight waves, for logits: two a SIMD wait for LDS in turn (125 x 776 x 10007: 17.0 -> 16.2 us); the second products, whose sums
+// over k are dealt to more workgroups, lose by it (22 x 752 x 112, gradient: 24 -> 32).
+typedef ProductShape<2, 1, 2, 4, 3> Spread;
+typedef ProductShape<1, 1, 2, 4, 3> Thin;                            // 64 x 128
 
 struct CeHeader { uint32_t count; float raise, lower; uint32_t pad; };
 
@@ -55,14 +59,14 @@ struct CeArgs {
     uint32_t* list;                                                  // numbers of the labelled rows
     int32_t* label_of;                                               // of listed row n
     void* h;                                                         // [rows_pad][width_pad]
-    float* stats;                                                    // forward: [parts][rows_pad][2]
+    float* stats;                                                    // forward: [parts][rows_pad][2]; parts of 32 columns at least
     float* said;                                                     // forward: s_ny
     float *lse_of, *g_of;                                            // backward, of listed row n
     void* d;                                                         // [rows_pad][piece]
     void* d_rest;                                                    // [CE_FINE_ROWS][piece]: what d's rounding left off
     float* dw_sums;                                                  // [parts][columns of whole tiles][width_pad]
     float* dh_sums;                                                  // [parts][rows of whole tiles][width_pad]
-    float* dbias_sums;                                               // [parts][vocab_pad]
+    float* dbias_sums;                                               // [parts][vocab_pad]; parts of 32 rows at least
     uint32_t piece, vocab_pad;
     uint32_t logit_tile_n, logit_parts_n;                            // rows of a tile of logits, and parts they leave of the bias's gradient
     __device__ __forceinline__ uint32_t dbias_parts(uint32_t count) const { return (count + logit_tile_n - 1) / logit_tile_n * logit_parts_n; }
@@ -237,6 +241,10 @@ template <class S>
 struct RowFacts {
     uint32_t label[S::NT];
     float g[S::NT], lse[S::NT];
+    __device__ __forceinline__ explicit RowFacts(const uint32_t* labels) {
+#pragma unroll
+        for (int n = 0; n < S::NT; ++n) label[n] = labels[n * 32];
+    }
     __device__ __forceinline__ RowFacts(const CeArgs& a, uint32_t row, bool backward) {
 #pragma unroll
         for (int n = 0; n < S::NT; ++n) {
@@ -251,7 +259,7 @@ struct RowFacts {
 
 // Where a workgroup has a CU for itself it stays, and the next tile's first operands are on their way while this one's logits are
 // worked on (2458 rows x 1024 x 30522: 164 -> 157 us; small tiles, of which there are few, gain nothing and lose 1.4 us).
-template <class S> constexpr bool STAYS = S::WAVES == 8;
+template <class S> constexpr bool STAYS = S::TILE_M == 256;
 
 // Tiles of logits; `finish` is called with a tile's sums, its place, its bias and its rows' facts.
 template <typename T, class S, bool BACKWARD, class F>
@@ -286,38 +294,108 @@ __device__ __forceinline__ void logit_tiles(const CeArgs& a, const T* weight, ui
     }
 }
 
+// What a tile of logits leaves: the largest and the sum of exponentials of its part of a row, and the label's logit.
+template <class S>
+__device__ __forceinline__ void part_of_rows(const CeArgs& a, const f32x16 (&c)[S::MT][S::NT], uint32_t v0, uint32_t part_n, const float* bias,
+                                             const RowFacts<S>& facts, uint32_t count) {
+    const uint32_t lane = threadIdx.x % WAVE, part = v0 / (S::MT * 32);
+    const bool biased = a.bias || v0 + S::MT * 32 > a.vocab;
+#pragma unroll
+    for (int n = 0; n < S::NT; ++n) {
+        const uint32_t row = part_n * (S::NT * 32) + n * 32 + lane % 32;
+        float s[S::MT * 16];
+        logits_of_row<S>(s, c, n, bias, biased);
+        float top = -__builtin_inff();
+#pragma unroll
+        for (int i = 0; i < S::MT * 16; ++i) top = fmaxf(top, s[i]);
+        top = max_halves(top);
+        const float base = top == -__builtin_inff() ? 0.0f : -top * LOG2E;
+        float sum = 0.0f;
+#pragma unroll
+        for (int i = 0; i < S::MT * 16; ++i) sum += __builtin_amdgcn_exp2f(fmaf(s[i], LOG2E, base));
+        sum = sum_halves(sum);
+        if (lane < 32 && row < count)
+            *reinterpret_cast<float2*>(a.stats + ((uint64_t)part * a.rows_pad + row) * 2) = make_float2(top, sum);
+        const uint32_t mine = facts.label[n] - v0 - lane / 32 * 16;      // far above a wave's part where it is none of its
+        if (__ballot(mine < S::MT * 32u)) {
+#pragma unroll
+            for (int m = 0; m < S::MT; ++m)
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    if (mine == m * 32u + r) a.said[row] = s[m * 16 + r];
+        }
+    }
+}
+
 template <typename T, class S>
 __global__ __launch_bounds__(S::THREADS) void cross_entropy_forward_kernel(CeArgs a, const T* weight) {
     logit_tiles<T, S, false>(a, weight, 0, a.vocab, [&](const f32x16 (&c)[S::MT][S::NT], uint32_t v0, uint32_t part_n, const float* bias,
                                                         const RowFacts<S>& facts, uint32_t count) {
-        const uint32_t lane = threadIdx.x % WAVE, part = v0 / (S::MT * 32);
-        const bool biased = a.bias || v0 + S::MT * 32 > a.vocab;
-#pragma unroll
-        for (int n = 0; n < S::NT; ++n) {
-            const uint32_t row = part_n * (S::NT * 32) + n * 32 + lane % 32;
-            float s[S::MT * 16];
-            logits_of_row<S>(s, c, n, bias, biased);
-            float top = -__builtin_inff();
-#pragma unroll
-            for (int i = 0; i < S::MT * 16; ++i) top = fmaxf(top, s[i]);
-            top = max_halves(top);
-            const float base = top == -__builtin_inff() ? 0.0f : -top * LOG2E;
-            float sum = 0.0f;
-#pragma unroll
-            for (int i = 0; i < S::MT * 16; ++i) sum += __builtin_amdgcn_exp2f(fmaf(s[i], LOG2E, base));
-            sum = sum_halves(sum);
-            if (lane < 32 && row < count)
-                *reinterpret_cast<float2*>(a.stats + ((uint64_t)part * a.rows_pad + row) * 2) = make_float2(top, sum);
-            const uint32_t mine = facts.label[n] - v0 - lane / 32 * 16;      // far above a wave's part where it is none of its
-            if (__ballot(mine < S::MT * 32u)) {
-#pragma unroll
-                for (int m = 0; m < S::MT; ++m)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r)
-                        if (mine == m * 32u + r) a.said[row] = s[m * 16 + r];
-            }
-        }
+        part_of_rows<S>(a, c, v0, part_n, bias, facts, count);
     });
+}
+
+// Few rows, of few tiles, are taken as they lie: every workgroup lists the labelled ones by itself and fetches its tile's by their numbers, so nothing
+// is laid side by side first (125 x 776 x 10007: 20.4 -> 17.0 us, 481 x 80 x 2048 14.1 -> 11.1).  The first one writes the list and the other rows' zeros.
+template <typename T, class S>
+__global__ __launch_bounds__(S::THREADS) void cross_entropy_direct_kernel(CeArgs a, const T* h, const T* weight, float* loss, float* lse) {
+    typedef Product<T, S, KMajor<T, S::TILE_M, S::WAVES, true>, ListedRows<T, S::TILE_N, S::WAVES>> Logits;
+    constexpr uint32_t CHUNKS = CE_DIRECT / S::THREADS;
+    static_assert(CHUNKS * S::THREADS == CE_DIRECT && CHUNKS * S::WAVES <= WAVE && S::THREADS >= S::TILE_N, "");
+    __shared__ __attribute__((aligned(1024))) char lds[S::BYTES];
+    __shared__ float bias[S::TILE_M];
+    __shared__ uint32_t counts[WAVE], row_of[S::TILE_N], label_of[S::TILE_N];
+    const uint32_t lane = threadIdx.x % WAVE, wave = uniform(threadIdx.x / WAVE);
+    int64_t y[CHUNKS];
+#pragma unroll
+    for (uint32_t k = 0; k < CHUNKS; ++k) {
+        const uint32_t row = k * S::THREADS + threadIdx.x;
+        y[k] = row < a.rows ? a.labels[row] : -1;
+    }
+    if (threadIdx.x < WAVE) counts[threadIdx.x] = 0;
+    if (threadIdx.x < S::TILE_N) row_of[threadIdx.x] = label_of[threadIdx.x] = NO_ROW;
+    __syncthreads();
+    uint64_t listed[CHUNKS];                                         // lanes whose row has a label
+#pragma unroll
+    for (uint32_t k = 0; k < CHUNKS; ++k) {
+        listed[k] = __ballot(labelled(y[k], a.vocab));
+        if (lane == 0) counts[k * S::WAVES + wave] = __popcll(listed[k]);
+    }
+    __syncthreads();
+    const uint32_t up_to = wave_inclusive_scan_u32(counts[lane]), count = uniform(__shfl(up_to, WAVE - 1, WAVE));
+    const TilePlace tile = tile_place(blockIdx.x, (a.vocab + S::TILE_M - 1) / S::TILE_M, (count + S::TILE_N - 1) / S::TILE_N);
+    const bool writes = blockIdx.x == 0;
+    if (!tile.there && !writes) return;
+#pragma unroll
+    for (uint32_t k = 0; k < CHUNKS; ++k) {
+        const uint32_t row = k * S::THREADS + threadIdx.x, group = k * S::WAVES + wave;
+        const uint32_t before = group ? __shfl(up_to, group - 1, WAVE) : 0;
+        const uint32_t n = before + __popcll(listed[k] & ((1ull << lane) - 1));
+        if (listed[k] >> lane & 1) {
+            if (tile.there && n / S::TILE_N == tile.n) {
+                row_of[n % S::TILE_N] = row;
+                label_of[n % S::TILE_N] = (uint32_t)y[k];
+            }
+            if (writes) a.list[n] = row;
+        } else if (writes && row < a.rows) {
+            loss[row] = 0.0f;
+            if (lse) lse[row] = 0.0f;
+        }
+    }
+    if (writes && threadIdx.x == 0) *a.header = {count, 1.0f, 1.0f, 0};
+    if (!tile.there) return;
+    const uint32_t v = tile.m * S::TILE_M;
+    load_bias<S>(bias, a, v);
+    __syncthreads();
+    Logits p({weight + v * a.weight_stride, weight + (a.vocab - 1) * a.weight_stride + a.width, (uint32_t)(a.weight_stride * 2)},
+             {h, h + (a.rows - 1) * a.h_stride + a.width, (uint32_t)(a.h_stride * 2), row_of}, a.width, lds);
+    f32x16 c[S::MT][S::NT];
+    clear<S>(c);
+    p.begin();
+    p.run(c, lds);
+    const uint32_t in_tile = S::wave_n() * (S::NT * 32);
+    part_of_rows<S>(a, c, v + S::wave_m() * (S::MT * 32), tile.n * S::WN + S::wave_n(), bias + S::wave_m() * (S::MT * 32),
+                    RowFacts<S>(label_of + in_tile + lane % 32), count);
 }
 
 // Sixteen rows a workgroup, and 64 threads a row, each every 64th part.
@@ -681,7 +759,7 @@ static bool ce_plan(uint64_t rows, uint32_t width, uint32_t vocab, CePlan& p) {
     p.label_at = place(4ull * p.rows_pad);
     p.h_at = place(2ull * p.rows_pad * p.width_pad);
     const size_t shared = at;
-    p.stats_at = place(8ull * p.rows_pad * (p.vocab_pad / 64));
+    p.stats_at = place(8ull * p.rows_pad * (p.vocab_pad / 32));
     p.said_at = place(4ull * p.rows_pad);
     p.forward_bytes = at;
     at = shared;
@@ -694,7 +772,7 @@ static bool ce_plan(uint64_t rows, uint32_t width, uint32_t vocab, CePlan& p) {
     const uint64_t once = ((uint64_t)p.rows_pad + CE_FINE_ROWS) * p.width_pad;
     p.dh_at = place(4 * (once > parts(p.small_products) ? once : parts(p.small_products)));
     p.dw_at = place(p.split_dweight ? 4 * parts(p.small_products) : 0);
-    p.dbias_at = place(4ull * (p.rows_pad / 64) * p.vocab_pad);
+    p.dbias_at = place(4ull * (p.rows_pad / 32) * p.vocab_pad);
     p.backward_bytes = at;
     return true;
 }
@@ -759,14 +837,28 @@ static unsigned ce_logit_groups(const CePlan& p, uint64_t tiles) {
     return (unsigned)(p.small_logits || tiles < stay ? tiles : stay);
 }
 
+template <class S>
+static int ce_join(const CeArgs& a, float* loss, float* lse, hipStream_t s) {
+    hipLaunchKernelGGL(cross_entropy_join_kernel, dim3((a.rows + 15) / 16), dim3(CE_JOIN_THREADS), 0, s, a, (a.vocab + S::TILE_M - 1) / S::TILE_M * S::WM, loss, lse);
+    return launch_status();
+}
+
 template <typename T, class S>
 static int ce_forward(const CeArgs& a, const CePlan& p, const void* weight, float* loss, float* lse, hipStream_t s) {
     timing_before(s);
     hipLaunchKernelGGL((cross_entropy_forward_kernel<T, S>), dim3(ce_logit_groups(p, p.logit_groups)), dim3(S::THREADS), 0, s, a, (const T*)weight);
     timing_after(s);
     if (const int status = launch_status()) return status;
-    hipLaunchKernelGGL(cross_entropy_join_kernel, dim3((a.rows + 15) / 16), dim3(CE_JOIN_THREADS), 0, s, a, (a.vocab + S::TILE_M - 1) / S::TILE_M * S::WM, loss, lse);
-    return launch_status();
+    return ce_join<S>(a, loss, lse, s);
+}
+
+template <typename T, class S>
+static int ce_forward_direct(const CeArgs& a, const CePlan& p, const void* h, const void* weight, float* loss, float* lse, hipStream_t s) {
+    timing_before(s);
+    hipLaunchKernelGGL((cross_entropy_direct_kernel<T, S>), dim3((unsigned)tile_groups(((a.vocab + S::TILE_M - 1ull) / S::TILE_M) * ((a.rows + S::TILE_N - 1ull) / S::TILE_N))), dim3(S::THREADS), 0, s, a, (const T*)h, (const T*)weight, loss, lse);
+    timing_after(s);
+    if (const int status = launch_status()) return status;
+    return ce_join<S>(a, loss, lse, s);
 }
 
 struct CeGradients { void *dh, *dweight; float* dbias; };
@@ -802,14 +894,14 @@ static int ce_products(const CeArgs& a, const CePlan& p, const void* weight, con
 template <typename T, typename W>
 static int ce_backward(CeArgs a, const CePlan& p, const void* weight, CeGradients g, hipStream_t s) {
     if (a.rows == 0) g.dh = nullptr;
-    a.logit_tile_n = p.small_logits ? Small::TILE_N : Large::TILE_N;
-    a.logit_parts_n = p.small_logits ? Small::WN : Large::WN;
+    a.logit_tile_n = p.small_logits ? Spread::TILE_N : Large::TILE_N;
+    a.logit_parts_n = p.small_logits ? Spread::WN : Large::WN;
     for (uint64_t from = 0; from < a.vocab; from += p.piece) {
         const uint32_t first = (uint32_t)from, columns = a.vocab - first < p.piece ? a.vocab - first : p.piece;
         const dim3 groups(ce_logit_groups(p, p.piece_groups));
         timing_before(s);
         if (p.small_logits)
-            hipLaunchKernelGGL((cross_entropy_gradient_kernel<T, Small>), groups, dim3(Small::THREADS), 0, s, a, (const T*)weight, first, columns);
+            hipLaunchKernelGGL((cross_entropy_gradient_kernel<T, Spread>), groups, dim3(Spread::THREADS), 0, s, a, (const T*)weight, first, columns);
         else
             hipLaunchKernelGGL((cross_entropy_gradient_kernel<T, Large>), groups, dim3(Large::THREADS), 0, s, a, (const T*)weight, first, columns);
         timing_after(s);
@@ -820,10 +912,21 @@ static int ce_backward(CeArgs a, const CePlan& p, const void* weight, CeGradient
     return OKT_OK;
 }
 
+// Whether every workgroup of the logits can list the rows by itself, and reach them all from the first one.
+static bool ce_direct(const CeArgs& a, const CePlan& p) {
+    return p.small_logits && a.rows <= CE_DIRECT && ce_extent(a.rows, a.h_stride, a.width, 2) < 1ull << 31;
+}
+
+// Tiles of 64 columns for 128 where that leaves no CU with two (125 x 776 x 10007, 157 of them: 16.2 -> 15.2 us; 3 x 880 x 18612, 291: 16.3 -> 19.8).
+static bool ce_thin(const CeArgs& a) {
+    return ((a.vocab + Thin::TILE_M - 1ull) / Thin::TILE_M) * ((a.rows + Thin::TILE_N - 1ull) / Thin::TILE_N) <= (uint64_t)device_cus();
+}
+
 template <typename T>
 static int ce_run_forward(const CeArgs& a, const CePlan& p, const void* h, const void* weight, float* loss, float* lse, hipStream_t s) {
+    if (ce_direct(a, p)) return ce_thin(a) ? ce_forward_direct<T, Thin>(a, p, h, weight, loss, lse, s) : ce_forward_direct<T, Spread>(a, p, h, weight, loss, lse, s);
     if (const int status = ce_listed<T>(a, h, loss, nullptr, lse, nullptr, nullptr, s)) return status;
-    return p.small_logits ? ce_forward<T, Small>(a, p, weight, loss, lse, s) : ce_forward<T, Large>(a, p, weight, loss, lse, s);
+    return p.small_logits ? ce_forward<T, Spread>(a, p, weight, loss, lse, s) : ce_forward<T, Large>(a, p, weight, loss, lse, s);
 }
 template <typename T>
 static int ce_run_backward(const CeArgs& a, const CePlan& p, const void* h, const void* weight, const float* lse, const float* dloss, const CeGradients& g, bool wide,

@@ -34,27 +34,46 @@ struct OperandSource {
 template <typename T, int ROWS, int WAVES, bool ORDERED>
 struct KMajor {
     static constexpr int LOADS = ROWS / 8 / WAVES, BYTES = ROWS * PRODUCT_K * 2;
-    static_assert(LOADS % 4 == 0, "a wave's blocks begin at a multiple of four");
     OperandSource from;
     uint32_t at[LOADS], read[4];
+
+    // Which sixteen-byte chunk of its row a lane fetches with fetch i of its wave's; blocks repeat after four.
+    static __device__ __forceinline__ uint32_t chunk(int i) {
+        return kmajor_chunk<ORDERED>(threadIdx.x % WAVE, LOADS % 4 == 0 ? i : threadIdx.x / WAVE * LOADS + i);
+    }
 
     // `end`: of the tensor's last row
     __device__ __forceinline__ KMajor(const T* tile, const T* end, uint32_t row_bytes) {
         const uint32_t lane = threadIdx.x % WAVE, wave = threadIdx.x / WAVE;
         from = {(uint64_t)tile, (uint64_t)end - (uint64_t)tile};
 #pragma unroll
-        for (int i = 0; i < LOADS; ++i) at[i] = ((wave * LOADS + i) * 8 + lane / 8) * row_bytes + kmajor_chunk<ORDERED>(lane, i) * 16;
+        for (int i = 0; i < LOADS; ++i) at[i] = ((wave * LOADS + i) * 8 + lane / 8) * row_bytes + chunk(i) * 16;
 #pragma unroll
         for (uint32_t s = 0; s < 4; ++s) read[s] = kmajor_read<ORDERED>(lane, s);
     }
     // Fetch i of the wave's of a piece of which the tensor has `there` k.
     __device__ __forceinline__ void fetch(int i, uint32_t lds, i32x4 buffer, uint32_t there) const {
         const uint32_t to = lds + uniform(threadIdx.x / WAVE) * (LOADS * 1024) + i * 1024;
-        fetch_to_lds(to, there >= PRODUCT_K || kmajor_chunk<ORDERED>(threadIdx.x % WAVE, i) * 8 < there ? at[i] : OUTSIDE, buffer);
+        fetch_to_lds(to, there >= PRODUCT_K || chunk(i) * 8 < there ? at[i] : OUTSIDE, buffer);
     }
     __device__ __forceinline__ void advance() { from.advance(PRODUCT_K * 2); }
     __device__ __forceinline__ frag<T> operand(const char* piece, int square, int s) const {
         return *reinterpret_cast<const frag<T>*>(piece + read[s] + square * KMAJOR_SQUARE);
+    }
+};
+
+// The same with rows from a table in LDS, all within 2^31 bytes of the tensor's first; zeros for those that are NO_ROW.
+constexpr uint32_t NO_ROW = 0xffffffffu;
+template <typename T, int ROWS, int WAVES>
+struct ListedRows : KMajor<T, ROWS, WAVES, false> {
+    typedef KMajor<T, ROWS, WAVES, false> Base;
+    __device__ __forceinline__ ListedRows(const T* tensor, const T* end, uint32_t row_bytes, const uint32_t* rows) : Base(tensor, end, 0) {
+        const uint32_t lane = threadIdx.x % WAVE, wave = threadIdx.x / WAVE;
+#pragma unroll
+        for (int i = 0; i < Base::LOADS; ++i) {
+            const uint32_t row = rows[(wave * Base::LOADS + i) * 8 + lane / 8];
+            this->at[i] = row == NO_ROW ? OUTSIDE : row * row_bytes + Base::chunk(i) * 16;
+        }
     }
 };
 

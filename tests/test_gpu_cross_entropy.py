@@ -272,3 +272,29 @@ def test_a_gradient_that_all_rows_share_is_not_rounded(rows, one_g, kind):
     within(dw, want, (g * rounded * said + one) @ np.abs(h), "dweight")
     within(db, want_db, one.sum(1), "dbias")
     assert (dh == 0).all()
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f16"])
+@pytest.mark.parametrize("labelled", [1.0, 0.4, 0.004, 0.0])
+@pytest.mark.parametrize("rows,vocab", [(2048, 700), (2049, 700), (2048, 1030), (1, 16_385), (129, 8193), (120, 40_000)])
+def test_rows_as_they_lie_and_side_by_side(rows, vocab, labelled, kind):
+    """Up to 2048 rows are read as they lie where tiles are few, from 2049 on they are laid side by side; tiles of 64 columns, one too many of them for the
+    CUs, more tiles than one a CU.  Between the rows there is NaN, as in those without a label."""
+    c = Case(rows, 136, vocab, kind, labelled, bias=True, seed=95, pad=8)
+    c.h._base[:, 136:] = float("nan")
+    c.h[(c.labels < 0) | (c.labels >= vocab)] = float("nan")
+    loss, lse = c.forward()
+    c.h[(c.labels < 0) | (c.labels >= vocab)] = 0.0
+    check(c, loss, lse)
+    again = c.forward()
+    assert torch.equal(again[0], loss) and torch.equal(again[1], lse)
+
+
+@pytest.mark.parametrize("rows", [1024, 1025])
+def test_rows_far_apart(rows):
+    """The last one begins just below 2^31 bytes behind the first, and at it, where 32-bit offsets from the first row end."""
+    c = Case(rows, 64, 300, labelled=0.9, seed=96)
+    far = torch.full((rows, 1 << 20), float("nan"), dtype=torch.bfloat16, device=DEV)
+    far[:, :64] = c.h
+    c.h = far[:, :64]
+    check(c, *c.forward())
