@@ -40,8 +40,9 @@ constexpr float LOG2E = 1.44269504088896340736f;
 typedef ProductShape<4, 2, 2, 4, 2> Large;                           // 256 x 256, one workgroup of eight waves a CU
 typedef ProductShape<2, 2, 2, 2, 2> Narrow;                          // 128 x 128, two workgroups a CU: many tiles of a short sum
 typedef ProductShape<2, 2, 2, 2, 3> Small;                           // 128 x 128, four waves and two pieces on their way
-// The same by eight waves, for logits: two a SIMD wait for LDS in turn (125 x 776 x 10007: 17.0 -> 16.2 us); the second products, whose sums
-// over k are dealt to more workgroups, lose by it (22 x 752 x 112, gradient: 24 -> 32).
+// The same by eight waves, for logits: two a SIMD wait for LDS in turn (125 x 776 x 10007: 17.0 -> 16.2 us).  The second products, whose
+// sums over k are dealt to more workgroups, gain little by it and lose where LDS bounds them (78 x 136 x 143, gradient: 20.9 -> 20.5;
+// 700 x 1024 x 3000 46.0 -> 48.5).
 typedef ProductShape<2, 1, 2, 4, 3> Spread;
 typedef ProductShape<1, 1, 2, 4, 3> Thin;                            // 64 x 128
 
