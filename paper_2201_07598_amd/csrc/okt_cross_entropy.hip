@@ -441,11 +441,11 @@ __global__ __launch_bounds__(CE_JOIN_THREADS) void cross_entropy_join_kernel(CeA
 
 // ------------------------------------------------------------------ the gradient of the logits
 
-// Sums over the 32 lanes of a half of N values each; lane l % 32 gets those of values N / 32 (l % 32) on.  Every step hands over the half of the
+// Sums over the 32 lanes of a half of N values each; lane l % 32 gets those of values N (l % 32) / 32 on (of 16 values two lanes the same).  Every step hands over the half of the
 // values that the other lane goes on with, so all steps together cost two exchanges a value and not five.
 template <int N>
 __device__ __forceinline__ void sums_over_lanes(float (&v)[N]) {
-    static_assert(N == 64 || N == 32, "");
+    static_assert(N == 64 || N == 32 || N == 16, "");
 #pragma unroll
     for (int i = 0; i < N / 2; ++i) {
         const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v[i]), __float_as_uint(v[i + N / 2]), false, false);
@@ -460,7 +460,11 @@ __device__ __forceinline__ void sums_over_lanes(float (&v)[N]) {
     OKT_HALVE(N / 4, 8, 0x140)        // row_mirror
     OKT_HALVE(N / 8, 4, 0x141)        // row_half_mirror
     OKT_HALVE(N / 16, 2, 0x4E)        // quad_perm [2, 3, 0, 1]
-    OKT_HALVE(N / 32, 1, 0xB1)        // quad_perm [1, 0, 3, 2]
+    if constexpr (N >= 32) {
+        OKT_HALVE(N / 32, 1, 0xB1)    // quad_perm [1, 0, 3, 2]
+    } else {
+        v[0] += __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v[0]), 0xB1, 0xf, 0xf, true));
+    }
 #undef OKT_HALVE
 }
 
@@ -514,8 +518,8 @@ __global__ __launch_bounds__(S::THREADS) void cross_entropy_gradient_kernel(CeAr
         }
         if (!a.dbias_sums) return;
         sums_over_lanes(sums);
-        constexpr int EACH = S::MT * 16 / 32;
-        const uint32_t first = lane % 32 * EACH;
+        constexpr int EACH = S::MT > 1 ? S::MT / 2 : 1;
+        const uint32_t first = lane % 32 * (S::MT * 16) / 32;
         float* to = a.dbias_sums + (uint64_t)part_n * a.vocab_pad + v0 + first / 16 * 32 + lane / 32 * 16 + first % 16;
 #pragma unroll
         for (int i = 0; i < EACH; ++i) to[i] = sums[i];
@@ -862,6 +866,13 @@ static int ce_forward_direct(const CeArgs& a, const CePlan& p, const void* h, co
     return ce_join<S>(a, loss, lse, s);
 }
 
+// Tiles of 64 columns for 128 where that leaves no CU with two (125 x 776 x 10007, 157 of them: 16.2 -> 15.2 us; 3 x 880 x 18612, 291: 16.3 -> 19.8;
+// gradient of 1000 x 2048 x 500, 64 of them: 48.1 -> 45.7, of 300 x 4096 x 5000 100.8 -> 96.5).
+static uint64_t ce_thin_tiles(uint64_t columns, uint64_t rows) {
+    return (columns + Thin::TILE_M - 1) / Thin::TILE_M * (rows ? (rows + Thin::TILE_N - 1) / Thin::TILE_N : 1);
+}
+static bool ce_thin(uint64_t columns, uint64_t rows) { return ce_thin_tiles(columns, rows) <= device_cus(); }
+
 struct CeGradients { void *dh, *dweight; float* dbias; };
 
 template <typename T, typename W, class S>
@@ -895,13 +906,17 @@ static int ce_products(const CeArgs& a, const CePlan& p, const void* weight, con
 template <typename T, typename W>
 static int ce_backward(CeArgs a, const CePlan& p, const void* weight, CeGradients g, hipStream_t s) {
     if (a.rows == 0) g.dh = nullptr;
+    static_assert(Thin::TILE_N == Spread::TILE_N && Thin::WN == Spread::WN, "");
     a.logit_tile_n = p.small_logits ? Spread::TILE_N : Large::TILE_N;
     a.logit_parts_n = p.small_logits ? Spread::WN : Large::WN;
     for (uint64_t from = 0; from < a.vocab; from += p.piece) {
         const uint32_t first = (uint32_t)from, columns = a.vocab - first < p.piece ? a.vocab - first : p.piece;
         const dim3 groups(ce_logit_groups(p, p.piece_groups));
         timing_before(s);
-        if (p.small_logits)
+        if (p.small_logits && ce_thin(columns, a.rows))
+            hipLaunchKernelGGL((cross_entropy_gradient_kernel<T, Thin>), dim3((unsigned)tile_groups(ce_thin_tiles(columns, a.rows))), dim3(Thin::THREADS), 0, s, a,
+                               (const T*)weight, first, columns);
+        else if (p.small_logits)
             hipLaunchKernelGGL((cross_entropy_gradient_kernel<T, Spread>), groups, dim3(Spread::THREADS), 0, s, a, (const T*)weight, first, columns);
         else
             hipLaunchKernelGGL((cross_entropy_gradient_kernel<T, Large>), groups, dim3(Large::THREADS), 0, s, a, (const T*)weight, first, columns);
@@ -918,14 +933,9 @@ static bool ce_direct(const CeArgs& a, const CePlan& p) {
     return p.small_logits && a.rows <= CE_DIRECT && ce_extent(a.rows, a.h_stride, a.width, 2) < 1ull << 31;
 }
 
-// Tiles of 64 columns for 128 where that leaves no CU with two (125 x 776 x 10007, 157 of them: 16.2 -> 15.2 us; 3 x 880 x 18612, 291: 16.3 -> 19.8).
-static bool ce_thin(const CeArgs& a) {
-    return ((a.vocab + Thin::TILE_M - 1ull) / Thin::TILE_M) * ((a.rows + Thin::TILE_N - 1ull) / Thin::TILE_N) <= (uint64_t)device_cus();
-}
-
 template <typename T>
 static int ce_run_forward(const CeArgs& a, const CePlan& p, const void* h, const void* weight, float* loss, float* lse, hipStream_t s) {
-    if (ce_direct(a, p)) return ce_thin(a) ? ce_forward_direct<T, Thin>(a, p, h, weight, loss, lse, s) : ce_forward_direct<T, Spread>(a, p, h, weight, loss, lse, s);
+    if (ce_direct(a, p)) return ce_thin(a.vocab, a.rows) ? ce_forward_direct<T, Thin>(a, p, h, weight, loss, lse, s) : ce_forward_direct<T, Spread>(a, p, h, weight, loss, lse, s);
     if (const int status = ce_listed<T>(a, h, loss, nullptr, lse, nullptr, nullptr, s)) return status;
     return p.small_logits ? ce_forward<T, Spread>(a, p, weight, loss, lse, s) : ce_forward<T, Large>(a, p, weight, loss, lse, s);
 }
