@@ -785,6 +785,10 @@ def _positions(t, batch, length, axes):
     """(pointer, batch stride, token stride) of int32 [batch, length, axes] or [length, axes]; one axis may be left out."""
     if t is None:
         return 0, 0, 0
+    if t.dtype is _TORCH.int32 and t.is_cuda and t.shape == (batch, length, axes):
+        strides = t.stride()
+        if axes == 1 or strides[2] == 1:
+            return t.data_ptr(), strides[0], strides[1]
     if not t.is_cuda:
         raise TypeError("positions must be a CUDA tensor (device memory)")
     if t.dtype is not _TORCH.int32:
@@ -812,10 +816,10 @@ def _rotary_struct(dtype, shape, kv_heads, inv_freq, positions, axis_of_pair, ad
             raise ValueError(f"axis_of_pair needs one axis a pair ({pairs}), got {len(axis_of_pair)}")
         table = bytes(axis_of_pair)
         axes = 1 if table.count(0) == pairs else max(table) + 1
-    if positions is not None and positions.dim() == 3:
-        axes = max(axes, positions.shape[2])
-    elif positions is not None and axes > 1 and positions.dim() == 2:
-        axes = max(axes, positions.shape[1])
+    if positions is not None:
+        places = positions.shape
+        if len(places) == 3 or (len(places) == 2 and axes > 1):
+            axes = max(axes, places[-1])
     at, by_batch, by_token = _positions(positions, batch, length, axes)
     return _ROTARY.pack(
         batch, length, heads, kv_heads, dim, 2 * pairs, _DTYPES[dtype], _NORM_KINDS[kind], eps, 1 if adjacent else 0, axes, 0, table,
@@ -839,7 +843,7 @@ def okt_norm_rotary_forward(q, k, q_out, k_out, inv_freq, *, positions=None, axi
     pk, sk, pko, sko, kv_heads = 0, _NO_HEADS, 0, _NO_HEADS, 0
     if k is not None:
         keys = k.shape
-        if len(keys) != 4 or keys[:2] != shape[:2] or keys[3] != shape[3]:
+        if len(keys) != 4 or keys[0] != shape[0] or keys[1] != shape[1] or keys[3] != shape[3]:
             raise ValueError("q and k must agree in batch, length and head_dim")
         kv_heads = keys[2]
         pk, sk = _heads(k, dtype, keys, "k")
@@ -867,7 +871,7 @@ def okt_norm_rotary_backward(q, k, dq, dk, dq_out, dk_out, inv_freq, ws=None, *,
     pk, sk, pdk, sdk, pko, sko, kv_heads = 0, _NO_HEADS, 0, _NO_HEADS, 0, _NO_HEADS, 0
     if dk is not None:
         keys = dk.shape
-        if len(keys) != 4 or keys[:2] != shape[:2] or keys[3] != shape[3]:
+        if len(keys) != 4 or keys[0] != shape[0] or keys[1] != shape[1] or keys[3] != shape[3]:
             raise ValueError("dq and dk must agree in batch, length and head_dim")
         kv_heads = keys[2]
         if k is None and k_weight is not None:

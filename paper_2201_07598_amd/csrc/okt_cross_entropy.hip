@@ -18,7 +18,7 @@
 // over the number of rows and p one over the vocabulary's size, and fp16 ends at 2^-24.
 //
 // The matrix units bound the large sizes, at the clock that their power leaves: 8192 rows x 4096 x 128000 bf16 take 6.4 ms forward
-// (1.34 PFLOP/s) and 20.1 backward (1.71: operands near 0 take less power).  15 % of 16384 rows x 1024 x 30522 with a bias: 156 to 162 us
+// (1.34 PFLOP/s) and 20.1 backward (1.71: operands near 0 take less power).  15 % of 16384 rows x 1024 x 30522 with a bias: 147 to 163 us
 // forward, of which the launches before and behind the product are 15 to 20, and 474 to 487 backward.  One row to a few
 // hundred: W's way from memory, and two launches (125 x 776 x 10007 fp16 15 us).
 #include <math.h>
@@ -413,6 +413,9 @@ __global__ __launch_bounds__(CE_JOIN_THREADS) void cross_entropy_join_kernel(CeA
     const uint32_t count = uniform(a.header->count), r = threadIdx.x % 16, share = threadIdx.x / 16, row = blockIdx.x * 16 + r;
     if (blockIdx.x * 16 >= count) return;
     RowSum v = {-__builtin_inff(), 0.0f};
+    const bool last = threadIdx.x < 16 && row < count;               // has the row's sum in the end
+    const uint32_t to = last ? a.list[row] : 0;
+    const float said = last ? a.said[row] : 0.0f;
     if (row < count)
 #pragma unroll 4
         for (uint32_t p = share; p < parts; p += CE_JOIN_THREADS / 16) {
@@ -432,10 +435,9 @@ __global__ __launch_bounds__(CE_JOIN_THREADS) void cross_entropy_join_kernel(CeA
 #pragma unroll
     for (int k = 4; k < CE_JOIN_THREADS / WAVE; k += 4) v = together(v, waves[k + share][r]);
     v = lanes(v);
-    if (share != 0 || row >= count) return;
+    if (!last) return;
     const float all = v.top == -__builtin_inff() && v.sum == 0.0f ? v.top : v.top + logf(v.sum);
-    const uint32_t to = a.list[row];
-    loss[to] = all - a.said[row];
+    loss[to] = all - said;
     if (lse) lse[to] = all;
 }
 
