@@ -729,7 +729,7 @@ int okt_norm_rotary_forward(const okt_norm_rotary* op, const void* d_q, const vo
  *   d_q, d_k  in   as the forward pass read them; looked at where there is a weight (else may be NULL)
  *   d_dq_out, d_dk_out  out  may be d_dq and d_dk, or d_q and d_k, with their strides; overlap nothing otherwise
  *   d_dq_weight_out, d_dk_weight_out  out  fp32[head_dim], 4-byte aligned; NULL: not wanted, and where there is no weight.  Queries
- *             and keys that share a weight need one each, to be added by the caller
+ *             and keys that share a weight need one each, to be added by the caller; overlap nothing
  * The workspace is needed for weights' gradients only.  Two launches, one without those.
  */
 int okt_norm_rotary_backward(const okt_norm_rotary* op, const void* d_q, const void* d_k, const void* d_dq, const void* d_dk,

@@ -44,6 +44,7 @@ struct RotArgs {
     uint32_t dim, rot, tile, groups, pair_shift;                     // tokens a tile; workgroups (backward); pairs rounded up, as a shift
     Divider length;
     int kind;
+    uint32_t axes;
     bool adjacent;
     float eps, share;                                                // share: 1 / dim
     const float* inv_freq;
@@ -456,6 +457,7 @@ static bool rot_args(const okt_norm_rotary* op, RotArgs& a) {
     while (1u << a.pair_shift < op->head_dim / 2) ++a.pair_shift;
     a.rot = op->rot_dim;
     a.kind = op->kind;
+    a.axes = op->axes;
     a.adjacent = op->adjacent != 0;
     a.eps = op->eps;
     a.inv_freq = op->d_inv_freq;
@@ -500,13 +502,28 @@ static bool reachable(int64_t apart, const Axis* axes, int n, int64_t dim) {
     return false;
 }
 
+static uint64_t placed_bytes(const RotArgs& a, const Placed& t, size_t e) {
+    const uint64_t batch = a.tokens / a.length.by, length = a.length.by;
+    return ((batch - 1) * t.s.batch + (length - 1) * t.s.row + (uint64_t)(t.heads - 1) * t.s.head + a.dim) * e;
+}
+
+// What a call reads beside the heads: weights, frequencies, positions.  Outputs are held apart from those by first and last element.
+static bool over_parameters(const RotArgs& a, const void* out, uint64_t bytes) {
+    const struct { const void* p; uint64_t bytes; } t[] = {
+        {a.t[0].weight, 4ull * a.dim}, {a.t[1].weight, 4ull * a.dim}, {a.rot ? a.inv_freq : nullptr, 2ull * a.rot},
+        {a.tokens && a.rot ? a.positions : nullptr,
+         a.tokens ? 4 * ((a.tokens / a.length.by - 1) * a.position_stride[0] + (a.length.by - 1) * a.position_stride[1] + a.axes) : 0}};
+    for (const auto& x : t)
+        if (x.p && overlap(out, bytes, x.p, x.bytes)) return true;
+    return false;
+}
+
 // Whether an output and another tensor share an element, one in the very place of the other aside, which the caller sees.  Where
 // their strides are alike, as parts of one projection's are, by their heads; else by their first and last elements.
 static bool clash(const RotArgs& a, const Placed& x, const Placed& y, size_t e) {
     if (!x.p || !y.p || !x.heads || !y.heads) return false;
     const uint64_t batch = a.tokens / a.length.by, length = a.length.by;
-    const auto extent = [&](const Placed& t) { return ((batch - 1) * t.s.batch + (length - 1) * t.s.row + (uint64_t)(t.heads - 1) * t.s.head + a.dim) * e; };
-    if (!overlap(x.p, extent(x), y.p, extent(y))) return false;
+    if (!overlap(x.p, placed_bytes(a, x, e), y.p, placed_bytes(a, y, e))) return false;
     if ((batch > 1 && x.s.batch != y.s.batch) || (length > 1 && x.s.row != y.s.row) || (x.heads > 1 && y.heads > 1 && x.s.head != y.s.head)) return true;
     const int64_t bytes = (int64_t)((uintptr_t)y.p - (uintptr_t)x.p);
     const int64_t b = (int64_t)batch - 1, l = (int64_t)length - 1;
@@ -572,6 +589,7 @@ int okt_norm_rotary_forward(const okt_norm_rotary* op, const void* d_q, const vo
         out[n] = {p.out[n], a.t[n].out, a.t[n].heads};
         if (!a.t[n].heads) continue;
         if (!p.x[n] || !p.out[n] || !aligned(p.x[n], e) || !aligned(p.out[n], e) || shares_places(a, a.t[n].out, a.t[n].heads)) return OKT_ERR_INVALID_ARG;
+        if (over_parameters(a, p.out[n], placed_bytes(a, out[n], e))) return OKT_ERR_INVALID_ARG;
     }
     if (clash(a, out[0], out[1], e)) return OKT_ERR_INVALID_ARG;
     for (int n = 0; n < 2; ++n)
@@ -598,6 +616,14 @@ int okt_norm_rotary_backward(const okt_norm_rotary* op, const void* d_q, const v
         if (!a.t[n].heads || a.tokens == 0) continue;
         if ((a.t[n].weight && !p.x[n]) || !p.d[n] || !p.out[n] || !aligned(p.x[n], e) || !aligned(p.d[n], e) || !aligned(p.out[n], e) ||
             shares_places(a, a.t[n].out, a.t[n].heads)) return OKT_ERR_INVALID_ARG;
+        if (over_parameters(a, p.out[n], placed_bytes(a, out[n], e))) return OKT_ERR_INVALID_ARG;
+    }
+    for (float* to : g.to) {                                         // of the weights, written by the second launch
+        if (!to) continue;
+        if (over_parameters(a, to, 4ull * a.dim)) return OKT_ERR_INVALID_ARG;
+        for (int n = 0; n < 2 && a.tokens; ++n)
+            for (const Placed& t : {in[n], d[n], out[n]})
+                if (t.p && t.heads && overlap(to, 4ull * a.dim, t.p, placed_bytes(a, t, e))) return OKT_ERR_INVALID_ARG;
     }
     if (g.to[0] && g.to[1] && overlap(g.to[0], 4ull * a.dim, g.to[1], 4ull * a.dim)) return OKT_ERR_INVALID_ARG;
     const bool sums = g.to[0] || g.to[1];

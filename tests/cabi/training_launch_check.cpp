@@ -165,6 +165,21 @@ static void rotation_places() {
     judge(run(0, k0, far, (H - G) * D), false, 0, "keys over the last queries", 0, 0, 0, 0);
     judge(run(0, k0, far, (H + G) * D), true, 1, "keys over the values", 0, 0, 0, 0);
     judge(run(0, k0, row * S * B, far), true, 1, "behind", 0, 0, 0, 0);
+    // a weight and the positions right before and behind the queries' output, and one element further in
+    const int64_t size = ((B * S - 1) * row + H * D) * 2;
+    char* out = base + 2 * far;
+    op.position_stride[0] = S;
+    op.position_stride[1] = 1;
+    for (int in : {0, 4}) {
+        op.d_q_weight = (const float*)(out - 4 * D + in);
+        judge(run(0, k0, far, 2 * far), in == 0, in == 0, "behind a weight", in, 0, 0, 0);
+        op.d_q_weight = (const float*)(out + size - in);
+        judge(run(0, k0, far, 2 * far), in == 0, in == 0, "before a weight", in, 0, 0, 0);
+        op.d_q_weight = nullptr;
+        op.d_positions = (const int32_t*)(out - 4 * B * S + in);
+        judge(run(0, k0, far, 2 * far), in == 0, in == 0, "behind the positions", in, 0, 0, 0);
+        op.d_positions = nullptr;
+    }
     // heads with q, k, v of each side by side
     for (uint64_t* s : {op.q_stride, op.k_stride, op.q_out_stride, op.k_out_stride}) s[2] = 3 * D;
     op.heads = op.kv_heads = 3;

@@ -129,6 +129,21 @@ def test_rotary_weights_gradients_are_apart():
         assert okt.load_library().okt_norm_rotary_backward(*args) == INVALID
 
 
+def test_rotary_outputs_are_apart_from_parameters():
+    """An output over a weight, the frequencies or the positions, from their first to their last element, and a weight's gradient over anything."""
+    lib, last = okt.load_library(), (4096 + 7 * 512 + 3 * 64 + 63) * 2          # of the queries
+    parts = [({"q_weight": AT[11]}, 256), ({"k_weight": AT[11]}, 256), ({"freq": AT[11]}, 128), ({"positions": AT[11], "by": (8, 1)}, 64)]
+    for change, size in parts:
+        struct = rotary_struct(**change)
+        for to in (AT[11], AT[11] + size - 2, AT[11] - last):
+            assert lib.okt_norm_rotary_forward(struct, AT[0], AT[1], to, AT[3], None) == INVALID, change
+            assert lib.okt_norm_rotary_backward(struct, *AT[:4], to, AT[5], None, None, None, 0, None) == INVALID, change
+    struct = rotary_struct(q_weight=AT[11], k_weight=AT[12], positions=AT[13])
+    for to in (AT[0] + last - 2, AT[1], AT[2], AT[3] - 252, AT[4], AT[5] + 128, AT[10] + 124, AT[11], AT[12] + 252, AT[13]):
+        assert lib.okt_norm_rotary_backward(struct, *AT[:6], to, None, AT[9], 1 << 30, None) == INVALID, to
+        assert lib.okt_norm_rotary_backward(struct, *AT[:6], None, to, AT[9], 1 << 30, None) == INVALID, to
+
+
 @pytest.mark.timeout(30)
 def test_rotary_without_a_batch_takes_any_length():
     lib = okt.load_library()
