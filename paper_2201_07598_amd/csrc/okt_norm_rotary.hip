@@ -11,6 +11,7 @@
 // has lost 2^-7 of a turn in fp32.  Then lanes take heads: eight elements a lane as two fours, which are the two halves of four pairs (or
 // four adjacent pairs), so a pair never leaves its lane and a norm's sums cross 8, 16 or 32 lanes inside the vector unit.
 #include <algorithm>
+#include <initializer_list>
 #include <math.h>
 
 #include "okt_attention_layout.h"
@@ -483,36 +484,64 @@ static bool rot_args(const okt_norm_rotary* op, RotArgs& a) {
 
 struct Placed { const void* p; HeadStrides s; uint32_t heads; };
 
+// Steps along an axis of a tensor, or of the place of one of its heads less that of another's.
+struct Axis { int64_t stride, least, most; };
+constexpr uint64_t ROT_FARTHEST = 1ull << 50;                        // elements: no memory has so many
+constexpr int ROT_TRIES = 1 << 14;
+
+// Elements from a tensor's first to behind its last one, where `n` are together and every axis makes so many steps of a stride; ROT_FARTHEST
+// where that is more.
+struct Steps { uint64_t count, stride; };
+static uint64_t extent(uint64_t n, std::initializer_list<Steps> axes) {
+    for (const Steps& t : axes)
+        if (t.count && t.stride) n = t.stride < (ROT_FARTHEST - n) / t.count ? n + t.count * t.stride : ROT_FARTHEST;
+    return n;
+}
+static uint64_t extent(const RotArgs& a, const HeadStrides& s, uint32_t heads) {
+    const uint32_t length = a.length.by, batch = a.tokens / length;
+    return extent(a.dim, {{batch - 1, s.batch}, {length - 1, s.row}, {heads - 1, s.head}});
+}
+
+// Whether `apart` elements are some steps along the axes, each axis' within its size, and less than a head's length besides. The axes by falling
+// stride: of each, the numbers of steps come into question whose rest those behind it can reach, which are two or fewer where a stride is more
+// than they reach together. Where strides lie otherwise there may be many; after `tries` of them all the answer is yes.
+static bool reachable(int64_t apart, const Axis* axes, int n, int64_t dim, int& tries) {
+    if (n == 0) return apart > -dim && apart < dim;
+    const int64_t stride = axes->stride;
+    if (stride == 0) return reachable(apart, axes + 1, n - 1, dim, tries);
+    int64_t low = apart - (dim - 1), high = apart + dim - 1;         // of what this axis' steps have to make
+    for (int i = 1; i < n; ++i) {
+        low -= axes[i].most * axes[i].stride;
+        high -= axes[i].least * axes[i].stride;
+    }
+    if (high < axes->least * stride || low > axes->most * stride) return false;
+    const int64_t first = low <= axes->least * stride ? axes->least : low / stride + (low % stride > 0);
+    const int64_t last = high >= axes->most * stride ? axes->most : high / stride - (high % stride < 0);
+    for (int64_t k = first; k <= last; ++k) {
+        if (n == 1 || tries-- <= 0) return true;                     // the steps of the last axis were chosen so
+        if (reachable(apart - k * stride, axes + 1, n - 1, dim, tries)) return true;
+    }
+    return false;
+}
+
+static void by_stride(Axis (&axes)[3]) {
+    std::sort(axes, axes + 3, [](const Axis& p, const Axis& q) { return p.stride > q.stride; });
+}
+
 // An output whose tokens or heads are the same memory.
 static bool shares_places(const RotArgs& a, const HeadStrides& s, uint32_t heads) {
     const uint32_t batch = a.tokens / a.length.by;
     return (batch > 1 && s.batch < a.dim) || (a.length.by > 1 && s.row < a.dim) || (heads > 1 && s.head < a.dim);
 }
 
-// Whether `apart` elements are some steps along the axes, each axis' within its size, and less than a head's length besides; the axes by
-// falling stride, so that of each only the two nearest numbers of steps come into question.
-struct Axis { int64_t stride, least, most; };
-static bool reachable(int64_t apart, const Axis* axes, int n, int64_t dim) {
-    if (n == 0) return apart > -dim && apart < dim;
-    if (axes->stride == 0) return reachable(apart, axes + 1, n - 1, dim);
-    int64_t q = apart / axes->stride;
-    if (apart % axes->stride < 0) --q;
-    for (int64_t k = q; k <= q + 1; ++k)
-        if (k <= axes->most && k >= axes->least && reachable(apart - k * axes->stride, axes + 1, n - 1, dim)) return true;
-    return false;
-}
-
-static uint64_t placed_bytes(const RotArgs& a, const Placed& t, size_t e) {
-    const uint64_t batch = a.tokens / a.length.by, length = a.length.by;
-    return ((batch - 1) * t.s.batch + (length - 1) * t.s.row + (uint64_t)(t.heads - 1) * t.s.head + a.dim) * e;
-}
+static uint64_t placed_bytes(const RotArgs& a, const Placed& t, size_t e) { return extent(a, t.s, t.heads) * e; }
 
 // What a call reads beside the heads: weights, frequencies, positions.  Outputs are held apart from those by first and last element.
 static bool over_parameters(const RotArgs& a, const void* out, uint64_t bytes) {
     const struct { const void* p; uint64_t bytes; } t[] = {
         {a.t[0].weight, 4ull * a.dim}, {a.t[1].weight, 4ull * a.dim}, {a.rot ? a.inv_freq : nullptr, 2ull * a.rot},
         {a.tokens && a.rot ? a.positions : nullptr,
-         a.tokens ? 4 * ((a.tokens / a.length.by - 1) * a.position_stride[0] + (a.length.by - 1) * a.position_stride[1] + a.axes) : 0}};
+         a.tokens ? 4 * extent(a.axes, {{a.tokens / a.length.by - 1, a.position_stride[0]}, {a.length.by - 1, a.position_stride[1]}}) : 0}};
     for (const auto& x : t)
         if (x.p && overlap(out, bytes, x.p, x.bytes)) return true;
     return false;
@@ -524,13 +553,15 @@ static bool clash(const RotArgs& a, const Placed& x, const Placed& y, size_t e) 
     if (!x.p || !y.p || !x.heads || !y.heads) return false;
     const uint64_t batch = a.tokens / a.length.by, length = a.length.by;
     if (!overlap(x.p, placed_bytes(a, x, e), y.p, placed_bytes(a, y, e))) return false;
+    if (extent(a, x.s, x.heads) >= ROT_FARTHEST || extent(a, y.s, y.heads) >= ROT_FARTHEST) return true;
     if ((batch > 1 && x.s.batch != y.s.batch) || (length > 1 && x.s.row != y.s.row) || (x.heads > 1 && y.heads > 1 && x.s.head != y.s.head)) return true;
     const int64_t bytes = (int64_t)((uintptr_t)y.p - (uintptr_t)x.p);
     const int64_t b = (int64_t)batch - 1, l = (int64_t)length - 1;
     Axis axes[3] = {{(int64_t)(batch > 1 ? x.s.batch : 0), -b, b}, {(int64_t)(length > 1 ? x.s.row : 0), -l, l},
                     {(int64_t)(x.heads > 1 ? x.s.head : y.heads > 1 ? y.s.head : 0), 1 - (int64_t)y.heads, (int64_t)x.heads - 1}};
-    std::sort(axes, axes + 3, [](const Axis& p, const Axis& q) { return p.stride > q.stride; });
-    return reachable(bytes / (int64_t)e, axes, 3, a.dim);
+    by_stride(axes);
+    int tries = ROT_TRIES;
+    return reachable(bytes / (int64_t)e, axes, 3, a.dim, tries);
 }
 static bool same(const RotArgs& a, const Placed& x, const Placed& y) {
     return x.p == y.p && (x.s.batch == y.s.batch || a.tokens == a.length.by) && (x.s.row == y.s.row || a.length.by == 1) &&

@@ -1,0 +1,101 @@
+// Host check of which places the rotation writes, without a GPU: thousands of small layouts, of which every element is listed one by one.
+//   pairs   with strides alike, outputs are refused exactly where they share an element with one another or with an input that lies elsewhere
+// Pointers are made up and never read.  Prints the number of cases and of violations.
+#include <cstdio>
+#include <cstring>
+#include <random>
+#include <set>
+
+#include "launch_stub.h"
+#include "okt.h"
+
+static long cases = 0, bad = 0, refused = 0;
+static char* at(uint64_t n) { return (char*)(n << 44); }
+
+struct Layout { uint32_t batch, length, heads, dim; uint64_t s[3]; };
+
+static std::set<int64_t> elements(const Layout& t, int64_t from, bool* twice = nullptr) {
+    std::set<int64_t> out;
+    for (uint32_t b = 0; b < t.batch; ++b)
+        for (uint32_t i = 0; i < t.length; ++i)
+            for (uint32_t h = 0; h < t.heads; ++h)
+                for (uint32_t e = 0; e < t.dim; ++e)
+                    if (!out.insert(from + (int64_t)(b * t.s[0] + i * t.s[1] + h * t.s[2] + e)).second && twice) *twice = true;
+    return out;
+}
+static bool meet(const std::set<int64_t>& a, const std::set<int64_t>& b) {
+    for (int64_t x : a)
+        if (b.count(x)) return true;
+    return false;
+}
+
+static okt_norm_rotary op_of(uint32_t batch, uint32_t length, uint32_t heads, uint32_t kv_heads, uint32_t dim) {
+    okt_norm_rotary op;
+    std::memset(&op, 0, sizeof op);
+    op.batch = batch;
+    op.length = length;
+    op.heads = heads;
+    op.kv_heads = kv_heads;
+    op.head_dim = op.rot_dim = dim;
+    op.dtype = OKT_BF16;
+    op.kind = OKT_NORM_RMS;
+    op.axes = 1;
+    op.d_inv_freq = (const float*)at(9);
+    return op;
+}
+static void put(uint64_t (&to)[3], const uint64_t (&s)[3]) { std::memcpy(to, s, sizeof to); }
+
+static void judge(int status, bool accepted, const char* what, const Layout& t, int64_t apart) {
+    ++cases;
+    refused += !accepted;
+    const bool launched = !g_launched.empty();
+    g_launched.clear();
+    if (status == (accepted ? OKT_OK : OKT_ERR_INVALID_ARG) && launched == accepted) return;
+    if (++bad < 20)
+        std::printf("%s: %u x %u x %u x %u, strides %llu %llu %llu, apart %lld: status %d where %s\n", what, t.batch, t.length, t.heads, t.dim,
+                    (unsigned long long)t.s[0], (unsigned long long)t.s[1], (unsigned long long)t.s[2], (long long)apart, status, accepted ? "it is fine" : "memory is shared");
+}
+
+static std::mt19937 rng(1);
+static uint32_t pick(uint32_t n) { return rng() % n; }
+
+static Layout random_layout() {
+    Layout t = {1 + pick(3), 1 + pick(4), 1 + pick(4), 8u * (1 + pick(3)), {}};
+    for (uint64_t& s : t.s) s = pick(5) == 0 ? 8 * pick(60) : (pick(2) ? t.dim : 8) * pick(14) + (pick(8) == 0 ? pick(8) : 0);
+    if (pick(2)) {                                                   // as they mostly lie: one axis inside the other, with and without gaps
+        uint64_t size = t.dim;
+        uint32_t order[3] = {0, 1, 2}, n[3] = {t.batch, t.length, t.heads};
+        for (int i = 2; i > 0; --i) std::swap(order[i], order[pick(i + 1)]);
+        for (uint32_t axis : order) {
+            t.s[axis] = size + (pick(3) == 0 ? 8 * pick(5) : 0) - (pick(6) == 0 ? 8 : 0);
+            size += t.s[axis] * (n[axis] - 1);
+        }
+    }
+    return t;
+}
+
+static void pairs() {
+    for (int n = 0; n < 40000; ++n) {
+        const Layout t = random_layout();
+        bool twice = false;
+        Layout k = t;
+        k.heads = 1 + pick(4);
+        const int64_t apart = pick(2) ? 8 * (int64_t)pick(200) - 800 : (int64_t)t.dim * (pick(60)) - 30 * (int64_t)t.dim;
+        const std::set<int64_t> q_out = elements(t, 0, &twice), k_out = elements(k, apart, &twice);
+        if (twice) continue;
+        okt_norm_rotary op = op_of(t.batch, t.length, t.heads, k.heads, t.dim);
+        for (uint64_t (*s)[3] : {&op.q_out_stride, &op.k_out_stride, &op.q_stride, &op.k_stride}) put(*s, t.s);
+        char* far = at(2);
+        judge(okt_norm_rotary_forward(&op, at(1), at(3), far, far + 2 * apart, nullptr), !meet(q_out, k_out), "outputs", t, apart);
+        judge(okt_norm_rotary_forward(&op, at(1), far + 2 * apart, far, at(3), nullptr), !meet(q_out, k_out), "over the other's input", t, apart);
+        const std::set<int64_t> q = elements(t, apart);
+        judge(okt_norm_rotary_forward(&op, far + 2 * apart, at(1), far, at(3), nullptr), apart == 0 || !meet(q_out, q), "over its own input", t, apart);
+    }
+}
+
+int main(int argc, char** argv) {
+    const std::string what = argc > 1 ? argv[1] : "";
+    if (what == "pairs") pairs();
+    std::printf("%ld cases, %ld to refuse, %ld violations\n", cases, refused, bad);
+    return bad || !cases ? 1 : 0;
+}
