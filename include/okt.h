@@ -720,7 +720,8 @@ typedef struct okt_norm_rotary {
 /* Bytes of workspace the backward pass needs (the forward pass needs none); 0 if sizes are out of range.  Pure host arithmetic. */
 size_t okt_norm_rotary_workspace_bytes(uint32_t batch, uint32_t length, uint32_t heads, uint32_t kv_heads, uint32_t head_dim);
 
-/* d_q_out may be d_q with its strides, d_k_out d_k; they overlap nothing otherwise.  One launch. */
+/* d_q_out may be d_q with its strides, d_k_out d_k; they overlap nothing otherwise, nor do two heads of one of them.  (Whether they do is worked out from
+ * the strides; where those lie so across one another that it takes more than 2^14 steps, the call is refused.)  One launch. */
 int okt_norm_rotary_forward(const okt_norm_rotary* op, const void* d_q, const void* d_k, void* d_q_out, void* d_k_out,
                             void* stream);
 

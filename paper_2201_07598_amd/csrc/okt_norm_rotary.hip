@@ -528,10 +528,22 @@ static void by_stride(Axis (&axes)[3]) {
     std::sort(axes, axes + 3, [](const Axis& p, const Axis& q) { return p.stride > q.stride; });
 }
 
-// An output whose tokens or heads are the same memory.
+// An output of which two heads share an element: some steps along the axes, the first of them forward, lead less than a head's length away.
 static bool shares_places(const RotArgs& a, const HeadStrides& s, uint32_t heads) {
-    const uint32_t batch = a.tokens / a.length.by;
-    return (batch > 1 && s.batch < a.dim) || (a.length.by > 1 && s.row < a.dim) || (heads > 1 && s.head < a.dim);
+    const int64_t batch = a.tokens / a.length.by, length = a.length.by;
+    if ((batch > 1 && s.batch < a.dim) || (length > 1 && s.row < a.dim) || (heads > 1 && s.head < a.dim)) return true;
+    if (extent(a, s, heads) >= ROT_FARTHEST) return true;
+    const auto axis = [](uint64_t stride, int64_t size) { return Axis{(int64_t)(size > 1 ? stride : 0), 1 - size, size - 1}; };
+    Axis axes[3] = {axis(s.batch, batch), axis(s.row, length), axis(s.head, heads)};
+    by_stride(axes);
+    int tries = ROT_TRIES;
+    for (int n = 0; n < 3 && axes[n].stride; ++n) {
+        Axis forward[3];
+        std::copy(axes, axes + 3, forward);
+        forward[n].least = 1;
+        if (reachable(0, forward + n, 3 - n, a.dim, tries)) return true;
+    }
+    return false;
 }
 
 static uint64_t placed_bytes(const RotArgs& a, const Placed& t, size_t e) { return extent(a, t.s, t.heads) * e; }

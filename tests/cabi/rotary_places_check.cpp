@@ -1,6 +1,9 @@
 // Host check of which places the rotation writes, without a GPU: thousands of small layouts, of which every element is listed one by one.
+//   self    an output is refused exactly where two of its heads share an element
 //   pairs   with strides alike, outputs are refused exactly where they share an element with one another or with an input that lies elsewhere
+//   far     strides and sizes at the ends of what the header allows: refused or launched, and soon
 // Pointers are made up and never read.  Prints the number of cases and of violations.
+#include <chrono>
 #include <cstdio>
 #include <cstring>
 #include <random>
@@ -74,6 +77,21 @@ static Layout random_layout() {
     return t;
 }
 
+static void self() {
+    for (int n = 0; n < 20000; ++n) {
+        const Layout t = random_layout();
+        bool twice = false;
+        elements(t, 0, &twice);
+        okt_norm_rotary op = op_of(t.batch, t.length, t.heads, 0, t.dim);
+        const uint64_t plain[3] = {(uint64_t)t.length * t.heads * t.dim, (uint64_t)t.heads * t.dim, t.dim};
+        put(op.q_stride, plain);
+        put(op.dq_stride, plain);
+        put(op.q_out_stride, t.s);
+        judge(okt_norm_rotary_forward(&op, at(1), nullptr, at(2), nullptr, nullptr), !twice, "self", t, 0);
+        judge(okt_norm_rotary_backward(&op, nullptr, nullptr, at(1), nullptr, at(2), nullptr, nullptr, nullptr, nullptr, 0, nullptr), !twice, "self backward", t, 0);
+    }
+}
+
 static void pairs() {
     for (int n = 0; n < 40000; ++n) {
         const Layout t = random_layout();
@@ -93,9 +111,32 @@ static void pairs() {
     }
 }
 
+static void far() {
+    const uint32_t most = (1u << 24) - 1;
+    const uint64_t top = 1ull << 40;
+    const struct { uint32_t batch, length, heads; uint64_t s[3]; int accepted; } t[] = {
+        {1, most, 1, {0, 8, 0}, 1}, {1, most, 1, {0, 7, 0}, 0}, {4095, 4096, 16, {4096 * 128, 128, 8}, 1}, {4095, 4096, 16, {4096 * 128 - 8, 128, 8}, 0},
+        {1, 1, 1u << 16, {0, 0, 8}, 1}, {2, 2, 2, {1u << 30, 1u << 20, 1u << 10}, 1},
+        // an extent that no memory has
+        {2, most / 2, 1, {top, top, 0}, 0}, {most, 1, 1, {top, 0, 0}, 0}, {4096, 4095, 1, {top, top - 8, 0}, 0},
+        // lengths that would take long to look through one by one: either answer, as long as it comes
+        {4096, 4095, 1u << 12, {8 * 4099, 8 * 4097, 8 * 4093}, -1}, {4096, 4095, 1u << 16, {8 * 65537, 8 * 65539, 8 * 65521}, -1}};
+    for (const auto& x : t) {
+        okt_norm_rotary op = op_of(x.batch, x.length, x.heads, 0, 8);
+        put(op.q_out_stride, x.s);
+        const auto begin = std::chrono::steady_clock::now();
+        const int status = okt_norm_rotary_forward(&op, at(1), nullptr, at(2), nullptr, nullptr);
+        const double seconds = std::chrono::duration<double>(std::chrono::steady_clock::now() - begin).count();
+        judge(status, x.accepted < 0 ? status == OKT_OK : x.accepted, "far", {x.batch, x.length, x.heads, 8, {x.s[0], x.s[1], x.s[2]}}, 0);
+        if (seconds > 0.05 && ++bad) std::printf("far: %u x %u x %u took %.2f s\n", x.batch, x.length, x.heads, seconds);
+    }
+}
+
 int main(int argc, char** argv) {
     const std::string what = argc > 1 ? argv[1] : "";
+    if (what == "self") self();
     if (what == "pairs") pairs();
+    if (what == "far") far();
     std::printf("%ld cases, %ld to refuse, %ld violations\n", cases, refused, bad);
     return bad || !cases ? 1 : 0;
 }

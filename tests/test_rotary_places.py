@@ -43,3 +43,23 @@ def test_keys_between_the_steps_of_queries():
     change = dict(batch=1, length=2, heads=3, kv_heads=3, strides=(10_000, 192, 128) * 6)
     for apart in (64, 128, 192, 256, 320):
         assert forward(AT[0], AT[1], AT[2], AT[2] + 2 * apart, **change) == INVALID, apart
+
+
+def test_an_output_that_overlaps_itself(places):
+    places("self")
+
+
+def test_ends_of_sizes_and_strides(places):
+    places("far")
+
+
+@pytest.mark.parametrize("sizes,strides", [
+    ((1, 2, 2), (10_000, 64, 64)), ((2, 2, 1), (512, 512, 64)), ((2, 1, 2), (64, 512, 64)), ((3, 3, 4), (8 * 64, 4 * 64 - 8, 64)), ((1, 3, 3), (0, 96, 192))])
+def test_two_heads_in_one_place(sizes, strides):
+    """Strides that are all a head's length or more, and yet two heads share elements."""
+    batch, length, heads = sizes
+    apart = (1 << 16, 1 << 12, 1 << 8)
+    change = dict(batch=batch, length=length, heads=heads, kv_heads=1)
+    assert forward(*AT[:4], strides=apart * 2 + strides + apart * 3, **change) == INVALID
+    struct = rotary_struct(strides=apart * 2 + strides + apart * 3, **change)
+    assert okt.load_library().okt_norm_rotary_backward(struct, None, None, *AT[2:6], None, None, None, 0, None) == INVALID
