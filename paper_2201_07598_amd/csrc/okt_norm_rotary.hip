@@ -155,12 +155,12 @@ __device__ __forceinline__ void rot_angles(const RotArgs& a, RotShared& s, uint3
 // Where a lane's two fours lie in a head, and back and forth between them and pairs.
 struct LanePlace {
     uint32_t first, second, unit;
-    bool there;
+    bool there, turned;                                              // unrotated elements pass: their partners' infinities times a sine of 0 are NaN
     template <int LANES>
     static __device__ __forceinline__ LanePlace of(const RotArgs& a) {
         const uint32_t unit = threadIdx.x % LANES;
         const bool apart = !a.adjacent && unit < a.rot / 8;
-        return {apart ? unit * 4 : unit * 8, apart ? a.rot / 2 + unit * 4 : unit * 8 + 4, unit, unit * 8 < a.dim};
+        return {apart ? unit * 4 : unit * 8, apart ? a.rot / 2 + unit * 4 : unit * 8 + 4, unit, unit * 8 < a.dim, unit * 8 < a.rot};
     }
     template <bool NT, typename T>
     __device__ __forceinline__ void store(T* head, const Eights& v, bool adjacent) const {
@@ -277,9 +277,9 @@ struct Forward {
                     c *= r;
                     d *= r;
                 }
-                if (at.there)
-                    at.template store<NT>(out + s.place[now.at[k].token].out[N] + (uint64_t)now.at[k].head * t.out.head,
-                             Eights{fma_four(v.a, c, -(v.b * d)), fma_four(v.a, d, v.b * c)}, a.adjacent);
+                Eights y = {fma_four(v.a, c, -(v.b * d)), fma_four(v.a, d, v.b * c)};
+                if (a.rot < a.dim && !at.turned) y = {v.a * c, v.b * c};
+                if (at.there) at.template store<NT>(out + s.place[now.at[k].token].out[N] + (uint64_t)now.at[k].head * t.out.head, y, a.adjacent);
             }
             now.load(a, s, at, walk, count, x, nullptr);
         }
@@ -325,6 +325,7 @@ struct Backward {
                 const f32x4 c = s.cosine[angle], e = s.sine[angle];
                 const Eights d = LanePlace::pairs({wide_four<T>(now.d[k][0]), wide_four<T>(now.d[k][1])}, a.adjacent);
                 Eights g = {fma_four(d.a, c, d.b * e), fma_four(d.b, c, -(d.a * e))};
+                if (a.rot < a.dim && !at.turned) g = d;
                 if (t.weight) {
                     Eights v = LanePlace::pairs({wide_four<T>(now.x[k][0]), wide_four<T>(now.x[k][1])}, a.adjacent);
                     const float r = head_statistics<LANES>(a, at, v);

@@ -1,0 +1,65 @@
+"""The operators at the ends of a training step where numbers end: infinities and NaN beside finite values, losses of nothing,
+denominators near nothing."""
+import pytest
+import torch
+
+import paper_2201_07598_amd as okt
+from operators_harness import DEV, rand
+from test_gpu_norm_rotary import Case, run_forward
+
+pytestmark = pytest.mark.gpu
+INF, NAN = float("inf"), float("nan")
+
+
+def same(a, b):
+    return torch.equal(torch.nan_to_num(a.float(), nan=1e30, posinf=2e30, neginf=-2e30), torch.nan_to_num(b.float(), nan=1e30, posinf=2e30, neginf=-2e30))
+
+
+# ------------------------------------------------------------------ rotation
+
+UNROTATED = [(kind, dim, rot, adjacent) for kind in ("f32", "bf16", "f16") for dim, rot in ((64, 32), (80, 0), (128, 120), (256, 8)) for adjacent in (False, True)]
+
+
+def spoil(t, clean, rot):
+    """Every element from `rot` on in a token of its own, in heads 0 to 2; where `clean` is what comes of it, it goes there as well."""
+    for i, e in enumerate(range(rot, t.shape[-1])):
+        for head, value in enumerate((INF, -INF, NAN)):
+            t[0, i, head, e] = value
+            clean[0, i, head, e] = value
+
+
+@pytest.mark.parametrize("kind,dim,rot,adjacent", UNROTATED)
+def test_what_is_not_rotated_stays_beside_anything(kind, dim, rot, adjacent):
+    c = Case(batch=1, length=dim - rot, heads=4, kv_heads=3, dim=dim, rot=rot, kind=kind, norm=None, adjacent=adjacent, seed=20)
+    clean = run_forward(c)
+    spoil(c.q, clean[0], rot)
+    spoil(c.k, clean[1], rot)
+    for got, want in zip(run_forward(c), clean):
+        assert same(got, want)
+
+
+@pytest.mark.parametrize("kind,dim,rot,adjacent", UNROTATED)
+def test_gradients_of_what_is_not_rotated_stay_beside_anything(kind, dim, rot, adjacent):
+    c = Case(batch=1, length=dim - rot, heads=4, kv_heads=3, dim=dim, rot=rot, kind=kind, norm=None, adjacent=adjacent, seed=21)
+    grads = [rand(c.q.shape, kind, 1), rand(c.k.shape, kind, 2)]
+    outs = [[torch.zeros_like(t) for t in grads] for _ in range(2)]
+    okt.okt_norm_rotary_backward(c.q, c.k, *grads, *outs[0], c.inv_freq, **c.options)
+    for g, clean in zip(grads, outs[0]):
+        spoil(g, clean, rot)
+    okt.okt_norm_rotary_backward(c.q, c.k, *grads, *outs[1], c.inv_freq, **c.options)
+    for got, want in zip(outs[1], outs[0]):
+        assert same(got, want)
+
+
+@pytest.mark.parametrize("kind,dim,rot,adjacent", UNROTATED)
+def test_normed_heads_with_an_infinity(kind, dim, rot, adjacent):
+    """The mean square is infinite and its root's reciprocal 0, so what is finite becomes 0 and the infinity itself NaN."""
+    c = Case(batch=1, length=dim - rot, heads=4, kv_heads=3, dim=dim, rot=rot, kind=kind, adjacent=adjacent, seed=22)
+    clean = run_forward(c)
+    for t, want in zip((c.q, c.k), clean):
+        want[0, :, 0] = 0.0
+        for i, e in enumerate(range(rot, dim)):
+            t[0, i, 0, e] = INF
+            want[0, i, 0, e] = NAN
+    for got, want in zip(run_forward(c), clean):
+        assert same(got + 0.0, want)
