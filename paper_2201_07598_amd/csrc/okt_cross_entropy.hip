@@ -310,10 +310,11 @@ __device__ __forceinline__ void part_of_rows(const CeArgs& a, const f32x16 (&c)[
 #pragma unroll
         for (int i = 0; i < S::MT * 16; ++i) top = fmaxf(top, s[i]);
         top = max_halves(top);
-        const float base = top == -__builtin_inff() ? 0.0f : -top * LOG2E;
+        // the largest is taken off first: off a rounded product with log2 e, its own exponential would not be 1 and a sure row's loss not 0
+        const float base = top == -__builtin_inff() ? 0.0f : top;
         float sum = 0.0f;
 #pragma unroll
-        for (int i = 0; i < S::MT * 16; ++i) sum += __builtin_amdgcn_exp2f(fmaf(s[i], LOG2E, base));
+        for (int i = 0; i < S::MT * 16; ++i) sum += __builtin_amdgcn_exp2f((s[i] - base) * LOG2E);
         sum = sum_halves(sum);
         if (lane < 32 && row < count)
             *reinterpret_cast<float2*>(a.stats + ((uint64_t)part * a.rows_pad + row) * 2) = make_float2(top, sum);
@@ -486,12 +487,12 @@ __global__ __launch_bounds__(S::THREADS) void cross_entropy_gradient_kernel(CeAr
         for (int n = 0; n < S::NT; ++n) {
             const uint32_t row = part_n * (S::NT * 32) + n * 32 + lane % 32;
             const bool there = row < count;
-            const float g = facts.g[n] * raise, base = -facts.lse[n] * LOG2E;
+            const float g = facts.g[n] * raise;
             const uint32_t mine = facts.label[n] - v0 - lane / 32 * 16;
             float s[S::MT * 16];
             logits_of_row<S>(s, c, n, bias, biased);
 #pragma unroll
-            for (int i = 0; i < S::MT * 16; ++i) s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], LOG2E, base));
+            for (int i = 0; i < S::MT * 16; ++i) s[i] = __builtin_amdgcn_exp2f((s[i] - facts.lse[n]) * LOG2E);
             if (__ballot(mine < S::MT * 32u)) {
 #pragma unroll
                 for (int m = 0; m < S::MT; ++m)

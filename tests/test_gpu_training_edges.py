@@ -5,6 +5,7 @@ import torch
 
 import paper_2201_07598_amd as okt
 from operators_harness import DEV, rand
+from test_gpu_cross_entropy import Case as Loss
 from test_gpu_norm_rotary import Case, run_forward
 
 pytestmark = pytest.mark.gpu
@@ -63,3 +64,33 @@ def test_normed_heads_with_an_infinity(kind, dim, rot, adjacent):
             want[0, i, 0, e] = NAN
     for got, want in zip(run_forward(c), clean):
         assert same(got + 0.0, want)
+
+
+# ------------------------------------------------------------------ cross entropy
+
+@pytest.mark.parametrize("kind", ["bf16", "f16"])
+@pytest.mark.parametrize("rows,vocab,bias", [(3, 1, False), (300, 1, True), (2100, 1, False), (300, 700, False), (130, 9000, True), (2600, 5001, True)])
+def test_a_sure_row_has_no_loss_and_no_gradient(rows, vocab, bias, kind):
+    """One logit, of 10 to 300, is 140 or more above all others (or the only one): its exponential is the whole sum, to the last bit."""
+    c = Loss(rows, 64, vocab, kind, bias=bias, seed=30)
+    c.weight.zero_()
+    c.weight[:, 0] = -1.0
+    c.weight[0, 0] = 1.0
+    c.labels.zero_()
+    c.y = c.labels.cpu()
+    c.h[:, 0] = torch.linspace(10.0 if vocab == 1 else 100.0, 300.0, rows, device=DEV).to(c.h.dtype)
+    loss, lse = c.forward()
+    dh, dw, db = c.backward(lse)
+    assert bool((lse > 9.0).all())
+    for t in (loss, dh, dw) + ((db,) if bias else ()):
+        assert not t.any()
+
+
+@pytest.mark.parametrize("rows,vocab", [(500, 40), (300, 1500), (2600, 5001)])
+def test_no_loss_is_below_nothing(rows, vocab):
+    """The sum has the largest entry's exponential, 1, and others that are not negative; so lse is the label's logit at least."""
+    c = Loss(rows, 96, vocab, bias=True, scale=40.0, seed=31)
+    logits = c.h.float() @ c.weight.float().t() + c.bias
+    c.labels.copy_(logits.argmax(1))
+    loss, _ = c.forward()
+    assert bool((loss >= 0).all()) and bool((loss == 0).any()) and bool((loss > 0).any())
