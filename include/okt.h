@@ -747,8 +747,8 @@ int okt_norm_rotary_backward(const okt_norm_rotary* op, const void* d_q, const v
  * The logits are made again, a piece of the vocabulary at a time.  Products are taken by the matrix units from 16-bit inputs with fp32
  * sums.  For the second products d is rounded to the tensors' type, so dh and dW have the precision of that type, also where dW is fp32 (so that it
  * can lie in the flat vector of the accumulate calls); with up to 256 labelled rows, where the rounding of single entries would show, d goes in as two
- * parts of that type.  d is rounded as a multiple of the largest |g|, so a g that all rows share costs nothing.  db is summed in fp32
- * before any rounding.  In fp16 a d below 2^-40 of the largest |g| is rounded to 0.  A bias of -infinity takes an entry out of the vocabulary.
+ * parts of that type.  d is rounded as a multiple of the largest finite |g|, so a g that all rows share costs nothing.  db is summed in fp32
+ * before any rounding.  In fp16 a d below 2^-40 of that |g| is rounded to 0.  A bias of -infinity takes an entry out of the vocabulary.
  * Tensors are rows of `width` contiguous elements, 16-byte aligned, strides (in elements; 0 stands for width) multiples of 8, at most
  * 2^20; an fp32 dW needs 4-byte alignment and any stride.
  */

@@ -56,7 +56,7 @@ struct CeArgs {
     const int64_t* labels;
     // workspace
     CeHeader* header;
-    float2* counts;                                                  // of every block: labelled rows (as bits), largest |g|
+    float2* counts;                                                  // of every block: labelled rows (as bits), largest finite |g|
     uint32_t* list;                                                  // numbers of the labelled rows
     int32_t* label_of;                                               // of listed row n
     void* h;                                                         // [rows_pad][width_pad]
@@ -81,14 +81,14 @@ constexpr uint32_t CE_DIRECT = 2048;                                 // up to so
 
 __device__ __forceinline__ bool labelled(int64_t y, uint32_t vocab) { return y >= 0 && y < (int64_t)vocab; }
 
-struct CeCount { uint32_t before, all; float top; };                 // labelled rows, and the largest |g| of those
+struct CeCount { uint32_t before, all; float top; };                 // labelled rows, and the largest finite |g| of those
 
 __device__ __forceinline__ CeCount count_together(CeCount c, CeCount (&waves)[CE_THREADS / WAVE]) {
 #pragma unroll
     for (int m = 1; m < WAVE; m <<= 1) {
         c.before += __shfl_xor(c.before, m, WAVE);
         c.all += __shfl_xor(c.all, m, WAVE);
-        c.top = fmaxf(c.top, __shfl_xor(c.top, m, WAVE));            // a NaN does not raise it
+        c.top = fmaxf(c.top, __shfl_xor(c.top, m, WAVE));
     }
     if (threadIdx.x % WAVE == 0) waves[threadIdx.x / WAVE] = c;
     __syncthreads();
@@ -104,7 +104,8 @@ __device__ __forceinline__ CeCount count_together(CeCount c, CeCount (&waves)[CE
 
 __device__ __forceinline__ CeCount count_row(const CeArgs& a, const float* dloss, uint64_t row, uint64_t first) {
     if (row >= a.rows || !labelled(a.labels[row], a.vocab)) return {0, 0, 0.0f};
-    return {row < first ? 1u : 0u, 1u, dloss ? fabsf(dloss[row * a.dloss_step]) : 0.0f};
+    const float g = dloss ? fabsf(dloss[row * a.dloss_step]) : 0.0f;
+    return {row < first ? 1u : 0u, 1u, g < __builtin_inff() ? g : 0.0f};      // what is not finite is its own row's alone
 }
 
 __device__ __forceinline__ void add_to(CeCount& c, const CeCount& more) {
@@ -144,7 +145,7 @@ __global__ __launch_bounds__(CE_THREADS) void cross_entropy_gather_kernel(CeArgs
     c = count_together(c, waves);
     if (blockIdx.x == 0 && threadIdx.x == 0) {
         int e = 0;                                                   // top = half 2^(e - 1), half in [1, 2)
-        const bool use = c.top > 0.0f && c.top < __builtin_inff();
+        const bool use = c.top > 0.0f;
         const float half = use ? 2.0f * frexpf(c.top, &e) : 1.0f;
         const int by = use && __is_same(T, _Float16) ? min(16 - e, 120) : 0;
         *a.header = {c.all, ldexpf(1.0f / half, by), ldexpf(half, -by), 0};

@@ -94,3 +94,19 @@ def test_no_loss_is_below_nothing(rows, vocab):
     c.labels.copy_(logits.argmax(1))
     loss, _ = c.forward()
     assert bool((loss >= 0).all()) and bool((loss == 0).any()) and bool((loss > 0).any())
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f16"])
+@pytest.mark.parametrize("value", [INF, -INF, NAN])
+@pytest.mark.parametrize("rows", [300, 3000])
+def test_a_gradient_that_is_not_finite_stays_in_its_row(rows, value, kind):
+    """The largest finite one is what all others are rounded as multiples of."""
+    c = Loss(rows, 64, 900, kind, seed=32)
+    _, lse = c.forward()
+    clean = c.backward(lse)[0]
+    order = c.g.abs().argsort()
+    at = int(order[rows // 2])
+    c.g[at] = value
+    dh = c.backward(lse)[0]
+    rest = torch.arange(rows, device=DEV) != at
+    assert torch.equal(dh[rest], clean[rest]) and not bool(torch.isfinite(dh[at]).any())
