@@ -844,7 +844,7 @@ typedef struct okt_adamw {
     uint32_t site;
     double lr;                    /* finite; not looked at with d_lr */
     double beta1, beta2;          /* 0 <= beta < 1 */
-    double eps;                   /* >= 0 */
+    double eps;                   /* >= 0; above 0 it is taken as 2^-126 at least */
     const int64_t* d_step;        /* int64[1] on the device: t; below 1 is taken as 1 */
     const float* d_lr;            /* fp32[1] on the device, or NULL */
     const float* d_grad_scale;    /* fp32[1] on the device, or NULL for 1 */

@@ -164,7 +164,7 @@ __device__ __forceinline__ float adam_element(float p, float g, float& m, float&
     m = a.beta1 * m + a.rest1 * g;
     v = a.beta2 * v + a.rest2 * g * g;
     w = sqrtf(v);
-    // a denominator is 0 or above 2^-75, so its reciprocal is good to an ulp
+    // a root is 0 or above 2^-75 and eps 0 or a normal number, so the reciprocal is good to an ulp
     return p * r.keep - r.size * (m * __builtin_amdgcn_rcpf(w * r.root + a.eps));
 }
 
@@ -386,7 +386,7 @@ int okt_adamw_step(const okt_adamw* op, const void* d_plan, void* stream) {
     if (op->chunks == 0) return OKT_OK;
     if (!d_plan || !aligned(d_plan, 16)) return OKT_ERR_INVALID_ARG;
     const AdamScalars a = {op->d_step, op->d_lr, op->d_grad_scale, op->d_skip, op->d_seed, log(op->beta1), log(op->beta2), op->lr,
-                           (float)op->beta1, (float)op->beta2, (float)(1.0 - op->beta1), (float)(1.0 - op->beta2), (float)op->eps, op->site};
+                           (float)op->beta1, (float)op->beta2, (float)(1.0 - op->beta1), (float)(1.0 - op->beta2), op->eps > 0.0 ? fmaxf((float)op->eps, 0x1p-126f) : 0.0f, op->site};
     const hipStream_t s = (hipStream_t)stream;
     const AdamTensor* tensors = (const AdamTensor*)d_plan;
     const uint32_t* tensor_of = (const uint32_t*)(tensors + op->tensors);

@@ -5,6 +5,7 @@ import torch
 
 import paper_2201_07598_amd as okt
 from operators_harness import DEV, rand
+from test_gpu_adamw import State, int64
 from test_gpu_cross_entropy import Case as Loss
 from test_gpu_norm_rotary import Case, run_forward
 
@@ -110,3 +111,17 @@ def test_a_gradient_that_is_not_finite_stays_in_its_row(rows, value, kind):
     dh = c.backward(lse)[0]
     rest = torch.arange(rows, device=DEV) != at
     assert torch.equal(dh[rest], clean[rest]) and not bool(torch.isfinite(dh[at]).any())
+
+
+# ------------------------------------------------------------------ AdamW
+
+@pytest.mark.parametrize("eight", [False, True])
+@pytest.mark.parametrize("eps", [1e-8, 1e-38, 3e-39, 1e-45, 1e-60, 2.0 ** -1074])
+def test_any_eps_above_zero_divides_nothing_by_something(eps, eight):
+    """Averages and gradients of 0 change no parameter, as 0 over eps is 0."""
+    s = State([300], seed=33, eight=eight)
+    for t in (s.g_all, s.m_all, s.v_all):
+        t.view(torch.uint8).zero_()
+    p = s.p[0].clone()
+    okt.okt_adamw_step(s.plan(), int64(3), lr=0.1, eps=eps)
+    assert torch.equal(s.p[0], p)
