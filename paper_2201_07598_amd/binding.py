@@ -818,7 +818,8 @@ def _rotary_struct(dtype, shape, kv_heads, inv_freq, positions, axis_of_pair, ad
         axes = 1 if table.count(0) == pairs else max(table) + 1
     if positions is not None:
         places = positions.shape
-        if len(places) == 3 or (len(places) == 2 and axes > 1):
+        # two sizes are [batch, length] where they can be and one axis turns all pairs, else [length, axes]
+        if len(places) == 3 or (len(places) == 2 and (axes > 1 or (places[0] == length and places != (batch, length)))):
             axes = max(axes, places[-1])
     at, by_batch, by_token = _positions(positions, batch, length, axes)
     return _ROTARY.pack(

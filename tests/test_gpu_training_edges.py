@@ -67,6 +67,19 @@ def test_normed_heads_with_an_infinity(kind, dim, rot, adjacent):
         assert same(got + 0.0, want)
 
 
+@pytest.mark.parametrize("places", ["one row for all", "a row a sequence"])
+def test_positions_of_several_axes_turned_by_the_first(places):
+    """Without axis_of_pair the first axis turns all pairs, however many the positions have."""
+    c = Case(batch=2, length=6, seed=23)
+    room = torch.randint(0, 1000, (6, 3) if places == "one row for all" else (2, 6, 3), generator=torch.Generator().manual_seed(1)).to(torch.int32).to(DEV)
+    first = room[..., 0].contiguous().expand(2, 6).unsqueeze(-1)
+    c.options["positions"] = first
+    want = run_forward(c)
+    c.options["positions"] = room
+    for got, plain in zip(run_forward(c), want):
+        assert torch.equal(got, plain)
+
+
 # ------------------------------------------------------------------ cross entropy
 
 @pytest.mark.parametrize("kind", ["bf16", "f16"])
