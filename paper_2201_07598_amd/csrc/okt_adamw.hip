@@ -379,7 +379,7 @@ int okt_adamw_step(const okt_adamw* op, const void* d_plan, void* stream) {
     if (!op || (op->state != OKT_STATE_F32 && op->state != OKT_STATE_E4M3) || op->tensors == 0 || op->chunks > ADAM_MAX_CHUNKS)
         return OKT_ERR_INVALID_ARG;
     const auto share = [](double b) { return b >= 0.0 && b < 1.0; };
-    if (!share(op->beta1) || !share(op->beta2) || !(op->eps >= 0.0) || !isfinite(op->eps) || !isfinite((float)op->lr)) return OKT_ERR_INVALID_ARG;
+    if (!share(op->beta1) || !share(op->beta2) || !(op->eps >= 0.0) || !isfinite(op->eps) || (!op->d_lr && !isfinite((float)op->lr))) return OKT_ERR_INVALID_ARG;
     if (!op->d_step || !aligned(op->d_step, 8) || !aligned(op->d_seed, 8)) return OKT_ERR_INVALID_ARG;
     for (const float* p : {op->d_lr, op->d_grad_scale, op->d_skip})
         if (!aligned(p, 4)) return OKT_ERR_INVALID_ARG;
