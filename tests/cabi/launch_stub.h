@@ -4,15 +4,14 @@
 #define LAUNCH_STUB_H
 
 #include <cstdint>
-#include <cstdlib>
 #include <string>
 #include <vector>
 
-#include <cxxabi.h>
 #include <dlfcn.h>
 
 struct LaunchDim { uint32_t x, y, z; };
-struct Launched { std::string kernel; LaunchDim grid, block; };
+struct Launched { std::string kernel;            // as the linker knows it
+                  LaunchDim grid, block; };
 static std::vector<Launched> g_launched;
 
 extern "C" {
@@ -30,13 +29,7 @@ int __hipPopCallConfiguration(LaunchDim* grid, LaunchDim* block, size_t* shared,
 }
 int hipLaunchKernel(const void* kernel, LaunchDim grid, LaunchDim block, void**, size_t, void*) {
     Dl_info info;
-    std::string name;
-    if (dladdr(kernel, &info) && info.dli_sname) {
-        int status = 0;
-        char* plain = abi::__cxa_demangle(info.dli_sname, nullptr, nullptr, &status);
-        name = plain ? plain : info.dli_sname;
-        std::free(plain);
-    }
+    const char* name = dladdr(kernel, &info) && info.dli_sname ? info.dli_sname : "";
     g_launched.push_back({name, grid, block});
     return 0;
 }
