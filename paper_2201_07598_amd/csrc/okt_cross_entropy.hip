@@ -21,6 +21,7 @@
 // (1.34 PFLOP/s) and 20.1 backward (1.71: operands near 0 take less power).  15 % of 16384 rows x 1024 x 30522 with a bias: 147 to 163 us
 // forward, of which the launches before and behind the product are 15 to 20, and 474 to 487 backward.  One row to a few
 // hundred: W's way from memory, and two launches (125 x 776 x 10007 fp16 15 us).
+#include <algorithm>
 #include <math.h>
 
 #include "okt_product.h"
@@ -60,14 +61,14 @@ struct CeArgs {
     uint32_t* list;                                                  // numbers of the labelled rows
     int32_t* label_of;                                               // of listed row n
     void* h;                                                         // [rows_pad][width_pad]
-    float* stats;                                                    // forward: [parts][rows_pad][2]; parts of 32 columns at least
+    float* stats;                                                    // forward: [parts][rows_pad][2], see ce_stats_columns
     float* said;                                                     // forward: s_ny
     float *lse_of, *g_of;                                            // backward, of listed row n
     void* d;                                                         // [rows_pad][piece]
     void* d_rest;                                                    // [CE_FINE_ROWS][piece]: what d's rounding left off
     float* dw_sums;                                                  // [parts][columns of whole tiles][width_pad]
     float* dh_sums;                                                  // [parts][rows of whole tiles][width_pad]
-    float* dbias_sums;                                               // [parts][vocab_pad]; parts of 32 rows at least
+    float* dbias_sums;                                               // [parts][vocab_pad], see ce_dbias_rows
     uint32_t piece, vocab_pad;
     uint32_t logit_tile_n, logit_parts_n;                            // rows of a tile of logits, and parts they leave of the bias's gradient
     __device__ __forceinline__ uint32_t dbias_parts(uint32_t count) const { return (count + logit_tile_n - 1) / logit_tile_n * logit_parts_n; }
@@ -726,6 +727,11 @@ static bool ce_small_split(uint64_t m, uint64_t n, uint64_t k) {
     return n <= 128 || tiles * (parts ? parts : 1) < 200;
 }
 
+// Columns and rows of the least part of a tile of logits that leaves its sums by itself: what one of its waves has.  (Which of the small tiles are
+// taken is seen at the launch.)
+static uint32_t ce_stats_columns(bool small) { return 32 * (small ? std::min(Thin::MT, Spread::MT) : Large::MT); }
+static uint32_t ce_dbias_rows(bool small) { return 32 * (small ? std::min(Thin::NT, Spread::NT) : Large::NT); }
+
 static bool ce_plan(uint64_t rows, uint32_t width, uint32_t vocab, CePlan& p) {
     if (rows > CE_MAX || vocab == 0 || vocab > CE_MAX || width < 8 || width > CE_MAX_WIDTH || width % 8 != 0) return false;
     const uint64_t some = rows ? rows : 1;
@@ -768,7 +774,7 @@ static bool ce_plan(uint64_t rows, uint32_t width, uint32_t vocab, CePlan& p) {
     p.label_at = place(4ull * p.rows_pad);
     p.h_at = place(2ull * p.rows_pad * p.width_pad);
     const size_t shared = at;
-    p.stats_at = place(8ull * p.rows_pad * (p.vocab_pad / 32));
+    p.stats_at = place(8ull * p.rows_pad * (p.vocab_pad / ce_stats_columns(p.small_logits)));
     p.said_at = place(4ull * p.rows_pad);
     p.forward_bytes = at;
     at = shared;
@@ -781,7 +787,7 @@ static bool ce_plan(uint64_t rows, uint32_t width, uint32_t vocab, CePlan& p) {
     const uint64_t once = ((uint64_t)p.rows_pad + CE_FINE_ROWS) * p.width_pad;
     p.dh_at = place(4 * (once > parts(p.small_products) ? once : parts(p.small_products)));
     p.dw_at = place(p.split_dweight ? 4 * parts(p.small_products) : 0);
-    p.dbias_at = place(4ull * (p.rows_pad / 32) * p.vocab_pad);
+    p.dbias_at = place(4ull * (p.rows_pad / ce_dbias_rows(p.small_logits)) * p.vocab_pad);
     p.backward_bytes = at;
     return true;
 }

@@ -36,6 +36,21 @@ def test_loss_and_gradients(n):
         assert a is None or torch.equal(a, b)
 
 
+@pytest.mark.parametrize("rows,width,vocab,labelled", [(2, 8, 3, 1.0), (125, 776, 10_007, 1.0), (120, 40_000 // 64 * 8, 9000, 0.5), (300, 64, 777, 1.0), (2049, 64, 700, 1.0),
+                                                     (2600, 64, 5001, 0.9), (10, 256, 70_000, 1.0), (16_384, 64, 4000, 1.0), (65_000, 64, 16_500, 0.02)])
+def test_nothing_is_written_behind_the_workspace(rows, width, vocab, labelled):
+    c = Case(rows, width, vocab, labelled=labelled, bias=True, seed=250)
+    room, c.ws = c.ws, None
+    guard = torch.full((room.numel() + (1 << 22),), 171, dtype=torch.uint8, device=DEV)
+    c.ws = guard[:room.numel()]
+    loss, lse = c.forward()
+    c.backward(lse)
+    assert bool((guard[room.numel():] == 171).all())
+    c.ws = room
+    again = c.forward()
+    assert torch.equal(loss, again[0]) and torch.equal(lse, again[1])
+
+
 # ------------------------------------------------------------------ rotation
 
 # one call moves more than 256 MiB, a sequence of it less

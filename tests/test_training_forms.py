@@ -6,6 +6,7 @@ import subprocess
 
 import pytest
 
+import paper_2201_07598_amd as okt
 import test_gpu_training_sizes as sizes
 from test_operators_abi import ROOT
 
@@ -57,3 +58,15 @@ def test_steps(launched, n):
     for length in lengths:
         if length:
             assert "adamw_kernelILb%dELb0E" % eight in launched("adamw", eight, length)[0]
+
+
+@pytest.mark.parametrize("rows,width,vocab", [(8192, 4096, 128_000), (131_072, 1024, 128_000), (16_384, 1024, 30_522)])
+def test_a_workspace_has_room_for_the_parts_of_large_tiles(rows, width, vocab):
+    """A wave of a large tile leaves two numbers for 128 columns of a row, and one for 64 rows of a column; d of a piece is a GiB or 4096 columns, and the rest
+    are vectors and sums of dh and dW."""
+    pad = lambda n, by: -(-n // by) * by  # noqa: E731
+    stats = 8 * rows * pad(vocab, 256) // 128
+    dbias = 4 * rows // 64 * pad(vocab, 256)
+    d = 2 * rows * max(4096, 2 ** 30 // (2 * rows))
+    others = rows * (2 + 4) * pad(width, 64) + 20 * rows + 4 * 256 * 256 * 256 + 2 * 256 * (d // rows) + (1 << 20)
+    assert okt.okt_cross_entropy_workspace_bytes(rows, width, vocab) <= max(stats, dbias + d) + others
