@@ -801,7 +801,8 @@ int okt_cross_entropy_backward(const okt_cross_entropy* op, const void* d_h, con
  * all zero codes, with any finite scales, are averages of zero.  A magnitude y between neighbouring values a < b of e4m3 becomes one of them by the
  * 16-bit value r of the random field (okt_dropout), 2^15 without d_seed: m becomes b where frac + r / 2^16 >= 1 with
  * frac = (y - a) / (b - a) to 20 bits, so its expectation is y and 2^15 rounds to nearest; the root becomes b where y^2 - a^2 >
- * r / 2^16 (b^2 - a^2), so the expectation of its square is y^2.  A v above 0 never becomes 0.  Element e of tensor i of the plan:
+ * r / 2^16 (b^2 - a^2), so the expectation of its square is y^2.  A v above 0 never becomes 0: below the
+ * least value of e4m3 its root is that value, so there the expectation is above v.  Element e of tensor i of the plan:
  * c0 = (e / 4) mod 2^32, c1 = (e / 4) >> 32, c2 = i; value e % 4 for m, 4 + e % 4 for v.
  * Rounded to nearest, an average moves only where a step changes it by half a code; give a seed.  A block with a NaN or an infinity
  * has the scale NaN and codes 0: all of it is NaN from then on.
@@ -832,7 +833,8 @@ size_t okt_adamw_plan_bytes(const okt_adamw_tensor* h_tensors, uint32_t count);
 
 /*
  * Checks the tensors and writes their plan to HOST memory (8-byte aligned, plan_bytes of it); the caller copies it to the device
- * (16-byte aligned) and keeps it there as long as the tensors stay where they are.  No GPU.
+ * (16-byte aligned) and keeps it there as long as the tensors, gradients among them, stay where they are; it is made again for others.  (It sorts what all tensors
+ * take up, in the plan's own memory, which holds nothing of use after a refusal.)  No GPU.
  *   h_chunks_out  out  what okt_adamw.chunks has to be
  */
 int okt_adamw_plan(const okt_adamw_tensor* h_tensors, uint32_t count, int state, void* h_plan_out, size_t plan_bytes,

@@ -967,7 +967,7 @@ ADAMW_BLOCK = 256                               # OKT_ADAMW_BLOCK
 
 class AdamWPlan:
     """What okt_adamw_step needs of its tensors, on their device; keeps them alive.  To be made again when one of
-    them moves (okt_adamw_plan); their contents may change at will."""
+    them moves (okt_adamw_plan), a gradient too, so gradients are to be written in place; their contents may change at will."""
 
     def __init__(self, device_bytes, tensors, chunks, state, held):
         self.device_bytes, self.tensors, self.chunks, self.state, self.held = device_bytes, tensors, chunks, state, held

@@ -10,7 +10,7 @@
 // Forward, a tile of logits is a matrix product whose epilogue leaves the largest and the sum of exponentials of its part of a row; a
 // second kernel joins a row's parts.  Backward the logits are made again, a piece of the vocabulary at a time, and leave the
 // epilogue as d, rounded to the tensors' type, in the workspace; two more products take it from there.  dW of a piece is final; dh
-// is summed over the pieces in fp32.  Four products where a kept matrix of logits would need three.
+// is summed over the pieces in fp32.  Both passes together make four products where a kept matrix of logits would need three.
 //
 // d is taken times a factor that makes the largest |g| a power of two, and the sums times its reciprocal: the gradient of a mean is one
 // number for all rows, and its rounding, the same in every entry, would be an error of the whole result (the largest entry of a row is
@@ -18,9 +18,9 @@
 // over the number of rows and p one over the vocabulary's size, and fp16 ends at 2^-24.
 //
 // The matrix units bound the large sizes, at the clock that their power leaves: 8192 rows x 4096 x 128000 bf16 take 6.4 ms forward
-// (1.34 PFLOP/s) and 20.1 backward (1.71: operands near 0 take less power).  15 % of 16384 rows x 1024 x 30522 with a bias: 147 to 163 us
-// forward, of which the launches before and behind the product are 15 to 20, and 474 to 487 backward.  One row to a few
-// hundred: W's way from memory, and two launches (125 x 776 x 10007 fp16 15 us).
+// (1.34 PFLOP/s) and 20.0 backward (three products, 1.29: logits 1.31, dh 1.37, dW, of whose operands both have to be turned, 1.24).  15 % of
+// 16384 rows x 1024 x 30522 with a bias: 149 to 165 us forward, of which the launches before and behind the product are 15 to 20, and 470 to 488
+// backward, 511 with dW in fp32.  One row to a few hundred: W's way from memory, and two launches (125 x 776 x 10007 fp16 15 us).
 #include <algorithm>
 #include <math.h>
 
@@ -32,7 +32,7 @@ constexpr uint32_t CE_PAD = 256;                                     // rows, an
 constexpr uint64_t CE_PIECE_BYTES = 1ull << 30;                    // of d in the workspace
 constexpr uint32_t CE_SPLIT_TILES = 256;                             // of a gradient, with the parts that its sum is dealt to where tiles are fewer
 constexpr uint32_t CE_SPLIT_PIECES = 8;                              // pieces of k that a part has at least: fewer are not worth their sums' way
-constexpr uint32_t CE_FINE_ROWS = 256;                               // up to so many, d goes into the second products in two parts
+constexpr uint32_t CE_FINE_ROWS = 256;                               // up to so many, d goes into the second products in two parts (256 x 4096 x 128000 1776 us, 300 rows, in one, 1515)
 constexpr uint32_t CE_MAX = 1u << 22;                                // rows, vocabulary
 constexpr uint32_t CE_MAX_WIDTH = 1u << 15;
 constexpr int CE_THREADS = 256;
@@ -718,7 +718,8 @@ struct CePlan {
 
 static uint64_t ce_up(uint64_t n, uint64_t by) { return (n + by - 1) / by * by; }
 
-// Tiles of 256 x 256 where they fill the chip, else of 128 x 128, two workgroups a CU.
+// Tiles of 256 x 256 where they fill the chip, else of 128 x 128, two workgroups a CU; and those for up to 128 rows, of which the others are half
+// zeros (x 4096 x 128000, forward: 128 rows 217 us in small tiles, 270 in large ones; 129 rows 329 and 271, 513 785 and 616; 300 x 1024 x 30522 43.7 and 37.2).
 static bool ce_small(uint64_t m, uint64_t n) { return n <= 128 || (m + 255) / 256 * ((n + 255) / 256) < 200; }
 
 // The same where a sum over k can be dealt to several workgroups.
@@ -748,7 +749,7 @@ static bool ce_plan(uint64_t rows, uint32_t width, uint32_t vocab, CePlan& p) {
     p.logit_groups = tile_groups(tiles(vocab, p.small_logits) * tiles(some, p.small_logits));
     p.piece_groups = tile_groups(tiles(p.piece, p.small_logits) * tiles(some, p.small_logits));
     if (p.logit_groups > UINT32_MAX / 2) return false;
-    // few rows, for which dW is much to write and little to sum (10 x 256 x 100000: 108 -> 83 us, 100 x 4096 x 60000 628 -> 552;
+    // few rows, for which dW is much to write and little to sum (10 x 256 x 100000: 108 -> 83 to 87 us, 100 x 4096 x 60000 628 -> 552 to 574;
     // 45 x 1632 x 2982, with few tiles, would go from 42 to 50)
     p.narrow_products = some <= CE_FINE_ROWS && tiles(p.width_pad, true) * tiles(p.piece, true) > 1024;
     if (p.narrow_products) p.small_products = true;

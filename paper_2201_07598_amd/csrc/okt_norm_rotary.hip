@@ -24,7 +24,8 @@ constexpr uint32_t ROT_MAX_DIM = 256, ROT_MAX_TOKENS = 32;           // of a wor
 constexpr uint32_t ROT_ANGLES = 1024;                                // a workgroup's tokens times pairs
 constexpr uint32_t ROT_BACKWARD_GROUPS = 1024;
 // Heads of a lane that are on their way together.  (8 x 4096 tokens of 16 + 4 heads of 128 bf16, backward: one 119 us, two 108, four 128,
-// which takes registers of half the waves; forward two and four 74, one 83.)
+// which takes registers of half the waves; forward two and four 74, one 83.  fp32, of twice the registers: backward one 191, two 202, forward one 129 and
+// two 125; 3 x 1001 tokens of 12 + 12 heads of 80 22.0 and 28.4, forward 12.5 and 12.7.)
 template <typename T> constexpr int ROT_AHEAD = 2;
 template <> constexpr int ROT_AHEAD<float> = 1;
 // Calls that move more than this go around the caches, of which they would find nothing again (the sizes above: 73 and 108 us through them, 68 and 102
