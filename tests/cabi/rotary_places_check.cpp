@@ -48,7 +48,7 @@ static okt_norm_rotary op_of(uint32_t batch, uint32_t length, uint32_t heads, ui
 }
 static void put(uint64_t (&to)[3], const uint64_t (&s)[3]) { std::memcpy(to, s, sizeof to); }
 
-static void judge(int status, bool accepted, const char* what, const Layout& t, int64_t apart) {
+static void expect(int status, bool accepted, const char* what, const Layout& t, int64_t apart) {
     ++cases;
     refused += !accepted;
     const bool launched = !g_launched.empty();
@@ -87,8 +87,8 @@ static void self() {
         put(op.q_stride, plain);
         put(op.dq_stride, plain);
         put(op.q_out_stride, t.s);
-        judge(okt_norm_rotary_forward(&op, at(1), nullptr, at(2), nullptr, nullptr), !twice, "self", t, 0);
-        judge(okt_norm_rotary_backward(&op, nullptr, nullptr, at(1), nullptr, at(2), nullptr, nullptr, nullptr, nullptr, 0, nullptr), !twice, "self backward", t, 0);
+        expect(okt_norm_rotary_forward(&op, at(1), nullptr, at(2), nullptr, nullptr), !twice, "self", t, 0);
+        expect(okt_norm_rotary_backward(&op, nullptr, nullptr, at(1), nullptr, at(2), nullptr, nullptr, nullptr, nullptr, 0, nullptr), !twice, "self backward", t, 0);
     }
 }
 
@@ -104,10 +104,10 @@ static void pairs() {
         okt_norm_rotary op = op_of(t.batch, t.length, t.heads, k.heads, t.dim);
         for (uint64_t (*s)[3] : {&op.q_out_stride, &op.k_out_stride, &op.q_stride, &op.k_stride}) put(*s, t.s);
         char* far = at(2);
-        judge(okt_norm_rotary_forward(&op, at(1), at(3), far, far + 2 * apart, nullptr), !meet(q_out, k_out), "outputs", t, apart);
-        judge(okt_norm_rotary_forward(&op, at(1), far + 2 * apart, far, at(3), nullptr), !meet(q_out, k_out), "over the other's input", t, apart);
+        expect(okt_norm_rotary_forward(&op, at(1), at(3), far, far + 2 * apart, nullptr), !meet(q_out, k_out), "outputs", t, apart);
+        expect(okt_norm_rotary_forward(&op, at(1), far + 2 * apart, far, at(3), nullptr), !meet(q_out, k_out), "over the other's input", t, apart);
         const std::set<int64_t> q = elements(t, apart);
-        judge(okt_norm_rotary_forward(&op, far + 2 * apart, at(1), far, at(3), nullptr), apart == 0 || !meet(q_out, q), "over its own input", t, apart);
+        expect(okt_norm_rotary_forward(&op, far + 2 * apart, at(1), far, at(3), nullptr), apart == 0 || !meet(q_out, q), "over its own input", t, apart);
     }
 }
 
@@ -127,7 +127,7 @@ static void far() {
         const auto begin = std::chrono::steady_clock::now();
         const int status = okt_norm_rotary_forward(&op, at(1), nullptr, at(2), nullptr, nullptr);
         const double seconds = std::chrono::duration<double>(std::chrono::steady_clock::now() - begin).count();
-        judge(status, x.accepted < 0 ? status == OKT_OK : x.accepted, "far", {x.batch, x.length, x.heads, 8, {x.s[0], x.s[1], x.s[2]}}, 0);
+        expect(status, x.accepted < 0 ? status == OKT_OK : x.accepted, "far", {x.batch, x.length, x.heads, 8, {x.s[0], x.s[1], x.s[2]}}, 0);
         if (seconds > 0.05 && ++bad) std::printf("far: %u x %u x %u took %.2f s\n", x.batch, x.length, x.heads, seconds);
     }
 }

@@ -1,4 +1,4 @@
-"""Which places the rotation may write, on the CPU: every call is judged by a host program that lists the elements one by one, with
+"""Which places the rotation may write, on the CPU: every call is looked at by a host program that lists the elements one by one, with
 the launches taken by a stand-in for the runtime."""
 import os
 import shutil
